@@ -421,6 +421,83 @@ int ppo_lmhead_bwd(const void *H, const void *W, int64_t M, int64_t K, int64_t V
                    void *dlogits, void *dH, void *dW, void *workspace, void *stream);
 
 /*
+ * Log-probs of given tokens with entropy, log-sum-exp and the k most likely alternatives, in one pass
+ * (step 1 for callers that report or distil more than the sampled token).  With z = logits[r, :] / temperature:
+ *     logprob[r, i] = z[tokens[r, i]] - lse,   entropy, lse as in ppo_logprob_entropy,
+ *     top_ids[r, 0..k) = the k largest logits, descending, ties by the lowest index,
+ *     top_logprob[r, i] = z[top_ids[r, i]] - lse
+ *   logits [rows, V] dtype, row pitch row_stride >= V elements; any element-aligned address and any V
+ *   tokens [rows, n] i32 with logprob [rows, n] f32 (n = 0: both unused), 0 <= n <= PPO_TOPK_MAX
+ *   mask   nullable [rows] u8: rows with 0 are not read; their ids are -1, their other outputs 0
+ *   top_ids [rows, k] i32 with top_logprob [rows, k] f32 (k = 0: both unused), 0 <= k <= min(PPO_TOPK_MAX, V)
+ *   entropy, lse  nullable [rows] f32;  workspace nullable (status word)
+ * Logits of -inf or below -1e30 have probability 0; they still appear among the alternatives, in the order of their
+ * values, when fewer than k others are left.  A row with a NaN, a +inf or no logit above -1e30 has NaN outputs and
+ * ids -1 and sets PPO_DEV_BAD_ROW; a token outside [0, V) gives a NaN log-prob and sets PPO_DEV_BAD_TOKEN.
+ * Errors: PPO_ERR_DTYPE, PPO_ERR_SHAPE, PPO_ERR_PARAM (temperature), PPO_ERR_NULL, PPO_ERR_ALIGN.  rows == 0 is a
+ * successful no-op.  Rows whose k-th largest values are many equal ones (constant rows, fewer than k logits left
+ * unbanned) take a slower exact selection.
+ */
+#define PPO_TOPK_MAX 128
+int ppo_logprob_topk(const void *logits, int dtype, int64_t rows, int64_t V, int64_t row_stride,
+                     const int32_t *tokens, int32_t n, const uint8_t *mask, float temperature, int32_t k,
+                     float *logprob, float *entropy, float *lse, int32_t *top_ids, float *top_logprob,
+                     void *workspace, void *stream);
+
+/*
+ * Gradient of everything ppo_logprob_topk returns, back to the logits.  With p = softmax(z) from the given lse:
+ *     dlogits[r, j] = ( sum of the gradients given for token j
+ *                       + p_j * (dlse[r] - G - dentropy[r] * (ln p_j + entropy[r])) ) / temperature,
+ *     G = sum_i dlogprob[r, i] + sum_i dtop_logprob[r, i]
+ *   tokens [rows, n] with dlogprob [rows, n];  top_ids [rows, k] with dtop_logprob [rows, k]  (n or k = 0: unused);
+ *       0 <= n, k <= PPO_TOPK_MAX (k is not limited by V here).  An index may occur several times in one row, in either
+ *       list: its gradients add up.  The alternatives may be another model's
+ *   lse [rows] f32, and entropy [rows] f32 where dentropy is given: the forward call's, for the same logits
+ *   dentropy, dlse  nullable [rows] f32;  mask nullable [rows] u8: rows with 0 are zero-filled, never read
+ *   dlogits [rows, V] dtype, row pitch dlogits_stride >= V, != logits; elements behind a row's V are left alone
+ *   workspace nullable (status word).  A token outside [0, V) makes its row NaN and sets PPO_DEV_BAD_TOKEN.
+ * Sums are fp32 in a fixed order, each element is rounded once: results are bit-reproducible.
+ */
+int ppo_logprob_topk_bwd(const void *logits, int dtype, int64_t rows, int64_t V, int64_t row_stride,
+                         const int32_t *tokens, int32_t n, const float *dlogprob, const int32_t *top_ids, int32_t k,
+                         const float *dtop_logprob, const float *lse, const float *entropy, const float *dentropy,
+                         const float *dlse, const uint8_t *mask, float temperature, void *dlogits,
+                         int64_t dlogits_stride, void *workspace, void *stream);
+
+/*
+ * Operands of ppo_fp8_matmul: e4m3 values (1 byte: 4 exponent bits, 3 mantissa bits, largest 448) with one fp32 scale
+ * per block of 1 x 128 or 128 x 128 elements.  y [R, C] = x (transpose 0) or x^T (transpose 1: x is [C, R]):
+ *     a = max(max |y| over the block, 2^-100),  scale = a / 448,  q = e4m3(y * (448 / a)), ties to even
+ *   x       dtype, row pitch x_stride elements (>= C, or >= R when transposed)
+ *   q       [R, C] e4m3, row pitch q_stride bytes: a multiple of 16, >= C; 16-byte aligned; bytes behind a row's C
+ *           are left alone
+ *   scales  block_rows 1: [ceil(C/128), R];  block_rows 128: [ceil(R/128), ceil(C/128)]
+ * The last block of a row or column may be shorter.  A block with a NaN or an infinity gets scale NaN and NaN values.
+ * Errors: PPO_ERR_DTYPE, PPO_ERR_SHAPE (sizes, pitches), PPO_ERR_PARAM (block_rows not 1 or 128), PPO_ERR_NULL,
+ * PPO_ERR_ALIGN.  R == 0 is a successful no-op.
+ */
+int ppo_fp8_quantize(const void *x, int dtype, int64_t R, int64_t C, int64_t x_stride, int transpose, int block_rows,
+                     void *q, int64_t q_stride, float *scales, void *stream);
+
+/*
+ * Product of two such matrices, e.g. the LM head on 8-bit weights (A = hidden states, B = W^T) or its gradient on the
+ * hidden states (A = dlogits, B = W):
+ *     C[m, n] = sum_b a_scales[b, m] * sb[b, n] * sum_{k in block b} A[m, k] * B[n, k],   blocks of 128 along K
+ *   A [M, K] e4m3, row pitch lda bytes;  a_scales [ceil(K/128), M] f32          (ppo_fp8_quantize, block_rows 1)
+ *   B [N, K] e4m3, row pitch ldb bytes;  block_n 128: b_scales [ceil(N/128), ceil(K/128)] f32, sb[b, n] =
+ *                                        b_scales[n / 128, b];  block_n 1: b_scales [ceil(K/128), N] f32
+ *   C [M, N] out_dtype (PPO_F32 or PPO_BF16), row pitch ldc elements; elements behind a row's N are left alone
+ * Pitches lda and ldb are multiples of 16, A and B 16-byte aligned; M, N, K are any sizes (M == 0: successful no-op).
+ * Sums are fp32: within a block on the tensor cores, over blocks in registers; each element is rounded once, and the
+ * order is fixed by the sizes.  Bytes of A and B behind K in a row are not used, whatever they hold.
+ *   workspace  nullable: the status word (PPO_DEV_TIMEOUT when a bounded wait ran out; C is invalid then)
+ * Errors: PPO_ERR_DTYPE, PPO_ERR_SHAPE, PPO_ERR_PARAM (block_n not 1 or 128), PPO_ERR_NULL, PPO_ERR_ALIGN.
+ */
+int ppo_fp8_matmul(const void *A, int64_t lda, const float *a_scales, const void *B, int64_t ldb,
+                   const float *b_scales, int block_n, int64_t M, int64_t N, int64_t K, void *C, int out_dtype,
+                   int64_t ldc, void *workspace, void *stream);
+
+/*
  * The whole path in one call.  ppo_step_io names every buffer of one PPO iteration over a batch of
  * B responses x T tokens; all pointers of one struct live in the same memory space.
  *   inputs   policy_logits, ref_logits [B,T,V] (dtype); loss_logits [B,T,V] or NULL (= policy_logits);

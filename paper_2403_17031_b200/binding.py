@@ -123,6 +123,15 @@ _SIGS = {
     "ppo_pairwise_loss": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p,
                                     C.c_void_p]),
     "ppo_dpo_loss": (C.c_int, [C.c_void_p] * 6 + [C.c_int64, C.c_int32, C.c_float] + [C.c_void_p] * 6),
+    "ppo_logprob_topk": (C.c_int, [C.c_void_p, C.c_int, C.c_int64, C.c_int64, C.c_int64, C.c_void_p, C.c_int32, C.c_void_p,
+                                   C.c_float, C.c_int32] + [C.c_void_p] * 7),
+    "ppo_logprob_topk_bwd": (C.c_int, [C.c_void_p, C.c_int, C.c_int64, C.c_int64, C.c_int64, C.c_void_p, C.c_int32,
+                                       C.c_void_p, C.c_void_p, C.c_int32] + [C.c_void_p] * 6 +
+                             [C.c_float, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p]),
+    "ppo_fp8_quantize": (C.c_int, [C.c_void_p, C.c_int, C.c_int64, C.c_int64, C.c_int64, C.c_int, C.c_int, C.c_void_p,
+                                   C.c_int64, C.c_void_p, C.c_void_p]),
+    "ppo_fp8_matmul": (C.c_int, [C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_int, C.c_int64,
+                                 C.c_int64, C.c_int64, C.c_void_p, C.c_int, C.c_int64, C.c_void_p, C.c_void_p]),
     "ppo_lmhead_logprob_entropy": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int64, C.c_int64, C.c_int64, C.c_void_p,
                                              C.c_void_p, C.c_float, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
                                              C.c_void_p]),
@@ -541,3 +550,163 @@ def logprob_entropy_pair(policy_logits, ref_logits, tokens, temperature: float, 
                                         _ptr(workspace), _stream())
     _check("ppo_logprob_entropy_pair", rc)
     return lp, ent, rlp
+
+
+# ---------------------------------------------------------------- alternatives, 8-bit operands
+TOPK_MAX = 128
+
+
+def _call(name: str, first: torch.Tensor, tensors, *args):
+    """One entry point on the device of `first` and that device's current stream (the last argument). `tensors`: the other
+    tensors of the call; all have to be on that device."""
+    dev = first.device
+    for t in tensors:
+        if t is not None and t.device != dev:
+            raise TypeError("%s: tensors on %s and %s" % (name, dev, t.device))
+    fn = getattr(lib(), name)
+    if dev.index == torch.cuda.current_device():
+        _check(name, fn(*args, _stream()))
+    else:
+        with torch.cuda.device(dev):
+            _check(name, fn(*args, _stream()))
+
+
+def _rows_of(t: torch.Tensor, name: str):
+    """(rows, V, row pitch) of a CUDA tensor [..., V] whose rows are contiguous: contiguous as a whole, or 2-D."""
+    if not t.is_cuda:
+        raise TypeError("%s must be a CUDA tensor" % name)
+    V = t.shape[-1] if t.dim() else 0
+    rows = t.numel() // V if V else 0
+    if t.is_contiguous():
+        return rows, V, V
+    if t.dim() != 2 or (t.stride(1) != 1 and V > 1):
+        raise TypeError("%s rows must be contiguous" % name)
+    return rows, V, max(t.stride(0), V) if rows <= 1 else t.stride(0)
+
+
+def _per_row(t: Optional[torch.Tensor], rows: int, dtype, name: str) -> int:
+    """Entries per row of a contiguous [rows, n] array (0 when absent)."""
+    if t is None:
+        return 0
+    if rows and t.numel() % rows:
+        raise ValueError("%s has %d entries for %d rows" % (name, t.numel(), rows))
+    _ptr(t, dtype, name)
+    return t.numel() // rows if rows else 0
+
+
+def _one_per_row(t: Optional[torch.Tensor], rows: int, dtype, name: str):
+    if t is not None and t.numel() != rows:
+        raise ValueError("%s has %d entries for %d rows" % (name, t.numel(), rows))
+    return _ptr(t, dtype, name)
+
+
+def logprob_topk(logits: torch.Tensor, tokens: Optional[torch.Tensor], k: int, temperature: float,
+                 mask: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, out=None):
+    """Log-probs of given tokens, entropy, log-sum-exp and the k most likely alternatives of logits [..., V].
+    tokens [...] or [..., n] int32, or None. Returns dict(logprob (shape of tokens) | None, entropy, lse [...],
+    top_ids, top_logprob [..., k] | None); `out`: the same dict with the tensors to write to."""
+    rows, V, stride = _rows_of(logits, "logits")
+    lead = logits.shape[:-1]
+    i32, f32 = torch.int32, torch.float32
+    n = _per_row(tokens, rows, i32, "tokens")
+    if out is None:
+        dev = logits.device
+        out = {"logprob": None if tokens is None else torch.empty(tokens.shape, dtype=f32, device=dev),
+               "entropy": torch.empty(lead, dtype=f32, device=dev), "lse": torch.empty(lead, dtype=f32, device=dev),
+               "top_ids": torch.empty((*lead, k), dtype=i32, device=dev) if k > 0 else None,
+               "top_logprob": torch.empty((*lead, k), dtype=f32, device=dev) if k > 0 else None}
+    lp, ent, lse, ids, tlp = (out.get(name) for name in ("logprob", "entropy", "lse", "top_ids", "top_logprob"))
+    # (without rows there is nothing to count)
+    if rows and (n != _per_row(lp, rows, f32, "logprob") or k != _per_row(ids, rows, i32, "top_ids") or
+                 k != _per_row(tlp, rows, f32, "top_logprob")):
+        raise ValueError("logprob needs %d and top_ids / top_logprob need %d entries per row" % (n, k))
+    _call("ppo_logprob_topk", logits, (tokens, mask, lp, ent, lse, ids, tlp, workspace), C.c_void_p(logits.data_ptr()),
+          _logits_dtype(logits), rows, V, stride, _ptr(tokens), n, _one_per_row(mask, rows, torch.uint8, "mask"),
+          float(temperature), int(k), _ptr(lp), _one_per_row(ent, rows, f32, "entropy"), _one_per_row(lse, rows, f32, "lse"),
+          _ptr(ids), _ptr(tlp), _ptr(workspace))
+    return out
+
+
+def logprob_topk_bwd(logits: torch.Tensor, lse: torch.Tensor, temperature: float, tokens=None, dlogprob=None,
+                     top_ids=None, dtop_logprob=None, entropy=None, dentropy=None, dlse=None, mask=None, workspace=None,
+                     dlogits: Optional[torch.Tensor] = None):
+    """Gradients on what logprob_topk returned -> gradient on logits [..., V]. tokens / dlogprob and top_ids /
+    dtop_logprob come in pairs [..., n] and [..., k] (each pair optional; the alternatives may be another model's);
+    lse, and entropy where dentropy is given, are the forward call's. Returns dict(dlogits)."""
+    rows, V, stride = _rows_of(logits, "logits")
+    i32, f32 = torch.int32, torch.float32
+    n, k = _per_row(tokens, rows, i32, "tokens"), _per_row(top_ids, rows, i32, "top_ids")
+    if n != _per_row(dlogprob, rows, f32, "dlogprob") or k != _per_row(dtop_logprob, rows, f32, "dtop_logprob"):
+        raise ValueError("tokens / dlogprob and top_ids / dtop_logprob need the same number of entries")
+    if dlogits is None:
+        dlogits = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+    drows, dV, dstride = _rows_of(dlogits, "dlogits")
+    if (drows, dV) != (rows, V) or dlogits.dtype != logits.dtype:
+        raise TypeError("dlogits must have the shape and dtype of the logits")
+    _call("ppo_logprob_topk_bwd", logits, (tokens, dlogprob, top_ids, dtop_logprob, lse, entropy, dentropy, dlse, mask, dlogits,
+                                           workspace),
+          C.c_void_p(logits.data_ptr()), _logits_dtype(logits), rows, V, stride, _ptr(tokens), n, _ptr(dlogprob),
+          _ptr(top_ids), k, _ptr(dtop_logprob), _one_per_row(lse, rows, f32, "lse"),
+          _one_per_row(entropy, rows, f32, "entropy"), _one_per_row(dentropy, rows, f32, "dentropy"),
+          _one_per_row(dlse, rows, f32, "dlse"), _one_per_row(mask, rows, torch.uint8, "mask"), float(temperature),
+          C.c_void_p(dlogits.data_ptr()), dstride, _ptr(workspace))
+    return {"dlogits": dlogits}
+
+
+def fp8_quantize(x: torch.Tensor, block_rows: int = 1, transpose: bool = False, out=None):
+    """x [R, C] (or [C, R] with transpose) -> (q [R, C] float8_e4m3fn, scales): one scale per row and 128 columns
+    (block_rows 1, scales [ceil(C/128), R]) or per 128 x 128 block (block_rows 128, scales [ceil(R/128), ceil(C/128)]).
+    q has a row pitch of a multiple of 16 bytes. `out`: (q, scales) to write to."""
+    if x.dim() != 2:
+        raise TypeError("x must be a matrix")
+    rows, cols, stride = _rows_of(x, "x")
+    rows = x.shape[0]
+    R, Cc = (cols, rows) if transpose else (rows, cols)
+    kb = -(-Cc // 128)
+    shape = (kb, R) if block_rows == 1 else (-(-R // 128), kb)
+    if out is None:
+        q = torch.empty((R, -(-Cc // 16) * 16), dtype=torch.float8_e4m3fn, device=x.device)[:, :Cc]
+        out = (q, torch.empty(shape, dtype=torch.float32, device=x.device))
+    q, scales = out
+    if tuple(scales.shape) != shape:
+        raise ValueError("scales must have shape %s" % (shape,))
+    qp, ldq = _fp8_operand(q, "q")
+    if tuple(q.shape) != (R, Cc):
+        raise ValueError("q must have shape %s" % ((R, Cc),))
+    _call("ppo_fp8_quantize", x, (q, scales), C.c_void_p(x.data_ptr()), _logits_dtype(x), R, Cc, stride, 1 if transpose else 0,
+          int(block_rows), qp, ldq, _ptr(scales, torch.float32, "scales"))
+    return out
+
+
+def _fp8_operand(t: torch.Tensor, name: str):
+    """(pointer, row pitch in bytes) of an 8-bit matrix with contiguous rows."""
+    if not t.is_cuda or t.dim() != 2 or t.dtype != torch.float8_e4m3fn:
+        raise TypeError("%s must be a CUDA matrix of float8_e4m3fn" % name)
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        raise TypeError("%s rows must be contiguous" % name)
+    # (the stride of a single row is anyone's choice)
+    pitch = -(-t.shape[1] // 16) * 16 if t.shape[0] <= 1 else t.stride(0)
+    return C.c_void_p(t.data_ptr()), pitch
+
+
+def fp8_matmul(a: torch.Tensor, a_scales: torch.Tensor, b: torch.Tensor, b_scales: torch.Tensor, block_n: int = 128,
+               out_dtype: torch.dtype = torch.bfloat16, workspace: Optional[torch.Tensor] = None, out=None):
+    """[M, N] = a [M, K] . b [N, K]^T of two block-scaled 8-bit matrices (fp8_quantize): a_scales [ceil(K/128), M],
+    b_scales [ceil(N/128), ceil(K/128)] (block_n 128) or [ceil(K/128), N] (block_n 1). Result in bf16 or fp32."""
+    ap, lda = _fp8_operand(a, "a")
+    bp, ldb = _fp8_operand(b, "b")
+    (M, K), (N, K2) = a.shape, b.shape
+    if K != K2:
+        raise ValueError("a [M,K] and b [N,K] disagree on K")
+    kb = -(-K // 128)
+    if tuple(a_scales.shape) != (kb, M) or tuple(b_scales.shape) != ((kb, N) if block_n == 1 else (-(-N // 128), kb)):
+        raise ValueError("scales do not fit the operands' blocks")
+    if out is None:
+        out = torch.empty((M, N), dtype=out_dtype, device=a.device)
+    if out.dim() != 2 or tuple(out.shape) != (M, N):
+        raise ValueError("out must have shape %s" % ((M, N),))
+    _, _, ldc = _rows_of(out, "out")
+    _call("ppo_fp8_matmul", a, (a_scales, b, b_scales, out, workspace), ap, lda, _ptr(a_scales, torch.float32, "a_scales"), bp,
+          ldb, _ptr(b_scales, torch.float32, "b_scales"), int(block_n), M, N, K, C.c_void_p(out.data_ptr()),
+          _logits_dtype(out), ldc, _ptr(workspace))
+    return out

@@ -1,0 +1,672 @@
+// Log-probs of given tokens with entropy, log-sum-exp and the k most likely alternatives of every row, in one pass
+// over the logits (ppo_logprob_topk), and the gradient on all of those back to the logits (ppo_logprob_topk_bwd).
+//
+// Forward. The statistics are those of step 1: sums of 2^(y - ref) and 2^(y - ref) (y - ref) with y = logit log2(e) /
+// temperature, relative to the maximum of the row's first pack. Beside them every thread keeps the maximum of the
+// elements it streams (its "segment": packs tid, tid + 256, ...). Selection then works on segments:
+//   the k-th largest of the 256 segment maxima is a threshold t with at least k elements >= t, so nothing below t is
+//   among the k best; only segments whose maximum reaches t hold candidates, and those few (about k of 256) are
+//   re-read from L2. Candidates are ranked by counting against each other on the 64-bit key (value, ~index), which is
+//   unique: ties go to the lowest index and the order in which candidates arrive does not matter.
+// A slice whose candidates overflow the list (rows of equal values, fewer than k unbanned tokens) is selected by
+// radix passes over it instead.
+// Few rows: a cluster of CL blocks shares a row; each selects the k best of its slice, and block 0 merges the sorted
+// lists and the sums through distributed shared memory.
+// Bound: the read of the logits (V * size bytes per row).
+#include <cooperative_groups.h>
+
+#include "ppo_rows.cuh"
+
+namespace ppo {
+namespace topk {
+
+namespace cg = cooperative_groups;
+
+constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kMaxIds = 128;       // largest k and largest number of given tokens
+// longest candidate list: every element of a slice with fewer than k packs (at most 127 packs of 8 and 14 loose
+// elements) fits, so that the radix fallback always has at least k packs
+constexpr int kCap = 1280;
+
+struct Args {
+    const void *logits;
+    int V;
+    int64_t row_stride;
+    const int32_t *tokens;
+    int n;
+    const uint8_t *mask;
+    float c;
+    int k;
+    float *logprob, *entropy, *lse;
+    int32_t *top_ids;
+    float *top_logprob;
+    int *status;
+};
+
+struct Smem {
+    unsigned long long cand[kCap];
+    unsigned long long best[kMaxIds];    // the slice's best, sorted
+    uint32_t seg_key[kThreads];          // segment maxima as ordered keys; the fallback's histogram
+    uint16_t list[kThreads];             // segments that hold candidates
+    float red[96];
+    SoftmaxState st;
+    uint32_t threshold;
+    int n_list, n_cand, n_best, bin, need;
+};
+
+// whole numbers that order like the values (-0 equals +0); 0 is below every value
+__device__ __forceinline__ uint32_t ordered(float x)
+{
+    const uint32_t b = __float_as_uint(x + 0.f);
+    return (b >> 31) ? ~b : (b | 0x80000000u);
+}
+__device__ __forceinline__ float unordered(uint32_t u) { return __uint_as_float((u >> 31) ? (u & 0x7fffffffu) : ~u); }
+__device__ __forceinline__ unsigned long long make_key(uint32_t u, int j)
+{
+    return ((unsigned long long)u << 32) | (uint32_t)~(uint32_t)j;
+}
+
+// One pack into the sums (clamped at kNegBig, so a -inf logit adds exact zeros) and into the segment maximum.
+template <typename T>
+__device__ __forceinline__ void accumulate(const uint4 &v, float c, float nm, FixedAcc &a, float &tmax)
+{
+    float x[Pack<T>::N], xmax;
+    Pack<T>::unpack(v, x, xmax);
+    tmax = fmaxf(tmax, xmax);
+    const float2 cc = make_float2(c, c), nn = make_float2(nm, nm);
+    float2 s = make_float2(a.s0, a.s1), u = make_float2(a.u0, a.u1);
+#pragma unroll
+    for (int q = 0; q < Pack<T>::N; q += 2) {
+        const float2 t = __ffma2_rn(make_float2(x[q], x[q + 1]), cc, nn);
+        const float2 e = make_float2(ex2(t.x), ex2(t.y));
+        s = __fadd2_rn(s, e);
+        u = __ffma2_rn(e, t, u);
+    }
+    a.s0 = s.x; a.s1 = s.y;
+    a.u0 = u.x; a.u1 = u.y;
+}
+
+// What block `rank` of CL handles of a row: elements [e0, e1), of which packs [p0, p1) of the 16-byte aligned body
+// (body element i of the row is head + i) and at most 2 (N - 1) loose elements at the row's ends.
+struct Slice {
+    int head, p0, p1, e0, e1;
+};
+
+template <typename T>
+__device__ __forceinline__ Slice slice_of(const T *src, int V, int rank, int CL)
+{
+    constexpr int N = Pack<T>::N;
+    Slice s;
+    s.head = min(V, (int)(((16u - (reinterpret_cast<uintptr_t>(src) & 15u)) & 15u) / sizeof(T)));
+    const int nvec = (V - s.head) / N;
+    const int per = (nvec + CL - 1) / CL;
+    s.p0 = min(nvec, rank * per);
+    s.p1 = min(nvec, s.p0 + per);
+    s.e0 = rank == 0 ? 0 : s.head + s.p0 * N;
+    s.e1 = rank == CL - 1 ? V : s.head + s.p1 * N;
+    return s;
+}
+
+// element index of the slice's loose element number t, or -1
+template <typename T>
+__device__ __forceinline__ int loose_element(const Slice &s, int t)
+{
+    constexpr int N = Pack<T>::N;
+    const int lead = (s.e0 == 0) ? s.head : 0;
+    if (t < lead) return t;
+    const int j = s.head + s.p1 * N + (t - lead);
+    return j < s.e1 ? j : -1;
+}
+
+// The k best of elements [e0, e1) into sm.cand (unsorted, k of them), for any values: radix passes find the k-th
+// largest value, then all larger ones and the first of the equal ones (in index order) are taken.
+template <typename T>
+__device__ __noinline__ void select_by_radix(const T *src, int e0, int e1, int k, Smem &sm)
+{
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    uint32_t prefix = 0;
+    int need = k;
+    for (int shift = 24; shift >= 0; shift -= 8) {
+        sm.seg_key[tid] = 0;
+        __syncthreads();
+        for (int j0 = e0; j0 < e1; j0 += kThreads) {
+            const int j = j0 + tid;
+            uint32_t u = 0;
+            bool active = j < e1;
+            if (active) {
+                u = ordered(Pack<T>::load1(src + j));
+                active = shift == 24 || (u >> (shift + 8)) == prefix;
+            }
+            const uint32_t votes = __ballot_sync(0xffffffffu, active);
+            if (active) {
+                const uint32_t bin = (u >> shift) & 255u, peers = __match_any_sync(votes, bin);
+                if (lane == __ffs(peers) - 1) atomicAdd(&sm.seg_key[bin], (uint32_t)__popc(peers));
+            }
+        }
+        __syncthreads();
+        if (tid == 0) {
+            int bin = 255, left = need;
+            for (; bin > 0 && (int)sm.seg_key[bin] < left; --bin) left -= (int)sm.seg_key[bin];
+            sm.bin = bin;
+            sm.need = left;
+        }
+        __syncthreads();
+        prefix = (prefix << 8) | (uint32_t)sm.bin;
+        need = sm.need;
+        __syncthreads();
+    }
+    const int greater = k - need;                        // strictly above the k-th value
+    if (tid == 0) sm.n_cand = 0;
+    __syncthreads();
+    int taken = 0;
+    for (int j0 = e0; j0 < e1; j0 += kThreads) {
+        const int j = j0 + tid;
+        const uint32_t u = j < e1 ? ordered(Pack<T>::load1(src + j)) : 0;
+        if (u > prefix) sm.cand[atomicAdd(&sm.n_cand, 1)] = make_key(u, j);
+        if (taken < need) {                              // the same in every thread
+            const bool tie = j < e1 && u == prefix;
+            const uint32_t votes = __ballot_sync(0xffffffffu, tie);
+            if (lane == 0) sm.seg_key[warp] = (uint32_t)__popc(votes);
+            __syncthreads();
+            int before = taken, total = 0;
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) {
+                if (w < warp) before += (int)sm.seg_key[w];
+                total += (int)sm.seg_key[w];
+            }
+            before += __popc(votes & ((1u << lane) - 1u));
+            if (tie && before < need) sm.cand[greater + before] = make_key(u, j);
+            taken += total;
+            __syncthreads();
+        }
+    }
+    __syncthreads();
+    if (tid == 0) sm.n_cand = k;
+    __syncthreads();
+}
+
+// The slice's best min(k, length) elements into sm.best, sorted; tmax = this thread's segment maximum.
+template <typename T>
+__device__ __forceinline__ void select_best(const T *src, const Slice &sl, int k, float tmax, Smem &sm)
+{
+    constexpr int N = Pack<T>::N;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int len = sl.e1 - sl.e0;
+    const int want = min(k, len);
+    const uint32_t mine = sl.p0 + tid < sl.p1 ? ordered(tmax) : 0u;
+    sm.seg_key[tid] = mine;
+    if (tid == 0) { sm.n_list = 0; sm.n_cand = 0; }
+    __syncthreads();
+    if (warp == 0) {
+        // bisection for a threshold that at least k and at most a few more maxima reach
+        uint32_t key[kThreads / 32], top = 0, low = 0xffffffffu;
+#pragma unroll
+        for (int q = 0; q < kThreads / 32; ++q) {
+            key[q] = sm.seg_key[q * 32 + lane];
+            top = max(top, key[q]);
+            low = min(low, key[q]);
+        }
+        uint32_t lo = __reduce_min_sync(0xffffffffu, low), hi = __reduce_max_sync(0xffffffffu, top);
+        // invariant: count(>= lo) >= k (256 >= k); count(>= hi + 1) = 0
+        while (lo < hi) {
+            const uint32_t mid = lo + (hi - lo + 1) / 2;
+            int cnt = 0;
+#pragma unroll
+            for (int q = 0; q < kThreads / 32; ++q) cnt += key[q] >= mid;
+            cnt = (int)__reduce_add_sync(0xffffffffu, (unsigned)cnt);
+            if (cnt >= k) {
+                lo = mid;
+                if (cnt <= k + (k >> 3) + 1) break;
+            } else {
+                hi = mid - 1;
+            }
+        }
+        // maxima are clamped at kNegBig: at that level everything is a candidate
+        if (lane == 0) sm.threshold = lo <= ordered(0.99f * kNegBig) ? 0u : lo;
+    }
+    __syncthreads();
+    const uint32_t thr = sm.threshold;
+    if (mine != 0 && mine >= thr) sm.list[atomicAdd(&sm.n_list, 1)] = (uint16_t)tid;
+    const int loose = tid < 2 * (N - 1) ? loose_element<T>(sl, tid) : -1;
+    if (loose >= 0) {
+        const int at = atomicAdd(&sm.n_cand, 1);
+        sm.cand[at] = make_key(ordered(Pack<T>::load1(src + loose)), loose);
+    }
+    __syncthreads();
+    const uint4 *body = reinterpret_cast<const uint4 *>(src + sl.head);
+    const int n_list = sm.n_list;
+    for (int q = warp; q < n_list; q += kWarps) {
+        for (int i = sl.p0 + sm.list[q] + lane * kThreads; i < sl.p1; i += 32 * kThreads) {
+            float x[N];
+            Pack<T>::unpack_raw(body[i], x);
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                const uint32_t u = ordered(x[e]);
+                if (u >= thr) {
+                    const int at = atomicAdd(&sm.n_cand, 1);
+                    if (at < kCap) sm.cand[at] = make_key(u, sl.head + i * N + e);
+                }
+            }
+        }
+    }
+    __syncthreads();
+    if (sm.n_cand > kCap) {
+        __syncthreads();
+        select_by_radix(src, sl.e0, sl.e1, want, sm);
+    }
+    const int n = sm.n_cand;
+    for (int i = tid; i < n; i += kThreads) {
+        const unsigned long long key = sm.cand[i];
+        int rank = 0;
+        for (int j = 0; j < n; ++j) rank += sm.cand[j] > key;
+        if (rank < want) sm.best[rank] = key;
+    }
+    if (tid == 0) sm.n_best = want;
+    __syncthreads();
+}
+
+template <typename T, int CL>
+__global__ void __launch_bounds__(kThreads)
+topk_kernel(const Args a)
+{
+    __shared__ Smem sm;
+    const int tid = threadIdx.x;
+    const int64_t row = blockIdx.x / CL;
+    const int rank = blockIdx.x % CL;
+    if (a.mask && !a.mask[row]) {
+        if (rank == 0) {
+            if (tid < a.n) a.logprob[row * a.n + tid] = 0.f;
+            if (tid < a.k) {
+                a.top_ids[row * a.k + tid] = -1;
+                a.top_logprob[row * a.k + tid] = 0.f;
+            }
+            if (tid == 0) {
+                if (a.entropy) a.entropy[row] = 0.f;
+                if (a.lse) a.lse[row] = 0.f;
+            }
+        }
+        return;
+    }
+    const T *src = reinterpret_cast<const T *>(a.logits) + row * a.row_stride;
+    const Slice sl = slice_of(src, a.V, rank, CL);
+    const uint4 *body = reinterpret_cast<const uint4 *>(src + sl.head);
+    float x_tok = 0.f;
+    bool tok_ok = true;
+    if (rank == 0 && tid < a.n) {
+        const int tok = a.tokens[row * a.n + tid];
+        tok_ok = (unsigned)tok < (unsigned)a.V;
+        if (tok_ok) x_tok = Pack<T>::load1(src + tok);
+    }
+    float m_common = 0.f;                               // the same in every block of the row
+    if (a.V - sl.head >= Pack<T>::N) {
+        float x[Pack<T>::N], xmax;
+        Pack<T>::unpack(body[0], x, xmax);
+        m_common = safe_reference(xmax, a.c);
+    }
+    const float nm = -m_common;
+    FixedAcc acc;
+    acc.init();
+    float tmax = kNegBig;
+    {
+        constexpr int U = 4;
+        int i = sl.p0 + tid;
+        for (; i + (U - 1) * kThreads < sl.p1; i += U * kThreads) {
+            uint4 v[U];
+#pragma unroll
+            for (int q = 0; q < U; ++q) v[q] = ld_stream(body + i + q * kThreads);
+#pragma unroll
+            for (int q = 0; q < U; ++q) accumulate<T>(v[q], a.c, nm, acc, tmax);
+        }
+        uint4 v[U - 1];
+#pragma unroll
+        for (int q = 0; q < U - 1; ++q)
+            if (i + q * kThreads < sl.p1) v[q] = ld_stream(body + i + q * kThreads);
+#pragma unroll
+        for (int q = 0; q < U - 1; ++q)
+            if (i + q * kThreads < sl.p1) accumulate<T>(v[q], a.c, nm, acc, tmax);
+    }
+    const int loose = tid < 2 * (Pack<T>::N - 1) ? loose_element<T>(sl, tid) : -1;
+    const float x_loose = loose >= 0 ? Pack<float>::clampf(Pack<T>::load1(src + loose)) : kNegBig;
+    SoftmaxState st;
+    st.m = m_common;
+    st.s = acc.s0 + acc.s1;
+    st.u = acc.u0 + acc.u1;
+    if (loose >= 0) st.add(fmaf(x_loose, a.c, nm));
+    if (!(st.s < 1.0e37f) || !(fabsf(st.u) < 1.0e37f)) {   // overflow (or NaN / +inf): again with a moving reference
+        st.init();
+        for (int i = sl.p0 + tid; i < sl.p1; i += kThreads) accumulate_online<T>(body[i], a.c, st);
+        if (loose >= 0) {
+            const float y = x_loose * a.c;
+            if (y > st.m) st.rebase(y);
+            st.add(fmaf(x_loose, a.c, -st.m));
+        }
+    }
+    st = block_merge_common<kThreads>(st, m_common, sm.red);
+    if (tid == 0) sm.st = st;
+    __syncthreads();
+    st = sm.st;
+    const bool finite = st.s < 1.0e37f;                   // false for NaN; a slice without weight (s = 0) is selected from
+    if (a.k > 0) {
+        if (finite) {
+            select_best(src, sl, a.k, tmax, sm);
+        } else if (tid == 0) {
+            sm.n_best = 0;
+        }
+        __syncthreads();
+    }
+    if (CL > 1) {
+        cg::cluster_group cluster = cg::this_cluster();
+        cluster.sync();
+        if (rank == 0) {
+            for (int r = 1; r < CL; ++r) st = merge(st, *cluster.map_shared_rank(&sm.st, r));
+            // lists into this block's candidates, k slots each, then ranks by counting with bisection
+            int lens[CL];
+            for (int r = 0; r < CL; ++r) lens[r] = a.k > 0 ? *cluster.map_shared_rank(&sm.n_best, r) : 0;
+            for (int i = tid; i < CL * a.k; i += kThreads) {
+                const int r = i / a.k, q = i - r * a.k;
+                sm.cand[i] = q < lens[r] ? cluster.map_shared_rank(&sm.best[0], r)[q] : 0ull;
+            }
+            __syncthreads();
+            for (int i = tid; i < CL * a.k; i += kThreads) {
+                const unsigned long long key = sm.cand[i];
+                if (key == 0ull) continue;
+                int pos = 0;
+                for (int r = 0; r < CL; ++r) {             // entries of list r above key (lists descend, keys differ)
+                    int lo = 0, hi = a.k;
+                    while (lo < hi) {
+                        const int mid = (lo + hi) / 2;
+                        if (sm.cand[r * a.k + mid] > key) lo = mid + 1; else hi = mid;
+                    }
+                    pos += lo;
+                }
+                if (pos < a.k) sm.best[pos] = key;
+            }
+        }
+        cluster.sync();
+        if (rank != 0) return;
+    }
+    const bool good = st.s > 0.f && st.s < 1.0e37f && st.m < 3.0e38f;
+    const float nan = __uint_as_float(0x7fffffffu);
+    const float l2s = log2f(st.s);
+    // In base-2 units the log-sum-exp is m + log2 s with m possibly in the thousands. Log-probs subtract it in fp64
+    // (a few values per row), so they are as accurate as their own size; lse itself is rounded once.
+    const double ln2 = 0.69314718055994530942, lse2 = (double)st.m + (double)l2s, c = (double)a.c;
+    const float lse = good ? (float)(lse2 * ln2) : nan;
+    if (tid < a.n) {
+        a.logprob[row * a.n + tid] = good && tok_ok ? (float)(((double)x_tok * c - lse2) * ln2) : nan;
+        if (!tok_ok && a.status) atomicOr(a.status, PPO_DEV_BAD_TOKEN);
+    }
+    if (tid < a.k) {
+        const unsigned long long key = sm.best[tid];
+        a.top_ids[row * a.k + tid] = good ? (int)~(uint32_t)key : -1;
+        a.top_logprob[row * a.k + tid] = good ? (float)(((double)unordered((uint32_t)(key >> 32)) * c - lse2) * ln2) : nan;
+    }
+    if (tid == 0) {
+        if (a.entropy) a.entropy[row] = good ? kLn2 * (l2s - st.u / st.s) : nan;
+        if (a.lse) a.lse[row] = lse;
+        if (!good && a.status) atomicOr(a.status, PPO_DEV_BAD_ROW);
+    }
+}
+
+template <typename T, int CL>
+static int launch(const Args &a, int64_t rows, cudaStream_t s)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(rows * CL));
+    cfg.blockDim = dim3(kThreads);
+    cfg.stream = s;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = CL;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = CL > 1 ? 1 : 0;
+    PPO_RETURN_IF_CUDA(cudaLaunchKernelEx(&cfg, topk_kernel<T, CL>, a));
+    return PPO_OK;
+}
+
+template <typename T>
+static int launch_any(const Args &a, int64_t rows, cudaStream_t s)
+{
+    // few rows: split each over a cluster while there are SMs to fill and every thread still streams a pack or more
+    const int64_t packs = a.V / Pack<T>::N;
+    if (rows * 8 <= 2 * 148 && packs >= 8 * kThreads) return launch<T, 8>(a, rows, s);
+    if (rows * 4 <= 2 * 148 && packs >= 4 * kThreads) return launch<T, 4>(a, rows, s);
+    if (rows * 2 <= 2 * 148 && packs >= 2 * kThreads) return launch<T, 2>(a, rows, s);
+    return launch<T, 1>(a, rows, s);
+}
+
+// ---------------------------------------------------------------- backward
+// With p_j = exp(z_j - lse), G the sum of all given gradients and h the gradient on the entropy H:
+//     dlogits_j = ( p_j (dlse - G - h (ln p_j + H)) + sum of the gradients given for token j ) / temperature
+// One read and one write of the row; the statistics come from the forward call. A block handles a chunk of a row: it
+// writes the dense part, then the elements that are given tokens once more with their gradients added (all in fp32,
+// rounded once; a token given several times is summed in the order given, by the first of its places).
+// Bound: bytes (read + write of the logits' size).
+struct BwdArgs {
+    const void *logits;
+    void *dlogits;
+    int V, chunks, packs_per_chunk;
+    int64_t ls, ds;
+    const int32_t *tokens, *top_ids;
+    const float *dlogprob, *dtop;
+    int n, k;
+    const float *lse, *entropy, *dentropy, *dlse;
+    const uint8_t *mask;
+    float c_hi, c_lo, inv_tau;      // log2(e) / temperature as a sum of two floats
+    int *status;
+};
+
+struct RowTerm {
+    float c_hi, c_lo, o_hi, o_lo, a0, a1;
+    // log2 p, accurate to a few ulps of itself however large z and lse are
+    __device__ __forceinline__ float log2p(float x) const
+    {
+        const float t = fmaf(x, c_hi, -o_hi);
+        return t < -200.f ? -200.f : t + fmaf(x, c_lo, -o_lo);   // p is 0 there, -inf included (a NaN stays one)
+    }
+    __device__ __forceinline__ float grad(float x) const
+    {
+        const float t = log2p(x);
+        return ex2(t) * fmaf(a1, t, a0);
+    }
+};
+
+template <typename T>
+__global__ void __launch_bounds__(kThreads)
+topk_bwd_kernel(const BwdArgs a)
+{
+    constexpr int N = Pack<T>::N, U = 4;
+    __shared__ float red[kWarps];
+    __shared__ int ids[2 * kMaxIds];
+    __shared__ float gs[2 * kMaxIds];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int64_t row = blockIdx.x / a.chunks;
+    const int chunk = blockIdx.x % a.chunks;
+    const T *src = reinterpret_cast<const T *>(a.logits) + row * a.ls;
+    T *dst = reinterpret_cast<T *>(a.dlogits) + row * a.ds;
+    // packs are aligned in dlogits; where the logits sit at another offset they are read element by element
+    const int head = min(a.V, (int)(((16u - (reinterpret_cast<uintptr_t>(dst) & 15u)) & 15u) / sizeof(T)));
+    const int nvec = (a.V - head) / N;
+    const int p0 = chunk * a.packs_per_chunk, p1 = min(nvec, p0 + a.packs_per_chunk);
+    const bool first = chunk == 0, last = chunk == a.chunks - 1;
+    const int e0 = first ? 0 : head + p0 * N, e1 = last ? a.V : head + p1 * N;
+    uint4 *out = reinterpret_cast<uint4 *>(dst + head);
+    // loose elements: before the first pack of the row and behind its last
+    int loose = -1;
+    if (first && tid < head) loose = tid;
+    if (last && tid >= 32 && tid - 32 < a.V - head - nvec * N) loose = head + nvec * N + (tid - 32);
+    if (a.mask && !a.mask[row]) {
+        const uint4 z = make_uint4(0u, 0u, 0u, 0u);
+        for (int i = p0 + tid; i < p1; i += kThreads) st_stream(out + i, z);
+        if (loose >= 0) Pack<T>::store1(dst + loose, 0.f);
+        return;
+    }
+    const bool vec_in = ((reinterpret_cast<uintptr_t>(src + head) & 15u) == 0);
+    const uint4 *in = reinterpret_cast<const uint4 *>(src + head);
+    uint4 v[U];
+    const int i0 = p0 + tid;
+    if (vec_in) {
+#pragma unroll
+        for (int q = 0; q < U; ++q)
+            if (i0 + q * kThreads < p1) v[q] = ld_stream(in + i0 + q * kThreads);
+    }
+    // the given tokens and the sum of their gradients
+    const int total = a.n + a.k;
+    int id = 0;
+    float g = 0.f;
+    if (tid < total) {
+        const bool top = tid >= a.n;
+        const int64_t at = top ? row * a.k + (tid - a.n) : row * a.n + tid;
+        id = top ? a.top_ids[at] : a.tokens[at];
+        g = top ? a.dtop[at] : a.dlogprob[at];
+        ids[tid] = id;
+        gs[tid] = g;
+    }
+    const float wsum = warp_sum_f(g);
+    if (lane == 0) red[warp] = wsum;
+    const int bad = __syncthreads_or((unsigned)id >= (unsigned)a.V);
+    float G = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) G += red[w];
+    RowTerm r;
+    {
+        const float lse = a.lse[row], h = a.dentropy ? a.dentropy[row] : 0.f, H = a.dentropy ? a.entropy[row] : 0.f;
+        const double off = (double)lse * 1.4426950408889634074;
+        r.c_hi = a.c_hi;
+        r.c_lo = a.c_lo;
+        r.o_hi = (float)off;
+        r.o_lo = (float)(off - (double)r.o_hi);
+        r.a0 = ((a.dlse ? a.dlse[row] : 0.f) - G - h * H) * a.inv_tau;
+        r.a1 = -h * kLn2 * a.inv_tau;
+        if (bad) r.a0 = __uint_as_float(0x7fffffffu);
+    }
+    if (bad && chunk == 0 && tid == 0 && a.status) atomicOr(a.status, PPO_DEV_BAD_TOKEN);
+    for (int i = i0; i < p1; i += U * kThreads) {
+        if (vec_in && i != i0) {
+#pragma unroll
+            for (int q = 0; q < U; ++q)
+                if (i + q * kThreads < p1) v[q] = ld_stream(in + i + q * kThreads);
+        }
+#pragma unroll
+        for (int q = 0; q < U; ++q) {
+            const int p = i + q * kThreads;
+            if (p >= p1) continue;
+            float x[N];
+            if (vec_in) {
+                Pack<T>::unpack_raw(v[q], x);
+            } else {
+#pragma unroll
+                for (int e = 0; e < N; ++e) x[e] = Pack<T>::load1(src + head + p * N + e);
+            }
+#pragma unroll
+            for (int e = 0; e < N; ++e) x[e] = r.grad(x[e]);
+            st_stream(out + p, Pack<T>::pack(x));
+        }
+    }
+    if (loose >= 0) Pack<T>::store1(dst + loose, r.grad(Pack<T>::load1(src + loose)));
+    __syncthreads();
+    if (tid < total && !bad && id >= e0 && id < e1) {
+        float sum = 0.f;
+        bool owner = true;
+        for (int j = 0; j < total; ++j)
+            if (ids[j] == id) {
+                owner = owner && j >= tid;
+                sum += gs[j];
+            }
+        if (owner) Pack<T>::store1(dst + id, fmaf(sum, a.inv_tau, r.grad(Pack<T>::load1(src + id))));
+    }
+}
+
+template <typename T>
+static int launch_bwd(BwdArgs a, int64_t rows, cudaStream_t s)
+{
+    const int nvec = a.V / Pack<T>::N;
+    a.packs_per_chunk = 4 * kThreads;
+    a.chunks = nvec > 0 ? (nvec + a.packs_per_chunk - 1) / a.packs_per_chunk : 1;
+    const int64_t blocks = rows * a.chunks;
+    if (blocks >= ((int64_t)1 << 31)) return PPO_ERR_SHAPE;
+    topk_bwd_kernel<T><<<(unsigned)blocks, kThreads, 0, s>>>(a);
+    return launch_status();
+}
+
+}   // namespace topk
+}   // namespace ppo
+
+using namespace ppo;
+
+extern "C" int ppo_logprob_topk(const void *logits, int dtype, int64_t rows, int64_t V, int64_t row_stride,
+                                const int32_t *tokens, int32_t n, const uint8_t *mask, float temperature, int32_t k,
+                                float *logprob, float *entropy, float *lse, int32_t *top_ids, float *top_logprob,
+                                void *workspace, void *stream)
+{
+    if (dtype != PPO_F32 && dtype != PPO_BF16) return PPO_ERR_DTYPE;
+    if (rows < 0 || rows >= ((int64_t)1 << 31) || V <= 0 || V >= ((int64_t)1 << 31) - 512 || row_stride < V || n < 0 ||
+        n > topk::kMaxIds || k < 0 || k > topk::kMaxIds || k > V)
+        return PPO_ERR_SHAPE;
+    if (!(temperature > 0.f) || !finite_f(temperature)) return PPO_ERR_PARAM;
+    if (rows == 0) return PPO_OK;
+    if (!logits || (n > 0 && (!tokens || !logprob)) || (k > 0 && (!top_ids || !top_logprob))) return PPO_ERR_NULL;
+    if (reinterpret_cast<uintptr_t>(logits) % (dtype == PPO_F32 ? 4 : 2)) return PPO_ERR_ALIGN;
+    topk::Args a = {};
+    a.logits = logits;
+    a.V = (int)V;
+    a.row_stride = row_stride;
+    a.tokens = tokens;
+    a.n = n;
+    a.mask = mask;
+    a.c = (float)(1.4426950408889634074 / (double)temperature);
+    a.k = k;
+    a.logprob = logprob;
+    a.entropy = entropy;
+    a.lse = lse;
+    a.top_ids = top_ids;
+    a.top_logprob = top_logprob;
+    a.status = workspace ? &ws_header(workspace)->status : nullptr;
+    cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+    return dtype == PPO_F32 ? topk::launch_any<float>(a, rows, s) : topk::launch_any<__nv_bfloat16>(a, rows, s);
+}
+
+extern "C" int ppo_logprob_topk_bwd(const void *logits, int dtype, int64_t rows, int64_t V, int64_t row_stride,
+                                    const int32_t *tokens, int32_t n, const float *dlogprob, const int32_t *top_ids,
+                                    int32_t k, const float *dtop_logprob, const float *lse, const float *entropy,
+                                    const float *dentropy, const float *dlse, const uint8_t *mask, float temperature,
+                                    void *dlogits, int64_t dlogits_stride, void *workspace, void *stream)
+{
+    if (dtype != PPO_F32 && dtype != PPO_BF16) return PPO_ERR_DTYPE;
+    if (rows < 0 || rows >= ((int64_t)1 << 31) || V <= 0 || V >= ((int64_t)1 << 31) - 512 || row_stride < V ||
+        dlogits_stride < V || n < 0 || n > topk::kMaxIds || k < 0 || k > topk::kMaxIds)
+        return PPO_ERR_SHAPE;
+    if (!(temperature > 0.f) || !finite_f(temperature)) return PPO_ERR_PARAM;
+    if (rows == 0) return PPO_OK;
+    if (!logits || !dlogits || !lse || (n > 0 && (!tokens || !dlogprob)) || (k > 0 && (!top_ids || !dtop_logprob)) ||
+        (dentropy && !entropy))
+        return PPO_ERR_NULL;
+    if (logits == dlogits) return PPO_ERR_PARAM;
+    const size_t es = dtype == PPO_F32 ? 4 : 2;
+    if (reinterpret_cast<uintptr_t>(logits) % es || reinterpret_cast<uintptr_t>(dlogits) % es) return PPO_ERR_ALIGN;
+    topk::BwdArgs a = {};
+    a.logits = logits;
+    a.dlogits = dlogits;
+    a.V = (int)V;
+    a.ls = row_stride;
+    a.ds = dlogits_stride;
+    a.tokens = tokens;
+    a.n = n;
+    a.dlogprob = dlogprob;
+    a.top_ids = top_ids;
+    a.k = k;
+    a.dtop = dtop_logprob;
+    a.lse = lse;
+    a.entropy = entropy;
+    a.dentropy = dentropy;
+    a.dlse = dlse;
+    a.mask = mask;
+    const double c = 1.4426950408889634074 / (double)temperature;
+    a.c_hi = (float)c;
+    a.c_lo = (float)(c - (double)a.c_hi);
+    a.inv_tau = 1.0f / temperature;
+    a.status = workspace ? &ws_header(workspace)->status : nullptr;
+    cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+    return dtype == PPO_F32 ? topk::launch_bwd<float>(a, rows, s) : topk::launch_bwd<__nv_bfloat16>(a, rows, s);
+}
