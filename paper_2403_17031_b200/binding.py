@@ -558,17 +558,34 @@ TOPK_MAX = 128
 
 def _call(name: str, first: torch.Tensor, tensors, *args):
     """One entry point on the device of `first` and that device's current stream (the last argument). `tensors`: the other
-    tensors of the call; all have to be on that device."""
-    dev = first.device
+    tensors of the call; all have to be on that device. Small calls are bound by this side of the boundary, so pointers
+    are passed as plain ints and the stream comes straight from the C layer."""
+    at = first.get_device()
     for t in tensors:
-        if t is not None and t.device != dev:
-            raise TypeError("%s: tensors on %s and %s" % (name, dev, t.device))
-    fn = getattr(lib(), name)
-    if dev.index == torch.cuda.current_device():
-        _check(name, fn(*args, _stream()))
+        if t is not None and t.get_device() != at:
+            raise TypeError("%s: tensors on %s and %s" % (name, first.device, t.device))
+    fn = getattr(_lib or lib(), name)
+    stream = torch._C._cuda_getCurrentRawStream(at)
+    if at == torch._C._cuda_getDevice():
+        rc = fn(*args, stream)
     else:
-        with torch.cuda.device(dev):
-            _check(name, fn(*args, _stream()))
+        with torch.cuda.device(at):
+            rc = fn(*args, stream)
+    if rc != 0:
+        raise PPOError(name, rc)
+
+
+def _addr(t: Optional[torch.Tensor], dtype, name: str):
+    """Address of a contiguous CUDA tensor of the given dtype, or None."""
+    if t is None:
+        return None
+    if not t.is_cuda or not t.is_contiguous() or t.dtype != dtype:
+        _ptr(t, dtype, name)                       # says what is wrong
+    return t.data_ptr()
+
+
+def _raw(t: Optional[torch.Tensor]):
+    return None if t is None else t.data_ptr()
 
 
 def _rows_of(t: torch.Tensor, name: str):
@@ -590,14 +607,14 @@ def _per_row(t: Optional[torch.Tensor], rows: int, dtype, name: str) -> int:
         return 0
     if rows and t.numel() % rows:
         raise ValueError("%s has %d entries for %d rows" % (name, t.numel(), rows))
-    _ptr(t, dtype, name)
+    _addr(t, dtype, name)
     return t.numel() // rows if rows else 0
 
 
 def _one_per_row(t: Optional[torch.Tensor], rows: int, dtype, name: str):
     if t is not None and t.numel() != rows:
         raise ValueError("%s has %d entries for %d rows" % (name, t.numel(), rows))
-    return _ptr(t, dtype, name)
+    return _addr(t, dtype, name)
 
 
 def logprob_topk(logits: torch.Tensor, tokens: Optional[torch.Tensor], k: int, temperature: float,
@@ -620,10 +637,10 @@ def logprob_topk(logits: torch.Tensor, tokens: Optional[torch.Tensor], k: int, t
     if rows and (n != _per_row(lp, rows, f32, "logprob") or k != _per_row(ids, rows, i32, "top_ids") or
                  k != _per_row(tlp, rows, f32, "top_logprob")):
         raise ValueError("logprob needs %d and top_ids / top_logprob need %d entries per row" % (n, k))
-    _call("ppo_logprob_topk", logits, (tokens, mask, lp, ent, lse, ids, tlp, workspace), C.c_void_p(logits.data_ptr()),
-          _logits_dtype(logits), rows, V, stride, _ptr(tokens), n, _one_per_row(mask, rows, torch.uint8, "mask"),
-          float(temperature), int(k), _ptr(lp), _one_per_row(ent, rows, f32, "entropy"), _one_per_row(lse, rows, f32, "lse"),
-          _ptr(ids), _ptr(tlp), _ptr(workspace))
+    _call("ppo_logprob_topk", logits, (tokens, mask, lp, ent, lse, ids, tlp, workspace), logits.data_ptr(),
+          _logits_dtype(logits), rows, V, stride, _raw(tokens), n, _one_per_row(mask, rows, torch.uint8, "mask"),
+          float(temperature), int(k), _raw(lp), _one_per_row(ent, rows, f32, "entropy"), _one_per_row(lse, rows, f32, "lse"),
+          _raw(ids), _raw(tlp), _raw(workspace))
     return out
 
 
@@ -645,11 +662,11 @@ def logprob_topk_bwd(logits: torch.Tensor, lse: torch.Tensor, temperature: float
         raise TypeError("dlogits must have the shape and dtype of the logits")
     _call("ppo_logprob_topk_bwd", logits, (tokens, dlogprob, top_ids, dtop_logprob, lse, entropy, dentropy, dlse, mask, dlogits,
                                            workspace),
-          C.c_void_p(logits.data_ptr()), _logits_dtype(logits), rows, V, stride, _ptr(tokens), n, _ptr(dlogprob),
-          _ptr(top_ids), k, _ptr(dtop_logprob), _one_per_row(lse, rows, f32, "lse"),
+          logits.data_ptr(), _logits_dtype(logits), rows, V, stride, _raw(tokens), n, _raw(dlogprob),
+          _raw(top_ids), k, _raw(dtop_logprob), _one_per_row(lse, rows, f32, "lse"),
           _one_per_row(entropy, rows, f32, "entropy"), _one_per_row(dentropy, rows, f32, "dentropy"),
           _one_per_row(dlse, rows, f32, "dlse"), _one_per_row(mask, rows, torch.uint8, "mask"), float(temperature),
-          C.c_void_p(dlogits.data_ptr()), dstride, _ptr(workspace))
+          dlogits.data_ptr(), dstride, _raw(workspace))
     return {"dlogits": dlogits}
 
 
@@ -673,8 +690,8 @@ def fp8_quantize(x: torch.Tensor, block_rows: int = 1, transpose: bool = False, 
     qp, ldq = _fp8_operand(q, "q")
     if tuple(q.shape) != (R, Cc):
         raise ValueError("q must have shape %s" % ((R, Cc),))
-    _call("ppo_fp8_quantize", x, (q, scales), C.c_void_p(x.data_ptr()), _logits_dtype(x), R, Cc, stride, 1 if transpose else 0,
-          int(block_rows), qp, ldq, _ptr(scales, torch.float32, "scales"))
+    _call("ppo_fp8_quantize", x, (q, scales), x.data_ptr(), _logits_dtype(x), R, Cc, stride, 1 if transpose else 0,
+          int(block_rows), qp, ldq, _addr(scales, torch.float32, "scales"))
     return out
 
 
@@ -686,7 +703,7 @@ def _fp8_operand(t: torch.Tensor, name: str):
         raise TypeError("%s rows must be contiguous" % name)
     # (the stride of a single row is anyone's choice)
     pitch = -(-t.shape[1] // 16) * 16 if t.shape[0] <= 1 else t.stride(0)
-    return C.c_void_p(t.data_ptr()), pitch
+    return t.data_ptr(), pitch
 
 
 def fp8_matmul(a: torch.Tensor, a_scales: torch.Tensor, b: torch.Tensor, b_scales: torch.Tensor, block_n: int = 128,
@@ -706,7 +723,7 @@ def fp8_matmul(a: torch.Tensor, a_scales: torch.Tensor, b: torch.Tensor, b_scale
     if out.dim() != 2 or tuple(out.shape) != (M, N):
         raise ValueError("out must have shape %s" % ((M, N),))
     _, _, ldc = _rows_of(out, "out")
-    _call("ppo_fp8_matmul", a, (a_scales, b, b_scales, out, workspace), ap, lda, _ptr(a_scales, torch.float32, "a_scales"), bp,
-          ldb, _ptr(b_scales, torch.float32, "b_scales"), int(block_n), M, N, K, C.c_void_p(out.data_ptr()),
-          _logits_dtype(out), ldc, _ptr(workspace))
+    _call("ppo_fp8_matmul", a, (a_scales, b, b_scales, out, workspace), ap, lda, _addr(a_scales, torch.float32, "a_scales"), bp,
+          ldb, _addr(b_scales, torch.float32, "b_scales"), int(block_n), M, N, K, out.data_ptr(),
+          _logits_dtype(out), ldc, _raw(workspace))
     return out

@@ -243,6 +243,276 @@ static int launch_narrow(Args a, const void *A, int64_t lda, const void *B, int6
     return PPO_OK;
 }
 
+// ---------------------------------------------------------------- wide kernel
+// Rows of A are the 128 lanes of the accumulator tile, 256 rows of B its columns. One persistent block per SM, 320
+// threads: warp 0 = TMA producer (4 stages of 48 KB), warp 1 = MMA issuer (two accumulators of 256 columns, one block
+// of K each), warps 2-9 = epilogue: warp (q, h) owns lanes 32 q .. and columns 128 h .., i.e. thread = one row and one
+// 128-column block of sb, so its factor is a single product sa * sb per block of K and the join is a packed fp32
+// multiply-add per two elements out of tensor memory. Finished tiles go through shared memory so that rows leave in
+// 128-byte runs.
+constexpr int kBM = 128, kBN = 256, kWideStages = 4, kWideThreads = 320;
+constexpr int kWideABytes = kBM * kBlockK, kWideBBytes = kBN * kBlockK, kWideStage = kWideABytes + kWideBBytes;
+constexpr int kStageOut = 32 * 128;        // per epilogue warp: 32 rows x 128 bytes
+constexpr int kWideSmem = kWideStages * kWideStage + 8 * kStageOut + 1024;
+
+struct WideSmem {
+    unsigned long long full[kWideStages], empty[kWideStages], tmem_full[2], tmem_empty[2];
+    uint32_t tmem_base;
+};
+
+struct WideArgs {
+    Args a;
+    int gm, gn, n_units, vec;
+};
+
+// unit -> output tile: blocks of gm x gn tiles (m fastest inside), column of blocks by column of blocks; a block's
+// tiles run at the same time and share their operand panels through L2
+__device__ __forceinline__ int2 tile_of(int u, int m_tiles, int n_tiles, int gm, int gn)
+{
+    const int col = u / (m_tiles * gn), width = min(gn, n_tiles - col * gn), rest = u - col * m_tiles * gn;
+    const int blk = rest / (gm * width), height = min(gm, m_tiles - blk * gm), in = rest - blk * gm * width;
+    return make_int2(blk * gm + in % height, col * gn + in / height);
+}
+
+// the loads of this thread so far have arrived in `r`
+__device__ __forceinline__ void tmem_wait16(uint32_t (&r)[16])
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]),
+                   "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])
+                 :
+                 : "memory");
+}
+
+// 32 rows x 128 bytes of a finished tile from this warp's staging buffer to global memory; elements past N stay unwritten
+template <typename T>
+__device__ __forceinline__ void store_rows(const unsigned char *stage, T *out, int64_t ldc, int m, int M, int n, int N, bool vec)
+{
+    constexpr int E = 16 / sizeof(T), W = 128 / sizeof(T);     // elements per 16 bytes, per row
+    const int lane = threadIdx.x & 31;
+    if (vec && n + W <= N) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int r = i * 4 + (lane >> 3), c = lane & 7;
+            const uint4 v = *reinterpret_cast<const uint4 *>(stage + r * 128 + ((c ^ (r & 7)) << 4));
+            if (m + r < M) *reinterpret_cast<uint4 *>(out + (int64_t)(m + r) * ldc + n + c * E) = v;
+        }
+    } else {
+        for (int r = 0; r < 32 && m + r < M; ++r)
+            for (int e = lane; e < W && n + e < N; e += 32)
+                out[(int64_t)(m + r) * ldc + n + e] =
+                    *reinterpret_cast<const T *>(stage + r * 128 + (((e / E) ^ (r & 7)) << 4) + (e % E) * sizeof(T));
+    }
+}
+
+template <bool PER_ROW>
+__global__ void __launch_bounds__(kWideThreads, 1)
+wide_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const WideArgs w)
+{
+    const Args &a = w.a;
+    extern __shared__ __align__(1024) unsigned char smem_raw[];
+    __shared__ WideSmem sm;
+    unsigned char *ring = smem_raw + ((1024u - (saddr(smem_raw) & 1023u)) & 1023u);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kWideStages; ++s) {
+            barrier_init(&sm.full[s], 1);
+            barrier_init(&sm.empty[s], 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            barrier_init(&sm.tmem_full[b], 1);
+            barrier_init(&sm.tmem_empty[b], 8);
+        }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) tmem_alloc_all(&sm.tmem_base);
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint32_t tmem_base = sm.tmem_base;
+    const int kbs = a.kb_total;
+
+    if (warp == 0) {
+        if (lane == 0) {
+            bool alive = true;
+            uint32_t it = 0;
+            for (int u = blockIdx.x; u < w.n_units && alive; u += gridDim.x) {
+                const int2 t = tile_of(u, a.m_tiles, a.n_tiles, w.gm, w.gn);
+                for (int kb = 0; kb < kbs; ++kb, ++it) {
+                    const int s = it % kWideStages;
+                    if (it >= kWideStages) wait_alive(alive, &sm.empty[s], ((it / kWideStages) - 1) & 1, a.status);
+                    if (!alive) break;
+                    unsigned char *stage = ring + (size_t)s * kWideStage;
+                    barrier_expect_tx(&sm.full[s], (uint32_t)kWideStage);
+                    tma_load_2d(stage, &map_a, kb * kBlockK, t.x * kBM, &sm.full[s]);
+                    tma_load_2d(stage + kWideABytes, &map_b, kb * kBlockK, t.y * kBN, &sm.full[s]);
+                }
+            }
+            // copies in flight land before the block may end
+            for (uint32_t i = it > kWideStages ? it - kWideStages : 0; i < it; ++i)
+                wait(&sm.full[i % kWideStages], (i / kWideStages) & 1, a.status);
+        }
+        __syncwarp();
+    } else if (warp == 1) {
+        if (lane == 0) {
+            constexpr uint32_t idesc = instr_desc_e4m3(kBM, kBN);
+            bool alive = true;
+            uint32_t it = 0;
+            for (int u = blockIdx.x; u < w.n_units; u += gridDim.x) {
+                for (int kb = 0; kb < kbs; ++kb, ++it) {
+                    const int s = it % kWideStages, buf = it & 1;
+                    if (it >= 2) wait_alive(alive, &sm.tmem_empty[buf], ((it >> 1) - 1) & 1, a.status);
+                    wait_alive(alive, &sm.full[s], (it / kWideStages) & 1, a.status);
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    const uint32_t a_addr = saddr(ring + (size_t)s * kWideStage), b_addr = a_addr + kWideABytes;
+#pragma unroll
+                    for (int kk = 0; kk < kBlockK / 32; ++kk)
+                        mma_f8(tmem_base + buf * kBN, smem_desc(a_addr + kk * 32, 16, 1024), smem_desc(b_addr + kk * 32, 16, 1024),
+                               idesc, kk ? 1u : 0u);
+                    commit(&sm.empty[s]);
+                    commit(&sm.tmem_full[buf]);
+                }
+            }
+        }
+        __syncwarp();
+    } else {
+        const int q = warp & 3, h = (warp - 2) >> 2;
+        unsigned char *stage = ring + (size_t)kWideStages * kWideStage + (warp - 2) * kStageOut;
+        float *sbs = reinterpret_cast<float *>(stage);          // PER_ROW: this warp's 128 factors of a block of K
+        const uint32_t taddr = tmem_base + h * 128 + ((uint32_t)(q * 32) << 16);
+        bool alive = true;
+        uint32_t it = 0;
+        for (int u = blockIdx.x; u < w.n_units; u += gridDim.x) {
+            const int2 t = tile_of(u, a.m_tiles, a.n_tiles, w.gm, w.gn);
+            const int m = t.x * kBM + q * 32 + lane, n = t.y * kBN + h * 128;
+            float2 acc[64];
+#pragma unroll
+            for (int j = 0; j < 64; ++j) acc[j] = make_float2(0.f, 0.f);
+            // scales of the next block of K, loaded one block ahead
+            float next_sa, next_sb = 0.f;
+            float4 next_row = make_float4(0.f, 0.f, 0.f, 0.f);
+            auto fetch = [&](int kb) {
+                next_sa = m < a.M ? __ldg(a.sa + (int64_t)kb * a.M + m) : 0.f;
+                if (PER_ROW) {
+                    const float *p = a.sb + (int64_t)kb * a.N + n;
+                    next_row.x = n + lane < a.N ? __ldg(p + lane) : 0.f;
+                    next_row.y = n + lane + 32 < a.N ? __ldg(p + lane + 32) : 0.f;
+                    next_row.z = n + lane + 64 < a.N ? __ldg(p + lane + 64) : 0.f;
+                    next_row.w = n + lane + 96 < a.N ? __ldg(p + lane + 96) : 0.f;
+                } else {
+                    next_sb = n < a.N ? __ldg(a.sb + (int64_t)(n / 128) * kbs + kb) : 0.f;
+                }
+            };
+            fetch(0);
+            for (int kb = 0; kb < kbs; ++kb, ++it) {
+                const uint32_t buf = it & 1;
+                const float f = PER_ROW ? next_sa : next_sa * next_sb;
+                if (PER_ROW) {
+                    __syncwarp();                               // everyone has read the block before
+                    sbs[lane] = next_row.x;
+                    sbs[lane + 32] = next_row.y;
+                    sbs[lane + 64] = next_row.z;
+                    sbs[lane + 96] = next_row.w;
+                }
+                if (kb + 1 < kbs) fetch(kb + 1);
+                wait_alive(alive, &sm.tmem_full[buf], (it >> 1) & 1, a.status);
+                __syncwarp();
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                uint32_t r[2][16];
+                tmem_ld16(taddr + buf * kBN, r[0]);
+#pragma unroll
+                for (int c = 0; c < 8; ++c) {
+                    tmem_wait16(r[c & 1]);
+                    if (c < 7) {
+                        tmem_ld16(taddr + buf * kBN + (c + 1) * 16, r[(c + 1) & 1]);
+                    } else {
+                        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                        __syncwarp();
+                        if (lane == 0) barrier_arrive(&sm.tmem_empty[buf]);
+                    }
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        float2 f0 = make_float2(f, f), f1 = f0;
+                        if (PER_ROW) {
+                            const float4 s4 = reinterpret_cast<const float4 *>(sbs)[c * 4 + j];
+                            f0 = __fmul2_rn(f0, make_float2(s4.x, s4.y));
+                            f1 = __fmul2_rn(f1, make_float2(s4.z, s4.w));
+                        }
+                        const uint32_t *p = r[c & 1] + j * 4;
+                        acc[c * 8 + j * 2] = __ffma2_rn(make_float2(__uint_as_float(p[0]), __uint_as_float(p[1])), f0, acc[c * 8 + j * 2]);
+                        acc[c * 8 + j * 2 + 1] =
+                            __ffma2_rn(make_float2(__uint_as_float(p[2]), __uint_as_float(p[3])), f1, acc[c * 8 + j * 2 + 1]);
+                    }
+                }
+            }
+            // the tile: 64 bf16 or 32 fp32 columns at a time; 16-byte piece c of row r lies at c ^ (r & 7)
+            const int m_warp = t.x * kBM + q * 32;
+            __syncwarp();
+            if (a.out_f32) {
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        *reinterpret_cast<float4 *>(stage + lane * 128 + ((j ^ (lane & 7)) << 4)) =
+                            make_float4(acc[c * 16 + j * 2].x, acc[c * 16 + j * 2].y, acc[c * 16 + j * 2 + 1].x, acc[c * 16 + j * 2 + 1].y);
+                    __syncwarp();
+                    store_rows(stage, reinterpret_cast<float *>(a.out), a.ldc, m_warp, a.M, n + c * 32, a.N, w.vec != 0);
+                    __syncwarp();
+                }
+            } else {
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        uint32_t v[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const __nv_bfloat162 b2 = __float22bfloat162_rn(acc[c * 32 + j * 4 + e]);
+                            v[e] = *reinterpret_cast<const uint32_t *>(&b2);
+                        }
+                        *reinterpret_cast<uint4 *>(stage + lane * 128 + ((j ^ (lane & 7)) << 4)) = make_uint4(v[0], v[1], v[2], v[3]);
+                    }
+                    __syncwarp();
+                    store_rows(stage, reinterpret_cast<__nv_bfloat16 *>(a.out), a.ldc, m_warp, a.M, n + c * 64, a.N, w.vec != 0);
+                    __syncwarp();
+                }
+            }
+        }
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    if (warp == 1) {
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        tmem_free_all(tmem_base);
+    }
+}
+
+static int launch_wide(Args a, const void *A, int64_t lda, const void *B, int64_t ldb, int64_t K, cudaStream_t s)
+{
+    CUtensorMap ma, mb;
+    int rc = make_map_8bit(&ma, A, (uint64_t)K, (uint64_t)a.M, (uint64_t)lda, kBM);
+    if (rc) return rc;
+    rc = make_map_8bit(&mb, B, (uint64_t)K, (uint64_t)a.N, (uint64_t)ldb, kBN);
+    if (rc) return rc;
+    a.m_tiles = (a.M + kBM - 1) / kBM;
+    a.n_tiles = (a.N + kBN - 1) / kBN;
+    const int64_t units = (int64_t)a.m_tiles * a.n_tiles;
+    if (units >= ((int64_t)1 << 30)) return PPO_ERR_SHAPE;
+    WideArgs w = {};
+    w.a = a;
+    w.gm = 37;
+    w.gn = 4;
+    w.n_units = (int)units;
+    w.vec = reinterpret_cast<uintptr_t>(a.out) % 16 == 0 && (a.ldc * (a.out_f32 ? 4 : 2)) % 16 == 0;
+    int dev = 0, sms = 148;
+    PPO_RETURN_IF_CUDA(cudaGetDevice(&dev));
+    PPO_RETURN_IF_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
+    auto kern = a.per_row ? wide_kernel<true> : wide_kernel<false>;
+    PPO_RETURN_IF_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kWideSmem));
+    kern<<<w.n_units < sms ? w.n_units : sms, kWideThreads, kWideSmem, s>>>(ma, mb, w);
+    return launch_status();
+}
+
 }   // namespace fp8
 }   // namespace ppo
 
@@ -276,5 +546,6 @@ extern "C" int ppo_fp8_matmul(const void *A, int64_t lda, const float *a_scales,
     a.status = workspace ? &ws_header(workspace)->status : nullptr;
     cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
     if (M <= 16) return fp8::launch_narrow<16>(a, A, lda, B, ldb, K, s);
-    return fp8::launch_narrow<64>(a, A, lda, B, ldb, K, s);
+    if (M <= 128) return fp8::launch_narrow<64>(a, A, lda, B, ldb, K, s);
+    return fp8::launch_wide(a, A, lda, B, ldb, K, s);
 }
