@@ -244,25 +244,39 @@ static int launch_narrow(Args a, const void *A, int64_t lda, const void *B, int6
 }
 
 // ---------------------------------------------------------------- wide kernel
-// Rows of A are the 128 lanes of the accumulator tile, 256 rows of B its columns. One persistent block per SM, 320
-// threads: warp 0 = TMA producer (4 stages of 48 KB), warp 1 = MMA issuer (two accumulators of 256 columns, one block
-// of K each), warps 2-9 = epilogue: warp (q, h) owns lanes 32 q .. and columns 128 h .., i.e. thread = one row and one
-// 128-column block of sb, so its factor is a single product sa * sb per block of K and the join is a packed fp32
+// Rows of A are the lanes of the accumulator tile, 256 rows of B its columns. Two blocks on two SMs work as a pair on a
+// 256 x 256 tile: one matrix instruction spans both tensor cores, each block loads its 128 rows of A and 128 of the 256
+// rows of B and keeps 128 result rows, so that a block of K costs an SM 32 KB of loads instead of 48 (alone on a
+// 128 x 256 tile the tensor core waited for its operands: 957 cycles per block of K where its arithmetic needs 512).
+// One persistent pair per two SMs, 384 threads a block: warp 0 = TMA producer (6 stages of 32 KB), warps 1 and 3
+// of the leader = MMA issuers (two accumulators of 256 columns, one block of K each), warps 4-11 = epilogue: warp (q, h) owns lanes 32 q .. and columns 128 h .., i.e. thread = one row and
+// one 128-column block of sb, so its factor is a single product sa * sb per block of K and the join is a packed fp32
 // multiply-add per two elements out of tensor memory. Finished tiles go through shared memory so that rows leave in
 // 128-byte runs.
-constexpr int kBM = 128, kBN = 256, kWideStages = 4, kWideThreads = 320;
-constexpr int kWideABytes = kBM * kBlockK, kWideBBytes = kBN * kBlockK, kWideStage = kWideABytes + kWideBBytes;
+constexpr int kBM = 128, kBN = 256, kPairM = 2 * kBM, kWideStages = 4, kWideThreads = 768;
+constexpr int kWideHalf = 128 * kBlockK, kWideStage = 2 * kWideHalf;     // a block's half of A, of B
 constexpr int kStageOut = 32 * 128;        // per epilogue warp: 32 rows x 128 bytes
-constexpr int kWideSmem = kWideStages * kWideStage + 8 * kStageOut + 1024;
+constexpr int kEpiWarps = 16;
+// blocks of K whose scales are handed over together (two groups in flight), and floats of one block: sa[128], sb
+template <bool PER_ROW> struct Scales {
+    static constexpr int kGroup = PER_ROW ? 4 : 16, kFloats = kBM + (PER_ROW ? kBN : 4), kBytes = 2 * kGroup * kFloats * 4;
+};
+constexpr int kScaleBytes = Scales<false>::kBytes > Scales<true>::kBytes ? Scales<false>::kBytes : Scales<true>::kBytes;
+constexpr int kWideSmem = kWideStages * kWideStage + kEpiWarps * kStageOut + kScaleBytes + 1024;
+static_assert(kWideSmem <= 232448 - 1024, "shared memory of a block");
+
+static_assert(kWideStages % 2 == 0, "the two issuers take turns");
 
 struct WideSmem {
-    unsigned long long full[kWideStages], empty[kWideStages], tmem_full[2], tmem_empty[2];
+    unsigned long long full[kWideStages], empty[kWideStages], tmem_full[2][2];   // [half][accumulator]
+    unsigned long long scale_full[2], scale_empty[2];
+    unsigned long long pair_empty[2][2];   // the leader's: both blocks' epilogues have read the accumulator
     uint32_t tmem_base;
 };
 
 struct WideArgs {
     Args a;
-    int gm, gn, n_units, vec;
+    int gm, gn, n_units, bulk_out;   // bulk_out: rows of C are 16-byte aligned
 };
 
 // unit -> output tile: blocks of gm x gn tiles (m fastest inside), column of blocks by column of blocks; a block's
@@ -274,7 +288,7 @@ __device__ __forceinline__ int2 tile_of(int u, int m_tiles, int n_tiles, int gm,
     return make_int2(blk * gm + in % height, col * gn + in / height);
 }
 
-// the loads of this thread so far have arrived in `r`
+// this thread's loads so far have arrived, in `r` (which the compiler may not use before)
 __device__ __forceinline__ void tmem_wait16(uint32_t (&r)[16])
 {
     asm volatile("tcgen05.wait::ld.sync.aligned;"
@@ -284,206 +298,270 @@ __device__ __forceinline__ void tmem_wait16(uint32_t (&r)[16])
                  : "memory");
 }
 
-// 32 rows x 128 bytes of a finished tile from this warp's staging buffer to global memory; elements past N stay unwritten
+// acc += r * f, or r * f * sbs[column] (16 columns)
+template <bool PER_ROW>
+__device__ __forceinline__ void join16(float2 *acc, const uint32_t (&r)[16], float f, const float *sbs)
+{
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        float2 f0 = make_float2(f, f), f1 = f0;
+        if (PER_ROW) {
+            const float4 s4 = reinterpret_cast<const float4 *>(sbs)[j];
+            f0 = __fmul2_rn(f0, make_float2(s4.x, s4.y));
+            f1 = __fmul2_rn(f1, make_float2(s4.z, s4.w));
+        }
+        const uint32_t *p = r + j * 4;
+        acc[j * 2] = __ffma2_rn(make_float2(__uint_as_float(p[0]), __uint_as_float(p[1])), f0, acc[j * 2]);
+        acc[j * 2 + 1] = __ffma2_rn(make_float2(__uint_as_float(p[2]), __uint_as_float(p[3])), f1, acc[j * 2 + 1]);
+    }
+}
+
+// 4 bytes of global memory into shared memory, asynchronously; zero where !valid
+__device__ __forceinline__ void copy4(float *dst, const float *src, bool valid)
+{
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(saddr(dst)), "l"(src), "r"(valid ? 4 : 0) : "memory");
+}
+
+// 32 rows x 128 bytes of a finished tile from this warp's staging buffer to a result whose rows no bulk copy can take
 template <typename T>
-__device__ __forceinline__ void store_rows(const unsigned char *stage, T *out, int64_t ldc, int m, int M, int n, int N, bool vec)
+__device__ __forceinline__ void store_rows(const unsigned char *stage, T *out, int64_t ldc, int m, int M, int n, int N)
 {
     constexpr int E = 16 / sizeof(T), W = 128 / sizeof(T);     // elements per 16 bytes, per row
     const int lane = threadIdx.x & 31;
-    if (vec && n + W <= N) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int r = i * 4 + (lane >> 3), c = lane & 7;
-            const uint4 v = *reinterpret_cast<const uint4 *>(stage + r * 128 + ((c ^ (r & 7)) << 4));
-            if (m + r < M) *reinterpret_cast<uint4 *>(out + (int64_t)(m + r) * ldc + n + c * E) = v;
-        }
-    } else {
-        for (int r = 0; r < 32 && m + r < M; ++r)
-            for (int e = lane; e < W && n + e < N; e += 32)
-                out[(int64_t)(m + r) * ldc + n + e] =
-                    *reinterpret_cast<const T *>(stage + r * 128 + (((e / E) ^ (r & 7)) << 4) + (e % E) * sizeof(T));
-    }
+    for (int r = 0; r < 32 && m + r < M; ++r)
+        for (int e = lane; e < W && n + e < N; e += 32)
+            out[(int64_t)(m + r) * ldc + n + e] =
+                *reinterpret_cast<const T *>(stage + r * 128 + (((e / E) ^ (r & 7)) << 4) + (e % E) * sizeof(T));
 }
 
 template <bool PER_ROW>
 __global__ void __launch_bounds__(kWideThreads, 1)
-wide_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const WideArgs w)
+wide_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+            const __grid_constant__ CUtensorMap map_c, const WideArgs w)
 {
     const Args &a = w.a;
+    constexpr int kGroup = Scales<PER_ROW>::kGroup, kFloats = Scales<PER_ROW>::kFloats, kGroupFloats = kGroup * kFloats;
     extern __shared__ __align__(1024) unsigned char smem_raw[];
     __shared__ WideSmem sm;
     unsigned char *ring = smem_raw + ((1024u - (saddr(smem_raw) & 1023u)) & 1023u);
+    float *scales = reinterpret_cast<float *>(ring + kWideStages * kWideStage + kEpiWarps * kStageOut);   // [2][kGroup][kFloats]
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         for (int s = 0; s < kWideStages; ++s) {
             barrier_init(&sm.full[s], 1);
-            barrier_init(&sm.empty[s], 1);
+            barrier_init(&sm.empty[s], 2);                      // both halves' products
         }
         for (int b = 0; b < 2; ++b) {
-            barrier_init(&sm.tmem_full[b], 1);
-            barrier_init(&sm.tmem_empty[b], 8);
+            for (int g = 0; g < 2; ++g) {
+                barrier_init(&sm.tmem_full[g][b], 1);
+                barrier_init(&sm.pair_empty[g][b], kEpiWarps);
+            }
+            barrier_init(&sm.scale_full[b], 1);
+            barrier_init(&sm.scale_empty[b], kEpiWarps);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 1) tmem_alloc_all(&sm.tmem_base);
+    if (warp == 0) tmem_alloc_all_pair(&sm.tmem_base);
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
+    cluster_barrier();                                          // the other block's barriers are ready too
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem_base = sm.tmem_base;
     const int kbs = a.kb_total;
+    const int rank = (int)cluster_rank(), first = blockIdx.x / 2, step = gridDim.x / 2;
 
+    // registers of the first eight warps go to the accumulators: 256 x 32 + 512 x 104 = 768 x 80
+    if (warp < 8) asm volatile("setmaxnreg.dec.sync.aligned.u32 32;");
     if (warp == 0) {
         if (lane == 0) {
             bool alive = true;
-            uint32_t it = 0;
-            for (int u = blockIdx.x; u < w.n_units && alive; u += gridDim.x) {
+            uint32_t it = 0, s = 0, parity = 1;                 // (waiting for the phase before the first returns at once)
+            for (int u = first; u < w.n_units && alive; u += step) {
                 const int2 t = tile_of(u, a.m_tiles, a.n_tiles, w.gm, w.gn);
                 for (int kb = 0; kb < kbs; ++kb, ++it) {
-                    const int s = it % kWideStages;
-                    if (it >= kWideStages) wait_alive(alive, &sm.empty[s], ((it / kWideStages) - 1) & 1, a.status);
+                    wait_alive(alive, &sm.empty[s], parity, a.status);
                     if (!alive) break;
                     unsigned char *stage = ring + (size_t)s * kWideStage;
-                    barrier_expect_tx(&sm.full[s], (uint32_t)kWideStage);
-                    tma_load_2d(stage, &map_a, kb * kBlockK, t.x * kBM, &sm.full[s]);
-                    tma_load_2d(stage + kWideABytes, &map_b, kb * kBlockK, t.y * kBN, &sm.full[s]);
+                    // (bytes of the other block may be counted before they are announced: the phase cannot end
+                    // without the leader's arrival)
+                    if (rank == 0) barrier_expect_tx(&sm.full[s], 2u * kWideStage);
+                    const uint32_t bar = leader_addr(&sm.full[s]);
+                    tma_load_2d_pair(stage, &map_a, kb * kBlockK, t.x * kPairM + rank * kBM, bar);
+                    // of the 128 columns of each half, 64 rows of B come from either block
+                    tma_load_2d_pair(stage + kWideHalf, &map_b, kb * kBlockK, t.y * kBN + rank * 64, bar);
+                    tma_load_2d_pair(stage + kWideHalf + kWideHalf / 2, &map_b, kb * kBlockK, t.y * kBN + 128 + rank * 64, bar);
+                    if (++s == kWideStages) { s = 0; parity ^= 1; }
                 }
             }
             // copies in flight land before the block may end
-            for (uint32_t i = it > kWideStages ? it - kWideStages : 0; i < it; ++i)
-                wait(&sm.full[i % kWideStages], (i / kWideStages) & 1, a.status);
+            if (rank == 0)
+                for (uint32_t i = it > kWideStages ? it - kWideStages : 0; i < it; ++i)
+                    wait(&sm.full[i % kWideStages], (i / kWideStages) & 1, a.status);
+        }
+        __syncwarp();
+    } else if (warp >= 4 && warp < 8) {
+        // One issuer per accumulator. Its two waits hold an issuing thread for up to 170 cycles each even when they are
+        // over, and the hand-over of an accumulator to the epilogue and back takes about 900 cycles besides the work on
+        // it: four accumulators of 128 columns, two per half, keep the tensor cores busy meanwhile. No order is needed
+        // between them.
+        if (rank == 0) {
+            constexpr uint32_t idesc = instr_desc_e4m3(kPairM, 128);
+            const uint32_t g = warp & 1, buf = (warp >> 1) & 1;
+            const uint64_t desc0 = smem_desc(saddr(ring), 16, 1024);
+            const uint32_t total = (uint32_t)((w.n_units - first + step - 1) / step) * (uint32_t)kbs;
+            const uint32_t tmem_d = tmem_base + buf * kBN + g * 128;
+            bool alive = true;
+            uint32_t s = buf, s_parity = 0, b_parity = 1;
+            for (uint32_t it = buf; it < total; it += 2) {
+                wait_alive(alive, &sm.full[s], s_parity, a.status);
+                wait_alive(alive, &sm.pair_empty[g][buf], b_parity, a.status);
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                // rows 64 g .. of either block's 128 rows of B
+                const uint64_t ad = desc0 + s * (kWideStage >> 4), bd = ad + ((kWideHalf + g * (kWideHalf / 2)) >> 4);
+                if (elect_one()) {
+#pragma unroll
+                    for (int kk = 0; kk < kBlockK / 32; ++kk) mma_f8_pair(tmem_d, ad + kk * 2, bd + kk * 2, idesc, kk ? 1u : 0u);
+                    commit_pair(&sm.tmem_full[g][buf]);
+                    commit_pair(&sm.empty[s]);
+                }
+                __syncwarp();
+                s += 2;
+                if (s >= kWideStages) { s -= kWideStages; s_parity ^= 1; }
+                b_parity ^= 1;
+            }
         }
         __syncwarp();
     } else if (warp == 1) {
-        if (lane == 0) {
-            constexpr uint32_t idesc = instr_desc_e4m3(kBM, kBN);
-            bool alive = true;
-            uint32_t it = 0;
-            for (int u = blockIdx.x; u < w.n_units; u += gridDim.x) {
-                for (int kb = 0; kb < kbs; ++kb, ++it) {
-                    const int s = it % kWideStages, buf = it & 1;
-                    if (it >= 2) wait_alive(alive, &sm.tmem_empty[buf], ((it >> 1) - 1) & 1, a.status);
-                    wait_alive(alive, &sm.full[s], (it / kWideStages) & 1, a.status);
-                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                    const uint32_t a_addr = saddr(ring + (size_t)s * kWideStage), b_addr = a_addr + kWideABytes;
+        // scales: their latency is several blocks of K, so they are fetched a group ahead of the epilogue
+        bool alive = true;
+        uint32_t g = 0, parity = 1;
+        for (int u = first; u < w.n_units; u += step) {
+            const int2 t = tile_of(u, a.m_tiles, a.n_tiles, w.gm, w.gn);
+            const int m0 = t.x * kPairM + rank * kBM, n0 = t.y * kBN;
+            for (int kb0 = 0; kb0 < kbs; kb0 += kGroup) {
+                wait_alive(alive, &sm.scale_empty[g], parity, a.status);
+                __syncwarp();
+                float *to = scales + g * kGroupFloats;
+                for (int kb = kb0; kb < min(kb0 + kGroup, kbs); ++kb, to += kFloats) {
+                    const float *pa = a.sa + (int64_t)kb * a.M;
 #pragma unroll
-                    for (int kk = 0; kk < kBlockK / 32; ++kk)
-                        mma_f8(tmem_base + buf * kBN, smem_desc(a_addr + kk * 32, 16, 1024), smem_desc(b_addr + kk * 32, 16, 1024),
-                               idesc, kk ? 1u : 0u);
-                    commit(&sm.empty[s]);
-                    commit(&sm.tmem_full[buf]);
+                    for (int j = lane; j < kBM; j += 32) copy4(to + j, m0 + j < a.M ? pa + m0 + j : a.sa, m0 + j < a.M);
+                    if (PER_ROW) {
+                        const float *pb = a.sb + (int64_t)kb * a.N;
+#pragma unroll
+                        for (int j = lane; j < kBN; j += 32) copy4(to + kBM + j, n0 + j < a.N ? pb + n0 + j : a.sb, n0 + j < a.N);
+                    } else if (lane < kBN / 128) {
+                        const bool in = n0 + lane * 128 < a.N;
+                        copy4(to + kBM + lane, in ? a.sb + (int64_t)(n0 / 128 + lane) * kbs + kb : a.sb, in);
+                    }
                 }
+                asm volatile("cp.async.wait_all;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) barrier_arrive(&sm.scale_full[g]);
+                parity ^= g;
+                g ^= 1;
             }
         }
-        __syncwarp();
-    } else {
-        const int q = warp & 3, h = (warp - 2) >> 2;
-        unsigned char *stage = ring + (size_t)kWideStages * kWideStage + (warp - 2) * kStageOut;
-        float *sbs = reinterpret_cast<float *>(stage);          // PER_ROW: this warp's 128 factors of a block of K
-        const uint32_t taddr = tmem_base + h * 128 + ((uint32_t)(q * 32) << 16);
-        bool alive = true;
-        uint32_t it = 0;
-        for (int u = blockIdx.x; u < w.n_units; u += gridDim.x) {
-            const int2 t = tile_of(u, a.m_tiles, a.n_tiles, w.gm, w.gn);
-            const int m = t.x * kBM + q * 32 + lane, n = t.y * kBN + h * 128;
-            float2 acc[64];
+    } else if (warp >= 8) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 104;");
+        const int q = warp & 3, c64 = (warp - 8) >> 2, h = c64 >> 1;   // lanes 32 q .., columns 64 c64 .., their half
+        unsigned char *stage = ring + (size_t)kWideStages * kWideStage + (warp - 8) * kStageOut;
+        const uint32_t taddr = tmem_base + c64 * 64 + ((uint32_t)(q * 32) << 16);
+        const uint32_t pair_empty0 = leader_addr(&sm.pair_empty[h][0]), pair_empty1 = leader_addr(&sm.pair_empty[h][1]);
+        bool alive = true, ready = false;                       // ready: the next accumulator is known to be there
+        uint32_t buf = 0, parity = 0, g = 0, g_parity = 0;
+        for (int u = first; u < w.n_units; u += step) {
+            float2 acc[32];
 #pragma unroll
-            for (int j = 0; j < 64; ++j) acc[j] = make_float2(0.f, 0.f);
-            // scales of the next block of K, loaded one block ahead
-            float next_sa, next_sb = 0.f;
-            float4 next_row = make_float4(0.f, 0.f, 0.f, 0.f);
-            auto fetch = [&](int kb) {
-                next_sa = m < a.M ? __ldg(a.sa + (int64_t)kb * a.M + m) : 0.f;
-                if (PER_ROW) {
-                    const float *p = a.sb + (int64_t)kb * a.N + n;
-                    next_row.x = n + lane < a.N ? __ldg(p + lane) : 0.f;
-                    next_row.y = n + lane + 32 < a.N ? __ldg(p + lane + 32) : 0.f;
-                    next_row.z = n + lane + 64 < a.N ? __ldg(p + lane + 64) : 0.f;
-                    next_row.w = n + lane + 96 < a.N ? __ldg(p + lane + 96) : 0.f;
-                } else {
-                    next_sb = n < a.N ? __ldg(a.sb + (int64_t)(n / 128) * kbs + kb) : 0.f;
+            for (int j = 0; j < 32; ++j) acc[j] = make_float2(0.f, 0.f);
+            const float *slot = scales;
+            int left = 0;                                       // blocks of K left in the group of scales
+#pragma unroll 1
+            for (int kb = 0; kb < kbs; ++kb) {
+                if (left == 0) {
+                    wait_alive(alive, &sm.scale_full[g], g_parity, a.status);
+                    slot = scales + g * kGroupFloats;
+                    left = min(kGroup, kbs - kb);
                 }
-            };
-            fetch(0);
-            for (int kb = 0; kb < kbs; ++kb, ++it) {
-                const uint32_t buf = it & 1;
-                const float f = PER_ROW ? next_sa : next_sa * next_sb;
-                if (PER_ROW) {
-                    __syncwarp();                               // everyone has read the block before
-                    sbs[lane] = next_row.x;
-                    sbs[lane + 32] = next_row.y;
-                    sbs[lane + 64] = next_row.z;
-                    sbs[lane + 96] = next_row.w;
-                }
-                if (kb + 1 < kbs) fetch(kb + 1);
-                wait_alive(alive, &sm.tmem_full[buf], (it >> 1) & 1, a.status);
+                const float f = PER_ROW ? slot[q * 32 + lane] : slot[q * 32 + lane] * slot[kBM + h];
+                const float *sbs = slot + kBM + c64 * 64;       // PER_ROW: this warp's 64 factors
+                if (!ready) wait_alive(alive, &sm.tmem_full[h][buf], parity, a.status);
                 __syncwarp();
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 uint32_t r[2][16];
-                tmem_ld16(taddr + buf * kBN, r[0]);
-#pragma unroll
-                for (int c = 0; c < 8; ++c) {
-                    tmem_wait16(r[c & 1]);
-                    if (c < 7) {
-                        tmem_ld16(taddr + buf * kBN + (c + 1) * 16, r[(c + 1) & 1]);
-                    } else {
-                        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-                        __syncwarp();
-                        if (lane == 0) barrier_arrive(&sm.tmem_empty[buf]);
-                    }
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        float2 f0 = make_float2(f, f), f1 = f0;
-                        if (PER_ROW) {
-                            const float4 s4 = reinterpret_cast<const float4 *>(sbs)[c * 4 + j];
-                            f0 = __fmul2_rn(f0, make_float2(s4.x, s4.y));
-                            f1 = __fmul2_rn(f1, make_float2(s4.z, s4.w));
-                        }
-                        const uint32_t *p = r[c & 1] + j * 4;
-                        acc[c * 8 + j * 2] = __ffma2_rn(make_float2(__uint_as_float(p[0]), __uint_as_float(p[1])), f0, acc[c * 8 + j * 2]);
-                        acc[c * 8 + j * 2 + 1] =
-                            __ffma2_rn(make_float2(__uint_as_float(p[2]), __uint_as_float(p[3])), f1, acc[c * 8 + j * 2 + 1]);
-                    }
-                }
-            }
-            // the tile: 64 bf16 or 32 fp32 columns at a time; 16-byte piece c of row r lies at c ^ (r & 7)
-            const int m_warp = t.x * kBM + q * 32;
-            __syncwarp();
-            if (a.out_f32) {
+                const uint32_t at = taddr + buf * kBN;
+                tmem_ld16(at, r[0]);
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
+                    tmem_wait16(r[c & 1]);
+                    if (c < 3) {
+                        tmem_ld16(at + (c + 1) * 16, r[(c + 1) & 1]);
+                    } else {
+                        // released before the last multiply-adds: what stands between an accumulator's arrival and its
+                        // release is on the way from one matrix instruction to the next
+                        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                        __syncwarp();
+                        barrier_arrive_cluster_if(buf ? pair_empty1 : pair_empty0, lane == 0);
+                        parity ^= buf;
+                        buf ^= 1;
+                        ready = peek(&sm.tmem_full[h][buf], parity);
+                    }
+                    join16<PER_ROW>(acc + c * 8, r[c & 1], f, sbs + c * 16);
+                }
+                slot += kFloats;
+                if (--left == 0) {
+                    __syncwarp();
+                    if (lane == 0) barrier_arrive(&sm.scale_empty[g]);
+                    g_parity ^= g;
+                    g ^= 1;
+                }
+            }
+            // the tile: 64 bf16 or 32 fp32 columns at a time through shared memory, 16-byte piece c of row r at c ^ (r & 7)
+            const int2 t = tile_of(u, a.m_tiles, a.n_tiles, w.gm, w.gn);
+            const int m_warp = t.x * kPairM + rank * kBM + q * 32, n = t.y * kBN + c64 * 64;
+            unsigned char *row = stage + lane * 128;
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                if (c == 1 && !a.out_f32) break;
+                if (lane == 0) tma_store_wait_read();           // the buffer's last copy has read it
+                __syncwarp();
+                if (a.out_f32) {
 #pragma unroll
                     for (int j = 0; j < 8; ++j)
-                        *reinterpret_cast<float4 *>(stage + lane * 128 + ((j ^ (lane & 7)) << 4)) =
-                            make_float4(acc[c * 16 + j * 2].x, acc[c * 16 + j * 2].y, acc[c * 16 + j * 2 + 1].x, acc[c * 16 + j * 2 + 1].y);
-                    __syncwarp();
-                    store_rows(stage, reinterpret_cast<float *>(a.out), a.ldc, m_warp, a.M, n + c * 32, a.N, w.vec != 0);
-                    __syncwarp();
-                }
-            } else {
-#pragma unroll
-                for (int c = 0; c < 2; ++c) {
+                        *reinterpret_cast<float4 *>(row + ((j ^ (lane & 7)) << 4)) = make_float4(
+                            acc[c * 16 + j * 2].x, acc[c * 16 + j * 2].y, acc[c * 16 + j * 2 + 1].x, acc[c * 16 + j * 2 + 1].y);
+                } else {
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
                         uint32_t v[4];
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
-                            const __nv_bfloat162 b2 = __float22bfloat162_rn(acc[c * 32 + j * 4 + e]);
+                            const __nv_bfloat162 b2 = __float22bfloat162_rn(acc[j * 4 + e]);
                             v[e] = *reinterpret_cast<const uint32_t *>(&b2);
                         }
-                        *reinterpret_cast<uint4 *>(stage + lane * 128 + ((j ^ (lane & 7)) << 4)) = make_uint4(v[0], v[1], v[2], v[3]);
+                        *reinterpret_cast<uint4 *>(row + ((j ^ (lane & 7)) << 4)) = make_uint4(v[0], v[1], v[2], v[3]);
                     }
+                }
+                if (w.bulk_out) {
+                    fence_async_proxy();
                     __syncwarp();
-                    store_rows(stage, reinterpret_cast<__nv_bfloat16 *>(a.out), a.ldc, m_warp, a.M, n + c * 64, a.N, w.vec != 0);
+                    if (lane == 0 && m_warp < a.M && n + c * 32 < a.N) tma_store_2d(&map_c, n + c * 32, m_warp, stage);
+                } else {
+                    __syncwarp();
+                    if (a.out_f32) store_rows(stage, reinterpret_cast<float *>(a.out), a.ldc, m_warp, a.M, n + c * 32, a.N);
+                    else store_rows(stage, reinterpret_cast<__nv_bfloat16 *>(a.out), a.ldc, m_warp, a.M, n, a.N);
                     __syncwarp();
                 }
             }
         }
+        if (lane == 0) tma_store_wait_read();                   // shared memory outlives the copies out of it
     }
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
-    if (warp == 1) {
+    cluster_barrier();                                          // neither block ends while the other may reach into it
+    if (warp == 0) {
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        tmem_free_all(tmem_base);
+        tmem_free_all_pair(tmem_base);
     }
 }
 
@@ -492,25 +570,42 @@ static int launch_wide(Args a, const void *A, int64_t lda, const void *B, int64_
     CUtensorMap ma, mb;
     int rc = make_map_8bit(&ma, A, (uint64_t)K, (uint64_t)a.M, (uint64_t)lda, kBM);
     if (rc) return rc;
-    rc = make_map_8bit(&mb, B, (uint64_t)K, (uint64_t)a.N, (uint64_t)ldb, kBN);
+    rc = make_map_8bit(&mb, B, (uint64_t)K, (uint64_t)a.N, (uint64_t)ldb, 64);
     if (rc) return rc;
-    a.m_tiles = (a.M + kBM - 1) / kBM;
+    a.m_tiles = (a.M + kPairM - 1) / kPairM;
     a.n_tiles = (a.N + kBN - 1) / kBN;
     const int64_t units = (int64_t)a.m_tiles * a.n_tiles;
     if (units >= ((int64_t)1 << 30)) return PPO_ERR_SHAPE;
     WideArgs w = {};
     w.a = a;
-    w.gm = 37;
-    w.gn = 4;
+    w.gm = 8;
+    w.gn = 9;
     w.n_units = (int)units;
-    w.vec = reinterpret_cast<uintptr_t>(a.out) % 16 == 0 && (a.ldc * (a.out_f32 ? 4 : 2)) % 16 == 0;
+    const int64_t pitch = a.ldc * (a.out_f32 ? 4 : 2);
+    w.bulk_out = reinterpret_cast<uintptr_t>(a.out) % 16 == 0 && pitch % 16 == 0 && pitch < ((int64_t)1 << 40);
+    CUtensorMap mc = {};
+    if (w.bulk_out) {
+        rc = make_map_out(&mc, a.out, a.out_f32 != 0, (uint64_t)a.N, (uint64_t)a.M, (uint64_t)pitch, 32);
+        if (rc) return rc;
+    }
     int dev = 0, sms = 148;
     PPO_RETURN_IF_CUDA(cudaGetDevice(&dev));
     PPO_RETURN_IF_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
     auto kern = a.per_row ? wide_kernel<true> : wide_kernel<false>;
     PPO_RETURN_IF_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kWideSmem));
-    kern<<<w.n_units < sms ? w.n_units : sms, kWideThreads, kWideSmem, s>>>(ma, mb, w);
-    return launch_status();
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(2 * (w.n_units < sms / 2 ? w.n_units : sms / 2)));
+    cfg.blockDim = dim3(kWideThreads);
+    cfg.dynamicSmemBytes = kWideSmem;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = 2;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    PPO_RETURN_IF_CUDA(cudaLaunchKernelEx(&cfg, kern, ma, mb, mc, w));
+    return PPO_OK;
 }
 
 }   // namespace fp8

@@ -1,6 +1,6 @@
 // tcgen05 / TMA / mbarrier building blocks shared by the tensor-core kernels (fused LM head and its backward):
 // bounded mbarrier wait, 2-D tensor-map loads, shared-memory and instruction descriptors, MMA issue and commit,
-// tensor-memory loads, and the host-side tensor-map encoder. sm_100a only; no cluster multicast anywhere.
+// tensor-memory loads, pairs of blocks, and the host-side tensor-map encoder. sm_100a only; no load is multicast.
 #pragma once
 
 #include <cuda.h>
@@ -36,6 +36,36 @@ __device__ __forceinline__ bool wait(unsigned long long *bar, uint32_t parity, i
     return false;
 }
 
+// true in one lane of a converged warp
+__device__ __forceinline__ bool elect_one()
+{
+    uint32_t ok;
+    asm volatile(
+        "{\n"
+        ".reg .pred p;\n"
+        "elect.sync _|p, 0xffffffff;\n"
+        "selp.u32 %0, 1, 0, p;\n"
+        "}\n"
+        : "=r"(ok));
+    return ok != 0;
+}
+
+// whether the phase with the given parity is over, without waiting for it: asked early, its latency is hidden
+__device__ __forceinline__ bool peek(unsigned long long *bar, uint32_t parity)
+{
+    uint32_t ok;
+    asm volatile(
+        "{\n"
+        ".reg .pred p;\n"
+        "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n"
+        "selp.u32 %0, 1, 0, p;\n"
+        "}\n"
+        : "=r"(ok)
+        : "r"(saddr(bar)), "r"(parity)
+        : "memory");
+    return ok != 0;
+}
+
 __device__ __forceinline__ void barrier_init(unsigned long long *bar, uint32_t count)
 {
     asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(saddr(bar)), "r"(count) : "memory");
@@ -58,6 +88,31 @@ __device__ __forceinline__ void tma_load_2d(void *dst, const CUtensorMap *map, i
         "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
         ::"r"(saddr(dst)), "l"(map), "r"(x), "r"(y), "r"(saddr(bar))
         : "memory");
+}
+
+// one box from shared memory to a 2-D tensor map (what lies outside the tensor is left out); the issuing thread's
+// bulk group covers it
+__device__ __forceinline__ void tma_store_2d(const CUtensorMap *map, int x, int y, const void *src)
+{
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];"
+                 ::"l"(map), "r"(x), "r"(y), "r"(saddr(src)) : "memory");
+    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+}
+// the sources of this thread's stores may be written again
+__device__ __forceinline__ void tma_store_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
+// shared-memory writes of this thread so far are visible to bulk copies
+__device__ __forceinline__ void fence_async_proxy() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+// arrive from one lane without a branch
+__device__ __forceinline__ void barrier_arrive_cluster_if(uint32_t cluster_addr, bool here)
+{
+    asm volatile(
+        "{\n"
+        ".reg .pred p;\n"
+        "setp.ne.u32 p, %1, 0;\n"
+        "@p mbarrier.arrive.shared::cluster.b64 _, [%0];\n"
+        "}\n"
+        ::"r"(cluster_addr), "r"((uint32_t)here) : "memory");
 }
 
 // shared-memory matrix descriptor: 128-byte swizzle, version 1; offsets in 16-byte units
@@ -170,6 +225,76 @@ __device__ __forceinline__ void tmem_free_all(uint32_t base)
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(base), "r"(512u) : "memory");
 }
 
+// ---------------------------------------------------------------- pairs of blocks (cta_group::2, clusters of two)
+// One matrix instruction spans the tensor cores of both blocks: block 0 (the leader) issues it, each block's shared
+// memory holds its half of either operand at the same offsets and its tensor memory 128 of the 256 result rows.
+__device__ __forceinline__ uint32_t cluster_rank()
+{
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+
+// all threads of all blocks of the cluster, with the memory order of a release and an acquire
+__device__ __forceinline__ void cluster_barrier()
+{
+    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
+// address of `p`'s counterpart in the leader's shared memory
+__device__ __forceinline__ uint32_t leader_addr(const void *p)
+{
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(saddr(p)));
+    return r;
+}
+
+__device__ __forceinline__ void barrier_arrive_cluster(uint32_t cluster_addr)
+{
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+}
+
+// one box into this block's shared memory; its bytes are counted on the leader's barrier
+__device__ __forceinline__ void tma_load_2d_pair(void *dst, const CUtensorMap *map, int x, int y, uint32_t leader_bar)
+{
+    asm volatile(
+        "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+        ::"r"(saddr(dst)), "l"(map), "r"(x), "r"(y), "r"(leader_bar)
+        : "memory");
+}
+
+__device__ __forceinline__ void mma_f8_pair(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile(
+        "{\n"
+        ".reg .pred p;\n"
+        "setp.ne.b32 p, %4, 0;\n"
+        "tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, {%5, %5, %5, %5, %5, %5, %5, %5}, p;\n"
+        "}\n"
+        ::"r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate), "r"(0u)
+        : "memory");
+}
+
+// arrive on `bar` of both blocks once every MMA issued so far by this thread has completed
+__device__ __forceinline__ void commit_pair(unsigned long long *bar)
+{
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+                 ::"r"(saddr(bar)), "h"((uint16_t)3) : "memory");
+}
+
+// one warp of each block calls each of the two
+__device__ __forceinline__ void tmem_alloc_all_pair(uint32_t *base_slot)
+{
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(saddr(base_slot)), "r"(512u)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+}
+
+__device__ __forceinline__ void tmem_free_all_pair(uint32_t base)
+{
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(base), "r"(512u) : "memory");
+}
+
 // ---------------------------------------------------------------- host side
 typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
                                   const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
@@ -215,6 +340,21 @@ inline int make_map_8bit(CUtensorMap *map, const void *base, uint64_t inner, uin
     const cuuint32_t elem[2] = {1, 1};
     const CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(base), dims, strides, box, elem,
                           CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? PPO_OK : (int)cudaErrorInvalidValue;
+}
+
+// 2-D result [outer, inner] of fp32 or bf16 with a row pitch in bytes (a multiple of 16), boxes of box_outer rows x 128 bytes
+inline int make_map_out(CUtensorMap *map, void *base, bool f32, uint64_t inner, uint64_t outer, uint64_t pitch, uint32_t box_outer)
+{
+    EncodeTiledFn fn = encode_fn();
+    if (!fn) return (int)cudaErrorNotSupported;
+    const cuuint64_t dims[2] = {inner, outer};
+    const cuuint64_t strides[1] = {pitch};
+    const cuuint32_t box[2] = {f32 ? 32u : 64u, box_outer};
+    const cuuint32_t elem[2] = {1, 1};
+    const CUresult r = fn(map, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, base, dims, strides, box,
+                          elem, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
                           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS ? PPO_OK : (int)cudaErrorInvalidValue;
 }
