@@ -578,8 +578,8 @@ static int launch_wide(Args a, const void *A, int64_t lda, const void *B, int64_
     if (units >= ((int64_t)1 << 30)) return PPO_ERR_SHAPE;
     WideArgs w = {};
     w.a = a;
-    w.gm = 8;
-    w.gn = 9;
+    w.gm = 5;
+    w.gn = 16;
     w.n_units = (int)units;
     const int64_t pitch = a.ldc * (a.out_f32 ? 4 : 2);
     w.bulk_out = reinterpret_cast<uintptr_t>(a.out) % 16 == 0 && pitch % 16 == 0 && pitch < ((int64_t)1 << 40);

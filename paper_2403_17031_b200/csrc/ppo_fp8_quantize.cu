@@ -9,6 +9,7 @@
 //                that neither side has bank conflicts).
 // A block with a NaN or an infinity has scale NaN and q NaN throughout.
 #include <cuda_fp8.h>
+#include <string.h>
 
 #include "ppo_rows.cuh"
 
@@ -19,43 +20,122 @@ constexpr int kThreads = 256;
 constexpr float kMax = 448.f;
 constexpr float kMinAmax = 7.8886090522101181e-31f;   // 2^-100: keeps 448 / a finite
 
-template <typename T>
-__device__ __forceinline__ void load8(const T *src, int valid, bool vec, float (&x)[8])
+// maximum that keeps a NaN
+__device__ __forceinline__ float max_nan(float a, float b)
 {
-    constexpr int N = Pack<T>::N;
-    if (vec && valid >= 8) {
-#pragma unroll
-        for (int h = 0; h < 8 / N; ++h) {
-            float y[N];
-            Pack<T>::unpack_raw(ld_stream(reinterpret_cast<const uint4 *>(src) + h), y);
-#pragma unroll
-            for (int e = 0; e < N; ++e) x[h * N + e] = y[e];
-        }
-    } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = e < valid ? Pack<T>::load1(src + e) : 0.f;
-    }
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
 }
 
-// maximum of |x| as a bit pattern (ordered like the values; infinities and NaN are above every finite one)
-__device__ __forceinline__ uint32_t abs_max8(const float (&x)[8], uint32_t m)
-{
+// Eight consecutive elements as they lie in memory, and maxima of their magnitudes: in the storage type for bf16 (two per
+// instruction), column by column or over all.
+template <typename T> struct Eight;
+
+template <> struct Eight<float> {
+    uint4 w[2];
+    struct Max {
+        float m;
+        __device__ __forceinline__ void init() { m = 0.f; }
+        __device__ __forceinline__ void add(const Eight &x)
+        {
+            float y[8];
+            x.get(y);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) m = max(m, __float_as_uint(x[e]) & 0x7fffffffu);
-    return m;
+            for (int e = 0; e < 8; ++e) m = max_nan(m, fabsf(y[e]));
+        }
+        __device__ __forceinline__ float value() const { return m; }
+    };
+    struct MaxByColumn {
+        float m[8];
+        __device__ __forceinline__ void init()
+        {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) m[e] = 0.f;
+        }
+        __device__ __forceinline__ void add(const Eight &x)
+        {
+            float y[8];
+            x.get(y);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) m[e] = max_nan(m[e], fabsf(y[e]));
+        }
+        __device__ __forceinline__ float value(int e) const { return m[e]; }
+    };
+    __device__ __forceinline__ void get(float (&x)[8]) const
+    {
+        const float *f = reinterpret_cast<const float *>(w);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = f[e];
+    }
+};
+
+template <> struct Eight<__nv_bfloat16> {
+    uint4 w[1];
+    static __device__ __forceinline__ __nv_bfloat162 as2(uint32_t v) { return *reinterpret_cast<__nv_bfloat162 *>(&v); }
+    struct MaxByColumn {
+        __nv_bfloat162 m[4];
+        __device__ __forceinline__ void init()
+        {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) m[e] = as2(0u);
+        }
+        __device__ __forceinline__ void add(const Eight &x)
+        {
+            m[0] = __hmax2_nan(m[0], __habs2(as2(x.w[0].x)));
+            m[1] = __hmax2_nan(m[1], __habs2(as2(x.w[0].y)));
+            m[2] = __hmax2_nan(m[2], __habs2(as2(x.w[0].z)));
+            m[3] = __hmax2_nan(m[3], __habs2(as2(x.w[0].w)));
+        }
+        __device__ __forceinline__ float value(int e) const
+        {
+            const uint32_t bits = *reinterpret_cast<const uint32_t *>(&m[e >> 1]);
+            return __uint_as_float((e & 1) ? bits & 0xffff0000u : bits << 16);
+        }
+    };
+    struct Max {
+        __nv_bfloat162 m;
+        __device__ __forceinline__ void init() { m = as2(0u); }
+        __device__ __forceinline__ void add(const Eight &x)
+        {
+            const __nv_bfloat162 a = __hmax2_nan(__habs2(as2(x.w[0].x)), __habs2(as2(x.w[0].y)));
+            const __nv_bfloat162 b = __hmax2_nan(__habs2(as2(x.w[0].z)), __habs2(as2(x.w[0].w)));
+            m = __hmax2_nan(m, __hmax2_nan(a, b));
+        }
+        __device__ __forceinline__ float value() const
+        {
+            const uint32_t bits = *reinterpret_cast<const uint32_t *>(&m);
+            return max_nan(__uint_as_float(bits << 16), __uint_as_float(bits & 0xffff0000u));
+        }
+    };
+    __device__ __forceinline__ void get(float (&x)[8]) const { Pack<__nv_bfloat16>::unpack_raw(w[0], x); }
+};
+
+template <typename T>
+__device__ __forceinline__ void load8(const T *src, int valid, bool vec, Eight<T> &x)
+{
+    if (vec && valid >= 8) {
+#pragma unroll
+        for (int h = 0; h < 8 / Pack<T>::N; ++h) x.w[h] = ld_stream(reinterpret_cast<const uint4 *>(src) + h);
+    } else {
+        T y[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[e] = e < valid ? src[e] : T(0.f);
+        memcpy(x.w, y, sizeof(y));
+    }
 }
 
 struct Scale {
     float s, r;     // scale, and what x is multiplied with
 };
 
-__device__ __forceinline__ Scale scale_of(uint32_t amax_bits)
+__device__ __forceinline__ Scale scale_of(float amax /* NaN when one was among the magnitudes */)
 {
     Scale o;
-    const float a = fmaxf(__uint_as_float(amax_bits), kMinAmax);
+    const float a = fmaxf(amax, kMinAmax);
     o.s = __fdiv_rn(a, kMax);
     o.r = __fdiv_rn(kMax, a);
-    if (amax_bits >= 0x7f800000u) o.s = o.r = __uint_as_float(0x7fffffffu);
+    if (!(amax <= 3.4028234664e38f)) o.s = o.r = __uint_as_float(0x7fffffffu);
     return o;
 }
 
@@ -63,8 +143,11 @@ __device__ __forceinline__ uint32_t q2(float lo, float hi)
 {
     return (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(lo, hi), __NV_SATFINITE, __NV_E4M3);
 }
-__device__ __forceinline__ uint2 q8(const float (&x)[8], float r)
+template <typename T>
+__device__ __forceinline__ uint2 q8(const Eight<T> &v, float r)
 {
+    float x[8];
+    v.get(x);
     return make_uint2(q2(x[0] * r, x[1] * r) | (q2(x[2] * r, x[3] * r) << 16),
                       q2(x[4] * r, x[5] * r) | (q2(x[6] * r, x[7] * r) << 16));
 }
@@ -99,21 +182,31 @@ rows_kernel(const Args a)
     const int c = tc * 256 + lane * 8, r0 = tr * 32;
     const T *x = reinterpret_cast<const T *>(a.x);
     const int valid = min(8, a.C - c);
-    float v[4][8];
+    Eight<T> v[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int r = r0 + i * 8 + warp;
         load8<T>(x + (int64_t)r * a.x_stride + c, r < a.R ? valid : 0, a.vec, v[i]);
     }
+    // the maximum over the block's 16 lanes, of four rows; lane i then divides for row i
+    float mine = 0.f;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        uint32_t m = abs_max8(v[i], 0u);
+        typename Eight<T>::Max mx;
+        mx.init();
+        mx.add(v[i]);
+        float m = mx.value();
 #pragma unroll
-        for (int off = 8; off > 0; off >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, off));
-        const Scale s = scale_of(m);
+        for (int off = 8; off > 0; off >>= 1) m = max_nan(m, __shfl_xor_sync(0xffffffffu, m, off));
+        if ((lane & 3) == i) mine = m;
+    }
+    const Scale s = scale_of(mine);
+    if ((lane & 15) < 4) sc[lane >> 4][(lane & 3) * 8 + warp] = s.s;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
         const int r = r0 + i * 8 + warp;
-        if (r < a.R) store8(a.q + (int64_t)r * a.q_stride + c, q8(v[i], s.r), valid);
-        if ((lane & 15) == 0) sc[lane >> 4][i * 8 + warp] = s.s;
+        const float ri = __shfl_sync(0xffffffffu, s.r, (lane & 16) + i);
+        if (r < a.R) store8(a.q + (int64_t)r * a.q_stride + c, q8(v[i], ri), valid);
     }
     __syncthreads();
     const int kb = tc * 2 + warp, r = r0 + lane;       // scales [ceil(C/128), R]
@@ -127,7 +220,7 @@ tile_kernel(const Args a)
 {
     static_assert(TRANS || BLOCK, "the rows kernel does the rest");
     __shared__ uint2 turn[TRANS ? 128 * 16 : 1];
-    __shared__ uint32_t red[BLOCK ? 8 : 16 * 128];
+    __shared__ float red[BLOCK ? 8 : 16 * 128];
     const int tid = threadIdx.x;
     // neighbouring blocks take neighbouring tiles along the contiguous direction of x
     const int tr = TRANS ? blockIdx.x % a.tiles_r : blockIdx.x / a.tiles_c;
@@ -136,7 +229,7 @@ tile_kernel(const Args a)
     const T *x = reinterpret_cast<const T *>(a.x);
     const int g = tid & 15, h = tid >> 4;
     // TRANS: x rows c0 + 8 h + i, columns (= rows of y) r0 + 8 g ..; else x rows r0 + 16 i + h, columns c0 + 8 g ..
-    float v[8][8];
+    Eight<T> v[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const int xr = TRANS ? c0 + h * 8 + i : r0 + i * 16 + h, xc = (TRANS ? r0 : c0) + g * 8;
@@ -145,47 +238,55 @@ tile_kernel(const Args a)
     }
     float r8[8];
     if (BLOCK) {
-        uint32_t m = 0;
+        typename Eight<T>::Max mx;
+        mx.init();
 #pragma unroll
-        for (int i = 0; i < 8; ++i) m = abs_max8(v[i], m);
-        m = __reduce_max_sync(0xffffffffu, m);
+        for (int i = 0; i < 8; ++i) mx.add(v[i]);
+        float m = mx.value();
+#pragma unroll
+        for (int off = 16; off > 0; off >>= 1) m = max_nan(m, __shfl_xor_sync(0xffffffffu, m, off));
         if ((tid & 31) == 0) red[tid >> 5] = m;
         __syncthreads();
 #pragma unroll
-        for (int w = 0; w < kThreads / 32; ++w) m = max(m, red[w]);
+        for (int w = 0; w < kThreads / 32; ++w) m = max_nan(m, red[w]);
         const Scale s = scale_of(m);
         if (tid == 0) a.scales[(int64_t)tr * a.tiles_c + tc] = s.s;
 #pragma unroll
         for (int e = 0; e < 8; ++e) r8[e] = s.r;
     } else {
+        typename Eight<T>::MaxByColumn mx;
+        mx.init();
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            uint32_t m = 0;
+        for (int i = 0; i < 8; ++i) mx.add(v[i]);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i][e]) & 0x7fffffffu);
-            red[h * 128 + g * 8 + e] = m;
-        }
+        for (int e = 0; e < 8; ++e) red[h * 128 + g * 8 + e] = mx.value(e);
         __syncthreads();
         if (tid < 128) {
-            uint32_t m = 0;
+            float m = 0.f;
 #pragma unroll
-            for (int w = 0; w < 16; ++w) m = max(m, red[w * 128 + tid]);
+            for (int w = 0; w < 16; ++w) m = max_nan(m, red[w * 128 + tid]);
             const Scale s = scale_of(m);
-            red[tid] = __float_as_uint(s.r);            // (row 0 of this column has been read by this thread only)
+            red[tid] = s.r;                                 // (row 0 of this column has been read by this thread only)
             if (r0 + tid < a.R) a.scales[(int64_t)tc * a.R + r0 + tid] = s.s;
         }
         __syncthreads();
 #pragma unroll
-        for (int e = 0; e < 8; ++e) r8[e] = __uint_as_float(red[g * 8 + e]);
+        for (int e = 0; e < 8; ++e) r8[e] = red[g * 8 + e];
     }
     if (TRANS) {
+        // two rows of x at a time: their columns' values go into two neighbouring bytes of a row of q
+        uint32_t out[8][4];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            float col[8];
+        for (int i = 0; i < 8; i += 2) {
+            float x0[8], x1[8];
+            v[i].get(x0);
+            v[i + 1].get(x1);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) col[i] = v[i][e];
-            turn[(g * 8 + e) * 16 + (h ^ g)] = q8(col, r8[e]);
+            for (int e = 0; e < 8; ++e) out[e][i >> 1] = q2(x0[e] * r8[e], x1[e] * r8[e]);
         }
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            turn[(g * 8 + e) * 16 + (h ^ g)] = make_uint2(out[e][0] | (out[e][1] << 16), out[e][2] | (out[e][3] << 16));
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < 8; ++i) {

@@ -2,12 +2,15 @@
 // over the logits (ppo_logprob_topk), and the gradient on all of those back to the logits (ppo_logprob_topk_bwd).
 //
 // Forward. The statistics are those of step 1: sums of 2^(y - ref) and 2^(y - ref) (y - ref) with y = logit log2(e) /
-// temperature, relative to the maximum of the row's first pack. Beside them every thread keeps the maximum of the
+// temperature, relative to a reference per warp. Beside them every thread keeps the maximum of the
 // elements it streams (its "segment": packs tid, tid + 256, ...). Selection then works on segments:
 //   the k-th largest of the 256 segment maxima is a threshold t with at least k elements >= t, so nothing below t is
-//   among the k best; only segments whose maximum reaches t hold candidates, and those few (about k of 256) are
-//   re-read from L2. Candidates are ranked by counting against each other on the 64-bit key (value, ~index), which is
-//   unique: ties go to the lowest index and the order in which candidates arrive does not matter.
+//   among the k best; only segments whose maximum reaches t hold candidates. Every thread also knows the pack of its
+//   maximum and the largest value outside it, so most of these segments (about k of 256) need that one pack re-read
+//   and only those with a second pack that reaches t are searched whole (searching all of them is sector traffic of
+//   0.4 of the row at k = 20 and more than the row at k = 64 in fp32: 85 instead of 48 us for 997 rows). Candidates are
+//   ranked by counting against each other on the 64-bit key (value, ~index), which is unique: ties go to the lowest
+//   index and the order in which candidates arrive does not matter.
 // A slice whose candidates overflow the list (rows of equal values, fewer than k unbanned tokens) is selected by
 // radix passes over it instead.
 // Few rows: a cluster of CL blocks shares a row; each selects the k best of its slice, and block 0 merges the sorted
@@ -47,11 +50,14 @@ struct Smem {
     unsigned long long cand[kCap];
     unsigned long long best[kMaxIds];    // the slice's best, sorted
     uint32_t seg_key[kThreads];          // segment maxima as ordered keys; the fallback's histogram
-    uint16_t list[kThreads];             // segments that hold candidates
+    uint32_t seg_key2[kThreads];         // largest value outside the pack that holds the maximum
+    int seg_pack[kThreads];              // that pack
+    uint16_t list[kThreads];             // segments that hold candidates: from the front those that have to be searched
+                                         // whole, from the back those whose candidates are all in one known pack
     float red[96];
     SoftmaxState st;
     uint32_t threshold;
-    int n_list, n_cand, n_best, bin, need;
+    int n_whole, n_single, n_cand, n_best, bin, need;
 };
 
 // whole numbers that order like the values (-0 equals +0); 0 is below every value
@@ -66,13 +72,25 @@ __device__ __forceinline__ unsigned long long make_key(uint32_t u, int j)
     return ((unsigned long long)u << 32) | (uint32_t)~(uint32_t)j;
 }
 
-// One pack into the sums (clamped at kNegBig, so a -inf logit adds exact zeros) and into the segment maximum.
+// What a thread knows of its segment: the maximum, the pack that holds it, the maximum of the other packs.
+struct Segment {
+    float top, second;
+    int pack;
+    __device__ __forceinline__ void add(float xmax, int i)
+    {
+        second = fmaxf(second, fminf(xmax, top));
+        pack = xmax > top ? i : pack;
+        top = fmaxf(top, xmax);
+    }
+};
+
+// One pack into the sums (clamped at kNegBig, so a -inf logit adds exact zeros) and into the segment.
 template <typename T>
-__device__ __forceinline__ void accumulate(const uint4 &v, float c, float nm, FixedAcc &a, float &tmax)
+__device__ __forceinline__ void accumulate(const uint4 &v, int i, float c, float nm, FixedAcc &a, Segment &seg)
 {
     float x[Pack<T>::N], xmax;
     Pack<T>::unpack(v, x, xmax);
-    tmax = fmaxf(tmax, xmax);
+    seg.add(xmax, i);
     const float2 cc = make_float2(c, c), nn = make_float2(nm, nm);
     float2 s = make_float2(a.s0, a.s1), u = make_float2(a.u0, a.u1);
 #pragma unroll
@@ -86,10 +104,17 @@ __device__ __forceinline__ void accumulate(const uint4 &v, float c, float nm, Fi
     a.u0 = u.x; a.u1 = u.y;
 }
 
+__device__ __forceinline__ float warp_max(float v)
+{
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, off));
+    return v;
+}
+
 // What block `rank` of CL handles of a row: elements [e0, e1), of which packs [p0, p1) of the 16-byte aligned body
 // (body element i of the row is head + i) and at most 2 (N - 1) loose elements at the row's ends.
 struct Slice {
-    int head, p0, p1, e0, e1;
+    int head, p0, p1, e0, e1, loose;
 };
 
 template <typename T>
@@ -104,6 +129,7 @@ __device__ __forceinline__ Slice slice_of(const T *src, int V, int rank, int CL)
     s.p1 = min(nvec, s.p0 + per);
     s.e0 = rank == 0 ? 0 : s.head + s.p0 * N;
     s.e1 = rank == CL - 1 ? V : s.head + s.p1 * N;
+    s.loose = s.e1 - s.e0 - (s.p1 - s.p0) * N;
     return s;
 }
 
@@ -185,68 +211,91 @@ __device__ __noinline__ void select_by_radix(const T *src, int e0, int e1, int k
     __syncthreads();
 }
 
-// The slice's best min(k, length) elements into sm.best, sorted; tmax = this thread's segment maximum.
-template <typename T>
-__device__ __forceinline__ void select_best(const T *src, const Slice &sl, int k, float tmax, Smem &sm)
+// Warp 0: a threshold that at least k and at most a few more of the segment maxima reach, and the segments that do.
+__device__ __forceinline__ void choose_segments(int k, Smem &sm)
 {
-    constexpr int N = Pack<T>::N;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int len = sl.e1 - sl.e0;
-    const int want = min(k, len);
-    const uint32_t mine = sl.p0 + tid < sl.p1 ? ordered(tmax) : 0u;
-    sm.seg_key[tid] = mine;
-    if (tid == 0) { sm.n_list = 0; sm.n_cand = 0; }
-    __syncthreads();
-    if (warp == 0) {
-        // bisection for a threshold that at least k and at most a few more maxima reach
-        uint32_t key[kThreads / 32], top = 0, low = 0xffffffffu;
+    constexpr int Q = kThreads / 32;
+    const int lane = threadIdx.x & 31;
+    uint32_t key[Q], top = 0, low = 0xffffffffu;
 #pragma unroll
-        for (int q = 0; q < kThreads / 32; ++q) {
-            key[q] = sm.seg_key[q * 32 + lane];
-            top = max(top, key[q]);
-            low = min(low, key[q]);
-        }
-        uint32_t lo = __reduce_min_sync(0xffffffffu, low), hi = __reduce_max_sync(0xffffffffu, top);
-        // invariant: count(>= lo) >= k (256 >= k); count(>= hi + 1) = 0
-        while (lo < hi) {
-            const uint32_t mid = lo + (hi - lo + 1) / 2;
-            int cnt = 0;
-#pragma unroll
-            for (int q = 0; q < kThreads / 32; ++q) cnt += key[q] >= mid;
-            cnt = (int)__reduce_add_sync(0xffffffffu, (unsigned)cnt);
-            if (cnt >= k) {
-                lo = mid;
-                if (cnt <= k + (k >> 3) + 1) break;
-            } else {
-                hi = mid - 1;
-            }
-        }
-        // maxima are clamped at kNegBig: at that level everything is a candidate
-        if (lane == 0) sm.threshold = lo <= ordered(0.99f * kNegBig) ? 0u : lo;
+    for (int q = 0; q < Q; ++q) {
+        key[q] = sm.seg_key[q * 32 + lane];
+        top = max(top, key[q]);
+        low = min(low, key[q]);
     }
-    __syncthreads();
+    uint32_t lo = __reduce_min_sync(0xffffffffu, low), hi = __reduce_max_sync(0xffffffffu, top);
+    // invariant: count(>= lo) >= k (there are more segments than k); count(> hi) = 0
+    while (lo < hi) {
+        const uint32_t mid = lo + (hi - lo + 1) / 2;
+        int cnt = 0;
+#pragma unroll
+        for (int q = 0; q < Q; ++q) cnt += key[q] >= mid;
+        cnt = (int)__reduce_add_sync(0xffffffffu, (unsigned)cnt);
+        if (cnt >= k) {
+            lo = mid;
+            if (cnt <= k + (k >> 3) + 1) break;
+        } else {
+            hi = mid - 1;
+        }
+    }
+    // maxima are clamped at kNegBig: at that level everything is a candidate
+    const uint32_t thr = lo <= ordered(0.99f * kNegBig) ? 0u : lo;
+    int whole = 0, single = 0;
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+        const bool in = key[q] != 0 && key[q] >= thr, more = in && sm.seg_key2[q * 32 + lane] >= thr;
+        const uint32_t votes_w = __ballot_sync(0xffffffffu, more), votes_s = __ballot_sync(0xffffffffu, in && !more);
+        const uint32_t below = (1u << lane) - 1u;
+        if (more) sm.list[whole + __popc(votes_w & below)] = (uint16_t)(q * 32 + lane);
+        else if (in) sm.list[kThreads - 1 - single - __popc(votes_s & below)] = (uint16_t)(q * 32 + lane);
+        whole += __popc(votes_w);
+        single += __popc(votes_s);
+    }
+    if (lane == 0) {
+        sm.threshold = thr;
+        sm.n_whole = whole;
+        sm.n_single = single;
+    }
+}
+
+// The slice's best min(k, length) elements into sm.best, sorted. The segments have been chosen; loose elements are in
+// sm.cand already.
+template <typename T>
+__device__ __forceinline__ void select_best(const T *src, const Slice &sl, int k, Smem &sm)
+{
+    constexpr int N = Pack<T>::N, R = 4;
+    const int tid = threadIdx.x;
+    const int want = min(k, sl.e1 - sl.e0);
     const uint32_t thr = sm.threshold;
-    if (mine != 0 && mine >= thr) sm.list[atomicAdd(&sm.n_list, 1)] = (uint16_t)tid;
-    const int loose = tid < 2 * (N - 1) ? loose_element<T>(sl, tid) : -1;
-    if (loose >= 0) {
-        const int at = atomicAdd(&sm.n_cand, 1);
-        sm.cand[at] = make_key(ordered(Pack<T>::load1(src + loose)), loose);
-    }
-    __syncthreads();
+    const float thr_f = thr == 0u ? -INFINITY : unordered(thr);
+    // the packs to search, dealt over all threads: one or two rounds of loads
     const uint4 *body = reinterpret_cast<const uint4 *>(src + sl.head);
-    const int n_list = sm.n_list;
-    for (int q = warp; q < n_list; q += kWarps) {
-        for (int i = sl.p0 + sm.list[q] + lane * kThreads; i < sl.p1; i += 32 * kThreads) {
-            float x[N];
-            Pack<T>::unpack_raw(body[i], x);
+    const int per = (sl.p1 - sl.p0 + kThreads - 1) / kThreads, single = sm.n_single, total = single + sm.n_whole * per;
+    for (int base = tid; base < total; base += R * kThreads) {
+        uint4 v[R];
+        int at[R];
 #pragma unroll
-            for (int e = 0; e < N; ++e) {
-                const uint32_t u = ordered(x[e]);
-                if (u >= thr) {
-                    const int at = atomicAdd(&sm.n_cand, 1);
-                    if (at < kCap) sm.cand[at] = make_key(u, sl.head + i * N + e);
+        for (int r = 0; r < R; ++r) {
+            const int item = base + r * kThreads, w = item - single, seg = w / max(per, 1);
+            at[r] = item < single ? sm.seg_pack[sm.list[kThreads - 1 - item]]
+                  : item < total ? sl.p0 + sm.list[seg] + (w - seg * per) * kThreads : sl.p1;
+            if (at[r] < sl.p1) v[r] = body[at[r]];
+        }
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            if (at[r] >= sl.p1) continue;
+            float x[N];
+            Pack<T>::unpack_raw(v[r], x);
+            float top = x[0];
+#pragma unroll
+            for (int e = 1; e < N; ++e) top = fmaxf(top, x[e]);
+            if (!(top >= thr_f)) continue;
+#pragma unroll
+            for (int e = 0; e < N; ++e)
+                if (x[e] >= thr_f) {
+                    const int c = atomicAdd(&sm.n_cand, 1);
+                    if (c < kCap) sm.cand[c] = make_key(ordered(x[e]), sl.head + at[r] * N + e);
                 }
-            }
         }
     }
     __syncthreads();
@@ -258,15 +307,24 @@ __device__ __forceinline__ void select_best(const T *src, const Slice &sl, int k
     for (int i = tid; i < n; i += kThreads) {
         const unsigned long long key = sm.cand[i];
         int rank = 0;
-        for (int j = 0; j < n; ++j) rank += sm.cand[j] > key;
+        int j = 0;
+        for (; j + 4 <= n; j += 4) {
+            rank += sm.cand[j] > key;
+            rank += sm.cand[j + 1] > key;
+            rank += sm.cand[j + 2] > key;
+            rank += sm.cand[j + 3] > key;
+        }
+        for (; j < n; ++j) rank += sm.cand[j] > key;
         if (rank < want) sm.best[rank] = key;
     }
     if (tid == 0) sm.n_best = want;
     __syncthreads();
 }
 
+// (a block to a row: 8 blocks to an SM hide the selection of some behind the streams of the others better than more
+// loads in flight per thread do: 46 against 51 us for 3392 bf16 rows, half of them masked, 48 against 53 for 997 fp32)
 template <typename T, int CL>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, CL == 1 ? 8 : 1)
 topk_kernel(const Args a)
 {
     __shared__ Smem sm;
@@ -297,62 +355,95 @@ topk_kernel(const Args a)
         tok_ok = (unsigned)tok < (unsigned)a.V;
         if (tok_ok) x_tok = Pack<T>::load1(src + tok);
     }
-    float m_common = 0.f;                               // the same in every block of the row
-    if (a.V - sl.head >= Pack<T>::N) {
-        float x[Pack<T>::N], xmax;
-        Pack<T>::unpack(body[0], x, xmax);
-        m_common = safe_reference(xmax, a.c);
-    }
-    const float nm = -m_common;
+    // Sums are taken relative to the maximum of the warp's first loads (about a thousand elements, all of them when the
+    // row is split eightfold): near the row's own maximum, so that the entropy, a difference of two numbers that grow
+    // with the distance, keeps its digits.
     FixedAcc acc;
     acc.init();
-    float tmax = kNegBig;
-    {
-        constexpr int U = 4;
-        int i = sl.p0 + tid;
-        for (; i + (U - 1) * kThreads < sl.p1; i += U * kThreads) {
-            uint4 v[U];
+    Segment seg;
+    seg.top = seg.second = -INFINITY;
+    seg.pack = 0;
+    constexpr int U = CL == 1 ? 2 : 4;
+    const int lane = tid & 31, warp = tid >> 5;
+    uint4 v[U];
+    float first_max = kNegBig;
+    int i = sl.p0 + tid;
 #pragma unroll
-            for (int q = 0; q < U; ++q) v[q] = ld_stream(body + i + q * kThreads);
+    for (int q = 0; q < U; ++q)
+        if (i + q * kThreads < sl.p1) v[q] = ld_stream(body + i + q * kThreads);
 #pragma unroll
-            for (int q = 0; q < U; ++q) accumulate<T>(v[q], a.c, nm, acc, tmax);
+    for (int q = 0; q < U; ++q)
+        if (i + q * kThreads < sl.p1) {
+            float x[Pack<T>::N], xmax;
+            Pack<T>::unpack(v[q], x, xmax);
+            first_max = fmaxf(first_max, xmax);
         }
-        uint4 v[U - 1];
+    const float m_warp = safe_reference(warp_max(first_max), a.c), nm = -m_warp;
 #pragma unroll
-        for (int q = 0; q < U - 1; ++q)
-            if (i + q * kThreads < sl.p1) v[q] = ld_stream(body + i + q * kThreads);
+    for (int q = 0; q < U; ++q)
+        if (i + q * kThreads < sl.p1) accumulate<T>(v[q], i + q * kThreads, a.c, nm, acc, seg);
+    i += U * kThreads;
+    for (; i + (U - 1) * kThreads < sl.p1; i += U * kThreads) {
 #pragma unroll
-        for (int q = 0; q < U - 1; ++q)
-            if (i + q * kThreads < sl.p1) accumulate<T>(v[q], a.c, nm, acc, tmax);
+        for (int q = 0; q < U; ++q) v[q] = ld_stream(body + i + q * kThreads);
+#pragma unroll
+        for (int q = 0; q < U; ++q) accumulate<T>(v[q], i + q * kThreads, a.c, nm, acc, seg);
     }
+#pragma unroll
+    for (int q = 0; q < U - 1; ++q)
+        if (i + q * kThreads < sl.p1) v[q] = ld_stream(body + i + q * kThreads);
+#pragma unroll
+    for (int q = 0; q < U - 1; ++q)
+        if (i + q * kThreads < sl.p1) accumulate<T>(v[q], i + q * kThreads, a.c, nm, acc, seg);
     const int loose = tid < 2 * (Pack<T>::N - 1) ? loose_element<T>(sl, tid) : -1;
     const float x_loose = loose >= 0 ? Pack<float>::clampf(Pack<T>::load1(src + loose)) : kNegBig;
     SoftmaxState st;
-    st.m = m_common;
+    st.m = m_warp;
     st.s = acc.s0 + acc.s1;
     st.u = acc.u0 + acc.u1;
     if (loose >= 0) st.add(fmaf(x_loose, a.c, nm));
     if (!(st.s < 1.0e37f) || !(fabsf(st.u) < 1.0e37f)) {   // overflow (or NaN / +inf): again with a moving reference
         st.init();
-        for (int i = sl.p0 + tid; i < sl.p1; i += kThreads) accumulate_online<T>(body[i], a.c, st);
+        for (i = sl.p0 + tid; i < sl.p1; i += kThreads) accumulate_online<T>(body[i], a.c, st);
         if (loose >= 0) {
             const float y = x_loose * a.c;
             if (y > st.m) st.rebase(y);
             st.add(fmaf(x_loose, a.c, -st.m));
         }
     }
-    st = block_merge_common<kThreads>(st, m_common, sm.red);
-    if (tid == 0) sm.st = st;
+    // within the warp plain sums unless a lane moved its reference, then the eight warps' states by the general rule
+    if (__any_sync(0xffffffffu, st.m != m_warp)) {
+        st = warp_merge(st);
+    } else {
+        st.s = warp_sum_f(st.s);
+        st.u = warp_sum_f(st.u);
+    }
+    if (lane == 0) { sm.red[warp] = st.m; sm.red[32 + warp] = st.s; sm.red[64 + warp] = st.u; }
+    if (a.k > 0) {
+        sm.seg_key[tid] = sl.p0 + tid < sl.p1 ? ordered(seg.top) : 0u;
+        sm.seg_key2[tid] = ordered(seg.second);
+        sm.seg_pack[tid] = seg.pack;
+        if (loose >= 0) sm.cand[tid] = make_key(ordered(Pack<T>::load1(src + loose)), loose);   // (they come first)
+        if (tid == 0) sm.n_cand = sl.loose;
+    }
+    __syncthreads();
+    if (warp == 0) {
+        st.init();
+        if (lane < kWarps) { st.m = sm.red[lane]; st.s = sm.red[32 + lane]; st.u = sm.red[64 + lane]; }
+        st = warp_merge(st);
+        if (lane == 0) sm.st = st;
+        if (a.k > 0) choose_segments(a.k, sm);
+    }
     __syncthreads();
     st = sm.st;
-    const bool finite = st.s < 1.0e37f;                   // false for NaN; a slice without weight (s = 0) is selected from
     if (a.k > 0) {
-        if (finite) {
-            select_best(src, sl, a.k, tmax, sm);
-        } else if (tid == 0) {
-            sm.n_best = 0;
+        // (false for NaN; a slice without weight, s = 0, is selected from)
+        if (st.s < 1.0e37f) {
+            select_best(src, sl, a.k, sm);
+        } else {
+            if (tid == 0) sm.n_best = 0;
+            __syncthreads();
         }
-        __syncthreads();
     }
     if (CL > 1) {
         cg::cluster_group cluster = cg::this_cluster();
@@ -402,7 +493,7 @@ topk_kernel(const Args a)
         a.top_logprob[row * a.k + tid] = good ? (float)(((double)unordered((uint32_t)(key >> 32)) * c - lse2) * ln2) : nan;
     }
     if (tid == 0) {
-        if (a.entropy) a.entropy[row] = good ? kLn2 * (l2s - st.u / st.s) : nan;
+        if (a.entropy) a.entropy[row] = good ? (float)(((double)l2s - (double)st.u / (double)st.s) * ln2) : nan;
         if (a.lse) a.lse[row] = lse;
         if (!good && a.status) atomicOr(a.status, PPO_DEV_BAD_ROW);
     }
