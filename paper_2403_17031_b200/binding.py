@@ -556,15 +556,10 @@ def logprob_entropy_pair(policy_logits, ref_logits, tokens, temperature: float, 
 TOPK_MAX = 128
 
 
-def _call(name: str, first: torch.Tensor, tensors, *args):
-    """One entry point on the device of `first` and that device's current stream (the last argument). `tensors`: the other
-    tensors of the call; all have to be on that device. Small calls are bound by this side of the boundary, so pointers
-    are passed as plain ints and the stream comes straight from the C layer."""
-    at = first.get_device()
-    for t in tensors:
-        if t is not None and t.get_device() != at:
-            raise TypeError("%s: tensors on %s and %s" % (name, first.device, t.device))
-    fn = getattr(_lib or lib(), name)
+def _call(fn_name: str, at: int, *args):
+    """One entry point on device `at` and that device's current stream (the last argument). Small calls are bound by this
+    side of the boundary, so pointers are passed as plain ints and the stream comes straight from the C layer."""
+    fn = getattr(_lib or lib(), fn_name)
     stream = torch._C._cuda_getCurrentRawStream(at)
     if at == torch._C._cuda_getDevice():
         rc = fn(*args, stream)
@@ -572,49 +567,45 @@ def _call(name: str, first: torch.Tensor, tensors, *args):
         with torch.cuda.device(at):
             rc = fn(*args, stream)
     if rc != 0:
-        raise PPOError(name, rc)
+        raise PPOError(fn_name, rc)
 
 
-def _addr(t: Optional[torch.Tensor], dtype, name: str):
-    """Address of a contiguous CUDA tensor of the given dtype, or None."""
+def _addr(t: Optional[torch.Tensor], dtype, at: int, name: str):
+    """Address of a contiguous tensor of the given dtype on device `at`, or None."""
     if t is None:
         return None
-    if not t.is_cuda or not t.is_contiguous() or t.dtype != dtype:
+    if t.dtype != dtype or t.get_device() != at or not t.is_contiguous():
         _ptr(t, dtype, name)                       # says what is wrong
+        raise TypeError("%s must be on the device of the call's first tensor, got %s" % (name, t.device))
     return t.data_ptr()
-
-
-def _raw(t: Optional[torch.Tensor]):
-    return None if t is None else t.data_ptr()
 
 
 def _rows_of(t: torch.Tensor, name: str):
     """(rows, V, row pitch) of a CUDA tensor [..., V] whose rows are contiguous: contiguous as a whole, or 2-D."""
     if not t.is_cuda:
         raise TypeError("%s must be a CUDA tensor" % name)
-    V = t.shape[-1] if t.dim() else 0
+    shape = t.shape
+    V = shape[-1] if shape else 0
     rows = t.numel() // V if V else 0
     if t.is_contiguous():
         return rows, V, V
-    if t.dim() != 2 or (t.stride(1) != 1 and V > 1):
+    if len(shape) != 2 or (t.stride(1) != 1 and V > 1):
         raise TypeError("%s rows must be contiguous" % name)
     return rows, V, max(t.stride(0), V) if rows <= 1 else t.stride(0)
 
 
-def _per_row(t: Optional[torch.Tensor], rows: int, dtype, name: str) -> int:
-    """Entries per row of a contiguous [rows, n] array (0 when absent)."""
+def _count(t: Optional[torch.Tensor], rows: int, per_row, name: str) -> int:
+    """Entries per row of a [rows, n] array (0 when absent); per_row: what it has to be (None: whatever it is)."""
     if t is None:
-        return 0
-    if rows and t.numel() % rows:
-        raise ValueError("%s has %d entries for %d rows" % (name, t.numel(), rows))
-    _addr(t, dtype, name)
-    return t.numel() // rows if rows else 0
-
-
-def _one_per_row(t: Optional[torch.Tensor], rows: int, dtype, name: str):
-    if t is not None and t.numel() != rows:
-        raise ValueError("%s has %d entries for %d rows" % (name, t.numel(), rows))
-    return _addr(t, dtype, name)
+        n = 0
+    else:
+        total = t.numel()
+        n = total // rows if rows else 0
+        if n * rows != total:
+            raise ValueError("%s has %d entries for %d rows" % (name, total, rows))
+    if per_row is not None and t is not None and rows and n != per_row:
+        raise ValueError("%s needs %d entries per row, not %d" % (name, per_row, n))
+    return n
 
 
 def logprob_topk(logits: torch.Tensor, tokens: Optional[torch.Tensor], k: int, temperature: float,
@@ -623,24 +614,25 @@ def logprob_topk(logits: torch.Tensor, tokens: Optional[torch.Tensor], k: int, t
     tokens [...] or [..., n] int32, or None. Returns dict(logprob (shape of tokens) | None, entropy, lse [...],
     top_ids, top_logprob [..., k] | None); `out`: the same dict with the tensors to write to."""
     rows, V, stride = _rows_of(logits, "logits")
-    lead = logits.shape[:-1]
-    i32, f32 = torch.int32, torch.float32
-    n = _per_row(tokens, rows, i32, "tokens")
+    at, i32, f32 = logits.get_device(), torch.int32, torch.float32
+    n = _count(tokens, rows, None, "tokens")
+    _count(mask, rows, 1, "mask")
     if out is None:
-        dev = logits.device
-        out = {"logprob": None if tokens is None else torch.empty(tokens.shape, dtype=f32, device=dev),
-               "entropy": torch.empty(lead, dtype=f32, device=dev), "lse": torch.empty(lead, dtype=f32, device=dev),
-               "top_ids": torch.empty((*lead, k), dtype=i32, device=dev) if k > 0 else None,
-               "top_logprob": torch.empty((*lead, k), dtype=f32, device=dev) if k > 0 else None}
-    lp, ent, lse, ids, tlp = (out.get(name) for name in ("logprob", "entropy", "lse", "top_ids", "top_logprob"))
-    # (without rows there is nothing to count)
-    if rows and (n != _per_row(lp, rows, f32, "logprob") or k != _per_row(ids, rows, i32, "top_ids") or
-                 k != _per_row(tlp, rows, f32, "top_logprob")):
-        raise ValueError("logprob needs %d and top_ids / top_logprob need %d entries per row" % (n, k))
-    _call("ppo_logprob_topk", logits, (tokens, mask, lp, ent, lse, ids, tlp, workspace), logits.data_ptr(),
-          _logits_dtype(logits), rows, V, stride, _raw(tokens), n, _one_per_row(mask, rows, torch.uint8, "mask"),
-          float(temperature), int(k), _raw(lp), _one_per_row(ent, rows, f32, "entropy"), _one_per_row(lse, rows, f32, "lse"),
-          _raw(ids), _raw(tlp), _raw(workspace))
+        lead = logits.shape[:-1]
+        empty = logits.new_empty
+        entropy = empty(lead, dtype=f32)
+        ids = empty((*lead, k), dtype=i32) if k > 0 else None
+        out = {"logprob": None if tokens is None else empty(tokens.shape, dtype=f32), "entropy": entropy,
+               "lse": torch.empty_like(entropy), "top_ids": ids,
+               "top_logprob": torch.empty_like(ids, dtype=f32) if k > 0 else None}
+    else:
+        for name, per_row in (("logprob", n), ("entropy", 1), ("lse", 1), ("top_ids", k), ("top_logprob", k)):
+            _count(out.get(name), rows, per_row, name)
+    get = out.get
+    _call("ppo_logprob_topk", at, logits.data_ptr(), _logits_dtype(logits), rows, V, stride, _addr(tokens, i32, at, "tokens"), n,
+          _addr(mask, torch.uint8, at, "mask"), temperature, k, _addr(get("logprob"), f32, at, "logprob"),
+          _addr(get("entropy"), f32, at, "entropy"), _addr(get("lse"), f32, at, "lse"), _addr(get("top_ids"), i32, at, "top_ids"),
+          _addr(get("top_logprob"), f32, at, "top_logprob"), _addr(workspace, torch.uint8, at, "workspace"))
     return out
 
 
@@ -651,22 +643,25 @@ def logprob_topk_bwd(logits: torch.Tensor, lse: torch.Tensor, temperature: float
     dtop_logprob come in pairs [..., n] and [..., k] (each pair optional; the alternatives may be another model's);
     lse, and entropy where dentropy is given, are the forward call's. Returns dict(dlogits)."""
     rows, V, stride = _rows_of(logits, "logits")
-    i32, f32 = torch.int32, torch.float32
-    n, k = _per_row(tokens, rows, i32, "tokens"), _per_row(top_ids, rows, i32, "top_ids")
-    if n != _per_row(dlogprob, rows, f32, "dlogprob") or k != _per_row(dtop_logprob, rows, f32, "dtop_logprob"):
-        raise ValueError("tokens / dlogprob and top_ids / dtop_logprob need the same number of entries")
+    at, i32, f32 = logits.get_device(), torch.int32, torch.float32
+    n, k = _count(tokens, rows, None, "tokens"), _count(top_ids, rows, None, "top_ids")
+    if (tokens is None) != (dlogprob is None) or (top_ids is None) != (dtop_logprob is None):
+        raise ValueError("tokens / dlogprob and top_ids / dtop_logprob come in pairs")
+    for t, per_row, name in ((dlogprob, n, "dlogprob"), (dtop_logprob, k, "dtop_logprob"), (lse, 1, "lse"), (entropy, 1, "entropy"),
+                             (dentropy, 1, "dentropy"), (dlse, 1, "dlse"), (mask, 1, "mask")):
+        _count(t, rows, per_row, name)
     if dlogits is None:
-        dlogits = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
-    drows, dV, dstride = _rows_of(dlogits, "dlogits")
-    if (drows, dV) != (rows, V) or dlogits.dtype != logits.dtype:
-        raise TypeError("dlogits must have the shape and dtype of the logits")
-    _call("ppo_logprob_topk_bwd", logits, (tokens, dlogprob, top_ids, dtop_logprob, lse, entropy, dentropy, dlse, mask, dlogits,
-                                           workspace),
-          logits.data_ptr(), _logits_dtype(logits), rows, V, stride, _raw(tokens), n, _raw(dlogprob),
-          _raw(top_ids), k, _raw(dtop_logprob), _one_per_row(lse, rows, f32, "lse"),
-          _one_per_row(entropy, rows, f32, "entropy"), _one_per_row(dentropy, rows, f32, "dentropy"),
-          _one_per_row(dlse, rows, f32, "dlse"), _one_per_row(mask, rows, torch.uint8, "mask"), float(temperature),
-          dlogits.data_ptr(), dstride, _raw(workspace))
+        dlogits = logits.new_empty(logits.shape)
+        dstride = V
+    else:
+        drows, dV, dstride = _rows_of(dlogits, "dlogits")
+        if (drows, dV) != (rows, V) or dlogits.dtype != logits.dtype or dlogits.get_device() != at:
+            raise TypeError("dlogits must have the shape, dtype and device of the logits")
+    _call("ppo_logprob_topk_bwd", at, logits.data_ptr(), _logits_dtype(logits), rows, V, stride, _addr(tokens, i32, at, "tokens"), n,
+          _addr(dlogprob, f32, at, "dlogprob"), _addr(top_ids, i32, at, "top_ids"), k, _addr(dtop_logprob, f32, at, "dtop_logprob"),
+          _addr(lse, f32, at, "lse"), _addr(entropy, f32, at, "entropy"), _addr(dentropy, f32, at, "dentropy"),
+          _addr(dlse, f32, at, "dlse"), _addr(mask, torch.uint8, at, "mask"), temperature, dlogits.data_ptr(), dstride,
+          _addr(workspace, torch.uint8, at, "workspace"))
     return {"dlogits": dlogits}
 
 
@@ -676,54 +671,59 @@ def fp8_quantize(x: torch.Tensor, block_rows: int = 1, transpose: bool = False, 
     q has a row pitch of a multiple of 16 bytes. `out`: (q, scales) to write to."""
     if x.dim() != 2:
         raise TypeError("x must be a matrix")
-    rows, cols, stride = _rows_of(x, "x")
-    rows = x.shape[0]
-    R, Cc = (cols, rows) if transpose else (rows, cols)
+    _, _, stride = _rows_of(x, "x")
+    at, f8 = x.get_device(), torch.float8_e4m3fn
+    Cc, R = x.shape if transpose else x.shape[::-1]
     kb = -(-Cc // 128)
     shape = (kb, R) if block_rows == 1 else (-(-R // 128), kb)
     if out is None:
-        q = torch.empty((R, -(-Cc // 16) * 16), dtype=torch.float8_e4m3fn, device=x.device)[:, :Cc]
-        out = (q, torch.empty(shape, dtype=torch.float32, device=x.device))
-    q, scales = out
-    if tuple(scales.shape) != shape:
-        raise ValueError("scales must have shape %s" % (shape,))
-    qp, ldq = _fp8_operand(q, "q")
-    if tuple(q.shape) != (R, Cc):
-        raise ValueError("q must have shape %s" % ((R, Cc),))
-    _call("ppo_fp8_quantize", x, (q, scales), x.data_ptr(), _logits_dtype(x), R, Cc, stride, 1 if transpose else 0,
-          int(block_rows), qp, ldq, _addr(scales, torch.float32, "scales"))
+        ldq = -(-Cc // 16) * 16
+        q = x.new_empty((R, ldq), dtype=f8)
+        out = (q if ldq == Cc else q[:, :Cc], x.new_empty(shape, dtype=torch.float32))
+        q, scales = out
+    else:
+        q, scales = out
+        if q.shape != (R, Cc) or scales.shape != shape:
+            raise ValueError("q must have shape %s, scales %s" % ((R, Cc), shape))
+        _, ldq = _fp8_operand(q, at, "q")
+    _call("ppo_fp8_quantize", at, x.data_ptr(), _logits_dtype(x), R, Cc, stride, 1 if transpose else 0, block_rows, q.data_ptr(),
+          ldq, _addr(scales, torch.float32, at, "scales"))
     return out
 
 
-def _fp8_operand(t: torch.Tensor, name: str):
-    """(pointer, row pitch in bytes) of an 8-bit matrix with contiguous rows."""
-    if not t.is_cuda or t.dim() != 2 or t.dtype != torch.float8_e4m3fn:
-        raise TypeError("%s must be a CUDA matrix of float8_e4m3fn" % name)
-    if t.shape[1] > 1 and t.stride(1) != 1:
+def _fp8_operand(t: torch.Tensor, at: int, name: str):
+    """(address, row pitch in bytes) of an 8-bit matrix with contiguous rows."""
+    if t.dtype != torch.float8_e4m3fn or t.dim() != 2 or t.get_device() != at or not t.is_cuda:
+        raise TypeError("%s must be a CUDA matrix of float8_e4m3fn on one device with the others" % name)
+    rows, cols = t.shape
+    s0, s1 = t.stride()
+    if cols > 1 and s1 != 1:
         raise TypeError("%s rows must be contiguous" % name)
     # (the stride of a single row is anyone's choice)
-    pitch = -(-t.shape[1] // 16) * 16 if t.shape[0] <= 1 else t.stride(0)
-    return t.data_ptr(), pitch
+    return t.data_ptr(), s0 if rows > 1 else -(-cols // 16) * 16
 
 
 def fp8_matmul(a: torch.Tensor, a_scales: torch.Tensor, b: torch.Tensor, b_scales: torch.Tensor, block_n: int = 128,
                out_dtype: torch.dtype = torch.bfloat16, workspace: Optional[torch.Tensor] = None, out=None):
     """[M, N] = a [M, K] . b [N, K]^T of two block-scaled 8-bit matrices (fp8_quantize): a_scales [ceil(K/128), M],
     b_scales [ceil(N/128), ceil(K/128)] (block_n 128) or [ceil(K/128), N] (block_n 1). Result in bf16 or fp32."""
-    ap, lda = _fp8_operand(a, "a")
-    bp, ldb = _fp8_operand(b, "b")
-    (M, K), (N, K2) = a.shape, b.shape
-    if K != K2:
+    at, f32 = a.get_device(), torch.float32
+    ap, lda = _fp8_operand(a, at, "a")
+    bp, ldb = _fp8_operand(b, at, "b")
+    M, K = a.shape
+    N = b.shape[0]
+    if K != b.shape[1]:
         raise ValueError("a [M,K] and b [N,K] disagree on K")
     kb = -(-K // 128)
-    if tuple(a_scales.shape) != (kb, M) or tuple(b_scales.shape) != ((kb, N) if block_n == 1 else (-(-N // 128), kb)):
+    if a_scales.shape != (kb, M) or b_scales.shape != ((kb, N) if block_n == 1 else (-(-N // 128), kb)):
         raise ValueError("scales do not fit the operands' blocks")
     if out is None:
-        out = torch.empty((M, N), dtype=out_dtype, device=a.device)
-    if out.dim() != 2 or tuple(out.shape) != (M, N):
-        raise ValueError("out must have shape %s" % ((M, N),))
-    _, _, ldc = _rows_of(out, "out")
-    _call("ppo_fp8_matmul", a, (a_scales, b, b_scales, out, workspace), ap, lda, _addr(a_scales, torch.float32, "a_scales"), bp,
-          ldb, _addr(b_scales, torch.float32, "b_scales"), int(block_n), M, N, K, out.data_ptr(),
-          _logits_dtype(out), ldc, _raw(workspace))
+        out = a.new_empty((M, N), dtype=out_dtype)
+        ldc = N
+    else:
+        if out.shape != (M, N) or out.get_device() != at:
+            raise ValueError("out must have shape %s, on the operands' device" % ((M, N),))
+        _, _, ldc = _rows_of(out, "out")
+    _call("ppo_fp8_matmul", at, ap, lda, _addr(a_scales, f32, at, "a_scales"), bp, ldb, _addr(b_scales, f32, at, "b_scales"), block_n,
+          M, N, K, out.data_ptr(), _logits_dtype(out), ldc, _addr(workspace, torch.uint8, at, "workspace"))
     return out
