@@ -39,7 +39,7 @@ __device__ __forceinline__ void wait_alive(bool &alive, unsigned long long *bar,
     if (alive) alive = wait(bar, parity, status);
 }
 
-constexpr int kNarrowStages = 6, kNarrowBufs = 2, kNarrowThreads = 192;
+constexpr int kNarrowStages = 4, kNarrowBufs = 2, kNarrowThreads = 192;
 
 template <int MT>
 struct NarrowSmem {
@@ -51,6 +51,26 @@ struct NarrowSmem {
 template <int MT> __host__ __device__ constexpr int narrow_stage_bytes() { return (128 + MT) * kBlockK; }
 // accumulator columns: a power of two, at least 32
 template <int MT> __host__ __device__ constexpr uint32_t narrow_columns() { return kNarrowBufs * MT < 32 ? 32 : kNarrowBufs * MT; }
+
+// four neighbouring results of row m; vec: all of them inside, at an aligned address
+__device__ __forceinline__ void store4(const Args &a, int m, int n, const float4 &v, bool vec)
+{
+    if (m >= a.M) return;
+    const float x[4] = {v.x, v.y, v.z, v.w};
+    if (a.out_f32) {
+        float *to = reinterpret_cast<float *>(a.out) + (int64_t)m * a.ldc + n;
+        if (vec) *reinterpret_cast<float4 *>(to) = v;
+        else
+            for (int e = 0; e < 4 && n + e < a.N; ++e) to[e] = x[e];
+    } else {
+        __nv_bfloat16 *to = reinterpret_cast<__nv_bfloat16 *>(a.out) + (int64_t)m * a.ldc + n;
+        if (vec) {
+            const __nv_bfloat162 lo = __floats2bfloat162_rn(x[0], x[1]), hi = __floats2bfloat162_rn(x[2], x[3]);
+            *reinterpret_cast<uint2 *>(to) = make_uint2(*reinterpret_cast<const uint32_t *>(&lo), *reinterpret_cast<const uint32_t *>(&hi));
+        } else
+            for (int e = 0; e < 4 && n + e < a.N; ++e) to[e] = __float2bfloat16_rn(x[e]);
+    }
+}
 
 template <int MT>
 __global__ void __launch_bounds__(kNarrowThreads)
@@ -189,14 +209,22 @@ narrow_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__
         }
         cluster.sync();
         if (warp >= 2) {
-            for (int j = rank; j < MT; j += split) {
-                float v = 0.f;
-                for (int r = 0; r < split; ++r) v += cluster.map_shared_rank(part, r)[j * 128 + nl];
-                const int m = m0 + j;
-                if (m < a.M && n < a.N) {
-                    if (a.out_f32) reinterpret_cast<float *>(a.out)[(int64_t)m * a.ldc + n] = v;
-                    else reinterpret_cast<__nv_bfloat16 *>(a.out)[(int64_t)m * a.ldc + n] = __float2bfloat16_rn(v);
+            // columns rank, rank + split, ... of the tile; a warp takes every fourth of them, a lane four rows of B, and
+            // the remote loads of two columns are under way together
+            const int r4 = lane * 4;
+            const bool vec = n0 + 128 <= a.N && (reinterpret_cast<uintptr_t>(a.out) & 15u) == 0 && (a.ldc & 3) == 0;
+            for (int j0 = rank + q * split; j0 < MT; j0 += 8 * split) {
+                const int j1 = j0 + 4 * split;
+                float4 v0 = make_float4(0.f, 0.f, 0.f, 0.f), v1 = v0;
+                for (int r = 0; r < split; ++r) {
+                    const float *from = cluster.map_shared_rank(part, r);
+                    const float4 x0 = *reinterpret_cast<const float4 *>(from + j0 * 128 + r4);
+                    const float4 x1 = *reinterpret_cast<const float4 *>(from + (j1 < MT ? j1 : j0) * 128 + r4);
+                    v0.x += x0.x; v0.y += x0.y; v0.z += x0.z; v0.w += x0.w;
+                    v1.x += x1.x; v1.y += x1.y; v1.z += x1.z; v1.w += x1.w;
                 }
+                store4(a, m0 + j0, n0 + r4, v0, vec);
+                if (j1 < MT) store4(a, m0 + j1, n0 + r4, v1, vec);
             }
         }
         cluster.sync();
@@ -212,6 +240,9 @@ narrow_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__
     }
 }
 
+// blocks that fit on the SMs at once, by their shared memory (73, 81 and 97 KB)
+template <int MT> constexpr int narrow_places() { return (MT == 16 ? 3 : 2) * 148; }
+
 template <int MT>
 static int launch_narrow(Args a, const void *A, int64_t lda, const void *B, int64_t ldb, int64_t K, cudaStream_t s)
 {
@@ -223,8 +254,9 @@ static int launch_narrow(Args a, const void *A, int64_t lda, const void *B, int6
     a.m_tiles = (a.M + MT - 1) / MT;
     a.n_tiles = (a.N + 127) / 128;
     const int64_t tiles = (int64_t)a.m_tiles * a.n_tiles;
+    // blocks of a tile's cluster: as many as fit on the SMs at once, each with two blocks of K or more
     int split = 1;
-    while (split < 8 && tiles * split < 2 * 148 && a.kb_total >= 4 * split) split *= 2;
+    while (split < 8 && tiles * split * 2 <= narrow_places<MT>() && a.kb_total >= 4 * split) split *= 2;
     if (tiles * split >= ((int64_t)1 << 31)) return PPO_ERR_SHAPE;
     const size_t smem = (size_t)kNarrowStages * narrow_stage_bytes<MT>() + 1024;
     PPO_RETURN_IF_CUDA(cudaFuncSetAttribute(narrow_kernel<MT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
@@ -641,6 +673,11 @@ extern "C" int ppo_fp8_matmul(const void *A, int64_t lda, const float *a_scales,
     a.status = workspace ? &ws_header(workspace)->status : nullptr;
     cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
     if (M <= 16) return fp8::launch_narrow<16>(a, A, lda, B, ldb, K, s);
-    if (M <= 128) return fp8::launch_narrow<64>(a, A, lda, B, ldb, K, s);
+    if (M <= 32) return fp8::launch_narrow<32>(a, A, lda, B, ldb, K, s);
+    // The wide kernel takes about 0.5 us per block of K and tile, whatever the SMs without a tile do; while there are so
+    // few 128 x 64 tiles that two blocks or more can share the K of each, those are faster (64 x 4096 x 8192: 13 against
+    // 38 us, 200 x 4096 x 8192: 31 against 39; with a block for each: 400 x 4096 x 8192 55 against 39).
+    const int64_t tiles64 = ((M + 63) / 64) * ((N + 127) / 128);
+    if (tiles64 * 2 <= fp8::narrow_places<64>()) return fp8::launch_narrow<64>(a, A, lda, B, ldb, K, s);
     return fp8::launch_wide(a, A, lda, B, ldb, K, s);
 }
