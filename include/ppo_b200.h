@@ -491,11 +491,16 @@ int ppo_fp8_quantize(const void *x, int dtype, int64_t R, int64_t C, int64_t x_s
  * Sums are fp32: within a block on the tensor cores, over blocks in registers; each element is rounded once, and the
  * order is fixed by the sizes.  Bytes of A and B behind K in a row are not used, whatever they hold.
  *   workspace  nullable: the status word (PPO_DEV_TIMEOUT when a bounded wait ran out; C is invalid then)
+ *   scratch    nullable: ppo_fp8_scratch_bytes(M, N, K) bytes on the device, 256-byte aligned, uninitialised, for this call
+ *              alone while it runs.  Where that size is not 0, tiles that would leave most SMs idle are cut along K with it;
+ *              without it (and where the size is 0) every tile is summed by one pair of SMs.  The order of the sums, and so
+ *              the last bits, differ between the two
  * Errors: PPO_ERR_DTYPE, PPO_ERR_SHAPE, PPO_ERR_PARAM (block_n not 1 or 128), PPO_ERR_NULL, PPO_ERR_ALIGN.
  */
+size_t ppo_fp8_scratch_bytes(int64_t M, int64_t N, int64_t K);
 int ppo_fp8_matmul(const void *A, int64_t lda, const float *a_scales, const void *B, int64_t ldb,
                    const float *b_scales, int block_n, int64_t M, int64_t N, int64_t K, void *C, int out_dtype,
-                   int64_t ldc, void *workspace, void *stream);
+                   int64_t ldc, void *workspace, void *scratch, void *stream);
 
 /*
  * The whole path in one call.  ppo_step_io names every buffer of one PPO iteration over a batch of

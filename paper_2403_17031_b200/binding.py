@@ -131,7 +131,8 @@ _SIGS = {
     "ppo_fp8_quantize": (C.c_int, [C.c_void_p, C.c_int, C.c_int64, C.c_int64, C.c_int64, C.c_int, C.c_int, C.c_void_p,
                                    C.c_int64, C.c_void_p, C.c_void_p]),
     "ppo_fp8_matmul": (C.c_int, [C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_int, C.c_int64,
-                                 C.c_int64, C.c_int64, C.c_void_p, C.c_int, C.c_int64, C.c_void_p, C.c_void_p]),
+                                 C.c_int64, C.c_int64, C.c_void_p, C.c_int, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p]),
+    "ppo_fp8_scratch_bytes": (C.c_size_t, [C.c_int64, C.c_int64, C.c_int64]),
     "ppo_lmhead_logprob_entropy": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int64, C.c_int64, C.c_int64, C.c_void_p,
                                              C.c_void_p, C.c_float, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
                                              C.c_void_p]),
@@ -703,10 +704,16 @@ def _fp8_operand(t: torch.Tensor, at: int, name: str):
     return t.data_ptr(), s0 if rows > 1 else -(-cols // 16) * 16
 
 
+def fp8_scratch_bytes(M: int, N: int, K: int) -> int:
+    return int(lib().ppo_fp8_scratch_bytes(M, N, K))
+
+
 def fp8_matmul(a: torch.Tensor, a_scales: torch.Tensor, b: torch.Tensor, b_scales: torch.Tensor, block_n: int = 128,
-               out_dtype: torch.dtype = torch.bfloat16, workspace: Optional[torch.Tensor] = None, out=None):
+               out_dtype: torch.dtype = torch.bfloat16, workspace: Optional[torch.Tensor] = None, out=None,
+               scratch: Optional[torch.Tensor] = None):
     """[M, N] = a [M, K] . b [N, K]^T of two block-scaled 8-bit matrices (fp8_quantize): a_scales [ceil(K/128), M],
-    b_scales [ceil(N/128), ceil(K/128)] (block_n 128) or [ceil(K/128), N] (block_n 1). Result in bf16 or fp32."""
+    b_scales [ceil(N/128), ceil(K/128)] (block_n 128) or [ceil(K/128), N] (block_n 1). Result in bf16 or fp32.
+    scratch: at least fp8_scratch_bytes(M, N, K) bytes (uint8); allocated here where the call can use it and none is given."""
     at, f32 = a.get_device(), torch.float32
     ap, lda = _fp8_operand(a, at, "a")
     bp, ldb = _fp8_operand(b, at, "b")
@@ -724,6 +731,12 @@ def fp8_matmul(a: torch.Tensor, a_scales: torch.Tensor, b: torch.Tensor, b_scale
         if out.shape != (M, N) or out.get_device() != at:
             raise ValueError("out must have shape %s, on the operands' device" % ((M, N),))
         _, _, ldc = _rows_of(out, "out")
+    need = fp8_scratch_bytes(M, N, K) if kb >= 48 else 0          # (none for a shorter K, whatever M and N)
+    if need and scratch is None:
+        scratch = a.new_empty(need, dtype=torch.uint8)
+    if scratch is not None and scratch.numel() < need:
+        raise ValueError("fp8_matmul needs %d bytes of scratch (fp8_scratch_bytes)" % need)
     _call("ppo_fp8_matmul", at, ap, lda, _addr(a_scales, f32, at, "a_scales"), bp, ldb, _addr(b_scales, f32, at, "b_scales"), block_n,
-          M, N, K, out.data_ptr(), _logits_dtype(out), ldc, _addr(workspace, torch.uint8, at, "workspace"))
+          M, N, K, out.data_ptr(), _logits_dtype(out), ldc, _addr(workspace, torch.uint8, at, "workspace"),
+          _addr(scratch, torch.uint8, at, "scratch"))
     return out

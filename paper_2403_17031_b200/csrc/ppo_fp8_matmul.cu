@@ -278,26 +278,31 @@ static int launch_narrow(Args a, const void *A, int64_t lda, const void *B, int6
 // ---------------------------------------------------------------- wide kernel
 // Rows of A are the lanes of the accumulator tile, 256 rows of B its columns. Two blocks on two SMs work as a pair on a
 // 256 x 256 tile: one matrix instruction spans both tensor cores, each block loads its 128 rows of A and 128 of the 256
-// rows of B and keeps 128 result rows, so that a block of K costs an SM 32 KB of loads instead of 48 (alone on a
-// 128 x 256 tile the tensor core waited for its operands: 957 cycles per block of K where its arithmetic needs 512).
-// One persistent pair per two SMs, 384 threads a block: warp 0 = TMA producer (6 stages of 32 KB), warps 1 and 3
-// of the leader = MMA issuers (two accumulators of 256 columns, one block of K each), warps 4-11 = epilogue: warp (q, h) owns lanes 32 q .. and columns 128 h .., i.e. thread = one row and
-// one 128-column block of sb, so its factor is a single product sa * sb per block of K and the join is a packed fp32
-// multiply-add per two elements out of tensor memory. Finished tiles go through shared memory so that rows leave in
-// 128-byte runs.
+// rows of B and keeps 128 result rows. One persistent pair per two SMs, 768 threads a block:
+//   warp 0      TMA producer (4 stages of 32 KB)
+//   warp 1      scales, a group of blocks of K ahead of the epilogue (their latency is several blocks of K)
+//   warps 4-7   of the leader: MMA issuers, one for each of four accumulators (half of the columns, one block of K)
+//   warps 8-23  epilogue: warp (q, c) owns lanes 32 q .. and columns 64 c .., i.e. a thread holds 64 results of one row
+//               and needs one factor sa * sb per block of K; the join is a packed fp32 multiply-add per two elements
+// Bounds: with few tiles the hand-over of accumulators (from the end of a product to the start of the next one into the
+// same accumulator lie about 1200 cycles of commits, barrier waits, which cost 100 to 200 cycles each even when they are
+// over, fences and reads; two accumulators per half hide half of it: 0.52 us per block of K and tile); with many, the
+// board's power limit: at 27136 x 50304 x 4096 a block of K takes 925 cycles, but the clock falls to 1.35 GHz. Compared
+// under that load: blocks alone on 128 x 256 tiles 7.3 ms, pairs 6.4 ms; 256 x 192 tiles, whose accumulators can be released
+// before anything is multiplied, 6.6 ms; one issuer instead of four 9 ms; 256-column accumulators 6.6 ms.
 constexpr int kBM = 128, kBN = 256, kPairM = 2 * kBM, kWideStages = 4, kWideThreads = 768;
-constexpr int kWideHalf = 128 * kBlockK, kWideStage = 2 * kWideHalf;     // a block's half of A, of B
+constexpr int kWideA = kBM * kBlockK, kWideB = kBN / 2 * kBlockK, kWideStage = kWideA + kWideB;   // a block's halves of A and B
 constexpr int kStageOut = 32 * 128;        // per epilogue warp: 32 rows x 128 bytes
-constexpr int kEpiWarps = 16;
-// blocks of K whose scales are handed over together (two groups in flight), and floats of one block: sa[128], sb
+constexpr int kEpiWarps = 4 * (kBN / 64);
+// blocks of K whose scales are handed over together (two groups in flight), and floats of one block: sa[128], sb (those of
+// the two 128-row blocks of B, or of each row)
 template <bool PER_ROW> struct Scales {
     static constexpr int kGroup = PER_ROW ? 4 : 16, kFloats = kBM + (PER_ROW ? kBN : 4), kBytes = 2 * kGroup * kFloats * 4;
 };
 constexpr int kScaleBytes = Scales<false>::kBytes > Scales<true>::kBytes ? Scales<false>::kBytes : Scales<true>::kBytes;
 constexpr int kWideSmem = kWideStages * kWideStage + kEpiWarps * kStageOut + kScaleBytes + 1024;
 static_assert(kWideSmem <= 232448 - 1024, "shared memory of a block");
-
-static_assert(kWideStages % 2 == 0, "the two issuers take turns");
+static_assert(kWideThreads == (8 + kEpiWarps) * 32 && kWideStage % 1024 == 0 && kWideA % 1024 == 0, "layout");
 
 struct WideSmem {
     unsigned long long full[kWideStages], empty[kWideStages], tmem_full[2][2];   // [half][accumulator]
@@ -306,9 +311,50 @@ struct WideSmem {
     uint32_t tmem_base;
 };
 
+// The pairs take tiles 0 .. n_whole in turn, whole. With `share` > 0 the other tiles, too few for all pairs, are cut along
+// K: end to end they are n_rest * kb_total blocks of K, of which pair c takes share, from c * share on. Such a pair leaves
+// its sums of a tile in the scratch buffer (at most two tiles), and join_kernel adds them up in the order of the pairs.
 struct WideArgs {
     Args a;
-    int gm, gn, n_units, bulk_out;   // bulk_out: rows of C are 16-byte aligned
+    int gm, gn, n_whole, n_rest, share, bulk_out;   // bulk_out: rows of C are 16-byte aligned
+    float *scratch;
+};
+
+constexpr int kTileFloats = kPairM * kBN;
+
+struct Piece {
+    int u, kb0, kb1;      // tile, blocks of K
+    int part;             // -1: whole; else which of the pair's sums in the scratch buffer
+    int u_next, r, r_end;
+    __device__ __forceinline__ void init(const WideArgs &w, int pair, int kbs)
+    {
+        u_next = pair;
+        r = min(pair * w.share, w.n_rest * kbs);
+        r_end = min(r + w.share, w.n_rest * kbs);
+        part = -1;
+    }
+    __device__ __forceinline__ bool next(const WideArgs &w, int pairs, int kbs)
+    {
+        if (u_next < w.n_whole) {
+            u = u_next;
+            u_next += pairs;
+            kb0 = 0;
+            kb1 = kbs;
+            return true;
+        }
+        if (r >= r_end) return false;
+        const int t = r / kbs;
+        u = w.n_whole + t;
+        kb0 = r - t * kbs;
+        kb1 = min(kbs, kb0 + r_end - r);
+        r += kb1 - kb0;
+        ++part;
+        return true;
+    }
+    __device__ __forceinline__ uint32_t blocks(const WideArgs &w, int pair, int pairs, int kbs) const   // of all pieces
+    {
+        return (uint32_t)(pair < w.n_whole ? (w.n_whole - pair + pairs - 1) / pairs : 0) * (uint32_t)kbs + (uint32_t)(r_end - r);
+    }
 };
 
 // unit -> output tile: blocks of gm x gn tiles (m fastest inside), column of blocks by column of blocks; a block's
@@ -386,7 +432,7 @@ wide_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
         for (int b = 0; b < 2; ++b) {
             for (int g = 0; g < 2; ++g) {
                 barrier_init(&sm.tmem_full[g][b], 1);
-                barrier_init(&sm.pair_empty[g][b], kEpiWarps);
+                barrier_init(&sm.pair_empty[g][b], kEpiWarps);  // half of each block's warps
             }
             barrier_init(&sm.scale_full[b], 1);
             barrier_init(&sm.scale_empty[b], kEpiWarps);
@@ -400,17 +446,19 @@ wide_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem_base = sm.tmem_base;
     const int kbs = a.kb_total;
-    const int rank = (int)cluster_rank(), first = blockIdx.x / 2, step = gridDim.x / 2;
+    const int rank = (int)cluster_rank(), pair = blockIdx.x / 2, pairs = gridDim.x / 2;
+    Piece piece;
+    piece.init(w, pair, kbs);
 
-    // registers of the first eight warps go to the accumulators: 256 x 32 + 512 x 104 = 768 x 80
+    // registers of the first eight warps go to the epilogue: 256 x 32 + 512 x 104 = 768 x 80
     if (warp < 8) asm volatile("setmaxnreg.dec.sync.aligned.u32 32;");
     if (warp == 0) {
         if (lane == 0) {
             bool alive = true;
             uint32_t it = 0, s = 0, parity = 1;                 // (waiting for the phase before the first returns at once)
-            for (int u = first; u < w.n_units && alive; u += step) {
-                const int2 t = tile_of(u, a.m_tiles, a.n_tiles, w.gm, w.gn);
-                for (int kb = 0; kb < kbs; ++kb, ++it) {
+            while (alive && piece.next(w, pairs, kbs)) {
+                const int2 t = tile_of(piece.u, a.m_tiles, a.n_tiles, w.gm, w.gn);
+                for (int kb = piece.kb0; kb < piece.kb1; ++kb, ++it) {
                     wait_alive(alive, &sm.empty[s], parity, a.status);
                     if (!alive) break;
                     unsigned char *stage = ring + (size_t)s * kWideStage;
@@ -420,8 +468,8 @@ wide_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
                     const uint32_t bar = leader_addr(&sm.full[s]);
                     tma_load_2d_pair(stage, &map_a, kb * kBlockK, t.x * kPairM + rank * kBM, bar);
                     // of the 128 columns of each half, 64 rows of B come from either block
-                    tma_load_2d_pair(stage + kWideHalf, &map_b, kb * kBlockK, t.y * kBN + rank * 64, bar);
-                    tma_load_2d_pair(stage + kWideHalf + kWideHalf / 2, &map_b, kb * kBlockK, t.y * kBN + 128 + rank * 64, bar);
+                    tma_load_2d_pair(stage + kWideA, &map_b, kb * kBlockK, t.y * kBN + rank * 64, bar);
+                    tma_load_2d_pair(stage + kWideA + kWideB / 2, &map_b, kb * kBlockK, t.y * kBN + 128 + rank * 64, bar);
                     if (++s == kWideStages) { s = 0; parity ^= 1; }
                 }
             }
@@ -432,16 +480,13 @@ wide_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
         }
         __syncwarp();
     } else if (warp >= 4 && warp < 8) {
-        // One issuer per accumulator. Its two waits hold an issuing thread for up to 170 cycles each even when they are
-        // over, and the hand-over of an accumulator to the epilogue and back takes about 900 cycles besides the work on
-        // it: four accumulators of 128 columns, two per half, keep the tensor cores busy meanwhile. No order is needed
-        // between them.
+        // One issuer per accumulator: while one waits, the others' products run. No order is needed between them.
         if (rank == 0) {
-            constexpr uint32_t idesc = instr_desc_e4m3(kPairM, 128);
+            constexpr uint32_t idesc = instr_desc_e4m3(kPairM, kBN / 2);
             const uint32_t g = warp & 1, buf = (warp >> 1) & 1;
             const uint64_t desc0 = smem_desc(saddr(ring), 16, 1024);
-            const uint32_t total = (uint32_t)((w.n_units - first + step - 1) / step) * (uint32_t)kbs;
-            const uint32_t tmem_d = tmem_base + buf * kBN + g * 128;
+            const uint32_t total = piece.blocks(w, pair, pairs, kbs);
+            const uint32_t tmem_d = tmem_base + buf * kBN + g * (kBN / 2);
             bool alive = true;
             uint32_t s = buf, s_parity = 0, b_parity = 1;
             for (uint32_t it = buf; it < total; it += 2) {
@@ -449,7 +494,7 @@ wide_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
                 wait_alive(alive, &sm.pair_empty[g][buf], b_parity, a.status);
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 // rows 64 g .. of either block's 128 rows of B
-                const uint64_t ad = desc0 + s * (kWideStage >> 4), bd = ad + ((kWideHalf + g * (kWideHalf / 2)) >> 4);
+                const uint64_t ad = desc0 + s * (kWideStage >> 4), bd = ad + ((kWideA + g * (kWideB / 2)) >> 4);
                 if (elect_one()) {
 #pragma unroll
                     for (int kk = 0; kk < kBlockK / 32; ++kk) mma_f8_pair(tmem_d, ad + kk * 2, bd + kk * 2, idesc, kk ? 1u : 0u);
@@ -464,17 +509,16 @@ wide_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
         }
         __syncwarp();
     } else if (warp == 1) {
-        // scales: their latency is several blocks of K, so they are fetched a group ahead of the epilogue
         bool alive = true;
         uint32_t g = 0, parity = 1;
-        for (int u = first; u < w.n_units; u += step) {
-            const int2 t = tile_of(u, a.m_tiles, a.n_tiles, w.gm, w.gn);
+        while (piece.next(w, pairs, kbs)) {
+            const int2 t = tile_of(piece.u, a.m_tiles, a.n_tiles, w.gm, w.gn);
             const int m0 = t.x * kPairM + rank * kBM, n0 = t.y * kBN;
-            for (int kb0 = 0; kb0 < kbs; kb0 += kGroup) {
+            for (int kb0 = piece.kb0; kb0 < piece.kb1; kb0 += kGroup) {
                 wait_alive(alive, &sm.scale_empty[g], parity, a.status);
                 __syncwarp();
                 float *to = scales + g * kGroupFloats;
-                for (int kb = kb0; kb < min(kb0 + kGroup, kbs); ++kb, to += kFloats) {
+                for (int kb = kb0; kb < min(kb0 + kGroup, piece.kb1); ++kb, to += kFloats) {
                     const float *pa = a.sa + (int64_t)kb * a.M;
 #pragma unroll
                     for (int j = lane; j < kBM; j += 32) copy4(to + j, m0 + j < a.M ? pa + m0 + j : a.sa, m0 + j < a.M);
@@ -482,9 +526,10 @@ wide_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
                         const float *pb = a.sb + (int64_t)kb * a.N;
 #pragma unroll
                         for (int j = lane; j < kBN; j += 32) copy4(to + kBM + j, n0 + j < a.N ? pb + n0 + j : a.sb, n0 + j < a.N);
-                    } else if (lane < kBN / 128) {
-                        const bool in = n0 + lane * 128 < a.N;
-                        copy4(to + kBM + lane, in ? a.sb + (int64_t)(n0 / 128 + lane) * kbs + kb : a.sb, in);
+                    } else if (lane < 2) {
+                        const int blk = n0 / 128 + lane;
+                        const bool in = blk * 128 < a.N;
+                        copy4(to + kBM + lane, in ? a.sb + (int64_t)blk * kbs + kb : a.sb, in);
                     }
                 }
                 asm volatile("cp.async.wait_all;" ::: "memory");
@@ -502,18 +547,18 @@ wide_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
         const uint32_t pair_empty0 = leader_addr(&sm.pair_empty[h][0]), pair_empty1 = leader_addr(&sm.pair_empty[h][1]);
         bool alive = true, ready = false;                       // ready: the next accumulator is known to be there
         uint32_t buf = 0, parity = 0, g = 0, g_parity = 0;
-        for (int u = first; u < w.n_units; u += step) {
+        while (piece.next(w, pairs, kbs)) {
             float2 acc[32];
 #pragma unroll
             for (int j = 0; j < 32; ++j) acc[j] = make_float2(0.f, 0.f);
             const float *slot = scales;
             int left = 0;                                       // blocks of K left in the group of scales
 #pragma unroll 1
-            for (int kb = 0; kb < kbs; ++kb) {
+            for (int kb = piece.kb0; kb < piece.kb1; ++kb) {
                 if (left == 0) {
                     wait_alive(alive, &sm.scale_full[g], g_parity, a.status);
                     slot = scales + g * kGroupFloats;
-                    left = min(kGroup, kbs - kb);
+                    left = min(kGroup, piece.kb1 - kb);
                 }
                 const float f = PER_ROW ? slot[q * 32 + lane] : slot[q * 32 + lane] * slot[kBM + h];
                 const float *sbs = slot + kBM + c64 * 64;       // PER_ROW: this warp's 64 factors
@@ -548,9 +593,17 @@ wide_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
                     g ^= 1;
                 }
             }
+            const int2 t = tile_of(piece.u, a.m_tiles, a.n_tiles, w.gm, w.gn);
+            const int n = t.y * kBN + c64 * 64;
+            const int m_warp = t.x * kPairM + rank * kBM + q * 32;
+            if (piece.part >= 0) {                              // a part of the tile's sum
+                float *to = w.scratch + (size_t)(pair * 2 + piece.part) * kTileFloats + (rank * kBM + q * 32 + lane) * kBN + c64 * 64;
+#pragma unroll
+                for (int j = 0; j < 16; ++j)
+                    reinterpret_cast<float4 *>(to)[j] = make_float4(acc[j * 2].x, acc[j * 2].y, acc[j * 2 + 1].x, acc[j * 2 + 1].y);
+                continue;
+            }
             // the tile: 64 bf16 or 32 fp32 columns at a time through shared memory, 16-byte piece c of row r at c ^ (r & 7)
-            const int2 t = tile_of(u, a.m_tiles, a.n_tiles, w.gm, w.gn);
-            const int m_warp = t.x * kPairM + rank * kBM + q * 32, n = t.y * kBN + c64 * 64;
             unsigned char *row = stage + lane * 128;
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
@@ -597,22 +650,91 @@ wide_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
     }
 }
 
-static int launch_wide(Args a, const void *A, int64_t lda, const void *B, int64_t ldb, int64_t K, cudaStream_t s)
+// The tiles that were cut along K: a thread adds up four neighbouring results over the pairs that hold parts of them, in
+// the order of K.
+constexpr int kJoinThreads = 256;
+__global__ void __launch_bounds__(kJoinThreads)
+join_kernel(const WideArgs w)
+{
+    const Args &a = w.a;
+    constexpr int kBlocks = kTileFloats / 4 / kJoinThreads;    // per tile
+    const int rest = blockIdx.x / kBlocks, at = (blockIdx.x % kBlocks) * kJoinThreads + threadIdx.x;
+    const int2 t = tile_of(w.n_whole + rest, a.m_tiles, a.n_tiles, w.gm, w.gn);
+    const int m = t.x * kPairM + at / (kBN / 4), n = t.y * kBN + at % (kBN / 4) * 4;
+    if (m >= a.M || n >= a.N) return;
+    const int first = rest * a.kb_total / w.share, last = ((rest + 1) * a.kb_total - 1) / w.share;
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int c = first; c <= last; ++c) {
+        const int part = rest - c * w.share / a.kb_total;       // the pair's first or second tile
+        const float4 x = reinterpret_cast<const float4 *>(w.scratch + (size_t)(c * 2 + part) * kTileFloats)[at];
+        v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
+    }
+    const bool vec = n + 4 <= a.N && (reinterpret_cast<uintptr_t>(a.out) & 15u) == 0 && (a.ldc & 3) == 0;
+    store4(a, m, n, v, vec);
+}
+
+static int pairs_of_device(int *pairs)
+{
+    int dev = 0, sms = 148;
+    PPO_RETURN_IF_CUDA(cudaGetDevice(&dev));
+    PPO_RETURN_IF_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
+    *pairs = sms / 2;
+    return PPO_OK;
+}
+
+// Tiles left over by the last full round of the pairs are cut along K when that saves each pair 48 blocks of K or more
+// (about 0.3 us each, against a second launch and a pass over the parts).
+struct WidePlan {
+    int m_tiles, n_tiles, n_whole, n_rest, share;
+};
+
+static WidePlan wide_plan(int64_t M, int64_t N, int kbs, int pairs)
+{
+    WidePlan p;
+    p.m_tiles = (int)((M + kPairM - 1) / kPairM);
+    p.n_tiles = (int)((N + kBN - 1) / kBN);
+    const int64_t units = (int64_t)p.m_tiles * p.n_tiles;
+    p.n_whole = (int)units;
+    p.n_rest = p.share = 0;
+    const int rest = (int)(units % pairs);
+    const int64_t share = ((int64_t)rest * kbs + pairs - 1) / pairs;
+    if (rest > 0 && kbs - share >= 48 && units < ((int64_t)1 << 30)) {
+        p.n_rest = rest;
+        p.n_whole = (int)units - rest;
+        p.share = (int)share;
+    }
+    return p;
+}
+
+static size_t wide_scratch_bytes(const WidePlan &p, int pairs) { return p.share ? (size_t)pairs * 2 * kTileFloats * 4 : 0; }
+
+static int launch_wide(Args a, const void *A, int64_t lda, const void *B, int64_t ldb, int64_t K, float *scratch, cudaStream_t s)
 {
     CUtensorMap ma, mb;
     int rc = make_map_8bit(&ma, A, (uint64_t)K, (uint64_t)a.M, (uint64_t)lda, kBM);
     if (rc) return rc;
     rc = make_map_8bit(&mb, B, (uint64_t)K, (uint64_t)a.N, (uint64_t)ldb, 64);
     if (rc) return rc;
-    a.m_tiles = (a.M + kPairM - 1) / kPairM;
-    a.n_tiles = (a.N + kBN - 1) / kBN;
-    const int64_t units = (int64_t)a.m_tiles * a.n_tiles;
+    int pairs = 0;
+    rc = pairs_of_device(&pairs);
+    if (rc) return rc;
+    WidePlan p = wide_plan(a.M, a.N, a.kb_total, pairs);
+    if (!scratch) {                                             // whole tiles only
+        p.n_whole += p.n_rest;
+        p.n_rest = p.share = 0;
+    }
+    const int64_t units = (int64_t)p.m_tiles * p.n_tiles;
     if (units >= ((int64_t)1 << 30)) return PPO_ERR_SHAPE;
+    a.m_tiles = p.m_tiles;
+    a.n_tiles = p.n_tiles;
     WideArgs w = {};
     w.a = a;
     w.gm = 5;
     w.gn = 16;
-    w.n_units = (int)units;
+    w.n_whole = p.n_whole;
+    w.n_rest = p.n_rest;
+    w.share = p.share;
+    w.scratch = scratch;
     const int64_t pitch = a.ldc * (a.out_f32 ? 4 : 2);
     w.bulk_out = reinterpret_cast<uintptr_t>(a.out) % 16 == 0 && pitch % 16 == 0 && pitch < ((int64_t)1 << 40);
     CUtensorMap mc = {};
@@ -620,13 +742,10 @@ static int launch_wide(Args a, const void *A, int64_t lda, const void *B, int64_
         rc = make_map_out(&mc, a.out, a.out_f32 != 0, (uint64_t)a.N, (uint64_t)a.M, (uint64_t)pitch, 32);
         if (rc) return rc;
     }
-    int dev = 0, sms = 148;
-    PPO_RETURN_IF_CUDA(cudaGetDevice(&dev));
-    PPO_RETURN_IF_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
     auto kern = a.per_row ? wide_kernel<true> : wide_kernel<false>;
     PPO_RETURN_IF_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kWideSmem));
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(2 * (w.n_units < sms / 2 ? w.n_units : sms / 2)));
+    cfg.gridDim = dim3((unsigned)(2 * (p.share || units > pairs ? pairs : (int)units)));
     cfg.blockDim = dim3(kWideThreads);
     cfg.dynamicSmemBytes = kWideSmem;
     cfg.stream = s;
@@ -637,7 +756,19 @@ static int launch_wide(Args a, const void *A, int64_t lda, const void *B, int64_
     cfg.attrs = attr;
     cfg.numAttrs = 1;
     PPO_RETURN_IF_CUDA(cudaLaunchKernelEx(&cfg, kern, ma, mb, mc, w));
-    return PPO_OK;
+    if (!p.share) return PPO_OK;
+    join_kernel<<<p.n_rest * (kTileFloats / 4 / kJoinThreads), kJoinThreads, 0, s>>>(w);
+    return launch_status();
+}
+
+// Rows of A in a tile of the narrow kernel, or 0 for the wide one. The wide kernel takes its time per block of K and tile
+// whatever the SMs without a tile do; while there are so few 128 x 64 tiles that two blocks or more can share the K of
+// each, those are faster (64 x 4096 x 8192: 13 against 38 us, 200 x 4096 x 8192: 27 against 39; with a block for each:
+// 400 x 4096 x 8192 55 against 39).
+static int narrow_rows(int64_t M, int64_t N)
+{
+    if (M <= 32) return M <= 16 ? 16 : 32;
+    return ((M + 63) / 64) * ((N + 127) / 128) * 2 <= narrow_places<64>() ? 64 : 0;
 }
 
 }   // namespace fp8
@@ -645,9 +776,21 @@ static int launch_wide(Args a, const void *A, int64_t lda, const void *B, int64_
 
 using namespace ppo;
 
+extern "C" size_t ppo_fp8_scratch_bytes(int64_t M, int64_t N, int64_t K)
+{
+    const int64_t limit = ((int64_t)1 << 31) - 512;
+    if (M <= 0 || N <= 0 || K <= 0 || M >= limit || N >= limit || K >= limit || fp8::narrow_rows(M, N)) return 0;
+    int pairs = 0;
+    if (fp8::pairs_of_device(&pairs) != PPO_OK) {
+        (void)cudaGetLastError();
+        pairs = 74;
+    }
+    return fp8::wide_scratch_bytes(fp8::wide_plan(M, N, (int)((K + 127) / 128), pairs), pairs);
+}
+
 extern "C" int ppo_fp8_matmul(const void *A, int64_t lda, const float *a_scales, const void *B, int64_t ldb,
                               const float *b_scales, int block_n, int64_t M, int64_t N, int64_t K, void *C,
-                              int out_dtype, int64_t ldc, void *workspace, void *stream)
+                              int out_dtype, int64_t ldc, void *workspace, void *scratch, void *stream)
 {
     if (out_dtype != PPO_F32 && out_dtype != PPO_BF16) return PPO_ERR_DTYPE;
     const int64_t limit = ((int64_t)1 << 31) - 512;
@@ -658,7 +801,7 @@ extern "C" int ppo_fp8_matmul(const void *A, int64_t lda, const float *a_scales,
     if (M == 0) return PPO_OK;
     if (!A || !a_scales || !B || !b_scales || !C) return PPO_ERR_NULL;
     if (reinterpret_cast<uintptr_t>(A) % 16 || reinterpret_cast<uintptr_t>(B) % 16 ||
-        reinterpret_cast<uintptr_t>(C) % (out_dtype == PPO_F32 ? 4 : 2))
+        reinterpret_cast<uintptr_t>(C) % (out_dtype == PPO_F32 ? 4 : 2) || reinterpret_cast<uintptr_t>(scratch) % 256)
         return PPO_ERR_ALIGN;
     fp8::Args a = {};
     a.M = (int)M;
@@ -672,12 +815,10 @@ extern "C" int ppo_fp8_matmul(const void *A, int64_t lda, const float *a_scales,
     a.out_f32 = out_dtype == PPO_F32;
     a.status = workspace ? &ws_header(workspace)->status : nullptr;
     cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-    if (M <= 16) return fp8::launch_narrow<16>(a, A, lda, B, ldb, K, s);
-    if (M <= 32) return fp8::launch_narrow<32>(a, A, lda, B, ldb, K, s);
-    // The wide kernel takes about 0.5 us per block of K and tile, whatever the SMs without a tile do; while there are so
-    // few 128 x 64 tiles that two blocks or more can share the K of each, those are faster (64 x 4096 x 8192: 13 against
-    // 38 us, 200 x 4096 x 8192: 31 against 39; with a block for each: 400 x 4096 x 8192 55 against 39).
-    const int64_t tiles64 = ((M + 63) / 64) * ((N + 127) / 128);
-    if (tiles64 * 2 <= fp8::narrow_places<64>()) return fp8::launch_narrow<64>(a, A, lda, B, ldb, K, s);
-    return fp8::launch_wide(a, A, lda, B, ldb, K, s);
+    switch (fp8::narrow_rows(M, N)) {
+    case 16: return fp8::launch_narrow<16>(a, A, lda, B, ldb, K, s);
+    case 32: return fp8::launch_narrow<32>(a, A, lda, B, ldb, K, s);
+    case 64: return fp8::launch_narrow<64>(a, A, lda, B, ldb, K, s);
+    }
+    return fp8::launch_wide(a, A, lda, B, ldb, K, reinterpret_cast<float *>(scratch), s);
 }

@@ -106,6 +106,27 @@ def test_matmul_matches_oracle(P, out_dtype, M, N, K, block_n):
     _check_matmul(P, M, N, K, block_n, out_dtype)
 
 
+@pytest.mark.parametrize("out_dtype,block_n", [(F32, 128), (BF16, 1)])
+@pytest.mark.parametrize("M,N,K", [(600, 2000, 12000), (257, 15000, 15400), (2600, 4100, 13200)])
+def test_matmul_with_tiles_cut_along_k(P, M, N, K, out_dtype, block_n):
+    """Sizes whose last round of tiles is shared by all pairs of SMs: with scratch and without, and bit for bit twice."""
+    assert P.fp8_scratch_bytes(M, N, K) > 0
+    a, sa, b, sb = _operands(P, M, N, K, block_n)
+    got = P.fp8_matmul(a, sa, b, sb, block_n, out_dtype)
+    scratch = torch.empty(P.fp8_scratch_bytes(M, N, K), dtype=torch.uint8, device="cuda").fill_(255)
+    out = torch.full((M, N + 1), 3.0, dtype=out_dtype, device="cuda")
+    again = P.fp8_matmul(a, sa, b, sb, block_n, out_dtype, out=out[:, :N], scratch=scratch)     # (rows at odd addresses)
+    assert torch.equal(got, again) and (out[:, N:] == 3.0).all()
+    cols = torch.cat([torch.arange(0, 130), torch.arange(N - 140, N)])
+    w, size = O.matmul(npy(a.float()), npy(sa), npy(b.float())[cols], npy(sb)[:, cols] if block_n == 1 else
+                       np.repeat(npy(sb), 128, axis=0)[cols].T.copy(), 1)
+    gamma = (128 + -(-K // 128) + 3) * 2.0 ** -23
+    err = np.abs(got[:, cols.cuda()].double().cpu().numpy() - w) - torch.finfo(out_dtype).eps / 2 * np.abs(w) - gamma * size
+    assert (err <= 0).all(), int((err > 0).sum())
+    with pytest.raises(ValueError):
+        P.fp8_matmul(a, sa, b, sb, block_n, out_dtype, scratch=scratch[256:])
+
+
 def test_matmul_results_do_not_depend_on_bytes_behind_k_or_on_the_pitch(P):
     M, N, K = 150, 260, 200
     a, sa, b, sb = _operands(P, M, N, K, 128)

@@ -58,11 +58,11 @@ def test_quantize_refusals(b):
 
 
 def test_matmul_refusals(b):
-    # A lda sa | B ldb sb block_n | M N K C out ldc ws stream
-    ok = [P(FAKE), 256, P(FAKE), P(FAKE), 256, P(FAKE), 128, 4, 100, 256, P(FAKE), b.PPO_BF16, 100, None, None]
+    # A lda sa | B ldb sb block_n | M N K C out ldc ws scratch stream
+    ok = [P(FAKE), 256, P(FAKE), P(FAKE), 256, P(FAKE), 128, 4, 100, 256, P(FAKE), b.PPO_BF16, 100, None, None, None]
     _codes(b.lib().ppo_fp8_matmul, ok, [
         (11, 3, -5), (7, -1, -2), (8, 0, -2), (9, 0, -2), (9, 257, -2), (1, 250, -2), (1, 264, -2), (4, 264, -2), (4, 240, -2),
-        (12, 99, -2), (7, (1 << 31) - 1, -2), (6, 64, -3), (0, None, -1), (2, None, -1), (3, None, -1), (5, None, -1),
+        (12, 99, -2), (14, P(FAKE + 16), -4), (7, (1 << 31) - 1, -2), (6, 64, -3), (0, None, -1), (2, None, -1), (3, None, -1), (5, None, -1),
         (10, None, -1), (0, P(FAKE + 8), -4), (3, P(FAKE + 8), -4), (10, P(FAKE + 1), -4), (7, 0, 0)])
 
 
