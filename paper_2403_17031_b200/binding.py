@@ -731,7 +731,7 @@ def fp8_matmul(a: torch.Tensor, a_scales: torch.Tensor, b: torch.Tensor, b_scale
         if out.shape != (M, N) or out.get_device() != at:
             raise ValueError("out must have shape %s, on the operands' device" % ((M, N),))
         _, _, ldc = _rows_of(out, "out")
-    need = fp8_scratch_bytes(M, N, K) if kb >= 48 else 0          # (none for a shorter K, whatever M and N)
+    need = fp8_scratch_bytes(M, N, K) if kb > 24 else 0            # (none for a shorter K, whatever M and N)
     if need and scratch is None:
         scratch = a.new_empty(need, dtype=torch.uint8)
     if scratch is not None and scratch.numel() < need:

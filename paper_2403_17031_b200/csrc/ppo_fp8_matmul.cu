@@ -449,6 +449,7 @@ wide_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
     const int rank = (int)cluster_rank(), pair = blockIdx.x / 2, pairs = gridDim.x / 2;
     Piece piece;
     piece.init(w, pair, kbs);
+    grid_dependents_may_launch();                               // join_kernel, which waits for the end of this one
 
     // registers of the first eight warps go to the epilogue: 256 x 32 + 512 x 104 = 768 x 80
     if (warp < 8) asm volatile("setmaxnreg.dec.sync.aligned.u32 32;");
@@ -597,10 +598,12 @@ wide_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
             const int n = t.y * kBN + c64 * 64;
             const int m_warp = t.x * kPairM + rank * kBM + q * 32;
             if (piece.part >= 0) {                              // a part of the tile's sum
-                float *to = w.scratch + (size_t)(pair * 2 + piece.part) * kTileFloats + (rank * kBM + q * 32 + lane) * kBN + c64 * 64;
+                // (four columns of 256 rows follow one another: a warp writes 512 bytes at a time)
+                float4 *to = reinterpret_cast<float4 *>(w.scratch + (size_t)(pair * 2 + piece.part) * kTileFloats) +
+                             c64 * 16 * kPairM + rank * kBM + q * 32 + lane;
 #pragma unroll
                 for (int j = 0; j < 16; ++j)
-                    reinterpret_cast<float4 *>(to)[j] = make_float4(acc[j * 2].x, acc[j * 2].y, acc[j * 2 + 1].x, acc[j * 2 + 1].y);
+                    to[j * kPairM] = make_float4(acc[j * 2].x, acc[j * 2].y, acc[j * 2 + 1].x, acc[j * 2 + 1].y);
                 continue;
             }
             // the tile: 64 bf16 or 32 fp32 columns at a time through shared memory, 16-byte piece c of row r at c ^ (r & 7)
@@ -650,27 +653,42 @@ wide_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
     }
 }
 
-// The tiles that were cut along K: a thread adds up four neighbouring results over the pairs that hold parts of them, in
-// the order of K.
-constexpr int kJoinThreads = 256;
+// The tiles that were cut along K: a block adds up 32 rows x 64 columns over the pairs that hold parts of them, in the order
+// of K, and turns them in shared memory so that rows leave in runs. Launched as a dependent of the wide kernel.
+constexpr int kJoinThreads = 256, kJoinBlocks = (kPairM / 32) * (kBN / 64);
 __global__ void __launch_bounds__(kJoinThreads)
 join_kernel(const WideArgs w)
 {
+    __shared__ float4 turn[32][17];
     const Args &a = w.a;
-    constexpr int kBlocks = kTileFloats / 4 / kJoinThreads;    // per tile
-    const int rest = blockIdx.x / kBlocks, at = (blockIdx.x % kBlocks) * kJoinThreads + threadIdx.x;
+    const int rest = blockIdx.x / kJoinBlocks, part_of = blockIdx.x % kJoinBlocks;
+    const int row0 = (part_of % (kPairM / 32)) * 32, j0 = part_of / (kPairM / 32) * 16;
     const int2 t = tile_of(w.n_whole + rest, a.m_tiles, a.n_tiles, w.gm, w.gn);
-    const int m = t.x * kPairM + at / (kBN / 4), n = t.y * kBN + at % (kBN / 4) * 4;
-    if (m >= a.M || n >= a.N) return;
+    const int m0 = t.x * kPairM + row0, n0 = t.y * kBN + j0 * 4;
     const int first = rest * a.kb_total / w.share, last = ((rest + 1) * a.kb_total - 1) / w.share;
-    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    const int lane = threadIdx.x & 31, jj = threadIdx.x >> 5;
+    grid_dependency_wait();
+    if (m0 >= a.M || n0 >= a.N) return;
+    float4 v[2];
+    v[0] = v[1] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
     for (int c = first; c <= last; ++c) {
         const int part = rest - c * w.share / a.kb_total;       // the pair's first or second tile
-        const float4 x = reinterpret_cast<const float4 *>(w.scratch + (size_t)(c * 2 + part) * kTileFloats)[at];
-        v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
+        const float4 *from = reinterpret_cast<const float4 *>(w.scratch + (size_t)(c * 2 + part) * kTileFloats) + row0 + lane;
+        const float4 x = from[(j0 + jj) * kPairM], y = from[(j0 + jj + 8) * kPairM];
+        v[0].x += x.x; v[0].y += x.y; v[0].z += x.z; v[0].w += x.w;
+        v[1].x += y.x; v[1].y += y.y; v[1].z += y.z; v[1].w += y.w;
     }
-    const bool vec = n + 4 <= a.N && (reinterpret_cast<uintptr_t>(a.out) & 15u) == 0 && (a.ldc & 3) == 0;
-    store4(a, m, n, v, vec);
+    turn[lane][jj] = v[0];
+    turn[lane][jj + 8] = v[1];
+    __syncthreads();
+    const int c4 = threadIdx.x & 15;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int r = (threadIdx.x >> 4) + h * 16, n = n0 + c4 * 4;
+        const bool vec = n + 4 <= a.N && (reinterpret_cast<uintptr_t>(a.out) & 15u) == 0 && (a.ldc & 3) == 0;
+        if (n < a.N) store4(a, m0 + r, n, turn[r][c4], vec);
+    }
 }
 
 static int pairs_of_device(int *pairs)
@@ -682,8 +700,9 @@ static int pairs_of_device(int *pairs)
     return PPO_OK;
 }
 
-// Tiles left over by the last full round of the pairs are cut along K when that saves each pair 48 blocks of K or more
-// (about 0.3 us each, against a second launch and a pass over the parts).
+// Tiles left over by the last full round of the pairs are cut along K when that saves each pair 24 blocks of K or more
+// (0.3 to 0.5 us each, against about 8 us for writing and joining the parts: 600 x 2000 x 8192 37 us whole, 27 cut; with 16
+// blocks saved 2000 x 2000 x 16384 72 whole, 80 cut).
 struct WidePlan {
     int m_tiles, n_tiles, n_whole, n_rest, share;
 };
@@ -698,7 +717,7 @@ static WidePlan wide_plan(int64_t M, int64_t N, int kbs, int pairs)
     p.n_rest = p.share = 0;
     const int rest = (int)(units % pairs);
     const int64_t share = ((int64_t)rest * kbs + pairs - 1) / pairs;
-    if (rest > 0 && kbs - share >= 48 && units < ((int64_t)1 << 30)) {
+    if (rest > 0 && kbs - share >= 24 && units < ((int64_t)1 << 30)) {
         p.n_rest = rest;
         p.n_whole = (int)units - rest;
         p.share = (int)share;
@@ -757,8 +776,8 @@ static int launch_wide(Args a, const void *A, int64_t lda, const void *B, int64_
     cfg.numAttrs = 1;
     PPO_RETURN_IF_CUDA(cudaLaunchKernelEx(&cfg, kern, ma, mb, mc, w));
     if (!p.share) return PPO_OK;
-    join_kernel<<<p.n_rest * (kTileFloats / 4 / kJoinThreads), kJoinThreads, 0, s>>>(w);
-    return launch_status();
+    PPO_RETURN_IF_CUDA(launch_dependent(join_kernel, dim3((unsigned)(p.n_rest * kJoinBlocks)), dim3(kJoinThreads), 0, s, w));
+    return PPO_OK;
 }
 
 // Rows of A in a tile of the narrow kernel, or 0 for the wide one. The wide kernel takes its time per block of K and tile
