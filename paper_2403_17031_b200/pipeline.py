@@ -147,3 +147,62 @@ class DPOStep:
 
     def device_status(self) -> int:
         return _b.last_device_status(self.workspace)
+
+
+class Fp8LMHead:
+    """A frozen LM head held in 8 bits: e4m3 values with one scale per 128 x 128 of the weight (half the memory of bf16,
+    and the products run at the 8-bit rate). score() gives what step 1 needs of a model - log-probs of given tokens,
+    entropy, log-sum-exp - and the k most likely alternatives; grad_hidden() takes gradients on those back to the hidden
+    states. Hidden states and logit gradients are quantised per row and 128 columns on the way; logits are bf16.
+
+    W [K, V] (bf16 or fp32) is quantised once, [V, K] for the logits and, with backward=True, [K, V] for the gradient.
+    Buffers for M rows are kept and overwritten by the next call; everything runs on the current CUDA stream, and the
+    calls can be captured into a CUDA graph.
+    """
+
+    def __init__(self, W: torch.Tensor, M: int, k: int, temperature: float, n: int = 1, backward: bool = False):
+        K, V = W.shape
+        self.M, self.K, self.V, self.k, self.n, self.temperature = M, K, V, k, n, float(temperature)
+        dev, f32, f8 = W.device, torch.float32, torch.float8_e4m3fn
+        pitch = lambda cols: -(-cols // 16) * 16
+        operand = lambda cols: (torch.empty((M, pitch(cols)), dtype=f8, device=dev)[:, :cols],
+                                torch.empty((-(-cols // 128), M), dtype=f32, device=dev))
+        scratch = lambda N, C: torch.empty(max(_b.fp8_scratch_bytes(M, N, C), 256), dtype=torch.uint8, device=dev)
+        self.workspace = _b.new_workspace(_b.workspace_bytes(M, 1, V), dev)
+        self.weight = _b.fp8_quantize(W, 128, transpose=True)
+        self.hidden = operand(K)
+        # (rows of 16-byte multiples, whatever V is)
+        self.logits = torch.empty((M, pitch(V)), dtype=torch.bfloat16, device=dev)[:, :V]
+        self._scratch = scratch(V, K)
+        self.out = {"logprob": torch.empty((M, n), dtype=f32, device=dev), "entropy": torch.empty(M, dtype=f32, device=dev),
+                    "lse": torch.empty(M, dtype=f32, device=dev),
+                    "top_ids": torch.empty((M, k), dtype=torch.int32, device=dev) if k else None,
+                    "top_logprob": torch.empty((M, k), dtype=f32, device=dev) if k else None}
+        if backward:
+            self.weight_bwd = _b.fp8_quantize(W, 128)
+            self.dlogits = torch.empty((M, pitch(V)), dtype=torch.bfloat16, device=dev)[:, :V]
+            self.dlogits_q = operand(V)
+            self.dhidden = torch.empty((M, K), dtype=torch.bfloat16, device=dev)
+            self._scratch_bwd = scratch(K, V)
+
+    def score(self, H, tokens, mask=None):
+        """H [M, K], tokens [M] or [M, n] int32, mask [M] u8 (rows with 0 are scored as 0, ids -1). Returns the dict of
+        logprob [M, n], entropy, lse [M], top_ids, top_logprob [M, k]."""
+        _b.fp8_quantize(H, 1, out=self.hidden)
+        _b.fp8_matmul(*self.hidden, *self.weight, workspace=self.workspace, out=self.logits, scratch=self._scratch)
+        return _b.logprob_topk(self.logits, tokens, self.k, self.temperature, mask=mask, workspace=self.workspace, out=self.out)
+
+    def grad_hidden(self, tokens, dlogprob, dtop_logprob=None, dentropy=None, dlse=None, top_ids=None, mask=None):
+        """Gradients on what the last score() returned -> gradient on its hidden states [M, K] bf16. top_ids: another model's
+        alternatives (default: the ones score() found, where dtop_logprob is given)."""
+        o = self.out
+        ids = top_ids if top_ids is not None or dtop_logprob is None else o["top_ids"]
+        _b.logprob_topk_bwd(self.logits, o["lse"], self.temperature, tokens=tokens, dlogprob=dlogprob, top_ids=ids,
+                            dtop_logprob=dtop_logprob, entropy=o["entropy"], dentropy=dentropy, dlse=dlse, mask=mask,
+                            workspace=self.workspace, dlogits=self.dlogits)
+        _b.fp8_quantize(self.dlogits, 1, out=self.dlogits_q)
+        return _b.fp8_matmul(*self.dlogits_q, *self.weight_bwd, workspace=self.workspace, out=self.dhidden,
+                             scratch=self._scratch_bwd)
+
+    def device_status(self) -> int:
+        return _b.last_device_status(self.workspace)
