@@ -631,7 +631,7 @@ def logprob_topk(logits: torch.Tensor, tokens: Optional[torch.Tensor], k: int, t
             _count(out.get(name), rows, per_row, name)
     get = out.get
     _call("ppo_logprob_topk", at, logits.data_ptr(), _logits_dtype(logits), rows, V, stride, _addr(tokens, i32, at, "tokens"), n,
-          _addr(mask, torch.uint8, at, "mask"), temperature, k, _addr(get("logprob"), f32, at, "logprob"),
+          _addr(mask, torch.uint8, at, "mask"), float(temperature), int(k), _addr(get("logprob"), f32, at, "logprob"),
           _addr(get("entropy"), f32, at, "entropy"), _addr(get("lse"), f32, at, "lse"), _addr(get("top_ids"), i32, at, "top_ids"),
           _addr(get("top_logprob"), f32, at, "top_logprob"), _addr(workspace, torch.uint8, at, "workspace"))
     return out
@@ -661,7 +661,7 @@ def logprob_topk_bwd(logits: torch.Tensor, lse: torch.Tensor, temperature: float
     _call("ppo_logprob_topk_bwd", at, logits.data_ptr(), _logits_dtype(logits), rows, V, stride, _addr(tokens, i32, at, "tokens"), n,
           _addr(dlogprob, f32, at, "dlogprob"), _addr(top_ids, i32, at, "top_ids"), k, _addr(dtop_logprob, f32, at, "dtop_logprob"),
           _addr(lse, f32, at, "lse"), _addr(entropy, f32, at, "entropy"), _addr(dentropy, f32, at, "dentropy"),
-          _addr(dlse, f32, at, "dlse"), _addr(mask, torch.uint8, at, "mask"), temperature, dlogits.data_ptr(), dstride,
+          _addr(dlse, f32, at, "dlse"), _addr(mask, torch.uint8, at, "mask"), float(temperature), dlogits.data_ptr(), dstride,
           _addr(workspace, torch.uint8, at, "workspace"))
     return {"dlogits": dlogits}
 
@@ -687,7 +687,7 @@ def fp8_quantize(x: torch.Tensor, block_rows: int = 1, transpose: bool = False, 
         if q.shape != (R, Cc) or scales.shape != shape:
             raise ValueError("q must have shape %s, scales %s" % ((R, Cc), shape))
         _, ldq = _fp8_operand(q, at, "q")
-    _call("ppo_fp8_quantize", at, x.data_ptr(), _logits_dtype(x), R, Cc, stride, 1 if transpose else 0, block_rows, q.data_ptr(),
+    _call("ppo_fp8_quantize", at, x.data_ptr(), _logits_dtype(x), R, Cc, stride, 1 if transpose else 0, int(block_rows), q.data_ptr(),
           ldq, _addr(scales, torch.float32, at, "scales"))
     return out
 
@@ -736,7 +736,7 @@ def fp8_matmul(a: torch.Tensor, a_scales: torch.Tensor, b: torch.Tensor, b_scale
         scratch = a.new_empty(need, dtype=torch.uint8)
     if scratch is not None and scratch.numel() < need:
         raise ValueError("fp8_matmul needs %d bytes of scratch (fp8_scratch_bytes)" % need)
-    _call("ppo_fp8_matmul", at, ap, lda, _addr(a_scales, f32, at, "a_scales"), bp, ldb, _addr(b_scales, f32, at, "b_scales"), block_n,
-          M, N, K, out.data_ptr(), _logits_dtype(out), ldc, _addr(workspace, torch.uint8, at, "workspace"),
+    _call("ppo_fp8_matmul", at, ap, lda, _addr(a_scales, f32, at, "a_scales"), bp, ldb, _addr(b_scales, f32, at, "b_scales"),
+          int(block_n), M, N, K, out.data_ptr(), _logits_dtype(out), ldc, _addr(workspace, torch.uint8, at, "workspace"),
           _addr(scratch, torch.uint8, at, "scratch"))
     return out

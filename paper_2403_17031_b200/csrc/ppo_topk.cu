@@ -378,7 +378,10 @@ topk_kernel(const Args a)
             Pack<T>::unpack(v[q], x, xmax);
             first_max = fmaxf(first_max, xmax);
         }
-    const float m_warp = safe_reference(warp_max(first_max), a.c), nm = -m_warp;
+    const float w_max = warp_max(first_max);
+    const float m_warp = safe_reference(w_max, a.c), nm = -m_warp;
+    // (a warp whose first loads hold no logit with weight has no reference: its sums are marked as overflown)
+    if (w_max <= -1.0e29f) acc.s0 = INFINITY;
 #pragma unroll
     for (int q = 0; q < U; ++q)
         if (i + q * kThreads < sl.p1) accumulate<T>(v[q], i + q * kThreads, a.c, nm, acc, seg);

@@ -119,6 +119,28 @@ def test_topk_rows_where_selection_is_hard(P, dtype, rows_each, V):
     _check(P, base, _tokens(12 * rows_each, V, 2), 64)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,V", [(3, 50304), (40, 30001), (200, 9001), (700, 4100)])
+def test_topk_rows_far_from_zero_with_banned_stretches(P, dtype, rows, V):
+    """Logits around -400 (2^-800 of anything near 0) with the first, the last or every other thousand of them banned."""
+    x = _logits(rows, V, dtype, seed=3, scale=2.0)
+    x -= 400
+    x[0::3, :min(3000, V - 40)] = -torch.inf
+    x[1::3, -3000:-1] = torch.finfo(dtype).min
+    x[2::3] = torch.where((torch.arange(V, device="cuda") // 1000) % 2 == 0, -torch.inf, x[2::3].float()).to(dtype)
+    _check(P, x, _tokens(rows, V), 30)
+    f = P.logprob_topk(x, None, 30, TAU)
+    d = P.logprob_topk_bwd(x, f["lse"], TAU, top_ids=f["top_ids"], dtop_logprob=torch.ones(rows, 30, device="cuda"),
+                           entropy=f["entropy"], dentropy=torch.ones(rows, device="cuda"))["dlogits"]
+    assert torch.isfinite(d).all() and (d[0, :30] == 0).all()
+
+
+def test_topk_takes_numbers_of_other_kinds(P):
+    x = _logits(5, 600, F32)
+    a, b = P.logprob_topk(x, None, np.int64(3), np.float32(0.7)), P.logprob_topk(x, None, 3, float(np.float32(0.7)))
+    assert torch.equal(a["top_logprob"], b["top_logprob"])
+
+
 def test_topk_rows_without_a_distribution(P):
     x = _logits(6, 5000, F32)
     x[0, 4321] = torch.nan
