@@ -9,6 +9,8 @@
 // columns, so that a tile never holds more than 16 idle rows and the stream of B, which bounds the call, is read by
 // full 128 x 128 boxes. K is split over a cluster of blocks when there are too few tiles to occupy the SMs; the
 // partial tiles are joined through distributed shared memory in rank order, so results do not depend on timing.
+// 1 x 50304 x 4096 (206 MB of weight): 37 us = 5.6 TB/s with three blocks an SM (6 stages and two blocks: 43 us), so that all
+// 393 tiles are under way at once.
 #include <cooperative_groups.h>
 
 #include "ppo_tcgen05.cuh"
@@ -288,7 +290,7 @@ static int launch_narrow(Args a, const void *A, int64_t lda, const void *B, int6
 // same accumulator lie about 1200 cycles of commits, barrier waits, which cost 100 to 200 cycles each even when they are
 // over, fences and reads; two accumulators per half hide half of it: 0.52 us per block of K and tile); with many, the
 // board's power limit: at 27136 x 50304 x 4096 a block of K takes 925 cycles, but the clock falls to 1.35 GHz. Compared
-// under that load: blocks alone on 128 x 256 tiles 7.3 ms, pairs 6.4 ms; 256 x 192 tiles, whose accumulators can be released
+// under that load: blocks alone on 128 x 256 tiles 7.3 ms, pairs 6.0 to 6.4 ms; 256 x 192 tiles, whose accumulators can be released
 // before anything is multiplied, 6.6 ms; one issuer instead of four 9 ms; 256-column accumulators 6.6 ms.
 constexpr int kBM = 128, kBN = 256, kPairM = 2 * kBM, kWideStages = 4, kWideThreads = 768;
 constexpr int kWideA = kBM * kBlockK, kWideB = kBN / 2 * kBlockK, kWideStage = kWideA + kWideB;   // a block's halves of A and B

@@ -8,6 +8,9 @@
 //                blocks, and every transposed case (q is turned in shared memory, 8 bytes at a time, XOR-placed so
 //                that neither side has bank conflicts).
 // A block with a NaN or an infinity has scale NaN and q NaN throughout.
+// [4096, 50304] bf16, transposed, 128 x 128: 102 us = 6.0 TB/s; 27136 x 4096 rows: 55 us = 6.1 TB/s. Magnitudes are compared in the
+// storage type, two to an instruction, and a warp divides once for all its rows: with integer maxima of widened values and
+// two divisions per 8 elements the arithmetic took twice as long as the bytes (219 and 101 us).
 #include <cuda_fp8.h>
 #include <string.h>
 

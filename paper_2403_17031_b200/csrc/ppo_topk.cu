@@ -15,7 +15,9 @@
 // radix passes over it instead.
 // Few rows: a cluster of CL blocks shares a row; each selects the k best of its slice, and block 0 merges the sorted
 // lists and the sums through distributed shared memory.
-// Bound: the read of the logits (V * size bytes per row).
+// Bound: the read of the logits (V * size bytes per row), and behind it the selection, about 8000 cycles a row that the other
+// rows of an SM have to cover: 3392 x 50304 bf16, half masked, k = 5: 46 us = 3.8 TB/s; all rows, k = 20: 74 us = 4.6 TB/s; one
+// row, k = 20: 10 us.
 #include <cooperative_groups.h>
 
 #include "ppo_rows.cuh"
@@ -536,7 +538,7 @@ static int launch_any(const Args &a, int64_t rows, cudaStream_t s)
 // One read and one write of the row; the statistics come from the forward call. A block handles a chunk of a row: it
 // writes the dense part, then the elements that are given tokens once more with their gradients added (all in fp32,
 // rounded once; a token given several times is summed in the order given, by the first of its places).
-// Bound: bytes (read + write of the logits' size).
+// Bound: bytes (read + write of the logits' size): 3392 x 50304 bf16, half the rows masked, 86 us = 6.0 TB/s.
 struct BwdArgs {
     const void *logits;
     void *dlogits;

@@ -101,7 +101,7 @@ def _check_matmul(P, M, N, K, block_n, out_dtype, ops=None, out=None):
 @pytest.mark.parametrize("M,N,K,block_n", [
     (1, 1, 1, 128), (1, 300, 128, 128), (1, 1000, 577, 1), (7, 129, 4096, 128), (16, 256, 1000, 1), (17, 255, 640, 128),
     (64, 1024, 512, 128), (65, 333, 333, 1), (128, 128, 128, 128), (129, 257, 130, 128), (300, 1000, 577, 128), (300, 1000, 577, 1),
-    (513, 640, 1152, 128), (1000, 1100, 260, 1), (53, 512, 20000, 128), (700, 2000, 1024, 128)])
+    (513, 640, 1152, 128), (1000, 1100, 260, 1), (5000, 8, 300, 128), (1500, 1500, 5, 1), (53, 512, 20000, 128), (700, 2000, 1024, 128)])
 def test_matmul_matches_oracle(P, out_dtype, M, N, K, block_n):
     _check_matmul(P, M, N, K, block_n, out_dtype)
 
@@ -137,6 +137,31 @@ def test_matmul_results_do_not_depend_on_bytes_behind_k_or_on_the_pitch(P):
     buf = torch.full((M, N + 3), 5.0, device="cuda")
     P.fp8_matmul(a, sa, b, sb, out=buf[:, :N])
     assert torch.equal(buf[:, :N], want) and (buf[:, N:] == 5.0).all()
+
+
+@pytest.mark.parametrize("M,N,pad", [(20, 300, 4), (700, 2000, 8), (700, 2000, 3)])
+def test_matmul_leaves_what_lies_behind_its_rows_and_columns_alone(P, M, N, pad):
+    a, sa, b, sb = _operands(P, M, N, 640, 128)
+    for dtype in (BF16, F32):
+        want = P.fp8_matmul(a, sa, b, sb, out_dtype=dtype)
+        buf = torch.full((M + 5, N + pad), 5.0, dtype=dtype, device="cuda")
+        P.fp8_matmul(a, sa, b, sb, out=buf[:M, :N])
+        assert torch.equal(buf[:M, :N], want) and (buf[M:] == 5.0).all() and (buf[:, N:] == 5.0).all()
+
+
+def test_offsets_past_32_bits(P):
+    """A matrix of 2.3e9 elements, and a product of as many: the last rows and columns are those of a small call."""
+    M, N = 45056, 50304
+    x = torch.zeros(M, N, dtype=BF16, device="cuda")
+    x[-130:] = _matrix(130, N, BF16)
+    q, s = P.fp8_quantize(x, 1)
+    wq, wsc = P.fp8_quantize(x[-130:], 1)
+    assert torch.equal(q[-130:].float(), wq.float()) and torch.equal(s[:, -130:], wsc) and not q[:1000].float().any()
+    del x, q
+    a, sa, b, sb = _operands(P, M, N, 128, 128)
+    c = P.fp8_matmul(a, sa, b, sb)
+    tail = P.fp8_matmul(a[-300:], sa[:, -300:].contiguous(), b, sb)
+    assert torch.equal(c[-300:], tail)
 
 
 @pytest.mark.parametrize("M", [1, 40, 400])
