@@ -9,8 +9,8 @@
 // columns, so that a tile never holds more than 16 idle rows and the stream of B, which bounds the call, is read by
 // full 128 x 128 boxes. K is split over a cluster of blocks when there are too few tiles to occupy the SMs; the
 // partial tiles are joined through distributed shared memory in rank order, so results do not depend on timing.
-// 1 x 50304 x 4096 (206 MB of weight): 37 us = 5.6 TB/s with three blocks an SM (6 stages and two blocks: 43 us), so that all
-// 393 tiles are under way at once.
+// 1 x 50304 x 4096 (206 MB of weight): 35.0 us = 5.9 TB/s with rings of three stages, so that four blocks fit on an SM and all
+// 393 tiles are under way at once (four stages and three blocks: 36.9 us, six and two: 43 us).
 #include <cooperative_groups.h>
 
 #include "ppo_tcgen05.cuh"
@@ -41,11 +41,12 @@ __device__ __forceinline__ void wait_alive(bool &alive, unsigned long long *bar,
     if (alive) alive = wait(bar, parity, status);
 }
 
-constexpr int kNarrowStages = 4, kNarrowBufs = 2, kNarrowThreads = 192;
+constexpr int kNarrowBufs = 2, kNarrowThreads = 192;
 
-template <int MT>
+// ST: stages of the ring
+template <int MT, int ST>
 struct NarrowSmem {
-    unsigned long long full[kNarrowStages], empty[kNarrowStages], tmem_full[kNarrowBufs], tmem_empty[kNarrowBufs];
+    unsigned long long full[ST], empty[ST], tmem_full[kNarrowBufs], tmem_empty[kNarrowBufs];
     uint32_t tmem_base;
     float4 scale[4][kNarrowBufs][MT / 4];     // per epilogue warp: the columns' factors of a block of K
 };
@@ -74,13 +75,13 @@ __device__ __forceinline__ void store4(const Args &a, int m, int n, const float4
     }
 }
 
-template <int MT>
+template <int MT, int ST>
 __global__ void __launch_bounds__(kNarrowThreads)
 narrow_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const Args a, int split)
 {
     constexpr int kStage = narrow_stage_bytes<MT>();
     extern __shared__ __align__(1024) unsigned char smem_raw[];
-    __shared__ NarrowSmem<MT> sm;
+    __shared__ NarrowSmem<MT, ST> sm;
     unsigned char *ring = smem_raw + ((1024u - (saddr(smem_raw) & 1023u)) & 1023u);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = blockIdx.x % split, tile = blockIdx.x / split;
@@ -88,7 +89,7 @@ narrow_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__
     const int kb0 = (int)((int64_t)a.kb_total * rank / split), kb1 = (int)((int64_t)a.kb_total * (rank + 1) / split);
 
     if (threadIdx.x == 0) {
-        for (int s = 0; s < kNarrowStages; ++s) {
+        for (int s = 0; s < ST; ++s) {
             barrier_init(&sm.full[s], 1);
             barrier_init(&sm.empty[s], 1);
         }
@@ -112,8 +113,8 @@ narrow_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__
             bool alive = true;
             int issued = 0;
             for (int kb = kb0; kb < kb1; ++kb, ++issued) {
-                const int s = issued % kNarrowStages;
-                if (issued >= kNarrowStages) wait_alive(alive, &sm.empty[s], ((issued / kNarrowStages) - 1) & 1, a.status);
+                const int s = issued % ST;
+                if (issued >= ST) wait_alive(alive, &sm.empty[s], ((issued / ST) - 1) & 1, a.status);
                 if (!alive) break;
                 unsigned char *stage = ring + (size_t)s * kStage;
                 barrier_expect_tx(&sm.full[s], (uint32_t)kStage);
@@ -121,8 +122,8 @@ narrow_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__
                 tma_load_2d(stage + 128 * kBlockK, &map_a, kb * kBlockK, m0, &sm.full[s]);
             }
             // copies in flight land before the block may end
-            for (int i = issued > kNarrowStages ? issued - kNarrowStages : 0; i < issued; ++i)
-                wait(&sm.full[i % kNarrowStages], (i / kNarrowStages) & 1, a.status);
+            for (int i = issued > ST ? issued - ST : 0; i < issued; ++i)
+                wait(&sm.full[i % ST], (i / ST) & 1, a.status);
         }
         __syncwarp();
     } else if (warp == 1) {
@@ -130,9 +131,9 @@ narrow_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__
             constexpr uint32_t idesc = instr_desc_e4m3(128, MT);
             bool alive = true;
             for (int i = 0; i < kb1 - kb0; ++i) {
-                const int s = i % kNarrowStages, buf = i % kNarrowBufs;
+                const int s = i % ST, buf = i % kNarrowBufs;
                 if (i >= kNarrowBufs) wait_alive(alive, &sm.tmem_empty[buf], ((i / kNarrowBufs) - 1) & 1, a.status);
-                wait_alive(alive, &sm.full[s], (i / kNarrowStages) & 1, a.status);
+                wait_alive(alive, &sm.full[s], (i / ST) & 1, a.status);
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 const uint32_t b_addr = saddr(ring + (size_t)s * kStage), a_addr = b_addr + 128 * kBlockK;
 #pragma unroll
@@ -242,8 +243,28 @@ narrow_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__
     }
 }
 
-// blocks that fit on the SMs at once, by their shared memory (73, 81 and 97 KB)
+// blocks that fit on the SMs at once, by their shared memory (73, 81 and 97 KB with four stages)
 template <int MT> constexpr int narrow_places() { return (MT == 16 ? 3 : 2) * 148; }
+
+template <int MT, int ST>
+static int launch_narrow_stages(const Args &a, const CUtensorMap &ma, const CUtensorMap &mb, int split, cudaStream_t s)
+{
+    const size_t smem = (size_t)ST * narrow_stage_bytes<MT>() + 1024;
+    PPO_RETURN_IF_CUDA(cudaFuncSetAttribute(narrow_kernel<MT, ST>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(a.m_tiles * a.n_tiles * split));
+    cfg.blockDim = dim3(kNarrowThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = split;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = split > 1 ? 1 : 0;
+    PPO_RETURN_IF_CUDA(cudaLaunchKernelEx(&cfg, narrow_kernel<MT, ST>, ma, mb, a, split));
+    return PPO_OK;
+}
 
 template <int MT>
 static int launch_narrow(Args a, const void *A, int64_t lda, const void *B, int64_t ldb, int64_t K, cudaStream_t s)
@@ -260,21 +281,11 @@ static int launch_narrow(Args a, const void *A, int64_t lda, const void *B, int6
     int split = 1;
     while (split < 8 && tiles * split * 2 <= narrow_places<MT>() && a.kb_total >= 4 * split) split *= 2;
     if (tiles * split >= ((int64_t)1 << 31)) return PPO_ERR_SHAPE;
-    const size_t smem = (size_t)kNarrowStages * narrow_stage_bytes<MT>() + 1024;
-    PPO_RETURN_IF_CUDA(cudaFuncSetAttribute(narrow_kernel<MT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(tiles * split));
-    cfg.blockDim = dim3(kNarrowThreads);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = s;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = split;
-    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = split > 1 ? 1 : 0;
-    PPO_RETURN_IF_CUDA(cudaLaunchKernelEx(&cfg, narrow_kernel<MT>, ma, mb, a, split));
-    return PPO_OK;
+    // Tiles of 16 columns: three stages once the SMs hold more than two blocks each, so that a fourth fits (1 x 50304 x 4096:
+    // 35.0 instead of 36.9 us, 1 x 50304 x 8192: 67.0 instead of 69.9), else four (4 x 16384 x 4096: 16.2 instead of 16.5 us)
+    if constexpr (MT == 16)
+        if (tiles * split > 2 * 148) return launch_narrow_stages<MT, 3>(a, ma, mb, split, s);
+    return launch_narrow_stages<MT, 4>(a, ma, mb, split, s);
 }
 
 // ---------------------------------------------------------------- wide kernel
