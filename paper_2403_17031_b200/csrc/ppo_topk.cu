@@ -2,22 +2,23 @@
 // over the logits (ppo_logprob_topk), and the gradient on all of those back to the logits (ppo_logprob_topk_bwd).
 //
 // Forward. The statistics are those of step 1: sums of 2^(y - ref) and 2^(y - ref) (y - ref) with y = logit log2(e) /
-// temperature, relative to a reference per warp. Beside them every thread keeps the maximum of the
-// elements it streams (its "segment": packs tid, tid + 256, ...). Selection then works on segments:
-//   the k-th largest of the 256 segment maxima is a threshold t with at least k elements >= t, so nothing below t is
-//   among the k best; only segments whose maximum reaches t hold candidates. Every thread also knows the pack of its
-//   maximum and the largest value outside it, so most of these segments (about k of 256) need that one pack re-read
-//   and only those with a second pack that reaches t are searched whole (searching all of them is sector traffic of
-//   0.4 of the row at k = 20 and more than the row at k = 64 in fp32: 85 instead of 48 us for 997 rows). Candidates are
-//   ranked by counting against each other on the 64-bit key (value, ~index), which is unique: ties go to the lowest
-//   index and the order in which candidates arrive does not matter.
+// temperature, relative to a reference per warp. Beside them every thread keeps the maximum of the elements it streams
+// (packs tid, tid + 256, ...), for each half of them (a "segment") on its own. Selection then works on those:
+//   the k-th largest of the 256 threads' maxima is a threshold t with at least k elements >= t, so nothing below t is
+//   among the k best; only segments whose maximum reaches t hold candidates. Every segment's maximum comes with its pack and
+//   the largest value outside that pack, so most of these segments (about k of 512) need that one pack re-read, by the thread
+//   that streamed it, and only those with a second pack that reaches t are searched whole, by half a warp: for 997 rows of
+//   50277 fp32, k = 64, one segment in 150. (Searching all of them is sector traffic of more than the row: 85 us instead of
+//   39 for these rows. One segment per thread: 51 us, k = 20 the same 37; four: 39, but 91 instead of 81 us for 3392 bf16
+//   rows.) Candidates are ranked by counting against each other on the 64-bit key (value, ~index), which is unique: ties go to
+//   the lowest index and the order in which candidates arrive does not matter.
 // A slice whose candidates overflow the list (rows of equal values, fewer than k unbanned tokens) is selected by
 // radix passes over it instead.
 // Few rows: a cluster of CL blocks shares a row; each selects the k best of its slice, and block 0 merges the sorted
 // lists and the sums through distributed shared memory.
-// Bound: the read of the logits (V * size bytes per row), and behind it the selection, about 8000 cycles a row that the other
-// rows of an SM have to cover: 3392 x 50304 bf16, half masked, k = 5: 46 us = 3.8 TB/s; all rows, k = 20: 74 us = 4.6 TB/s; one
-// row, k = 20: 10 us.
+// Bound: the read of the logits (V * size bytes per row; without alternatives 3392 x 50304 bf16 57 us = 6.0 TB/s), and behind it
+// the selection, which the other rows of an SM have to cover: k = 5: 64 us, k = 20: 68 us, half the rows masked, k = 5: 38 us =
+// 4.5 TB/s (1.4 rounds of blocks); one row, k = 20: 9 us.
 #include <cooperative_groups.h>
 
 #include "ppo_rows.cuh"
@@ -31,7 +32,9 @@ constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kMaxIds = 128;       // largest k and largest number of given tokens
 // longest candidate list: every element of a slice with fewer than k packs (at most 127 packs of 8 and 14 loose
 // elements) fits, so that the radix fallback always has at least k packs
-constexpr int kCap = 1280;
+constexpr int kParts = 2;              // segments of a thread
+// candidates of a row: with CL blocks a row also the merged lists
+template <int CL> constexpr int kCap = CL == 1 ? 512 : 1280;
 
 struct Args {
     const void *logits;
@@ -48,18 +51,33 @@ struct Args {
     int *status;
 };
 
+// What a thread knows of a segment: the maximum, the largest value outside the pack that holds it, that pack.
+struct Segment {
+    float top, second;
+    int pack;
+    __device__ __forceinline__ void init()
+    {
+        top = second = -INFINITY;
+        pack = 0x7fffffff;
+    }
+    __device__ __forceinline__ void add(float xmax, int i)
+    {
+        second = fmaxf(second, fminf(xmax, top));
+        pack = xmax > top ? i : pack;
+        top = fmaxf(top, xmax);
+    }
+};
+
+template <int CL>
 struct Smem {
-    unsigned long long cand[kCap];
+    unsigned long long cand[kCap<CL>];
     unsigned long long best[kMaxIds];    // the slice's best, sorted
-    uint32_t seg_key[kThreads];          // segment maxima as ordered keys; the fallback's histogram
-    uint32_t seg_key2[kThreads];         // largest value outside the pack that holds the maximum
-    int seg_pack[kThreads];              // that pack
-    uint16_t list[kThreads];             // segments that hold candidates: from the front those that have to be searched
-                                         // whole, from the back those whose candidates are all in one known pack
+    uint32_t seg_key[kThreads];          // maxima of the threads' elements as ordered keys; the fallback's histogram
+    Segment seg[kParts][kThreads];
     float red[96];
     SoftmaxState st;
     uint32_t threshold;
-    int n_whole, n_single, n_cand, n_best, bin, need;
+    int n_cand, n_best, bin, need;
 };
 
 // whole numbers that order like the values (-0 equals +0); 0 is below every value
@@ -73,18 +91,6 @@ __device__ __forceinline__ unsigned long long make_key(uint32_t u, int j)
 {
     return ((unsigned long long)u << 32) | (uint32_t)~(uint32_t)j;
 }
-
-// What a thread knows of its segment: the maximum, the pack that holds it, the maximum of the other packs.
-struct Segment {
-    float top, second;
-    int pack;
-    __device__ __forceinline__ void add(float xmax, int i)
-    {
-        second = fmaxf(second, fminf(xmax, top));
-        pack = xmax > top ? i : pack;
-        top = fmaxf(top, xmax);
-    }
-};
 
 // One pack into the sums (clamped at kNegBig, so a -inf logit adds exact zeros) and into the segment.
 template <typename T>
@@ -148,8 +154,8 @@ __device__ __forceinline__ int loose_element(const Slice &s, int t)
 
 // The k best of elements [e0, e1) into sm.cand (unsorted, k of them), for any values: radix passes find the k-th
 // largest value, then all larger ones and the first of the equal ones (in index order) are taken.
-template <typename T>
-__device__ __noinline__ void select_by_radix(const T *src, int e0, int e1, int k, Smem &sm)
+template <typename T, int CL>
+__device__ __noinline__ void select_by_radix(const T *src, int e0, int e1, int k, Smem<CL> &sm)
 {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     uint32_t prefix = 0;
@@ -213,8 +219,9 @@ __device__ __noinline__ void select_by_radix(const T *src, int e0, int e1, int k
     __syncthreads();
 }
 
-// Warp 0: a threshold that at least k and at most a few more of the segment maxima reach, and the segments that do.
-__device__ __forceinline__ void choose_segments(int k, Smem &sm)
+// Warp 0: a threshold that at least k and at most a few more of the threads' maxima reach.
+template <int CL>
+__device__ __forceinline__ void choose_threshold(int k, Smem<CL> &sm)
 {
     constexpr int Q = kThreads / 32;
     const int lane = threadIdx.x & 31;
@@ -226,7 +233,7 @@ __device__ __forceinline__ void choose_segments(int k, Smem &sm)
         low = min(low, key[q]);
     }
     uint32_t lo = __reduce_min_sync(0xffffffffu, low), hi = __reduce_max_sync(0xffffffffu, top);
-    // invariant: count(>= lo) >= k (there are more segments than k); count(> hi) = 0
+    // invariant: count(>= lo) >= k (there are more threads than k); count(> hi) = 0
     while (lo < hi) {
         const uint32_t mid = lo + (hi - lo + 1) / 2;
         int cnt = 0;
@@ -235,73 +242,76 @@ __device__ __forceinline__ void choose_segments(int k, Smem &sm)
         cnt = (int)__reduce_add_sync(0xffffffffu, (unsigned)cnt);
         if (cnt >= k) {
             lo = mid;
-            if (cnt <= k + (k >> 3) + 1) break;
+            if (cnt <= k + (k >> 3) + 3) break;
         } else {
             hi = mid - 1;
         }
     }
     // maxima are clamped at kNegBig: at that level everything is a candidate
-    const uint32_t thr = lo <= ordered(0.99f * kNegBig) ? 0u : lo;
-    int whole = 0, single = 0;
-#pragma unroll
-    for (int q = 0; q < Q; ++q) {
-        const bool in = key[q] != 0 && key[q] >= thr, more = in && sm.seg_key2[q * 32 + lane] >= thr;
-        const uint32_t votes_w = __ballot_sync(0xffffffffu, more), votes_s = __ballot_sync(0xffffffffu, in && !more);
-        const uint32_t below = (1u << lane) - 1u;
-        if (more) sm.list[whole + __popc(votes_w & below)] = (uint16_t)(q * 32 + lane);
-        else if (in) sm.list[kThreads - 1 - single - __popc(votes_s & below)] = (uint16_t)(q * 32 + lane);
-        whole += __popc(votes_w);
-        single += __popc(votes_s);
-    }
-    if (lane == 0) {
-        sm.threshold = thr;
-        sm.n_whole = whole;
-        sm.n_single = single;
-    }
+    if (lane == 0) sm.threshold = lo <= ordered(0.99f * kNegBig) ? 0u : lo;
 }
 
-// The slice's best min(k, length) elements into sm.best, sorted. The segments have been chosen; loose elements are in
-// sm.cand already.
-template <typename T>
-__device__ __forceinline__ void select_best(const T *src, const Slice &sl, int k, Smem &sm)
+// the elements of a pack that reach the threshold into the list of candidates
+template <typename T, int CL>
+__device__ __forceinline__ void take_candidates(const uint4 &v, int at, int head, float thr, Smem<CL> &sm)
 {
-    constexpr int N = Pack<T>::N, R = 4;
-    const int tid = threadIdx.x;
-    const int want = min(k, sl.e1 - sl.e0);
-    const uint32_t thr = sm.threshold;
-    const float thr_f = thr == 0u ? -INFINITY : unordered(thr);
-    // the packs to search, dealt over all threads: one or two rounds of loads
-    const uint4 *body = reinterpret_cast<const uint4 *>(src + sl.head);
-    const int per = (sl.p1 - sl.p0 + kThreads - 1) / kThreads, single = sm.n_single, total = single + sm.n_whole * per;
-    for (int base = tid; base < total; base += R * kThreads) {
-        uint4 v[R];
-        int at[R];
+    constexpr int N = Pack<T>::N;
+    float x[N];
+    Pack<T>::unpack_raw(v, x);
+    float top = x[0];
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            const int item = base + r * kThreads, w = item - single, seg = w / max(per, 1);
-            at[r] = item < single ? sm.seg_pack[sm.list[kThreads - 1 - item]]
-                  : item < total ? sl.p0 + sm.list[seg] + (w - seg * per) * kThreads : sl.p1;
-            if (at[r] < sl.p1) v[r] = body[at[r]];
+    for (int e = 1; e < N; ++e) top = fmaxf(top, x[e]);
+    if (!(top >= thr)) return;
+#pragma unroll
+    for (int e = 0; e < N; ++e)
+        if (x[e] >= thr) {
+            const int c = atomicAdd(&sm.n_cand, 1);
+            if (c < kCap<CL>) sm.cand[c] = make_key(ordered(x[e]), head + at * N + e);
         }
+}
+
+// The slice's best min(k, length) elements into sm.best, sorted. The threshold is known; loose elements are in sm.cand
+// already. `span`: packs of a segment.
+template <typename T, int CL>
+__device__ __forceinline__ void select_best(const T *src, const Slice &sl, int span, int k, Smem<CL> &sm)
+{
+    const int tid = threadIdx.x, lane = tid & 31;
+    const int want = min(k, sl.e1 - sl.e0);
+    const float thr = sm.threshold == 0u ? -INFINITY : unordered(sm.threshold);
+    const uint4 *body = reinterpret_cast<const uint4 *>(src + sl.head);
+    // a thread re-reads the one pack of its segments with candidates in no other
+    uint4 v[kParts];
+    int at[kParts];
+    bool whole[kParts];
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            if (at[r] >= sl.p1) continue;
-            float x[N];
-            Pack<T>::unpack_raw(v[r], x);
-            float top = x[0];
+    for (int s = 0; s < kParts; ++s) {
+        const Segment g = sm.seg[s][tid];
+        whole[s] = g.second >= thr;
+        at[s] = g.top >= thr && !whole[s] ? g.pack : sl.p1;
+        if (at[s] < sl.p1) v[s] = body[at[s]];
+    }
 #pragma unroll
-            for (int e = 1; e < N; ++e) top = fmaxf(top, x[e]);
-            if (!(top >= thr_f)) continue;
+    for (int s = 0; s < kParts; ++s)
+        if (at[s] < sl.p1) take_candidates<T, CL>(v[s], at[s], sl.head, thr, sm);
+    // the others are searched by half a warp each
 #pragma unroll
-            for (int e = 0; e < N; ++e)
-                if (x[e] >= thr_f) {
-                    const int c = atomicAdd(&sm.n_cand, 1);
-                    if (c < kCap) sm.cand[c] = make_key(ordered(x[e]), sl.head + at[r] * N + e);
-                }
+    for (int s = 0; s < kParts; ++s) {
+        uint32_t todo = __ballot_sync(0xffffffffu, whole[s]);
+        while (todo) {
+            const int l0 = __ffs(todo) - 1;
+            todo &= todo - 1;
+            const int l1 = __ffs(todo) - 1;                 // -1: none
+            todo &= todo - 1;
+            const int l = lane < 16 ? l0 : l1;
+            const int first = l < 0 ? sl.p1 : sl.p0 + (tid & ~31) + l + s * span * kThreads;
+            for (int j = lane & 15; j < span; j += 16) {
+                const int i = first + j * kThreads;
+                if (i < sl.p1) take_candidates<T, CL>(body[i], i, sl.head, thr, sm);
+            }
         }
     }
     __syncthreads();
-    if (sm.n_cand > kCap) {
+    if (sm.n_cand > kCap<CL>) {
         __syncthreads();
         select_by_radix(src, sl.e0, sl.e1, want, sm);
     }
@@ -323,13 +333,14 @@ __device__ __forceinline__ void select_best(const T *src, const Slice &sl, int k
     __syncthreads();
 }
 
-// (a block to a row: 8 blocks to an SM hide the selection of some behind the streams of the others better than more
-// loads in flight per thread do: 46 against 51 us for 3392 bf16 rows, half of them masked, 48 against 53 for 997 fp32)
+// (a block to a row: 8 blocks to an SM, 32 registers a thread, hide the selection of some behind the streams of the others better
+// than four loads in flight per thread and 4 blocks do: 38 against 41 us for 3392 bf16 rows, half of them masked, 39 against 46
+// for 997 fp32; what the stream does not need is therefore loaded behind it)
 template <typename T, int CL>
 __global__ void __launch_bounds__(kThreads, CL == 1 ? 8 : 1)
 topk_kernel(const Args a)
 {
-    __shared__ Smem sm;
+    __shared__ Smem<CL> sm;
     const int tid = threadIdx.x;
     const int64_t row = blockIdx.x / CL;
     const int rank = blockIdx.x % CL;
@@ -350,22 +361,17 @@ topk_kernel(const Args a)
     const T *src = reinterpret_cast<const T *>(a.logits) + row * a.row_stride;
     const Slice sl = slice_of(src, a.V, rank, CL);
     const uint4 *body = reinterpret_cast<const uint4 *>(src + sl.head);
-    float x_tok = 0.f;
-    bool tok_ok = true;
-    if (rank == 0 && tid < a.n) {
-        const int tok = a.tokens[row * a.n + tid];
-        tok_ok = (unsigned)tok < (unsigned)a.V;
-        if (tok_ok) x_tok = Pack<T>::load1(src + tok);
-    }
     // Sums are taken relative to the maximum of the warp's first loads (about a thousand elements, all of them when the
     // row is split eightfold): near the row's own maximum, so that the entropy, a difference of two numbers that grow
     // with the distance, keeps its digits.
     FixedAcc acc;
     acc.init();
     Segment seg;
-    seg.top = seg.second = -INFINITY;
-    seg.pack = 0;
+    seg.init();
     constexpr int U = CL == 1 ? 2 : 4;
+    // packs of a segment: a thread's share in kParts parts, whole rounds of loads
+    const int per_thread = (sl.p1 - sl.p0 + kThreads - 1) / kThreads, span = ((per_thread + kParts - 1) / kParts + U - 1) / U * U;
+    int part = 0;
     const int lane = tid & 31, warp = tid >> 5;
     uint4 v[U];
     float first_max = kNegBig;
@@ -388,11 +394,21 @@ topk_kernel(const Args a)
     for (int q = 0; q < U; ++q)
         if (i + q * kThreads < sl.p1) accumulate<T>(v[q], i + q * kThreads, a.c, nm, acc, seg);
     i += U * kThreads;
-    for (; i + (U - 1) * kThreads < sl.p1; i += U * kThreads) {
+    int next = sl.p0 + tid + span * kThreads;
+    const auto next_part = [&] {
+        sm.seg[part++][tid] = seg;
+        seg.init();
+        next += span * kThreads;
+    };
+    while (true) {
+        for (const int end = min(next, sl.p1 - (U - 1) * kThreads); i < end; i += U * kThreads) {
 #pragma unroll
-        for (int q = 0; q < U; ++q) v[q] = ld_stream(body + i + q * kThreads);
+            for (int q = 0; q < U; ++q) v[q] = ld_stream(body + i + q * kThreads);
 #pragma unroll
-        for (int q = 0; q < U; ++q) accumulate<T>(v[q], i + q * kThreads, a.c, nm, acc, seg);
+            for (int q = 0; q < U; ++q) accumulate<T>(v[q], i + q * kThreads, a.c, nm, acc, seg);
+        }
+        if (i != next) break;
+        next_part();
     }
 #pragma unroll
     for (int q = 0; q < U - 1; ++q)
@@ -400,6 +416,13 @@ topk_kernel(const Args a)
 #pragma unroll
     for (int q = 0; q < U - 1; ++q)
         if (i + q * kThreads < sl.p1) accumulate<T>(v[q], i + q * kThreads, a.c, nm, acc, seg);
+    float x_tok = 0.f;
+    bool tok_ok = true;
+    if (rank == 0 && tid < a.n) {
+        const int tok = a.tokens[row * a.n + tid];
+        tok_ok = (unsigned)tok < (unsigned)a.V;
+        if (tok_ok) x_tok = Pack<T>::load1(src + tok);
+    }
     const int loose = tid < 2 * (Pack<T>::N - 1) ? loose_element<T>(sl, tid) : -1;
     const float x_loose = loose >= 0 ? Pack<float>::clampf(Pack<T>::load1(src + loose)) : kNegBig;
     SoftmaxState st;
@@ -425,26 +448,28 @@ topk_kernel(const Args a)
     }
     if (lane == 0) { sm.red[warp] = st.m; sm.red[32 + warp] = st.s; sm.red[64 + warp] = st.u; }
     if (a.k > 0) {
-        sm.seg_key[tid] = sl.p0 + tid < sl.p1 ? ordered(seg.top) : 0u;
-        sm.seg_key2[tid] = ordered(seg.second);
-        sm.seg_pack[tid] = seg.pack;
+        float top = seg.top;
+        while (part < kParts) next_part();                 // (those behind the current one are empty)
+#pragma unroll
+        for (int s = 0; s < kParts; ++s) top = fmaxf(top, sm.seg[s][tid].top);
+        sm.seg_key[tid] = sl.p0 + tid < sl.p1 ? ordered(top) : 0u;
         if (loose >= 0) sm.cand[tid] = make_key(ordered(Pack<T>::load1(src + loose)), loose);   // (they come first)
         if (tid == 0) sm.n_cand = sl.loose;
     }
     __syncthreads();
-    if (warp == 0) {
+    if (warp == 0 && a.k > 0) choose_threshold(a.k, sm);
+    if (warp == 1) {
         st.init();
         if (lane < kWarps) { st.m = sm.red[lane]; st.s = sm.red[32 + lane]; st.u = sm.red[64 + lane]; }
         st = warp_merge(st);
         if (lane == 0) sm.st = st;
-        if (a.k > 0) choose_segments(a.k, sm);
     }
     __syncthreads();
     st = sm.st;
     if (a.k > 0) {
         // (false for NaN; a slice without weight, s = 0, is selected from)
         if (st.s < 1.0e37f) {
-            select_best(src, sl, a.k, sm);
+            select_best(src, sl, span, a.k, sm);
         } else {
             if (tid == 0) sm.n_best = 0;
             __syncthreads();

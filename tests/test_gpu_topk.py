@@ -335,3 +335,26 @@ def test_topk_offsets_past_32_bits(P):
     d = P.logprob_topk_bwd(x, o["lse"], TAU, tokens=tok, dlogprob=torch.ones(rows, 1, device="cuda"), mask=mask)["dlogits"]
     dt = P.logprob_topk_bwd(tail, o["lse"][-4:].contiguous(), TAU, tokens=tok[-4:].contiguous(), dlogprob=torch.ones(4, 1, device="cuda"))
     assert torch.equal(d[-4:], dt["dlogits"]) and not d[:1000].any()
+
+
+@pytest.mark.parametrize("dt", [BF16, F32])
+@pytest.mark.parametrize("rows,V", [(600, 32768), (600, 30011), (2, 50304)])
+def test_best_elements_at_regular_distances(P, dt, rows, V):
+    """The k best, all different, at one distance from each other: few or many of them in the same thread's share."""
+    g = torch.Generator(device="cuda").manual_seed(11)
+    x = torch.rand(rows, V, device="cuda", generator=g).mul(4).to(dt)            # all below 8
+    n = 8 if dt == BF16 else 4
+    dists = [1, n, 16 * n, 32 * n, 256 * n, 257 * n, 512 * n, 128 * n + 1]
+    k = 7
+    ids = torch.empty(rows, k, dtype=torch.int64)
+    for r in range(rows):
+        d = dists[r % len(dists)]
+        ids[r] = (torch.arange(k) * d + 37 * r) % V
+    assert all(len(set(row.tolist())) == k for row in ids)
+    ids = ids.cuda()
+    x.scatter_(1, ids, torch.arange(8 + k, 8, -1, device="cuda").to(dt).expand(rows, k))     # exact in both types
+    o = P.logprob_topk(x, None, k, 1.0)
+    assert torch.equal(o["top_ids"].long(), ids)
+    full = P.logprob_topk(x, None, 100, 1.0)["top_ids"].long()
+    want = torch.sort(x.float(), dim=1, descending=True, stable=True).indices[:, :100]
+    assert torch.equal(full, want)
