@@ -3,8 +3,9 @@
 //
 // Forward. The statistics are those of step 1: sums of 2^(y - ref) and 2^(y - ref) (y - ref) with y = logit log2(e) /
 // temperature, relative to a reference per warp. Beside them every thread keeps the maximum of the elements it streams
-// (packs tid, tid + 256, ...), for each half of them (a "segment") on its own. Selection then works on those:
-//   the k-th largest of the 256 threads' maxima is a threshold t with at least k elements >= t, so nothing below t is
+// (packs tid, tid + 256, ...), for each half of them (a "segment") on its own. (Short rows: 128 threads with one segment each.)
+// Selection then works on those:
+//   the k-th largest of the threads' maxima is a threshold t with at least k elements >= t, so nothing below t is
 //   among the k best; only segments whose maximum reaches t hold candidates. Every segment's maximum comes with its pack and
 //   the largest value outside that pack, so most of these segments (about k of 512) need that one pack re-read, by the thread
 //   that streamed it, and only those with a second pack that reaches t are searched whole, by half a warp: for 997 rows of
@@ -28,13 +29,7 @@ namespace topk {
 
 namespace cg = cooperative_groups;
 
-constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kMaxIds = 128;       // largest k and largest number of given tokens
-// longest candidate list: every element of a slice with fewer than k packs (at most 127 packs of 8 and 14 loose
-// elements) fits, so that the radix fallback always has at least k packs
-constexpr int kParts = 2;              // segments of a thread
-// candidates of a row: with CL blocks a row also the merged lists
-template <int CL> constexpr int kCap = CL == 1 ? 512 : 1280;
 
 struct Args {
     const void *logits;
@@ -68,11 +63,15 @@ struct Segment {
     }
 };
 
-template <int CL>
+// of a block of TH threads, one of CL that share a row
+template <int CL, int TH>
 struct Smem {
-    unsigned long long cand[kCap<CL>];
+    static constexpr int kThreads = TH;
+    static constexpr int kParts = TH == 256 ? 2 : 1;         // segments of a thread
+    static constexpr int kCap = CL == 1 ? 512 : 1280;        // candidates: with several blocks also their merged lists
+    unsigned long long cand[kCap];
     unsigned long long best[kMaxIds];    // the slice's best, sorted
-    uint32_t seg_key[kThreads];          // maxima of the threads' elements as ordered keys; the fallback's histogram
+    uint32_t seg_key[256];               // maxima of the threads' elements as ordered keys; the fallback's histogram
     Segment seg[kParts][kThreads];
     float red[96];
     SoftmaxState st;
@@ -154,14 +153,15 @@ __device__ __forceinline__ int loose_element(const Slice &s, int t)
 
 // The k best of elements [e0, e1) into sm.cand (unsorted, k of them), for any values: radix passes find the k-th
 // largest value, then all larger ones and the first of the equal ones (in index order) are taken.
-template <typename T, int CL>
-__device__ __noinline__ void select_by_radix(const T *src, int e0, int e1, int k, Smem<CL> &sm)
+template <typename T, typename S>
+__device__ __noinline__ void select_by_radix(const T *src, int e0, int e1, int k, S &sm)
 {
+    constexpr int kThreads = S::kThreads, kWarps = kThreads / 32;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     uint32_t prefix = 0;
     int need = k;
     for (int shift = 24; shift >= 0; shift -= 8) {
-        sm.seg_key[tid] = 0;
+        for (int i = tid; i < 256; i += kThreads) sm.seg_key[i] = 0;
         __syncthreads();
         for (int j0 = e0; j0 < e1; j0 += kThreads) {
             const int j = j0 + tid;
@@ -220,10 +220,10 @@ __device__ __noinline__ void select_by_radix(const T *src, int e0, int e1, int k
 }
 
 // Warp 0: a threshold that at least k and at most a few more of the threads' maxima reach.
-template <int CL>
-__device__ __forceinline__ void choose_threshold(int k, Smem<CL> &sm)
+template <typename S>
+__device__ __forceinline__ void choose_threshold(int k, S &sm)
 {
-    constexpr int Q = kThreads / 32;
+    constexpr int Q = S::kThreads / 32;
     const int lane = threadIdx.x & 31;
     uint32_t key[Q], top = 0, low = 0xffffffffu;
 #pragma unroll
@@ -252,8 +252,8 @@ __device__ __forceinline__ void choose_threshold(int k, Smem<CL> &sm)
 }
 
 // the elements of a pack that reach the threshold into the list of candidates
-template <typename T, int CL>
-__device__ __forceinline__ void take_candidates(const uint4 &v, int at, int head, float thr, Smem<CL> &sm)
+template <typename T, typename S>
+__device__ __forceinline__ void take_candidates(const uint4 &v, int at, int head, float thr, S &sm)
 {
     constexpr int N = Pack<T>::N;
     float x[N];
@@ -266,15 +266,16 @@ __device__ __forceinline__ void take_candidates(const uint4 &v, int at, int head
     for (int e = 0; e < N; ++e)
         if (x[e] >= thr) {
             const int c = atomicAdd(&sm.n_cand, 1);
-            if (c < kCap<CL>) sm.cand[c] = make_key(ordered(x[e]), head + at * N + e);
+            if (c < S::kCap) sm.cand[c] = make_key(ordered(x[e]), head + at * N + e);
         }
 }
 
 // The slice's best min(k, length) elements into sm.best, sorted. The threshold is known; loose elements are in sm.cand
 // already. `span`: packs of a segment.
-template <typename T, int CL>
-__device__ __forceinline__ void select_best(const T *src, const Slice &sl, int span, int k, Smem<CL> &sm)
+template <typename T, typename S>
+__device__ __forceinline__ void select_best(const T *src, const Slice &sl, int span, int k, S &sm)
 {
+    constexpr int kThreads = S::kThreads, kParts = S::kParts;
     const int tid = threadIdx.x, lane = tid & 31;
     const int want = min(k, sl.e1 - sl.e0);
     const float thr = sm.threshold == 0u ? -INFINITY : unordered(sm.threshold);
@@ -292,7 +293,7 @@ __device__ __forceinline__ void select_best(const T *src, const Slice &sl, int s
     }
 #pragma unroll
     for (int s = 0; s < kParts; ++s)
-        if (at[s] < sl.p1) take_candidates<T, CL>(v[s], at[s], sl.head, thr, sm);
+        if (at[s] < sl.p1) take_candidates<T>(v[s], at[s], sl.head, thr, sm);
     // the others are searched by half a warp each
 #pragma unroll
     for (int s = 0; s < kParts; ++s) {
@@ -306,12 +307,12 @@ __device__ __forceinline__ void select_best(const T *src, const Slice &sl, int s
             const int first = l < 0 ? sl.p1 : sl.p0 + (tid & ~31) + l + s * span * kThreads;
             for (int j = lane & 15; j < span; j += 16) {
                 const int i = first + j * kThreads;
-                if (i < sl.p1) take_candidates<T, CL>(body[i], i, sl.head, thr, sm);
+                if (i < sl.p1) take_candidates<T>(body[i], i, sl.head, thr, sm);
             }
         }
     }
     __syncthreads();
-    if (sm.n_cand > kCap<CL>) {
+    if (sm.n_cand > S::kCap) {
         __syncthreads();
         select_by_radix(src, sl.e0, sl.e1, want, sm);
     }
@@ -333,14 +334,15 @@ __device__ __forceinline__ void select_best(const T *src, const Slice &sl, int s
     __syncthreads();
 }
 
-// (a block to a row: 8 blocks to an SM, 32 registers a thread, hide the selection of some behind the streams of the others better
-// than four loads in flight per thread and 4 blocks do: 38 against 41 us for 3392 bf16 rows, half of them masked, 39 against 46
-// for 997 fp32; what the stream does not need is therefore loaded behind it)
-template <typename T, int CL>
-__global__ void __launch_bounds__(kThreads, CL == 1 ? 8 : 1)
+// (a block to a row: 8 blocks of 256 threads to an SM, 32 registers a thread, hide the selection of some behind the streams
+// of the others better than four loads in flight per thread and 4 blocks do: 38 against 41 us for 3392 bf16 rows, half of them
+// masked, 39 against 46 for 997 fp32; what the stream does not need is therefore loaded behind it)
+template <typename T, int CL, int TH>
+__global__ void __launch_bounds__(TH, CL == 1 ? 2048 / TH : 1)
 topk_kernel(const Args a)
 {
-    __shared__ Smem<CL> sm;
+    constexpr int kThreads = TH, kWarps = TH / 32, kParts = Smem<CL, TH>::kParts;
+    __shared__ Smem<CL, TH> sm;
     const int tid = threadIdx.x;
     const int64_t row = blockIdx.x / CL;
     const int rank = blockIdx.x % CL;
@@ -529,12 +531,12 @@ topk_kernel(const Args a)
     }
 }
 
-template <typename T, int CL>
+template <typename T, int CL, int TH>
 static int launch(const Args &a, int64_t rows, cudaStream_t s)
 {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(rows * CL));
-    cfg.blockDim = dim3(kThreads);
+    cfg.blockDim = dim3(TH);
     cfg.stream = s;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -542,7 +544,7 @@ static int launch(const Args &a, int64_t rows, cudaStream_t s)
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = CL > 1 ? 1 : 0;
-    PPO_RETURN_IF_CUDA(cudaLaunchKernelEx(&cfg, topk_kernel<T, CL>, a));
+    PPO_RETURN_IF_CUDA(cudaLaunchKernelEx(&cfg, topk_kernel<T, CL, TH>, a));
     return PPO_OK;
 }
 
@@ -551,10 +553,14 @@ static int launch_any(const Args &a, int64_t rows, cudaStream_t s)
 {
     // few rows: split each over a cluster while there are SMs to fill and every thread still streams a pack or more
     const int64_t packs = a.V / Pack<T>::N;
-    if (rows * 8 <= 2 * 148 && packs >= 8 * kThreads) return launch<T, 8>(a, rows, s);
-    if (rows * 4 <= 2 * 148 && packs >= 4 * kThreads) return launch<T, 4>(a, rows, s);
-    if (rows * 2 <= 2 * 148 && packs >= 2 * kThreads) return launch<T, 2>(a, rows, s);
-    return launch<T, 1>(a, rows, s);
+    if (rows * 8 <= 2 * 148 && packs >= 8 * 256) return launch<T, 8, 256>(a, rows, s);
+    if (rows * 4 <= 2 * 148 && packs >= 4 * 256) return launch<T, 4, 256>(a, rows, s);
+    if (rows * 2 <= 2 * 148 && packs >= 2 * 256) return launch<T, 2, 256>(a, rows, s);
+    // Short rows, enough of them to fill the SMs, few alternatives: half the threads and twice the blocks on an SM, so that more
+    // selections hide each other. bf16, 128 against 256 threads: 3392 x 4096, k = 20: 17 / 23 us, 3392 x 16384: 29 / 36 us; 200 x
+    // 16384: 8.6 / 7.5 us; 1000 x 16384, k = 64: 18.7 / 17.2 us; 997 x 50277 fp32 (longer rows), k = 20: 46 / 37 us.
+    if (packs <= 2048 && rows >= 4 * 148 && a.k <= 32) return launch<T, 1, 128>(a, rows, s);
+    return launch<T, 1, 256>(a, rows, s);
 }
 
 // ---------------------------------------------------------------- backward
@@ -564,6 +570,8 @@ static int launch_any(const Args &a, int64_t rows, cudaStream_t s)
 // writes the dense part, then the elements that are given tokens once more with their gradients added (all in fp32,
 // rounded once; a token given several times is summed in the order given, by the first of its places).
 // Bound: bytes (read + write of the logits' size): 3392 x 50304 bf16, half the rows masked, 86 us = 6.0 TB/s.
+constexpr int kBwdThreads = 256, kBwdWarps = kBwdThreads / 32;
+
 struct BwdArgs {
     const void *logits;
     void *dlogits;
@@ -594,11 +602,11 @@ struct RowTerm {
 };
 
 template <typename T>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kBwdThreads)
 topk_bwd_kernel(const BwdArgs a)
 {
     constexpr int N = Pack<T>::N, U = 2;
-    __shared__ float red[kWarps];
+    __shared__ float red[kBwdWarps];
     __shared__ int ids[2 * kMaxIds];
     __shared__ float gs[2 * kMaxIds];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -619,7 +627,7 @@ topk_bwd_kernel(const BwdArgs a)
     if (last && tid >= 32 && tid - 32 < a.V - head - nvec * N) loose = head + nvec * N + (tid - 32);
     if (a.mask && !a.mask[row]) {
         const uint4 z = make_uint4(0u, 0u, 0u, 0u);
-        for (int i = p0 + tid; i < p1; i += kThreads) st_stream(out + i, z);
+        for (int i = p0 + tid; i < p1; i += kBwdThreads) st_stream(out + i, z);
         if (loose >= 0) Pack<T>::store1(dst + loose, 0.f);
         return;
     }
@@ -630,7 +638,7 @@ topk_bwd_kernel(const BwdArgs a)
     if (vec_in) {
 #pragma unroll
         for (int q = 0; q < U; ++q)
-            if (i0 + q * kThreads < p1) v[q] = ld_stream(in + i0 + q * kThreads);
+            if (i0 + q * kBwdThreads < p1) v[q] = ld_stream(in + i0 + q * kBwdThreads);
     }
     // the given tokens and the sum of their gradients
     const int total = a.n + a.k;
@@ -649,7 +657,7 @@ topk_bwd_kernel(const BwdArgs a)
     const int bad = __syncthreads_or((unsigned)id >= (unsigned)a.V);
     float G = 0.f;
 #pragma unroll
-    for (int w = 0; w < kWarps; ++w) G += red[w];
+    for (int w = 0; w < kBwdWarps; ++w) G += red[w];
     RowTerm r;
     {
         const float lse = a.lse[row], h = a.dentropy ? a.dentropy[row] : 0.f, H = a.dentropy ? a.entropy[row] : 0.f;
@@ -663,15 +671,15 @@ topk_bwd_kernel(const BwdArgs a)
         if (bad) r.a0 = __uint_as_float(0x7fffffffu);
     }
     if (bad && chunk == 0 && tid == 0 && a.status) atomicOr(a.status, PPO_DEV_BAD_TOKEN);
-    for (int i = i0; i < p1; i += U * kThreads) {
+    for (int i = i0; i < p1; i += U * kBwdThreads) {
         if (vec_in && i != i0) {
 #pragma unroll
             for (int q = 0; q < U; ++q)
-                if (i + q * kThreads < p1) v[q] = ld_stream(in + i + q * kThreads);
+                if (i + q * kBwdThreads < p1) v[q] = ld_stream(in + i + q * kBwdThreads);
         }
 #pragma unroll
         for (int q = 0; q < U; ++q) {
-            const int p = i + q * kThreads;
+            const int p = i + q * kBwdThreads;
             if (p >= p1) continue;
             float x[N];
             if (vec_in) {
@@ -706,11 +714,11 @@ static int launch_bwd(BwdArgs a, int64_t rows, cudaStream_t s)
     // a block's share: 2048 packs (32 KB in, 32 KB out) once there are blocks for every place on the SMs, so that its reads
     // of the row's tokens and gradients weigh little (1024: 95 us instead of 86 for 3392 bf16 rows); else 1024, for more
     // blocks (4.7 us instead of 5.6 for 53 rows)
-    a.packs_per_chunk = (rows * (nvec / (8 * kThreads) + 1) >= 8 * 148 ? 8 : 4) * kThreads;
+    a.packs_per_chunk = (rows * (nvec / (8 * kBwdThreads) + 1) >= 8 * 148 ? 8 : 4) * kBwdThreads;
     a.chunks = nvec > 0 ? (nvec + a.packs_per_chunk - 1) / a.packs_per_chunk : 1;
     const int64_t blocks = rows * a.chunks;
     if (blocks >= ((int64_t)1 << 31)) return PPO_ERR_SHAPE;
-    topk_bwd_kernel<T><<<(unsigned)blocks, kThreads, 0, s>>>(a);
+    topk_bwd_kernel<T><<<(unsigned)blocks, kBwdThreads, 0, s>>>(a);
     return launch_status();
 }
 

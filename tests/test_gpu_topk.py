@@ -358,3 +358,55 @@ def test_best_elements_at_regular_distances(P, dt, rows, V):
     full = P.logprob_topk(x, None, 100, 1.0)["top_ids"].long()
     want = torch.sort(x.float(), dim=1, descending=True, stable=True).indices[:, :100]
     assert torch.equal(full, want)
+
+
+@pytest.mark.parametrize("dtype,rows,V,k,n,pad,skip", [
+    (F32, 600, 1, 1, 1, 0, 0), (BF16, 700, 7, 7, 2, 1, 1), (BF16, 601, 33, 32, 1, 0, 3), (F32, 600, 513, 32, 128, 3, 1),
+    (BF16, 1500, 1025, 31, 1, 0, 0), (F32, 600, 8190, 20, 1, 0, 0), (BF16, 600, 16391, 5, 1, 1, 0), (BF16, 600, 16400, 5, 1, 0, 0),
+    (F32, 592, 4100, 33, 1, 0, 0), (BF16, 591, 4100, 32, 1, 0, 0), (BF16, 600, 4100, 0, 1, 0, 0)])
+def test_topk_of_many_rows_of_little_length(P, dtype, rows, V, k, n, pad, skip):
+    """(either side of 592 rows, 16384 bf16 elements and 32 alternatives, where blocks of another size take over)"""
+    mask = (torch.arange(rows) % 3 != 1).to(torch.uint8).cuda()
+    _check(P, _logits(rows, V, dtype, pad, skip, seed=9), _tokens(rows, V, n), k, mask=mask)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("V", [150, 1200, 8001])
+def test_many_short_rows_where_selection_is_hard(P, dtype, V):
+    base = _logits(600, V, dtype, seed=8)
+    low = torch.finfo(dtype).min
+    at = torch.arange(V, device="cuda")
+    base[0::12] = 0.25
+    base[1::12] = -torch.inf
+    base[1::12, V - 5:V - 2] = torch.tensor([1.0, 2.0, 1.0], device="cuda", dtype=dtype)
+    base[2::12] = low
+    base[2::12, 100:104] = 3.0
+    base[3::12, 7] = -torch.inf
+    base[3::12, V // 2] = low
+    base[4::12] = torch.linspace(-20, 20, V, device="cuda").to(dtype)
+    base[5::12] = torch.linspace(20, -20, V, device="cuda").to(dtype)
+    base[6::12] = (at % 3).to(dtype)
+    base[7::12] = 0.0
+    base[7::12, ::2] = -0.0
+    base[8::12, 0] = 300.0
+    base[9::12] *= 20
+    base[9::12, V - 1] = 2000.0
+    base[10::12, :8] = -torch.inf
+    base[11::12, 40:] = -torch.inf
+    _check(P, base, _tokens(600, V, 2), 32)
+
+
+def test_many_short_rows_without_a_distribution(P):
+    x = _logits(600, 2000, BF16, seed=10)
+    x[5, 3] = torch.nan
+    x[6, 1999] = torch.inf
+    x[7] = -torch.inf
+    ws = P.new_workspace(P.workspace_bytes(600, 1, 2000))
+    o = P.logprob_topk(x, _tokens(600, 2000)[:, 0].contiguous(), 9, TAU, workspace=ws)
+    torch.cuda.synchronize()
+    assert P.last_device_status(ws) == 8
+    bad = torch.zeros(600, dtype=torch.bool, device="cuda")
+    bad[5:8] = True
+    assert (o["top_ids"][bad] == -1).all() and (o["top_ids"][~bad] >= 0).all()
+    for name in ("logprob", "entropy", "lse"):
+        assert torch.equal(torch.isnan(o[name]), bad), name
