@@ -417,12 +417,26 @@ __device__ __forceinline__ void copy4(float *dst, const float *src, bool valid)
 template <typename T>
 __device__ __forceinline__ void store_rows(const unsigned char *stage, T *out, int64_t ldc, int m, int M, int n, int N)
 {
-    constexpr int E = 16 / sizeof(T), W = 128 / sizeof(T);     // elements per 16 bytes, per row
+    // (four rows of reads before their writes: 3091 x 25533 x 1739, bf16, 190 us, one row at a time 254; N = 25536: 162 us)
+    constexpr int E = 16 / sizeof(T), W = 128 / sizeof(T), Q = W / 32, R = 4;     // elements per 16 bytes, per row; of a lane
     const int lane = threadIdx.x & 31;
-    for (int r = 0; r < 32 && m + r < M; ++r)
-        for (int e = lane; e < W && n + e < N; e += 32)
-            out[(int64_t)(m + r) * ldc + n + e] =
-                *reinterpret_cast<const T *>(stage + r * 128 + (((e / E) ^ (r & 7)) << 4) + (e % E) * sizeof(T));
+    T *to = out + (int64_t)m * ldc + n + lane;
+#pragma unroll 1
+    for (int r0 = 0; r0 < 32; r0 += R) {
+        T v[R][Q];
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int q = 0; q < Q; ++q) {
+                const int e = q * 32 + lane;
+                v[r][q] = *reinterpret_cast<const T *>(stage + (r0 + r) * 128 + (((e / E) ^ ((r0 + r) & 7)) << 4) + (e % E) * sizeof(T));
+            }
+#pragma unroll
+        for (int r = 0; r < R; ++r, to += ldc)
+#pragma unroll
+            for (int q = 0; q < Q; ++q)
+                if (m + r0 + r < M && n + q * 32 + lane < N) to[q * 32] = v[r][q];
+    }
 }
 
 template <bool PER_ROW>
