@@ -15,11 +15,11 @@
 //   the lowest index and the order in which candidates arrive does not matter.
 // A slice whose candidates overflow the list (rows of equal values, fewer than k unbanned tokens) is selected by
 // radix passes over it instead.
-// Few rows: a cluster of CL blocks shares a row; each selects the k best of its slice, and block 0 merges the sorted
-// lists and the sums through distributed shared memory.
+// Few rows: a cluster of CL blocks shares a row; each selects the k best of its slice, and block 0 ranks what is
+// in their lists and merges the sums, through distributed shared memory.
 // Bound: the read of the logits (V * size bytes per row; without alternatives 3392 x 50304 bf16 57 us = 6.0 TB/s), and behind it
 // the selection, which the other rows of an SM have to cover: k = 5: 64 us, k = 20: 68 us, half the rows masked, k = 5: 38 us =
-// 4.5 TB/s (1.4 rounds of blocks); one row, k = 20: 9 us.
+// 4.5 TB/s (1.4 rounds of blocks); one row, k = 20: 7.7 us.
 #include <cooperative_groups.h>
 
 #include "ppo_rows.cuh"
@@ -29,6 +29,7 @@ namespace topk {
 
 namespace cg = cooperative_groups;
 
+constexpr int kSharedK = 32;      // from here on the blocks of a cluster share a threshold
 constexpr int kMaxIds = 128;       // largest k and largest number of given tokens
 
 struct Args {
@@ -75,7 +76,7 @@ struct Smem {
     Segment seg[kParts][kThreads];
     float red[96];
     SoftmaxState st;
-    uint32_t threshold;
+    uint32_t threshold, second_threshold;
     int n_cand, n_best, bin, need;
 };
 
@@ -221,7 +222,7 @@ __device__ __noinline__ void select_by_radix(const T *src, int e0, int e1, int k
 
 // Warp 0: a threshold that at least k and at most a few more of the threads' maxima reach.
 template <typename S>
-__device__ __forceinline__ void choose_threshold(int k, S &sm)
+__device__ __forceinline__ void choose_threshold(int k, const S &sm, uint32_t &threshold)
 {
     constexpr int Q = S::kThreads / 32;
     const int lane = threadIdx.x & 31;
@@ -248,7 +249,7 @@ __device__ __forceinline__ void choose_threshold(int k, S &sm)
         }
     }
     // maxima are clamped at kNegBig: at that level everything is a candidate
-    if (lane == 0) sm.threshold = lo <= ordered(0.99f * kNegBig) ? 0u : lo;
+    if (lane == 0) threshold = lo <= ordered(0.99f * kNegBig) ? 0u : lo;
 }
 
 // the elements of a pack that reach the threshold into the list of candidates
@@ -270,15 +271,34 @@ __device__ __forceinline__ void take_candidates(const uint4 &v, int at, int head
         }
 }
 
-// The slice's best min(k, length) elements into sm.best, sorted. The threshold is known; loose elements are in sm.cand
+// the `want` best of n candidates into sm.best, sorted
+template <typename S>
+__device__ __forceinline__ void rank_candidates(int n, int want, S &sm)
+{
+    for (int i = threadIdx.x; i < n; i += S::kThreads) {
+        const unsigned long long key = sm.cand[i];
+        int rank = 0;
+        int j = 0;
+        for (; j + 4 <= n; j += 4) {
+            rank += sm.cand[j] > key;
+            rank += sm.cand[j + 1] > key;
+            rank += sm.cand[j + 2] > key;
+            rank += sm.cand[j + 3] > key;
+        }
+        for (; j < n; ++j) rank += sm.cand[j] > key;
+        if (rank < want) sm.best[rank] = key;
+    }
+}
+
+// The slice's best elements into sm.best, sorted: those that reach the threshold, k at most. Loose elements are in sm.cand
 // already. `span`: packs of a segment.
 template <typename T, typename S>
-__device__ __forceinline__ void select_best(const T *src, const Slice &sl, int span, int k, S &sm)
+__device__ __forceinline__ void select_best(const T *src, const Slice &sl, int span, int k, uint32_t threshold, S &sm)
 {
     constexpr int kThreads = S::kThreads, kParts = S::kParts;
     const int tid = threadIdx.x, lane = tid & 31;
     const int want = min(k, sl.e1 - sl.e0);
-    const float thr = sm.threshold == 0u ? -INFINITY : unordered(sm.threshold);
+    const float thr = threshold == 0u ? -INFINITY : unordered(threshold);
     const uint4 *body = reinterpret_cast<const uint4 *>(src + sl.head);
     // a thread re-reads the one pack of its segments with candidates in no other
     uint4 v[kParts];
@@ -317,20 +337,8 @@ __device__ __forceinline__ void select_best(const T *src, const Slice &sl, int s
         select_by_radix(src, sl.e0, sl.e1, want, sm);
     }
     const int n = sm.n_cand;
-    for (int i = tid; i < n; i += kThreads) {
-        const unsigned long long key = sm.cand[i];
-        int rank = 0;
-        int j = 0;
-        for (; j + 4 <= n; j += 4) {
-            rank += sm.cand[j] > key;
-            rank += sm.cand[j + 1] > key;
-            rank += sm.cand[j + 2] > key;
-            rank += sm.cand[j + 3] > key;
-        }
-        for (; j < n; ++j) rank += sm.cand[j] > key;
-        if (rank < want) sm.best[rank] = key;
-    }
-    if (tid == 0) sm.n_best = want;
+    rank_candidates(n, want, sm);
+    if (tid == 0) sm.n_best = min(n, want);
     __syncthreads();
 }
 
@@ -459,7 +467,11 @@ topk_kernel(const Args a)
         if (tid == 0) sm.n_cand = sl.loose;
     }
     __syncthreads();
-    if (warp == 0 && a.k > 0) choose_threshold(a.k, sm);
+    // With several blocks and k large, each finds a threshold that k / CL of its threads reach; the lowest of them has at least
+    // k elements of the row above it, and the lists stay short (one row of 50304, k = 128: 9.4 us, with lists of k from each block
+    // 40; from k = 32 on it is worth the exchange: k = 20, 120 rows: 10.6 us with it, 10.0 without).
+    const bool shared = CL > 1 && a.k >= kSharedK;
+    if (warp == 0 && a.k > 0) choose_threshold(shared ? (a.k + CL - 1) / CL : a.k, sm, sm.threshold);
     if (warp == 1) {
         st.init();
         if (lane < kWarps) { st.m = sm.red[lane]; st.s = sm.red[32 + lane]; st.u = sm.red[64 + lane]; }
@@ -468,10 +480,24 @@ topk_kernel(const Args a)
     }
     __syncthreads();
     st = sm.st;
+    uint32_t threshold = a.k > 0 ? sm.threshold : 0u;
+    if (shared) {
+        cg::cluster_group cluster = cg::this_cluster();
+        cluster.sync();
+        const uint32_t of_lane = *cluster.map_shared_rank(&sm.threshold, lane % CL);
+        threshold = __reduce_min_sync(0xffffffffu, of_lane);
+        const int alive = __popc(__ballot_sync(0xffffffffu, of_lane != 0u)) / (32 / CL);
+        if (threshold == 0u && alive > 0) {                // blocks of banned tokens: the others find k among themselves
+            if (warp == 0) choose_threshold((a.k + alive - 1) / alive, sm, sm.second_threshold);
+            cluster.sync();
+            const uint32_t second = *cluster.map_shared_rank(&sm.second_threshold, lane % CL);
+            threshold = __reduce_min_sync(0xffffffffu, of_lane != 0u ? second : 0xffffffffu);
+        }
+    }
     if (a.k > 0) {
         // (false for NaN; a slice without weight, s = 0, is selected from)
         if (st.s < 1.0e37f) {
-            select_best(src, sl, span, a.k, sm);
+            select_best(src, sl, span, a.k, threshold, sm);
         } else {
             if (tid == 0) sm.n_best = 0;
             __syncthreads();
@@ -481,28 +507,30 @@ topk_kernel(const Args a)
         cg::cluster_group cluster = cg::this_cluster();
         cluster.sync();
         if (rank == 0) {
-            for (int r = 1; r < CL; ++r) st = merge(st, *cluster.map_shared_rank(&sm.st, r));
-            // lists into this block's candidates, k slots each, then ranks by counting with bisection
-            int lens[CL];
-            for (int r = 0; r < CL; ++r) lens[r] = a.k > 0 ? *cluster.map_shared_rank(&sm.n_best, r) : 0;
-            for (int i = tid; i < CL * a.k; i += kThreads) {
-                const int r = i / a.k, q = i - r * a.k;
-                sm.cand[i] = q < lens[r] ? cluster.map_shared_rank(&sm.best[0], r)[q] : 0ull;
+            st.init();
+            int len = 0;
+            if (lane < CL) {
+                st = *cluster.map_shared_rank(&sm.st, lane);
+                if (a.k > 0) len = *cluster.map_shared_rank(&sm.n_best, lane);
             }
-            __syncthreads();
-            for (int i = tid; i < CL * a.k; i += kThreads) {
-                const unsigned long long key = sm.cand[i];
-                if (key == 0ull) continue;
-                int pos = 0;
-                for (int r = 0; r < CL; ++r) {             // entries of list r above key (lists descend, keys differ)
-                    int lo = 0, hi = a.k;
-                    while (lo < hi) {
-                        const int mid = (lo + hi) / 2;
-                        if (sm.cand[r * a.k + mid] > key) lo = mid + 1; else hi = mid;
-                    }
-                    pos += lo;
+            st = warp_merge(st);
+            if (a.k > 0) {
+                // warp r fetches the list of block r, to behind those of the blocks before it
+                int end = len;
+#pragma unroll
+                for (int off = 1; off < CL; off *= 2) {
+                    const int before = __shfl_up_sync(0xffffffffu, end, off);
+                    if (lane >= off) end += before;
                 }
-                if (pos < a.k) sm.best[pos] = key;
+                const int n = __shfl_sync(0xffffffffu, end, CL - 1);
+                const int to = __shfl_sync(0xffffffffu, end - len, warp), mine = __shfl_sync(0xffffffffu, len, warp);
+                if (warp < CL) {
+                    const unsigned long long *from = cluster.map_shared_rank(&sm.best[0], warp);
+                    for (int q = lane; q < mine; q += 32) sm.cand[to + q] = from[q];
+                }
+                __syncthreads();
+                rank_candidates(n, a.k, sm);
+                __syncthreads();
             }
         }
         cluster.sync();

@@ -410,3 +410,32 @@ def test_many_short_rows_without_a_distribution(P):
     assert (o["top_ids"][bad] == -1).all() and (o["top_ids"][~bad] >= 0).all()
     for name in ("logprob", "entropy", "lse"):
         assert torch.equal(torch.isnan(o[name]), bad), name
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,V", [(9, 50304), (60, 20011), (130, 9001), (9, 131080)])
+@pytest.mark.parametrize("k", [32, 100, 128])
+def test_few_rows_with_many_alternatives_and_banned_stretches(P, dtype, rows, V, k):
+    """The blocks that share a row agree on a threshold; some of them, or all, may have fewer than their part of the k."""
+    x = _logits(rows, V, dtype, seed=12)
+    at = torch.arange(V, device="cuda")
+    x[0::9, :V // 8 + 20] = -torch.inf                      # the first of eight blocks
+    x[1::9, V // 4:] = -torch.inf                           # all but two of eight
+    x[2::9, 60:] = -torch.inf                               # fewer than k left in all, all of them in the first block
+    x[3::9] = torch.where(at % (V // 70) == 0, x[3::9].float(), -torch.inf).to(dtype)     # about 70 left, everywhere
+    x[4::9, V // 2:] = torch.finfo(dtype).min
+    x[5::9, V // 8:V // 8 + 20] += 30                       # the best of them in one block
+    x[6::9] = torch.where((at < V // 2) | (at > V - 40), x[6::9].float(), -torch.inf).to(dtype)   # a few in the last block
+    x[7::9] = -torch.inf
+    x[7::9, V - 1] = 1.0
+    _check(P, x, _tokens(rows, V), k)
+
+
+def test_nan_in_one_block_of_a_shared_row(P):
+    x = _logits(2, 50304, BF16, seed=13)
+    x[0, 40000] = torch.nan
+    for k in (5, 64):
+        o = P.logprob_topk(x, None, k, TAU)
+        assert (o["top_ids"][0] == -1).all() and torch.isnan(o["lse"][0])
+        want = torch.sort(x[1].float(), descending=True, stable=True).indices[:k]
+        assert torch.equal(o["top_ids"][1].long(), want)
