@@ -344,9 +344,10 @@ __device__ __forceinline__ void select_best(const T *src, const Slice &sl, int s
 
 // (a block to a row: 8 blocks of 256 threads to an SM, 32 registers a thread, hide the selection of some behind the streams
 // of the others better than four loads in flight per thread and 4 blocks do: 38 against 41 us for 3392 bf16 rows, half of them
-// masked, 39 against 46 for 997 fp32; what the stream does not need is therefore loaded behind it)
+// masked, 39 against 46 for 997 fp32; what the stream does not need is therefore loaded behind it. Clusters: four blocks have to
+// fit, two let some of 37 clusters of 8 wait: 36 rows 7.5 us instead of 12)
 template <typename T, int CL, int TH>
-__global__ void __launch_bounds__(TH, CL == 1 ? 2048 / TH : 1)
+__global__ void __launch_bounds__(TH, CL == 1 ? 2048 / TH : 4)
 topk_kernel(const Args a)
 {
     constexpr int kThreads = TH, kWarps = TH / 32, kParts = Smem<CL, TH>::kParts;
@@ -583,7 +584,9 @@ static int launch_any(const Args &a, int64_t rows, cudaStream_t s)
     const int64_t packs = a.V / Pack<T>::N;
     if (rows * 8 <= 2 * 148 && packs >= 8 * 256) return launch<T, 8, 256>(a, rows, s);
     if (rows * 4 <= 2 * 148 && packs >= 4 * 256) return launch<T, 4, 256>(a, rows, s);
-    if (rows * 2 <= 2 * 148 && packs >= 2 * 256) return launch<T, 2, 256>(a, rows, s);
+    // (pairs for more rows if they are long: 250 rows of 50277 fp32 15 us instead of 20; shorter ones lose: 50304 bf16 12
+    // instead of 11)
+    if (rows * 2 <= (packs >= 8192 ? 4 : 2) * 148 && packs >= 2 * 256) return launch<T, 2, 256>(a, rows, s);
     // Short rows, enough of them to fill the SMs, few alternatives: half the threads and twice the blocks on an SM, so that more
     // selections hide each other. bf16, 128 against 256 threads: 3392 x 4096, k = 20: 17 / 23 us, 3392 x 16384: 29 / 36 us; 200 x
     // 16384: 8.6 / 7.5 us; 1000 x 16384, k = 64: 18.7 / 17.2 us; 997 x 50277 fp32 (longer rows), k = 20: 46 / 37 us.

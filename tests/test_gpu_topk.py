@@ -439,3 +439,9 @@ def test_nan_in_one_block_of_a_shared_row(P):
         assert (o["top_ids"][0] == -1).all() and torch.isnan(o["lse"][0])
         want = torch.sort(x[1].float(), descending=True, stable=True).indices[:k]
         assert torch.equal(o["top_ids"][1].long(), want)
+
+
+@pytest.mark.parametrize("rows", [36, 73, 148, 149, 250, 296, 297])
+def test_topk_of_long_fp32_rows_at_every_split(P, rows):
+    x = _logits(rows, 32801, F32, seed=14)
+    _check(P, x, _tokens(rows, 32801), 33)
