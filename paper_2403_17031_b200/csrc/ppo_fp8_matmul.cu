@@ -281,9 +281,10 @@ static int launch_narrow(Args a, const void *A, int64_t lda, const void *B, int6
     int split = 1;
     while (split < 8 && tiles * split * 2 <= narrow_places<MT>() && a.kb_total >= 4 * split) split *= 2;
     if (tiles * split >= ((int64_t)1 << 31)) return PPO_ERR_SHAPE;
-    // Tiles of 16 columns: three stages once the SMs hold more than two blocks each, so that a fourth fits (1 x 50304 x 4096:
-    // 35.0 instead of 36.9 us, 1 x 50304 x 8192: 67.0 instead of 69.9), else four (4 x 16384 x 4096: 16.2 instead of 16.5 us)
-    if constexpr (MT == 16)
+    // Tiles of 16 and 32 columns: three stages once the SMs hold more than two blocks each, so that another fits (1 x 50304 x
+    // 4096: 35.0 instead of 36.9 us, 32 x 50304 x 4096: 40.5 instead of 51, 32 x 38000 x 4096: 32 instead of 52), else four
+    // (4 x 16384 x 4096: 16.2 instead of 16.5 us)
+    if constexpr (MT <= 32)
         if (tiles * split > 2 * 148) return launch_narrow_stages<MT, 3>(a, ma, mb, split, s);
     return launch_narrow_stages<MT, 4>(a, ma, mb, split, s);
 }
