@@ -240,3 +240,10 @@ def test_a_chain_from_hidden_states_to_their_gradient(P):
     w2, w2s = P.fp8_quantize(w, 128)                          # [K, V], for the gradient
     assert torch.equal(w2.float(), wq.float().t()) and torch.equal(w2s, wsc.t())
     _check_matmul(P, M, K, V, 128, F32, (dq, ds, w2, w2s))
+
+
+@pytest.mark.parametrize("out_dtype,block_n", [(F32, 128), (BF16, 1)])
+@pytest.mark.parametrize("M,N,K", [(5, 40000, 1100), (16, 37889, 385), (32, 38017, 700), (17, 40001, 129), (20, 50304, 1024)])
+def test_matmul_of_few_rows_with_a_long_weight(P, M, N, K, out_dtype, block_n):
+    """(more tiles of 128 weight rows than two for each SM)"""
+    _check_matmul(P, M, N, K, block_n, out_dtype)
