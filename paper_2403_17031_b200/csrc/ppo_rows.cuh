@@ -88,6 +88,30 @@ template <> struct Pack<__nv_bfloat16> {
 __device__ __forceinline__ uint4 ld_stream(const uint4 *p) { return __ldcs(p); }
 __device__ __forceinline__ void st_stream(uint4 *p, const uint4 &v) { __stcs(p, v); }
 
+// A logit at or below this (-inf, a masking value; clamped to kNegBig) has weight 0 and must not become the reference of a
+// row's sums: at that magnitude x*c - ref is the rounding error of x*c, up to 2^75, instead of 0.
+constexpr float kNoWeight = -1.0e29f;
+
+// Reference (base-2 units) taken from a pack maximum.
+__device__ __forceinline__ float safe_reference(float xmax, float c) { return xmax > kNoWeight ? xmax * c : 0.f; }
+
+// Start of a sum with a moving reference. The reference is not below what a logit without weight comes to for any temperature
+// up to 1e19, so that none moves it there, and far enough above for 2^(x*c - ref) to be 0 for them. (Logits with weight come to
+// +-2^30 at the most: beyond that fp32 tells no probabilities apart.)
+__device__ __forceinline__ void init_online(SoftmaxState &st)
+{
+    st.init();
+    st.m = -1.0e10f;
+}
+
+// exponent of a clamped logit relative to the reference: finite, or NaN for a NaN (0 * -inf would spoil the entropy's sum)
+__device__ __forceinline__ float exponent_of(float x, float c, float nm)
+{
+    float t;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(t) : "f"(fmaf(x, c, nm)), "f"(kNegBig));
+    return t;
+}
+
 // fold one pack into the running state, moving the reference up when the pack exceeds it
 template <typename T>
 __device__ __forceinline__ void accumulate_online(const uint4 &v, float c, SoftmaxState &st)
@@ -98,12 +122,8 @@ __device__ __forceinline__ void accumulate_online(const uint4 &v, float c, Softm
     if (ymax > st.m) st.rebase(ymax);
     const float nm = -st.m;
 #pragma unroll
-    for (int k = 0; k < Pack<T>::N; ++k) st.add(fmaf(x[k], c, nm));
+    for (int k = 0; k < Pack<T>::N; ++k) st.add(exponent_of(x[k], c, nm));
 }
-
-// Reference (base-2 units) taken from a pack maximum. A pack that holds only -inf (clamped to
-// kNegBig) must not become the reference: at that magnitude x*c - ref no longer cancels exactly.
-__device__ __forceinline__ float safe_reference(float xmax, float c) { return xmax > -1.0e29f ? xmax * c : 0.f; }
 
 // Two independent accumulator pairs relative to a FIXED reference (nm = -reference).
 struct FixedAcc {
@@ -200,7 +220,7 @@ __device__ __forceinline__ SoftmaxState row_statistics(const T *__restrict__ src
             st.u = acc.u0 + acc.u1;
             if (!(st.s < 1.0e37f) || !(fabsf(st.u) < 1.0e37f)) {
                 // overflow (or NaN input): redo this thread's packs with a moving reference
-                st.init();
+                init_online(st);
                 for (i = threadIdx.x; i < nvec; i += THREADS)
                     accumulate_online<T>(STAGE ? stage4[i] : src4[i], c, st);
                 if (!ENTROPY) st.u = 0.f;
@@ -208,6 +228,7 @@ __device__ __forceinline__ SoftmaxState row_statistics(const T *__restrict__ src
         }
     } else {
         T *stage1 = reinterpret_cast<T *>(stage);
+        init_online(st);
         for (int j = threadIdx.x; j < V; j += THREADS) {
             const T raw = src[j];
             if (STAGE) stage1[j] = raw;

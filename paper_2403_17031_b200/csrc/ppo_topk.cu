@@ -400,7 +400,7 @@ topk_kernel(const Args a)
     const float w_max = warp_max(first_max);
     const float m_warp = safe_reference(w_max, a.c), nm = -m_warp;
     // (a warp whose first loads hold no logit with weight has no reference: its sums are marked as overflown)
-    if (w_max <= -1.0e29f) acc.s0 = INFINITY;
+    if (w_max <= kNoWeight) acc.s0 = INFINITY;
 #pragma unroll
     for (int q = 0; q < U; ++q)
         if (i + q * kThreads < sl.p1) accumulate<T>(v[q], i + q * kThreads, a.c, nm, acc, seg);
@@ -442,12 +442,12 @@ topk_kernel(const Args a)
     st.u = acc.u0 + acc.u1;
     if (loose >= 0) st.add(fmaf(x_loose, a.c, nm));
     if (!(st.s < 1.0e37f) || !(fabsf(st.u) < 1.0e37f)) {   // overflow (or NaN / +inf): again with a moving reference
-        st.init();
+        init_online(st);
         for (i = sl.p0 + tid; i < sl.p1; i += kThreads) accumulate_online<T>(body[i], a.c, st);
         if (loose >= 0) {
             const float y = x_loose * a.c;
             if (y > st.m) st.rebase(y);
-            st.add(fmaf(x_loose, a.c, -st.m));
+            st.add(exponent_of(x_loose, a.c, -st.m));
         }
     }
     // within the warp plain sums unless a lane moved its reference, then the eight warps' states by the general rule

@@ -250,3 +250,31 @@ def test_loss_from_logprob_matches_oracle(P, oracle):
     assert abs(got[6] - ent[m.astype(bool)].mean()) < 1e-5
     assert_abs(n * npy(o["dlogprob"]), n * ref["dlogprob"], 1e-4, "n*dlogprob")
     assert_abs(n * npy(o["dvalues"]), n * ref["dvalues"], 1e-4, "n*dvalues")
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("tau", [1.5, 1.7, 2.0, 4.0, 8.0])
+@pytest.mark.parametrize("V,skip", [(1000, 0), (1001, 1), (16384, 0), (50277, 3)])
+def test_banned_logits_at_high_temperatures(P, oracle, dtype, tau, V, skip, lp_engine):
+    """Log-probs, entropy and their gradient with whole stretches of -inf, the first of a row among them, for temperatures above log2(e)."""
+    rows = 24
+    x = torch.zeros(rows * V + skip, dtype=dtype, device="cuda")[skip:].view(rows, V)
+    x.copy_(_rand_logits(rows, V, dtype, seed=V))
+    x[0::4, :V // 2] = -torch.inf
+    x[1::4, V // 3:] = -torch.inf
+    x[2::4, ::2] = -torch.inf
+    x[3::4, V // 4:V // 2] = torch.finfo(dtype).min
+    tok = torch.full((rows,), V // 7 | 1, device="cuda", dtype=torch.int32)
+    tok[0::4] = V - 3
+    lp, ent, lse = P.logprob_entropy(x, tok, tau, want_lse=True)
+    rlp, rent, rlse = oracle.logprob_entropy(host_logits(x), npy(tok), np.float32(tau))
+    assert_abs(npy(lp), rlp, TOL_LOGPROB, "logprob")
+    assert_abs(npy(ent), rent, TOL_LOGPROB, "entropy")
+    assert_abs(npy(lse), rlse, TOL_LOGPROB, "lse")
+    g = torch.ones(rows, device="cuda")
+    d = P.logprob_bwd(x, tok, torch.ones(rows, dtype=torch.uint8, device="cuda"), g, tau, P.new_workspace(P.workspace_bytes(rows, 1, V)))
+    z = x.double() / float(np.float32(tau))
+    want = -torch.softmax(z, 1)
+    want[torch.arange(rows), tok.long()] += 1
+    want /= float(np.float32(tau))
+    assert_grad(npy(d["dlogits"].float()), npy(want), dtype == torch.bfloat16, "dlogits")

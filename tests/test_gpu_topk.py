@@ -445,3 +445,64 @@ def test_nan_in_one_block_of_a_shared_row(P):
 def test_topk_of_long_fp32_rows_at_every_split(P, rows):
     x = _logits(rows, 32801, F32, seed=14)
     _check(P, x, _tokens(rows, 32801), 33)
+
+
+def _hard_rows(V, dtype, seed):
+    """Twelve kinds of rows: equal, tied, sorted, peaked or mostly banned values."""
+    base = _logits(12, V, dtype, seed=seed)
+    at, low = torch.arange(V, device="cuda"), torch.finfo(dtype).min
+    base[0] = 0.25
+    base[1] = -torch.inf
+    base[1, V - 5:V - 2] = torch.tensor([1.0, 2.0, 1.0], device="cuda", dtype=dtype)
+    base[2] = low
+    base[2, 100:104] = 3.0
+    base[3, 7], base[3, V // 2] = -torch.inf, low
+    base[4] = torch.linspace(-20, 20, V, device="cuda").to(dtype)
+    base[5] = torch.linspace(20, -20, V, device="cuda").to(dtype)
+    base[6] = (at % 3).to(dtype)
+    base[7, ::2] = low
+    base[8, 0] = 300.0
+    base[9, V - 1] = 2000.0
+    base[10, :V // 2] = -torch.inf
+    base[11, 40:] = -torch.inf
+    return base
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("tau", [1.5, 1.7, 2.0, 4.0, 8.0])
+@pytest.mark.parametrize("each,V,pad,skip", [(1, 50304, 0, 0), (3, 20001, 0, 1), (10, 9001, 0, 0), (20, 9001, 3, 2), (60, 4100, 0, 0)])
+def test_banned_stretches_at_high_temperatures(P, dtype, tau, each, V, pad, skip):
+    """Above log2(e) a masked logit times log2(e) / temperature lies nearer to 0 than the value it was clamped to. Each of the kernel's
+    splits of a row (1, 2, 4 and 8 blocks, blocks of 128 threads), aligned and odd rows."""
+    x = _logits(12 * each, V, dtype, pad, skip)
+    x.copy_(_hard_rows(V, dtype, 15).repeat(each, 1))
+    _check(P, x, _tokens(12 * each, V, 2), 30, tau=tau)
+    x -= 400                                                   # (keeps -inf; bf16's lowest value stays where it is too)
+    _check(P, x, _tokens(12 * each, V, 2), 30, tau=tau)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("tau", [1.5, 2.0, 2.8853900817779268])
+def test_rows_without_a_distribution_at_high_temperatures(P, dtype, tau):
+    """(the last temperature is 2 log2(e): its factor 0.5 scales exactly, without a rounding error that gives the row away)"""
+    x = _logits(6, 5001, dtype)
+    x[0, 4321] = torch.nan
+    x[1, 0] = torch.inf
+    x[2] = -torch.inf
+    x[3] = torch.finfo(dtype).min
+    x[5] = -torch.inf
+    x[5, 5000] = torch.nan                                     # a NaN among nothing but banned logits
+    _check(P, x, _tokens(6, 5001), 9, tau=tau, status=8)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("tau", [2.0, 8.0])
+@pytest.mark.parametrize("rows,k", [(9, 20), (9, 128), (60, 64)])
+def test_few_rows_with_banned_blocks_at_high_temperatures(P, dtype, tau, rows, k):
+    V = 50304
+    x = _logits(rows, V, dtype, seed=16)
+    x[0::4, :V // 8 + 20] = -torch.inf
+    x[1::4, V // 4:] = torch.finfo(dtype).min
+    x[2::4, 60:] = -torch.inf
+    x[3::4] = torch.where(torch.arange(V, device="cuda") % (V // 70) == 0, x[3::4].float(), -torch.inf).to(dtype)
+    _check(P, x, _tokens(rows, V), k, tau=tau)
