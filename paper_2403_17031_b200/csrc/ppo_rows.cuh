@@ -104,6 +104,11 @@ __device__ __forceinline__ void init_online(SoftmaxState &st)
     st.m = -1.0e10f;
 }
 
+// Sums relative to a fixed reference above this are taken again with a moving one. A state's sums may be merged into a state whose
+// reference lies further up than fp32's smallest normal number (2^-126, where ex2 returns 0): what is lost then is at most 2^80 of
+// 2^126, and products of the sums with the distance of two references (2^31 at most) stay finite.
+constexpr float kSumLimit = 1.2e24f;
+
 // exponent of a clamped logit relative to the reference: finite, or NaN for a NaN (0 * -inf would spoil the entropy's sum)
 __device__ __forceinline__ float exponent_of(float x, float c, float nm)
 {
@@ -160,9 +165,9 @@ __device__ __forceinline__ void accumulate_fixed(const uint4 &v, float c, float 
 // Fast path: the softmax sums do not need the exact maximum as reference, only one that keeps
 // 2^(y - ref) inside fp32 range. Every thread of the row uses the same fixed reference m_common
 // (see row_reference) and never moves it, which removes the per-pack maximum, compare and rescale
-// from the inner loop and lets the block merge its threads by plain addition. If a later element exceeds the reference by more than ~2^127 the sum overflows to
-// inf, and a -inf logit turns the entropy sum into NaN (0 * -inf); both are detected after the loop
-// and the thread redoes its packs with the clamped online update.
+// from the inner loop and lets the block merge its threads by plain addition. If a later element lies so
+// far above the reference that a sum passes kSumLimit, or a -inf logit turns the entropy sum into NaN (0 * -inf),
+// it is detected after the loop and the thread redoes its packs with the clamped online update.
 // Common reference of a row for the vector path: the maximum of the row's first pack (every thread
 // reads the same 16 bytes), in base-2 units.
 template <typename T>
@@ -218,7 +223,7 @@ __device__ __forceinline__ SoftmaxState row_statistics(const T *__restrict__ src
             }
             st.s = acc.s0 + acc.s1;
             st.u = acc.u0 + acc.u1;
-            if (!(st.s < 1.0e37f) || !(fabsf(st.u) < 1.0e37f)) {
+            if (!(st.s < kSumLimit) || !(fabsf(st.u) < kSumLimit)) {
                 // overflow (or NaN input): redo this thread's packs with a moving reference
                 init_online(st);
                 for (i = threadIdx.x; i < nvec; i += THREADS)

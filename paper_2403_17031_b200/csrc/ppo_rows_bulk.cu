@@ -242,10 +242,10 @@ struct ThreadStats {
         acc.s.y *= a;
         m = nm;
     }
-    // the sums left fp32 range, or a -inf/NaN logit turned the entropy sum into NaN
+    // the sums left the range in which they can be merged, or a -inf/NaN logit turned the entropy sum into NaN
     __device__ __forceinline__ bool broken() const
     {
-        return !(acc.s.x + acc.s.y < 1.0e35f) || !(fabsf(acc.u.x + acc.u.y) < 1.0e35f);
+        return !(acc.s.x + acc.s.y < kSumLimit) || !(fabsf(acc.u.x + acc.u.y) < kSumLimit);
     }
     // slow path for one pack: clamped values, reference moved up to the pack maximum when needed
     __device__ __forceinline__ void pack_safe(const uint4 &v, float c)

@@ -441,7 +441,7 @@ topk_kernel(const Args a)
     st.s = acc.s0 + acc.s1;
     st.u = acc.u0 + acc.u1;
     if (loose >= 0) st.add(fmaf(x_loose, a.c, nm));
-    if (!(st.s < 1.0e37f) || !(fabsf(st.u) < 1.0e37f)) {   // overflow (or NaN / +inf): again with a moving reference
+    if (!(st.s < kSumLimit) || !(fabsf(st.u) < kSumLimit)) {   // too far above (or NaN / +inf): again with a moving reference
         init_online(st);
         for (i = sl.p0 + tid; i < sl.p1; i += kThreads) accumulate_online<T>(body[i], a.c, st);
         if (loose >= 0) {

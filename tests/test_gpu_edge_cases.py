@@ -278,3 +278,23 @@ def test_banned_logits_at_high_temperatures(P, oracle, dtype, tau, V, skip, lp_e
     want[torch.arange(rows), tok.long()] += 1
     want /= float(np.float32(tau))
     assert_grad(npy(d["dlogits"].float()), npy(want), dtype == torch.bfloat16, "dlogits")
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V", [1000, 1001, 16384, 50304])
+def test_logits_that_are_masked_softly(P, oracle, dtype, V, lp_engine):
+    """Most of a row, its first elements among them, around 2^-126 of the rest: references so far apart that fp32 cannot scale the sums
+    that were taken with one to the other."""
+    g = torch.Generator().manual_seed(20)
+    for base in (-60, -78, -80, -82, -83, -83.5, -84, -86, -88, -120):
+        x = torch.full((8, V), float(base))
+        for r in range(8):
+            x[r, 8 + torch.randperm(V - 8, generator=g)[:min(1000, V // 4)]] = 0.0
+            x[r, [0, 9, V // 2, V - 1][r % 4]] = 4.25
+        x = x.to(dtype).cuda()
+        tok = torch.full((8,), V // 2, device="cuda", dtype=torch.int32)
+        lp, ent, lse = P.logprob_entropy(x, tok, 1.0, want_lse=True)
+        rlp, rent, rlse = oracle.logprob_entropy(host_logits(x), npy(tok), np.float32(1.0))
+        assert_abs(npy(lp), rlp, TOL_LOGPROB, "logprob at %s" % base)
+        assert_abs(npy(ent), rent, TOL_LOGPROB, "entropy at %s" % base)
+        assert_abs(npy(lse), rlse, TOL_LOGPROB, "lse at %s" % base)

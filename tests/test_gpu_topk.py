@@ -506,3 +506,24 @@ def test_few_rows_with_banned_blocks_at_high_temperatures(P, dtype, tau, rows, k
     x[2::4, 60:] = -torch.inf
     x[3::4] = torch.where(torch.arange(V, device="cuda") % (V // 70) == 0, x[3::4].float(), -torch.inf).to(dtype)
     _check(P, x, _tokens(rows, V), k, tau=tau)
+
+
+def _soft_masked_rows(V, dtype, base, best, seed):
+    """[8, V]: all logits at `base` but for some hundreds at 0, in the whole row or its second half, and one at `best`."""
+    g = torch.Generator().manual_seed(seed)
+    x = torch.full((8, V), float(base))
+    for r in range(8):
+        first = V // 2 if r >= 3 else 0
+        x[r, first + torch.randperm(V - first, generator=g)[:V // 30]] = 0.0
+        x[r, [0, V - 2, V // 2, 3][r % 4]] = best
+    return x.to(dtype).cuda()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("each,V", [(1, 50304), (12, 9000), (40, 9001), (90, 4096)])
+def test_logits_that_are_masked_softly(P, dtype, each, V):
+    """Bases around 2^-126 of the rest: references of different warps so far apart that fp32 cannot scale one's sums to the other's."""
+    for base, best in ((-60, 4.25), (-76, 12), (-78, 10), (-79, 9), (-80, 8), (-80, 12), (-82, 4.25), (-83.5, 4.25), (-85, 4.25), (-88, 4.25),
+                       (-120, 4.25), (-300, 4.25)):
+        x = _soft_masked_rows(V, dtype, base, best, 19).repeat(each, 1)
+        _check(P, x, _tokens(8 * each, V), 20, tau=1.0)
