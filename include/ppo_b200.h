@@ -431,9 +431,11 @@ int ppo_lmhead_bwd(const void *H, const void *W, int64_t M, int64_t K, int64_t V
  *   mask   nullable [rows] u8: rows with 0 are not read; their ids are -1, their other outputs 0
  *   top_ids [rows, k] i32 with top_logprob [rows, k] f32 (k = 0: both unused), 0 <= k <= min(PPO_TOPK_MAX, V)
  *   entropy, lse  nullable [rows] f32;  workspace nullable (status word)
- * Logits of -inf or below -1e30 have probability 0; they still appear among the alternatives, in the order of their
- * values, when fewer than k others are left.  A row with a NaN, a +inf or no logit above -1e30 has NaN outputs and
- * ids -1 and sets PPO_DEV_BAD_ROW; a token outside [0, V) gives a NaN log-prob and sets PPO_DEV_BAD_TOKEN.
+ * Logits of -inf or at most -1e29 have probability 0 (temperatures up to 1e19); they still appear among the
+ * alternatives, in the order of their values, when fewer than k others are left.  A row with a NaN or a +inf, or whose
+ * largest logit lies outside +-7.4e8 temperature (2^30 in the base-2 units of the sums; one without a logit above -1e29
+ * does), has NaN outputs and ids -1 and sets PPO_DEV_BAD_ROW; a token outside [0, V) gives a NaN log-prob and sets
+ * PPO_DEV_BAD_TOKEN.
  * Errors: PPO_ERR_DTYPE, PPO_ERR_SHAPE, PPO_ERR_PARAM (temperature), PPO_ERR_NULL, PPO_ERR_ALIGN.  rows == 0 is a
  * successful no-op.  Rows whose k-th largest values are many equal ones (constant rows, fewer than k logits left
  * unbanned) take a slower exact selection.

@@ -527,3 +527,42 @@ def test_logits_that_are_masked_softly(P, dtype, each, V):
                        (-120, 4.25), (-300, 4.25)):
         x = _soft_masked_rows(V, dtype, base, best, 19).repeat(each, 1)
         _check(P, x, _tokens(8 * each, V), 20, tau=1.0)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,V", [(24, 50304), (300, 9001)])
+def test_logits_of_great_magnitude(P, dtype, rows, V):
+    """Up to 7e8 temperature: as accurate as fp32 outputs of that size are; above: no distribution, in either direction. (The factor
+    log2(e) / temperature is rounded to 24 bits, which moves a log-prob by up to 2^-24 of its logit: the second term of _same; here the
+    terms of a log-prob are far larger than itself, so it is taken of those.)"""
+    x = _logits(rows, V, dtype, seed=17, scale=1.0)
+    scale = torch.tensor([1e3, 1e5, 1e7, 6e8, 1e9, 1e10, 1e13, 1e20], device="cuda").repeat(rows // 4)[:rows, None]
+    sign = torch.where(torch.arange(rows, device="cuda") % 16 < 8, 1.0, -1.0)[:, None]
+    x.copy_((x.float().abs() * 1e-4 + 0.9).clamp_max(1.0) * scale * sign)      # all of a row near its largest
+    o = P.logprob_topk(x, _tokens(rows, V), 20, 1.0)
+    bad = (x.float().max(1).values.abs() > 7.45e8).tolist()
+    ids = torch.sort(x.float(), dim=1, descending=True, stable=True).indices[:, :20]
+    z = x.double()
+    w = z.logsumexp(1)
+    assert any(bad) and not all(bad)
+    for r in range(rows):
+        if bad[r]:
+            assert (o["top_ids"][r] == -1).all() and torch.isnan(o["lse"][r]) and torch.isnan(o["top_logprob"][r]).all(), r
+            continue
+        assert torch.equal(o["top_ids"][r].long(), ids[r]), r
+        tol = TOL_LOGPROB + 2.0 ** -23 * float(w[r].abs())
+        assert abs(float(o["lse"][r]) - float(w[r])) <= tol, r
+        spread = float(z[r].max() - z[r].min())
+        d = (o["top_logprob"][r].double() - (z[r][ids[r]] - w[r])).abs().max()
+        assert float(d) <= TOL_LOGPROB + 2.0 ** -23 * spread, r
+
+
+def test_rows_of_great_magnitude_at_a_tiny_temperature(P):
+    """The same limit on logits / temperature, and masked logits whose quotient leaves fp32's range."""
+    x = _logits(8, 9001, F32, seed=18, scale=1e-3)
+    x[:, ::3] = -torch.inf
+    x[::2, 1::3] = torch.finfo(F32).min
+    for tau in (1e-6, 1e-9, 1e-11):
+        _check(P, x, _tokens(8, 9001), 10, tau=tau)
+    o = P.logprob_topk(x, None, 10, 1e-13)
+    assert (o["top_ids"] == -1).all() and torch.isnan(o["lse"]).all()
