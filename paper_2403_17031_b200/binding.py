@@ -609,6 +609,12 @@ def _count(t: Optional[torch.Tensor], rows: int, per_row, name: str) -> int:
     return n
 
 
+def check_mask(mask: torch.Tensor, rows: int, device: torch.device):
+    """Raises unless mask is a contiguous [rows] uint8 tensor (any shape of that many elements) on the device."""
+    _count(mask, rows, 1, "mask")
+    _addr(mask, torch.uint8, device.index, "mask")
+
+
 def logprob_topk(logits: torch.Tensor, tokens: Optional[torch.Tensor], k: int, temperature: float,
                  mask: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, out=None):
     """Log-probs of given tokens, entropy, log-sum-exp and the k most likely alternatives of logits [..., V].

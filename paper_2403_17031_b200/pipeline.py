@@ -163,6 +163,7 @@ class Fp8LMHead:
     def __init__(self, W: torch.Tensor, M: int, k: int, temperature: float, n: int = 1, backward: bool = False):
         K, V = W.shape
         self.M, self.K, self.V, self.k, self.n, self.temperature = M, K, V, k, n, float(temperature)
+        self.backward = backward
         dev, f32, f8 = W.device, torch.float32, torch.float8_e4m3fn
         pitch = lambda cols: -(-cols // 16) * 16
         operand = lambda cols: (torch.empty((M, pitch(cols)), dtype=f8, device=dev)[:, :cols],
@@ -183,19 +184,36 @@ class Fp8LMHead:
             self.dlogits = torch.empty((M, pitch(V)), dtype=torch.bfloat16, device=dev)[:, :V]
             self.dlogits_q = operand(V)
             self.dhidden = torch.empty((M, K), dtype=torch.bfloat16, device=dev)
+            self.mask = torch.ones(M, dtype=torch.uint8, device=dev)          # of the last score()
+            self._mask_bwd = torch.empty_like(self.mask)
             self._scratch_bwd = scratch(K, V)
 
     def score(self, H, tokens, mask=None):
         """H [M, K], tokens [M] or [M, n] int32, mask [M] u8 (rows with 0 are scored as 0, ids -1). Returns the dict of
-        logprob [M, n], entropy, lse [M], top_ids, top_logprob [M, k]."""
+        logprob [M, n], entropy, lse [M], top_ids, top_logprob [M, k]. With backward=True the mask is kept (copied) for
+        grad_hidden()."""
         _b.fp8_quantize(H, 1, out=self.hidden)
         _b.fp8_matmul(*self.hidden, *self.weight, workspace=self.workspace, out=self.logits, scratch=self._scratch)
-        return _b.logprob_topk(self.logits, tokens, self.k, self.temperature, mask=mask, workspace=self.workspace, out=self.out)
+        _b.logprob_topk(self.logits, tokens, self.k, self.temperature, mask=mask, workspace=self.workspace, out=self.out)
+        if self.backward:
+            if mask is None:
+                self.mask.fill_(1)
+            else:
+                torch.ne(mask.view(self.M), 0, out=self.mask)
+        return self.out
 
     def grad_hidden(self, tokens, dlogprob, dtop_logprob=None, dentropy=None, dlse=None, top_ids=None, mask=None):
-        """Gradients on what the last score() returned -> gradient on its hidden states [M, K] bf16. top_ids: another model's
-        alternatives (default: the ones score() found, where dtop_logprob is given)."""
+        """Gradients on what the last score() returned -> gradient on its hidden states [M, K] bf16, zeros in the rows that it masked
+        and in those with 0 in `mask`. top_ids: another model's alternatives (default: the ones score() found, where dtop_logprob
+        is given)."""
+        if not self.backward:
+            raise ValueError("grad_hidden needs Fp8LMHead(..., backward=True)")
         o = self.out
+        if mask is None:
+            mask = self.mask
+        else:
+            _b.check_mask(mask, self.M, self.mask.device)
+            mask = torch.logical_and(mask.view(self.M), self.mask, out=self._mask_bwd)
         ids = top_ids if top_ids is not None or dtop_logprob is None else o["top_ids"]
         _b.logprob_topk_bwd(self.logits, o["lse"], self.temperature, tokens=tokens, dlogprob=dlogprob, top_ids=ids,
                             dtop_logprob=dtop_logprob, entropy=o["entropy"], dentropy=dentropy, dlse=dlse, mask=mask,

@@ -110,3 +110,49 @@ def test_eight_bit_scores_are_near_the_bf16_heads(P):
     sd = K ** 0.5 * 0.036 * 2 ** 0.5 * 0.1                      # rms |h| = 1, rms |w| = 0.1
     assert (o["logprob"][:, 0] - lp).abs().max() <= 8 * 2 ** 0.5 * sd
     assert (o["lse"] - lse).abs().max() <= 8 * sd
+
+
+def test_gradient_keeps_to_the_mask_of_its_scores(P):
+    """grad_hidden() without a mask, with the one of score() and with another one; scores without a mask afterwards."""
+    from paper_2403_17031_b200.pipeline import Fp8LMHead
+    M, K, V, k = 53, 256, 3000, 6
+    W, H, tokens, mask, g, gt, dh = _setup(M, K, V, 1, k)
+    mask *= 2                                                   # (anything but 0 is a row)
+    real = mask.bool()
+    assert 0 < int(real.sum()) < M
+    head = Fp8LMHead(W, M, k, 0.7, backward=True)
+    free = {n: v.clone() for n, v in head.score(H, tokens).items()}
+    full = head.grad_hidden(tokens, g, gt, dentropy=dh).clone()
+    for top in (gt, None):
+        o = head.score(H, tokens, mask)
+        assert torch.equal(o["top_ids"][real], free["top_ids"][real]) and (o["top_ids"][~real] == -1).all()
+        a = head.grad_hidden(tokens, g, top, dentropy=dh).clone()
+        assert torch.equal(head.grad_hidden(tokens, g, top, dentropy=dh, mask=mask), a)
+        assert not a[~real].any() and a[real].any(1).all() and head.device_status() == 0
+        if top is gt:
+            assert torch.equal(a[real], full[real])
+        fewer = mask.clone().view(1, M)
+        fewer[0, :M // 2] = 0
+        fewer[0, M // 2:] = 1                                   # (the masked ones among these have no scores either)
+        b = head.grad_hidden(tokens, g, top, dentropy=dh, mask=fewer)
+        both = real & fewer[0].bool()
+        assert torch.equal(b[both], a[both]) and not b[~both].any() and head.device_status() == 0
+    for wrong, error in ((mask[:-1], ValueError), (mask.float(), TypeError), (mask.cpu(), TypeError)):
+        with pytest.raises(error):
+            head.grad_hidden(tokens, g, gt, mask=wrong)
+        with pytest.raises(error):
+            head.score(H, tokens, wrong)
+    head.score(H, tokens)
+    assert torch.equal(head.grad_hidden(tokens, g, gt, dentropy=dh), full)
+    # a graph takes the mask as it is at its replay
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        head.score(H, tokens, mask)
+        head.grad_hidden(tokens, g, gt, dentropy=dh)
+    other = (torch.arange(M, device="cuda") % 3 != 0).to(torch.uint8)
+    mask.copy_(other)
+    head.score(H, tokens)                                       # (in between, without one)
+    graph.replay()
+    assert torch.equal(head.dhidden[other.bool()], full[other.bool()]) and not head.dhidden[~other.bool()].any()
+    with pytest.raises(ValueError):
+        Fp8LMHead(W, M, k, 0.7).grad_hidden(tokens, g)
