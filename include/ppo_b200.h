@@ -492,7 +492,8 @@ int ppo_fp8_quantize(const void *x, int dtype, int64_t R, int64_t C, int64_t x_s
  * Pitches lda and ldb are multiples of 16, A and B 16-byte aligned; M, N, K are any sizes (M == 0: successful no-op).
  * Sums are fp32: within a block on the tensor cores, over blocks in registers; each element is rounded once, and the
  * order is fixed by the sizes.  Bytes of A and B behind K in a row are not used, whatever they hold.
- *   workspace  nullable: the status word (PPO_DEV_TIMEOUT when a bounded wait ran out; C is invalid then)
+ *   workspace  nullable: the status word (PPO_DEV_TIMEOUT when a bounded wait ran out).  With and without it, a result that
+ *              was not computed because of that is NaN
  *   scratch    nullable: ppo_fp8_scratch_bytes(M, N, K) bytes on the device, 256-byte aligned, uninitialised, for this call
  *              alone while it runs.  Where that size is not 0, tiles that would leave most SMs idle are cut along K with it;
  *              without it (and where the size is 0) every tile is summed by one pair of SMs.  The order of the sums, and so

@@ -35,7 +35,17 @@ struct Args {
     int *status;
 };
 
-// A wait that is skipped once one has run out: the block then reaches its end quickly, with the same control flow.
+// PPO_TEST_WITHHOLD_FP8 (never defined in the product build): a test build in which, from the third block of K on (the second group of
+// scales), 1: products, 2: scales or 3: released accumulators are never announced, so that the waits for them run out.
+#ifndef PPO_TEST_WITHHOLD_FP8
+#define PPO_TEST_WITHHOLD_FP8 0
+#endif
+enum Withheld { kProducts = 1, kScaleGroups = 2, kReleases = 3 };
+__device__ __forceinline__ bool withheld(Withheld what, int done, int allowed) { return PPO_TEST_WITHHOLD_FP8 == what && done >= allowed; }
+
+// A wait that is skipped once one has run out: the block then reaches its end quickly, with the same control flow. Whoever has given
+// up announces nothing any more, so that the others' waits run out too instead of going on with what nobody computed, and an
+// epilogue warp that has given up stores NaN: without a status word that is the only sign.
 __device__ __forceinline__ void wait_alive(bool &alive, unsigned long long *bar, uint32_t parity, int *status)
 {
     if (alive) alive = wait(bar, parity, status);
@@ -48,6 +58,7 @@ template <int MT, int ST>
 struct NarrowSmem {
     unsigned long long full[ST], empty[ST], tmem_full[kNarrowBufs], tmem_empty[kNarrowBufs];
     uint32_t tmem_base;
+    int issued;                               // blocks of K whose products were issued
     float4 scale[4][kNarrowBufs][MT / 4];     // per epilogue warp: the columns' factors of a block of K
 };
 
@@ -130,10 +141,12 @@ narrow_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__
         if (lane == 0) {
             constexpr uint32_t idesc = instr_desc_e4m3(128, MT);
             bool alive = true;
-            for (int i = 0; i < kb1 - kb0; ++i) {
+            int i = 0;
+            for (; i < kb1 - kb0 && !withheld(kProducts, i, 2); ++i) {
                 const int s = i % ST, buf = i % kNarrowBufs;
                 if (i >= kNarrowBufs) wait_alive(alive, &sm.tmem_empty[buf], ((i / kNarrowBufs) - 1) & 1, a.status);
                 wait_alive(alive, &sm.full[s], (i / ST) & 1, a.status);
+                if (!alive) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 const uint32_t b_addr = saddr(ring + (size_t)s * kStage), a_addr = b_addr + 128 * kBlockK;
 #pragma unroll
@@ -143,6 +156,9 @@ narrow_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__
                 commit(&sm.empty[s]);
                 commit(&sm.tmem_full[buf]);
             }
+            sm.issued = i;
+            // every product has ended before tensor memory is freed
+            if (i > 0) wait(&sm.tmem_full[(i - 1) % kNarrowBufs], ((i - 1) / kNarrowBufs) & 1, a.status);
         }
         __syncwarp();
     } else {
@@ -180,7 +196,7 @@ narrow_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__
                 if (g == MT / 16 - 1) {
                     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                     __syncwarp();
-                    if (lane == 0) barrier_arrive(&sm.tmem_empty[buf]);
+                    if (lane == 0 && alive && !withheld(kReleases, i, 2)) barrier_arrive(&sm.tmem_empty[buf]);
                 }
 #pragma unroll
                 for (int j4 = 0; j4 < 4; ++j4) {
@@ -194,6 +210,10 @@ narrow_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__
                 }
             }
         }
+        if (!alive) {
+#pragma unroll
+            for (int j = 0; j < MT; ++j) acc[j] = __uint_as_float(0x7fffffffu);
+        }
     }
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
@@ -205,7 +225,7 @@ narrow_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__
     // its barriers, though, and the block must not end before them: a lane for each. (Beside the stores: one after the other and
     // before the barrier above, these waits took 64 x 4096 x 8192 from 13.7 to 14.6 us.)
     const auto drain = [&] {
-        const int i = kb1 - kb0 - 1 - lane;
+        const int i = sm.issued - 1 - lane;
         if (warp == 1 && lane < ST && i >= 0) wait(&sm.empty[i % ST], (i / ST) & 1, a.status);
     };
     const int q = warp & 3, nl = q * 32 + lane, n = n0 + nl;
@@ -332,6 +352,7 @@ struct WideSmem {
     unsigned long long full[kWideStages], empty[kWideStages], tmem_full[2][2];   // [half][accumulator]
     unsigned long long scale_full[2], scale_empty[2];
     unsigned long long pair_empty[2][2];   // the leader's: both blocks' epilogues have read the accumulator
+    unsigned long long nobody[2];          // takes the arrivals of warps that have given up
     uint32_t tmem_base;
 };
 
@@ -474,6 +495,7 @@ wide_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
             }
             barrier_init(&sm.scale_full[b], 1);
             barrier_init(&sm.scale_empty[b], kEpiWarps);
+            barrier_init(&sm.nobody[b], 1);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -531,13 +553,13 @@ wide_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
             const uint32_t tmem_d = tmem_base + buf * kBN + g * (kBN / 2);
             bool alive = true;
             uint32_t s = buf, s_parity = 0, b_parity = 1;
-            for (uint32_t it = buf; it < total; it += 2) {
+            for (uint32_t it = buf; it < total && !withheld(kProducts, it, 2); it += 2) {
                 wait_alive(alive, &sm.full[s], s_parity, a.status);
                 wait_alive(alive, &sm.pair_empty[g][buf], b_parity, a.status);
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 // rows 64 g .. of either block's 128 rows of B
                 const uint64_t ad = desc0 + s * (kWideStage >> 4), bd = ad + ((kWideA + g * (kWideB / 2)) >> 4);
-                if (elect_one()) {
+                if (elect_one() && alive) {                     // (the same lane every time)
 #pragma unroll
                     for (int kk = 0; kk < kBlockK / 32; ++kk) mma_f8_pair(tmem_d, ad + kk * 2, bd + kk * 2, idesc, kk ? 1u : 0u);
                     commit_pair(&sm.tmem_full[g][buf]);
@@ -546,19 +568,23 @@ wide_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
                 __syncwarp();
                 s += 2;
                 if (s >= kWideStages) { s -= kWideStages; s_parity ^= 1; }
-                b_parity ^= 1;
+                b_parity ^= (uint32_t)alive;
             }
+            // every product has ended before tensor memory is freed (b_parity is now that of the last one's phase, or that of the
+            // phase before the first)
+            if (elect_one()) wait(&sm.tmem_full[g][buf], b_parity, a.status);
         }
         __syncwarp();
     } else if (warp == 1) {
         bool alive = true;
         uint32_t g = 0, parity = 1;
-        while (piece.next(w, pairs, kbs)) {
+        while (alive && piece.next(w, pairs, kbs)) {
             const int2 t = tile_of(piece.u, a.m_tiles, a.n_tiles, w.gm, w.gn);
             const int m0 = t.x * kPairM + rank * kBM, n0 = t.y * kBN;
             for (int kb0 = piece.kb0; kb0 < piece.kb1; kb0 += kGroup) {
                 wait_alive(alive, &sm.scale_empty[g], parity, a.status);
-                __syncwarp();
+                alive = __all_sync(0xffffffffu, alive);
+                if (!alive) break;
                 float *to = scales + g * kGroupFloats;
                 for (int kb = kb0; kb < min(kb0 + kGroup, piece.kb1); ++kb, to += kFloats) {
                     const float *pa = a.sa + (int64_t)kb * a.M;
@@ -576,7 +602,7 @@ wide_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
                 }
                 asm volatile("cp.async.wait_all;" ::: "memory");
                 __syncwarp();
-                if (lane == 0) barrier_arrive(&sm.scale_full[g]);
+                if (lane == 0 && !withheld(kScaleGroups, (int)g, 1)) barrier_arrive(&sm.scale_full[g]);
                 parity ^= g;
                 g ^= 1;
             }
@@ -586,8 +612,17 @@ wide_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
         const int q = warp & 3, c64 = (warp - 8) >> 2, h = c64 >> 1;   // lanes 32 q .., columns 64 c64 .., their half
         unsigned char *stage = ring + (size_t)kWideStages * kWideStage + (warp - 8) * kStageOut;
         const uint32_t taddr = tmem_base + c64 * 64 + ((uint32_t)(q * 32) << 16);
-        const uint32_t pair_empty0 = leader_addr(&sm.pair_empty[h][0]), pair_empty1 = leader_addr(&sm.pair_empty[h][1]);
         bool alive = true, ready = false;                       // ready: the next accumulator is known to be there
+        // what this warp's arrivals count on: once it has given up, barriers that nobody waits for (the hot loop pays nothing for it;
+        // arrivals under a condition cost 2 %)
+        uint32_t pair_empty = leader_addr(&sm.pair_empty[h][0]), scale_empty = saddr(&sm.scale_empty[0]);
+        const auto wait_or_leave = [&](unsigned long long *bar, uint32_t parity) {
+            if (alive && !wait(bar, parity, a.status)) {
+                alive = false;
+                pair_empty = leader_addr(&sm.nobody[0]);
+                scale_empty = saddr(&sm.nobody[0]);
+            }
+        };
         uint32_t buf = 0, parity = 0, g = 0, g_parity = 0;
         while (piece.next(w, pairs, kbs)) {
             float2 acc[32];
@@ -598,13 +633,13 @@ wide_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
 #pragma unroll 1
             for (int kb = piece.kb0; kb < piece.kb1; ++kb) {
                 if (left == 0) {
-                    wait_alive(alive, &sm.scale_full[g], g_parity, a.status);
+                    wait_or_leave(&sm.scale_full[g], g_parity);
                     slot = scales + g * kGroupFloats;
                     left = min(kGroup, piece.kb1 - kb);
                 }
                 const float f = PER_ROW ? slot[q * 32 + lane] : slot[q * 32 + lane] * slot[kBM + h];
                 const float *sbs = slot + kBM + c64 * 64;       // PER_ROW: this warp's 64 factors
-                if (!ready) wait_alive(alive, &sm.tmem_full[h][buf], parity, a.status);
+                if (!ready) wait_or_leave(&sm.tmem_full[h][buf], parity);
                 __syncwarp();
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 uint32_t r[2][16];
@@ -620,7 +655,7 @@ wide_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
                         // release is on the way from one matrix instruction to the next
                         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                         __syncwarp();
-                        barrier_arrive_cluster_if(buf ? pair_empty1 : pair_empty0, lane == 0);
+                        barrier_arrive_cluster_if(pair_empty + buf * 8, lane == 0 && !withheld(kReleases, kb - piece.kb0, 2));
                         parity ^= buf;
                         buf ^= 1;
                         ready = peek(&sm.tmem_full[h][buf], parity);
@@ -630,10 +665,14 @@ wide_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
                 slot += kFloats;
                 if (--left == 0) {
                     __syncwarp();
-                    if (lane == 0) barrier_arrive(&sm.scale_empty[g]);
+                    if (lane == 0) barrier_arrive_cluster(scale_empty + g * 8);
                     g_parity ^= g;
                     g ^= 1;
                 }
+            }
+            if (!alive) {
+#pragma unroll
+                for (int j = 0; j < 32; ++j) acc[j].x = acc[j].y = __uint_as_float(0x7fffffffu);
             }
             const int2 t = tile_of(piece.u, a.m_tiles, a.n_tiles, w.gm, w.gn);
             const int n = t.y * kBN + c64 * 64;

@@ -10,7 +10,10 @@
 namespace ppo {
 namespace tc {
 
-constexpr uint32_t kWaitTries = 1u << 19;               // x up to ~2 us per try
+#ifndef PPO_TC_WAIT_TRIES
+#define PPO_TC_WAIT_TRIES (1u << 19)
+#endif
+constexpr uint32_t kWaitTries = PPO_TC_WAIT_TRIES;      // x up to ~2 us per try (a test build makes the waits short)
 
 __device__ __forceinline__ uint32_t saddr(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
 

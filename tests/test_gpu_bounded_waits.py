@@ -92,3 +92,44 @@ def test_a_wait_that_runs_out_is_reported_and_nothing_hangs(P, tmp_path_factory,
     assert P.last_device_status(ws) == 0
     for k in ("losses", "dlogits", "dvalues", "new_logprob", "entropy", "dlogprob"):
         assert torch.equal(o2[k], want[k]), k
+
+
+def _fp8_variant(tmp, withhold):
+    from paper_2403_17031_b200 import binding, build
+    path = build.build_variant(os.path.join(str(tmp), "libfp8_withhold%d.so" % withhold),
+                               ["PPO_TEST_WITHHOLD_FP8=%d" % withhold, "PPO_TC_WAIT_TRIES=32768"], only=["ppo_fp8_matmul.cu"])
+    fn = C.CDLL(path).ppo_fp8_matmul
+    fn.restype, fn.argtypes = binding._SIGS["ppo_fp8_matmul"]
+    return fn
+
+
+@pytest.mark.parametrize("withhold", [1, 2, 3], ids=["products", "scales", "releases"])
+def test_a_block_scaled_product_whose_waits_run_out_is_nan_with_and_without_a_status_word(P, tmp_path_factory, withhold):
+    """Every kernel form: clusters that join parts of K, single blocks, whole tiles of a pair, tiles cut along K. In the test build something
+    is not announced from the third block of K (the second group of scales) on; every result needs more than that."""
+    fn = _fp8_variant(tmp_path_factory.mktemp("fp8"), withhold)
+    g = torch.Generator(device="cuda").manual_seed(12)
+    cases = [(700, 2000, 6400, 128, False), (700, 2000, 2048, 1, False), (600, 2000, 12000, 128, True)]
+    if withhold != 2:                                                      # (the narrow kernel's warps fetch their scales themselves)
+        cases += [(16, 256, 8192, 128, False), (60, 1000, 8192, 1, False), (1, 50304, 1024, 128, False)]
+    for M, N, K, block_n, cut in cases:
+        a, sa = P.fp8_quantize(torch.randn(M, K, generator=g, device="cuda"), 1)
+        b, sb = P.fp8_quantize(torch.randn(N, K, generator=g, device="cuda"), block_n)
+        need = P.fp8_scratch_bytes(M, N, K)
+        assert (need > 0) or not cut
+        scratch = torch.zeros(need, dtype=torch.uint8, device="cuda") if cut else None
+        out = torch.zeros(M, N, device="cuda")
+        ws = P.new_workspace(256)
+        p = lambda t: C.c_void_p(t.data_ptr()) if t is not None else None   # noqa: E731
+        st = C.c_void_p(torch.cuda.current_stream().cuda_stream)
+        for status in (ws, None):
+            out.zero_()
+            assert fn(p(a), a.stride(0), p(sa), p(b), b.stride(0), p(sb), block_n, M, N, K, p(out), 0, N, p(status), p(scratch), st) == 0
+            torch.cuda.synchronize()
+            assert torch.isnan(out).all(), (M, N, K, int(torch.isnan(out).sum()))
+        assert P.last_device_status(ws) & DEV_TIMEOUT
+        # the context is alive and the product library gives the right result in the same buffers
+        P.fp8_matmul(a, sa, b, sb, block_n, torch.float32, out=out, workspace=ws, scratch=scratch)
+        assert P.last_device_status(ws) == 0
+        want = P.fp8_matmul(a, sa, b, sb, block_n, torch.float32, scratch=torch.empty_like(scratch) if cut else None)
+        assert torch.isfinite(out).all() and torch.equal(out, want)
