@@ -494,7 +494,8 @@ int ppo_fp8_quantize(const void *x, int dtype, int64_t R, int64_t C, int64_t x_s
  * order is fixed by the sizes.  Bytes of A and B behind K in a row are not used, whatever they hold.
  *   workspace  nullable: the status word (PPO_DEV_TIMEOUT when a bounded wait ran out).  With and without it, a result that
  *              was not computed because of that is NaN
- *   scratch    nullable: ppo_fp8_scratch_bytes(M, N, K) bytes on the device, 256-byte aligned, uninitialised, for this call
+ *   scratch    nullable: ppo_fp8_scratch_bytes(M, N, K) bytes (asked with the call's device as the current one: the size
+ *              depends on its number of SMs), 256-byte aligned, uninitialised, for this call
  *              alone while it runs.  Where that size is not 0, tiles that would leave most SMs idle are cut along K with it;
  *              without it (and where the size is 0) every tile is summed by one pair of SMs.  The order of the sums, and so
  *              the last bits, differ between the two

@@ -557,16 +557,18 @@ def logprob_entropy_pair(policy_logits, ref_logits, tokens, temperature: float, 
 TOPK_MAX = 128
 
 
+def _on_device(at: int, fn, *args):
+    """fn(*args) with device `at` as the current one."""
+    if at == torch._C._cuda_getDevice():
+        return fn(*args)
+    with torch.cuda.device(at):
+        return fn(*args)
+
+
 def _call(fn_name: str, at: int, *args):
     """One entry point on device `at` and that device's current stream (the last argument). Small calls are bound by this
     side of the boundary, so pointers are passed as plain ints and the stream comes straight from the C layer."""
-    fn = getattr(_lib or lib(), fn_name)
-    stream = torch._C._cuda_getCurrentRawStream(at)
-    if at == torch._C._cuda_getDevice():
-        rc = fn(*args, stream)
-    else:
-        with torch.cuda.device(at):
-            rc = fn(*args, stream)
+    rc = _on_device(at, getattr(_lib or lib(), fn_name), *args, torch._C._cuda_getCurrentRawStream(at))
     if rc != 0:
         raise PPOError(fn_name, rc)
 
@@ -710,8 +712,11 @@ def _fp8_operand(t: torch.Tensor, at: int, name: str):
     return t.data_ptr(), s0 if rows > 1 else -(-cols // 16) * 16
 
 
-def fp8_scratch_bytes(M: int, N: int, K: int) -> int:
-    return int(lib().ppo_fp8_scratch_bytes(M, N, K))
+def fp8_scratch_bytes(M: int, N: int, K: int, device: Optional[torch.device] = None) -> int:
+    """Bytes of scratch with which fp8_matmul cuts tiles along K on `device` (default: the current one); it depends on its SMs."""
+    fn = lib().ppo_fp8_scratch_bytes
+    at = None if device is None else torch.device(device).index
+    return int(fn(M, N, K) if at is None else _on_device(at, fn, M, N, K))
 
 
 def fp8_matmul(a: torch.Tensor, a_scales: torch.Tensor, b: torch.Tensor, b_scales: torch.Tensor, block_n: int = 128,
@@ -737,7 +742,7 @@ def fp8_matmul(a: torch.Tensor, a_scales: torch.Tensor, b: torch.Tensor, b_scale
         if out.shape != (M, N) or out.get_device() != at:
             raise ValueError("out must have shape %s, on the operands' device" % ((M, N),))
         _, _, ldc = _rows_of(out, "out")
-    need = fp8_scratch_bytes(M, N, K) if kb > 24 else 0            # (none for a shorter K, whatever M and N)
+    need = fp8_scratch_bytes(M, N, K, a.device) if kb > 24 else 0  # (none for a shorter K, whatever M and N)
     if need and scratch is None:
         scratch = a.new_empty(need, dtype=torch.uint8)
     if scratch is not None and scratch.numel() < need:

@@ -168,7 +168,7 @@ class Fp8LMHead:
         pitch = lambda cols: -(-cols // 16) * 16
         operand = lambda cols: (torch.empty((M, pitch(cols)), dtype=f8, device=dev)[:, :cols],
                                 torch.empty((-(-cols // 128), M), dtype=f32, device=dev))
-        scratch = lambda N, C: torch.empty(max(_b.fp8_scratch_bytes(M, N, C), 256), dtype=torch.uint8, device=dev)
+        scratch = lambda N, C: torch.empty(max(_b.fp8_scratch_bytes(M, N, C, dev), 256), dtype=torch.uint8, device=dev)
         self.workspace = _b.new_workspace(_b.workspace_bytes(M, 1, V), dev)
         self.weight = _b.fp8_quantize(W, 128, transpose=True)
         self.hidden = operand(K)

@@ -77,3 +77,30 @@ def test_binding_refuses_cpu_tensors(b):
     q = torch.zeros(4, 256).to(torch.float8_e4m3fn)
     with pytest.raises(TypeError):
         b.fp8_matmul(q, torch.zeros(2, 4), q, torch.zeros(1, 2))
+
+
+def test_scratch_is_sized_for_the_operands_device(b, monkeypatch):
+    """The plan of a product follows the SMs of the device that runs it, which need not be the current one."""
+    current = [0]
+
+    class Guard:
+        def __init__(self, at):
+            self.at = at
+
+        def __enter__(self):
+            self.old, current[0] = current[0], self.at
+
+        def __exit__(self, *_):
+            current[0] = self.old
+
+    class Lib:
+        @staticmethod
+        def ppo_fp8_scratch_bytes(M, N, K):
+            return 1000 + current[0]
+
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: current[0], raising=False)
+    monkeypatch.setattr(torch.cuda, "device", Guard)
+    monkeypatch.setattr(b, "lib", lambda: Lib)
+    assert b.fp8_scratch_bytes(600, 2000, 12000) == 1000
+    assert b.fp8_scratch_bytes(600, 2000, 12000, torch.device("cuda", 3)) == 1003
+    assert b.fp8_scratch_bytes(600, 2000, 12000, "cuda") == 1000 and current == [0]
