@@ -233,13 +233,16 @@ def new_workspace(nbytes: int, device="cuda") -> torch.Tensor:
     """Allocate (torch) and clear a workspace of at least `nbytes`."""
     ws = torch.empty(max(int(nbytes), 256), dtype=torch.uint8, device=device)
     assert ws.data_ptr() % 256 == 0
-    _check("ppo_workspace_init", lib().ppo_workspace_init(_ptr(ws), ws.numel(), _stream()))
+    with torch.cuda.device(ws.device):                 # and the stream that its device's calls will use
+        _check("ppo_workspace_init", lib().ppo_workspace_init(_ptr(ws), ws.numel(), _stream()))
     return ws
 
 
 def last_device_status(workspace: torch.Tensor) -> int:
     st = C.c_int(0)
-    _check("ppo_last_device_status", lib().ppo_last_device_status(_ptr(workspace), _stream(), C.byref(st)))
+    ws = _ptr(workspace)
+    with torch.cuda.device(workspace.device):
+        _check("ppo_last_device_status", lib().ppo_last_device_status(ws, _stream(), C.byref(st)))
     return int(st.value)
 
 

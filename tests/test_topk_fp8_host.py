@@ -104,3 +104,40 @@ def test_scratch_is_sized_for_the_operands_device(b, monkeypatch):
     assert b.fp8_scratch_bytes(600, 2000, 12000) == 1000
     assert b.fp8_scratch_bytes(600, 2000, 12000, torch.device("cuda", 3)) == 1003
     assert b.fp8_scratch_bytes(600, 2000, 12000, "cuda") == 1000 and current == [0]
+
+
+def test_workspaces_are_cleared_and_read_on_the_stream_of_their_device(b, monkeypatch):
+    current, seen = ["cuda:0"], []
+
+    class Guard:
+        def __init__(self, at):
+            self.at = at
+
+        def __enter__(self):
+            self.old, current[0] = current[0], str(self.at)
+
+        def __exit__(self, *_):
+            current[0] = self.old
+
+    class Lib:
+        @staticmethod
+        def ppo_workspace_init(ws, n, stream):
+            seen.append((stream, current[0]))
+            return 0
+
+        @staticmethod
+        def ppo_last_device_status(ws, stream, code):
+            seen.append((stream, current[0]))
+            return 0
+
+    class Tensor:                                        # stands in for 256 bytes on the second device
+        device = torch.device("cuda", 1)
+        data_ptr, numel = staticmethod(lambda: 256), staticmethod(lambda: 256)
+
+    monkeypatch.setattr(torch.cuda, "device", Guard)
+    monkeypatch.setattr(torch, "empty", lambda *a, **k: Tensor)
+    monkeypatch.setattr(b, "lib", lambda: Lib)
+    monkeypatch.setattr(b, "_ptr", lambda t: t.data_ptr())
+    monkeypatch.setattr(b, "_stream", lambda: "stream of " + current[0])
+    assert b.last_device_status(b.new_workspace(256, "cuda:1")) == 0
+    assert seen == [("stream of cuda:1", "cuda:1")] * 2 and current == ["cuda:0"]
