@@ -247,3 +247,39 @@ def test_a_chain_from_hidden_states_to_their_gradient(P):
 def test_matmul_of_few_rows_with_a_long_weight(P, M, N, K, out_dtype, block_n):
     """(more tiles of 128 weight rows than two for each SM)"""
     _check_matmul(P, M, N, K, block_n, out_dtype)
+
+
+@pytest.mark.parametrize("M,N,K", [(600, 2000, 12000), (257, 15000, 15400)])
+def test_tiles_cut_along_k_on_another_stream_in_graphs_and_two_at_a_time(P, M, N, K):
+    """The sums and their join (a dependent launch), with scratch of the caller's and scratch allocated inside the call."""
+    a, sa, b, sb = _operands(P, M, N, K, 128)
+    a2, sa2 = P.fp8_quantize(_matrix(M, K, BF16, seed=5), 1)
+    need = P.fp8_scratch_bytes(M, N, K)
+    assert need > 0
+    wants = [P.fp8_matmul(a, sa, b, sb, out_dtype=F32), P.fp8_matmul(a2, sa2, b, sb, out_dtype=F32)]
+    assert not torch.equal(*wants)
+    outs = [torch.zeros_like(w) for w in wants]
+    scratch = torch.empty(need, dtype=torch.uint8, device="cuda").fill_(255)
+    calls = [lambda: P.fp8_matmul(a, sa, b, sb, out=outs[0], scratch=scratch), lambda: P.fp8_matmul(a2, sa2, b, sb, out=outs[1])]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    for s, call in zip(streams, calls):
+        with torch.cuda.stream(s):
+            call()
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, w) for o, w in zip(outs, wants))
+    graphs = []
+    for s, call in zip(streams, calls):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1], stream=s):
+            call()
+            call()                                              # (the second call's kernels follow the first one's join)
+    for _ in range(5):
+        for o in outs:
+            o.zero_()
+        torch.cuda.synchronize()
+        for s, graph in zip(streams, graphs):
+            with torch.cuda.stream(s):
+                graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(o, w) for o, w in zip(outs, wants))

@@ -156,3 +156,73 @@ def test_gradient_keeps_to_the_mask_of_its_scores(P):
     assert torch.equal(head.dhidden[other.bool()], full[other.bool()]) and not head.dhidden[~other.bool()].any()
     with pytest.raises(ValueError):
         Fp8LMHead(W, M, k, 0.7).grad_hidden(tokens, g)
+
+
+def test_heads_whose_gradient_is_cut_along_the_vocabulary(P):
+    """Scratch of more than its least size: the gradient's product against the product of whole tiles and the same call again; two heads
+    in flight; captured."""
+    from paper_2403_17031_b200.pipeline import Fp8LMHead
+    M, K, V, k = 600, 2000, 12000, 4
+    W, H, tokens, mask, g, gt, dh = _setup(M, K, V, 1, k)
+    heads = [Fp8LMHead(W if i == 0 else (W * 0.5).contiguous(), M, k, 0.7, backward=True) for i in range(2)]
+    assert P.fp8_scratch_bytes(M, K, V) > 256 and heads[0]._scratch_bwd.numel() == P.fp8_scratch_bytes(M, K, V)
+    wants = []
+    for h in heads:
+        h.score(H, tokens, mask)
+        wants.append(h.grad_hidden(tokens, g, gt, dentropy=dh).clone())
+        y, size = F.matmul(npy(h.dlogits_q[0].float()), npy(h.dlogits_q[1]), npy(h.weight_bwd[0].float()), npy(h.weight_bwd[1]), 128)
+        gamma = (128 + -(-V // 128) + 3) * 2.0 ** -23
+        assert (np.abs(wants[-1].double().cpu().numpy() - y) <= 2.0 ** -8 * np.abs(y) + gamma * size + 1e-38).all()
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    graphs = []
+    for h, s in zip(heads, streams):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1], stream=s):
+            h.score(H, tokens, mask)
+            h.grad_hidden(tokens, g, gt, dentropy=dh)
+    for how in ("eager", "replayed", "replayed"):
+        for h in heads:
+            h.dhidden.zero_()
+            h._scratch_bwd.fill_(255)
+        torch.cuda.synchronize()
+        for h, s, graph in zip(heads, streams, graphs):
+            with torch.cuda.stream(s):
+                if how == "eager":
+                    h.score(H, tokens, mask)
+                    h.grad_hidden(tokens, g, gt, dentropy=dh)
+                else:
+                    graph.replay()
+        torch.cuda.synchronize()
+        for h, w in zip(heads, wants):
+            assert torch.equal(h.dhidden, w) and h.device_status() == 0, how
+
+
+def test_eight_bit_gradient_is_near_the_bf16_heads(P):
+    """dH_k = sum_v d_v W_kv against the bf16 head's, d the gradient of the token's log-prob. Off by, in standard deviations of independent
+    errors: e4m3 (rms 0.036 relative) of d and W: 0.036 sqrt(2) sqrt(sum (d W)^2); d itself by p_v (e_v - sum p e) for logits off by e (rms
+    `sd`, as for the scores above): at most 2 sd |g| sqrt(sum (p W)^2). Eight of either, and the roundings to bf16 on the way (the logits',
+    half a step of |z| <= 16 moves p by 2^-5 and again by 2^-5 through lse: 2^-4 |g| sum p |W|; d's and the result's in either head: 2^-8
+    of their terms each)."""
+    from paper_2403_17031_b200.pipeline import Fp8LMHead
+    M, K, V = 96, 512, 4096
+    W, H, tokens, mask, g, *_ = _setup(M, K, V, 1, 1)
+    head = Fp8LMHead(W, M, 0, 1.0, backward=True)
+    head.score(H, tokens, mask)
+    assert float(head.logits.abs().max()) <= 16
+    got = head.grad_hidden(tokens, g).double()
+    tok = tokens[:, 0].contiguous()
+    ws = P.new_workspace(P.lmhead_workspace_bytes(M, K, V))
+    _, _, lse = P.lmhead_logprob_entropy(H, W, tok, 1.0, ws)
+    want = P.lmhead_bwd(H, W, tok, lse, g[:, 0].contiguous(), 1.0, ws, mask=mask, want_dW=False)["dH"].double()
+    real = mask.bool()
+    assert not got[~real].any() and not want[~real].any()
+    w2 = W.double()
+    p = torch.softmax(H.double() @ w2, 1)
+    d = -p * g.double()
+    d[torch.arange(M, device="cuda"), tok.long()] += g[:, 0].double()
+    sd = K ** 0.5 * 0.036 * 2 ** 0.5 * 0.1
+    absg = g.double().abs()
+    bound = 8 * (0.036 * 2 ** 0.5 * (d * d @ (w2 * w2).t()).sqrt() + 2 * sd * absg * (p * p @ (w2 * w2).t()).sqrt())
+    bound += 2.0 ** -4 * absg * (p @ w2.abs().t()) + 4 * 2.0 ** -8 * (d.abs() @ w2.abs().t())
+    assert ((got - want).abs() <= bound)[real].all()
