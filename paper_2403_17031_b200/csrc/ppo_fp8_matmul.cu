@@ -361,7 +361,10 @@ struct WideSmem {
 // its sums of a tile in the scratch buffer (at most two tiles), and join_kernel adds them up in the order of the pairs.
 struct WideArgs {
     Args a;
-    int gm, gn, n_whole, n_rest, share, bulk_out;   // bulk_out: rows of C are 16-byte aligned
+    int gm, gn, n_whole, n_rest, share;
+    // Bulk stores take the boxes that end at or before this column: none where rows of C are not 16-byte aligned, those inside N where
+    // N is not a multiple of 16 bytes (a box is clipped in units of 16 bytes: it would write zeros behind N), else all.
+    int bulk_cols;
     float *scratch;
 };
 
@@ -710,7 +713,7 @@ wide_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
                         *reinterpret_cast<uint4 *>(row + ((j ^ (lane & 7)) << 4)) = make_uint4(v[0], v[1], v[2], v[3]);
                     }
                 }
-                if (w.bulk_out) {
+                if (n + c * 32 + (a.out_f32 ? 32 : 64) <= w.bulk_cols) {
                     fence_async_proxy();
                     __syncwarp();
                     if (lane == 0 && m_warp < a.M && n + c * 32 < a.N) tma_store_2d(&map_c, n + c * 32, m_warp, stage);
@@ -835,9 +838,10 @@ static int launch_wide(Args a, const void *A, int64_t lda, const void *B, int64_
     w.share = p.share;
     w.scratch = scratch;
     const int64_t pitch = a.ldc * (a.out_f32 ? 4 : 2);
-    w.bulk_out = reinterpret_cast<uintptr_t>(a.out) % 16 == 0 && pitch % 16 == 0 && pitch < ((int64_t)1 << 40);
+    if (reinterpret_cast<uintptr_t>(a.out) % 16 == 0 && pitch % 16 == 0 && pitch < ((int64_t)1 << 40))
+        w.bulk_cols = a.N % (a.out_f32 ? 4 : 8) ? a.N : 0x7fffffff;
     CUtensorMap mc = {};
-    if (w.bulk_out) {
+    if (w.bulk_cols) {
         rc = make_map_out(&mc, a.out, a.out_f32 != 0, (uint64_t)a.N, (uint64_t)a.M, (uint64_t)pitch, 32);
         if (rc) return rc;
     }

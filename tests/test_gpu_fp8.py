@@ -283,3 +283,15 @@ def test_tiles_cut_along_k_on_another_stream_in_graphs_and_two_at_a_time(P, M, N
                 graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(o, w) for o, w in zip(outs, wants))
+
+
+@pytest.mark.parametrize("dtype,N,pad", [(F32, 2045, 3), (F32, 2046, 2), (F32, 2047, 1), (F32, 1985, 31), (BF16, 2041, 7), (BF16, 2044, 4),
+                                         (BF16, 2047, 1), (BF16, 1985, 63), (BF16, 1983, 1), (F32, 257, 3), (BF16, 257, 7)])
+@pytest.mark.parametrize("M,K", [(700, 640), (2000, 300), (600, 12000)])
+def test_matmul_leaves_columns_behind_an_odd_edge_alone(P, M, K, dtype, N, pad):
+    """Rows of C at a pitch of 16 bytes that end inside 16 bytes."""
+    a, sa, b, sb = _operands(P, M, N, K, 128)
+    want = P.fp8_matmul(a, sa, b, sb, out_dtype=F32)
+    buf = torch.full((M, N + pad), 5.0, dtype=dtype, device="cuda")
+    P.fp8_matmul(a, sa, b, sb, out=buf[:, :N])
+    assert torch.equal(buf[:, :N], want.to(dtype)) and (buf[:, N:] == 5.0).all()
