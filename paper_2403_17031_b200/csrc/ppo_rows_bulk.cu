@@ -252,8 +252,8 @@ struct ThreadStats {
     {
         float x[Pack<T>::N], xm;
         Pack<T>::unpack(v, x, xm);
-        const float nm = safe_reference(xm, c);
-        if (nm > m) rebase(nm);
+        const float nm = xm * c;
+        if (xm > kNoWeight && nm > m) rebase(nm);      // (masked logits move no reference, however far below 0 the row lies)
         accumulate_pairs<T, ENTROPY, true>(v, c, -m, acc);
     }
     // fold up to two packs of one chunk

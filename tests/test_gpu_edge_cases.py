@@ -298,3 +298,30 @@ def test_logits_that_are_masked_softly(P, oracle, dtype, V, lp_engine):
         assert_abs(npy(lp), rlp, TOL_LOGPROB, "logprob at %s" % base)
         assert_abs(npy(ent), rent, TOL_LOGPROB, "entropy at %s" % base)
         assert_abs(npy(lse), rlse, TOL_LOGPROB, "lse at %s" % base)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("offset", [-60.0, -100.0, -400.0])
+@pytest.mark.parametrize("V,live", [(50304, 50257), (16384, 9000), (1000, 990)])
+def test_rows_far_below_zero_with_masked_padding(P, oracle, dtype, V, live, offset, lp_engine):
+    """Logits far from 0, as some models give, with the vocabulary's padding masked: log-probs, entropy, and the loss kernel's gradient."""
+    B, T, tau = 4, 6, 0.7
+    rows = B * T
+    x = _rand_logits(rows, V, dtype, seed=V) + offset
+    x[:, live:] = -torch.inf
+    x[1::3, 40:48] = torch.finfo(dtype).min
+    tok = torch.full((rows,), live // 3, device="cuda", dtype=torch.int32)
+    lp, ent, lse = P.logprob_entropy(x, tok, tau, want_lse=True)
+    rlp, rent, rlse = oracle.logprob_entropy(host_logits(x), npy(tok), np.float32(tau))
+    assert_abs(npy(lp), rlp, TOL_LOGPROB, "logprob")
+    assert_abs(npy(ent), rent, TOL_LOGPROB, "entropy")
+    assert_abs(npy(lse), rlse, TOL_LOGPROB, "lse")
+    ws = P.new_workspace(P.workspace_bytes(B, T, V))
+    mask = torch.ones(rows, dtype=torch.uint8, device="cuda")
+    d = P.logprob_bwd(x, tok, mask, torch.ones(rows, device="cuda"), tau, ws, want_aux=True)
+    assert_abs(npy(d["new_logprob"]), rlp, TOL_LOGPROB, "new_logprob")
+    z = x.double() / float(np.float32(tau))
+    want = -torch.softmax(z, 1)
+    want[torch.arange(rows), tok.long()] += 1
+    want /= float(np.float32(tau))
+    assert_grad(npy(d["dlogits"].float()), npy(want), dtype == torch.bfloat16, "dlogits")
