@@ -179,6 +179,7 @@ __device__ __forceinline__ SoftmaxState block_merge_common(SoftmaxState st, floa
     }
     if (__syncthreads_or(differs)) {
         __syncthreads();                                 // everyone has left the fast path's use of red
+        if (st.s == 0.f) st.m = kNegBig;                 // (m_common may lie far above the others' references)
         return block_merge<THREADS>(st, red);
     }
     SoftmaxState r;

@@ -92,16 +92,20 @@ __device__ __forceinline__ void st_stream(uint4 *p, const uint4 &v) { __stcs(p, 
 // row's sums: at that magnitude x*c - ref is the rounding error of x*c, up to 2^75, instead of 0.
 constexpr float kNoWeight = -1.0e29f;
 
-// Reference (base-2 units) taken from a pack maximum.
+// Reference (base-2 units) taken from a pack maximum; 0 from a pack without weight. Sums that come out as good as 0 with the
+// latter say nothing: the row may lie far below 0, and they are taken again (reference_missed).
 __device__ __forceinline__ float safe_reference(float xmax, float c) { return xmax > kNoWeight ? xmax * c : 0.f; }
+
+__device__ __forceinline__ bool reference_missed(float m, float s) { return m == 0.f && s < 1.0e-18f; }
 
 // Start of a sum with a moving reference. The reference is not below what a logit without weight comes to for any temperature
 // up to 1e19, so that none moves it there, and far enough above for 2^(x*c - ref) to be 0 for them. (Logits with weight come to
 // +-2^30 at the most: beyond that fp32 tells no probabilities apart.)
+constexpr float kNoReference = -1.0e10f;
 __device__ __forceinline__ void init_online(SoftmaxState &st)
 {
     st.init();
-    st.m = -1.0e10f;
+    st.m = kNoReference;
 }
 
 // Sums relative to a fixed reference above this are taken again with a moving one. A state's sums may be merged into a state whose
@@ -223,8 +227,8 @@ __device__ __forceinline__ SoftmaxState row_statistics(const T *__restrict__ src
             }
             st.s = acc.s0 + acc.s1;
             st.u = acc.u0 + acc.u1;
-            if (!(st.s < kSumLimit) || !(fabsf(st.u) < kSumLimit)) {
-                // overflow (or NaN input): redo this thread's packs with a moving reference
+            if (!(st.s < kSumLimit) || !(fabsf(st.u) < kSumLimit) || reference_missed(m_common, st.s)) {
+                // overflow (or NaN input, or a first pack without weight): redo this thread's packs with a moving reference
                 init_online(st);
                 for (i = threadIdx.x; i < nvec; i += THREADS)
                     accumulate_online<T>(STAGE ? stage4[i] : src4[i], c, st);

@@ -625,7 +625,8 @@ row_engine_kernel(const EngineArgs a)
             if (c == 0) {   // every thread reads the row's first pack: one reference for the whole row
                 float x[N], xmax;
                 Pack<T>::unpack(buf[0], x, xmax);
-                m_common = safe_reference(xmax, a.c);
+                // (without a weight in it, every thread moves from the lowest reference there is to its own first chunk's)
+                m_common = xmax > kNoWeight ? xmax * a.c : kNoReference;
                 ts.init(m_common);
                 // the next row is known now: request its scalars
                 row_n = sm.ring[(k + 1) & 3];

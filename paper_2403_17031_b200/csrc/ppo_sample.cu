@@ -240,9 +240,9 @@ sample_kernel(const SampleArgs a)
     float s, u;
     Race best;
     sums_and_race<T, VECTOR, false>(src, V, a.c, m, (uint32_t)row, a, sm, s, u, best);
-    if (!(s < 1.0e37f) || !(fabsf(u) < 1.0e37f)) {   // (s and u are the same in every thread)
+    if (!(s < 1.0e37f) || !(fabsf(u) < 1.0e37f) || reference_missed(m, s)) {   // (s and u are the same in every thread)
         // a sum overflowed (an element lies more than ~2^127 above the reference) or the row holds a NaN or
-        // +inf: take the exact maximum (NaN-blind; a NaN then shows up in the sums again) and repeat
+        // +inf, or its first pack only masked logits: take the exact maximum (NaN-blind; a NaN then shows up in the sums again) and repeat
         float mx = kNegBig;
         if (VECTOR) {
             const uint4 *src4 = reinterpret_cast<const uint4 *>(src);

@@ -325,3 +325,36 @@ def test_rows_far_below_zero_with_masked_padding(P, oracle, dtype, V, live, offs
     want[torch.arange(rows), tok.long()] += 1
     want /= float(np.float32(tau))
     assert_grad(npy(d["dlogits"].float()), npy(want), dtype == torch.bfloat16, "dlogits")
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("offset", [0.0, -60.0, -100.0, -400.0, 300.0])
+@pytest.mark.parametrize("V,first", [(50304, 8), (16384, 9000), (1000, 70), (1001, 8)])
+def test_rows_far_from_zero_whose_first_logits_are_masked(P, oracle, dtype, V, first, offset, lp_engine):
+    """No reference for the sums in a row's first elements: log-probs, entropy, the gradient, and a drawn token's."""
+    rows, tau = 12, 0.7
+    x = _rand_logits(rows, V, dtype, seed=V) + offset
+    x[:, :first] = -torch.inf
+    x[::2, V // 2 + 20:V // 2 + 90] = torch.finfo(dtype).min
+    tok = torch.full((rows,), V - 3, device="cuda", dtype=torch.int32)
+    lp, ent, lse = P.logprob_entropy(x, tok, tau, want_lse=True)
+    rlp, rent, rlse = oracle.logprob_entropy(host_logits(x), npy(tok), np.float32(tau))
+    assert_abs(npy(lp), rlp, TOL_LOGPROB, "logprob")
+    assert_abs(npy(ent), rent, TOL_LOGPROB, "entropy")
+    assert_abs(npy(lse), rlse, TOL_LOGPROB, "lse")
+    ws = P.new_workspace(P.workspace_bytes(rows, 1, V))
+    mask = torch.ones(rows, dtype=torch.uint8, device="cuda")
+    d = P.logprob_bwd(x, tok, mask, torch.ones(rows, device="cuda"), tau, ws, want_aux=True)
+    assert_abs(npy(d["new_logprob"]), rlp, TOL_LOGPROB, "new_logprob")
+    z = x.double() / float(np.float32(tau))
+    want = -torch.softmax(z, 1)
+    want[torch.arange(rows), tok.long()] += 1
+    want /= float(np.float32(tau))
+    assert_grad(npy(d["dlogits"].float()), npy(want), dtype == torch.bfloat16, "dlogits")
+    drawn, slp, sent, slse = P.sample_logprob_entropy(x, tau, 5, want_lse=True, workspace=ws)
+    assert P.last_device_status(ws) == 0
+    assert (drawn >= first).all() and torch.isfinite(x[torch.arange(rows), drawn.long()]).all()
+    assert_abs(npy(slse), rlse, TOL_LOGPROB, "lse of the draw")
+    assert_abs(npy(sent), rent, TOL_LOGPROB, "entropy of the draw")
+    want_lp, _, _ = oracle.logprob_entropy(host_logits(x), npy(drawn), np.float32(tau))
+    assert_abs(npy(slp), want_lp, TOL_LOGPROB, "log-prob of the draw")
