@@ -46,7 +46,6 @@ constexpr int kZeroBytes = 4096;                    // shared zeros, source of t
 #endif
 constexpr int kReuseReserveRows = PPO_REUSE_RESERVE_ROWS;
 constexpr int kMaxChunks = 14;                      // barriers provided per block
-constexpr size_t kMaxRowBytes = 224 * 1024;         // the largest row one block can hold
 #ifndef PPO_WAIT_TRIES
 #define PPO_WAIT_TRIES (1u << 20)
 #endif
@@ -64,6 +63,9 @@ struct EngineSmem {
     double lred[6 * 32];
     alignas(128) unsigned char zeros[kZeroBytes];
 };
+// the largest row one block can hold, in whole groups of 128 bytes beside its own shared memory
+constexpr size_t kMaxRowBytes = (227 * 1024 - sizeof(EngineSmem)) / 128 * 128;
+static_assert(kMaxRowBytes <= kMaxChunks * 2 * 512 * 16, "barriers for every chunk of the largest row");
 
 __device__ __forceinline__ uint32_t smem_addr(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
 

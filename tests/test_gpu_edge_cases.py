@@ -358,3 +358,23 @@ def test_rows_far_from_zero_whose_first_logits_are_masked(P, oracle, dtype, V, f
     assert_abs(npy(sent), rent, TOL_LOGPROB, "entropy of the draw")
     want_lp, _, _ = oracle.logprob_entropy(host_logits(x), npy(drawn), np.float32(tau))
     assert_abs(npy(slp), want_lp, TOL_LOGPROB, "log-prob of the draw")
+
+
+@pytest.mark.parametrize("dtype,V", [(torch.float32, 56444), (torch.float32, 56448), (torch.float32, 56452), (torch.float32, 57344), (torch.float32, 57348),
+                                     (torch.bfloat16, 112896), (torch.bfloat16, 112904), (torch.bfloat16, 114688)])
+def test_rows_of_about_the_size_of_an_sms_shared_memory(P, oracle, dtype, V, lp_engine):
+    rows = 5
+    x = _rand_logits(rows, V, dtype, seed=V)
+    tok = torch.randint(0, V, (rows,), device="cuda", dtype=torch.int32)
+    lp, ent, _ = P.logprob_entropy(x, tok, 0.7)
+    rlp, rent, _ = oracle.logprob_entropy(host_logits(x), npy(tok), np.float32(0.7))
+    assert_abs(npy(lp), rlp, TOL_LOGPROB, "logprob")
+    assert_abs(npy(ent), rent, TOL_LOGPROB, "entropy")
+    d = P.logprob_bwd(x, tok, torch.ones(rows, dtype=torch.uint8, device="cuda"), torch.ones(rows, device="cuda"), 0.7,
+                      P.new_workspace(P.workspace_bytes(rows, 1, V)), want_aux=True)
+    assert_abs(npy(d["new_logprob"]), rlp, TOL_LOGPROB, "new_logprob")
+    z = x.double() / float(np.float32(0.7))
+    want = -torch.softmax(z, 1)
+    want[torch.arange(rows), tok.long()] += 1
+    want /= float(np.float32(0.7))
+    assert_grad(npy(d["dlogits"].float()), npy(want), dtype == torch.bfloat16, "dlogits")
