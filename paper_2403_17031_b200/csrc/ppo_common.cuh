@@ -54,10 +54,14 @@ inline int32_t *ws_order(void *ws, int64_t rows)
 
 inline bool finite_f(float x) { return isfinite(x); }
 
+// (an error that is returned is not left behind for the next call's launch_status)
 #define PPO_RETURN_IF_CUDA(expr)                      \
     do {                                              \
         cudaError_t e__ = (expr);                     \
-        if (e__ != cudaSuccess) return (int)e__;      \
+        if (e__ != cudaSuccess) {                     \
+            (void)cudaGetLastError();                 \
+            return (int)e__;                          \
+        }                                             \
     } while (0)
 
 inline int launch_status()
