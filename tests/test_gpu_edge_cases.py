@@ -378,3 +378,23 @@ def test_rows_of_about_the_size_of_an_sms_shared_memory(P, oracle, dtype, V, lp_
     want[torch.arange(rows), tok.long()] += 1
     want /= float(np.float32(0.7))
     assert_grad(npy(d["dlogits"].float()), npy(want), dtype == torch.bfloat16, "dlogits")
+
+
+def test_a_returned_cuda_error_is_not_left_for_the_next_call(P, tmp_path):
+    """What the entry points return on a failed CUDA call (here one that names no device), and what a launch check after it sees."""
+    import ctypes as C
+    import subprocess
+
+    from paper_2403_17031_b200 import build
+    src = tmp_path / "probe.cu"
+    src.write_text("""
+#include "ppo_common.cuh"
+static int fails() { PPO_RETURN_IF_CUDA(cudaSetDevice(-5)); return 0; }
+extern "C" int returned() { return fails(); }
+extern "C" int left_behind() { fails(); return ppo::launch_status(); }
+""")
+    out = str(tmp_path / "probe.so")
+    subprocess.check_call([build._nvcc(), *build.NVCC_FLAGS, "-I", build.INCLUDE, "-I", build.CSRC, "-shared", "-cudart", "static", str(src),
+                           "-o", out])
+    probe = C.CDLL(out)
+    assert probe.returned() == 101 and probe.left_behind() == 0      # (cudaErrorInvalidDevice)

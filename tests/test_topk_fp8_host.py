@@ -141,22 +141,3 @@ def test_workspaces_are_cleared_and_read_on_the_stream_of_their_device(b, monkey
     monkeypatch.setattr(b, "_stream", lambda: "stream of " + current[0])
     assert b.last_device_status(b.new_workspace(256, "cuda:1")) == 0
     assert seen == [("stream of cuda:1", "cuda:1")] * 2 and current == ["cuda:0"]
-
-
-def test_a_returned_cuda_error_is_not_left_for_the_next_call(tmp_path):
-    """What the entry points return on a failed CUDA call, and what a launch check after it sees (no GPU: any CUDA error will do)."""
-    import subprocess
-
-    from paper_2403_17031_b200 import build
-    src = tmp_path / "probe.cu"
-    src.write_text("""
-#include "ppo_common.cuh"
-static int fails() { PPO_RETURN_IF_CUDA(cudaSetDevice(-5)); return 0; }
-extern "C" int returned() { return fails(); }
-extern "C" int left_behind() { fails(); return ppo::launch_status(); }
-""")
-    out = str(tmp_path / "probe.so")
-    subprocess.check_call([build._nvcc(), *build.NVCC_FLAGS, "-I", build.INCLUDE, "-I", build.CSRC, "-shared", "-cudart", "static", str(src),
-                           "-o", out])
-    probe = C.CDLL(out)
-    assert probe.returned() > 0 and probe.left_behind() == 0
