@@ -9,7 +9,7 @@
 // columns, so that a tile never holds more than 16 idle rows and the stream of B, which bounds the call, is read by
 // full 128 x 128 boxes. K is split over a cluster of blocks when there are too few tiles to occupy the SMs; the
 // partial tiles are joined through distributed shared memory in rank order, so results do not depend on timing.
-// 1 x 50304 x 4096 (206 MB of weight): 35.0 us = 5.9 TB/s with rings of three stages, so that four blocks fit on an SM and all
+// 1 x 50304 x 4096 (206 MB of weight): 35.6 us = 5.8 TB/s with rings of three stages, so that four blocks fit on an SM and all
 // 393 tiles are under way at once (four stages and three blocks: 36.9 us, six and two: 43 us).
 #include <cooperative_groups.h>
 
@@ -312,7 +312,7 @@ static int launch_narrow(Args a, const void *A, int64_t lda, const void *B, int6
     while (split < 8 && tiles * split * 2 <= narrow_places<MT>() && a.kb_total >= 4 * split) split *= 2;
     if (tiles * split >= ((int64_t)1 << 31)) return PPO_ERR_SHAPE;
     // Tiles of 16 and 32 columns: three stages once the SMs hold more than two blocks each, so that another fits (1 x 50304 x
-    // 4096: 35.0 instead of 36.9 us, 32 x 50304 x 4096: 40.5 instead of 51, 32 x 38000 x 4096: 32 instead of 52), else four
+    // 4096: 35.6 instead of 36.9 us, 32 x 50304 x 4096: 40.5 instead of 51, 32 x 38000 x 4096: 32 instead of 52), else four
     // (4 x 16384 x 4096: 16.2 instead of 16.5 us)
     if constexpr (MT <= 32)
         if (tiles * split > 2 * 148) return launch_narrow_stages<MT, 3>(a, ma, mb, split, s);

@@ -156,6 +156,8 @@ class Fp8LMHead:
     states. Hidden states and logit gradients are quantised per row and 128 columns on the way; logits are bf16.
 
     W [K, V] (bf16 or fp32) is quantised once, [V, K] for the logits and, with backward=True, [K, V] for the gradient.
+    Masked rows are multiplied like the others (their results are left out): for scores of a large batch that is half padding the
+    fused bf16 head, which leaves them out of its product, is the faster one.
     Buffers for M rows are kept and overwritten by the next call; everything runs on the current CUDA stream, and the
     calls can be captured into a CUDA graph.
     """
