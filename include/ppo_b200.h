@@ -58,7 +58,8 @@ extern "C" {
 #define PPO_DEV_BAD_TOKEN 1      /* a token id was outside [0, V): that row's outputs are NaN */
 #define PPO_DEV_EMPTY_MASK 2     /* mask selected no element: statistics / losses are 0 */
 #define PPO_DEV_TIMEOUT 4        /* a bounded wait inside a kernel gave up; outputs are invalid */
-#define PPO_DEV_BAD_ROW 8        /* ppo_sample_logprob_entropy, ppo_logprob_topk: a row had a NaN / +inf or no finite logit: ids -1 */
+#define PPO_DEV_BAD_ROW 8        /* ppo_sample_logprob_entropy, ppo_logprob_topk: a row had a NaN / +inf or no finite logit (the latter
+                                    also: one beyond its range): ids -1 */
 #define PPO_DEV_BAD_REUSE 16     /* ppo_loss_fwd_bwd_next_epoch: the workspace does not hold this mask's row order; nothing was written */
 
 /* indices into the losses[8] output of ppo_loss_fwd_bwd */

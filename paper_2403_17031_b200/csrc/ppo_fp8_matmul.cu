@@ -616,8 +616,8 @@ wide_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
         unsigned char *stage = ring + (size_t)kWideStages * kWideStage + (warp - 8) * kStageOut;
         const uint32_t taddr = tmem_base + c64 * 64 + ((uint32_t)(q * 32) << 16);
         bool alive = true, ready = false;                       // ready: the next accumulator is known to be there
-        // what this warp's arrivals count on: once it has given up, barriers that nobody waits for (the hot loop pays nothing for it;
-        // arrivals under a condition cost 2 %)
+        // what this warp's arrivals count on: once it has given up, barriers that nobody waits for (27136 x 50304 x 4096: 0.5 to
+        // 1 % for it; arrivals under a condition 2 to 3 %)
         uint32_t pair_empty = leader_addr(&sm.pair_empty[h][0]), scale_empty = saddr(&sm.scale_empty[0]);
         const auto wait_or_leave = [&](unsigned long long *bar, uint32_t parity) {
             if (alive && !wait(bar, parity, a.status)) {
