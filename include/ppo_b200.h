@@ -60,6 +60,7 @@ extern "C" {
 #define PPO_DEV_TIMEOUT 4        /* a bounded wait inside a kernel gave up; outputs are invalid */
 #define PPO_DEV_BAD_ROW 8        /* ppo_sample_logprob_entropy, ppo_logprob_topk: a row had a NaN / +inf or no finite logit (the latter
                                     also: one beyond its range): ids -1 */
+#define PPO_DEV_BAD_GRAD 32      /* ppo_grad_clip: a gradient held a NaN or an infinity: all results are NaN */
 #define PPO_DEV_BAD_REUSE 16     /* ppo_loss_fwd_bwd_next_epoch: the workspace does not hold this mask's row order; nothing was written */
 
 /* indices into the losses[8] output of ppo_loss_fwd_bwd */
@@ -506,6 +507,92 @@ size_t ppo_fp8_scratch_bytes(int64_t M, int64_t N, int64_t K);
 int ppo_fp8_matmul(const void *A, int64_t lda, const float *a_scales, const void *B, int64_t ldb,
                    const float *b_scales, int block_n, int64_t M, int64_t N, int64_t K, void *C, int out_dtype,
                    int64_t ldc, void *workspace, void *scratch, void *stream);
+
+/*
+ * Cross entropy at the LM head with both of its gradients, the supervised fine-tuning loss, without a matrix of M x V
+ * in memory: with z = H W / temperature [M, V] over the real rows (mask != 0 and label != ignore_id), n of them,
+ *     lse[r] = log sum_j exp(z[r, j]),   nll[r] = lse[r] - z[r, labels[r]],   loss = (sum of nll) / n,
+ *     dH, dW = gradients of scale * loss on H and W
+ *   H [M, K] bf16, row pitch ldh;  W bf16: w_layout PPO_W_KV: stored [K, V] (as in ppo_lmhead_logprob_entropy), PPO_W_VK:
+ *       stored [V, K] (the weight of a linear layer); row pitch ldw.  ldh and ldw are multiples of 8 (else
+ *       PPO_ERR_UNSUPPORTED), H and W 16-byte aligned; M, K and V are any sizes
+ *   labels [M] i32;  mask nullable [M] u8.  Rows that are not real are not multiplied; their nll, lse and dH are 0.  A real
+ *       row whose label is outside [0, V) makes loss, its nll, its row of dH and all of dW NaN and sets PPO_DEV_BAD_TOKEN
+ *   denom nullable [1] f32 device: divides the sum instead of n, e.g. the number of tokens of all micro-batches
+ *   loss [1] f32 device;  nll [M], lse nullable [M] f32
+ *   dH [M, K] bf16, row pitch lddh;  dW bf16, stored like W, row pitch lddw (any pitch >= the row's length, any address; 16-byte
+ *       aligned rows are faster); each nullable: without both the call is the loss alone.  Elements behind a row's end are
+ *       left alone.  No output may overlap an input
+ *   piece_rows   rows that are multiplied at a time (rounded up to 256; 0: at most 8192): scratch holds a piece x V in 16 bits,
+ *       and fp32 sums of dW where there are several pieces
+ *   workspace nullable (status word; n == 0 gives loss 0, zero gradients and PPO_DEV_EMPTY_MASK)
+ *   scratch  ppo_lmhead_xent_scratch_bytes(M, K, V, piece_rows, dH given, dW given) bytes, 256-byte aligned,
+ *       uninitialised, for this call alone while it runs (NULL where M == 0)
+ * Sums are fp32 on the tensor cores in an order that the sizes fix, so results are bit-reproducible; 2^(z - reference) and
+ * gradient factor times H are rounded to bf16 on the way to the gradients, which are rounded once more.
+ * Errors: PPO_ERR_PARAM (w_layout, temperature, scale), PPO_ERR_SHAPE, PPO_ERR_NULL, PPO_ERR_UNSUPPORTED, PPO_ERR_ALIGN.
+ * M == 0: loss and dW are 0.
+ */
+#define PPO_W_KV 0
+#define PPO_W_VK 1
+size_t ppo_lmhead_xent_scratch_bytes(int64_t M, int64_t K, int64_t V, int64_t piece_rows, int want_dh, int want_dw);
+int ppo_lmhead_xent(const void *H, int64_t ldh, const void *W, int64_t ldw, int w_layout, int64_t M, int64_t K, int64_t V,
+                    const int32_t *labels, const uint8_t *mask, int32_t ignore_id, float temperature, float scale,
+                    const float *denom, int64_t piece_rows, float *loss, float *nll, float *lse, void *dH, int64_t lddh,
+                    void *dW, int64_t lddw, void *workspace, void *scratch, void *stream);
+
+/*
+ * Rows of an embedding table, scaled: out[i, :] = scale * E[tokens[i], :]   (i < N)
+ *   table E [V, K] dtype, row pitch lde >= K elements;  out [N, K] out_dtype, row pitch ldo >= K; elements behind a row's K
+ *         are left alone.  Either may be fp32 or bf16, at any element-aligned address (16-byte accesses where K is a
+ *         multiple of 8 and both addresses and pitches are multiples of 16 bytes); each element is rounded once
+ *   tokens [N] i32;  a token outside [0, V) makes its row NaN and sets PPO_DEV_BAD_TOKEN
+ *   workspace nullable (status word)
+ * Errors: PPO_ERR_DTYPE, PPO_ERR_SHAPE, PPO_ERR_PARAM (scale not finite), PPO_ERR_NULL, PPO_ERR_ALIGN.  N == 0 is a
+ * successful no-op.
+ */
+int ppo_embed(const void *table, int dtype, int64_t V, int64_t K, int64_t lde, const int32_t *tokens, int64_t N,
+              float scale, void *out, int out_dtype, int64_t ldo, void *workspace, void *stream);
+
+/*
+ * Gradient of the table: dE[v, :] = scale * sum over the i with tokens[i] == v of dY[i, :].
+ *   dY [N, K] dtype, row pitch ldy;  dE [V, K] out_dtype, row pitch lde (elements behind a row's K are left alone)
+ *   padding_id  a token whose positions are left out: the gradient of its row is 0 (negative: none)
+ *   accumulate  0: dE is overwritten, with zeros in the rows of tokens that do not occur;  else the sums are added to
+ *               dE (each element rounded once more) and other rows are neither read nor written
+ *   workspace nullable (status word): a token outside [0, V) belongs to no row; it is left out and sets PPO_DEV_BAD_TOKEN
+ *   scratch   ppo_embed_bwd_scratch_bytes(N, K, V) bytes, 256-byte aligned, uninitialised, for this call alone while it
+ *             runs (NULL where N == 0)
+ * The positions of a token are summed in fp32, in an order that the sizes fix (ascending within chunks of neighbours in
+ * the order of tokens, then chunk by chunk): results are bit-reproducible.  dY must not overlap dE.
+ * Errors: PPO_ERR_DTYPE, PPO_ERR_SHAPE, PPO_ERR_PARAM (scale not finite), PPO_ERR_NULL, PPO_ERR_ALIGN.
+ */
+size_t ppo_embed_bwd_scratch_bytes(int64_t N, int64_t K, int64_t V);
+int ppo_embed_bwd(const void *dY, int dtype, int64_t N, int64_t K, int64_t ldy, const int32_t *tokens, int64_t V,
+                  float scale, int32_t padding_id, void *dE, int out_dtype, int64_t lde, int accumulate, void *workspace,
+                  void *scratch, void *stream);
+
+/*
+ * Global norm of n gradients and their clipping:
+ *     norm[0] = |scale| * sqrt(sum over all tensors and elements of x^2),   norm[1] = coef = min(1, max_norm / norm[0]),
+ *     out = x * (scale * coef), rounded once
+ *   in, out           host arrays of n device pointers; out NULL: in place. out[i] may be in[i] (same type); apart from
+ *                     that no two tensors overlap
+ *   numel, in_dtype   host arrays [n]: elements (>= 0, contiguous, any element-aligned address) and PPO_F32 or PPO_BF16
+ *   out_dtype         host array [n], NULL with out
+ *   scale             finite, not 0: e.g. 1 / (loss scale), applied before the norm;  max_norm > 0, may be infinite
+ *   norm [2] f32 device;  workspace nullable (status word)
+ *   scratch           ppo_grad_clip_scratch_bytes(n) bytes, 256-byte aligned, uninitialised, for this call alone while it runs
+ * In place, where scale * coef is 1 nothing is written.  A NaN or an infinity among the gradients makes norm (norm[0] may
+ * be an infinity) and every result NaN and sets PPO_DEV_BAD_GRAD.  Squares are summed in fp64 (runs of eight in fp32) in a
+ * fixed order, whatever the values' magnitude; a norm beyond fp32's range is returned as an infinity, coef stays right.
+ * The pointers travel as kernel arguments: the host arrays may be reused when the call returns, and a captured call keeps
+ * them.  Errors: PPO_ERR_SHAPE (n, numel), PPO_ERR_PARAM, PPO_ERR_NULL, PPO_ERR_DTYPE, PPO_ERR_ALIGN.
+ */
+size_t ppo_grad_clip_scratch_bytes(int32_t n);
+int ppo_grad_clip(int32_t n, const void *const *in /* host */, const int64_t *numel /* host */,
+                  const int32_t *in_dtype /* host */, void *const *out /* host */, const int32_t *out_dtype /* host */,
+                  float scale, float max_norm, float *norm, void *workspace, void *scratch, void *stream);
 
 /*
  * The whole path in one call.  ppo_step_io names every buffer of one PPO iteration over a batch of

@@ -17,7 +17,7 @@ PPO_F32, PPO_BF16 = 0, 1
 OPT_LOSS_ROW_CACHE = 1
 OPT_ROW_ENGINE = 2
 LOSS_NAMES = ("pg_loss", "vf_loss", "loss", "approx_kl", "pg_clipfrac", "vf_clipfrac", "entropy", "n")
-DEV_BAD_TOKEN, DEV_EMPTY_MASK, DEV_TIMEOUT, DEV_BAD_ROW, DEV_BAD_REUSE = 1, 2, 4, 8, 16
+DEV_BAD_TOKEN, DEV_EMPTY_MASK, DEV_TIMEOUT, DEV_BAD_ROW, DEV_BAD_REUSE, DEV_BAD_GRAD = 1, 2, 4, 8, 16, 32
 
 _ERR = {-1: "PPO_ERR_NULL", -2: "PPO_ERR_SHAPE", -3: "PPO_ERR_PARAM", -4: "PPO_ERR_ALIGN", -5: "PPO_ERR_DTYPE",
         -6: "PPO_ERR_UNSUPPORTED"}
@@ -133,6 +133,18 @@ _SIGS = {
     "ppo_fp8_matmul": (C.c_int, [C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_int, C.c_int64,
                                  C.c_int64, C.c_int64, C.c_void_p, C.c_int, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p]),
     "ppo_fp8_scratch_bytes": (C.c_size_t, [C.c_int64, C.c_int64, C.c_int64]),
+    "ppo_lmhead_xent_scratch_bytes": (C.c_size_t, [C.c_int64] * 4 + [C.c_int, C.c_int]),
+    "ppo_lmhead_xent": (C.c_int, [C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_int, C.c_int64, C.c_int64, C.c_int64,
+                                  C.c_void_p, C.c_void_p, C.c_int32, C.c_float, C.c_float, C.c_void_p, C.c_int64, C.c_void_p,
+                                  C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p,
+                                  C.c_void_p, C.c_void_p]),
+    "ppo_embed": (C.c_int, [C.c_void_p, C.c_int, C.c_int64, C.c_int64, C.c_int64, C.c_void_p, C.c_int64, C.c_float, C.c_void_p,
+                            C.c_int, C.c_int64, C.c_void_p, C.c_void_p]),
+    "ppo_embed_bwd_scratch_bytes": (C.c_size_t, [C.c_int64, C.c_int64, C.c_int64]),
+    "ppo_embed_bwd": (C.c_int, [C.c_void_p, C.c_int, C.c_int64, C.c_int64, C.c_int64, C.c_void_p, C.c_int64, C.c_float,
+                                C.c_int32, C.c_void_p, C.c_int, C.c_int64, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p]),
+    "ppo_grad_clip_scratch_bytes": (C.c_size_t, [C.c_int32]),
+    "ppo_grad_clip": (C.c_int, [C.c_int32] + [C.c_void_p] * 5 + [C.c_float, C.c_float] + [C.c_void_p] * 4),
     "ppo_lmhead_logprob_entropy": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int64, C.c_int64, C.c_int64, C.c_void_p,
                                              C.c_void_p, C.c_float, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
                                              C.c_void_p]),
@@ -754,3 +766,186 @@ def fp8_matmul(a: torch.Tensor, a_scales: torch.Tensor, b: torch.Tensor, b_scale
           int(block_n), M, N, K, out.data_ptr(), _logits_dtype(out), ldc, _addr(workspace, torch.uint8, at, "workspace"),
           _addr(scratch, torch.uint8, at, "scratch"))
     return out
+
+
+# ---------------------------------------------------------------- supervised fine-tuning
+def _matrix(t: torch.Tensor, at: int, name: str):
+    """(address, row pitch, dtype code) of a fp32 / bf16 matrix on device `at` whose rows are contiguous."""
+    if t.dim() != 2 or t.get_device() != at:
+        raise TypeError("%s must be a matrix on the device of the call's first tensor" % name)
+    _, _, pitch = _rows_of(t, name)
+    return t.data_ptr(), pitch, _logits_dtype(t)
+
+
+W_KV, W_VK = 0, 1
+
+
+def _head_weight(W: torch.Tensor, at: int, name: str):
+    """(address, row pitch, layout, V) of a bf16 weight [K, V] that is stored by rows ([K, V]) or by columns ([V, K], e.g. the
+    transpose of a linear layer's weight)."""
+    if W.dim() != 2 or W.get_device() != at or W.dtype != torch.bfloat16:
+        raise TypeError("%s must be a bfloat16 matrix on the device of the call's first tensor" % name)
+    K, V = W.shape
+    s0, s1 = W.stride()
+    if s1 == 1 and (s0 >= V or K <= 1):
+        return W.data_ptr(), s0 if K > 1 else -(-V // 8) * 8, W_KV
+    if s0 == 1 and (s1 >= K or V <= 1):
+        return W.data_ptr(), s1 if V > 1 else -(-K // 8) * 8, W_VK
+    raise TypeError("%s must be stored by rows or by columns" % name)
+
+
+def lmhead_xent_scratch_bytes(M: int, K: int, V: int, piece_rows: int = 0, want_dH: bool = True, want_dW: bool = True) -> int:
+    return int(lib().ppo_lmhead_xent_scratch_bytes(M, K, V, piece_rows, 1 if want_dH else 0, 1 if want_dW else 0))
+
+
+def lmhead_xent(H: torch.Tensor, W: torch.Tensor, labels: torch.Tensor, mask: Optional[torch.Tensor] = None,
+                ignore_id: int = -100, temperature: float = 1.0, scale: float = 1.0, denom: Optional[torch.Tensor] = None,
+                want_dH: bool = True, want_dW: bool = True, piece_rows: int = 0, workspace: Optional[torch.Tensor] = None,
+                scratch: Optional[torch.Tensor] = None, out=None):
+    """Cross entropy of labels [M] int32 under softmax(H [M, K] . W [K, V] / temperature), bf16, and its gradients, without the
+    logits in memory. W (and dW) may be stored by rows or by columns. Rows with mask 0 or label ignore_id are left out of the
+    mean; denom (a [1] f32 tensor) divides the sum instead of their number; scale multiplies the gradients.
+    Returns dict(loss (0-d f32), nll, lse [M] f32, dH [M, K] | None, dW [K, V] | None bf16); `out`: the same dict with the
+    tensors to write to (lse, dH and dW may be absent). scratch: at least lmhead_xent_scratch_bytes(...) bytes (uint8),
+    allocated here where none is given."""
+    at, f32, bf16 = H.get_device(), torch.float32, torch.bfloat16
+    if H.dim() != 2 or H.dtype != bf16 or not H.is_cuda:
+        raise TypeError("H must be a CUDA matrix of bfloat16")
+    M, K, ldh = _rows_of(H, "H")
+    wp, ldw, layout = _head_weight(W, at, "W")
+    V = W.shape[1]
+    if W.shape[0] != K:
+        raise ValueError("H [M,K] and W [K,V] disagree on K")
+    for t, name in ((labels, "labels"), (mask, "mask")):
+        _count(t, M, 1, name)
+    if M <= 1 and not (H.is_contiguous() and K % 8 == 0):
+        ldh = max(ldh, -(-K // 8) * 8)                  # (the pitch of a single row is anyone's choice)
+    if out is None:
+        empty = H.new_empty
+        dW = None
+        if want_dW:
+            dW = empty((K, V)) if layout == W_KV else empty((V, K)).t()
+        out = {"loss": empty((), dtype=f32), "nll": empty(M, dtype=f32), "lse": empty(M, dtype=f32),
+               "dH": empty((M, K)) if want_dH else None, "dW": dW}
+    get = out.get
+    dH, dW = get("dH"), get("dW")
+    for name, n in (("loss", 1), ("nll", M), ("lse", M)):
+        t = get(name)
+        if t is not None and t.numel() != n:
+            raise ValueError("%s must have %d elements" % (name, n))
+    dhp = dwp = None
+    lddh, lddw = K, K if layout == W_VK else V
+    if dH is not None:
+        dhp, lddh, _ = _matrix(dH, at, "dH")
+        if dH.shape != (M, K) or dH.dtype != bf16:
+            raise ValueError("dH must be a bfloat16 [%d, %d]" % (M, K))
+    if dW is not None:
+        dwp, lddw, dlayout = _head_weight(dW, at, "dW")
+        if dW.shape != W.shape or (dlayout != layout and min(K, V) > 1):
+            raise ValueError("dW must have the shape and the layout of W")
+    need = lmhead_xent_scratch_bytes(M, K, V, piece_rows, dH is not None, dW is not None)
+    if scratch is None:
+        scratch = H.new_empty(max(need, 1), dtype=torch.uint8)
+    elif scratch.numel() < need:
+        raise ValueError("lmhead_xent needs %d bytes of scratch (lmhead_xent_scratch_bytes)" % need)
+    u8 = torch.uint8
+    _call("ppo_lmhead_xent", at, H.data_ptr(), ldh, wp, ldw, layout, M, K, V, _addr(labels, torch.int32, at, "labels"),
+          _addr(mask, u8, at, "mask"), int(ignore_id), float(temperature), float(scale), _addr(denom, f32, at, "denom"),
+          int(piece_rows), _addr(get("loss"), f32, at, "loss"), _addr(get("nll"), f32, at, "nll"), _addr(get("lse"), f32, at, "lse"),
+          dhp, lddh, dwp, lddw, _addr(workspace, u8, at, "workspace"), _addr(scratch, u8, at, "scratch"))
+    return out
+
+
+def embed(table: torch.Tensor, tokens: torch.Tensor, scale: float = 1.0, out_dtype: Optional[torch.dtype] = None,
+          workspace: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """scale * table[tokens]: table [V, K] fp32 or bf16, tokens [...] int32 -> [..., K] in out_dtype (default: the table's).
+    `out`: the tensor to write to, [..., K] contiguous or [N, K] with a row pitch."""
+    at = table.get_device()
+    tp, lde, dt = _matrix(table, at, "table")
+    V, K = table.shape
+    N = tokens.numel()
+    if out is None:
+        out = table.new_empty((*tokens.shape, K), dtype=out_dtype)
+        ldo = K
+    else:
+        rows, cols, ldo = _rows_of(out, "out")
+        if (rows, cols) != (N, K) or out.get_device() != at:
+            raise ValueError("out must hold %d rows of %d, on the table's device" % (N, K))
+    _call("ppo_embed", at, tp, dt, V, K, lde, _addr(tokens, torch.int32, at, "tokens"), N, float(scale), out.data_ptr(),
+          _logits_dtype(out), ldo, _addr(workspace, torch.uint8, at, "workspace"))
+    return out
+
+
+def embed_bwd_scratch_bytes(N: int, K: int, V: int) -> int:
+    return int(lib().ppo_embed_bwd_scratch_bytes(N, K, V))
+
+
+def embed_bwd(dY: torch.Tensor, tokens: torch.Tensor, V: int, scale: float = 1.0, padding_id: int = -1,
+              out_dtype: Optional[torch.dtype] = None, accumulate: bool = False, workspace: Optional[torch.Tensor] = None,
+              scratch: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Gradient dY [..., K] on embed()'s rows -> gradient of the table [V, K] in out_dtype (default: dY's). Positions with
+    padding_id (negative: none) are left out. accumulate: add to `out`, in the rows of the tokens that occur.
+    scratch: at least embed_bwd_scratch_bytes(N, K, V) bytes (uint8), allocated here where none is given."""
+    at = dY.get_device()
+    N, K, ldy = _rows_of(dY, "dY")
+    _count(tokens, N, 1, "tokens")
+    if out is None:
+        if accumulate:
+            raise ValueError("accumulate needs the tensor to add to")
+        out = dY.new_empty((V, K), dtype=out_dtype)
+    op, lde, odt = _matrix(out, at, "out")
+    if out.shape != (V, K):
+        raise ValueError("out must have shape %s" % ((V, K),))
+    need = embed_bwd_scratch_bytes(N, K, V)
+    if scratch is None:
+        scratch = dY.new_empty(max(need, 1), dtype=torch.uint8)
+    elif scratch.numel() < need:
+        raise ValueError("embed_bwd needs %d bytes of scratch (embed_bwd_scratch_bytes)" % need)
+    _call("ppo_embed_bwd", at, dY.data_ptr(), _logits_dtype(dY), N, K, ldy, _addr(tokens, torch.int32, at, "tokens"), V,
+          float(scale), int(padding_id), op, odt, lde, 1 if accumulate else 0, _addr(workspace, torch.uint8, at, "workspace"),
+          _addr(scratch, torch.uint8, at, "scratch"))
+    return out
+
+
+def grad_clip_scratch_bytes(n: int) -> int:
+    return int(lib().ppo_grad_clip_scratch_bytes(n))
+
+
+def grad_clip(grads, max_norm: float, scale: float = 1.0, out=None, workspace: Optional[torch.Tensor] = None,
+              scratch: Optional[torch.Tensor] = None, norm: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Scales a list of gradients (contiguous, fp32 or bf16) by scale * min(1, max_norm / norm) with the norm over all of
+    scale * gradients; in place, or into the list `out` (each fp32 or bf16). Returns norm [2] f32: the norm before clipping
+    and the factor min(1, max_norm / norm)."""
+    n = len(grads)
+    if not n:
+        raise ValueError("grad_clip needs a gradient")
+    at = grads[0].get_device()
+    if not grads[0].is_cuda:
+        raise TypeError("gradients must be CUDA tensors")
+
+    def arrays(tensors, name):
+        for t in tensors:
+            if t.get_device() != at or not t.is_contiguous():
+                raise TypeError("%s must be contiguous tensors on one device" % name)
+        return (C.c_void_p * n)(*[t.data_ptr() for t in tensors]), (C.c_int32 * n)(*[_logits_dtype(t) for t in tensors])
+
+    ins, in_dtype = arrays(grads, "gradients")
+    numel = [t.numel() for t in grads]
+    outs = out_dtype = None
+    if out is not None:
+        if [t.numel() for t in out] != numel:
+            raise ValueError("out must hold a tensor of the same size for each gradient")
+        outs, out_dtype = arrays(out, "out")
+    if norm is None:
+        norm = grads[0].new_empty(2, dtype=torch.float32)
+    elif norm.numel() != 2:
+        raise ValueError("norm has two elements")
+    need = grad_clip_scratch_bytes(n)
+    if scratch is None:
+        scratch = grads[0].new_empty(need, dtype=torch.uint8)
+    elif scratch.numel() < need:
+        raise ValueError("grad_clip needs %d bytes of scratch (grad_clip_scratch_bytes)" % need)
+    _call("ppo_grad_clip", at, n, ins, (C.c_int64 * n)(*numel), in_dtype, outs, out_dtype, float(scale), float(max_norm),
+          _addr(norm, torch.float32, at, "norm"), _addr(workspace, torch.uint8, at, "workspace"),
+          _addr(scratch, torch.uint8, at, "scratch"))
+    return norm

@@ -405,15 +405,6 @@ struct Piece {
     }
 };
 
-// unit -> output tile: blocks of gm x gn tiles (m fastest inside), column of blocks by column of blocks; a block's
-// tiles run at the same time and share their operand panels through L2
-__device__ __forceinline__ int2 tile_of(int u, int m_tiles, int n_tiles, int gm, int gn)
-{
-    const int col = u / (m_tiles * gn), width = min(gn, n_tiles - col * gn), rest = u - col * m_tiles * gn;
-    const int blk = rest / (gm * width), height = min(gm, m_tiles - blk * gm), in = rest - blk * gm * width;
-    return make_int2(blk * gm + in % height, col * gn + in / height);
-}
-
 // this thread's loads so far have arrived, in `r` (which the compiler may not use before)
 __device__ __forceinline__ void tmem_wait16(uint32_t (&r)[16])
 {

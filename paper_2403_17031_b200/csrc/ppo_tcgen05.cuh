@@ -266,6 +266,18 @@ __device__ __forceinline__ void tma_load_2d_pair(void *dst, const CUtensorMap *m
         : "memory");
 }
 
+__device__ __forceinline__ void mma_pair(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile(
+        "{\n"
+        ".reg .pred p;\n"
+        "setp.ne.b32 p, %4, 0;\n"
+        "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, {%5, %5, %5, %5, %5, %5, %5, %5}, p;\n"
+        "}\n"
+        ::"r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate), "r"(0u)
+        : "memory");
+}
+
 __device__ __forceinline__ void mma_f8_pair(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate)
 {
     asm volatile(
@@ -298,6 +310,15 @@ __device__ __forceinline__ void tmem_free_all_pair(uint32_t base)
     asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(base), "r"(512u) : "memory");
 }
 
+// unit -> output tile: blocks of gm x gn tiles (m fastest inside), column of blocks by column of blocks; a block's
+// tiles run at the same time and share their operand panels through L2
+__device__ __forceinline__ int2 tile_of(int u, int m_tiles, int n_tiles, int gm, int gn)
+{
+    const int col = u / (m_tiles * gn), width = min(gn, n_tiles - col * gn), rest = u - col * m_tiles * gn;
+    const int blk = rest / (gm * width), height = min(gm, m_tiles - blk * gm), in = rest - blk * gm * width;
+    return make_int2(blk * gm + in % height, col * gn + in / height);
+}
+
 // ---------------------------------------------------------------- host side
 typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
                                   const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
@@ -316,19 +337,25 @@ inline EncodeTiledFn encode_fn()
     return fn;
 }
 
-// 2-D bf16 tensor [outer, inner] (inner contiguous), box [box_outer, 64], 128-byte swizzle, zero fill outside
-inline int make_map(CUtensorMap *map, const void *base, uint64_t inner, uint64_t outer, uint32_t box_outer)
+// 2-D bf16 tensor [outer, inner] (inner contiguous, rows `pitch` elements apart: a multiple of 8), box [box_outer, 64],
+// 128-byte swizzle, zero fill outside
+inline int make_map_pitch(CUtensorMap *map, const void *base, uint64_t inner, uint64_t outer, uint64_t pitch, uint32_t box_outer)
 {
     EncodeTiledFn fn = encode_fn();
     if (!fn) return (int)cudaErrorNotSupported;
     const cuuint64_t dims[2] = {inner, outer};
-    const cuuint64_t strides[1] = {inner * 2};
+    const cuuint64_t strides[1] = {pitch * 2};
     const cuuint32_t box[2] = {64, box_outer};
     const cuuint32_t elem[2] = {1, 1};
     const CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(base), dims, strides, box, elem,
                           CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS ? PPO_OK : (int)cudaErrorInvalidValue;
+}
+
+inline int make_map(CUtensorMap *map, const void *base, uint64_t inner, uint64_t outer, uint32_t box_outer)
+{
+    return make_map_pitch(map, base, inner, outer, inner, box_outer);
 }
 
 // 2-D tensor of 8-bit elements [outer, inner] with a row pitch in bytes (a multiple of 16), box [box_outer, 128]
