@@ -14,8 +14,13 @@
 // The reference is a multiple of 64 near the largest y of the row's 128 columns, so U and its sums stay inside fp32's (and
 // bf16's) exponents for logits of any size, and almost always all of a row's references are the same; where they are not, the
 // columns with a smaller one are multiplied by 2^(difference), which is exact, before product 2.
-// Roundings to 16 bits: U (the gradient on the logits, which the fused LM head's backward rounds as well), a H, and the
-// results. Statistics, sums and nll are fp32, the loss fp64.
+//
+// Roundings to 16 bits: U, a H, and the results. Statistics, sums and nll are fp32, the loss fp64. What the rounding of U
+// would do to the gradients is kept small in three ways. S in the gradient is the sum of the rounded U, so that D is the
+// gradient of a softmax whose probabilities are off by half a step each and still add up to 1: a direction that all columns
+// of W share drops out of dH (logits far from 0 have one), as it should. U' at the label, about -S, is the largest element
+// of its row by far; what its own rounding leaves, e = (U - S) - U', comes back in fp32: in product 2 as e W[:, label], in
+// the epilogue, and in product 3 by a factor that makes a U' exact there (the row's other elements take that half step).
 //
 // Product kernel: persistent pairs of blocks (cta_group::2) on 256 x 256 tiles; per block one TMA producer warp (stages of
 // 64 along the contraction, 128-byte swizzle), in the leader one issuer warp, eight epilogue warps that drain one 256-column
@@ -52,13 +57,16 @@ struct Args {
     float c;                                               // log2(e) / tau
     const int32_t *labels, *order;                         // order[i]: the original row of real row i
     float *picked;                                         // [rows] accumulator at the label
-    float2 *part;                                          // [rows][chunks] reference, sum
+    float4 *part;                                          // [rows][chunks] reference, sum, sum of the rounded values
     int chunks, store;
     // results
     __nv_bfloat16 *out;
     int64_t ldo;
     int bulk_cols;                                         // bulk stores take boxes that end at or before this column
-    const float *row_scale;                                // kHidden
+    // kHidden
+    const float2 *row_scale;                               // [rows] a, a e
+    const __nv_bfloat16 *W;
+    int64_t ldw;
     float *scratch;                                        // kHidden: parts of tiles cut along the contraction; kWeight: sums over the pieces
 };
 
@@ -169,19 +177,59 @@ __device__ __forceinline__ void store_rows(const unsigned char *stage, __nv_bflo
     }
 }
 
-// 32 values of a row, the half `h` of 64 columns, into the staging buffer
-__device__ __forceinline__ void stage32(unsigned char *stage, int lane, int h, const float *v)
+__device__ __forceinline__ uint32_t pack2(float lo, float hi)
+{
+    const __nv_bfloat162 b2 = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t *>(&b2);
+}
+__device__ __forceinline__ float low(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float high(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
+
+// 32 values of a row, the half `h` of 64 columns, into the staging buffer; returns the sum of what was stored
+__device__ __forceinline__ float stage32(unsigned char *stage, int lane, int h, const float *v)
 {
     unsigned char *row = stage + lane * 128;
+    float s = 0.f;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         uint32_t w[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const __nv_bfloat162 b2 = __floats2bfloat162_rn(v[j * 8 + e * 2], v[j * 8 + e * 2 + 1]);
-            w[e] = *reinterpret_cast<const uint32_t *>(&b2);
+            w[e] = pack2(v[j * 8 + e * 2], v[j * 8 + e * 2 + 1]);
+            s += low(w[e]) + high(w[e]);
         }
         *reinterpret_cast<uint4 *>(row + (((h * 4 + j) ^ (lane & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    return s;
+}
+
+// f * W[k .. k + N, label] added to N neighbouring elements of a row of dH; VK: W is stored [V, K]
+template <bool VK, int N>
+__device__ __forceinline__ void add_label(const Args &a, float f, int label, int k, float *v)
+{
+    if (VK) {
+        const __nv_bfloat16 *w = a.W + (int64_t)label * a.ldw + k;
+#pragma unroll
+        for (int j = 0; j < N; j += 4) {
+            if (k + j + 4 <= a.dim_n) {
+                const uint2 x = __ldg(reinterpret_cast<const uint2 *>(w + j));
+                v[j] = fmaf(f, low(x.x), v[j]);
+                v[j + 1] = fmaf(f, high(x.x), v[j + 1]);
+                v[j + 2] = fmaf(f, low(x.y), v[j + 2]);
+                v[j + 3] = fmaf(f, high(x.y), v[j + 3]);
+            } else {
+#pragma unroll
+                for (int e = j; e < j + 4; ++e)
+                    if (k + e < a.dim_n) v[e] = fmaf(f, __bfloat162float(w[e]), v[e]);
+            }
+        }
+    } else {
+        const __nv_bfloat16 *w = a.W + (int64_t)k * a.ldw + label;
+        float x[N];
+#pragma unroll
+        for (int j = 0; j < N; ++j) x[j] = k + j < a.dim_n ? __bfloat162float(w[(int64_t)j * a.ldw]) : 0.f;
+#pragma unroll
+        for (int j = 0; j < N; ++j) v[j] = fmaf(f, x[j], v[j]);
     }
 }
 
@@ -314,7 +362,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             const uint32_t taddr = tmem_base + buf * kTile + h * 128 + ((uint32_t)(q * 32) << 16);
             bool ok = false;
             int label = -1, out_row = -1;
-            float scale = 0.f;
+            float2 scale = make_float2(0.f, 0.f);
             if (PRODUCT == kLogits) {
                 ok = row < rows;
                 if (ok) label = a.labels[a.order[a.row0 + row]] - n;
@@ -323,6 +371,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                 if (ok && work.part < 0) {
                     out_row = a.order[a.row0 + row];
                     scale = a.row_scale[row];
+                    label = scale.y != 0.f ? a.labels[out_row] : -1;
                 }
             } else {
                 ok = row < a.dim_m;
@@ -385,7 +434,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                     }
                 }
                 const float ref = 64.f * rintf(fmaxf(m * a.c, -1e9f) * (1.f / 64.f));
-                float s = 0.f;
+                float s = 0.f, rounded = 0.f;
 #pragma unroll 1
                 for (int cc = 0; cc < 4; ++cc) {
                     float v[32];
@@ -404,11 +453,11 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                     }
                     if (a.store) {
                         if ((cc & 1) == 0) reuse();
-                        stage32(stage, lane, cc & 1, v);
+                        rounded += stage32(stage, lane, cc & 1, v);
                         if ((cc & 1) && n + (cc - 1) * 32 < a.dim_n) send((cc - 1) * 32, true);
                     }
                 }
-                if (ok && n < a.dim_n) a.part[(size_t)row * a.chunks + n / kChunk] = make_float2(ref, s);
+                if (ok && n < a.dim_n) a.part[(size_t)row * a.chunks + n / kChunk] = make_float4(ref, s, rounded, 0.f);
             } else if (PRODUCT == kHidden) {
                 // (four columns of 256 rows follow one another in scratch: a warp writes 512 bytes at a time)
                 float4 *part = reinterpret_cast<float4 *>(a.scratch + (size_t)(pair * 2 + max(work.part, 0)) * kTileFloats) +
@@ -424,7 +473,8 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                         continue;
                     }
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) v[j] *= scale;
+                    for (int j = 0; j < 32; ++j) v[j] *= scale.x;
+                    if (label >= 0) add_label<B_MN, 32>(a, scale.y, label, n + cc * 32, v);
                     stage32(stage, lane, cc & 1, v);
                     if ((cc & 1) && n + (cc - 1) * 32 < a.dim_n) send((cc - 1) * 32, false);
                 }
@@ -478,6 +528,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
 // The tiles of dH that were cut along the vocabulary: a block adds up 32 rows x 64 columns over the pairs that hold parts of
 // them, in the order of the contraction, and turns them in shared memory so that rows leave in runs.
 constexpr int kJoinThreads = 256, kJoinBlocks = (kTile / 32) * (kTile / 64);
+template <bool VK>
 __global__ void __launch_bounds__(kJoinThreads)
 join_kernel(const Args a, int pairs)
 {
@@ -510,13 +561,14 @@ join_kernel(const Args a, int pairs)
     for (int h = 0; h < 2; ++h) {
         const int r = (threadIdx.x >> 4) + h * 16, n = n0 + c4 * 4;
         if (m0 + r >= rows || n >= a.dim_n) continue;
-        const float s = a.row_scale[m0 + r];
+        const float2 s = a.row_scale[m0 + r];
         const float4 x = turn[r][c4];
-        const float y[4] = {x.x * s, x.y * s, x.z * s, x.w * s};
-        __nv_bfloat16 *to = a.out + (int64_t)a.order[a.row0 + m0 + r] * a.ldo + n;
+        float y[4] = {x.x * s.x, x.y * s.x, x.z * s.x, x.w * s.x};
+        const int row = a.order[a.row0 + m0 + r];
+        if (s.y != 0.f) add_label<VK, 4>(a, s.y, a.labels[row], n, y);
+        __nv_bfloat16 *to = a.out + (int64_t)row * a.ldo + n;
         if (n + 4 <= a.dim_n && reinterpret_cast<uintptr_t>(to) % 8 == 0) {
-            const __nv_bfloat162 lo = __floats2bfloat162_rn(y[0], y[1]), hi = __floats2bfloat162_rn(y[2], y[3]);
-            *reinterpret_cast<uint2 *>(to) = make_uint2(*reinterpret_cast<const uint32_t *>(&lo), *reinterpret_cast<const uint32_t *>(&hi));
+            *reinterpret_cast<uint2 *>(to) = make_uint2(pack2(y[0], y[1]), pack2(y[2], y[3]));
         } else {
             for (int e = 0; e < 4 && n + e < a.dim_n; ++e) to[e] = __float2bfloat16_rn(y[e]);
         }
@@ -539,8 +591,9 @@ struct RowArgs {
     __nv_bfloat16 *scaled;                                      // [rows_max, Kp] a H; null: no gradients
     __nv_bfloat16 *u;                                           // [rows_max, Vp]
     int64_t Vp;
-    float *picked, *row_scale;
-    float2 *part;
+    float *picked;
+    float2 *row_scale;
+    float4 *part;
     int chunks, row0, rows_max;
     float *loss, *nll, *lse;
     __nv_bfloat16 *dH;
@@ -613,11 +666,11 @@ pack_kernel(const RowArgs a)
     }
 }
 
-// A row's statistics out of its chunks', its loss and the factor of its gradient; U at the label; a H
+// A row's statistics out of its chunks', its loss and the factors of its gradient; U at the label; a H
 __global__ void __launch_bounds__(kRowThreads)
 row_kernel(const RowArgs a)
 {
-    __shared__ float red[64];
+    __shared__ float red[3][kRowThreads / 32];
     const int n_real = *a.n_real, rows = max(0, min(a.rows_max, n_real - a.row0)), r = blockIdx.x;
     __nv_bfloat16 *scaled = a.scaled ? a.scaled + (int64_t)r * a.Kp : nullptr;
     if (r >= rows) {
@@ -629,54 +682,69 @@ row_kernel(const RowArgs a)
     const int row = a.order[a.row0 + r], lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int label = a.labels[row];
     const bool bad = label < 0 || label >= a.V;
-    const float2 *part = a.part + (size_t)r * a.chunks;
+    const float4 *part = a.part + (size_t)r * a.chunks;
     float m = kNoRef;
     for (int t = threadIdx.x; t < a.chunks; t += kRowThreads) m = fmaxf(m, part[t].x);
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, off));
-    if (lane == 0) red[warp] = m;
+    if (lane == 0) red[0][warp] = m;
     __syncthreads();
-    m = red[0];
 #pragma unroll
-    for (int w = 1; w < kRowThreads / 32; ++w) m = fmaxf(m, red[w]);
-    float s = 0.f;
+    for (int w = 0; w < kRowThreads / 32; ++w) m = fmaxf(m, red[0][w]);
+    float s = 0.f, sr = 0.f;                                    // sums of U and of the rounded U
     for (int t = threadIdx.x; t < a.chunks; t += kRowThreads) {
-        const float2 p = part[t];
+        const float4 p = part[t];
         const float f = ex2(p.x - m);
         s = fmaf(p.y, f, s);
+        sr = fmaf(p.z, f, sr);
         if (p.x != m && a.u) {
-            // (16-byte pieces of 8 columns; the columns behind V are zeros)
+            // (16-byte pieces of 8 columns; the columns behind V are not used)
             uint4 *u = reinterpret_cast<uint4 *>(a.u + (int64_t)r * a.Vp + (int64_t)t * kChunk);
             const int64_t left = a.Vp - (int64_t)t * kChunk;
             for (int j = 0; j < kChunk / 8 && j * 8 < left; ++j) {
                 uint4 v = u[j];
                 uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const __nv_bfloat162 b2 = __floats2bfloat162_rn(__uint_as_float(w[e] << 16) * f, __uint_as_float(w[e] & 0xffff0000u) * f);
-                    w[e] = *reinterpret_cast<const uint32_t *>(&b2);
-                }
+                for (int e = 0; e < 4; ++e) w[e] = pack2(low(w[e]) * f, high(w[e]) * f);
                 u[j] = make_uint4(w[0], w[1], w[2], w[3]);
             }
         }
     }
     s = warp_sum_f(s);
-    if (lane == 0) red[32 + warp] = s;
+    sr = warp_sum_f(sr);
+    if (lane == 0) {
+        red[1][warp] = s;
+        red[2][warp] = sr;
+    }
     __syncthreads();
-    s = 0.f;
+    s = sr = 0.f;
 #pragma unroll
-    for (int w = 0; w < kRowThreads / 32; ++w) s += red[32 + w];
-    const float l2s = log2f(s);
-    const float nan = __int_as_float(0x7fffffff);
-    const float y = bad ? nan : a.picked[r] * a.c;              // the label's logit, base 2
-    const float f = bad ? nan : a.scale * a.inv_tau / ((a.denom ? *a.denom : (float)n_real) * s);
+    for (int w = 0; w < kRowThreads / 32; ++w) {
+        s += red[1][w];
+        sr += red[2][w];
+    }
+    const float l2s = log2f(s), nan = __int_as_float(0x7fffffff);
+    const float acc = bad ? nan : a.picked[r];
     if (threadIdx.x == 0) {
-        a.nll[row] = ((m - y) + l2s) * kLn2;
+        a.nll[row] = ((m - acc * a.c) + l2s) * kLn2;
         if (a.lse) a.lse[row] = (m + l2s) * kLn2;
-        if (a.row_scale) a.row_scale[r] = f;
-        if (a.u && !bad) a.u[(int64_t)r * a.Vp + label] = __float2bfloat16_rn(ex2(y - m) - s);
         if (bad && a.status) atomicOr(a.status, PPO_DEV_BAD_TOKEN);
     }
+    if (!a.u) return;
+    // U at the label, as product 1 stored it, less S; in bf16, and what that leaves
+    float f2 = nan, f3 = nan, left = 0.f;
+    if (!bad) {
+        const float ref = part[label / kChunk].x;
+        const float u = __bfloat162float(__float2bfloat16_rn(ex2(fmaf(acc, a.c, -ref)))) * ex2(ref - m);
+        const float want = u - sr;
+        const __nv_bfloat16 stored = __float2bfloat16_rn(want);
+        const float got = __bfloat162float(stored);
+        f2 = a.scale * a.inv_tau / ((a.denom ? *a.denom : (float)n_real) * sr);
+        f3 = got != 0.f ? f2 * (want / got) : f2;
+        left = f2 * (want - got);
+        if (threadIdx.x == 0) a.u[(int64_t)r * a.Vp + label] = stored;
+    }
+    if (threadIdx.x == 0) a.row_scale[r] = make_float2(f2, left);
     if (!scaled) return;
     const __nv_bfloat16 *h = a.H + (int64_t)row * a.ldh;
     for (int k = threadIdx.x * 8; k < a.K; k += kRowThreads * 8) {
@@ -684,13 +752,10 @@ row_kernel(const RowArgs a)
             const uint4 v = *reinterpret_cast<const uint4 *>(h + k);
             uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const __nv_bfloat162 b2 = __floats2bfloat162_rn(__uint_as_float(w[e] << 16) * f, __uint_as_float(w[e] & 0xffff0000u) * f);
-                w[e] = *reinterpret_cast<const uint32_t *>(&b2);
-            }
+            for (int e = 0; e < 4; ++e) w[e] = pack2(low(w[e]) * f3, high(w[e]) * f3);
             *reinterpret_cast<uint4 *>(scaled + k) = make_uint4(w[0], w[1], w[2], w[3]);
         } else {
-            for (int e = k; e < a.K; ++e) scaled[e] = __float2bfloat16_rn(__bfloat162float(h[e]) * f);
+            for (int e = k; e < a.K; ++e) scaled[e] = __float2bfloat16_rn(__bfloat162float(h[e]) * f3);
         }
     }
 }
@@ -742,8 +807,8 @@ static Layout layout_of(int64_t M, int64_t K, int64_t V, int64_t piece_rows, boo
     l.n_real = take(4);
     l.order = take((size_t)M * 4);
     l.picked = take(rows * 4);
-    l.row_scale = take(rows * 4);
-    l.part = take(rows * (size_t)l.chunks * sizeof(float2));
+    l.row_scale = take(rows * sizeof(float2));
+    l.part = take(rows * (size_t)l.chunks * sizeof(float4));
     l.packed = take((size_t)M * l.Kp * 2);
     l.scaled = take(dw ? rows * l.Kp * 2 : 0);
     l.u = take(grad ? rows * (size_t)l.Vp * 2 : 0);
@@ -846,8 +911,8 @@ extern "C" int ppo_lmhead_xent(const void *H, int64_t ldh, const void *W, int64_
     r.u = grad ? reinterpret_cast<__nv_bfloat16 *>(mem + l.u) : nullptr;
     r.Vp = l.Vp;
     r.picked = reinterpret_cast<float *>(mem + l.picked);
-    r.row_scale = grad ? reinterpret_cast<float *>(mem + l.row_scale) : nullptr;
-    r.part = reinterpret_cast<float2 *>(mem + l.part);
+    r.row_scale = reinterpret_cast<float2 *>(mem + l.row_scale);
+    r.part = reinterpret_cast<float4 *>(mem + l.part);
     r.chunks = l.chunks; r.rows_max = l.rows_max;
     r.loss = loss; r.nll = nll; r.lse = lse; r.dH = reinterpret_cast<__nv_bfloat16 *>(dH);
     r.status = status;
@@ -873,7 +938,7 @@ extern "C" int ppo_lmhead_xent(const void *H, int64_t ldh, const void *W, int64_
     Args a1 = a, a2 = a, a3 = a;
     a1.dim_m = l.rows_max; a1.dim_n = (int)V; a1.dim_k = (int)K; a1.gm = 9; a1.gn = 8;
     a2.dim_m = l.rows_max; a2.dim_n = (int)K; a2.dim_k = (int)V; a2.gm = 9; a2.gn = 8;
-    a2.out = r.dH; a2.ldo = lddh;
+    a2.out = r.dH; a2.ldo = lddh; a2.W = reinterpret_cast<const __nv_bfloat16 *>(W); a2.ldw = ldw;
     a2.scratch = reinterpret_cast<float *>(mem + l.parts);
     a3.dim_m = (int)w_outer; a3.dim_n = (int)w_inner; a3.dim_k = l.rows_max; a3.gm = 8; a3.gn = 9;
     a3.out = reinterpret_cast<__nv_bfloat16 *>(dW); a3.ldo = lddw;
@@ -902,7 +967,7 @@ extern "C" int ppo_lmhead_xent(const void *H, int64_t ldh, const void *W, int64_
             rc = vk ? launch_product<false, true, kHidden>(m_u2, m_u2, m_w2, m_u2, a2, pairs, s)
                     : launch_product<false, false, kHidden>(m_u2, m_u2, m_w2, m_u2, a2, pairs, s);
             if (rc) return rc;
-            join_kernel<<<(unsigned)((pairs - 1) * kJoinBlocks), kJoinThreads, 0, s>>>(a2, pairs);
+            (vk ? join_kernel<true> : join_kernel<false>)<<<(unsigned)((pairs - 1) * kJoinBlocks), kJoinThreads, 0, s>>>(a2, pairs);
             if ((rc = launch_status())) return rc;
         }
         if (dW) {

@@ -3,8 +3,10 @@
 Tolerances, element by element. A logit is a sum of K products in fp32, each addition off by at most 2^-23 of its absolute partial sum
 (rounded or cut off): ez = (K + 4) 2^-23 max_j sum_k |h_k w_kj| / tau, and its scaling to base 2 adds 2^-23 of its size. The log-sum-exp
 moves by at most the largest of these; its own sum of up to 128 exponentials (2^-22 each), joined over the chunks, adds less than
-(128 + chunks) 2^-23. U is off by those, relative, and by half a step of bf16 (2^-8); so is a H by half a step; results by half a step of
-their own; the products over V columns or M rows by (V + 4) 2^-23 and (M + 4) 2^-23 of the sums of the absolute products."""
+(128 + chunks) 2^-23. U is off by those, relative, and by half a step of bf16 (2^-8); the sum of the rounded U, which divides it, by another
+half step at most: two for dH, in the worst case, and as much for 1 - p at the label. In dW a H adds half a step and the factor that
+makes U at the label exact one more. Results are off by half a step of their own; the products over V columns or M rows by (V + 4) 2^-23 and
+(M + 4) 2^-23 of the sums of the absolute products."""
 import numpy as np
 import pytest
 import torch
@@ -66,12 +68,12 @@ def check(o, H, W, labels, real, tau, scale=1.0, denom=None):
         p[r, npy(labels)[r]] = abs(scale) / (d * tau) * er[r, 0]
     tiny = 2.0 ** -120
     if o["dH"] is not None:
-        tol = (STEP * D + p) @ np.abs(w).T + (V + 4) * EPS * (D @ np.abs(w).T) + STEP * np.abs(want["dH"]) + tiny
+        tol = (2 * STEP * D + p) @ np.abs(w).T + (V + 4) * EPS * (D @ np.abs(w).T) + STEP * np.abs(want["dH"]) + tiny
         assert (np.abs(f64(o["dH"]) - want["dH"]) <= 1.01 * tol).all()
         assert not f64(o["dH"])[~real].any()
     if o["dW"] is not None:
         ah = np.abs(h) * real[:, None]
-        tol = ah.T @ (2 * STEP * D + p) + (M + 4) * EPS * (ah.T @ D) + STEP * np.abs(want["dW"]) + tiny
+        tol = ah.T @ (4 * STEP * D + p) + (M + 4) * EPS * (ah.T @ D) + STEP * np.abs(want["dW"]) + tiny
         assert (np.abs(f64(o["dW"]) - want["dW"]) <= 1.01 * tol).all()
     return want
 
@@ -119,6 +121,18 @@ def test_logits_far_from_zero(P, shift):
     H[:, 0] = 4
     W[0] = shift / 4
     check(P.lmhead_xent(H, W, labels), H, W, labels, np.ones(200), 1.0)
+
+
+@pytest.mark.parametrize("layout", ["kv", "vk"])
+def test_what_all_columns_share_drops_out(P, layout):
+    """sum_j D_j = 0: a row of W that is the same in all columns gets no gradient through H but what fp32 leaves: the sums of V and of the row's
+    products, the rounded sum that divides them and the label's part, (2 V + 16) 2^-23 of sum |D| |w| in all."""
+    H, W, labels = make(200, 64, 3000, layout, seed=16)
+    H[:, 0] = 8
+    W[0] = -11.25
+    o = P.lmhead_xent(H, W, labels)
+    want = check(o, H, W, labels, np.ones(200), 1.0)
+    assert (np.abs(f64(o["dH"][:, 0])) <= 11.25 * np.abs(want["D"]).sum(1) * (2 * 3000 + 16) * EPS).all()
 
 
 def test_columns_of_different_sizes(P):
