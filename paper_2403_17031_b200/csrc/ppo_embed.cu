@@ -11,79 +11,22 @@
 // written once; a run that crosses chunks leaves a partial sum per chunk, and those are added in the order of the chunks.
 // Every sum is fp32 in ascending order of the positions, without atomics: results do not depend on timing. Rows of tokens
 // that do not occur are zero-filled by other blocks of the same launch.
-#include "ppo_common.cuh"
+#include "ppo_packs.cuh"
 
 namespace ppo {
 namespace embed {
 
 constexpr int kThreads = 256;
 
-// ---------------------------------------------------------------- loads and stores of VEC elements as fp32
-template <typename T, int VEC> struct Pack;
-template <> struct Pack<float, 1> {
-    float v[1];
-    __device__ __forceinline__ void load(const float *p) { v[0] = __ldg(p); }
-    __device__ __forceinline__ void load_last(const float *p) { v[0] = __ldcs(p); }
-    __device__ __forceinline__ static void store(float *p, const float *x) { __stcs(p, x[0]); }
-};
-template <> struct Pack<__nv_bfloat16, 1> {
-    float v[1];
-    __device__ __forceinline__ void load(const __nv_bfloat16 *p) { v[0] = __bfloat162float(*p); }
-    __device__ __forceinline__ void load_last(const __nv_bfloat16 *p) { v[0] = __bfloat162float(*p); }
-    __device__ __forceinline__ static void store(__nv_bfloat16 *p, const float *x) { *p = __float2bfloat16_rn(x[0]); }
-};
-template <> struct Pack<float, 8> {
-    float v[8];
-    __device__ __forceinline__ void set(const float4 &a, const float4 &b)
-    {
-        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-    }
-    __device__ __forceinline__ void load(const float *p)
-    {
-        set(__ldg(reinterpret_cast<const float4 *>(p)), __ldg(reinterpret_cast<const float4 *>(p) + 1));
-    }
-    __device__ __forceinline__ void load_last(const float *p)
-    {
-        set(__ldcs(reinterpret_cast<const float4 *>(p)), __ldcs(reinterpret_cast<const float4 *>(p) + 1));
-    }
-    __device__ __forceinline__ static void store(float *p, const float *x)
-    {
-        __stcs(reinterpret_cast<float4 *>(p), make_float4(x[0], x[1], x[2], x[3]));
-        __stcs(reinterpret_cast<float4 *>(p) + 1, make_float4(x[4], x[5], x[6], x[7]));
-    }
-};
-template <> struct Pack<__nv_bfloat16, 8> {
-    float v[8];
-    __device__ __forceinline__ void set(const uint4 &a)
-    {
-        const uint32_t w[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            v[2 * j] = __uint_as_float(w[j] << 16);
-            v[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
-        }
-    }
-    __device__ __forceinline__ void load(const __nv_bfloat16 *p) { set(__ldg(reinterpret_cast<const uint4 *>(p))); }
-    __device__ __forceinline__ void load_last(const __nv_bfloat16 *p) { set(__ldcs(reinterpret_cast<const uint4 *>(p))); }
-    __device__ __forceinline__ static void store(__nv_bfloat16 *p, const float *x)
-    {
-        uint32_t w[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const __nv_bfloat162 h = __floats2bfloat162_rn(x[2 * j], x[2 * j + 1]);
-            w[j] = *reinterpret_cast<const uint32_t *>(&h);
-        }
-        __stcs(reinterpret_cast<uint4 *>(p), make_uint4(w[0], w[1], w[2], w[3]));
-    }
-};
-
 // A thread's columns of a row: Q packs of VEC neighbours, packs `lanes` apart so that a warp's accesses are contiguous.
-// VEC 8 where all rows are 16-byte aligned, else single elements, four of them in flight.
-template <int VEC> __host__ __device__ constexpr int packs_per_thread() { return VEC == 8 ? 1 : 4; }
+// Rows at odd addresses are read element by element, four of them in flight.
+template <int VEC> __host__ __device__ constexpr int packs_per_thread() { return VEC == 1 ? 4 : 1; }
 
-static bool aligned_rows(const void *p, int64_t pitch, int dtype)
+static int widest(int64_t K, const void *a, int64_t lda, int ta, const void *b, int64_t ldb, int tb)
 {
-    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && pitch % (dtype == PPO_F32 ? 4 : 8) == 0;
+    for (int vec = 8; vec > 1; vec /= 2)
+        if (K % vec == 0 && packs_fit(a, lda, ta, vec) && packs_fit(b, ldb, tb, vec)) return vec;
+    return 1;
 }
 
 // ---------------------------------------------------------------- forward
@@ -131,212 +74,39 @@ lookup_kernel(const FwdArgs a)
     }
 }
 
-template <typename TI, typename TO>
-static int launch_lookup(const FwdArgs &a, bool vec, cudaStream_t s)
+template <typename TI, typename TO, int VEC>
+static void launch_lookup_vec(const FwdArgs &a, cudaStream_t s)
 {
     // four rows per block once they fill the SMs
-    const bool many = a.N >= 4 * 8 * 148;
-    const unsigned grid = (unsigned)(many ? (a.N + 3) / 4 : a.N);
-    if (vec && many) lookup_kernel<TI, TO, 8, 4><<<grid, kThreads, 0, s>>>(a);
-    else if (vec) lookup_kernel<TI, TO, 8, 1><<<grid, kThreads, 0, s>>>(a);
-    else if (many) lookup_kernel<TI, TO, 1, 4><<<grid, kThreads, 0, s>>>(a);
-    else lookup_kernel<TI, TO, 1, 1><<<grid, kThreads, 0, s>>>(a);
+    if (a.N >= 4 * 8 * 148) lookup_kernel<TI, TO, VEC, 4><<<(unsigned)((a.N + 3) / 4), kThreads, 0, s>>>(a);
+    else lookup_kernel<TI, TO, VEC, 1><<<(unsigned)a.N, kThreads, 0, s>>>(a);
+}
+
+template <typename TI, typename TO>
+static int launch_lookup(const FwdArgs &a, int vec, cudaStream_t s)
+{
+    if (vec == 8) launch_lookup_vec<TI, TO, 8>(a, s);
+    else if (vec == 4) launch_lookup_vec<TI, TO, 4>(a, s);
+    else launch_lookup_vec<TI, TO, 1>(a, s);
     return launch_status();
 }
 
-// ---------------------------------------------------------------- sorting the positions by token
-// Keys are token ids; a position that counts for no row (padding id, id outside [0, V)) has the key V and comes last.
-struct SortArgs {
-    const int32_t *tokens;
-    int64_t V;
-    int N, padding_id;
-    int32_t *key, *pos;            // sorted
-    uint8_t *present;              // [V], cleared before; nullable
-    int *status;
-};
-
-__device__ __forceinline__ int key_of(const SortArgs &a, int i)
-{
-    const int t = a.tokens[i];
-    return t < 0 || t >= a.V || t == a.padding_id ? (int)a.V : t;
-}
-
-__device__ __forceinline__ void note_token(const SortArgs &a, int i, int key)
-{
-    if (key < a.V) {
-        if (a.present) a.present[key] = 1;
-    } else if (a.status) {
-        const int t = a.tokens[i];
-        if (t < 0 || t >= a.V) atomicOr(a.status, PPO_DEV_BAD_TOKEN);
-    }
-}
-
-// Few positions: each one's place is the number of positions before it, counted. A warp counts for four positions.
-constexpr int kRankPer = 4, kRankMax = 8192;
-__global__ void __launch_bounds__(kThreads)
-rank_kernel(const SortArgs a)
-{
-    const int lane = threadIdx.x & 31;
-    const int i0 = (blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5)) * kRankPer;
-    if (i0 >= a.N) return;
-    int key[kRankPer], n[kRankPer];
-#pragma unroll
-    for (int r = 0; r < kRankPer; ++r) {
-        key[r] = i0 + r < a.N ? key_of(a, i0 + r) : 0;
-        n[r] = 0;
-    }
-#pragma unroll 4
-    for (int j = lane; j < a.N; j += 32) {
-        const int k = key_of(a, j);
-#pragma unroll
-        for (int r = 0; r < kRankPer; ++r) n[r] += k < key[r] || (k == key[r] && j < i0 + r);
-    }
-#pragma unroll
-    for (int r = 0; r < kRankPer; ++r) {
-        n[r] = __reduce_add_sync(0xffffffffu, n[r]);
-        if (lane == r && i0 + r < a.N) {
-            a.key[n[r]] = key[r];
-            a.pos[n[r]] = i0 + r;
-            note_token(a, i0 + r, key[r]);
-        }
-    }
-}
-
-// Many positions: least significant digit first, 8 bits a pass, each pass stable: digits counted per tile, the counts
-// summed in digit order, the tile's entries moved. A warp owns 512 neighbouring entries of a tile.
-constexpr int kTile = 4096, kDigits = 256, kWarps = kThreads / 32, kPerWarp = kTile / kWarps;
-
-struct PassArgs {
-    SortArgs s;
-    const int32_t *key_in, *pos_in;      // null in the first pass
-    int32_t *key_out, *pos_out;
-    int32_t *counts;                     // [kDigits][tiles]
-    int tiles, shift, last;
-};
-
-__device__ __forceinline__ void load_entry(const PassArgs &a, int i, int &key, int &pos)
-{
-    key = a.key_in ? a.key_in[i] : key_of(a.s, i);
-    pos = a.pos_in ? a.pos_in[i] : i;
-}
-
-__global__ void __launch_bounds__(kThreads)
-count_kernel(const PassArgs a)
-{
-    __shared__ int n[kDigits];
-    n[threadIdx.x] = 0;
-    __syncthreads();
-    const int i0 = blockIdx.x * kTile;
-#pragma unroll 4
-    for (int j = threadIdx.x; j < kTile; j += kThreads) {
-        if (i0 + j < a.s.N) {
-            int key, pos;
-            load_entry(a, i0 + j, key, pos);
-            atomicAdd(&n[(key >> a.shift) & (kDigits - 1)], 1);
-        }
-    }
-    __syncthreads();
-    a.counts[(size_t)threadIdx.x * a.tiles + blockIdx.x] = n[threadIdx.x];
-}
-
-// exclusive sum over `n` counts, in place; one block
-constexpr int kScanThreads = 1024;
-__global__ void __launch_bounds__(kScanThreads)
-scan_kernel(int32_t *__restrict__ counts, int n)
-{
-    __shared__ int warp_sum[32];
-    __shared__ int carry;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    if (threadIdx.x == 0) carry = 0;
-    __syncthreads();
-    for (int base = 0; base < n; base += kScanThreads * 8) {
-        const int i = base + threadIdx.x * 8;
-        int v[8], sum = 0;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            v[e] = i + e < n ? counts[i + e] : 0;
-            sum += v[e];
-        }
-        int incl = sum;
-#pragma unroll
-        for (int off = 1; off < 32; off <<= 1) {
-            const int o = __shfl_up_sync(0xffffffffu, incl, off);
-            if (lane >= off) incl += o;
-        }
-        if (lane == 31) warp_sum[warp] = incl;
-        __syncthreads();
-        int before = carry;
-        for (int w = 0; w < warp; ++w) before += warp_sum[w];
-        int run = before + incl - sum;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            if (i + e < n) counts[i + e] = run;
-            run += v[e];
-        }
-        __syncthreads();
-        if (threadIdx.x == kScanThreads - 1) carry = run;
-        __syncthreads();
-    }
-}
-
-__global__ void __launch_bounds__(kThreads)
-scatter_kernel(const PassArgs a)
-{
-    __shared__ int at[kWarps][kDigits];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    for (int j = threadIdx.x; j < kWarps * kDigits; j += kThreads) (&at[0][0])[j] = 0;
-    __syncthreads();
-    const int i0 = blockIdx.x * kTile + warp * kPerWarp;
-    for (int j = lane; j < kPerWarp; j += 32) {
-        if (i0 + j < a.s.N) {
-            int key, pos;
-            load_entry(a, i0 + j, key, pos);
-            atomicAdd(&at[warp][(key >> a.shift) & (kDigits - 1)], 1);
-        }
-    }
-    __syncthreads();
-    {   // the warps' first places of each digit
-        int run = a.counts[(size_t)threadIdx.x * a.tiles + blockIdx.x];
-#pragma unroll
-        for (int w = 0; w < kWarps; ++w) {
-            const int n = at[w][threadIdx.x];
-            at[w][threadIdx.x] = run;
-            run += n;
-        }
-    }
-    __syncthreads();
-    for (int j = lane; j < kPerWarp; j += 32) {
-        const bool in = i0 + j < a.s.N;
-        int key = 0, pos = 0;
-        if (in) load_entry(a, i0 + j, key, pos);
-        const int digit = in ? (key >> a.shift) & (kDigits - 1) : kDigits;
-        const unsigned same = __match_any_sync(0xffffffffu, digit);
-        const int before = __popc(same & ((1u << lane) - 1));
-        int to = 0;
-        if (in) to = at[warp][digit] + before;
-        __syncwarp();
-        if (in && before == 0) at[warp][digit] += __popc(same);
-        __syncwarp();
-        if (in) {
-            a.key_out[to] = key;
-            a.pos_out[to] = pos;
-            if (a.last) note_token(a.s, pos, key);
-        }
-    }
-}
-
-// ---------------------------------------------------------------- sums
+// ---------------------------------------------------------------- the rows of the gradient
 struct BwdArgs {
     const void *dY;
-    const int32_t *key, *pos;       // sorted
-    const uint8_t *present;
+    const int32_t *tokens;
+    const int32_t *key, *pos;       // sorted by token
+    uint8_t *present;               // [V] the token occurs
     void *dE;
     float *part;                    // [chunks][2][K]: a run that comes from the chunk before; one that goes on in the next
     int64_t V, ldy, lde;
-    int N, K, chunk, chunks, accumulate;
+    int N, K, chunk, chunks, accumulate, padding_id;
     float scale;
     int lanes, groups, slabs;       // threads per chunk and slab, chunks per block (lanes * groups = kThreads)
-    int chunk_blocks, fill_rows;    // blocks that sum; rows per block of the others
+    int fill_rows;                  // rows per block that zero-fills
+    int64_t fill0;                  // first row of this launch's
+    int work_blocks;                // blocks before those
+    int *status;
 };
 
 template <typename TO, int VEC>
@@ -347,29 +117,310 @@ __device__ __forceinline__ void write_row(const BwdArgs &a, int64_t v, int k, fl
     for (int e = 0; e < VEC; ++e) x[e] *= a.scale;
     if (a.accumulate) {
         Pack<TO, VEC> old;
-        old.load_last(to);
+        old.load_once(to);
 #pragma unroll
         for (int e = 0; e < VEC; ++e) x[e] += old.v[e];
     }
     Pack<TO, VEC>::store(to, x);
 }
 
+// The zero rows are most of what few positions write, so they go along with the launches that sort, which leave nearly all of
+// the memory's time unused.
+template <typename TO, int VEC>
+__device__ __forceinline__ void fill_rows(const BwdArgs &a, int block)
+{
+    float zero[VEC];
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) zero[e] = 0.f;
+    const int64_t v0 = a.fill0 + (int64_t)block * a.fill_rows;
+    for (int64_t v = v0; v < v0 + a.fill_rows && v < a.V; ++v) {
+        if (a.present[v]) continue;
+        TO *to = reinterpret_cast<TO *>(a.dE) + v * a.lde;
+        for (int k = threadIdx.x * VEC; k < a.K; k += blockDim.x * VEC) Pack<TO, VEC>::store(to + k, zero);
+    }
+}
+
+__device__ __forceinline__ int key_of(const BwdArgs &a, int t) { return t < 0 || t >= a.V || t == a.padding_id ? (int)a.V : t; }
+
+// ---------------------------------------------------------------- a handful of positions: one launch, no sorting
+// A block owns a few rows. It looks all tokens through for them, in order, and writes its rows: sums or zeros.
+constexpr int kDirectMax = 256, kDirectRows = 16;
+template <typename TI, typename TO, int VEC>
+__global__ void __launch_bounds__(kThreads)
+direct_kernel(const BwdArgs a)
+{
+    __shared__ int row[kDirectMax], pos[kDirectMax], warp_n[kThreads / 32];
+    const int64_t v0 = (int64_t)blockIdx.x * kDirectRows;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int t = -1;
+    if ((int)threadIdx.x < a.N) {
+        const int raw = a.tokens[threadIdx.x];
+        if (blockIdx.x == 0 && a.status && (raw < 0 || raw >= a.V)) atomicOr(a.status, PPO_DEV_BAD_TOKEN);
+        const int64_t off = key_of(a, raw) - v0;
+        if (key_of(a, raw) < a.V && off >= 0 && off < kDirectRows) t = (int)off;
+    }
+    const unsigned mine = __ballot_sync(0xffffffffu, t >= 0);
+    if (lane == 0) warp_n[warp] = __popc(mine);
+    __syncthreads();
+    int at = __popc(mine & ((1u << lane) - 1)), n = 0;
+#pragma unroll
+    for (int w = 0; w < kThreads / 32; ++w) {
+        if (w < warp) at += warp_n[w];
+        n += warp_n[w];
+    }
+    if (t >= 0) {
+        row[at] = t;
+        pos[at] = threadIdx.x;
+    }
+    __syncthreads();
+    const TI *dY = reinterpret_cast<const TI *>(a.dY);
+    const int rows = (int)min((int64_t)kDirectRows, a.V - v0);
+    unsigned occur = 0;
+    for (int i = 0; i < n; ++i) occur |= 1u << row[i];
+    // zero rows, then the others
+    if (!a.accumulate && occur != (1u << rows) - 1) {
+        float zero[VEC];
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) zero[e] = 0.f;
+#pragma unroll 4
+        for (int r = 0; r < rows; ++r) {
+            if (occur >> r & 1) continue;
+            TO *to = reinterpret_cast<TO *>(a.dE) + (v0 + r) * a.lde;
+            for (int k = threadIdx.x * VEC; k < a.K; k += kThreads * VEC) Pack<TO, VEC>::store(to + k, zero);
+        }
+    }
+    for (; occur; occur &= occur - 1) {
+        const int r = __ffs(occur) - 1;
+        for (int k = threadIdx.x * VEC; k < a.K; k += kThreads * VEC) {
+            float acc[VEC];
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) acc[e] = 0.f;
+            for (int i = 0; i < n;) {
+                constexpr int U = 8;                            // rows in flight
+                Pack<TI, VEC> p[U];
+                int got = 0;
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    while (i < n && row[i] != r) ++i;
+                    if (i < n) {
+                        p[u].load(dY + (int64_t)pos[i++] * a.ldy + k);
+                        got = u + 1;
+                    }
+                }
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+                    if (u < got)
+#pragma unroll
+                        for (int e = 0; e < VEC; ++e) acc[e] += p[u].v[e];
+            }
+            write_row<TO, VEC>(a, v0 + r, k, acc);
+        }
+    }
+}
+
+// ---------------------------------------------------------------- sorting the positions by token
+// Keys are token ids; a position that counts for no row (padding id, id outside [0, V)) has the key V and comes last.
+__device__ __forceinline__ void note_token(const BwdArgs &a, int t, int key)
+{
+    if (key < a.V) {
+        if (!a.accumulate) a.present[key] = 1;
+    } else if (a.status && (t < 0 || t >= a.V)) {
+        atomicOr(a.status, PPO_DEV_BAD_TOKEN);
+    }
+}
+
+// Up to 8192 positions of up to 2^19 tokens: each one's place is the number of (key, position) pairs below its own, counted.
+// A warp counts for four positions. (8192 positions: 67 M comparisons, 5 us; the passes below take 35.)
+constexpr int kRankPer = 4, kRankMax = 8192, kRankBits = 13, kRankWarps = kThreads / 32;
+constexpr int64_t kRankVocabulary = (int64_t)1 << (32 - kRankBits);
+__global__ void __launch_bounds__(kThreads)
+rank_kernel(const BwdArgs a, int32_t *__restrict__ key_out, int32_t *__restrict__ pos_out)
+{
+    __shared__ uint32_t pair[kRankMax];
+    for (int j = threadIdx.x; j < a.N; j += kThreads) pair[j] = (uint32_t)key_of(a, a.tokens[j]) << kRankBits | (uint32_t)j;
+    __syncthreads();
+    const int lane = threadIdx.x & 31;
+    const int i0 = (blockIdx.x * kRankWarps + (threadIdx.x >> 5)) * kRankPer;
+    uint32_t mine[kRankPer];
+    int n[kRankPer];
+#pragma unroll
+    for (int r = 0; r < kRankPer; ++r) {
+        mine[r] = i0 + r < a.N ? pair[i0 + r] : 0;
+        n[r] = 0;
+    }
+#pragma unroll 8
+    for (int j = lane; j < a.N; j += 32) {
+        const uint32_t p = pair[j];
+#pragma unroll
+        for (int r = 0; r < kRankPer; ++r) n[r] += p < mine[r];
+    }
+#pragma unroll
+    for (int r = 0; r < kRankPer; ++r) {
+        n[r] = __reduce_add_sync(0xffffffffu, n[r]);
+        if (lane == r && i0 + r < a.N) {
+            const int key = (int)(mine[r] >> kRankBits);
+            key_out[n[r]] = key;
+            pos_out[n[r]] = i0 + r;
+            note_token(a, a.tokens[i0 + r], key);
+        }
+    }
+}
+
+// More: least significant digit first, 8 bits a pass, each pass stable: digits counted per tile, the counts summed in digit
+// order, the tile's entries moved. A warp owns neighbouring entries of a tile. A pass that moves an entry counts it for the
+// next one, whose tile it knows, so that only the first pass has a launch for counting.
+constexpr int kTile = 2048, kDigits = 256, kWarps = kThreads / 32, kPerWarp = kTile / kWarps;
+
+struct PassArgs {
+    const int32_t *key_in, *pos_in;      // null in the first pass
+    int32_t *key_out, *pos_out;
+    int32_t *counts, *next_counts;       // [kDigits][tiles]; next_counts null in the last pass
+    int tiles, shift;
+};
+
+__device__ __forceinline__ void load_entry(const BwdArgs &a, const PassArgs &p, int i, int &key, int &pos)
+{
+    key = p.key_in ? p.key_in[i] : key_of(a, a.tokens[i]);
+    pos = p.pos_in ? p.pos_in[i] : i;
+}
+
+__global__ void __launch_bounds__(kThreads)
+count_kernel(const BwdArgs a, const PassArgs p)
+{
+    __shared__ int n[kDigits];
+    n[threadIdx.x] = 0;
+    __syncthreads();
+    const int i0 = blockIdx.x * kTile;
+#pragma unroll
+    for (int j = 0; j < kTile; j += kThreads) {
+        const int i = i0 + j + threadIdx.x;
+        int digit = kDigits;
+        if (i < a.N) {
+            const int t = a.tokens[i], key = key_of(a, t);
+            digit = key & (kDigits - 1);
+            note_token(a, t, key);
+        }
+        // (frequent tokens: one addition for the warp's equal digits)
+        const unsigned same = __match_any_sync(0xffffffffu, digit);
+        if (digit < kDigits && (same & ((1u << (threadIdx.x & 31)) - 1)) == 0) atomicAdd(&n[digit], __popc(same));
+    }
+    __syncthreads();
+    p.counts[(size_t)threadIdx.x * p.tiles + blockIdx.x] = n[threadIdx.x];
+}
+
+// exclusive sum over the counts, in place; one block
+constexpr int kScanThreads = 1024;
+template <typename TO, int VEC>
+__global__ void __launch_bounds__(kScanThreads)
+scan_kernel(const BwdArgs a, const PassArgs p)
+{
+    if (blockIdx.x > 0) {
+        fill_rows<TO, VEC>(a, blockIdx.x - 1);
+        return;
+    }
+    __shared__ int warp_sum[32];
+    __shared__ int carry;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n = p.tiles * kDigits;
+    int4 *counts = reinterpret_cast<int4 *>(p.counts);          // (kDigits counts a tile: a multiple of 8)
+    if (threadIdx.x == 0) carry = 0;
+    __syncthreads();
+    for (int base = 0; base < n; base += kScanThreads * 8) {
+        const int i = base + threadIdx.x * 8;
+        int v[8] = {0, 0, 0, 0, 0, 0, 0, 0}, sum = 0;
+        if (i < n) {
+            const int4 x = counts[i / 4], y = counts[i / 4 + 1];
+            v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w; v[4] = y.x; v[5] = y.y; v[6] = y.z; v[7] = y.w;
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int x = v[e];
+            v[e] = sum;
+            sum += x;
+        }
+        int incl = sum;
+#pragma unroll
+        for (int off = 1; off < 32; off <<= 1) {
+            const int o = __shfl_up_sync(0xffffffffu, incl, off);
+            if (lane >= off) incl += o;
+        }
+        if (lane == 31) warp_sum[warp] = incl;
+        __syncthreads();
+        const int w = warp_sum[lane];
+        const int before = carry + __reduce_add_sync(0xffffffffu, lane < warp ? w : 0) + incl - sum;
+        if (i < n) {
+            counts[i / 4] = make_int4(before + v[0], before + v[1], before + v[2], before + v[3]);
+            counts[i / 4 + 1] = make_int4(before + v[4], before + v[5], before + v[6], before + v[7]);
+        }
+        __syncthreads();
+        if (threadIdx.x == kScanThreads - 1) carry = before + sum;
+        __syncthreads();
+    }
+}
+
+template <typename TO, int VEC>
+__global__ void __launch_bounds__(kThreads)
+scatter_kernel(const BwdArgs a, const PassArgs p)
+{
+    if ((int)blockIdx.x >= a.work_blocks) {
+        fill_rows<TO, VEC>(a, blockIdx.x - a.work_blocks);
+        return;
+    }
+    __shared__ int at[kWarps][kDigits];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    for (int j = threadIdx.x; j < kWarps * kDigits; j += kThreads) (&at[0][0])[j] = 0;
+    const int i0 = blockIdx.x * kTile + warp * kPerWarp;
+    constexpr int R = kPerWarp / 32;
+    int key[R], pos[R], before[R];
+    unsigned same[R];
+#pragma unroll
+    for (int j = 0; j < R; ++j) {
+        const int i = i0 + j * 32 + lane;
+        key[j] = -1;
+        if (i < a.N) load_entry(a, p, i, key[j], pos[j]);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < R; ++j) {
+        const int digit = key[j] >= 0 ? (key[j] >> p.shift) & (kDigits - 1) : kDigits;
+        same[j] = __match_any_sync(0xffffffffu, digit);
+        before[j] = __popc(same[j] & ((1u << lane) - 1));
+        if (key[j] >= 0 && before[j] == 0) atomicAdd(&at[warp][digit], __popc(same[j]));
+    }
+    __syncthreads();
+    {   // the warps' first places of each digit
+        int run = p.counts[(size_t)threadIdx.x * p.tiles + blockIdx.x];
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) {
+            const int n = at[w][threadIdx.x];
+            at[w][threadIdx.x] = run;
+            run += n;
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < R; ++j) {
+        const int digit = (key[j] >> p.shift) & (kDigits - 1);
+        int to = 0;
+        if (key[j] >= 0) to = at[warp][digit] + before[j];
+        __syncwarp();
+        if (key[j] >= 0 && before[j] == 0) at[warp][digit] += __popc(same[j]);
+        __syncwarp();
+        if (key[j] >= 0) {
+            p.key_out[to] = key[j];
+            p.pos_out[to] = pos[j];
+            if (p.next_counts) atomicAdd(&p.next_counts[(size_t)((key[j] >> (p.shift + 8)) & (kDigits - 1)) * p.tiles + to / kTile], 1);
+        }
+    }
+}
+
+// ---------------------------------------------------------------- sums
 template <typename TI, typename TO, int VEC>
 __global__ void __launch_bounds__(kThreads)
 sum_kernel(const BwdArgs a)
 {
     constexpr int Q = packs_per_thread<VEC>(), U = 8 / Q;      // rows in flight
-    if ((int)blockIdx.x >= a.chunk_blocks) {
-        // zero rows
-        const int64_t v0 = (int64_t)(blockIdx.x - a.chunk_blocks) * a.fill_rows;
-        float zero[VEC];
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) zero[e] = 0.f;
-        for (int64_t v = v0; v < v0 + a.fill_rows && v < a.V; ++v) {
-            if (a.present[v]) continue;
-            TO *to = reinterpret_cast<TO *>(a.dE) + v * a.lde;
-            for (int k = threadIdx.x * VEC; k < a.K; k += kThreads * VEC) Pack<TO, VEC>::store(to + k, zero);
-        }
+    if ((int)blockIdx.x >= a.work_blocks) {
+        fill_rows<TO, VEC>(a, blockIdx.x - a.work_blocks);
         return;
     }
     const int lane = threadIdx.x % a.lanes, group = threadIdx.x / a.lanes;
@@ -398,8 +449,7 @@ sum_kernel(const BwdArgs a)
             if (!in[q]) continue;
             if (from_before || goes_on) {
                 float *to = a.part + ((size_t)c * 2 + (from_before ? 0 : 1)) * a.K + k[q];
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) to[e] = acc[q][e];
+                Pack<float, VEC>::store(to, acc[q]);
             } else {
                 write_row<TO, VEC>(a, cur, k[q], acc[q]);
             }
@@ -415,7 +465,7 @@ sum_kernel(const BwdArgs a)
             const TI *row = dY + (real ? (int64_t)a.pos[e + u] : 0) * a.ldy;
 #pragma unroll
             for (int q = 0; q < Q; ++q) {
-                if (real && in[q]) p[u][q].load_last(row + k[q]);
+                if (real && in[q]) p[u][q].load_once(row + k[q]);
                 else
 #pragma unroll
                     for (int x = 0; x < VEC; ++x) p[u][q].v[x] = 0.f;
@@ -442,47 +492,54 @@ sum_kernel(const BwdArgs a)
 }
 
 // The runs that cross chunks: the block of the chunk in which such a run begins adds the partial sums up.
-template <typename TO>
+template <typename TO, int VEC>
 __global__ void __launch_bounds__(kThreads)
 join_kernel(const BwdArgs a)
 {
-    const int c = blockIdx.x / a.slabs, k0 = (blockIdx.x % a.slabs) * kThreads + threadIdx.x;
+    const int c = blockIdx.x / a.slabs, k = ((blockIdx.x % a.slabs) * kThreads + threadIdx.x) * VEC;
     const int e0 = c * a.chunk, e1 = e0 + a.chunk;              // (the last chunk has no block)
-    const int t = a.key[e1 - 1];
-    if (t >= a.V || a.key[e1] != t) return;                     // no run goes on
-    if (e0 > 0 && a.key[e0 - 1] == t) return;                   // it began in an earlier chunk
+    const int t = a.key[e1 - 1], next = a.key[e1], before = e0 > 0 ? a.key[e0 - 1] : -1;
+    if (t >= a.V || next != t) return;                          // no run goes on
+    if (before == t) return;                                    // it began in an earlier chunk
     int lo = c + 1, hi = a.chunks - 1;                          // last chunk that begins with t
     while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
         if (a.key[(size_t)mid * a.chunk] == t) lo = mid;
         else hi = mid - 1;
     }
-    if (k0 >= a.K) return;
-    float sum = a.part[((size_t)c * 2 + 1) * a.K + k0];
+    if (k >= a.K) return;
+    Pack<float, VEC> sum;
+    sum.load(a.part + ((size_t)c * 2 + 1) * a.K + k);
 #pragma unroll 8
-    for (int i = c + 1; i <= lo; ++i) sum += a.part[(size_t)i * 2 * a.K + k0];
-    write_row<TO, 1>(a, t, k0, &sum);
+    for (int i = c + 1; i <= lo; ++i) {
+        Pack<float, VEC> x;
+        x.load(a.part + (size_t)i * 2 * a.K + k);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) sum.v[e] += x.v[e];
+    }
+    write_row<TO, VEC>(a, t, k, sum.v);
 }
 
 // ---------------------------------------------------------------- host side
 struct Plan {
-    int chunk, chunks, lanes, groups, slabs, tiles, passes;
-    size_t key, pos, key2, pos2, counts, present, part, bytes;
+    int chunk, chunks, tiles, passes;
+    bool direct;
+    size_t key, pos, key2, pos2, counts, first_zero, present, zero_bytes, part, bytes;
 };
 
-static Plan plan_of(int64_t N, int64_t K, int64_t V, bool vec)
+// (the same for every alignment: the caller asks for the scratch before it has the tensors)
+static Plan plan_of(int64_t N, int64_t K, int64_t V)
 {
-    Plan p;
-    const int64_t packs = vec ? (K + 7) / 8 : (K + 3) / 4;      // threads for a row
-    p.lanes = 8;
-    while (p.lanes < kThreads && p.lanes < packs) p.lanes *= 2;
-    p.groups = kThreads / p.lanes;
-    p.slabs = (int)((packs + p.lanes - 1) / p.lanes);
+    Plan p = {};
+    p.direct = N <= kDirectMax;
+    if (p.direct) {
+        p.bytes = 256;
+        return p;
+    }
     p.chunk = N > 65536 ? 128 : 32;
     p.chunks = (int)((N + p.chunk - 1) / p.chunk);
-    p.tiles = N <= kRankMax ? 0 : (int)((N + kTile - 1) / kTile);
-    p.passes = 0;
-    if (p.tiles) {
+    if (N > kRankMax || V >= kRankVocabulary) {
+        p.tiles = (int)((N + kTile - 1) / kTile);
         int bits = 1;
         while (bits < 32 && (V >> bits)) ++bits;
         p.passes = (bits + 7) / 8;
@@ -493,64 +550,108 @@ static Plan plan_of(int64_t N, int64_t K, int64_t V, bool vec)
         at += align256(n);
         return here;
     };
-    p.key = take((size_t)N * 4);
-    p.pos = take((size_t)N * 4);
-    p.key2 = take(p.tiles ? (size_t)N * 4 : 0);
-    p.pos2 = take(p.tiles ? (size_t)N * 4 : 0);
-    p.counts = take((size_t)p.tiles * kDigits * 4);
+    const size_t ints = (size_t)N * 4, counts = (size_t)p.tiles * kDigits * 4;
+    p.key = take(ints);
+    p.pos = take(ints);
+    p.key2 = take(p.tiles ? ints : 0);
+    p.pos2 = take(p.tiles ? ints : 0);
+    p.counts = take(counts * p.passes);
     p.present = take((size_t)V);
+    // cleared first: the counts of the passes behind the first, and `present`
+    p.first_zero = p.passes > 1 ? p.counts + counts : p.present;
+    p.zero_bytes = at - p.first_zero;
     p.part = take((size_t)p.chunks * 2 * (size_t)K * 4);
     p.bytes = at;
     return p;
 }
 
-static int launch_sort(const SortArgs &sa, const Plan &p, unsigned char *scratch, cudaStream_t s)
+// Zero rows are handed out to the launches: `parts` of them, in equal shares, the last one what is left.
+struct Fill {
+    int64_t next, blocks, share;
+    int rows;
+    void init(const BwdArgs &a, int parts)
+    {
+        rows = a.fill_rows;
+        next = 0;
+        blocks = a.accumulate ? 0 : (a.V + rows - 1) / rows;
+        share = blocks / parts;
+    }
+    unsigned take(BwdArgs &a, bool all)
+    {
+        const int64_t n = all ? blocks - next : share;
+        a.fill0 = next * rows;
+        next += n;
+        return (unsigned)n;
+    }
+};
+
+template <typename TI, typename TO, int VEC>
+static int launch_bwd(BwdArgs a, const Plan &p, unsigned char *mem, cudaStream_t s)
 {
-    if (!p.tiles) {
-        const int per_block = kThreads / 32 * kRankPer;
-        rank_kernel<<<(sa.N + per_block - 1) / per_block, kThreads, 0, s>>>(sa);
+    if (p.direct) {
+        direct_kernel<TI, TO, VEC><<<(unsigned)((a.V + kDirectRows - 1) / kDirectRows), kThreads, 0, s>>>(a);
         return launch_status();
     }
-    PassArgs a = {};
-    a.s = sa;
-    a.tiles = p.tiles;
-    a.counts = reinterpret_cast<int32_t *>(scratch + p.counts);
-    int32_t *key[2] = {sa.key, reinterpret_cast<int32_t *>(scratch + p.key2)};
-    int32_t *pos[2] = {sa.pos, reinterpret_cast<int32_t *>(scratch + p.pos2)};
-    int to = (p.passes & 1) ^ 1;                                // the last pass writes the first pair
-    for (int pass = 0; pass < p.passes; ++pass, to ^= 1) {
-        a.key_out = key[to];
-        a.pos_out = pos[to];
-        a.shift = pass * 8;
-        a.last = pass == p.passes - 1;
-        count_kernel<<<p.tiles, kThreads, 0, s>>>(a);
-        int rc = launch_status();
-        if (rc) return rc;
-        scan_kernel<<<1, kScanThreads, 0, s>>>(a.counts, p.tiles * kDigits);
-        rc = launch_status();
-        if (rc) return rc;
-        scatter_kernel<<<p.tiles, kThreads, 0, s>>>(a);
-        rc = launch_status();
-        if (rc) return rc;
-        a.key_in = a.key_out;
-        a.pos_in = a.pos_out;
+    int rc;
+    Fill fill;
+    int32_t *key[2] = {reinterpret_cast<int32_t *>(mem + p.key), reinterpret_cast<int32_t *>(mem + p.key2)};
+    int32_t *pos[2] = {reinterpret_cast<int32_t *>(mem + p.pos), reinterpret_cast<int32_t *>(mem + p.pos2)};
+    a.key = key[0];
+    a.pos = pos[0];
+    if (!a.accumulate || p.passes > 1) PPO_RETURN_IF_CUDA(cudaMemsetAsync(mem + p.first_zero, 0, p.zero_bytes, s));
+    if (!p.tiles) {
+        fill.init(a, 1);
+        const int per_block = kRankWarps * kRankPer;
+        rank_kernel<<<(a.N + per_block - 1) / per_block, kThreads, 0, s>>>(a, key[0], pos[0]);
+        if ((rc = launch_status())) return rc;
+    } else {
+        fill.init(a, 2 * p.passes + 2);
+        PassArgs ps = {};
+        ps.tiles = p.tiles;
+        int to = (p.passes & 1) ^ 1;                            // the last pass writes the first pair
+        for (int pass = 0; pass < p.passes; ++pass, to ^= 1) {
+            ps.counts = reinterpret_cast<int32_t *>(mem + p.counts) + (size_t)pass * p.tiles * kDigits;
+            ps.next_counts = pass + 1 < p.passes ? ps.counts + (size_t)p.tiles * kDigits : nullptr;
+            ps.key_out = key[to];
+            ps.pos_out = pos[to];
+            ps.shift = pass * 8;
+            if (pass == 0) {
+                count_kernel<<<p.tiles, kThreads, 0, s>>>(a, ps);
+                if ((rc = launch_status())) return rc;
+            }
+            unsigned extra = fill.take(a, false);
+            scan_kernel<TO, VEC><<<1 + extra, kScanThreads, 0, s>>>(a, ps);
+            if ((rc = launch_status())) return rc;
+            extra = fill.take(a, false);
+            a.work_blocks = p.tiles;
+            scatter_kernel<TO, VEC><<<p.tiles + extra, kThreads, 0, s>>>(a, ps);
+            if ((rc = launch_status())) return rc;
+            ps.key_in = ps.key_out;
+            ps.pos_in = ps.pos_out;
+        }
     }
-    return PPO_OK;
+    const int64_t packs = (a.K + VEC * packs_per_thread<VEC>() - 1) / (VEC * packs_per_thread<VEC>());   // threads for a row
+    a.lanes = 8;
+    while (a.lanes < kThreads && a.lanes < packs) a.lanes *= 2;
+    a.groups = kThreads / a.lanes;
+    a.slabs = (int)((packs + a.lanes - 1) / a.lanes);
+    const int64_t blocks = (int64_t)((p.chunks + a.groups - 1) / a.groups) * a.slabs;
+    const int join_slabs = (int)((a.K + kThreads * VEC - 1) / (kThreads * VEC));
+    if (blocks + a.V / a.fill_rows + 1 >= ((int64_t)1 << 31) || (int64_t)p.chunks * join_slabs >= ((int64_t)1 << 31)) return PPO_ERR_SHAPE;
+    a.work_blocks = (int)blocks;
+    const unsigned extra = fill.take(a, true);
+    sum_kernel<TI, TO, VEC><<<(unsigned)blocks + extra, kThreads, 0, s>>>(a);
+    rc = launch_status();
+    if (rc || p.chunks < 2) return rc;
+    a.slabs = join_slabs;
+    join_kernel<TO, VEC><<<(unsigned)((p.chunks - 1) * join_slabs), kThreads, 0, s>>>(a);
+    return launch_status();
 }
 
 template <typename TI, typename TO>
-static int launch_sums(const BwdArgs &a, bool vec, cudaStream_t s)
+static int launch_bwd_types(const BwdArgs &a, const Plan &p, int vec, unsigned char *mem, cudaStream_t s)
 {
-    const int64_t fill = a.accumulate ? 0 : (a.V + a.fill_rows - 1) / a.fill_rows;
-    const unsigned grid = (unsigned)(a.chunk_blocks + fill);
-    if (vec) sum_kernel<TI, TO, 8><<<grid, kThreads, 0, s>>>(a);
-    else sum_kernel<TI, TO, 1><<<grid, kThreads, 0, s>>>(a);
-    int rc = launch_status();
-    if (rc || a.chunks < 2) return rc;
-    BwdArgs j = a;
-    j.slabs = (a.K + kThreads - 1) / kThreads;
-    join_kernel<TO><<<(unsigned)((a.chunks - 1) * j.slabs), kThreads, 0, s>>>(j);
-    return launch_status();
+    return vec == 8 ? launch_bwd<TI, TO, 8>(a, p, mem, s) : vec == 4 ? launch_bwd<TI, TO, 4>(a, p, mem, s) : launch_bwd<TI, TO, 1>(a, p, mem, s);
 }
 
 static bool dtype_ok(int d) { return d == PPO_F32 || d == PPO_BF16; }
@@ -579,7 +680,7 @@ extern "C" int ppo_embed(const void *table, int dtype, int64_t V, int64_t K, int
     a.N = N; a.V = V; a.K = (int)K; a.lde = lde; a.ldo = ldo; a.scale = scale;
     a.status = workspace ? &ws_header(workspace)->status : nullptr;
     cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-    const bool vec = K % 8 == 0 && aligned_rows(table, lde, dtype) && aligned_rows(out, ldo, out_dtype);
+    const int vec = widest(K, table, lde, dtype, out, ldo, out_dtype);
     if (dtype == PPO_F32)
         return out_dtype == PPO_F32 ? launch_lookup<float, float>(a, vec, s) : launch_lookup<float, __nv_bfloat16>(a, vec, s);
     return out_dtype == PPO_F32 ? launch_lookup<__nv_bfloat16, float>(a, vec, s) : launch_lookup<__nv_bfloat16, __nv_bfloat16>(a, vec, s);
@@ -589,7 +690,7 @@ extern "C" size_t ppo_embed_bwd_scratch_bytes(int64_t N, int64_t K, int64_t V)
 {
     using namespace embed;
     if (N <= 0 || K <= 0 || V <= 0 || N >= kLimit || K >= kLimit || V >= kLimit) return 0;
-    return plan_of(N, K, V, false).bytes;
+    return plan_of(N, K, V).bytes;
 }
 
 extern "C" int ppo_embed_bwd(const void *dY, int dtype, int64_t N, int64_t K, int64_t ldy, const int32_t *tokens, int64_t V,
@@ -611,30 +712,20 @@ extern "C" int ppo_embed_bwd(const void *dY, int dtype, int64_t N, int64_t K, in
         PPO_RETURN_IF_CUDA(cudaMemset2DAsync(dE, (size_t)lde * size_of(out_dtype), 0, (size_t)K * size_of(out_dtype), (size_t)V, s));
         return PPO_OK;
     }
-    const bool vec = K % 8 == 0 && aligned_rows(dY, ldy, dtype) && aligned_rows(dE, lde, out_dtype);
-    const Plan p = plan_of(N, K, V, vec);
+    const int vec = widest(K, dY, ldy, dtype, dE, lde, out_dtype);
+    const Plan p = plan_of(N, K, V);
     unsigned char *mem = reinterpret_cast<unsigned char *>(scratch);
-    SortArgs sa = {};
-    sa.tokens = tokens; sa.V = V; sa.N = (int)N; sa.padding_id = padding_id;
-    sa.key = reinterpret_cast<int32_t *>(mem + p.key);
-    sa.pos = reinterpret_cast<int32_t *>(mem + p.pos);
-    sa.present = accumulate ? nullptr : mem + p.present;
-    sa.status = workspace ? &ws_header(workspace)->status : nullptr;
-    if (!accumulate) PPO_RETURN_IF_CUDA(cudaMemsetAsync(sa.present, 0, (size_t)V, s));
-    int rc = launch_sort(sa, p, mem, s);
-    if (rc) return rc;
     BwdArgs a = {};
-    a.dY = dY; a.key = sa.key; a.pos = sa.pos; a.present = sa.present; a.dE = dE;
+    a.dY = dY; a.tokens = tokens; a.dE = dE; a.padding_id = padding_id;
+    a.present = mem + p.present;
     a.part = reinterpret_cast<float *>(mem + p.part);
     a.V = V; a.ldy = ldy; a.lde = lde; a.N = (int)N; a.K = (int)K;
     a.chunk = p.chunk; a.chunks = p.chunks; a.accumulate = accumulate != 0; a.scale = scale;
-    a.lanes = p.lanes; a.groups = p.groups; a.slabs = p.slabs;
-    const int64_t blocks = (int64_t)((p.chunks + p.groups - 1) / p.groups) * p.slabs;
     a.fill_rows = (int)(K >= 16384 ? 1 : 65536 / K < 256 ? 65536 / K : 256);
-    if (blocks + V / a.fill_rows + 1 >= ((int64_t)1 << 31) || (int64_t)p.chunks * ((K + kThreads - 1) / kThreads) >= ((int64_t)1 << 31))
-        return PPO_ERR_SHAPE;
-    a.chunk_blocks = (int)blocks;
+    a.status = workspace ? &ws_header(workspace)->status : nullptr;
     if (dtype == PPO_F32)
-        return out_dtype == PPO_F32 ? launch_sums<float, float>(a, vec, s) : launch_sums<float, __nv_bfloat16>(a, vec, s);
-    return out_dtype == PPO_F32 ? launch_sums<__nv_bfloat16, float>(a, vec, s) : launch_sums<__nv_bfloat16, __nv_bfloat16>(a, vec, s);
+        return out_dtype == PPO_F32 ? launch_bwd_types<float, float>(a, p, vec, mem, s)
+                                    : launch_bwd_types<float, __nv_bfloat16>(a, p, vec, mem, s);
+    return out_dtype == PPO_F32 ? launch_bwd_types<__nv_bfloat16, float>(a, p, vec, mem, s)
+                                : launch_bwd_types<__nv_bfloat16, __nv_bfloat16>(a, p, vec, mem, s);
 }

@@ -10,7 +10,7 @@
 //
 // Squares are fp32 and summed eight at a time before they go to fp64 (a conversion per element would bound the pass: 16 per
 // clock and SM). Eight squares that overflow, or that are small enough to lose digits, are taken again in fp64.
-#include "ppo_common.cuh"
+#include "ppo_packs.cuh"
 
 namespace ppo {
 namespace clip {
@@ -27,7 +27,7 @@ struct Table {
     void *out[N];
     int64_t numel[N];
     int32_t first[N];                             // first chunk
-    uint8_t type[N];                              // bit 0: bf16 in, bit 1: bf16 out, bit 2: 16-byte accesses, bit 3: in place
+    uint8_t type[N];                              // bit 0: bf16 in, bit 1: bf16 out, bit 2: packs of 8, bit 3: in place
 };
 
 struct Args {
@@ -38,26 +38,6 @@ struct Args {
     float *norm;                                  // [2] norm, coef
     int *status;
 };
-
-__device__ __forceinline__ float up(uint32_t w, int hi) { return __uint_as_float(hi ? w & 0xffff0000u : w << 16); }
-
-__device__ __forceinline__ void load8(const void *p, bool bf16, float *x)
-{
-    if (bf16) {
-        const uint4 v = *reinterpret_cast<const uint4 *>(p);
-        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = up(w[j >> 1], j & 1);
-    } else {
-        const float4 a = reinterpret_cast<const float4 *>(p)[0], b = reinterpret_cast<const float4 *>(p)[1];
-        x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
-    }
-}
-
-__device__ __forceinline__ float load1(const void *p, bool bf16, int64_t i)
-{
-    return bf16 ? __bfloat162float(reinterpret_cast<const __nv_bfloat16 *>(p)[i]) : reinterpret_cast<const float *>(p)[i];
-}
 
 template <int COUNT>
 __device__ __forceinline__ double squares(const float *x)
@@ -91,6 +71,48 @@ __device__ __forceinline__ int tensor_of(const Table<N> &t, int n, int chunk)
     return lo;
 }
 
+// elements [e0, e1) of one tensor
+template <typename TI>
+__device__ __forceinline__ double sum_chunk(const TI *in, int64_t e0, int64_t e1, bool packs)
+{
+    double sum = 0.0;
+    const int64_t whole = packs ? e0 + ((e1 - e0) & ~7ll) : e0;
+#pragma unroll 4
+    for (int64_t j = e0 + threadIdx.x * 8; j < whole; j += kThreads * 8) {
+        Pack<TI, 8> x;
+        x.load(in + j);
+        sum += squares<8>(x.v);
+    }
+#pragma unroll 4
+    for (int64_t j = whole + threadIdx.x; j < e1; j += kThreads) {
+        Pack<TI, 1> x;
+        x.load(in + j);
+        sum += squares<1>(x.v);
+    }
+    return sum;
+}
+
+template <typename TI, typename TO>
+__device__ __forceinline__ void scale_chunk(const TI *in, TO *out, float f, int64_t e0, int64_t e1, bool packs)
+{
+    const int64_t whole = packs ? e0 + ((e1 - e0) & ~7ll) : e0;
+#pragma unroll 4
+    for (int64_t j = e0 + threadIdx.x * 8; j < whole; j += kThreads * 8) {
+        Pack<TI, 8> x;
+        x.load(in + j);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x.v[k] *= f;
+        Pack<TO, 8>::store(out + j, x.v);
+    }
+#pragma unroll 4
+    for (int64_t j = whole + threadIdx.x; j < e1; j += kThreads) {
+        Pack<TI, 1> x;
+        x.load(in + j);
+        x.v[0] *= f;
+        Pack<TO, 1>::store(out + j, x.v);
+    }
+}
+
 template <int N>
 __global__ void __launch_bounds__(kThreads)
 norm_kernel(const __grid_constant__ Table<N> t, const Args a)
@@ -98,26 +120,10 @@ norm_kernel(const __grid_constant__ Table<N> t, const Args a)
     __shared__ double red[32];
     double sum = 0.0;
     for (int c = blockIdx.x; c < a.chunks; c += gridDim.x) {
-        const int i = tensor_of(t, a.n, c);
-        const bool bf16 = t.type[i] & 1;
+        const int i = tensor_of(t, a.n, c), type = t.type[i];
         const int64_t e0 = (int64_t)(c - t.first[i]) * kChunk, e1 = min(e0 + (int64_t)kChunk, t.numel[i]);
-        const unsigned char *in = reinterpret_cast<const unsigned char *>(t.in[i]);
-        int64_t e = e0;
-        if (t.type[i] & 4) {
-            const int64_t whole = e0 + ((e1 - e0) & ~7ll);
-#pragma unroll 4
-            for (int64_t j = e0 + threadIdx.x * 8; j < whole; j += kThreads * 8) {
-                float x[8];
-                load8(in + j * (bf16 ? 2 : 4), bf16, x);
-                sum += squares<8>(x);
-            }
-            e = whole;
-        }
-#pragma unroll 4
-        for (int64_t j = e + threadIdx.x; j < e1; j += kThreads) {
-            const float x = load1(in, bf16, j);
-            sum += squares<1>(&x);
-        }
+        sum += type & 1 ? sum_chunk(reinterpret_cast<const __nv_bfloat16 *>(t.in[i]), e0, e1, type & 4)
+                        : sum_chunk(reinterpret_cast<const float *>(t.in[i]), e0, e1, type & 4);
     }
     sum = block_sum<kThreads>(sum, red);
     if (threadIdx.x == 0) a.part[(size_t)a.launch * kMaxBlocks + blockIdx.x] = sum;
@@ -147,38 +153,16 @@ scale_kernel(const __grid_constant__ Table<N> t, const Args a)
         const int i = tensor_of(t, a.n, c);
         const int type = t.type[i];
         if ((type & 8) && f == 1.f) continue;
-        const bool in16 = type & 1, out16 = type & 2;
         const int64_t e0 = (int64_t)(c - t.first[i]) * kChunk, e1 = min(e0 + (int64_t)kChunk, t.numel[i]);
-        const unsigned char *in = reinterpret_cast<const unsigned char *>(t.in[i]);
-        unsigned char *out = reinterpret_cast<unsigned char *>(t.out[i]);
-        int64_t e = e0;
-        if (type & 4) {
-            const int64_t whole = e0 + ((e1 - e0) & ~7ll);
-#pragma unroll 2
-            for (int64_t j = e0 + threadIdx.x * 8; j < whole; j += kThreads * 8) {
-                float x[8];
-                load8(in + j * (in16 ? 2 : 4), in16, x);
-#pragma unroll
-                for (int k = 0; k < 8; ++k) x[k] *= f;
-                if (out16) {
-                    uint32_t w[4];
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const __nv_bfloat162 h = __floats2bfloat162_rn(x[2 * k], x[2 * k + 1]);
-                        w[k] = *reinterpret_cast<const uint32_t *>(&h);
-                    }
-                    __stcs(reinterpret_cast<uint4 *>(out + j * 2), make_uint4(w[0], w[1], w[2], w[3]));
-                } else {
-                    __stcs(reinterpret_cast<float4 *>(out + j * 4), make_float4(x[0], x[1], x[2], x[3]));
-                    __stcs(reinterpret_cast<float4 *>(out + j * 4) + 1, make_float4(x[4], x[5], x[6], x[7]));
-                }
-            }
-            e = whole;
-        }
-        for (int64_t j = e + threadIdx.x; j < e1; j += kThreads) {
-            const float x = load1(in, in16, j) * f;
-            if (out16) reinterpret_cast<__nv_bfloat16 *>(out)[j] = __float2bfloat16_rn(x);
-            else reinterpret_cast<float *>(out)[j] = x;
+        const float *in32 = reinterpret_cast<const float *>(t.in[i]);
+        const __nv_bfloat16 *in16 = reinterpret_cast<const __nv_bfloat16 *>(t.in[i]);
+        float *out32 = reinterpret_cast<float *>(t.out[i]);
+        __nv_bfloat16 *out16 = reinterpret_cast<__nv_bfloat16 *>(t.out[i]);
+        switch (type & 3) {
+        case 0: scale_chunk(in32, out32, f, e0, e1, type & 4); break;
+        case 1: scale_chunk(in16, out32, f, e0, e1, type & 4); break;
+        case 2: scale_chunk(in32, out16, f, e0, e1, type & 4); break;
+        default: scale_chunk(in16, out16, f, e0, e1, type & 4);
         }
     }
 }
@@ -202,7 +186,7 @@ static int launch_group(bool scale, const void *const *in, void *const *out, con
         t.first[k] = (int32_t)chunks;
         const int32_t od = out ? out_dtype[i] : in_dtype[i];
         t.type[k] = (in_dtype[i] == PPO_BF16) | (od == PPO_BF16) << 1 |
-                    ((reinterpret_cast<uintptr_t>(t.in[k]) | reinterpret_cast<uintptr_t>(t.out[k])) % 16 == 0) << 2 |
+                    (packs_fit(t.in[k], 8, in_dtype[i], 8) && packs_fit(t.out[k], 8, od, 8)) << 2 |
                     (t.in[k] == t.out[k]) << 3;
         chunks += (numel[i] + kChunk - 1) / kChunk;
         if (chunks >= ((int64_t)1 << 30)) return PPO_ERR_SHAPE;
