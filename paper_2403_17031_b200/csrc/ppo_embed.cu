@@ -67,9 +67,11 @@ lookup_kernel(const FwdArgs a)
         for (int r = 0; r < ROWS; ++r) p[r].load(row[r] + k);
 #pragma unroll
         for (int r = 0; r < ROWS; ++r) {
+            float x[VEC];
+            p[r].get(x);
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) p[r].v[e] *= scale[r];
-            if (i0 + r < a.N) Pack<TO, VEC>::store(out + r * a.ldo + k, p[r].v);
+            for (int e = 0; e < VEC; ++e) x[e] *= scale[r];
+            if (i0 + r < a.N) Pack<TO, VEC>::store(out + r * a.ldo + k, x);
         }
     }
 }
@@ -96,7 +98,7 @@ struct BwdArgs {
     const void *dY;
     const int32_t *tokens;
     const int32_t *key, *pos;       // sorted by token
-    uint8_t *present;               // [V] the token occurs
+    uint8_t *present;               // one byte a token, at present_at(): it occurs
     void *dE;
     float *part;                    // [chunks][2][K]: a run that comes from the chunk before; one that goes on in the next
     int64_t V, ldy, lde;
@@ -116,28 +118,38 @@ __device__ __forceinline__ void write_row(const BwdArgs &a, int64_t v, int k, fl
 #pragma unroll
     for (int e = 0; e < VEC; ++e) x[e] *= a.scale;
     if (a.accumulate) {
-        Pack<TO, VEC> old;
-        old.load_once(to);
+        Pack<TO, VEC> p;
+        p.load_once(to);
+        float old[VEC];
+        p.get(old);
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) x[e] += old.v[e];
+        for (int e = 0; e < VEC; ++e) x[e] += old[e];
     }
     Pack<TO, VEC>::store(to, x);
 }
 
 // The zero rows are most of what few positions write, so they go along with the launches that sort, which leave nearly all of
 // the memory's time unused.
-template <typename TO, int VEC>
+template <typename TO>
+__device__ __forceinline__ void zero_row(const BwdArgs &a, int64_t v)
+{
+    zero_bytes(reinterpret_cast<unsigned char *>(reinterpret_cast<TO *>(a.dE) + v * a.lde), (int64_t)a.K * sizeof(TO));
+}
+
+// Place of a token's byte: neighbouring tokens in different 32-byte sectors. The most frequent tokens of a vocabulary are
+// neighbours, and stores to one sector follow one another (326656 positions: counting takes 28 us with the bytes in order, 11 so).
+__device__ __forceinline__ uint8_t *present_at(const BwdArgs &a, int64_t v)
+{
+    const int64_t sectors = (a.V + 31) / 32;
+    return a.present + (v % sectors) * 32 + v / sectors;
+}
+
+template <typename TO>
 __device__ __forceinline__ void fill_rows(const BwdArgs &a, int block)
 {
-    float zero[VEC];
-#pragma unroll
-    for (int e = 0; e < VEC; ++e) zero[e] = 0.f;
     const int64_t v0 = a.fill0 + (int64_t)block * a.fill_rows;
-    for (int64_t v = v0; v < v0 + a.fill_rows && v < a.V; ++v) {
-        if (a.present[v]) continue;
-        TO *to = reinterpret_cast<TO *>(a.dE) + v * a.lde;
-        for (int k = threadIdx.x * VEC; k < a.K; k += blockDim.x * VEC) Pack<TO, VEC>::store(to + k, zero);
-    }
+    for (int64_t v = v0 + threadIdx.x / 32; v < v0 + a.fill_rows && v < a.V; v += blockDim.x / 32)
+        if (!*present_at(a, v)) zero_row<TO>(a, v);
 }
 
 __device__ __forceinline__ int key_of(const BwdArgs &a, int t) { return t < 0 || t >= a.V || t == a.padding_id ? (int)a.V : t; }
@@ -178,16 +190,9 @@ direct_kernel(const BwdArgs a)
     unsigned occur = 0;
     for (int i = 0; i < n; ++i) occur |= 1u << row[i];
     // zero rows, then the others
-    if (!a.accumulate && occur != (1u << rows) - 1) {
-        float zero[VEC];
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) zero[e] = 0.f;
-#pragma unroll 4
-        for (int r = 0; r < rows; ++r) {
-            if (occur >> r & 1) continue;
-            TO *to = reinterpret_cast<TO *>(a.dE) + (v0 + r) * a.lde;
-            for (int k = threadIdx.x * VEC; k < a.K; k += kThreads * VEC) Pack<TO, VEC>::store(to + k, zero);
-        }
+    if (!a.accumulate) {
+        for (int r = warp; r < rows; r += kThreads / 32)
+            if (!(occur >> r & 1)) zero_row<TO>(a, v0 + r);
     }
     for (; occur; occur &= occur - 1) {
         const int r = __ffs(occur) - 1;
@@ -208,10 +213,13 @@ direct_kernel(const BwdArgs a)
                     }
                 }
 #pragma unroll
-                for (int u = 0; u < U; ++u)
-                    if (u < got)
+                for (int u = 0; u < U; ++u) {
+                    if (u >= got) break;
+                    float x[VEC];
+                    p[u].get(x);
 #pragma unroll
-                        for (int e = 0; e < VEC; ++e) acc[e] += p[u].v[e];
+                    for (int e = 0; e < VEC; ++e) acc[e] += x[e];
+                }
             }
             write_row<TO, VEC>(a, v0 + r, k, acc);
         }
@@ -223,20 +231,22 @@ direct_kernel(const BwdArgs a)
 __device__ __forceinline__ void note_token(const BwdArgs &a, int t, int key)
 {
     if (key < a.V) {
-        if (!a.accumulate) a.present[key] = 1;
+        if (!a.accumulate) *present_at(a, key) = 1;
     } else if (a.status && (t < 0 || t >= a.V)) {
         atomicOr(a.status, PPO_DEV_BAD_TOKEN);
     }
 }
 
 // Up to 8192 positions of up to 2^19 tokens: each one's place is the number of (key, position) pairs below its own, counted.
-// A warp counts for four positions. (8192 positions: 67 M comparisons, 5 us; the passes below take 35.)
-constexpr int kRankPer = 4, kRankMax = 8192, kRankBits = 13, kRankWarps = kThreads / 32;
+// A warp counts for two positions. (8192 positions: 67 M comparisons, 5 us; the passes below take 35.)
+constexpr int kRankPer = 2, kRankMax = 8192, kRankBits = 13, kRankWarps = kThreads / 32;
 constexpr int64_t kRankVocabulary = (int64_t)1 << (32 - kRankBits);
 __global__ void __launch_bounds__(kThreads)
 rank_kernel(const BwdArgs a, int32_t *__restrict__ key_out, int32_t *__restrict__ pos_out)
 {
     __shared__ uint32_t pair[kRankMax];
+    grid_dependents_may_launch();
+#pragma unroll 8
     for (int j = threadIdx.x; j < a.N; j += kThreads) pair[j] = (uint32_t)key_of(a, a.tokens[j]) << kRankBits | (uint32_t)j;
     __syncthreads();
     const int lane = threadIdx.x & 31;
@@ -284,25 +294,35 @@ __device__ __forceinline__ void load_entry(const BwdArgs &a, const PassArgs &p, 
     pos = p.pos_in ? p.pos_in[i] : i;
 }
 
+constexpr int kSeen = 1024;
 __global__ void __launch_bounds__(kThreads)
 count_kernel(const BwdArgs a, const PassArgs p)
 {
-    __shared__ int n[kDigits];
+    // Frequent tokens: one addition for a warp's equal digits, and no second note of a token that the block noted last in its
+    // place of `seen` (text has a third of its tokens in one sector of `present`, whose stores would follow one another:
+    // 326656 positions 38 us).
+    __shared__ int n[kDigits], seen[kSeen];
+    grid_dependents_may_launch();
     n[threadIdx.x] = 0;
-    __syncthreads();
-    const int i0 = blockIdx.x * kTile;
 #pragma unroll
-    for (int j = 0; j < kTile; j += kThreads) {
-        const int i = i0 + j + threadIdx.x;
-        int digit = kDigits;
-        if (i < a.N) {
-            const int t = a.tokens[i], key = key_of(a, t);
-            digit = key & (kDigits - 1);
-            note_token(a, t, key);
-        }
-        // (frequent tokens: one addition for the warp's equal digits)
+    for (int j = 0; j < kSeen; j += kThreads) seen[j + threadIdx.x] = -1;
+    constexpr int R = kTile / kThreads;
+    const int i0 = blockIdx.x * kTile + threadIdx.x;
+    int t[R];
+#pragma unroll
+    for (int j = 0; j < R; ++j) t[j] = i0 + j * kThreads < a.N ? a.tokens[i0 + j * kThreads] : 0;
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < R; ++j) {
+        const bool in = i0 + j * kThreads < a.N;
+        const int key = key_of(a, t[j]), digit = in ? key & (kDigits - 1) : kDigits;
         const unsigned same = __match_any_sync(0xffffffffu, digit);
-        if (digit < kDigits && (same & ((1u << (threadIdx.x & 31)) - 1)) == 0) atomicAdd(&n[digit], __popc(same));
+        if (in && (same & ((1u << (threadIdx.x & 31)) - 1)) == 0) atomicAdd(&n[digit], __popc(same));
+        // (all that counts for no row has one key: of those each is looked at)
+        if (in && (key >= a.V || seen[key & (kSeen - 1)] != key)) {
+            seen[key & (kSeen - 1)] = key;
+            note_token(a, t[j], key);
+        }
     }
     __syncthreads();
     p.counts[(size_t)threadIdx.x * p.tiles + blockIdx.x] = n[threadIdx.x];
@@ -310,12 +330,14 @@ count_kernel(const BwdArgs a, const PassArgs p)
 
 // exclusive sum over the counts, in place; one block
 constexpr int kScanThreads = 1024;
-template <typename TO, int VEC>
+template <typename TO>
 __global__ void __launch_bounds__(kScanThreads)
 scan_kernel(const BwdArgs a, const PassArgs p)
 {
+    grid_dependents_may_launch();
+    grid_dependency_wait();
     if (blockIdx.x > 0) {
-        fill_rows<TO, VEC>(a, blockIdx.x - 1);
+        fill_rows<TO>(a, blockIdx.x - 1);
         return;
     }
     __shared__ int warp_sum[32];
@@ -357,12 +379,14 @@ scan_kernel(const BwdArgs a, const PassArgs p)
     }
 }
 
-template <typename TO, int VEC>
+template <typename TO>
 __global__ void __launch_bounds__(kThreads)
 scatter_kernel(const BwdArgs a, const PassArgs p)
 {
+    grid_dependents_may_launch();
+    grid_dependency_wait();
     if ((int)blockIdx.x >= a.work_blocks) {
-        fill_rows<TO, VEC>(a, blockIdx.x - a.work_blocks);
+        fill_rows<TO>(a, blockIdx.x - a.work_blocks);
         return;
     }
     __shared__ int at[kWarps][kDigits];
@@ -408,24 +432,46 @@ scatter_kernel(const BwdArgs a, const PassArgs p)
         if (key[j] >= 0) {
             p.key_out[to] = key[j];
             p.pos_out[to] = pos[j];
-            if (p.next_counts) atomicAdd(&p.next_counts[(size_t)((key[j] >> (p.shift + 8)) & (kDigits - 1)) * p.tiles + to / kTile], 1);
+        }
+        if (p.next_counts) {
+            // one addition for the warp's equal ones, as above
+            const int at2 = key[j] >= 0 ? ((key[j] >> (p.shift + 8)) & (kDigits - 1)) * p.tiles + to / kTile : -1;
+            const unsigned equal = __match_any_sync(0xffffffffu, at2);
+            if (at2 >= 0 && (equal & ((1u << lane) - 1)) == 0) atomicAdd(&p.next_counts[at2], __popc(equal));
         }
     }
 }
 
 // ---------------------------------------------------------------- sums
 template <typename TI, typename TO, int VEC>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, 3)
 sum_kernel(const BwdArgs a)
 {
-    constexpr int Q = packs_per_thread<VEC>(), U = 8 / Q;      // rows in flight
+    constexpr int Q = packs_per_thread<VEC>(), U = (VEC * sizeof(TI) > 16 ? 4 : 8) / Q;      // rows in flight
+    grid_dependents_may_launch();
+    grid_dependency_wait();
     if ((int)blockIdx.x >= a.work_blocks) {
-        fill_rows<TO, VEC>(a, blockIdx.x - a.work_blocks);
+        fill_rows<TO>(a, blockIdx.x - a.work_blocks);
         return;
     }
+    extern __shared__ int2 entries[];                           // [groups][chunk] key, position
     const int lane = threadIdx.x % a.lanes, group = threadIdx.x / a.lanes;
-    const int slab = blockIdx.x % a.slabs, c = (blockIdx.x / a.slabs) * a.groups + group;
+    const int slab = blockIdx.x % a.slabs, c0 = (blockIdx.x / a.slabs) * a.groups, c = c0 + group;
+    {
+        const int64_t first = (int64_t)c0 * a.chunk;
+#pragma unroll 4
+        for (int j = threadIdx.x; j < a.groups * a.chunk; j += kThreads)
+            entries[j] = first + j < a.N ? make_int2(a.key[first + j], a.pos[first + j]) : make_int2(-1, 0);
+    }
+    const int e0 = c * a.chunk;
+    int before = -1, behind = -1;
+    if (c < a.chunks) {
+        if (e0 > 0) before = a.key[e0 - 1];
+        if (c + 1 < a.chunks) behind = a.key[e0 + a.chunk];
+    }
+    __syncthreads();
     if (c >= a.chunks) return;
+    const int2 *mine = entries + group * a.chunk;
     int k[Q];
     bool in[Q];
 #pragma unroll
@@ -433,15 +479,14 @@ sum_kernel(const BwdArgs a)
         k[q] = ((slab * Q + q) * a.lanes + lane) * VEC;
         in[q] = k[q] < a.K;
     }
-    const int e0 = c * a.chunk, e1 = min(e0 + a.chunk, a.N);
     const TI *dY = reinterpret_cast<const TI *>(a.dY);
     float acc[Q][VEC];
 #pragma unroll
     for (int q = 0; q < Q; ++q)
 #pragma unroll
         for (int e = 0; e < VEC; ++e) acc[q][e] = 0.f;
-    int cur = a.key[e0];
-    bool from_before = e0 > 0 && a.key[e0 - 1] == cur;
+    int cur = mine[0].x;
+    bool from_before = before == cur;
     const auto flush = [&](bool goes_on) {
         if (cur >= a.V) return;
 #pragma unroll
@@ -455,27 +500,25 @@ sum_kernel(const BwdArgs a)
             }
         }
     };
-    for (int e = e0; e < e1 && cur < a.V; e += U) {
+    for (int e = 0; e < a.chunk; e += U) {                      // (a chunk is a multiple of 8)
+        if (mine[e].x < 0 || mine[e].x >= a.V) break;
         Pack<TI, VEC> p[U][Q];
-        int key[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            key[u] = e + u < e1 ? a.key[e + u] : -1;
-            const bool real = key[u] >= 0 && key[u] < a.V;
-            const TI *row = dY + (real ? (int64_t)a.pos[e + u] : 0) * a.ldy;
+            const int2 en = mine[e + u];
+            const TI *row = dY + (int64_t)en.y * a.ldy;
 #pragma unroll
             for (int q = 0; q < Q; ++q) {
-                if (real && in[q]) p[u][q].load_once(row + k[q]);
-                else
-#pragma unroll
-                    for (int x = 0; x < VEC; ++x) p[u][q].v[x] = 0.f;
+                if ((unsigned)en.x < (unsigned)a.V && in[q]) p[u][q].load_once(row + k[q]);
+                else p[u][q].zero();
             }
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            if (key[u] >= 0 && key[u] != cur) {
+            const int key = mine[e + u].x;
+            if (key >= 0 && key != cur) {
                 flush(false);
-                cur = key[u];
+                cur = key;
                 from_before = false;
 #pragma unroll
                 for (int q = 0; q < Q; ++q)
@@ -483,12 +526,15 @@ sum_kernel(const BwdArgs a)
                     for (int x = 0; x < VEC; ++x) acc[q][x] = 0.f;
             }
 #pragma unroll
-            for (int q = 0; q < Q; ++q)
+            for (int q = 0; q < Q; ++q) {
+                float x[VEC];
+                p[u][q].get(x);
 #pragma unroll
-                for (int x = 0; x < VEC; ++x) acc[q][x] += p[u][q].v[x];
+                for (int i = 0; i < VEC; ++i) acc[q][i] += x[i];
+            }
         }
     }
-    flush(e1 < a.N && a.key[e1] == cur);
+    flush(behind == cur);
 }
 
 // The runs that cross chunks: the block of the chunk in which such a run begins adds the partial sums up.
@@ -496,6 +542,7 @@ template <typename TO, int VEC>
 __global__ void __launch_bounds__(kThreads)
 join_kernel(const BwdArgs a)
 {
+    grid_dependency_wait();
     const int c = blockIdx.x / a.slabs, k = ((blockIdx.x % a.slabs) * kThreads + threadIdx.x) * VEC;
     const int e0 = c * a.chunk, e1 = e0 + a.chunk;              // (the last chunk has no block)
     const int t = a.key[e1 - 1], next = a.key[e1], before = e0 > 0 ? a.key[e0 - 1] : -1;
@@ -508,16 +555,19 @@ join_kernel(const BwdArgs a)
         else hi = mid - 1;
     }
     if (k >= a.K) return;
-    Pack<float, VEC> sum;
-    sum.load(a.part + ((size_t)c * 2 + 1) * a.K + k);
-#pragma unroll 8
+    Pack<float, VEC> p;
+    float sum[VEC];
+    p.load(a.part + ((size_t)c * 2 + 1) * a.K + k);
+    p.get(sum);
+#pragma unroll 16
     for (int i = c + 1; i <= lo; ++i) {
-        Pack<float, VEC> x;
-        x.load(a.part + (size_t)i * 2 * a.K + k);
+        p.load(a.part + (size_t)i * 2 * a.K + k);
+        float x[VEC];
+        p.get(x);
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) sum.v[e] += x.v[e];
+        for (int e = 0; e < VEC; ++e) sum[e] += x[e];
     }
-    write_row<TO, VEC>(a, t, k, sum.v);
+    write_row<TO, VEC>(a, t, k, sum);
 }
 
 // ---------------------------------------------------------------- host side
@@ -556,7 +606,7 @@ static Plan plan_of(int64_t N, int64_t K, int64_t V)
     p.key2 = take(p.tiles ? ints : 0);
     p.pos2 = take(p.tiles ? ints : 0);
     p.counts = take(counts * p.passes);
-    p.present = take((size_t)V);
+    p.present = take(((size_t)V + 31) / 32 * 32);
     // cleared first: the counts of the passes behind the first, and `present`
     p.first_zero = p.passes > 1 ? p.counts + counts : p.present;
     p.zero_bytes = at - p.first_zero;
@@ -620,12 +670,10 @@ static int launch_bwd(BwdArgs a, const Plan &p, unsigned char *mem, cudaStream_t
                 if ((rc = launch_status())) return rc;
             }
             unsigned extra = fill.take(a, false);
-            scan_kernel<TO, VEC><<<1 + extra, kScanThreads, 0, s>>>(a, ps);
-            if ((rc = launch_status())) return rc;
+            PPO_RETURN_IF_CUDA(launch_dependent(scan_kernel<TO>, dim3(1 + extra), dim3(kScanThreads), 0, s, a, ps));
             extra = fill.take(a, false);
             a.work_blocks = p.tiles;
-            scatter_kernel<TO, VEC><<<p.tiles + extra, kThreads, 0, s>>>(a, ps);
-            if ((rc = launch_status())) return rc;
+            PPO_RETURN_IF_CUDA(launch_dependent(scatter_kernel<TO>, dim3(p.tiles + extra), dim3(kThreads), 0, s, a, ps));
             ps.key_in = ps.key_out;
             ps.pos_in = ps.pos_out;
         }
@@ -636,16 +684,17 @@ static int launch_bwd(BwdArgs a, const Plan &p, unsigned char *mem, cudaStream_t
     a.groups = kThreads / a.lanes;
     a.slabs = (int)((packs + a.lanes - 1) / a.lanes);
     const int64_t blocks = (int64_t)((p.chunks + a.groups - 1) / a.groups) * a.slabs;
-    const int join_slabs = (int)((a.K + kThreads * VEC - 1) / (kThreads * VEC));
+    constexpr int kJoinVec = VEC > 4 ? 4 : VEC;
+    const int join_slabs = (int)((a.K + kThreads * kJoinVec - 1) / (kThreads * kJoinVec));
     if (blocks + a.V / a.fill_rows + 1 >= ((int64_t)1 << 31) || (int64_t)p.chunks * join_slabs >= ((int64_t)1 << 31)) return PPO_ERR_SHAPE;
     a.work_blocks = (int)blocks;
     const unsigned extra = fill.take(a, true);
-    sum_kernel<TI, TO, VEC><<<(unsigned)blocks + extra, kThreads, 0, s>>>(a);
-    rc = launch_status();
-    if (rc || p.chunks < 2) return rc;
+    PPO_RETURN_IF_CUDA(launch_dependent(sum_kernel<TI, TO, VEC>, dim3((unsigned)blocks + extra), dim3(kThreads),
+                                        (size_t)a.groups * a.chunk * sizeof(int2), s, a));
+    if (p.chunks < 2) return PPO_OK;
     a.slabs = join_slabs;
-    join_kernel<TO, VEC><<<(unsigned)((p.chunks - 1) * join_slabs), kThreads, 0, s>>>(a);
-    return launch_status();
+    PPO_RETURN_IF_CUDA(launch_dependent(join_kernel<TO, kJoinVec>, dim3((unsigned)((p.chunks - 1) * join_slabs)), dim3(kThreads), 0, s, a));
+    return PPO_OK;
 }
 
 template <typename TI, typename TO>
@@ -721,7 +770,9 @@ extern "C" int ppo_embed_bwd(const void *dY, int dtype, int64_t N, int64_t K, in
     a.part = reinterpret_cast<float *>(mem + p.part);
     a.V = V; a.ldy = ldy; a.lde = lde; a.N = (int)N; a.K = (int)K;
     a.chunk = p.chunk; a.chunks = p.chunks; a.accumulate = accumulate != 0; a.scale = scale;
-    a.fill_rows = (int)(K >= 16384 ? 1 : 65536 / K < 256 ? 65536 / K : 256);
+    // (64 KB a block, eight rows for its warps at least)
+    const int64_t row_bytes = K * (int64_t)size_of(out_dtype);
+    a.fill_rows = (int)(row_bytes >= 8192 ? 8 : 65536 / row_bytes < 256 ? 65536 / row_bytes : 256);
     a.status = workspace ? &ws_header(workspace)->status : nullptr;
     if (dtype == PPO_F32)
         return out_dtype == PPO_F32 ? launch_bwd_types<float, float>(a, p, vec, mem, s)

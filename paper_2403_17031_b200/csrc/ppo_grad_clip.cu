@@ -79,15 +79,19 @@ __device__ __forceinline__ double sum_chunk(const TI *in, int64_t e0, int64_t e1
     const int64_t whole = packs ? e0 + ((e1 - e0) & ~7ll) : e0;
 #pragma unroll 4
     for (int64_t j = e0 + threadIdx.x * 8; j < whole; j += kThreads * 8) {
-        Pack<TI, 8> x;
-        x.load(in + j);
-        sum += squares<8>(x.v);
+        Pack<TI, 8> p;
+        p.load(in + j);
+        float x[8];
+        p.get(x);
+        sum += squares<8>(x);
     }
 #pragma unroll 4
     for (int64_t j = whole + threadIdx.x; j < e1; j += kThreads) {
-        Pack<TI, 1> x;
-        x.load(in + j);
-        sum += squares<1>(x.v);
+        Pack<TI, 1> p;
+        p.load(in + j);
+        float x[1];
+        p.get(x);
+        sum += squares<1>(x);
     }
     return sum;
 }
@@ -98,18 +102,22 @@ __device__ __forceinline__ void scale_chunk(const TI *in, TO *out, float f, int6
     const int64_t whole = packs ? e0 + ((e1 - e0) & ~7ll) : e0;
 #pragma unroll 4
     for (int64_t j = e0 + threadIdx.x * 8; j < whole; j += kThreads * 8) {
-        Pack<TI, 8> x;
-        x.load(in + j);
+        Pack<TI, 8> p;
+        p.load(in + j);
+        float x[8];
+        p.get(x);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) x.v[k] *= f;
-        Pack<TO, 8>::store(out + j, x.v);
+        for (int k = 0; k < 8; ++k) x[k] *= f;
+        Pack<TO, 8>::store(out + j, x);
     }
 #pragma unroll 4
     for (int64_t j = whole + threadIdx.x; j < e1; j += kThreads) {
-        Pack<TI, 1> x;
-        x.load(in + j);
-        x.v[0] *= f;
-        Pack<TO, 1>::store(out + j, x.v);
+        Pack<TI, 1> p;
+        p.load(in + j);
+        float x[1];
+        p.get(x);
+        x[0] *= f;
+        Pack<TO, 1>::store(out + j, x);
     }
 }
 
@@ -118,6 +126,8 @@ __global__ void __launch_bounds__(kThreads)
 norm_kernel(const __grid_constant__ Table<N> t, const Args a)
 {
     __shared__ double red[32];
+    grid_dependents_may_launch();
+    grid_dependency_wait();
     double sum = 0.0;
     for (int c = blockIdx.x; c < a.chunks; c += gridDim.x) {
         const int i = tensor_of(t, a.n, c), type = t.type[i];
@@ -134,6 +144,8 @@ __global__ void __launch_bounds__(kThreads)
 scale_kernel(const __grid_constant__ Table<N> t, const Args a)
 {
     __shared__ double red[32];
+    grid_dependents_may_launch();
+    grid_dependency_wait();
     double sum = 0.0;
     for (int j = threadIdx.x; j < a.launches * kMaxBlocks; j += kThreads)
         if (j % kMaxBlocks < a.blocks) sum += a.part[j];
@@ -192,8 +204,12 @@ static int launch_group(bool scale, const void *const *in, void *const *out, con
         if (chunks >= ((int64_t)1 << 30)) return PPO_ERR_SHAPE;
     }
     a.chunks = (int)chunks;
-    if (scale) scale_kernel<N><<<a.blocks, kThreads, 0, s>>>(t, a);
-    else norm_kernel<N><<<a.blocks, kThreads, 0, s>>>(t, a);
+    // (the first launch waits for all work before the call)
+    if (scale || a.launch > 0) {
+        PPO_RETURN_IF_CUDA(launch_dependent(scale ? scale_kernel<N> : norm_kernel<N>, dim3(a.blocks), dim3(kThreads), 0, s, t, a));
+        return PPO_OK;
+    }
+    norm_kernel<N><<<a.blocks, kThreads, 0, s>>>(t, a);
     return launch_status();
 }
 
