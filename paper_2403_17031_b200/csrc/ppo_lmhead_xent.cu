@@ -11,9 +11,10 @@
 //      piece of the logits is needed between the products.
 //   2  dH = a (U' W^T)
 //   3  dW = (a H)^T U', over all pieces: fp32 sums in scratch, tile by tile in the order in which the epilogue holds them
-// The reference is a multiple of 64 near the largest y of the row's 128 columns, so U and its sums stay inside fp32's (and
-// bf16's) exponents for logits of any size, and almost always all of a row's references are the same; where they are not, the
-// columns with a smaller one are multiplied by 2^(difference), which is exact, before product 2.
+// A row's reference is set before product 1, from the mean of 64 neighbouring logits, and serves columns whose largest y lies between 32
+// below and 96 above that mean: U and its sums stay inside fp32's (and bf16's) exponents, for logits of any size. 128 columns whose
+// largest lies elsewhere move their own reference by multiples of 128; where a row's references differ, the columns with a
+// smaller one are multiplied by 2^(difference), which is exact, before product 2.
 //
 // Roundings to 16 bits: U, a H, and the results. Statistics, sums and nll are fp32, the loss fp64. What the rounding of U
 // would do to the gradients is kept small in three ways. S in the gradient is the sum of the rounded U, so that D is the
@@ -33,11 +34,11 @@ namespace xent {
 
 using namespace tc;
 
-constexpr int kBM = 128, kTile = 256, kBlockK = 64, kStages = 6;
+constexpr int kBM = 128, kTile = 256, kBlockK = 64, kStages = 5;
 constexpr int kHalf = kBM * kBlockK * 2, kStage = 2 * kHalf, kBox = 64 * kBlockK * 2;    // bytes: a block's half of A or of B
 constexpr int kEpiWarps = 8, kThreads = (4 + kEpiWarps) * 32;
-constexpr int kStageOut = 32 * 128;                        // per epilogue warp: 32 rows x 64 bf16
-constexpr int kSmem = kStages * kStage + kEpiWarps * kStageOut + 1024;
+constexpr int kStageOut = 32 * 128;                        // two per epilogue warp: 32 rows x 64 bf16
+constexpr int kSmem = kStages * kStage + 2 * kEpiWarps * kStageOut + 1024;
 constexpr int kChunk = 128;                                // columns with one reference
 constexpr int kMaxPairs = 80;
 constexpr int kTileFloats = kTile * kTile;
@@ -56,6 +57,7 @@ struct Args {
     // kLogits
     float c;                                               // log2(e) / tau
     const int32_t *labels, *order;                         // order[i]: the original row of real row i
+    const float *base;                                     // [M] reference of real row i
     float *picked;                                         // [rows] accumulator at the label
     float4 *part;                                          // [rows][chunks] reference, sum, sum of the rounded values
     int chunks, store;
@@ -259,6 +261,8 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     cluster_barrier();                                          // the other block's barriers are ready too
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem_base = sm.tmem_base;
+    grid_dependents_may_launch();
+    grid_dependency_wait();
     const int rank = (int)cluster_rank(), pair = blockIdx.x / 2, pairs = gridDim.x / 2;
     const int rows = rows_of(a);
     const Plan plan = plan_of<PRODUCT>(a, rows, pairs);
@@ -348,7 +352,8 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         __syncwarp();
     } else if (warp >= 4) {
         const int q = warp & 3, h = (warp - 4) >> 2;            // lanes 32 q .., columns 128 h .. of the tile
-        unsigned char *stage = ring + (size_t)kStages * kStage + (warp - 4) * kStageOut;
+        unsigned char *const stages = ring + (size_t)kStages * kStage + (warp - 4) * 2 * kStageOut;
+        unsigned char *stage = stages;
         const uint32_t tmem_empty = leader_addr(&sm.tmem_empty[0]);
         const float nan = __int_as_float(0x7fffffff);
         bool alive = true;
@@ -362,10 +367,14 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             const uint32_t taddr = tmem_base + buf * kTile + h * 128 + ((uint32_t)(q * 32) << 16);
             bool ok = false;
             int label = -1, out_row = -1;
+            float base = 0.f;
             float2 scale = make_float2(0.f, 0.f);
             if (PRODUCT == kLogits) {
                 ok = row < rows;
-                if (ok) label = a.labels[a.order[a.row0 + row]] - n;
+                if (ok) {
+                    label = a.labels[a.order[a.row0 + row]] - n;
+                    base = a.base[a.row0 + row];
+                }
             } else if (PRODUCT == kHidden) {
                 ok = row < rows;
                 if (ok && work.part < 0) {
@@ -413,8 +422,10 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                     __syncwarp();
                 }
             };
-            const auto reuse = [&] {                            // the buffer's last copy has read it
-                if (lane == 0) tma_store_wait_read();
+            // the other staging buffer, whose last copy has read it
+            const auto reuse = [&] {
+                stage = stage == stages ? stages + kStageOut : stages;
+                if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
                 __syncwarp();
             };
 
@@ -433,7 +444,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                         for (int j = 0; j < 32; ++j) m = j < left ? fmaxf(m, v[j]) : m;
                     }
                 }
-                const float ref = 64.f * rintf(fmaxf(m * a.c, -1e9f) * (1.f / 64.f));
+                const float ref = base + 128.f * rintf((fmaxf(m * a.c, -1e9f) - base) * (1.f / 128.f));
                 float s = 0.f, rounded = 0.f;
 #pragma unroll 1
                 for (int cc = 0; cc < 4; ++cc) {
@@ -467,6 +478,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                     float v[32];
                     read(cc, cc == 3, v);
                     if (work.part >= 0) {
+                        if (!ok) continue;
 #pragma unroll
                         for (int j = 0; j < 8; ++j)
                             part[(cc * 8 + j) * kTile] = make_float4(v[j * 4], v[j * 4 + 1], v[j * 4 + 2], v[j * 4 + 3]);
@@ -533,6 +545,8 @@ __global__ void __launch_bounds__(kJoinThreads)
 join_kernel(const Args a, int pairs)
 {
     __shared__ float4 turn[32][17];
+    grid_dependents_may_launch();
+    grid_dependency_wait();
     const int rows = rows_of(a);
     const Plan p = plan_of<kHidden>(a, rows, pairs);
     const int rest = blockIdx.x / kJoinBlocks, part_of = blockIdx.x % kJoinBlocks;
@@ -587,6 +601,11 @@ struct RowArgs {
     const float *denom;
     int32_t *order;                                             // [M] real rows, ascending; then the others
     int *n_real;
+    const __nv_bfloat16 *W;
+    int64_t ldw;
+    int vk;
+    float *w_mean;                                              // [K] mean of kSample columns of W
+    float *base;                                                // [M] reference of real row i
     __nv_bfloat16 *packed;                                      // [M, Kp] (written when some row is left out)
     __nv_bfloat16 *scaled;                                      // [rows_max, Kp] a H; null: no gradients
     __nv_bfloat16 *u;                                           // [rows_max, Vp]
@@ -600,20 +619,94 @@ struct RowArgs {
     int *status;
 };
 
-constexpr int kOrderThreads = 1024, kOrderPer = 8;
+// The mean of kSample neighbouring columns of W, from the middle of the vocabulary, for 128 hidden elements: a thread loads
+// eight neighbours in memory, eight (stored [K, V]) or 64 (stored [V, K]) threads share an element. (One element after the
+// other, 64 loads each: 36 us at K = 4096, most of it misses of the address translation.)
+constexpr int kOrderThreads = 1024, kOrderPer = 8, kSample = 64, kMeanPer = kOrderThreads / 8;
+__device__ __forceinline__ void mean_columns(const RowArgs &a, int k0, float (*part)[kMeanPer])
+{
+    const int v0 = min(a.V / 2, max(0, a.V - kSample)) & ~7, n = min(kSample, a.V - v0);
+    float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    if (a.vk) {
+        // four times 16 rows of W
+        const int k = k0 + (threadIdx.x & 15) * 8;
+#pragma unroll
+        for (int j = threadIdx.x >> 4; j < kSample; j += kOrderThreads / 16) {
+            if (j >= n) break;
+            const __nv_bfloat16 *w = a.W + (int64_t)(v0 + j) * a.ldw + k;
+            if (k + 8 <= a.K) {
+                const uint4 y = *reinterpret_cast<const uint4 *>(w);
+                const uint32_t z[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] += e & 1 ? high(z[e / 2]) : low(z[e / 2]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (k + e < a.K) x[e] += __bfloat162float(w[e]);
+            }
+        }
+        // lanes 16 apart hold other rows for the same elements; then the warps
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] += __shfl_xor_sync(0xffffffffu, x[e], 16);
+        if ((threadIdx.x & 31) < 16)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) part[threadIdx.x >> 5][(threadIdx.x & 15) * 8 + e] = x[e];
+        __syncthreads();
+        if (threadIdx.x < kMeanPer && k0 + (int)threadIdx.x < a.K) {
+            float s = 0.f;
+            for (int w = 0; w < kOrderThreads / 32; ++w) s += part[w][threadIdx.x];
+            a.w_mean[k0 + threadIdx.x] = s / (float)n;
+        }
+        return;
+    }
+    const int k = k0 + (threadIdx.x >> 3), v = v0 + (threadIdx.x & 7) * 8;
+    float s = 0.f;
+    if (k < a.K) {
+        const __nv_bfloat16 *w = a.W + (int64_t)k * a.ldw + v;
+        if (v + 8 <= a.V) {
+            const uint4 y = *reinterpret_cast<const uint4 *>(w);
+            s = low(y.x) + high(y.x) + low(y.y) + high(y.y) + low(y.z) + high(y.z) + low(y.w) + high(y.w);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (v + e < a.V) s += __bfloat162float(w[e]);
+        }
+    }
+#pragma unroll
+    for (int off = 1; off < 8; off <<= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
+    if (k < a.K && (threadIdx.x & 7) == 0) a.w_mean[k] = s / (float)n;
+}
+
+// Block 0: the real rows' order. The others: mean_columns.
 __global__ void __launch_bounds__(kOrderThreads)
 order_kernel(const RowArgs a)
 {
+    grid_dependents_may_launch();
+    __shared__ float part[kOrderThreads / 32][kMeanPer];
+    if (blockIdx.x > 0) {
+        mean_columns(a, (blockIdx.x - 1) * kMeanPer, part);
+        return;
+    }
     __shared__ int warp_sum[32], carry;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     if (threadIdx.x == 0) carry = 0;
     __syncthreads();
+    const bool wide = reinterpret_cast<uintptr_t>(a.labels) % 16 == 0 && reinterpret_cast<uintptr_t>(a.mask) % 8 == 0;
     for (int64_t base = 0; base < a.M; base += kOrderThreads * kOrderPer) {
         const int64_t i0 = base + threadIdx.x * kOrderPer;
         unsigned bits = 0;
+        if (wide && i0 + kOrderPer <= a.M) {
+            const int4 x = reinterpret_cast<const int4 *>(a.labels + i0)[0], y = reinterpret_cast<const int4 *>(a.labels + i0)[1];
+            const uint2 m = a.mask ? *reinterpret_cast<const uint2 *>(a.mask + i0) : make_uint2(~0u, ~0u);
+            const int l[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
 #pragma unroll
-        for (int e = 0; e < kOrderPer; ++e)
-            if (i0 + e < a.M && (!a.mask || a.mask[i0 + e]) && a.labels[i0 + e] != a.ignore_id) bits |= 1u << e;
+            for (int e = 0; e < 8; ++e)
+                if (((e < 4 ? m.x : m.y) >> (8 * (e & 3)) & 255) && l[e] != a.ignore_id) bits |= 1u << e;
+        } else {
+#pragma unroll
+            for (int e = 0; e < kOrderPer; ++e)
+                if (i0 + e < a.M && (!a.mask || a.mask[i0 + e]) && a.labels[i0 + e] != a.ignore_id) bits |= 1u << e;
+        }
         const int mine = __popc(bits);
         int incl = mine;
 #pragma unroll
@@ -623,9 +716,8 @@ order_kernel(const RowArgs a)
         }
         if (lane == 31) warp_sum[warp] = incl;
         __syncthreads();
-        int before = carry;
-        for (int w = 0; w < warp; ++w) before += warp_sum[w];
-        int at = before + incl - mine;
+        const int w = warp_sum[lane];
+        int at = carry + __reduce_add_sync(0xffffffffu, lane < warp ? w : 0) + incl - mine;
 #pragma unroll
         for (int e = 0; e < kOrderPer; ++e) {
             if (i0 + e >= a.M) break;
@@ -641,12 +733,14 @@ order_kernel(const RowArgs a)
 }
 
 constexpr int kRowThreads = 256;
-// real rows packed where some are left out; those get their zeros
+// real rows: their reference, and a packed copy where some rows are left out; those get their zeros
 __global__ void __launch_bounds__(kRowThreads)
 pack_kernel(const RowArgs a)
 {
+    __shared__ float red[kRowThreads / 32];
+    grid_dependents_may_launch();
+    grid_dependency_wait();
     const int n = *a.n_real, i = blockIdx.x;
-    if (n == a.M) return;
     const int row = a.order[i];
     if (i >= n) {
         if (threadIdx.x == 0) {
@@ -659,10 +753,31 @@ pack_kernel(const RowArgs a)
     }
     const __nv_bfloat16 *from = a.H + (int64_t)row * a.ldh;
     __nv_bfloat16 *to = a.packed + (int64_t)i * a.Kp;
+    float s = 0.f;
     for (int k = threadIdx.x * 8; k < a.K; k += kRowThreads * 8) {
-        if (k + 8 <= a.K) *reinterpret_cast<uint4 *>(to + k) = *reinterpret_cast<const uint4 *>(from + k);
-        else
-            for (int e = k; e < a.K; ++e) to[e] = from[e];
+        if (k + 8 <= a.K) {
+            const uint4 v = *reinterpret_cast<const uint4 *>(from + k);
+            if (n < a.M) *reinterpret_cast<uint4 *>(to + k) = v;
+            const float4 p = *reinterpret_cast<const float4 *>(a.w_mean + k), q = *reinterpret_cast<const float4 *>(a.w_mean + k + 4);
+            s = fmaf(low(v.x), p.x, s); s = fmaf(high(v.x), p.y, s); s = fmaf(low(v.y), p.z, s); s = fmaf(high(v.y), p.w, s);
+            s = fmaf(low(v.z), q.x, s); s = fmaf(high(v.z), q.y, s); s = fmaf(low(v.w), q.z, s); s = fmaf(high(v.w), q.w, s);
+        } else {
+            for (int e = k; e < a.K; ++e) {
+                if (n < a.M) to[e] = from[e];
+                s = fmaf(__bfloat162float(from[e]), a.w_mean[e], s);
+            }
+        }
+    }
+    s = warp_sum_f(s);
+    if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = s;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        s = 0.f;
+#pragma unroll
+        for (int w = 0; w < kRowThreads / 32; ++w) s += red[w];
+        // the middle of the window; whole numbers, so that y - reference loses nothing that y does not
+        s = rintf(s * a.c) + 32.f;
+        a.base[i] = fabsf(s) < 1e9f ? s : 0.f;
     }
 }
 
@@ -671,6 +786,8 @@ __global__ void __launch_bounds__(kRowThreads)
 row_kernel(const RowArgs a)
 {
     __shared__ float red[3][kRowThreads / 32];
+    grid_dependents_may_launch();
+    grid_dependency_wait();
     const int n_real = *a.n_real, rows = max(0, min(a.rows_max, n_real - a.row0)), r = blockIdx.x;
     __nv_bfloat16 *scaled = a.scaled ? a.scaled + (int64_t)r * a.Kp : nullptr;
     if (r >= rows) {
@@ -765,6 +882,7 @@ __global__ void __launch_bounds__(kLossThreads)
 loss_kernel(const RowArgs a)
 {
     __shared__ double red[32];
+    grid_dependency_wait();
     double s = 0.0;
 #pragma unroll 4
     for (int i = threadIdx.x; i < a.M; i += kLossThreads) s += (double)a.nll[i];
@@ -780,7 +898,7 @@ loss_kernel(const RowArgs a)
 struct Layout {
     int pieces, rows_max, chunks, Kp;
     int64_t Vp;
-    size_t n_real, order, picked, row_scale, part, packed, scaled, u, parts, sums, bytes;
+    size_t n_real, order, base, w_mean, picked, row_scale, part, packed, scaled, u, parts, sums, bytes;
 };
 
 // Pieces of at most 8192 rows by default: at V = 50304 that is 824 MB of U, and the sums of dW, read and written once a
@@ -806,6 +924,8 @@ static Layout layout_of(int64_t M, int64_t K, int64_t V, int64_t piece_rows, boo
     const size_t rows = (size_t)l.rows_max;
     l.n_real = take(4);
     l.order = take((size_t)M * 4);
+    l.base = take((size_t)M * 4);
+    l.w_mean = take((size_t)K * 4);
     l.picked = take(rows * 4);
     l.row_scale = take(rows * sizeof(float2));
     l.part = take(rows * (size_t)l.chunks * sizeof(float4));
@@ -839,13 +959,21 @@ static int launch_product(const CUtensorMap &ma, const CUtensorMap &ma_all, cons
     cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = kSmem;
     cfg.stream = s;
-    cudaLaunchAttribute attr[1];
+    cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = 2;
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    PPO_RETURN_IF_CUDA(cudaLaunchKernelEx(&cfg, kern, ma, ma_all, mb, mo, a));
+    cfg.numAttrs = 2;
+    cudaError_t e = cudaLaunchKernelEx(&cfg, kern, ma, ma_all, mb, mo, a);
+    if (e != cudaSuccess) {   // attribute not accepted in this context: ordinary launch (same results, no overlap)
+        (void)cudaGetLastError();
+        cfg.numAttrs = 1;
+        e = cudaLaunchKernelEx(&cfg, kern, ma, ma_all, mb, mo, a);
+    }
+    PPO_RETURN_IF_CUDA(e);
     return PPO_OK;
 }
 
@@ -906,6 +1034,9 @@ extern "C" int ppo_lmhead_xent(const void *H, int64_t ldh, const void *W, int64_
     r.c = kLog2e / temperature; r.inv_tau = 1.f / temperature; r.scale = scale; r.denom = denom;
     r.n_real = reinterpret_cast<int *>(mem + l.n_real);
     r.order = reinterpret_cast<int32_t *>(mem + l.order);
+    r.W = reinterpret_cast<const __nv_bfloat16 *>(W); r.ldw = ldw; r.vk = vk;
+    r.w_mean = reinterpret_cast<float *>(mem + l.w_mean);
+    r.base = reinterpret_cast<float *>(mem + l.base);
     r.packed = reinterpret_cast<__nv_bfloat16 *>(mem + l.packed);
     r.scaled = dW ? reinterpret_cast<__nv_bfloat16 *>(mem + l.scaled) : nullptr;
     r.u = grad ? reinterpret_cast<__nv_bfloat16 *>(mem + l.u) : nullptr;
@@ -933,7 +1064,7 @@ extern "C" int ppo_lmhead_xent(const void *H, int64_t ldh, const void *W, int64_
 
     Args a = {};
     a.n_real = r.n_real; a.M = (int)M; a.rows_max = l.rows_max; a.status = status;
-    a.c = r.c; a.labels = labels; a.order = r.order; a.picked = r.picked; a.part = r.part; a.chunks = l.chunks; a.store = grad;
+    a.c = r.c; a.labels = labels; a.order = r.order; a.base = r.base; a.picked = r.picked; a.part = r.part; a.chunks = l.chunks; a.store = grad;
     a.row_scale = r.row_scale;
     Args a1 = a, a2 = a, a3 = a;
     a1.dim_m = l.rows_max; a1.dim_n = (int)V; a1.dim_k = (int)K; a1.gm = 9; a1.gn = 8;
@@ -952,23 +1083,22 @@ extern "C" int ppo_lmhead_xent(const void *H, int64_t ldh, const void *W, int64_
         }
     }
 
-    order_kernel<<<1, kOrderThreads, 0, s>>>(r);
+    // (the first launch waits for all work before the call, the others for the one before them)
+    order_kernel<<<1 + (unsigned)((K + kMeanPer - 1) / kMeanPer), kOrderThreads, 0, s>>>(r);
     if ((rc = launch_status())) return rc;
-    pack_kernel<<<(unsigned)M, kRowThreads, 0, s>>>(r);
-    if ((rc = launch_status())) return rc;
+    PPO_RETURN_IF_CUDA(launch_dependent(pack_kernel, dim3((unsigned)M), dim3(kRowThreads), 0, s, r));
     for (int p = 0; p < l.pieces; ++p) {
         r.row0 = a1.row0 = a2.row0 = a3.row0 = p * l.rows_max;
         rc = vk ? launch_product<false, false, kLogits>(m_packed, m_h, m_w1, m_u1, a1, pairs, s)
                 : launch_product<false, true, kLogits>(m_packed, m_h, m_w1, m_u1, a1, pairs, s);
         if (rc) return rc;
-        row_kernel<<<(unsigned)l.rows_max, kRowThreads, 0, s>>>(r);
-        if ((rc = launch_status())) return rc;
+        PPO_RETURN_IF_CUDA(launch_dependent(row_kernel, dim3((unsigned)l.rows_max), dim3(kRowThreads), 0, s, r));
         if (dH) {
             rc = vk ? launch_product<false, true, kHidden>(m_u2, m_u2, m_w2, m_u2, a2, pairs, s)
                     : launch_product<false, false, kHidden>(m_u2, m_u2, m_w2, m_u2, a2, pairs, s);
             if (rc) return rc;
-            (vk ? join_kernel<true> : join_kernel<false>)<<<(unsigned)((pairs - 1) * kJoinBlocks), kJoinThreads, 0, s>>>(a2, pairs);
-            if ((rc = launch_status())) return rc;
+            PPO_RETURN_IF_CUDA(launch_dependent(vk ? join_kernel<true> : join_kernel<false>, dim3((unsigned)((pairs - 1) * kJoinBlocks)),
+                                                dim3(kJoinThreads), 0, s, a2, pairs));
         }
         if (dW) {
             rc = vk ? launch_product<true, true, kWeight>(m_u3, m_u3, m_scaled, m_dw, a3, pairs, s)
@@ -976,6 +1106,6 @@ extern "C" int ppo_lmhead_xent(const void *H, int64_t ldh, const void *W, int64_
             if (rc) return rc;
         }
     }
-    loss_kernel<<<1, kLossThreads, 0, s>>>(r);
-    return launch_status();
+    PPO_RETURN_IF_CUDA(launch_dependent(loss_kernel, dim3(1), dim3(kLossThreads), 0, s, r));
+    return PPO_OK;
 }
