@@ -34,16 +34,26 @@ namespace xent {
 
 using namespace tc;
 
-constexpr int kBM = 128, kTile = 256, kBlockK = 64, kStages = 5;
-constexpr int kHalf = kBM * kBlockK * 2, kStage = 2 * kHalf, kBox = 64 * kBlockK * 2;    // bytes: a block's half of A or of B
+constexpr int kBM = 128, kBN = 256, kBlockK = 64, kBox = 64 * kBlockK * 2;
 constexpr int kEpiWarps = 8, kThreads = (4 + kEpiWarps) * 32;
 constexpr int kStageOut = 32 * 128;                        // two per epilogue warp: 32 rows x 64 bf16
-constexpr int kSmem = kStages * kStage + 2 * kEpiWarps * kStageOut + 1024;
 constexpr int kChunk = 128;                                // columns with one reference
-constexpr int kMaxPairs = 80;
-constexpr int kTileFloats = kTile * kTile;
+constexpr int kMaxSms = 160;
 constexpr float kNoRef = -1.0e30f;
-static_assert(kSmem <= 232448 - 1024, "shared memory of a block");
+// 2^-64 and 2^64: the largest of a chunk's U lies between them, its smaller ones down to 2^-126 and their sums stay normal numbers
+constexpr float kLeast = 5.421010862427522e-20f, kMost = 1.8446744073709552e19f;
+
+// Pairs of blocks share a tile of 256 x 256: each loads half of either operand. Up to 128 rows, blocks alone on tiles of
+// 128 x 256: half of a pair's tile would be idle rows, and the tensor cores would take longer over them than memory over W.
+template <bool PAIR>
+struct Shape {
+    static constexpr int kM = PAIR ? 2 * kBM : kBM, kRowsB = PAIR ? kBN / 2 : kBN;   // tile rows; a block's share of B
+    static constexpr int kBytesA = kBM * kBlockK * 2, kBytesB = kRowsB * kBlockK * 2, kStage = kBytesA + kBytesB;
+    static constexpr int kStages = PAIR ? 5 : 3;
+    static constexpr int kSmem = kStages * kStage + 2 * kEpiWarps * kStageOut + 1024;
+    static constexpr int kTileFloats = kM * kBN;
+    static_assert(kSmem <= 232448 - 1024, "shared memory of a block");
+};
 
 enum Product { kLogits = 1, kHidden = 2, kWeight = 3 };
 
@@ -56,8 +66,9 @@ struct Args {
     int *status;
     // kLogits
     float c;                                               // log2(e) / tau
+    int in_place;                                          // H may be read where it lies
     const int32_t *labels, *order;                         // order[i]: the original row of real row i
-    const float *base;                                     // [M] reference of real row i
+    const int2 *info;                                      // [M] label and reference (as bits) of real row i
     float *picked;                                         // [rows] accumulator at the label
     float4 *part;                                          // [rows][chunks] reference, sum, sum of the rounded values
     int chunks, store;
@@ -87,32 +98,36 @@ __device__ __forceinline__ void wait_alive(bool &alive, unsigned long long *bar,
 #define PPO_TEST_WITHHOLD_XENT 0
 #endif
 
+template <int STAGES>
 struct Smem {
-    unsigned long long full[kStages], empty[kStages], tmem_full[2], tmem_empty[2];
+    unsigned long long full[STAGES], empty[STAGES], tmem_full[2], tmem_empty[2];
     uint32_t tmem_base;
 };
 
-// The pairs take tiles 0 .. n_whole in turn, whole. With `share` > 0 the other tiles, too few for all pairs, are cut along
-// the contraction: end to end they are n_rest * kbs blocks, of which pair c takes share, from c * share on (at most two
-// tiles), and join_kernel adds the parts up in the order of the pairs.
+// The workers (pairs, or blocks) take tiles 0 .. n_whole in turn, whole. With `share` > 0 the other tiles, too few for all, are
+// cut along the contraction: end to end they are n_rest * kbs blocks, of which worker c takes share, from c * share on (at
+// most two tiles), and join_kernel adds the parts up in the order of the workers.
 struct Plan {
     int m_tiles, n_tiles, n_whole, n_rest, share, kbs;
 };
 
-template <int PRODUCT>
-__device__ __forceinline__ Plan plan_of(const Args &a, int rows, int pairs)
+template <bool PAIR, int PRODUCT>
+__device__ __forceinline__ Plan plan_of(const Args &a, int rows, int workers)
 {
+    constexpr int kM = Shape<PAIR>::kM;
     Plan p;
-    p.m_tiles = ((PRODUCT == kWeight ? a.dim_m : rows) + kTile - 1) / kTile;
-    p.n_tiles = (a.dim_n + kTile - 1) / kTile;
+    p.m_tiles = ((PRODUCT == kWeight ? a.dim_m : rows) + kM - 1) / kM;
+    p.n_tiles = (a.dim_n + kBN - 1) / kBN;
     p.kbs = ((PRODUCT == kWeight ? rows : a.dim_k) + kBlockK - 1) / kBlockK;
     p.n_whole = p.m_tiles * p.n_tiles;
     p.n_rest = p.share = 0;
     if (PRODUCT == kWeight && rows == 0 && a.row0 > 0) p.n_whole = 0;      // nothing to add
     if (PRODUCT == kHidden) {
-        // cut when that saves each pair 24 blocks of the contraction or more
-        const int rest = p.n_whole % pairs, share = (int)(((int64_t)rest * p.kbs + pairs - 1) / pairs);
-        if (rest > 0 && p.kbs - share >= 24) {
+        // Cut when that saves each worker enough blocks of the contraction: 24, and two a tile for the joining and for the
+        // operands that tiles at different places of the contraction do not share through L2 (62 tiles left of 432 at 6912 x
+        // 4096 x 50304, 127 blocks saved: 2250 us cut, 2130 whole).
+        const int rest = p.n_whole % workers, share = (int)(((int64_t)rest * p.kbs + workers - 1) / workers);
+        if (rest > 0 && p.kbs - share >= 24 + 2 * rest) {
             p.n_rest = rest;
             p.n_whole -= rest;
             p.share = share;
@@ -123,20 +138,20 @@ __device__ __forceinline__ Plan plan_of(const Args &a, int rows, int pairs)
 
 struct Work {
     int u, kb0, kb1;      // tile, blocks of the contraction
-    int part;             // -1: whole; else which of the pair's parts
+    int part;             // -1: whole; else which of the worker's parts
     int u_next, r, r_end;
-    __device__ __forceinline__ void init(const Plan &p, int pair)
+    __device__ __forceinline__ void init(const Plan &p, int worker)
     {
-        u_next = pair;
-        r = min(pair * p.share, p.n_rest * p.kbs);
+        u_next = worker;
+        r = min(worker * p.share, p.n_rest * p.kbs);
         r_end = min(r + p.share, p.n_rest * p.kbs);
         part = -1;
     }
-    __device__ __forceinline__ bool next(const Plan &p, int pairs)
+    __device__ __forceinline__ bool next(const Plan &p, int workers)
     {
         if (u_next < p.n_whole) {
             u = u_next;
-            u_next += pairs;
+            u_next += workers;
             kb0 = 0;
             kb1 = p.kbs;
             return true;
@@ -187,22 +202,23 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi)
 __device__ __forceinline__ float low(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float high(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 
-// 32 values of a row, the half `h` of 64 columns, into the staging buffer; returns the sum of what was stored
-__device__ __forceinline__ float stage32(unsigned char *stage, int lane, int h, const float *v)
+// eight neighbouring columns of this lane's row, the c8-th of the buffer's 64
+__device__ __forceinline__ void stage8(unsigned char *stage, int c8, const uint32_t *w)
 {
-    unsigned char *row = stage + lane * 128;
-    float s = 0.f;
+    const int lane = threadIdx.x & 31;
+    *reinterpret_cast<uint4 *>(stage + lane * 128 + ((c8 ^ (lane & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// 64 columns
+__device__ __forceinline__ void stage64(unsigned char *stage, const float *v)
+{
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
+    for (int j = 0; j < 8; ++j) {
         uint32_t w[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            w[e] = pack2(v[j * 8 + e * 2], v[j * 8 + e * 2 + 1]);
-            s += low(w[e]) + high(w[e]);
-        }
-        *reinterpret_cast<uint4 *>(row + (((h * 4 + j) ^ (lane & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+        for (int e = 0; e < 4; ++e) w[e] = pack2(v[j * 8 + e * 2], v[j * 8 + e * 2 + 1]);
+        stage8(stage, j, w);
     }
-    return s;
 }
 
 // f * W[k .. k + N, label] added to N neighbouring elements of a row of dH; VK: W is stored [V, K]
@@ -235,13 +251,15 @@ __device__ __forceinline__ void add_label(const Args &a, float f, int label, int
     }
 }
 
-template <bool A_MN, bool B_MN, int PRODUCT>
+template <bool PAIR, bool A_MN, bool B_MN, int PRODUCT>
 __global__ void __launch_bounds__(kThreads, 1)
 product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_a_all,
                const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_out, const Args a)
 {
+    using S = Shape<PAIR>;
+    constexpr int kStages = S::kStages;
     extern __shared__ __align__(1024) unsigned char smem_raw[];
-    __shared__ Smem sm;
+    __shared__ Smem<kStages> sm;
     unsigned char *ring = smem_raw + ((1024u - (saddr(smem_raw) & 1023u)) & 1023u);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
@@ -251,53 +269,62 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         }
         for (int b = 0; b < 2; ++b) {
             barrier_init(&sm.tmem_full[b], 1);
-            barrier_init(&sm.tmem_empty[b], 2 * kEpiWarps);      // both blocks' epilogues
+            barrier_init(&sm.tmem_empty[b], (PAIR ? 2 : 1) * kEpiWarps);    // (of a pair: both blocks' epilogues)
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 0) tmem_alloc_all_pair(&sm.tmem_base);
+    if (warp == 0) {
+        if (PAIR) tmem_alloc_all_pair(&sm.tmem_base);
+        else tmem_alloc_all(&sm.tmem_base);
+    }
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
-    cluster_barrier();                                          // the other block's barriers are ready too
+    if (PAIR) cluster_barrier();                                // the other block's barriers are ready too
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem_base = sm.tmem_base;
     grid_dependents_may_launch();
     grid_dependency_wait();
-    const int rank = (int)cluster_rank(), pair = blockIdx.x / 2, pairs = gridDim.x / 2;
+    const int rank = PAIR ? (int)cluster_rank() : 0;
+    const int worker = PAIR ? blockIdx.x / 2 : blockIdx.x, workers = PAIR ? gridDim.x / 2 : gridDim.x;
     const int rows = rows_of(a);
-    const Plan plan = plan_of<PRODUCT>(a, rows, pairs);
+    const Plan plan = plan_of<PAIR, PRODUCT>(a, rows, workers);
     Work work;
-    work.init(plan, pair);
+    work.init(plan, worker);
 
     if (warp == 0) {
         if (lane == 0) {
-            // (all rows real: they have not been packed)
-            const CUtensorMap *ma = PRODUCT == kLogits && *a.n_real == a.M ? &map_a_all : &map_a;
+            // (where all rows are real they need not have been packed)
+            const CUtensorMap *ma = PRODUCT == kLogits && a.in_place && *a.n_real == a.M ? &map_a_all : &map_a;
             const int row0 = PRODUCT == kLogits ? a.row0 : 0;
             bool alive = true;
             uint32_t it = 0, s = 0, parity = 1;                 // (waiting for the phase before the first returns at once)
-            while (alive && work.next(plan, pairs)) {
+            while (alive && work.next(plan, workers)) {
                 const int2 t = tile_of(work.u, plan.m_tiles, plan.n_tiles, a.gm, a.gn);
-                const int m0 = t.x * kTile + rank * kBM, n0 = t.y * kTile + rank * kBM;
+                const int m0 = t.x * S::kM + rank * kBM, n0 = t.y * kBN + rank * S::kRowsB;
                 for (int kb = work.kb0; kb < work.kb1; ++kb, ++it) {
                     wait_alive(alive, &sm.empty[s], parity, a.status);
                     if (!alive) break;
-                    unsigned char *stage = ring + (size_t)s * kStage;
+                    unsigned char *stage = ring + (size_t)s * S::kStage;
                     // (bytes of the other block may be counted before they are announced: the phase cannot end
                     // without the leader's arrival)
-                    if (rank == 0) barrier_expect_tx(&sm.full[s], 2u * kStage);
-                    const uint32_t bar = leader_addr(&sm.full[s]);
+                    if (rank == 0) barrier_expect_tx(&sm.full[s], (PAIR ? 2u : 1u) * S::kStage);
+                    const uint32_t bar = PAIR ? leader_addr(&sm.full[s]) : saddr(&sm.full[s]);
+                    const auto load = [&](unsigned char *dst, const CUtensorMap *map, int x, int y) {
+                        if (PAIR) tma_load_2d_pair(dst, map, x, y, bar);
+                        else tma_load_2d(dst, map, x, y, &sm.full[s]);
+                    };
                     if (A_MN) {                                 // stored [k, m]: boxes of 64 (m) x 64 (k)
-                        tma_load_2d_pair(stage, ma, m0, kb * kBlockK, bar);
-                        tma_load_2d_pair(stage + kBox, ma, m0 + 64, kb * kBlockK, bar);
+                        load(stage, ma, m0, kb * kBlockK);
+                        load(stage + kBox, ma, m0 + 64, kb * kBlockK);
                     } else {                                    // stored [m, k]: one box of 64 (k) x 128 (m)
-                        tma_load_2d_pair(stage, ma, kb * kBlockK, row0 + m0, bar);
+                        load(stage, ma, kb * kBlockK, row0 + m0);
                     }
                     if (B_MN) {
-                        tma_load_2d_pair(stage + kHalf, &map_b, n0, kb * kBlockK, bar);
-                        tma_load_2d_pair(stage + kHalf + kBox, &map_b, n0 + 64, kb * kBlockK, bar);
+#pragma unroll
+                        for (int j = 0; j < S::kRowsB / 64; ++j)
+                            load(stage + S::kBytesA + j * kBox, &map_b, n0 + j * 64, kb * kBlockK);
                     } else {
-                        tma_load_2d_pair(stage + kHalf, &map_b, kb * kBlockK, n0, bar);
+                        load(stage + S::kBytesA, &map_b, kb * kBlockK, n0);
                     }
                     if (++s == kStages) { s = 0; parity ^= 1; }
                 }
@@ -313,33 +340,38 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         __syncwarp();
     } else if (warp == 1) {
         if (rank == 0 && lane == 0) {
-            constexpr uint32_t idesc = instr_desc(A_MN, B_MN, kTile, kTile);
+            constexpr uint32_t idesc = instr_desc(A_MN, B_MN, S::kM, kBN);
+            const auto announce = [](unsigned long long *bar) {
+                if (PAIR) commit_pair(bar);
+                else commit(bar);
+            };
             bool alive = true;
             uint32_t s = 0, s_parity = 0, tiles = 0;
-            while (alive && work.next(plan, pairs)) {
+            while (alive && work.next(plan, workers)) {
                 if (work.kb0 == work.kb1) continue;             // an empty contraction: the epilogue knows
                 const uint32_t buf = tiles & 1;
                 wait_alive(alive, &sm.tmem_empty[buf], ((tiles >> 1) & 1) ^ 1, a.status);
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                const uint32_t tmem_d = tmem_base + buf * kTile;
+                const uint32_t tmem_d = tmem_base + buf * kBN;
                 for (int kb = work.kb0; kb < work.kb1; ++kb) {
                     wait_alive(alive, &sm.full[s], s_parity, a.status);
                     if (!alive) break;
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                    const uint32_t a_addr = saddr(ring + (size_t)s * kStage), b_addr = a_addr + kHalf;
+                    const uint32_t a_addr = saddr(ring + (size_t)s * S::kStage), b_addr = a_addr + S::kBytesA;
 #pragma unroll
                     for (int kk = 0; kk < kBlockK / 16; ++kk) {
                         // K-major: 8-row groups 1024 bytes apart, 16 contraction elements are 32 bytes. MN-major: 64-wide
                         // boxes, 8 contraction rows 1024 bytes apart, 16 of them are 2048 bytes.
                         const uint64_t ad = A_MN ? smem_desc(a_addr + kk * 2048, kBox, 1024) : smem_desc(a_addr + kk * 32, 16, 1024);
                         const uint64_t bd = B_MN ? smem_desc(b_addr + kk * 2048, kBox, 1024) : smem_desc(b_addr + kk * 32, 16, 1024);
-                        mma_pair(tmem_d, ad, bd, idesc, kb > work.kb0 || kk ? 1u : 0u);
+                        if (PAIR) mma_pair(tmem_d, ad, bd, idesc, kb > work.kb0 || kk ? 1u : 0u);
+                        else mma(tmem_d, ad, bd, idesc, kb > work.kb0 || kk ? 1u : 0u);
                     }
-                    commit_pair(&sm.empty[s]);
+                    announce(&sm.empty[s]);
                     if (++s == kStages) { s = 0; s_parity ^= 1; }
                 }
                 if (alive && PPO_TEST_WITHHOLD_XENT != 1) {
-                    commit_pair(&sm.tmem_full[buf]);
+                    announce(&sm.tmem_full[buf]);
                     ++tiles;
                 }
             }
@@ -352,28 +384,29 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         __syncwarp();
     } else if (warp >= 4) {
         const int q = warp & 3, h = (warp - 4) >> 2;            // lanes 32 q .., columns 128 h .. of the tile
-        unsigned char *const stages = ring + (size_t)kStages * kStage + (warp - 4) * 2 * kStageOut;
-        unsigned char *stage = stages;
-        const uint32_t tmem_empty = leader_addr(&sm.tmem_empty[0]);
+        unsigned char *const stage = ring + (size_t)kStages * S::kStage + (warp - 4) * 2 * kStageOut;
+        const uint32_t tmem_empty = PAIR ? leader_addr(&sm.tmem_empty[0]) : saddr(&sm.tmem_empty[0]);
         const float nan = __int_as_float(0x7fffffff);
+        const bool first = a.row0 == 0, last = a.row0 + a.rows_max >= *a.n_real;
         bool alive = true;
         uint32_t tiles = 0;
-        while (work.next(plan, pairs)) {
+        while (work.next(plan, workers)) {
             const int2 t = tile_of(work.u, plan.m_tiles, plan.n_tiles, a.gm, a.gn);
-            const int m_warp = t.x * kTile + rank * kBM + q * 32, n = t.y * kTile + h * 128;
+            const int m_warp = t.x * S::kM + rank * kBM + q * 32, n = t.y * kBN + h * 128;
             const int row = m_warp + lane;
             const bool empty = work.kb0 == work.kb1;
             const uint32_t buf = tiles & 1;
-            const uint32_t taddr = tmem_base + buf * kTile + h * 128 + ((uint32_t)(q * 32) << 16);
+            const uint32_t taddr = tmem_base + buf * kBN + h * 128 + ((uint32_t)(q * 32) << 16);
             bool ok = false;
             int label = -1, out_row = -1;
-            float base = 0.f;
+            float ref = 0.f;
             float2 scale = make_float2(0.f, 0.f);
             if (PRODUCT == kLogits) {
                 ok = row < rows;
                 if (ok) {
-                    label = a.labels[a.order[a.row0 + row]] - n;
-                    base = a.base[a.row0 + row];
+                    const int2 info = a.info[a.row0 + row];
+                    label = (int)((unsigned)info.x - (unsigned)n);
+                    ref = __int_as_float(info.y);
                 }
             } else if (PRODUCT == kHidden) {
                 ok = row < rows;
@@ -391,138 +424,167 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                 alive = __all_sync(0xffffffffu, alive);
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             }
-            // this warp's read of 32 columns; after the tile's last one the accumulator is released
-            const auto read = [&](int cc, bool last, float *v) {
-                if (empty) {
+            // 64 columns of this lane's row
+            const auto read = [&](int half, float (&v)[64]) {
+                if (empty || !alive) {
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) v[j] = 0.f;
+                    for (int j = 0; j < 64; ++j) v[j] = alive ? 0.f : nan;
                     return;
                 }
-                uint32_t r[32];
+                uint32_t r0[32], r1[32];
                 __syncwarp();
-                tmem_ld32(taddr + cc * 32, r);
+                tmem_ld32(taddr + half * 64, r0);
+                tmem_ld32(taddr + half * 64 + 32, r1);
                 asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-                if (last) {
-                    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-                    __syncwarp();
-                    barrier_arrive_cluster_if(tmem_empty + buf * 8, lane == 0 && alive && PPO_TEST_WITHHOLD_XENT != 2);
-                }
 #pragma unroll
-                for (int j = 0; j < 32; ++j) v[j] = alive ? __uint_as_float(r[j]) : nan;
-            };
-            // 64 columns of the staging buffer, from column c64 of the warp's half
-            const auto send = [&](int c64, bool bulk) {
-                if (bulk) {
-                    fence_async_proxy();
-                    __syncwarp();
-                    if (lane == 0) tma_store_2d(&map_out, n + c64, m_warp, stage);
-                } else {
-                    __syncwarp();
-                    store_rows(stage, a.out, a.ldo, out_row, n + c64, a.dim_n);
-                    __syncwarp();
+                for (int j = 0; j < 32; ++j) {
+                    v[j] = __uint_as_float(r0[j]);
+                    v[j + 32] = __uint_as_float(r1[j]);
                 }
             };
-            // the other staging buffer, whose last copy has read it
+            const auto release = [&] {                          // nothing of the accumulator is needed any more
+                if (empty) return;
+                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                __syncwarp();
+                const bool arrive = lane == 0 && alive && PPO_TEST_WITHHOLD_XENT != 2;
+                if (PAIR) barrier_arrive_cluster_if(tmem_empty + buf * 8, arrive);
+                else if (arrive) barrier_arrive(&sm.tmem_empty[buf]);
+            };
+            // the staging buffers, whose last copies have read them
             const auto reuse = [&] {
-                stage = stage == stages ? stages + kStageOut : stages;
-                if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+                if (lane == 0) tma_store_wait_read();
+                __syncwarp();
+            };
+            // both buffers, 128 columns, by bulk copies as far as they may go
+            const auto send = [&](int bulk_cols, bool rows_here) {
+                fence_async_proxy();
+                __syncwarp();
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    const int col = n + half * 64;
+                    if (col >= a.dim_n) break;
+                    if (col + 64 <= bulk_cols) {
+                        if (lane == 0 && rows_here) tma_store_2d(&map_out, col, m_warp, stage + half * kStageOut);
+                    } else {
+                        store_rows(stage + half * kStageOut, a.out, a.ldo, out_row, col, a.dim_n);
+                    }
+                }
                 __syncwarp();
             };
 
             if (PRODUCT == kLogits) {
-                float m = kNoRef;
+                // U with the row's reference. Where a lane's largest value has left the window, which is looked at when all
+                // 128 are there, once more with another one.
+                float s = 0.f, rounded = 0.f, c = a.c;
+                const bool plain = __all_sync(0xffffffffu, ok) && n + 128 <= a.dim_n;
+                if (a.store) reuse();
 #pragma unroll 1
-                for (int cc = 0; cc < 4; ++cc) {
-                    float v[32];
-                    read(cc, false, v);
-                    const int left = a.dim_n - n - cc * 32;
-                    if (left >= 32) {
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) m = fmaxf(m, v[j]);
-                    } else {
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) m = j < left ? fmaxf(m, v[j]) : m;
-                    }
-                }
-                const float ref = base + 128.f * rintf((fmaxf(m * a.c, -1e9f) - base) * (1.f / 128.f));
-                float s = 0.f, rounded = 0.f;
+                for (int turn = 0; turn < 2; ++turn) {
+                    float top = 0.f;
+                    s = rounded = 0.f;
 #pragma unroll 1
-                for (int cc = 0; cc < 4; ++cc) {
-                    float v[32];
-                    read(cc, cc == 3, v);
-                    if ((unsigned)(label - cc * 32) < 32u) {
+                    for (int half = 0; half < 2; ++half) {
+                        float v[64];
+                        read(half, v);
+                        if (turn == 0 && (unsigned)(label - half * 64) < 64u) {
 #pragma unroll
-                        for (int j = 0; j < 32; ++j)
-                            if (label - cc * 32 == j) a.picked[row] = v[j];
-                    }
-                    const int left = ok ? a.dim_n - n - cc * 32 : 0;
+                            for (int j = 0; j < 64; ++j)
+                                if (label - half * 64 == j) a.picked[row] = v[j];
+                        }
+                        const int left = plain ? 64 : ok ? a.dim_n - n - half * 64 : 0;
+                        float s1 = 0.f, r1 = 0.f;
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) {
-                        const float e = ex2(fmaf(v[j], a.c, -ref));
-                        v[j] = j < left ? e : 0.f;
-                        s += v[j];
+                        for (int j = 0; j < 8; ++j) {
+                            uint32_t w[4];
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                const int i = j * 8 + e * 2;
+                                float x = ex2(fmaf(v[i], c, -ref)), y = ex2(fmaf(v[i + 1], c, -ref));
+                                if (!plain) {
+                                    x = i < left ? x : 0.f;
+                                    y = i + 1 < left ? y : 0.f;
+                                }
+                                top = fmaxf(top, fmaxf(x, y));
+                                s += x;
+                                s1 += y;
+                                w[e] = pack2(x, y);
+                                rounded += low(w[e]);
+                                r1 += high(w[e]);
+                            }
+                            if (a.store) stage8(stage + half * kStageOut, j, w);
+                        }
+                        s += s1;
+                        rounded += r1;
                     }
-                    if (a.store) {
-                        if ((cc & 1) == 0) reuse();
-                        rounded += stage32(stage, lane, cc & 1, v);
-                        if ((cc & 1) && n + (cc - 1) * 32 < a.dim_n) send((cc - 1) * 32, true);
+                    // (a lane without a column has 0 everywhere)
+                    const bool out = ok && n < a.dim_n && !(top >= kLeast && top <= kMost);
+                    if (turn == 1 || !__any_sync(0xffffffffu, out)) break;
+                    float m = kNoRef;
+#pragma unroll 1
+                    for (int half = 0; half < 2; ++half) {
+                        float v[64];
+                        read(half, v);
+                        const int left = a.dim_n - n - half * 64;
+#pragma unroll
+                        for (int j = 0; j < 64; ++j) m = j < left ? fmaxf(m, v[j]) : m;
                     }
+                    if (out) ref += 128.f * rintf((fmaxf(m * c, -1e9f) - ref) * (1.f / 128.f));
                 }
+                release();
+                if (a.store) send(0x7fffffff, true);
                 if (ok && n < a.dim_n) a.part[(size_t)row * a.chunks + n / kChunk] = make_float4(ref, s, rounded, 0.f);
             } else if (PRODUCT == kHidden) {
-                // (four columns of 256 rows follow one another in scratch: a warp writes 512 bytes at a time)
-                float4 *part = reinterpret_cast<float4 *>(a.scratch + (size_t)(pair * 2 + max(work.part, 0)) * kTileFloats) +
-                               h * 32 * kTile + rank * kBM + q * 32 + lane;
+                // (four columns of a tile's rows follow one another in scratch: a warp writes 512 bytes at a time)
+                float4 *part = reinterpret_cast<float4 *>(a.scratch + (size_t)(worker * 2 + max(work.part, 0)) * S::kTileFloats) +
+                               h * 32 * S::kM + rank * kBM + q * 32 + lane;
 #pragma unroll 1
-                for (int cc = 0; cc < 4; ++cc) {
-                    float v[32];
-                    read(cc, cc == 3, v);
+                for (int half = 0; half < 2; ++half) {
+                    float v[64];
+                    read(half, v);
+                    if (half == 1) release();
                     if (work.part >= 0) {
                         if (!ok) continue;
 #pragma unroll
-                        for (int j = 0; j < 8; ++j)
-                            part[(cc * 8 + j) * kTile] = make_float4(v[j * 4], v[j * 4 + 1], v[j * 4 + 2], v[j * 4 + 3]);
+                        for (int j = 0; j < 16; ++j)
+                            part[(half * 16 + j) * S::kM] = make_float4(v[j * 4], v[j * 4 + 1], v[j * 4 + 2], v[j * 4 + 3]);
                         continue;
                     }
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) v[j] *= scale.x;
-                    if (label >= 0) add_label<B_MN, 32>(a, scale.y, label, n + cc * 32, v);
-                    stage32(stage, lane, cc & 1, v);
-                    if ((cc & 1) && n + (cc - 1) * 32 < a.dim_n) send((cc - 1) * 32, false);
-                }
-            } else {
-                const bool first = a.row0 == 0, last = a.row0 + a.rows_max >= *a.n_real;
-                float4 *sum = reinterpret_cast<float4 *>(a.scratch + ((size_t)t.x * plan.n_tiles + t.y) * kTileFloats) +
-                              h * 32 * kTile + rank * kBM + q * 32 + lane;
-#pragma unroll 1
-                for (int cc = 0; cc < 4; ++cc) {
-                    float4 old[8];
-                    if (!first) {
+                    for (int j = 0; j < 64; ++j) v[j] *= scale.x;
+                    if (label >= 0) {
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) old[j] = sum[(cc * 8 + j) * kTile];
+                        for (int j = 0; j < 64; j += 16) add_label<B_MN, 16>(a, scale.y, label, n + half * 64 + j, v + j);
                     }
-                    float v[32];
-                    read(cc, cc == 3, v);
+                    stage64(stage + half * kStageOut, v);
+                }
+                if (work.part < 0) send(0, true);
+            } else {
+                float4 *sum = reinterpret_cast<float4 *>(a.scratch + ((size_t)t.x * plan.n_tiles + t.y) * S::kTileFloats) +
+                              h * 32 * S::kM + rank * kBM + q * 32 + lane;
+                if (last) reuse();
+#pragma unroll 1
+                for (int half = 0; half < 2; ++half) {
+                    float v[64];
+                    read(half, v);
+                    if (half == 1) release();
                     if (!first) {
+                        float4 old[16];
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) {
+                        for (int j = 0; j < 16; ++j) old[j] = sum[(half * 16 + j) * S::kM];
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) {
                             v[j * 4] += old[j].x; v[j * 4 + 1] += old[j].y; v[j * 4 + 2] += old[j].z; v[j * 4 + 3] += old[j].w;
                         }
                     }
-                    if (!last) {
+                    if (last) {
+                        stage64(stage + half * kStageOut, v);
+                    } else {
 #pragma unroll
-                        for (int j = 0; j < 8; ++j)
-                            sum[(cc * 8 + j) * kTile] = make_float4(v[j * 4], v[j * 4 + 1], v[j * 4 + 2], v[j * 4 + 3]);
-                        continue;
-                    }
-                    if ((cc & 1) == 0) reuse();
-                    stage32(stage, lane, cc & 1, v);
-                    const int col = n + (cc - 1) * 32;
-                    if ((cc & 1) && col < a.dim_n) {
-                        const bool bulk = col + 64 <= a.bulk_cols;
-                        if (!bulk || m_warp < a.dim_m) send((cc - 1) * 32, bulk);
+                        for (int j = 0; j < 16; ++j)
+                            sum[(half * 16 + j) * S::kM] = make_float4(v[j * 4], v[j * 4 + 1], v[j * 4 + 2], v[j * 4 + 3]);
                     }
                 }
+                if (last) send(a.bulk_cols, m_warp < a.dim_m);
             }
             if (!empty) ++tiles;
         }
@@ -530,30 +592,33 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     }
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
-    cluster_barrier();                                          // neither block ends while the other may reach into it
+    if (PAIR) cluster_barrier();                                // neither block ends while the other may reach into it
     if (warp == 0) {
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        tmem_free_all_pair(tmem_base);
+        if (PAIR) tmem_free_all_pair(tmem_base);
+        else tmem_free_all(tmem_base);
     }
 }
 
 // The tiles of dH that were cut along the vocabulary: a block adds up 32 rows x 64 columns over the pairs that hold parts of
 // them, in the order of the contraction, and turns them in shared memory so that rows leave in runs.
-constexpr int kJoinThreads = 256, kJoinBlocks = (kTile / 32) * (kTile / 64);
-template <bool VK>
+constexpr int kJoinThreads = 256;
+template <bool PAIR> constexpr int join_blocks() { return (Shape<PAIR>::kM / 32) * (kBN / 64); }
+template <bool PAIR, bool VK>
 __global__ void __launch_bounds__(kJoinThreads)
-join_kernel(const Args a, int pairs)
+join_kernel(const Args a, int workers)
 {
+    constexpr int kM = Shape<PAIR>::kM, kTileFloats = Shape<PAIR>::kTileFloats, kBlocks = (kM / 32) * (kBN / 64);
     __shared__ float4 turn[32][17];
     grid_dependents_may_launch();
     grid_dependency_wait();
     const int rows = rows_of(a);
-    const Plan p = plan_of<kHidden>(a, rows, pairs);
-    const int rest = blockIdx.x / kJoinBlocks, part_of = blockIdx.x % kJoinBlocks;
+    const Plan p = plan_of<PAIR, kHidden>(a, rows, workers);
+    const int rest = blockIdx.x / kBlocks, part_of = blockIdx.x % kBlocks;
     if (rest >= p.n_rest) return;
-    const int row0 = (part_of % (kTile / 32)) * 32, j0 = part_of / (kTile / 32) * 16;
+    const int row0 = (part_of % (kM / 32)) * 32, j0 = part_of / (kM / 32) * 16;
     const int2 t = tile_of(p.n_whole + rest, p.m_tiles, p.n_tiles, a.gm, a.gn);
-    const int m0 = t.x * kTile + row0, n0 = t.y * kTile + j0 * 4;
+    const int m0 = t.x * kM + row0, n0 = t.y * kBN + j0 * 4;
     if (m0 >= rows || n0 >= a.dim_n) return;
     const int first = (int)((int64_t)rest * p.kbs / p.share), last = (int)(((int64_t)(rest + 1) * p.kbs - 1) / p.share);
     const int lane = threadIdx.x & 31, jj = threadIdx.x >> 5;
@@ -561,9 +626,9 @@ join_kernel(const Args a, int pairs)
     v[0] = v[1] = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
     for (int c = first; c <= last; ++c) {
-        const int part = rest - (int)((int64_t)c * p.share / p.kbs);     // the pair's first or second tile
+        const int part = rest - (int)((int64_t)c * p.share / p.kbs);     // the worker's first or second tile
         const float4 *from = reinterpret_cast<const float4 *>(a.scratch + (size_t)(c * 2 + part) * kTileFloats) + row0 + lane;
-        const float4 x = from[(j0 + jj) * kTile], y = from[(j0 + jj + 8) * kTile];
+        const float4 x = from[(j0 + jj) * kM], y = from[(j0 + jj + 8) * kM];
         v[0].x += x.x; v[0].y += x.y; v[0].z += x.z; v[0].w += x.w;
         v[1].x += y.x; v[1].y += y.y; v[1].z += y.z; v[1].w += y.w;
     }
@@ -605,8 +670,9 @@ struct RowArgs {
     int64_t ldw;
     int vk;
     float *w_mean;                                              // [K] mean of kSample columns of W
-    float *base;                                                // [M] reference of real row i
-    __nv_bfloat16 *packed;                                      // [M, Kp] (written when some row is left out)
+    int2 *info;                                                 // [M] label and reference of real row i
+    int in_place;                                               // product 1 reads H where it lies when all rows are real
+    __nv_bfloat16 *packed;                                      // [M, Kp] real rows (unless they can be read in place)
     __nv_bfloat16 *scaled;                                      // [rows_max, Kp] a H; null: no gradients
     __nv_bfloat16 *u;                                           // [rows_max, Vp]
     int64_t Vp;
@@ -733,7 +799,7 @@ order_kernel(const RowArgs a)
 }
 
 constexpr int kRowThreads = 256;
-// real rows: their reference, and a packed copy where some rows are left out; those get their zeros
+// real rows: label and reference, and a packed copy where they are not read in place; the rows left out get their zeros
 __global__ void __launch_bounds__(kRowThreads)
 pack_kernel(const RowArgs a)
 {
@@ -753,17 +819,18 @@ pack_kernel(const RowArgs a)
     }
     const __nv_bfloat16 *from = a.H + (int64_t)row * a.ldh;
     __nv_bfloat16 *to = a.packed + (int64_t)i * a.Kp;
+    const bool pack = n < a.M || !a.in_place;
     float s = 0.f;
     for (int k = threadIdx.x * 8; k < a.K; k += kRowThreads * 8) {
         if (k + 8 <= a.K) {
             const uint4 v = *reinterpret_cast<const uint4 *>(from + k);
-            if (n < a.M) *reinterpret_cast<uint4 *>(to + k) = v;
+            if (pack) *reinterpret_cast<uint4 *>(to + k) = v;
             const float4 p = *reinterpret_cast<const float4 *>(a.w_mean + k), q = *reinterpret_cast<const float4 *>(a.w_mean + k + 4);
             s = fmaf(low(v.x), p.x, s); s = fmaf(high(v.x), p.y, s); s = fmaf(low(v.y), p.z, s); s = fmaf(high(v.y), p.w, s);
             s = fmaf(low(v.z), q.x, s); s = fmaf(high(v.z), q.y, s); s = fmaf(low(v.w), q.z, s); s = fmaf(high(v.w), q.w, s);
         } else {
             for (int e = k; e < a.K; ++e) {
-                if (n < a.M) to[e] = from[e];
+                if (pack) to[e] = from[e];
                 s = fmaf(__bfloat162float(from[e]), a.w_mean[e], s);
             }
         }
@@ -777,7 +844,7 @@ pack_kernel(const RowArgs a)
         for (int w = 0; w < kRowThreads / 32; ++w) s += red[w];
         // the middle of the window; whole numbers, so that y - reference loses nothing that y does not
         s = rintf(s * a.c) + 32.f;
-        a.base[i] = fabsf(s) < 1e9f ? s : 0.f;
+        a.info[i] = make_int2(a.labels[row], __float_as_int(fabsf(s) < 1e9f ? s : 0.f));
     }
 }
 
@@ -895,10 +962,12 @@ loss_kernel(const RowArgs a)
 }
 
 // ---------------------------------------------------------------- host side
+constexpr int kPieceRows = 256;                                 // a piece is a multiple of this
+
 struct Layout {
     int pieces, rows_max, chunks, Kp;
     int64_t Vp;
-    size_t n_real, order, base, w_mean, picked, row_scale, part, packed, scaled, u, parts, sums, bytes;
+    size_t n_real, order, info, w_mean, picked, row_scale, part, packed, scaled, u, parts, sums, bytes;
 };
 
 // Pieces of at most 8192 rows by default: at V = 50304 that is 824 MB of U, and the sums of dW, read and written once a
@@ -909,11 +978,12 @@ static Layout layout_of(int64_t M, int64_t K, int64_t V, int64_t piece_rows, boo
     const int64_t most = piece_rows > 0 ? piece_rows : 8192;
     l.pieces = (int)((M + most - 1) / most);
     const int64_t even = (M + l.pieces - 1) / l.pieces;
-    l.rows_max = (int)((even + kTile - 1) / kTile * kTile);
+    l.rows_max = (int)((even + kPieceRows - 1) / kPieceRows * kPieceRows);
     l.pieces = (int)((M + l.rows_max - 1) / l.rows_max);
     l.chunks = (int)((V + kChunk - 1) / kChunk);
-    l.Kp = (int)((K + 7) / 8 * 8);
-    l.Vp = (V + 7) / 8 * 8;
+    // (rows of whole 128-byte lines: a row of a box that begins inside a line costs two requests)
+    l.Kp = (int)((K + 63) / 64 * 64);
+    l.Vp = (V + 63) / 64 * 64;
     size_t at = 0;
     const auto take = [&](size_t n) {
         const size_t here = at;
@@ -924,7 +994,7 @@ static Layout layout_of(int64_t M, int64_t K, int64_t V, int64_t piece_rows, boo
     const size_t rows = (size_t)l.rows_max;
     l.n_real = take(4);
     l.order = take((size_t)M * 4);
-    l.base = take((size_t)M * 4);
+    l.info = take((size_t)M * sizeof(int2));
     l.w_mean = take((size_t)K * 4);
     l.picked = take(rows * 4);
     l.row_scale = take(rows * sizeof(float2));
@@ -932,49 +1002,77 @@ static Layout layout_of(int64_t M, int64_t K, int64_t V, int64_t piece_rows, boo
     l.packed = take((size_t)M * l.Kp * 2);
     l.scaled = take(dw ? rows * l.Kp * 2 : 0);
     l.u = take(grad ? rows * (size_t)l.Vp * 2 : 0);
-    l.parts = take(dh ? (size_t)kMaxPairs * 2 * kTileFloats * 4 : 0);
-    const size_t tiles = (size_t)((K + kTile - 1) / kTile) * (size_t)((V + kTile - 1) / kTile);
-    l.sums = take(dw && l.pieces > 1 ? tiles * kTileFloats * 4 : 0);
+    l.parts = take(dh ? (size_t)kMaxSms * 2 * Shape<false>::kTileFloats * 4 : 0);
+    const size_t tiles = (size_t)((K + kBN - 1) / kBN) * (size_t)((V + kBN - 1) / kBN);
+    l.sums = take(dw && l.pieces > 1 ? tiles * Shape<true>::kTileFloats * 4 : 0);
     l.bytes = at;
     return l;
 }
 
-static int pairs_of_device(int *pairs)
+static int sms_of_device(int *sms)
 {
-    int dev = 0, sms = 148;
+    int dev = 0;
+    *sms = 148;
     PPO_RETURN_IF_CUDA(cudaGetDevice(&dev));
-    PPO_RETURN_IF_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
-    *pairs = sms / 2 < kMaxPairs ? sms / 2 : kMaxPairs;
+    PPO_RETURN_IF_CUDA(cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev));
+    if (*sms > kMaxSms) *sms = kMaxSms;
     return PPO_OK;
 }
 
-template <bool A_MN, bool B_MN, int PRODUCT>
-static int launch_product(const CUtensorMap &ma, const CUtensorMap &ma_all, const CUtensorMap &mb, const CUtensorMap &mo, Args a,
-                          int pairs, cudaStream_t s)
+template <bool PAIR, bool A_MN, bool B_MN, int PRODUCT>
+static int launch_product(const CUtensorMap &ma, const CUtensorMap &ma_all, const CUtensorMap &mb, const CUtensorMap &mo, const Args &a,
+                          int sms, cudaStream_t s)
 {
-    auto kern = product_kernel<A_MN, B_MN, PRODUCT>;
-    PPO_RETURN_IF_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem));
+    auto kern = product_kernel<PAIR, A_MN, B_MN, PRODUCT>;
+    PPO_RETURN_IF_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<PAIR>::kSmem));
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(2 * pairs));
+    cfg.gridDim = dim3((unsigned)(PAIR ? sms / 2 * 2 : sms));
     cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = kSmem;
+    cfg.dynamicSmemBytes = Shape<PAIR>::kSmem;
     cfg.stream = s;
     cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = 2;
-    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = 2;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 2;
+    cfg.numAttrs = PAIR ? 2 : 1;
     cudaError_t e = cudaLaunchKernelEx(&cfg, kern, ma, ma_all, mb, mo, a);
-    if (e != cudaSuccess) {   // attribute not accepted in this context: ordinary launch (same results, no overlap)
+    if (e != cudaSuccess) {   // the first attribute is not accepted in this context: ordinary launch (same results, no overlap)
         (void)cudaGetLastError();
-        cfg.numAttrs = 1;
+        cfg.attrs = attr + 1;
+        cfg.numAttrs = PAIR ? 1 : 0;
         e = cudaLaunchKernelEx(&cfg, kern, ma, ma_all, mb, mo, a);
     }
     PPO_RETURN_IF_CUDA(e);
     return PPO_OK;
+}
+
+// the three products of a piece
+struct Maps {
+    CUtensorMap packed, h, w1, w2, u_out, u2, u3, scaled, dw;
+};
+
+template <bool PAIR>
+static int launch_piece(const Maps &m, const RowArgs &r, const Args &a1, const Args &a2, const Args &a3, bool vk, bool dh, bool dw, int sms,
+                        cudaStream_t s)
+{
+    int rc = vk ? launch_product<PAIR, false, false, kLogits>(m.packed, m.h, m.w1, m.u_out, a1, sms, s)
+                : launch_product<PAIR, false, true, kLogits>(m.packed, m.h, m.w1, m.u_out, a1, sms, s);
+    if (rc) return rc;
+    PPO_RETURN_IF_CUDA(launch_dependent(row_kernel, dim3((unsigned)r.rows_max), dim3(kRowThreads), 0, s, r));
+    if (dh) {
+        rc = vk ? launch_product<PAIR, false, true, kHidden>(m.u2, m.u2, m.w2, m.u2, a2, sms, s)
+                : launch_product<PAIR, false, false, kHidden>(m.u2, m.u2, m.w2, m.u2, a2, sms, s);
+        if (rc) return rc;
+        const int workers = PAIR ? sms / 2 : sms;
+        PPO_RETURN_IF_CUDA(launch_dependent(vk ? join_kernel<PAIR, true> : join_kernel<PAIR, false>,
+                                            dim3((unsigned)((workers - 1) * join_blocks<PAIR>())), dim3(kJoinThreads), 0, s, a2, workers));
+    }
+    if (!dw) return PPO_OK;
+    return vk ? launch_product<PAIR, true, true, kWeight>(m.u3, m.u3, m.scaled, m.dw, a3, sms, s)
+              : launch_product<PAIR, true, true, kWeight>(m.scaled, m.scaled, m.u3, m.dw, a3, sms, s);
 }
 
 constexpr int64_t kLimit = ((int64_t)1 << 31) - 16384;
@@ -1020,12 +1118,12 @@ extern "C" int ppo_lmhead_xent(const void *H, int64_t ldh, const void *W, int64_
         if (dW) PPO_RETURN_IF_CUDA(cudaMemset2DAsync(dW, (size_t)lddw * 2, 0, (size_t)w_inner * 2, (size_t)w_outer, s));
         return PPO_OK;
     }
-    int pairs = 0;
-    int rc = pairs_of_device(&pairs);
+    int sms = 0;
+    int rc = sms_of_device(&sms);
     if (rc) return rc;
     const Layout l = layout_of(M, K, V, piece_rows, dH != nullptr, dW != nullptr);
     unsigned char *mem = reinterpret_cast<unsigned char *>(scratch);
-    const bool grad = dH || dW;
+    const bool grad = dH || dW, pair = M > kBM;
 
     RowArgs r = {};
     r.H = reinterpret_cast<const __nv_bfloat16 *>(H);
@@ -1036,7 +1134,8 @@ extern "C" int ppo_lmhead_xent(const void *H, int64_t ldh, const void *W, int64_
     r.order = reinterpret_cast<int32_t *>(mem + l.order);
     r.W = reinterpret_cast<const __nv_bfloat16 *>(W); r.ldw = ldw; r.vk = vk;
     r.w_mean = reinterpret_cast<float *>(mem + l.w_mean);
-    r.base = reinterpret_cast<float *>(mem + l.base);
+    r.info = reinterpret_cast<int2 *>(mem + l.info);
+    r.in_place = ldh % 64 == 0 && reinterpret_cast<uintptr_t>(H) % 128 == 0;
     r.packed = reinterpret_cast<__nv_bfloat16 *>(mem + l.packed);
     r.scaled = dW ? reinterpret_cast<__nv_bfloat16 *>(mem + l.scaled) : nullptr;
     r.u = grad ? reinterpret_cast<__nv_bfloat16 *>(mem + l.u) : nullptr;
@@ -1048,23 +1147,22 @@ extern "C" int ppo_lmhead_xent(const void *H, int64_t ldh, const void *W, int64_
     r.loss = loss; r.nll = nll; r.lse = lse; r.dH = reinterpret_cast<__nv_bfloat16 *>(dH);
     r.status = status;
 
-    CUtensorMap m_packed, m_h, m_w1, m_w2, m_u1, m_u2, m_u3, m_scaled, m_dw = {};
-    if ((rc = make_map_pitch(&m_packed, r.packed, (uint64_t)K, (uint64_t)M, (uint64_t)l.Kp, kBM))) return rc;
-    if ((rc = make_map_pitch(&m_h, H, (uint64_t)K, (uint64_t)M, (uint64_t)ldh, kBM))) return rc;
+    Maps m = {};
+    const int rows_b = pair ? kBN / 2 : kBN;                    // a block's share of B, stored by rows
+    if ((rc = make_map_pitch(&m.packed, r.packed, (uint64_t)K, (uint64_t)M, (uint64_t)l.Kp, kBM))) return rc;
+    if ((rc = make_map_pitch(&m.h, H, (uint64_t)K, (uint64_t)M, (uint64_t)ldh, kBM))) return rc;
     // product 1 takes W with the vocabulary as the result's columns, product 2 with the hidden size
-    if ((rc = make_map_pitch(&m_w1, W, (uint64_t)w_inner, (uint64_t)w_outer, (uint64_t)ldw, vk ? kBM : 64))) return rc;
-    if ((rc = make_map_pitch(&m_w2, W, (uint64_t)w_inner, (uint64_t)w_outer, (uint64_t)ldw, vk ? 64 : kBM))) return rc;
+    if ((rc = make_map_pitch(&m.w1, W, (uint64_t)w_inner, (uint64_t)w_outer, (uint64_t)ldw, vk ? rows_b : 64))) return rc;
+    if ((rc = make_map_pitch(&m.w2, W, (uint64_t)w_inner, (uint64_t)w_outer, (uint64_t)ldw, vk ? 64 : rows_b))) return rc;
     if (grad) {
-        if ((rc = make_map_pitch(&m_u1, r.u, (uint64_t)V, (uint64_t)l.rows_max, (uint64_t)l.Vp, 32))) return rc;   // stores
-        if ((rc = make_map_pitch(&m_u2, r.u, (uint64_t)V, (uint64_t)l.rows_max, (uint64_t)l.Vp, kBM))) return rc;
-        if ((rc = make_map_pitch(&m_u3, r.u, (uint64_t)V, (uint64_t)l.rows_max, (uint64_t)l.Vp, 64))) return rc;
-    } else {
-        m_u1 = m_h;
+        if ((rc = make_map_pitch(&m.u_out, r.u, (uint64_t)V, (uint64_t)l.rows_max, (uint64_t)l.Vp, 32))) return rc;
+        if ((rc = make_map_pitch(&m.u2, r.u, (uint64_t)V, (uint64_t)l.rows_max, (uint64_t)l.Vp, kBM))) return rc;
+        if ((rc = make_map_pitch(&m.u3, r.u, (uint64_t)V, (uint64_t)l.rows_max, (uint64_t)l.Vp, 64))) return rc;
     }
 
     Args a = {};
     a.n_real = r.n_real; a.M = (int)M; a.rows_max = l.rows_max; a.status = status;
-    a.c = r.c; a.labels = labels; a.order = r.order; a.base = r.base; a.picked = r.picked; a.part = r.part; a.chunks = l.chunks; a.store = grad;
+    a.c = r.c; a.labels = labels; a.order = r.order; a.info = r.info; a.in_place = r.in_place; a.picked = r.picked; a.part = r.part; a.chunks = l.chunks; a.store = grad;
     a.row_scale = r.row_scale;
     Args a1 = a, a2 = a, a3 = a;
     a1.dim_m = l.rows_max; a1.dim_n = (int)V; a1.dim_k = (int)K; a1.gm = 9; a1.gn = 8;
@@ -1075,11 +1173,11 @@ extern "C" int ppo_lmhead_xent(const void *H, int64_t ldh, const void *W, int64_
     a3.out = reinterpret_cast<__nv_bfloat16 *>(dW); a3.ldo = lddw;
     a3.scratch = reinterpret_cast<float *>(mem + l.sums);
     if (dW) {
-        if ((rc = make_map_pitch(&m_scaled, r.scaled, (uint64_t)K, (uint64_t)l.rows_max, (uint64_t)l.Kp, 64))) return rc;
+        if ((rc = make_map_pitch(&m.scaled, r.scaled, (uint64_t)K, (uint64_t)l.rows_max, (uint64_t)l.Kp, 64))) return rc;
         if (reinterpret_cast<uintptr_t>(dW) % 16 == 0 && lddw % 8 == 0 && lddw < ((int64_t)1 << 38)) {
             // (a box is clipped in units of 16 bytes: it would write zeros behind a row whose end is none)
             a3.bulk_cols = w_inner % 8 ? (int)w_inner : 0x7fffffff;
-            if ((rc = make_map_pitch(&m_dw, dW, (uint64_t)w_inner, (uint64_t)w_outer, (uint64_t)lddw, 32))) return rc;
+            if ((rc = make_map_pitch(&m.dw, dW, (uint64_t)w_inner, (uint64_t)w_outer, (uint64_t)lddw, 32))) return rc;
         }
     }
 
@@ -1089,22 +1187,9 @@ extern "C" int ppo_lmhead_xent(const void *H, int64_t ldh, const void *W, int64_
     PPO_RETURN_IF_CUDA(launch_dependent(pack_kernel, dim3((unsigned)M), dim3(kRowThreads), 0, s, r));
     for (int p = 0; p < l.pieces; ++p) {
         r.row0 = a1.row0 = a2.row0 = a3.row0 = p * l.rows_max;
-        rc = vk ? launch_product<false, false, kLogits>(m_packed, m_h, m_w1, m_u1, a1, pairs, s)
-                : launch_product<false, true, kLogits>(m_packed, m_h, m_w1, m_u1, a1, pairs, s);
+        rc = pair ? launch_piece<true>(m, r, a1, a2, a3, vk, dH != nullptr, dW != nullptr, sms, s)
+                  : launch_piece<false>(m, r, a1, a2, a3, vk, dH != nullptr, dW != nullptr, sms, s);
         if (rc) return rc;
-        PPO_RETURN_IF_CUDA(launch_dependent(row_kernel, dim3((unsigned)l.rows_max), dim3(kRowThreads), 0, s, r));
-        if (dH) {
-            rc = vk ? launch_product<false, true, kHidden>(m_u2, m_u2, m_w2, m_u2, a2, pairs, s)
-                    : launch_product<false, false, kHidden>(m_u2, m_u2, m_w2, m_u2, a2, pairs, s);
-            if (rc) return rc;
-            PPO_RETURN_IF_CUDA(launch_dependent(vk ? join_kernel<true> : join_kernel<false>, dim3((unsigned)((pairs - 1) * kJoinBlocks)),
-                                                dim3(kJoinThreads), 0, s, a2, pairs));
-        }
-        if (dW) {
-            rc = vk ? launch_product<true, true, kWeight>(m_u3, m_u3, m_scaled, m_dw, a3, pairs, s)
-                    : launch_product<true, true, kWeight>(m_scaled, m_scaled, m_u3, m_dw, a3, pairs, s);
-            if (rc) return rc;
-        }
     }
     PPO_RETURN_IF_CUDA(launch_dependent(loss_kernel, dim3(1), dim3(kLossThreads), 0, s, r));
     return PPO_OK;

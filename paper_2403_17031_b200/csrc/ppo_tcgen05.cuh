@@ -310,13 +310,24 @@ __device__ __forceinline__ void tmem_free_all_pair(uint32_t base)
     asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(base), "r"(512u) : "memory");
 }
 
+// n / d for n < 2^30 and quotients below 2^21: the fp32 quotient is off by one at most
+__device__ __forceinline__ int quotient(int n, int d)
+{
+    int q = (int)__fdividef((float)n, (float)d);
+    const int r = n - q * d;
+    q += r >= d ? 1 : 0;
+    q -= r < 0 ? 1 : 0;
+    return q;
+}
+
 // unit -> output tile: blocks of gm x gn tiles (m fastest inside), column of blocks by column of blocks; a block's
 // tiles run at the same time and share their operand panels through L2
 __device__ __forceinline__ int2 tile_of(int u, int m_tiles, int n_tiles, int gm, int gn)
 {
-    const int col = u / (m_tiles * gn), width = min(gn, n_tiles - col * gn), rest = u - col * m_tiles * gn;
-    const int blk = rest / (gm * width), height = min(gm, m_tiles - blk * gm), in = rest - blk * gm * width;
-    return make_int2(blk * gm + in % height, col * gn + in / height);
+    const int col = quotient(u, m_tiles * gn), width = min(gn, n_tiles - col * gn), rest = u - col * m_tiles * gn;
+    const int blk = quotient(rest, gm * width), height = min(gm, m_tiles - blk * gm), in = rest - blk * gm * width;
+    const int n = quotient(in, height);
+    return make_int2(blk * gm + in - n * height, col * gn + n);
 }
 
 // ---------------------------------------------------------------- host side
