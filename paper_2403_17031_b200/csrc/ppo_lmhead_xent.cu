@@ -34,7 +34,7 @@ namespace xent {
 
 using namespace tc;
 
-constexpr int kBM = 128, kBN = 256, kBlockK = 64, kBox = 64 * kBlockK * 2;
+constexpr int kBM = 128, kBlockK = 64, kBox = 64 * kBlockK * 2;
 constexpr int kEpiWarps = 8, kThreads = (4 + kEpiWarps) * 32;
 constexpr int kStageOut = 32 * 128;                        // two per epilogue warp: 32 rows x 64 bf16
 constexpr int kChunk = 128;                                // columns with one reference
@@ -43,15 +43,17 @@ constexpr float kNoRef = -1.0e30f;
 // 2^-64 and 2^64: the largest of a chunk's U lies between them, its smaller ones down to 2^-126 and their sums stay normal numbers
 constexpr float kLeast = 5.421010862427522e-20f, kMost = 1.8446744073709552e19f;
 
-// Pairs of blocks share a tile of 256 x 256: each loads half of either operand. Up to 128 rows, blocks alone on tiles of
-// 128 x 256: half of a pair's tile would be idle rows, and the tensor cores would take longer over them than memory over W.
+// Pairs of blocks share a tile of 256 x 256: each loads half of either operand, and its epilogue warps half of the columns each.
+// Up to 128 rows, blocks alone on tiles of 128 x 128: half of a pair's tile would be idle rows, the tensor cores would take longer over
+// them than memory over W, and there are too few wide tiles to share out evenly (197 of 256 columns at V = 50304, on 148
+// SMs: 101 us for product 1 of 53 rows). Two groups of epilogue warps then take turns at the tiles.
 template <bool PAIR>
 struct Shape {
-    static constexpr int kM = PAIR ? 2 * kBM : kBM, kRowsB = PAIR ? kBN / 2 : kBN;   // tile rows; a block's share of B
+    static constexpr int kM = PAIR ? 2 * kBM : kBM, kN = PAIR ? 256 : 128, kRowsB = 128;   // tile; a block's share of B
     static constexpr int kBytesA = kBM * kBlockK * 2, kBytesB = kRowsB * kBlockK * 2, kStage = kBytesA + kBytesB;
-    static constexpr int kStages = PAIR ? 5 : 3;
+    static constexpr int kStages = 5;
     static constexpr int kSmem = kStages * kStage + 2 * kEpiWarps * kStageOut + 1024;
-    static constexpr int kTileFloats = kM * kBN;
+    static constexpr int kTileFloats = kM * kN;
     static_assert(kSmem <= 232448 - 1024, "shared memory of a block");
 };
 
@@ -117,7 +119,7 @@ __device__ __forceinline__ Plan plan_of(const Args &a, int rows, int workers)
     constexpr int kM = Shape<PAIR>::kM;
     Plan p;
     p.m_tiles = ((PRODUCT == kWeight ? a.dim_m : rows) + kM - 1) / kM;
-    p.n_tiles = (a.dim_n + kBN - 1) / kBN;
+    p.n_tiles = (a.dim_n + Shape<PAIR>::kN - 1) / Shape<PAIR>::kN;
     p.kbs = ((PRODUCT == kWeight ? rows : a.dim_k) + kBlockK - 1) / kBlockK;
     p.n_whole = p.m_tiles * p.n_tiles;
     p.n_rest = p.share = 0;
@@ -269,7 +271,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         }
         for (int b = 0; b < 2; ++b) {
             barrier_init(&sm.tmem_full[b], 1);
-            barrier_init(&sm.tmem_empty[b], (PAIR ? 2 : 1) * kEpiWarps);    // (of a pair: both blocks' epilogues)
+            barrier_init(&sm.tmem_empty[b], PAIR ? 2 * kEpiWarps : kEpiWarps / 2);   // both blocks' warps; a group
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -300,7 +302,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             uint32_t it = 0, s = 0, parity = 1;                 // (waiting for the phase before the first returns at once)
             while (alive && work.next(plan, workers)) {
                 const int2 t = tile_of(work.u, plan.m_tiles, plan.n_tiles, a.gm, a.gn);
-                const int m0 = t.x * S::kM + rank * kBM, n0 = t.y * kBN + rank * S::kRowsB;
+                const int m0 = t.x * S::kM + rank * kBM, n0 = t.y * S::kN + rank * S::kRowsB;
                 for (int kb = work.kb0; kb < work.kb1; ++kb, ++it) {
                     wait_alive(alive, &sm.empty[s], parity, a.status);
                     if (!alive) break;
@@ -340,7 +342,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         __syncwarp();
     } else if (warp == 1) {
         if (rank == 0 && lane == 0) {
-            constexpr uint32_t idesc = instr_desc(A_MN, B_MN, S::kM, kBN);
+            constexpr uint32_t idesc = instr_desc(A_MN, B_MN, S::kM, S::kN);
             const auto announce = [](unsigned long long *bar) {
                 if (PAIR) commit_pair(bar);
                 else commit(bar);
@@ -352,7 +354,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                 const uint32_t buf = tiles & 1;
                 wait_alive(alive, &sm.tmem_empty[buf], ((tiles >> 1) & 1) ^ 1, a.status);
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                const uint32_t tmem_d = tmem_base + buf * kBN;
+                const uint32_t tmem_d = tmem_base + buf * S::kN;
                 for (int kb = work.kb0; kb < work.kb1; ++kb) {
                     wait_alive(alive, &sm.full[s], s_parity, a.status);
                     if (!alive) break;
@@ -383,20 +385,22 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         }
         __syncwarp();
     } else if (warp >= 4) {
-        const int q = warp & 3, h = (warp - 4) >> 2;            // lanes 32 q .., columns 128 h .. of the tile
+        // lanes 32 q ..; of a pair's tile columns 128 h .., else all of them in every second tile
+        const int q = warp & 3, group = (warp - 4) >> 2, h = PAIR ? group : 0;
         unsigned char *const stage = ring + (size_t)kStages * S::kStage + (warp - 4) * 2 * kStageOut;
         const uint32_t tmem_empty = PAIR ? leader_addr(&sm.tmem_empty[0]) : saddr(&sm.tmem_empty[0]);
         const float nan = __int_as_float(0x7fffffff);
         const bool first = a.row0 == 0, last = a.row0 + a.rows_max >= *a.n_real;
         bool alive = true;
         uint32_t tiles = 0;
-        while (work.next(plan, workers)) {
+        for (; work.next(plan, workers); ++tiles) {
+            if (!PAIR && (int)(tiles & 1) != group) continue;
             const int2 t = tile_of(work.u, plan.m_tiles, plan.n_tiles, a.gm, a.gn);
-            const int m_warp = t.x * S::kM + rank * kBM + q * 32, n = t.y * kBN + h * 128;
+            const int m_warp = t.x * S::kM + rank * kBM + q * 32, n = t.y * S::kN + h * 128;
             const int row = m_warp + lane;
             const bool empty = work.kb0 == work.kb1;
             const uint32_t buf = tiles & 1;
-            const uint32_t taddr = tmem_base + buf * kBN + h * 128 + ((uint32_t)(q * 32) << 16);
+            const uint32_t taddr = tmem_base + buf * S::kN + h * 128 + ((uint32_t)(q * 32) << 16);
             bool ok = false;
             int label = -1, out_row = -1;
             float ref = 0.f;
@@ -586,7 +590,6 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                 }
                 if (last) send(a.bulk_cols, m_warp < a.dim_m);
             }
-            if (!empty) ++tiles;
         }
         if (lane == 0) tma_store_wait_read();                   // shared memory outlives the copies out of it
     }
@@ -603,12 +606,12 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
 // The tiles of dH that were cut along the vocabulary: a block adds up 32 rows x 64 columns over the pairs that hold parts of
 // them, in the order of the contraction, and turns them in shared memory so that rows leave in runs.
 constexpr int kJoinThreads = 256;
-template <bool PAIR> constexpr int join_blocks() { return (Shape<PAIR>::kM / 32) * (kBN / 64); }
+template <bool PAIR> constexpr int join_blocks() { return (Shape<PAIR>::kM / 32) * (Shape<PAIR>::kN / 64); }
 template <bool PAIR, bool VK>
 __global__ void __launch_bounds__(kJoinThreads)
 join_kernel(const Args a, int workers)
 {
-    constexpr int kM = Shape<PAIR>::kM, kTileFloats = Shape<PAIR>::kTileFloats, kBlocks = (kM / 32) * (kBN / 64);
+    constexpr int kM = Shape<PAIR>::kM, kTileFloats = Shape<PAIR>::kTileFloats, kBlocks = (kM / 32) * (Shape<PAIR>::kN / 64);
     __shared__ float4 turn[32][17];
     grid_dependents_may_launch();
     grid_dependency_wait();
@@ -618,7 +621,7 @@ join_kernel(const Args a, int workers)
     if (rest >= p.n_rest) return;
     const int row0 = (part_of % (kM / 32)) * 32, j0 = part_of / (kM / 32) * 16;
     const int2 t = tile_of(p.n_whole + rest, p.m_tiles, p.n_tiles, a.gm, a.gn);
-    const int m0 = t.x * kM + row0, n0 = t.y * kBN + j0 * 4;
+    const int m0 = t.x * kM + row0, n0 = t.y * Shape<PAIR>::kN + j0 * 4;
     if (m0 >= rows || n0 >= a.dim_n) return;
     const int first = (int)((int64_t)rest * p.kbs / p.share), last = (int)(((int64_t)(rest + 1) * p.kbs - 1) / p.share);
     const int lane = threadIdx.x & 31, jj = threadIdx.x >> 5;
@@ -1002,8 +1005,8 @@ static Layout layout_of(int64_t M, int64_t K, int64_t V, int64_t piece_rows, boo
     l.packed = take((size_t)M * l.Kp * 2);
     l.scaled = take(dw ? rows * l.Kp * 2 : 0);
     l.u = take(grad ? rows * (size_t)l.Vp * 2 : 0);
-    l.parts = take(dh ? (size_t)kMaxSms * 2 * Shape<false>::kTileFloats * 4 : 0);
-    const size_t tiles = (size_t)((K + kBN - 1) / kBN) * (size_t)((V + kBN - 1) / kBN);
+    l.parts = take(dh ? (size_t)(M > kBM ? kMaxSms / 2 * Shape<true>::kTileFloats : kMaxSms * Shape<false>::kTileFloats) * 2 * 4 : 0);
+    const size_t tiles = (size_t)((K + 255) / 256) * (size_t)((V + 255) / 256);
     l.sums = take(dw && l.pieces > 1 ? tiles * Shape<true>::kTileFloats * 4 : 0);
     l.bytes = at;
     return l;
@@ -1148,7 +1151,7 @@ extern "C" int ppo_lmhead_xent(const void *H, int64_t ldh, const void *W, int64_
     r.status = status;
 
     Maps m = {};
-    const int rows_b = pair ? kBN / 2 : kBN;                    // a block's share of B, stored by rows
+    const int rows_b = Shape<true>::kRowsB;                     // a block's share of B, stored by rows
     if ((rc = make_map_pitch(&m.packed, r.packed, (uint64_t)K, (uint64_t)M, (uint64_t)l.Kp, kBM))) return rc;
     if ((rc = make_map_pitch(&m.h, H, (uint64_t)K, (uint64_t)M, (uint64_t)ldh, kBM))) return rc;
     // product 1 takes W with the vocabulary as the result's columns, product 2 with the hidden size
