@@ -298,6 +298,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             // (where all rows are real they need not have been packed)
             const CUtensorMap *ma = PRODUCT == kLogits && a.in_place && *a.n_real == a.M ? &map_a_all : &map_a;
             const int row0 = PRODUCT == kLogits ? a.row0 : 0;
+            const uint32_t full0 = PAIR ? leader_addr(&sm.full[0]) : 0;
             bool alive = true;
             uint32_t it = 0, s = 0, parity = 1;                 // (waiting for the phase before the first returns at once)
             while (alive && work.next(plan, workers)) {
@@ -310,7 +311,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                     // (bytes of the other block may be counted before they are announced: the phase cannot end
                     // without the leader's arrival)
                     if (rank == 0) barrier_expect_tx(&sm.full[s], (PAIR ? 2u : 1u) * S::kStage);
-                    const uint32_t bar = PAIR ? leader_addr(&sm.full[s]) : saddr(&sm.full[s]);
+                    const uint32_t bar = full0 + s * 8;
                     const auto load = [&](unsigned char *dst, const CUtensorMap *map, int x, int y) {
                         if (PAIR) tma_load_2d_pair(dst, map, x, y, bar);
                         else tma_load_2d(dst, map, x, y, &sm.full[s]);
@@ -343,6 +344,11 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     } else if (warp == 1) {
         if (rank == 0 && lane == 0) {
             constexpr uint32_t idesc = instr_desc(A_MN, B_MN, S::kM, S::kN);
+            // K-major: 8-row groups 1024 bytes apart; MN-major: 64-wide boxes, 8 contraction rows 1024 bytes apart. (A stage is added
+            // to descriptors made once: the thread's own instructions, which take turns with those of two epilogue warps,
+            // otherwise take longer than the products.)
+            const uint64_t a_desc = smem_desc(saddr(ring), A_MN ? kBox : 16, 1024);
+            const uint64_t b_desc = smem_desc(saddr(ring) + S::kBytesA, B_MN ? kBox : 16, 1024);
             const auto announce = [](unsigned long long *bar) {
                 if (PAIR) commit_pair(bar);
                 else commit(bar);
@@ -355,20 +361,20 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                 wait_alive(alive, &sm.tmem_empty[buf], ((tiles >> 1) & 1) ^ 1, a.status);
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 const uint32_t tmem_d = tmem_base + buf * S::kN;
+                uint32_t accumulate = 0;
                 for (int kb = work.kb0; kb < work.kb1; ++kb) {
                     wait_alive(alive, &sm.full[s], s_parity, a.status);
                     if (!alive) break;
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                    const uint32_t a_addr = saddr(ring + (size_t)s * S::kStage), b_addr = a_addr + S::kBytesA;
+                    const uint64_t ad = a_desc + s * (S::kStage >> 4), bd = b_desc + s * (S::kStage >> 4);
 #pragma unroll
                     for (int kk = 0; kk < kBlockK / 16; ++kk) {
-                        // K-major: 8-row groups 1024 bytes apart, 16 contraction elements are 32 bytes. MN-major: 64-wide
-                        // boxes, 8 contraction rows 1024 bytes apart, 16 of them are 2048 bytes.
-                        const uint64_t ad = A_MN ? smem_desc(a_addr + kk * 2048, kBox, 1024) : smem_desc(a_addr + kk * 32, 16, 1024);
-                        const uint64_t bd = B_MN ? smem_desc(b_addr + kk * 2048, kBox, 1024) : smem_desc(b_addr + kk * 32, 16, 1024);
-                        if (PAIR) mma_pair(tmem_d, ad, bd, idesc, kb > work.kb0 || kk ? 1u : 0u);
-                        else mma(tmem_d, ad, bd, idesc, kb > work.kb0 || kk ? 1u : 0u);
+                        // 16 contraction elements further: 32 bytes K-major, 16 rows of 128 MN-major
+                        const uint64_t ak = ad + kk * (A_MN ? 2048 >> 4 : 32 >> 4), bk = bd + kk * (B_MN ? 2048 >> 4 : 32 >> 4);
+                        if (PAIR) mma_pair(tmem_d, ak, bk, idesc, kk ? 1u : accumulate);
+                        else mma(tmem_d, ak, bk, idesc, kk ? 1u : accumulate);
                     }
+                    accumulate = 1;
                     announce(&sm.empty[s]);
                     if (++s == kStages) { s = 0; s_parity ^= 1; }
                 }
