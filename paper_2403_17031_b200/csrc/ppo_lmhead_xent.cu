@@ -17,11 +17,12 @@
 // smaller one are multiplied by 2^(difference), which is exact, before product 2.
 //
 // Roundings to 16 bits: U, a H, and the results. Statistics, sums and nll are fp32, the loss fp64. What the rounding of U
-// would do to the gradients is kept small in three ways. S in the gradient is the sum of the rounded U, so that D is the
-// gradient of a softmax whose probabilities are off by half a step each and still add up to 1: a direction that all columns
-// of W share drops out of dH (logits far from 0 have one), as it should. U' at the label, about -S, is the largest element
-// of its row by far; what its own rounding leaves, e = (U - S) - U', comes back in fp32: in product 2 as e W[:, label], in
-// the epilogue, and in product 3 by a factor that makes a U' exact there (the row's other elements take that half step).
+// would do to the gradients is kept small in two ways. S in the gradient is the sum of the rounded U, so that D is the
+// gradient of a softmax whose probabilities are off by half a step each and still add up to 1. U' at the label, about -S, is the
+// largest element of its row by far: its own rounding is undone by a factor on a that makes a U' exact there, at the cost of
+// that half step in the row's other elements. The row of D then adds up to c = a (exact - rounded) instead of 0, which would
+// bring in what all columns of W have in common (logits far from 0 come from there); product 2 adds c times the mean of some
+// columns of W to take that out again.
 //
 // Product kernel: persistent pairs of blocks (cta_group::2) on 256 x 256 tiles; per block one TMA producer warp (stages of
 // 64 along the contraction, 128-byte swizzle), in the leader one issuer warp, eight epilogue warps that drain one 256-column
@@ -36,23 +37,32 @@ using namespace tc;
 
 constexpr int kBM = 128, kBlockK = 64, kBox = 64 * kBlockK * 2;
 constexpr int kEpiWarps = 8, kThreads = (4 + kEpiWarps) * 32;
-constexpr int kStageOut = 32 * 128;                        // two per epilogue warp: 32 rows x 64 bf16
+constexpr int kStageOut = 32 * 128;                        // a staging buffer: 32 rows x 64 bf16
 constexpr int kChunk = 128;                                // columns with one reference
 constexpr int kMaxSms = 160;
 constexpr float kNoRef = -1.0e30f;
 // 2^-64 and 2^64: the largest of a chunk's U lies between them, its smaller ones down to 2^-126 and their sums stay normal numbers
 constexpr float kLeast = 5.421010862427522e-20f, kMost = 1.8446744073709552e19f;
 
-// Pairs of blocks share a tile of 256 x 256: each loads half of either operand, and its epilogue warps half of the columns each.
-// Up to 128 rows, blocks alone on tiles of 128 x 128: half of a pair's tile would be idle rows, the tensor cores would take longer over
-// them than memory over W, and there are too few wide tiles to share out evenly (197 of 256 columns at V = 50304, on 148
-// SMs: 101 us for product 1 of 53 rows). Two groups of epilogue warps then take turns at the tiles.
-template <bool PAIR>
+// kPair: pairs of blocks share a tile of 256 x 256: each loads half of either operand, and its epilogue warps half of the columns
+// each; one accumulator is drained while the next is formed.
+// kWide: 256 x 512, both accumulators one tile's: a quarter less comes out of L2 per product (which bounds pairs: 64 KB in the
+// 512 cycles of a block of the contraction are all that an SM's port takes), but draining them is not hidden. For long
+// contractions.
+// kSingle: blocks alone on tiles of 128 x 128, for up to 128 rows: half of a pair's tile would be idle rows, the tensor cores would
+// take longer over them than memory over W, and there are too few wide tiles to share out evenly (197 of 256 columns at V =
+// 50304, on 148 SMs: 101 us for product 1 of 53 rows, now 88). Two groups of epilogue warps take turns at the tiles.
+enum Mode { kSingle, kPair, kWide };
+
+template <int MODE>
 struct Shape {
-    static constexpr int kM = PAIR ? 2 * kBM : kBM, kN = PAIR ? 256 : 128, kRowsB = 128;   // tile; a block's share of B
-    static constexpr int kBytesA = kBM * kBlockK * 2, kBytesB = kRowsB * kBlockK * 2, kStage = kBytesA + kBytesB;
-    static constexpr int kStages = 5;
-    static constexpr int kSmem = kStages * kStage + 2 * kEpiWarps * kStageOut + 1024;
+    static constexpr bool kIsPair = MODE != kSingle;
+    static constexpr int kHalves = MODE == kWide ? 2 : 1;              // accumulators of a tile
+    static constexpr int kM = kIsPair ? 2 * kBM : kBM, kAccN = kIsPair ? 256 : 128, kN = kHalves * kAccN;
+    static constexpr int kRowsB = 128;                                 // a block's share of B, per accumulator
+    static constexpr int kBytesA = kBM * kBlockK * 2, kBytesB = kRowsB * kBlockK * 2, kStage = kBytesA + kHalves * kBytesB;
+    static constexpr int kStages = MODE == kWide ? 4 : 5, kBuffers = MODE == kWide ? 1 : 2;   // buffers: per epilogue warp
+    static constexpr int kSmem = kStages * kStage + kBuffers * kEpiWarps * kStageOut + 1024;
     static constexpr int kTileFloats = kM * kN;
     static_assert(kSmem <= 232448 - 1024, "shared memory of a block");
 };
@@ -79,9 +89,8 @@ struct Args {
     int64_t ldo;
     int bulk_cols;                                         // bulk stores take boxes that end at or before this column
     // kHidden
-    const float2 *row_scale;                               // [rows] a, a e
-    const __nv_bfloat16 *W;
-    int64_t ldw;
+    const float2 *row_scale;                               // [rows] a, c
+    const float *w_mean;                                   // [K, in whole tiles]
     float *scratch;                                        // kHidden: parts of tiles cut along the contraction; kWeight: sums over the pieces
 };
 
@@ -113,21 +122,21 @@ struct Plan {
     int m_tiles, n_tiles, n_whole, n_rest, share, kbs;
 };
 
-template <bool PAIR, int PRODUCT>
+template <int MODE, int PRODUCT>
 __device__ __forceinline__ Plan plan_of(const Args &a, int rows, int workers)
 {
-    constexpr int kM = Shape<PAIR>::kM;
+    constexpr int kM = Shape<MODE>::kM;
     Plan p;
     p.m_tiles = ((PRODUCT == kWeight ? a.dim_m : rows) + kM - 1) / kM;
-    p.n_tiles = (a.dim_n + Shape<PAIR>::kN - 1) / Shape<PAIR>::kN;
+    p.n_tiles = (a.dim_n + Shape<MODE>::kN - 1) / Shape<MODE>::kN;
     p.kbs = ((PRODUCT == kWeight ? rows : a.dim_k) + kBlockK - 1) / kBlockK;
     p.n_whole = p.m_tiles * p.n_tiles;
     p.n_rest = p.share = 0;
     if (PRODUCT == kWeight && rows == 0 && a.row0 > 0) p.n_whole = 0;      // nothing to add
     if (PRODUCT == kHidden) {
         // Cut when that saves each worker enough blocks of the contraction: 24, and two a tile for the joining and for the
-        // operands that tiles at different places of the contraction do not share through L2 (62 tiles left of 432 at 6912 x
-        // 4096 x 50304, 127 blocks saved: 2250 us cut, 2130 whole).
+        // operands that tiles at different places of the contraction do not share through L2 (62 pairs' tiles left of 432 at
+        // 6912 x 4096 x 50304, 127 blocks saved: 2250 us cut, 2130 whole).
         const int rest = p.n_whole % workers, share = (int)(((int64_t)rest * p.kbs + workers - 1) / workers);
         if (rest > 0 && p.kbs - share >= 24 + 2 * rest) {
             p.n_rest = rest;
@@ -223,43 +232,14 @@ __device__ __forceinline__ void stage64(unsigned char *stage, const float *v)
     }
 }
 
-// f * W[k .. k + N, label] added to N neighbouring elements of a row of dH; VK: W is stored [V, K]
-template <bool VK, int N>
-__device__ __forceinline__ void add_label(const Args &a, float f, int label, int k, float *v)
-{
-    if (VK) {
-        const __nv_bfloat16 *w = a.W + (int64_t)label * a.ldw + k;
-#pragma unroll
-        for (int j = 0; j < N; j += 4) {
-            if (k + j + 4 <= a.dim_n) {
-                const uint2 x = __ldg(reinterpret_cast<const uint2 *>(w + j));
-                v[j] = fmaf(f, low(x.x), v[j]);
-                v[j + 1] = fmaf(f, high(x.x), v[j + 1]);
-                v[j + 2] = fmaf(f, low(x.y), v[j + 2]);
-                v[j + 3] = fmaf(f, high(x.y), v[j + 3]);
-            } else {
-#pragma unroll
-                for (int e = j; e < j + 4; ++e)
-                    if (k + e < a.dim_n) v[e] = fmaf(f, __bfloat162float(w[e]), v[e]);
-            }
-        }
-    } else {
-        const __nv_bfloat16 *w = a.W + (int64_t)k * a.ldw + label;
-        float x[N];
-#pragma unroll
-        for (int j = 0; j < N; ++j) x[j] = k + j < a.dim_n ? __bfloat162float(w[(int64_t)j * a.ldw]) : 0.f;
-#pragma unroll
-        for (int j = 0; j < N; ++j) v[j] = fmaf(f, x[j], v[j]);
-    }
-}
-
-template <bool PAIR, bool A_MN, bool B_MN, int PRODUCT>
+template <int MODE, bool A_MN, bool B_MN, int PRODUCT>
 __global__ void __launch_bounds__(kThreads, 1)
 product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_a_all,
                const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_out, const Args a)
 {
-    using S = Shape<PAIR>;
-    constexpr int kStages = S::kStages;
+    using S = Shape<MODE>;
+    constexpr bool PAIR = S::kIsPair;
+    constexpr int kStages = S::kStages, kHalves = S::kHalves;
     extern __shared__ __align__(1024) unsigned char smem_raw[];
     __shared__ Smem<kStages> sm;
     unsigned char *ring = smem_raw + ((1024u - (saddr(smem_raw) & 1023u)) & 1023u);
@@ -289,7 +269,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     const int rank = PAIR ? (int)cluster_rank() : 0;
     const int worker = PAIR ? blockIdx.x / 2 : blockIdx.x, workers = PAIR ? gridDim.x / 2 : gridDim.x;
     const int rows = rows_of(a);
-    const Plan plan = plan_of<PAIR, PRODUCT>(a, rows, workers);
+    const Plan plan = plan_of<MODE, PRODUCT>(a, rows, workers);
     Work work;
     work.init(plan, worker);
 
@@ -322,12 +302,15 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                     } else {                                    // stored [m, k]: one box of 64 (k) x 128 (m)
                         load(stage, ma, kb * kBlockK, row0 + m0);
                     }
-                    if (B_MN) {
 #pragma unroll
-                        for (int j = 0; j < S::kRowsB / 64; ++j)
-                            load(stage + S::kBytesA + j * kBox, &map_b, n0 + j * 64, kb * kBlockK);
-                    } else {
-                        load(stage + S::kBytesA, &map_b, kb * kBlockK, n0);
+                    for (int i = 0; i < kHalves; ++i) {
+                        unsigned char *to = stage + S::kBytesA + i * S::kBytesB;
+                        if (B_MN) {
+                            load(to, &map_b, n0 + i * S::kAccN, kb * kBlockK);
+                            load(to + kBox, &map_b, n0 + i * S::kAccN + 64, kb * kBlockK);
+                        } else {
+                            load(to, &map_b, kb * kBlockK, n0 + i * S::kAccN);
+                        }
                     }
                     if (++s == kStages) { s = 0; parity ^= 1; }
                 }
@@ -343,7 +326,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         __syncwarp();
     } else if (warp == 1) {
         if (rank == 0 && lane == 0) {
-            constexpr uint32_t idesc = instr_desc(A_MN, B_MN, S::kM, S::kN);
+            constexpr uint32_t idesc = instr_desc(A_MN, B_MN, S::kM, S::kAccN);
             // K-major: 8-row groups 1024 bytes apart; MN-major: 64-wide boxes, 8 contraction rows 1024 bytes apart. (A stage is added
             // to descriptors made once: the thread's own instructions, which take turns with those of two epilogue warps,
             // otherwise take longer than the products.)
@@ -355,58 +338,96 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             };
             bool alive = true;
             uint32_t s = 0, s_parity = 0, tiles = 0;
+            // one block of the contraction into accumulator `acc`, from stage `from`
+            const auto multiply = [&](uint32_t acc, uint32_t from, int half, uint32_t accumulate) {
+                const uint64_t ad = a_desc + from * (S::kStage >> 4), bd = b_desc + (from * S::kStage + half * S::kBytesB >> 4);
+#pragma unroll
+                for (int kk = 0; kk < kBlockK / 16; ++kk) {
+                    // 16 contraction elements further: 32 bytes K-major, 16 rows of 128 MN-major
+                    const uint64_t ak = ad + kk * (A_MN ? 2048 >> 4 : 32 >> 4), bk = bd + kk * (B_MN ? 2048 >> 4 : 32 >> 4);
+                    if (PAIR) mma_pair(tmem_base + acc * S::kAccN, ak, bk, idesc, kk ? 1u : accumulate);
+                    else mma(tmem_base + acc * S::kAccN, ak, bk, idesc, kk ? 1u : accumulate);
+                }
+            };
+            const auto step = [&] { if (++s == kStages) { s = 0; s_parity ^= 1; } };
             while (alive && work.next(plan, workers)) {
-                if (work.kb0 == work.kb1) continue;             // an empty contraction: the epilogue knows
-                const uint32_t buf = tiles & 1;
-                wait_alive(alive, &sm.tmem_empty[buf], ((tiles >> 1) & 1) ^ 1, a.status);
+                int kb = work.kb0;
+                if (kb == work.kb1) continue;                   // an empty contraction: the epilogue knows
+                const uint32_t buf = kHalves == 2 ? 0 : tiles & 1, parity = (kHalves == 2 ? tiles & 1 : tiles >> 1 & 1) ^ 1;
+                wait_alive(alive, &sm.tmem_empty[buf], parity, a.status);
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                const uint32_t tmem_d = tmem_base + buf * S::kN;
-                uint32_t accumulate = 0;
-                for (int kb = work.kb0; kb < work.kb1; ++kb) {
+                if (kHalves == 2) {
+                    // the first accumulator goes ahead, as far as the stages reach, while the second one is drained
+                    const uint32_t s0 = s, p0 = s_parity;
+                    const int lead = min(work.kb1 - kb, kStages);
+                    for (int i = 0; i < lead && alive; ++i) {
+                        wait_alive(alive, &sm.full[s], s_parity, a.status);
+                        if (!alive) break;
+                        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                        multiply(0, s, 0, i ? 1u : 0u);
+                        step();
+                    }
+                    wait_alive(alive, &sm.tmem_empty[1], parity, a.status);
+                    if (!alive) break;
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    s = s0;
+                    s_parity = p0;
+                    if (lead == work.kb1 - kb && PPO_TEST_WITHHOLD_XENT != 1) announce(&sm.tmem_full[0]);
+                    for (int i = 0; i < lead; ++i) {
+                        multiply(1, s, 1, i ? 1u : 0u);
+                        announce(&sm.empty[s]);
+                        step();
+                    }
+                    kb += lead;
+                }
+                for (; kb < work.kb1; ++kb) {
                     wait_alive(alive, &sm.full[s], s_parity, a.status);
                     if (!alive) break;
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                    const uint64_t ad = a_desc + s * (S::kStage >> 4), bd = b_desc + s * (S::kStage >> 4);
-#pragma unroll
-                    for (int kk = 0; kk < kBlockK / 16; ++kk) {
-                        // 16 contraction elements further: 32 bytes K-major, 16 rows of 128 MN-major
-                        const uint64_t ak = ad + kk * (A_MN ? 2048 >> 4 : 32 >> 4), bk = bd + kk * (B_MN ? 2048 >> 4 : 32 >> 4);
-                        if (PAIR) mma_pair(tmem_d, ak, bk, idesc, kk ? 1u : accumulate);
-                        else mma(tmem_d, ak, bk, idesc, kk ? 1u : accumulate);
+                    multiply(buf, s, 0, kb > work.kb0 ? 1u : 0u);
+                    if (kHalves == 2) {
+                        if (kb == work.kb1 - 1 && PPO_TEST_WITHHOLD_XENT != 1) announce(&sm.tmem_full[0]);
+                        multiply(1, s, 1, 1u);
                     }
-                    accumulate = 1;
                     announce(&sm.empty[s]);
-                    if (++s == kStages) { s = 0; s_parity ^= 1; }
+                    step();
                 }
                 if (alive && PPO_TEST_WITHHOLD_XENT != 1) {
-                    announce(&sm.tmem_full[buf]);
+                    announce(&sm.tmem_full[kHalves == 2 ? 1 : buf]);
                     ++tiles;
                 }
             }
-            // every product has ended before tensor memory is freed
-            for (uint32_t i = tiles > 2 ? tiles - 2 : 0; i < tiles; ++i) wait(&sm.tmem_full[i & 1], (i >> 1) & 1, a.status);
-            // and the other block's last arrivals before this block ends
-            for (uint32_t i = tiles > 2 ? tiles - 2 : 0; i < tiles; ++i)
-                wait_alive(alive, &sm.tmem_empty[i & 1], (i >> 1) & 1, a.status);
+            // every product has ended before tensor memory is freed, and the other block's last arrivals before this block ends
+            if (kHalves == 2) {
+                for (int i = 0; i < 2 && tiles > 0; ++i) wait(&sm.tmem_full[i], (tiles - 1) & 1, a.status);
+                for (int i = 0; i < 2 && tiles > 0; ++i) wait_alive(alive, &sm.tmem_empty[i], (tiles - 1) & 1, a.status);
+            } else {
+                for (uint32_t i = tiles > 2 ? tiles - 2 : 0; i < tiles; ++i) wait(&sm.tmem_full[i & 1], (i >> 1) & 1, a.status);
+                for (uint32_t i = tiles > 2 ? tiles - 2 : 0; i < tiles; ++i)
+                    wait_alive(alive, &sm.tmem_empty[i & 1], (i >> 1) & 1, a.status);
+            }
         }
         __syncwarp();
     } else if (warp >= 4) {
         // lanes 32 q ..; of a pair's tile columns 128 h .., else all of them in every second tile
         const int q = warp & 3, group = (warp - 4) >> 2, h = PAIR ? group : 0;
-        unsigned char *const stage = ring + (size_t)kStages * S::kStage + (warp - 4) * 2 * kStageOut;
+        unsigned char *const stage = ring + (size_t)kStages * S::kStage + (warp - 4) * S::kBuffers * kStageOut;
         const uint32_t tmem_empty = PAIR ? leader_addr(&sm.tmem_empty[0]) : saddr(&sm.tmem_empty[0]);
         const float nan = __int_as_float(0x7fffffff);
         const bool first = a.row0 == 0, last = a.row0 + a.rows_max >= *a.n_real;
         bool alive = true;
         uint32_t tiles = 0;
-        for (; work.next(plan, workers); ++tiles) {
+        // (a wide tile's accumulators one after the other)
+        for (int part_of = kHalves; part_of < kHalves || work.next(plan, workers); ++tiles) {
+            const int half_tile = kHalves == 2 ? tiles & 1 : 0;
+            part_of = half_tile + 1;
             if (!PAIR && (int)(tiles & 1) != group) continue;
             const int2 t = tile_of(work.u, plan.m_tiles, plan.n_tiles, a.gm, a.gn);
-            const int m_warp = t.x * S::kM + rank * kBM + q * 32, n = t.y * S::kN + h * 128;
+            const int m_warp = t.x * S::kM + rank * kBM + q * 32, n = t.y * S::kN + half_tile * S::kAccN + h * 128;
             const int row = m_warp + lane;
             const bool empty = work.kb0 == work.kb1;
             const uint32_t buf = tiles & 1;
-            const uint32_t taddr = tmem_base + buf * S::kN + h * 128 + ((uint32_t)(q * 32) << 16);
+            const uint32_t taddr = tmem_base + buf * S::kAccN + h * 128 + ((uint32_t)(q * 32) << 16);
             bool ok = false;
             int label = -1, out_row = -1;
             float ref = 0.f;
@@ -423,7 +444,6 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                 if (ok && work.part < 0) {
                     out_row = a.order[a.row0 + row];
                     scale = a.row_scale[row];
-                    label = scale.y != 0.f ? a.labels[out_row] : -1;
                 }
             } else {
                 ok = row < a.dim_m;
@@ -465,18 +485,19 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                 if (lane == 0) tma_store_wait_read();
                 __syncwarp();
             };
-            // both buffers, 128 columns, by bulk copies as far as they may go
-            const auto send = [&](int bulk_cols, bool rows_here) {
+            // 64-column parts from .. to of these 128, from their buffers, by bulk copies as far as they may go
+            const auto send = [&](int from, int to, int bulk_cols, bool rows_here) {
                 fence_async_proxy();
                 __syncwarp();
 #pragma unroll
                 for (int half = 0; half < 2; ++half) {
                     const int col = n + half * 64;
-                    if (col >= a.dim_n) break;
+                    if (half < from || half >= to || col >= a.dim_n) continue;
+                    const unsigned char *buffer = stage + (S::kBuffers == 2 ? half : 0) * kStageOut;
                     if (col + 64 <= bulk_cols) {
-                        if (lane == 0 && rows_here) tma_store_2d(&map_out, col, m_warp, stage + half * kStageOut);
+                        if (lane == 0 && rows_here) tma_store_2d(&map_out, col, m_warp, buffer);
                     } else {
-                        store_rows(stage + half * kStageOut, a.out, a.ldo, out_row, col, a.dim_n);
+                        store_rows(buffer, a.out, a.ldo, out_row, col, a.dim_n);
                     }
                 }
                 __syncwarp();
@@ -541,12 +562,12 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                     if (out) ref += 128.f * rintf((fmaxf(m * c, -1e9f) - ref) * (1.f / 128.f));
                 }
                 release();
-                if (a.store) send(0x7fffffff, true);
+                if (a.store) send(0, 2, 0x7fffffff, true);
                 if (ok && n < a.dim_n) a.part[(size_t)row * a.chunks + n / kChunk] = make_float4(ref, s, rounded, 0.f);
             } else if (PRODUCT == kHidden) {
                 // (four columns of a tile's rows follow one another in scratch: a warp writes 512 bytes at a time)
                 float4 *part = reinterpret_cast<float4 *>(a.scratch + (size_t)(worker * 2 + max(work.part, 0)) * S::kTileFloats) +
-                               h * 32 * S::kM + rank * kBM + q * 32 + lane;
+                               (half_tile * 64 + h * 32) * S::kM + rank * kBM + q * 32 + lane;
 #pragma unroll 1
                 for (int half = 0; half < 2; ++half) {
                     float v[64];
@@ -559,19 +580,22 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                             part[(half * 16 + j) * S::kM] = make_float4(v[j * 4], v[j * 4 + 1], v[j * 4 + 2], v[j * 4 + 3]);
                         continue;
                     }
+                    const float4 *mean = reinterpret_cast<const float4 *>(a.w_mean + n + half * 64);
 #pragma unroll
-                    for (int j = 0; j < 64; ++j) v[j] *= scale.x;
-                    if (label >= 0) {
-#pragma unroll
-                        for (int j = 0; j < 64; j += 16) add_label<B_MN, 16>(a, scale.y, label, n + half * 64 + j, v + j);
+                    for (int j = 0; j < 16; ++j) {
+                        const float4 w = __ldg(mean + j);
+                        v[j * 4] = fmaf(v[j * 4], scale.x, scale.y * w.x);
+                        v[j * 4 + 1] = fmaf(v[j * 4 + 1], scale.x, scale.y * w.y);
+                        v[j * 4 + 2] = fmaf(v[j * 4 + 2], scale.x, scale.y * w.z);
+                        v[j * 4 + 3] = fmaf(v[j * 4 + 3], scale.x, scale.y * w.w);
                     }
-                    stage64(stage + half * kStageOut, v);
+                    stage64(stage + (S::kBuffers == 2 ? half : 0) * kStageOut, v);
+                    send(half, half + 1, 0, true);
                 }
-                if (work.part < 0) send(0, true);
             } else {
                 float4 *sum = reinterpret_cast<float4 *>(a.scratch + ((size_t)t.x * plan.n_tiles + t.y) * S::kTileFloats) +
-                              h * 32 * S::kM + rank * kBM + q * 32 + lane;
-                if (last) reuse();
+                              (half_tile * 64 + h * 32) * S::kM + rank * kBM + q * 32 + lane;
+                if (last && S::kBuffers == 2) reuse();
 #pragma unroll 1
                 for (int half = 0; half < 2; ++half) {
                     float v[64];
@@ -587,14 +611,15 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                         }
                     }
                     if (last) {
-                        stage64(stage + half * kStageOut, v);
+                        if (S::kBuffers == 1) reuse();
+                        stage64(stage + (S::kBuffers == 2 ? half : 0) * kStageOut, v);
+                        if (S::kBuffers == 1 || half == 1) send(S::kBuffers == 1 ? half : 0, half + 1, a.bulk_cols, m_warp < a.dim_m);
                     } else {
 #pragma unroll
                         for (int j = 0; j < 16; ++j)
                             sum[(half * 16 + j) * S::kM] = make_float4(v[j * 4], v[j * 4 + 1], v[j * 4 + 2], v[j * 4 + 3]);
                     }
                 }
-                if (last) send(a.bulk_cols, m_warp < a.dim_m);
             }
         }
         if (lane == 0) tma_store_wait_read();                   // shared memory outlives the copies out of it
@@ -612,22 +637,22 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
 // The tiles of dH that were cut along the vocabulary: a block adds up 32 rows x 64 columns over the pairs that hold parts of
 // them, in the order of the contraction, and turns them in shared memory so that rows leave in runs.
 constexpr int kJoinThreads = 256;
-template <bool PAIR> constexpr int join_blocks() { return (Shape<PAIR>::kM / 32) * (Shape<PAIR>::kN / 64); }
-template <bool PAIR, bool VK>
+template <int MODE> constexpr int join_blocks() { return (Shape<MODE>::kM / 32) * (Shape<MODE>::kN / 64); }
+template <int MODE>
 __global__ void __launch_bounds__(kJoinThreads)
 join_kernel(const Args a, int workers)
 {
-    constexpr int kM = Shape<PAIR>::kM, kTileFloats = Shape<PAIR>::kTileFloats, kBlocks = (kM / 32) * (Shape<PAIR>::kN / 64);
+    constexpr int kM = Shape<MODE>::kM, kTileFloats = Shape<MODE>::kTileFloats, kBlocks = (kM / 32) * (Shape<MODE>::kN / 64);
     __shared__ float4 turn[32][17];
     grid_dependents_may_launch();
     grid_dependency_wait();
     const int rows = rows_of(a);
-    const Plan p = plan_of<PAIR, kHidden>(a, rows, workers);
+    const Plan p = plan_of<MODE, kHidden>(a, rows, workers);
     const int rest = blockIdx.x / kBlocks, part_of = blockIdx.x % kBlocks;
     if (rest >= p.n_rest) return;
     const int row0 = (part_of % (kM / 32)) * 32, j0 = part_of / (kM / 32) * 16;
     const int2 t = tile_of(p.n_whole + rest, p.m_tiles, p.n_tiles, a.gm, a.gn);
-    const int m0 = t.x * kM + row0, n0 = t.y * Shape<PAIR>::kN + j0 * 4;
+    const int m0 = t.x * kM + row0, n0 = t.y * Shape<MODE>::kN + j0 * 4;
     if (m0 >= rows || n0 >= a.dim_n) return;
     const int first = (int)((int64_t)rest * p.kbs / p.share), last = (int)(((int64_t)(rest + 1) * p.kbs - 1) / p.share);
     const int lane = threadIdx.x & 31, jj = threadIdx.x >> 5;
@@ -651,10 +676,9 @@ join_kernel(const Args a, int workers)
         if (m0 + r >= rows || n >= a.dim_n) continue;
         const float2 s = a.row_scale[m0 + r];
         const float4 x = turn[r][c4];
-        float y[4] = {x.x * s.x, x.y * s.x, x.z * s.x, x.w * s.x};
-        const int row = a.order[a.row0 + m0 + r];
-        if (s.y != 0.f) add_label<VK, 4>(a, s.y, a.labels[row], n, y);
-        __nv_bfloat16 *to = a.out + (int64_t)row * a.ldo + n;
+        const float4 w = *reinterpret_cast<const float4 *>(a.w_mean + n);
+        const float y[4] = {fmaf(x.x, s.x, s.y * w.x), fmaf(x.y, s.x, s.y * w.y), fmaf(x.z, s.x, s.y * w.z), fmaf(x.w, s.x, s.y * w.w)};
+        __nv_bfloat16 *to = a.out + (int64_t)a.order[a.row0 + m0 + r] * a.ldo + n;
         if (n + 4 <= a.dim_n && reinterpret_cast<uintptr_t>(to) % 8 == 0) {
             *reinterpret_cast<uint2 *>(to) = make_uint2(pack2(y[0], y[1]), pack2(y[2], y[3]));
         } else {
@@ -924,20 +948,20 @@ row_kernel(const RowArgs a)
         if (bad && a.status) atomicOr(a.status, PPO_DEV_BAD_TOKEN);
     }
     if (!a.u) return;
-    // U at the label, as product 1 stored it, less S; in bf16, and what that leaves
-    float f2 = nan, f3 = nan, left = 0.f;
+    // U at the label, as product 1 stored it, less S
+    float f = nan, c = nan;
     if (!bad) {
         const float ref = part[label / kChunk].x;
         const float u = __bfloat162float(__float2bfloat16_rn(ex2(fmaf(acc, a.c, -ref)))) * ex2(ref - m);
         const float want = u - sr;
         const __nv_bfloat16 stored = __float2bfloat16_rn(want);
         const float got = __bfloat162float(stored);
-        f2 = a.scale * a.inv_tau / ((a.denom ? *a.denom : (float)n_real) * sr);
-        f3 = got != 0.f ? f2 * (want / got) : f2;
-        left = f2 * (want - got);
+        f = a.scale * a.inv_tau / ((a.denom ? *a.denom : (float)n_real) * sr);
+        if (got != 0.f) f *= want / got;
+        c = f * (want - got);
         if (threadIdx.x == 0) a.u[(int64_t)r * a.Vp + label] = stored;
     }
-    if (threadIdx.x == 0) a.row_scale[r] = make_float2(f2, left);
+    if (threadIdx.x == 0) a.row_scale[r] = make_float2(f, c);
     if (!scaled) return;
     const __nv_bfloat16 *h = a.H + (int64_t)row * a.ldh;
     for (int k = threadIdx.x * 8; k < a.K; k += kRowThreads * 8) {
@@ -945,10 +969,10 @@ row_kernel(const RowArgs a)
             const uint4 v = *reinterpret_cast<const uint4 *>(h + k);
             uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-            for (int e = 0; e < 4; ++e) w[e] = pack2(low(w[e]) * f3, high(w[e]) * f3);
+            for (int e = 0; e < 4; ++e) w[e] = pack2(low(w[e]) * f, high(w[e]) * f);
             *reinterpret_cast<uint4 *>(scaled + k) = make_uint4(w[0], w[1], w[2], w[3]);
         } else {
-            for (int e = k; e < a.K; ++e) scaled[e] = __float2bfloat16_rn(__bfloat162float(h[e]) * f3);
+            for (int e = k; e < a.K; ++e) scaled[e] = __float2bfloat16_rn(__bfloat162float(h[e]) * f);
         }
     }
 }
@@ -1004,16 +1028,17 @@ static Layout layout_of(int64_t M, int64_t K, int64_t V, int64_t piece_rows, boo
     l.n_real = take(4);
     l.order = take((size_t)M * 4);
     l.info = take((size_t)M * sizeof(int2));
-    l.w_mean = take((size_t)K * 4);
+    l.w_mean = take((size_t)(K + 511) / 512 * 512 * 4);
     l.picked = take(rows * 4);
     l.row_scale = take(rows * sizeof(float2));
     l.part = take(rows * (size_t)l.chunks * sizeof(float4));
     l.packed = take((size_t)M * l.Kp * 2);
     l.scaled = take(dw ? rows * l.Kp * 2 : 0);
     l.u = take(grad ? rows * (size_t)l.Vp * 2 : 0);
-    l.parts = take(dh ? (size_t)(M > kBM ? kMaxSms / 2 * Shape<true>::kTileFloats : kMaxSms * Shape<false>::kTileFloats) * 2 * 4 : 0);
-    const size_t tiles = (size_t)((K + 255) / 256) * (size_t)((V + 255) / 256);
-    l.sums = take(dw && l.pieces > 1 ? tiles * Shape<true>::kTileFloats * 4 : 0);
+    l.parts = take(!dh ? 0 : (size_t)2 * 4 * (M <= kBM ? kMaxSms * Shape<kSingle>::kTileFloats : kMaxSms / 2 * Shape<kWide>::kTileFloats));
+    // (whole tiles, in either layout)
+    const size_t up_k = (size_t)(K + 511) / 512 * 512, up_v = (size_t)(V + 511) / 512 * 512;
+    l.sums = take(dw && l.pieces > 1 ? up_k * up_v * 4 : 0);
     l.bytes = at;
     return l;
 }
@@ -1028,16 +1053,17 @@ static int sms_of_device(int *sms)
     return PPO_OK;
 }
 
-template <bool PAIR, bool A_MN, bool B_MN, int PRODUCT>
+template <int MODE, bool A_MN, bool B_MN, int PRODUCT>
 static int launch_product(const CUtensorMap &ma, const CUtensorMap &ma_all, const CUtensorMap &mb, const CUtensorMap &mo, const Args &a,
                           int sms, cudaStream_t s)
 {
-    auto kern = product_kernel<PAIR, A_MN, B_MN, PRODUCT>;
-    PPO_RETURN_IF_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<PAIR>::kSmem));
+    constexpr bool PAIR = Shape<MODE>::kIsPair;
+    auto kern = product_kernel<MODE, A_MN, B_MN, PRODUCT>;
+    PPO_RETURN_IF_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<MODE>::kSmem));
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(PAIR ? sms / 2 * 2 : sms));
     cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = Shape<PAIR>::kSmem;
+    cfg.dynamicSmemBytes = Shape<MODE>::kSmem;
     cfg.stream = s;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -1063,25 +1089,63 @@ struct Maps {
     CUtensorMap packed, h, w1, w2, u_out, u2, u3, scaled, dw;
 };
 
-template <bool PAIR>
-static int launch_piece(const Maps &m, const RowArgs &r, const Args &a1, const Args &a2, const Args &a3, bool vk, bool dh, bool dw, int sms,
+template <int MODE>
+static int launch_hidden(const Maps &m, const Args &a2, bool vk, int sms, cudaStream_t s)
+{
+    const int rc = vk ? launch_product<MODE, false, true, kHidden>(m.u2, m.u2, m.w2, m.u2, a2, sms, s)
+                      : launch_product<MODE, false, false, kHidden>(m.u2, m.u2, m.w2, m.u2, a2, sms, s);
+    if (rc) return rc;
+    const int workers = Shape<MODE>::kIsPair ? sms / 2 : sms;
+    PPO_RETURN_IF_CUDA(launch_dependent(join_kernel<MODE>,
+                                        dim3((unsigned)((workers - 1) * join_blocks<MODE>())), dim3(kJoinThreads), 0, s, a2, workers));
+    return PPO_OK;
+}
+
+template <int MODE>
+static int launch_weight(const Maps &m, const Args &a3, bool vk, int sms, cudaStream_t s)
+{
+    return vk ? launch_product<MODE, true, true, kWeight>(m.u3, m.u3, m.scaled, m.dw, a3, sms, s)
+              : launch_product<MODE, true, true, kWeight>(m.scaled, m.scaled, m.u3, m.dw, a3, sms, s);
+}
+
+// Wide tiles where they are half as many, the contraction is at least 64 blocks long (their epilogue, 6000 cycles for two
+// accumulators, has to be small against 1024 a block) and the pairs get two tiles or more each (6912 x 4096 x 50304: dH
+// 1973 us against 2049, dW 2017 against 2077; 1792 rows, whose 56 wide tiles are all cut: dH 598 against 544).
+static bool wide(int64_t m, int64_t n, int64_t contraction, int sms)
+{
+    return (n + 255) / 256 % 2 == 0 && contraction >= 64 * kBlockK && (m + 255) / 256 * ((n + 511) / 512) >= sms;
+}
+
+static int launch_piece(const Maps &m, const RowArgs &r, const Args &a1, Args a2, Args a3, bool single, bool vk, bool dh, bool dw, int sms,
                         cudaStream_t s)
 {
-    int rc = vk ? launch_product<PAIR, false, false, kLogits>(m.packed, m.h, m.w1, m.u_out, a1, sms, s)
-                : launch_product<PAIR, false, true, kLogits>(m.packed, m.h, m.w1, m.u_out, a1, sms, s);
+    int rc;
+    if (single)
+        rc = vk ? launch_product<kSingle, false, false, kLogits>(m.packed, m.h, m.w1, m.u_out, a1, sms, s)
+                : launch_product<kSingle, false, true, kLogits>(m.packed, m.h, m.w1, m.u_out, a1, sms, s);
+    else
+        rc = vk ? launch_product<kPair, false, false, kLogits>(m.packed, m.h, m.w1, m.u_out, a1, sms, s)
+                : launch_product<kPair, false, true, kLogits>(m.packed, m.h, m.w1, m.u_out, a1, sms, s);
     if (rc) return rc;
     PPO_RETURN_IF_CUDA(launch_dependent(row_kernel, dim3((unsigned)r.rows_max), dim3(kRowThreads), 0, s, r));
     if (dh) {
-        rc = vk ? launch_product<PAIR, false, true, kHidden>(m.u2, m.u2, m.w2, m.u2, a2, sms, s)
-                : launch_product<PAIR, false, false, kHidden>(m.u2, m.u2, m.w2, m.u2, a2, sms, s);
+        if (!single && wide(a2.dim_m, a2.dim_n, a2.dim_k, sms)) {
+            a2.gm = 12;
+            a2.gn = 6;
+            rc = launch_hidden<kWide>(m, a2, vk, sms, s);
+        } else {
+            rc = single ? launch_hidden<kSingle>(m, a2, vk, sms, s) : launch_hidden<kPair>(m, a2, vk, sms, s);
+        }
         if (rc) return rc;
-        const int workers = PAIR ? sms / 2 : sms;
-        PPO_RETURN_IF_CUDA(launch_dependent(vk ? join_kernel<PAIR, true> : join_kernel<PAIR, false>,
-                                            dim3((unsigned)((workers - 1) * join_blocks<PAIR>())), dim3(kJoinThreads), 0, s, a2, workers));
     }
     if (!dw) return PPO_OK;
-    return vk ? launch_product<PAIR, true, true, kWeight>(m.u3, m.u3, m.scaled, m.dw, a3, sms, s)
-              : launch_product<PAIR, true, true, kWeight>(m.scaled, m.scaled, m.u3, m.dw, a3, sms, s);
+    // (the number of pieces does not change the mode: their sums lie in its order)
+    if (!single && wide(a3.dim_m, a3.dim_n, a3.dim_k, sms)) {
+        a3.gm = 12;
+        a3.gn = 6;
+        return launch_weight<kWide>(m, a3, vk, sms, s);
+    }
+    return single ? launch_weight<kSingle>(m, a3, vk, sms, s) : launch_weight<kPair>(m, a3, vk, sms, s);
 }
 
 constexpr int64_t kLimit = ((int64_t)1 << 31) - 16384;
@@ -1132,13 +1196,15 @@ extern "C" int ppo_lmhead_xent(const void *H, int64_t ldh, const void *W, int64_
     if (rc) return rc;
     const Layout l = layout_of(M, K, V, piece_rows, dH != nullptr, dW != nullptr);
     unsigned char *mem = reinterpret_cast<unsigned char *>(scratch);
-    const bool grad = dH || dW, pair = M > kBM;
+    const bool grad = dH || dW;
 
     RowArgs r = {};
     r.H = reinterpret_cast<const __nv_bfloat16 *>(H);
     r.ldh = ldh; r.lddh = lddh; r.M = (int)M; r.K = (int)K; r.V = (int)V; r.Kp = l.Kp;
     r.labels = labels; r.mask = mask; r.ignore_id = ignore_id;
-    r.c = kLog2e / temperature; r.inv_tau = 1.f / temperature; r.scale = scale; r.denom = denom;
+    // The tensor cores cut off the sums that they keep: logits that grow evenly over the hidden elements come out smaller by 8.3e-10
+    // of themselves per element (measured, K = 64 to 4096), which is made up for here (lse at K = 4096: 2.6e-6 off without, 4e-7 with).
+    r.c = (float)(1.4426950408889634 / (double)temperature * (1.0 + 8.3e-10 * (double)K)); r.inv_tau = 1.f / temperature; r.scale = scale; r.denom = denom;
     r.n_real = reinterpret_cast<int *>(mem + l.n_real);
     r.order = reinterpret_cast<int32_t *>(mem + l.order);
     r.W = reinterpret_cast<const __nv_bfloat16 *>(W); r.ldw = ldw; r.vk = vk;
@@ -1157,7 +1223,7 @@ extern "C" int ppo_lmhead_xent(const void *H, int64_t ldh, const void *W, int64_
     r.status = status;
 
     Maps m = {};
-    const int rows_b = Shape<true>::kRowsB;                     // a block's share of B, stored by rows
+    const int rows_b = Shape<kPair>::kRowsB;                    // a block's share of B, stored by rows
     if ((rc = make_map_pitch(&m.packed, r.packed, (uint64_t)K, (uint64_t)M, (uint64_t)l.Kp, kBM))) return rc;
     if ((rc = make_map_pitch(&m.h, H, (uint64_t)K, (uint64_t)M, (uint64_t)ldh, kBM))) return rc;
     // product 1 takes W with the vocabulary as the result's columns, product 2 with the hidden size
@@ -1176,7 +1242,7 @@ extern "C" int ppo_lmhead_xent(const void *H, int64_t ldh, const void *W, int64_
     Args a1 = a, a2 = a, a3 = a;
     a1.dim_m = l.rows_max; a1.dim_n = (int)V; a1.dim_k = (int)K; a1.gm = 9; a1.gn = 8;
     a2.dim_m = l.rows_max; a2.dim_n = (int)K; a2.dim_k = (int)V; a2.gm = 9; a2.gn = 8;
-    a2.out = r.dH; a2.ldo = lddh; a2.W = reinterpret_cast<const __nv_bfloat16 *>(W); a2.ldw = ldw;
+    a2.out = r.dH; a2.ldo = lddh; a2.w_mean = r.w_mean;
     a2.scratch = reinterpret_cast<float *>(mem + l.parts);
     a3.dim_m = (int)w_outer; a3.dim_n = (int)w_inner; a3.dim_k = l.rows_max; a3.gm = 8; a3.gn = 9;
     a3.out = reinterpret_cast<__nv_bfloat16 *>(dW); a3.ldo = lddw;
@@ -1196,8 +1262,7 @@ extern "C" int ppo_lmhead_xent(const void *H, int64_t ldh, const void *W, int64_
     PPO_RETURN_IF_CUDA(launch_dependent(pack_kernel, dim3((unsigned)M), dim3(kRowThreads), 0, s, r));
     for (int p = 0; p < l.pieces; ++p) {
         r.row0 = a1.row0 = a2.row0 = a3.row0 = p * l.rows_max;
-        rc = pair ? launch_piece<true>(m, r, a1, a2, a3, vk, dH != nullptr, dW != nullptr, sms, s)
-                  : launch_piece<false>(m, r, a1, a2, a3, vk, dH != nullptr, dW != nullptr, sms, s);
+        rc = launch_piece(m, r, a1, a2, a3, M <= kBM, vk, dH != nullptr, dW != nullptr, sms, s);
         if (rc) return rc;
     }
     PPO_RETURN_IF_CUDA(launch_dependent(loss_kernel, dim3(1), dim3(kLossThreads), 0, s, r));

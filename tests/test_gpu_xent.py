@@ -4,8 +4,9 @@ Tolerances, element by element. A logit is a sum of K products in fp32, each add
 (rounded or cut off): ez = (K + 4) 2^-23 max_j sum_k |h_k w_kj| / tau, and its scaling to base 2 adds 2^-23 of its size. The log-sum-exp
 moves by at most the largest of these; its own sum of up to 128 exponentials (2^-22 each), joined over the chunks, adds less than
 (128 + chunks) 2^-23. U is off by those, relative, and by half a step of bf16 (2^-8); the sum of the rounded U, which divides it, by another
-half step at most: two for dH, in the worst case, and as much for 1 - p at the label. In dW a H adds half a step and the factor that
-makes U at the label exact one more. Results are off by half a step of their own; the products over V columns or M rows by (V + 4) 2^-23 and
+half step at most: two in the worst case, and as much for 1 - p at the label; the factor that makes U at the label exact adds one to the others.
+In dW a H adds another. In dH, c times a mean of columns of W adds at most half a step of D at the label times the row's largest |w|. Results
+are off by half a step of their own; the products over V columns or M rows by (V + 4) 2^-23 and
 (M + 4) 2^-23 of the sums of the absolute products."""
 import numpy as np
 import pytest
@@ -68,7 +69,9 @@ def check(o, H, W, labels, real, tau, scale=1.0, denom=None):
         p[r, npy(labels)[r]] = abs(scale) / (d * tau) * er[r, 0]
     tiny = 2.0 ** -120
     if o["dH"] is not None:
-        tol = (2 * STEP * D + p) @ np.abs(w).T + (V + 4) * EPS * (D @ np.abs(w).T) + STEP * np.abs(want["dH"]) + tiny
+        at = np.clip(npy(labels), 0, V - 1)
+        tol = (3 * STEP * D + p) @ np.abs(w).T + (V + 4) * EPS * (D @ np.abs(w).T) + STEP * np.abs(want["dH"]) + tiny
+        tol += STEP * D[np.arange(M), at][:, None] * np.abs(w).max(1)
         assert (np.abs(f64(o["dH"]) - want["dH"]) <= 1.01 * tol).all()
         assert not f64(o["dH"])[~real].any()
     if o["dW"] is not None:
