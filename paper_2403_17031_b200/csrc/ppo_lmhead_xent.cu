@@ -91,6 +91,7 @@ struct Args {
     // kHidden
     const float2 *row_scale;                               // [rows] a, c
     const float *w_mean;                                   // [K, in whole tiles]
+    const int2 *slices;                                    // of the tiles that are left over, and their length
     float *scratch;                                        // kHidden: parts of tiles cut along the contraction; kWeight: sums over the pieces
 };
 
@@ -115,11 +116,13 @@ struct Smem {
     uint32_t tmem_base;
 };
 
-// The workers (pairs, or blocks) take tiles 0 .. n_whole in turn, whole. With `share` > 0 the other tiles, too few for all, are
-// cut along the contraction: end to end they are n_rest * kbs blocks, of which worker c takes share, from c * share on (at
-// most two tiles), and join_kernel adds the parts up in the order of the workers.
+// The workers (pairs, or blocks) take tiles 0 .. n_whole in turn, whole, and then the slices along the contraction of the other
+// tiles, which are too few for all workers: first slices of all of them, second slices, ... so that workers that run at the
+// same time read the same blocks of their operands, through L2. (Cut end to end into equal shares, with each worker at a
+// place of its own, 38 tiles over for 74 pairs came at 1100 cycles a block instead of 600, from memory.) A slice's sums go
+// to scratch, and join_kernel adds them up in order.
 struct Plan {
-    int m_tiles, n_tiles, n_whole, n_rest, share, kbs;
+    int m_tiles, n_tiles, n_whole, n_rest, slices, length, kbs;     // length: of a slice, in blocks of the contraction
 };
 
 template <int MODE, int PRODUCT>
@@ -131,49 +134,40 @@ __device__ __forceinline__ Plan plan_of(const Args &a, int rows, int workers)
     p.n_tiles = (a.dim_n + Shape<MODE>::kN - 1) / Shape<MODE>::kN;
     p.kbs = ((PRODUCT == kWeight ? rows : a.dim_k) + kBlockK - 1) / kBlockK;
     p.n_whole = p.m_tiles * p.n_tiles;
-    p.n_rest = p.share = 0;
+    p.n_rest = 0;
+    p.slices = 1;
+    p.length = p.kbs;
     if (PRODUCT == kWeight && rows == 0 && a.row0 > 0) p.n_whole = 0;      // nothing to add
-    if (PRODUCT == kHidden) {
-        // Cut when that saves each worker enough blocks of the contraction: 24, and two a tile for the joining and for the
-        // operands that tiles at different places of the contraction do not share through L2 (62 pairs' tiles left of 432 at
-        // 6912 x 4096 x 50304, 127 blocks saved: 2250 us cut, 2130 whole).
-        const int rest = p.n_whole % workers, share = (int)(((int64_t)rest * p.kbs + workers - 1) / workers);
-        if (rest > 0 && p.kbs - share >= 24 + 2 * rest) {
-            p.n_rest = rest;
-            p.n_whole -= rest;
-            p.share = share;
-        }
+    if (PRODUCT == kHidden && a.slices->x > 1) {
+        p.n_rest = p.n_whole % workers;
+        p.slices = a.slices->x;
+        p.length = a.slices->y;
+        p.n_whole -= p.n_rest;
     }
     return p;
 }
 
 struct Work {
     int u, kb0, kb1;      // tile, blocks of the contraction
-    int part;             // -1: whole; else which of the worker's parts
-    int u_next, r, r_end;
-    __device__ __forceinline__ void init(const Plan &p, int worker)
-    {
-        u_next = worker;
-        r = min(worker * p.share, p.n_rest * p.kbs);
-        r_end = min(r + p.share, p.n_rest * p.kbs);
-        part = -1;
-    }
+    int part;             // -1: whole; else the slice's place in scratch
+    int next_unit;
+    __device__ __forceinline__ void init(int worker) { next_unit = worker; }
     __device__ __forceinline__ bool next(const Plan &p, int workers)
     {
-        if (u_next < p.n_whole) {
-            u = u_next;
-            u_next += workers;
-            kb0 = 0;
-            kb1 = p.kbs;
+        u = next_unit;
+        part = u - p.n_whole;
+        next_unit += workers;
+        kb0 = 0;
+        kb1 = p.kbs;
+        if (part < 0) {
+            part = -1;
             return true;
         }
-        if (r >= r_end) return false;
-        const int t = r / p.kbs;
-        u = p.n_whole + t;
-        kb0 = r - t * p.kbs;
-        kb1 = min(p.kbs, kb0 + r_end - r);
-        r += kb1 - kb0;
-        ++part;
+        if (part >= p.n_rest * p.slices) return false;
+        const int slice = part / p.n_rest;
+        u = p.n_whole + part - slice * p.n_rest;
+        kb0 = slice * p.length;
+        kb1 = min(p.kbs, kb0 + p.length);
         return true;
     }
 };
@@ -271,7 +265,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     const int rows = rows_of(a);
     const Plan plan = plan_of<MODE, PRODUCT>(a, rows, workers);
     Work work;
-    work.init(plan, worker);
+    work.init(worker);
 
     if (warp == 0) {
         if (lane == 0) {
@@ -566,7 +560,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                 if (ok && n < a.dim_n) a.part[(size_t)row * a.chunks + n / kChunk] = make_float4(ref, s, rounded, 0.f);
             } else if (PRODUCT == kHidden) {
                 // (four columns of a tile's rows follow one another in scratch: a warp writes 512 bytes at a time)
-                float4 *part = reinterpret_cast<float4 *>(a.scratch + (size_t)(worker * 2 + max(work.part, 0)) * S::kTileFloats) +
+                float4 *part = reinterpret_cast<float4 *>(a.scratch + (size_t)max(work.part, 0) * S::kTileFloats) +
                                (half_tile * 64 + h * 32) * S::kM + rank * kBM + q * 32 + lane;
 #pragma unroll 1
                 for (int half = 0; half < 2; ++half) {
@@ -634,8 +628,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     }
 }
 
-// The tiles of dH that were cut along the vocabulary: a block adds up 32 rows x 64 columns over the pairs that hold parts of
-// them, in the order of the contraction, and turns them in shared memory so that rows leave in runs.
+// The tiles of dH that were cut along the vocabulary: a block adds up 32 rows x 64 columns of their slices, in order, and turns them in shared memory so that rows leave in runs.
 constexpr int kJoinThreads = 256;
 template <int MODE> constexpr int join_blocks() { return (Shape<MODE>::kM / 32) * (Shape<MODE>::kN / 64); }
 template <int MODE>
@@ -654,14 +647,12 @@ join_kernel(const Args a, int workers)
     const int2 t = tile_of(p.n_whole + rest, p.m_tiles, p.n_tiles, a.gm, a.gn);
     const int m0 = t.x * kM + row0, n0 = t.y * Shape<MODE>::kN + j0 * 4;
     if (m0 >= rows || n0 >= a.dim_n) return;
-    const int first = (int)((int64_t)rest * p.kbs / p.share), last = (int)(((int64_t)(rest + 1) * p.kbs - 1) / p.share);
     const int lane = threadIdx.x & 31, jj = threadIdx.x >> 5;
     float4 v[2];
     v[0] = v[1] = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
-    for (int c = first; c <= last; ++c) {
-        const int part = rest - (int)((int64_t)c * p.share / p.kbs);     // the worker's first or second tile
-        const float4 *from = reinterpret_cast<const float4 *>(a.scratch + (size_t)(c * 2 + part) * kTileFloats) + row0 + lane;
+    for (int i = 0; i < p.slices; ++i) {
+        const float4 *from = reinterpret_cast<const float4 *>(a.scratch + (size_t)(i * p.n_rest + rest) * kTileFloats) + row0 + lane;
         const float4 x = from[(j0 + jj) * kM], y = from[(j0 + jj + 8) * kM];
         v[0].x += x.x; v[0].y += x.y; v[0].z += x.z; v[0].w += x.w;
         v[1].x += y.x; v[1].y += y.y; v[1].z += y.z; v[1].w += y.w;
@@ -713,6 +704,8 @@ struct RowArgs {
     float2 *row_scale;
     float4 *part;
     int chunks, row0, rows_max;
+    int tile_m, n_tiles, workers, kbs;                          // product 2: tile rows, tiles along K, workers, blocks along V
+    int2 *slices;
     float *loss, *nll, *lse;
     __nv_bfloat16 *dH;
     int *status;
@@ -881,6 +874,28 @@ pack_kernel(const RowArgs a)
     }
 }
 
+// How the tiles of product 2 that are too few for all workers are sliced: rounds x length, and for the joining 20 blocks' time
+// and that of one block for six slices, is least; scratch holds two tiles a worker. By one block, a thread for each number.
+__device__ __forceinline__ void choose_slices(const RowArgs &a, int rows)
+{
+    __shared__ unsigned best[kRowThreads / 32];
+    const int rest = (rows + a.tile_m - 1) / a.tile_m * a.n_tiles % a.workers;
+    unsigned mine = (unsigned)min(a.kbs, 1 << 20) << 10 | 1u;           // whole
+    for (int s = threadIdx.x + 2; rest > 0 && rest * s <= 2 * a.workers && s <= a.kbs; s += kRowThreads) {
+        const int length = (a.kbs + s - 1) / s, n = (a.kbs + length - 1) / length;       // (none empty)
+        const int cost = (rest * n + a.workers - 1) / a.workers * length + 20 + rest * n / 6;
+        mine = min(mine, (unsigned)min(cost, 1 << 20) << 10 | (unsigned)n);
+    }
+    mine = __reduce_min_sync(0xffffffffu, mine);
+    if ((threadIdx.x & 31) == 0) best[threadIdx.x >> 5] = mine;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int w = 1; w < kRowThreads / 32; ++w) mine = min(mine, best[w]);
+        const int n = (int)(mine & 1023u), length = (a.kbs + n - 1) / n;
+        *a.slices = make_int2(n, length);
+    }
+}
+
 // A row's statistics out of its chunks', its loss and the factors of its gradient; U at the label; a H
 __global__ void __launch_bounds__(kRowThreads)
 row_kernel(const RowArgs a)
@@ -888,7 +903,11 @@ row_kernel(const RowArgs a)
     __shared__ float red[3][kRowThreads / 32];
     grid_dependents_may_launch();
     grid_dependency_wait();
-    const int n_real = *a.n_real, rows = max(0, min(a.rows_max, n_real - a.row0)), r = blockIdx.x;
+    const int n_real = *a.n_real, rows = max(0, min(a.rows_max, n_real - a.row0)), r = (int)blockIdx.x - 1;
+    if (r < 0) {
+        choose_slices(a, rows);
+        return;
+    }
     __nv_bfloat16 *scaled = a.scaled ? a.scaled + (int64_t)r * a.Kp : nullptr;
     if (r >= rows) {
         // up to the next block of the contraction: zeros that product 3 reads (U has its own)
@@ -1000,7 +1019,7 @@ constexpr int kPieceRows = 256;                                 // a piece is a 
 struct Layout {
     int pieces, rows_max, chunks, Kp;
     int64_t Vp;
-    size_t n_real, order, info, w_mean, picked, row_scale, part, packed, scaled, u, parts, sums, bytes;
+    size_t n_real, slices, order, info, w_mean, picked, row_scale, part, packed, scaled, u, parts, sums, bytes;
 };
 
 // Pieces of at most 8192 rows by default: at V = 50304 that is 824 MB of U, and the sums of dW, read and written once a
@@ -1026,6 +1045,7 @@ static Layout layout_of(int64_t M, int64_t K, int64_t V, int64_t piece_rows, boo
     const bool grad = dh || dw;
     const size_t rows = (size_t)l.rows_max;
     l.n_real = take(4);
+    l.slices = take(8);
     l.order = take((size_t)M * 4);
     l.info = take((size_t)M * sizeof(int2));
     l.w_mean = take((size_t)(K + 511) / 512 * 512 * 4);
@@ -1116,7 +1136,17 @@ static bool wide(int64_t m, int64_t n, int64_t contraction, int sms)
     return (n + 255) / 256 % 2 == 0 && contraction >= 64 * kBlockK && (m + 255) / 256 * ((n + 511) / 512) >= sms;
 }
 
-static int launch_piece(const Maps &m, const RowArgs &r, const Args &a1, Args a2, Args a3, bool single, bool vk, bool dh, bool dw, int sms,
+template <int MODE>
+static void set_shape(RowArgs &r, const Args &a2, int sms)
+{
+    using S = Shape<MODE>;
+    r.tile_m = S::kM;
+    r.n_tiles = (a2.dim_n + S::kN - 1) / S::kN;
+    r.workers = S::kIsPair ? sms / 2 : sms;
+    r.kbs = (a2.dim_k + kBlockK - 1) / kBlockK;
+}
+
+static int launch_piece(const Maps &m, RowArgs r, const Args &a1, Args a2, Args a3, bool single, bool vk, bool dh, bool dw, int sms,
                         cudaStream_t s)
 {
     int rc;
@@ -1127,9 +1157,13 @@ static int launch_piece(const Maps &m, const RowArgs &r, const Args &a1, Args a2
         rc = vk ? launch_product<kPair, false, false, kLogits>(m.packed, m.h, m.w1, m.u_out, a1, sms, s)
                 : launch_product<kPair, false, true, kLogits>(m.packed, m.h, m.w1, m.u_out, a1, sms, s);
     if (rc) return rc;
-    PPO_RETURN_IF_CUDA(launch_dependent(row_kernel, dim3((unsigned)r.rows_max), dim3(kRowThreads), 0, s, r));
+    const bool wide_hidden = !single && wide(a2.dim_m, a2.dim_n, a2.dim_k, sms);
+    if (single) set_shape<kSingle>(r, a2, sms);
+    else if (wide_hidden) set_shape<kWide>(r, a2, sms);
+    else set_shape<kPair>(r, a2, sms);
+    PPO_RETURN_IF_CUDA(launch_dependent(row_kernel, dim3(1 + (unsigned)r.rows_max), dim3(kRowThreads), 0, s, r));
     if (dh) {
-        if (!single && wide(a2.dim_m, a2.dim_n, a2.dim_k, sms)) {
+        if (wide_hidden) {
             a2.gm = 12;
             a2.gn = 6;
             rc = launch_hidden<kWide>(m, a2, vk, sms, s);
@@ -1243,6 +1277,7 @@ extern "C" int ppo_lmhead_xent(const void *H, int64_t ldh, const void *W, int64_
     a1.dim_m = l.rows_max; a1.dim_n = (int)V; a1.dim_k = (int)K; a1.gm = 9; a1.gn = 8;
     a2.dim_m = l.rows_max; a2.dim_n = (int)K; a2.dim_k = (int)V; a2.gm = 9; a2.gn = 8;
     a2.out = r.dH; a2.ldo = lddh; a2.w_mean = r.w_mean;
+    a2.slices = r.slices = reinterpret_cast<int2 *>(mem + l.slices);
     a2.scratch = reinterpret_cast<float *>(mem + l.parts);
     a3.dim_m = (int)w_outer; a3.dim_n = (int)w_inner; a3.dim_k = l.rows_max; a3.gm = 8; a3.gn = 9;
     a3.out = reinterpret_cast<__nv_bfloat16 *>(dW); a3.ldo = lddw;
