@@ -226,3 +226,62 @@ class Fp8LMHead:
 
     def device_status(self) -> int:
         return _b.last_device_status(self.workspace)
+
+
+class SFTStep:
+    """The vocabulary-sized parts of one supervised fine-tuning step (the paper's first stage, before the reward model and PPO):
+    the model's input out of the embedding table, cross entropy at the LM head with its gradients, the gradient of the table,
+    and the clipping of all gradients by their common norm. The model between embed() and loss() is the caller's, and so are
+    the weights and the optimiser. Everything runs on the current CUDA stream and can be captured into a CUDA graph; results
+    are this object's buffers, overwritten by the next step.
+
+    W [K, V] is the LM head's weight, stored by rows or by columns (the transpose of a linear layer's weight): its gradient is
+    stored the same way. N: positions of a batch. grad_dtype: of the table's gradient."""
+
+    def __init__(self, W: torch.Tensor, N: int, padding_id: int = -1, ignore_id: int = -100, temperature: float = 1.0,
+                 embed_scale: float = 1.0, grad_dtype: torch.dtype = torch.bfloat16, piece_rows: int = 0):
+        K, V = W.shape
+        self.N, self.K, self.V = N, K, V
+        self.padding_id, self.ignore_id, self.temperature = padding_id, ignore_id, float(temperature)
+        self.embed_scale, self.piece_rows = float(embed_scale), piece_rows
+        dev, f32, bf16, u8 = W.device, torch.float32, torch.bfloat16, torch.uint8
+        self.workspace = _b.new_workspace(_b.workspace_bytes(N, 1, V), dev)
+        scratch = lambda n: torch.empty(max(n, 256), dtype=u8, device=dev)          # noqa: E731
+        # (one buffer: the two calls that need it do not overlap)
+        self._scratch = scratch(max(_b.lmhead_xent_scratch_bytes(N, K, V, piece_rows), _b.embed_bwd_scratch_bytes(N, K, V)))
+        self._clip_scratch = None
+        self.out = {"hidden": torch.empty((N, K), dtype=bf16, device=dev), "loss": torch.empty((), dtype=f32, device=dev),
+                    "nll": torch.empty(N, dtype=f32, device=dev), "lse": torch.empty(N, dtype=f32, device=dev),
+                    "dH": torch.empty((N, K), dtype=bf16, device=dev), "dW": torch.empty_like(W),
+                    "dE": torch.empty((V, K), dtype=grad_dtype, device=dev), "norm": torch.empty(2, dtype=f32, device=dev)}
+
+    def embed(self, table, tokens):
+        """Rows of the table [V, K] for tokens [N] int32, times embed_scale, in bf16."""
+        return _b.embed(table, tokens, scale=self.embed_scale, workspace=self.workspace, out=self.out["hidden"])
+
+    def loss(self, H, W, labels, mask=None, scale: float = 1.0):
+        """Mean cross entropy of labels [N] under the head's logits for the hidden states H [N, K], without masked rows and
+        ignored labels; dH and dW are the gradients of scale * loss. Returns the dict of buffers."""
+        o = self.out
+        _b.lmhead_xent(H, W, labels, mask=mask, ignore_id=self.ignore_id, temperature=self.temperature, scale=scale,
+                       piece_rows=self.piece_rows, workspace=self.workspace, scratch=self._scratch,
+                       out={n: o[n] for n in ("loss", "nll", "lse", "dH", "dW")})
+        return o
+
+    def grad_embed(self, dX, tokens, accumulate: bool = False):
+        """Gradient dX [N, K] on embed()'s result -> gradient of the table (accumulate: added to the one there is)."""
+        return _b.embed_bwd(dX, tokens, self.V, scale=self.embed_scale, padding_id=self.padding_id, accumulate=accumulate,
+                            workspace=self.workspace, scratch=self._scratch, out=self.out["dE"])
+
+    def clip(self, max_norm: float, others=(), scale: float = 1.0):
+        """Clips dW, dE and the model's other gradients together, in place. Returns [norm before clipping, factor]."""
+        o = self.out
+        dW = o["dW"] if o["dW"].is_contiguous() else o["dW"].t()                    # (the same elements, in memory's order)
+        grads = [dW, o["dE"], *others]
+        need = _b.grad_clip_scratch_bytes(len(grads))
+        if self._clip_scratch is None or self._clip_scratch.numel() < need:
+            self._clip_scratch = torch.empty(need, dtype=torch.uint8, device=o["norm"].device)
+        return _b.grad_clip(grads, max_norm, scale=scale, workspace=self.workspace, scratch=self._clip_scratch, norm=o["norm"])
+
+    def device_status(self) -> int:
+        return _b.last_device_status(self.workspace)
