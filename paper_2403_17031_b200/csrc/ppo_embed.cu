@@ -155,8 +155,10 @@ __device__ __forceinline__ void fill_rows(const BwdArgs &a, int block)
 __device__ __forceinline__ int key_of(const BwdArgs &a, int t) { return t < 0 || t >= a.V || t == a.padding_id ? (int)a.V : t; }
 
 // ---------------------------------------------------------------- a handful of positions: one launch, no sorting
-// A block owns a few rows. It looks all tokens through for them, in order, and writes its rows: sums or zeros.
-constexpr int kDirectMax = 256, kDirectRows = 16;
+// A block owns a few rows. It looks all tokens through for them, in order, and writes its rows: sums or zeros. (A third of the
+// positions of text are of one block's rows: 300 positions x 1024 take 57 us in this form, 38 sorted.)
+constexpr int kDirectMax = 128, kDirectRows = 16;
+static_assert(kDirectMax <= kThreads, "a thread for each position");
 template <typename TI, typename TO, int VEC>
 __global__ void __launch_bounds__(kThreads)
 direct_kernel(const BwdArgs a)
@@ -276,16 +278,21 @@ rank_kernel(const BwdArgs a, int32_t *__restrict__ key_out, int32_t *__restrict_
     }
 }
 
+// Tiles up to which each block sums the counts itself, instead of a launch for it (20000 positions: 57 us with the launches).
+constexpr int kSumTiles = 128, kAheadTiles = 16;
+
 // More: least significant digit first, 8 bits a pass, each pass stable: digits counted per tile, the counts summed in digit
-// order, the tile's entries moved. A warp owns neighbouring entries of a tile. A pass that moves an entry counts it for the
-// next one, whose tile it knows, so that only the first pass has a launch for counting.
+// order, the tile's entries moved. A warp owns neighbouring entries of a tile. With few tiles a pass that moves an entry counts
+// it for the next one, whose tile it knows, and saves that pass the launch for counting (150000 positions: 35 us a pass so, 13 and 6 for
+// the launch without).
 constexpr int kTile = 2048, kDigits = 256, kWarps = kThreads / 32, kPerWarp = kTile / kWarps;
 
 struct PassArgs {
     const int32_t *key_in, *pos_in;      // null in the first pass
     int32_t *key_out, *pos_out;
-    int32_t *counts, *next_counts;       // [kDigits][tiles]; next_counts null in the last pass
-    int tiles, shift;
+    int32_t *counts, *next_counts;       // [kDigits][pitch], zeros behind the tiles; next_counts null in the last pass
+    int tiles, pitch, shift;
+    int summed;                          // the counts have been summed up (many tiles)
 };
 
 __device__ __forceinline__ void load_entry(const BwdArgs &a, const PassArgs &p, int i, int &key, int &pos)
@@ -308,24 +315,27 @@ count_kernel(const BwdArgs a, const PassArgs p)
     for (int j = 0; j < kSeen; j += kThreads) seen[j + threadIdx.x] = -1;
     constexpr int R = kTile / kThreads;
     const int i0 = blockIdx.x * kTile + threadIdx.x;
+    // (the first pass takes the tokens, the others keys that have been noted)
     int t[R];
+    if (p.key_in) grid_dependency_wait();
+    const int32_t *from = p.key_in ? p.key_in : a.tokens;
 #pragma unroll
-    for (int j = 0; j < R; ++j) t[j] = i0 + j * kThreads < a.N ? a.tokens[i0 + j * kThreads] : 0;
+    for (int j = 0; j < R; ++j) t[j] = i0 + j * kThreads < a.N ? from[i0 + j * kThreads] : 0;
     __syncthreads();
 #pragma unroll
     for (int j = 0; j < R; ++j) {
         const bool in = i0 + j * kThreads < a.N;
-        const int key = key_of(a, t[j]), digit = in ? key & (kDigits - 1) : kDigits;
+        const int key = p.key_in ? t[j] : key_of(a, t[j]), digit = in ? (key >> p.shift) & (kDigits - 1) : kDigits;
         const unsigned same = __match_any_sync(0xffffffffu, digit);
         if (in && (same & ((1u << (threadIdx.x & 31)) - 1)) == 0) atomicAdd(&n[digit], __popc(same));
         // (all that counts for no row has one key: of those each is looked at)
-        if (in && (key >= a.V || seen[key & (kSeen - 1)] != key)) {
+        if (in && !p.key_in && (key >= a.V || seen[key & (kSeen - 1)] != key)) {
             seen[key & (kSeen - 1)] = key;
             note_token(a, t[j], key);
         }
     }
     __syncthreads();
-    p.counts[(size_t)threadIdx.x * p.tiles + blockIdx.x] = n[threadIdx.x];
+    p.counts[(size_t)threadIdx.x * p.pitch + blockIdx.x] = n[threadIdx.x];
 }
 
 // exclusive sum over the counts, in place; one block
@@ -342,7 +352,7 @@ scan_kernel(const BwdArgs a, const PassArgs p)
     }
     __shared__ int warp_sum[32];
     __shared__ int carry;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n = p.tiles * kDigits;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n = p.pitch * kDigits;
     int4 *counts = reinterpret_cast<int4 *>(p.counts);          // (kDigits counts a tile: a multiple of 8)
     if (threadIdx.x == 0) carry = 0;
     __syncthreads();
@@ -412,7 +422,34 @@ scatter_kernel(const BwdArgs a, const PassArgs p)
     }
     __syncthreads();
     {   // the warps' first places of each digit
-        int run = p.counts[(size_t)threadIdx.x * p.tiles + blockIdx.x];
+        int run;
+        const int32_t *mine = p.counts + (size_t)threadIdx.x * p.pitch;
+        if (p.summed) {
+            run = mine[blockIdx.x];
+        } else {
+            // a thread for a digit: its count in the tiles before this one and in all; then the digits before it
+            __shared__ int warp_sum[kWarps];
+            int total = 0;
+            run = 0;
+#pragma unroll 4
+            for (int t = 0; t < p.pitch; t += 4) {
+                const int4 c = *reinterpret_cast<const int4 *>(mine + t);
+                total += c.x + c.y + c.z + c.w;
+                const int b = (int)blockIdx.x - t;
+                run += (b > 0 ? c.x : 0) + (b > 1 ? c.y : 0) + (b > 2 ? c.z : 0) + (b > 3 ? c.w : 0);
+            }
+            int incl = total;
+#pragma unroll
+            for (int off = 1; off < 32; off <<= 1) {
+                const int o = __shfl_up_sync(0xffffffffu, incl, off);
+                if (lane >= off) incl += o;
+            }
+            if (lane == 31) warp_sum[warp] = incl;
+            __syncthreads();
+            run += incl - total;
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) run += w < warp ? warp_sum[w] : 0;
+        }
 #pragma unroll
         for (int w = 0; w < kWarps; ++w) {
             const int n = at[w][threadIdx.x];
@@ -435,7 +472,7 @@ scatter_kernel(const BwdArgs a, const PassArgs p)
         }
         if (p.next_counts) {
             // one addition for the warp's equal ones, as above
-            const int at2 = key[j] >= 0 ? ((key[j] >> (p.shift + 8)) & (kDigits - 1)) * p.tiles + to / kTile : -1;
+            const int at2 = key[j] >= 0 ? ((key[j] >> (p.shift + 8)) & (kDigits - 1)) * p.pitch + to / kTile : -1;
             const unsigned equal = __match_any_sync(0xffffffffu, at2);
             if (at2 >= 0 && (equal & ((1u << lane) - 1)) == 0) atomicAdd(&p.next_counts[at2], __popc(equal));
         }
@@ -586,7 +623,9 @@ static Plan plan_of(int64_t N, int64_t K, int64_t V)
         p.bytes = 256;
         return p;
     }
-    p.chunk = N > 65536 ? 128 : 32;
+    // 128 entries, or so many that 3500 blocks have work: 2048 columns of a chunk each (150000 x 1000: 90 us with 586 blocks)
+    p.chunk = 128;
+    while (p.chunk > 32 && N / p.chunk * K < (int64_t)3500 * 2048) p.chunk /= 2;
     p.chunks = (int)((N + p.chunk - 1) / p.chunk);
     if (N > kRankMax || V >= kRankVocabulary) {
         p.tiles = (int)((N + kTile - 1) / kTile);
@@ -600,22 +639,22 @@ static Plan plan_of(int64_t N, int64_t K, int64_t V)
         at += align256(n);
         return here;
     };
-    const size_t ints = (size_t)N * 4, counts = (size_t)p.tiles * kDigits * 4;
+    const size_t ints = (size_t)N * 4, counts = align256((size_t)(p.tiles + 3) / 4 * 4 * kDigits * 4);
     p.key = take(ints);
     p.pos = take(ints);
     p.key2 = take(p.tiles ? ints : 0);
     p.pos2 = take(p.tiles ? ints : 0);
     p.counts = take(counts * p.passes);
     p.present = take(((size_t)V + 31) / 32 * 32);
-    // cleared first: the counts of the passes behind the first, and `present`
-    p.first_zero = p.passes > 1 ? p.counts + counts : p.present;
+    // cleared first: the counts, and `present`
+    p.first_zero = p.counts;
     p.zero_bytes = at - p.first_zero;
     p.part = take((size_t)p.chunks * 2 * (size_t)K * 4);
     p.bytes = at;
     return p;
 }
 
-// Zero rows are handed out to the launches: `parts` of them, in equal shares, the last one what is left.
+// Zero rows are handed out to the launches in `parts` shares; 0 shares: all that is left.
 struct Fill {
     int64_t next, blocks, share;
     int rows;
@@ -626,9 +665,9 @@ struct Fill {
         blocks = a.accumulate ? 0 : (a.V + rows - 1) / rows;
         share = blocks / parts;
     }
-    unsigned take(BwdArgs &a, bool all)
+    unsigned take(BwdArgs &a, int shares)
     {
-        const int64_t n = all ? blocks - next : share;
+        const int64_t n = shares ? shares * share : blocks - next;
         a.fill0 = next * rows;
         next += n;
         return (unsigned)n;
@@ -648,30 +687,38 @@ static int launch_bwd(BwdArgs a, const Plan &p, unsigned char *mem, cudaStream_t
     int32_t *pos[2] = {reinterpret_cast<int32_t *>(mem + p.pos), reinterpret_cast<int32_t *>(mem + p.pos2)};
     a.key = key[0];
     a.pos = pos[0];
-    if (!a.accumulate || p.passes > 1) PPO_RETURN_IF_CUDA(cudaMemsetAsync(mem + p.first_zero, 0, p.zero_bytes, s));
+    const size_t counts = align256((size_t)(p.tiles + 3) / 4 * 4 * kDigits * 4);
+    if (!a.accumulate || p.passes > 0) PPO_RETURN_IF_CUDA(cudaMemsetAsync(mem + p.first_zero, 0, p.zero_bytes, s));
     if (!p.tiles) {
         fill.init(a, 1);
         const int per_block = kRankWarps * kRankPer;
         rank_kernel<<<(a.N + per_block - 1) / per_block, kThreads, 0, s>>>(a, key[0], pos[0]);
         if ((rc = launch_status())) return rc;
     } else {
-        fill.init(a, 2 * p.passes + 2);
+        // (moving the entries leaves the memory more time than the other launches do)
+        fill.init(a, 4 * p.passes);
         PassArgs ps = {};
         ps.tiles = p.tiles;
+        ps.pitch = (p.tiles + 3) / 4 * 4;
+        ps.summed = p.tiles > kSumTiles;
         int to = (p.passes & 1) ^ 1;                            // the last pass writes the first pair
         for (int pass = 0; pass < p.passes; ++pass, to ^= 1) {
-            ps.counts = reinterpret_cast<int32_t *>(mem + p.counts) + (size_t)pass * p.tiles * kDigits;
-            ps.next_counts = pass + 1 < p.passes ? ps.counts + (size_t)p.tiles * kDigits : nullptr;
+            ps.counts = reinterpret_cast<int32_t *>(mem + p.counts + pass * counts);
+            ps.next_counts = pass + 1 < p.passes && p.tiles <= kAheadTiles ? reinterpret_cast<int32_t *>(mem + p.counts + (pass + 1) * counts) : nullptr;
             ps.key_out = key[to];
             ps.pos_out = pos[to];
             ps.shift = pass * 8;
             if (pass == 0) {
                 count_kernel<<<p.tiles, kThreads, 0, s>>>(a, ps);
                 if ((rc = launch_status())) return rc;
+            } else if (p.tiles > kAheadTiles) {
+                PPO_RETURN_IF_CUDA(launch_dependent(count_kernel, dim3(p.tiles), dim3(kThreads), 0, s, a, ps));
             }
-            unsigned extra = fill.take(a, false);
-            PPO_RETURN_IF_CUDA(launch_dependent(scan_kernel<TO>, dim3(1 + extra), dim3(kScanThreads), 0, s, a, ps));
-            extra = fill.take(a, false);
+            if (ps.summed) {
+                const unsigned extra = fill.take(a, 1);
+                PPO_RETURN_IF_CUDA(launch_dependent(scan_kernel<TO>, dim3(1 + extra), dim3(kScanThreads), 0, s, a, ps));
+            }
+            const unsigned extra = fill.take(a, ps.summed ? 3 : 4);
             a.work_blocks = p.tiles;
             PPO_RETURN_IF_CUDA(launch_dependent(scatter_kernel<TO>, dim3(p.tiles + extra), dim3(kThreads), 0, s, a, ps));
             ps.key_in = ps.key_out;
@@ -688,7 +735,7 @@ static int launch_bwd(BwdArgs a, const Plan &p, unsigned char *mem, cudaStream_t
     const int join_slabs = (int)((a.K + kThreads * kJoinVec - 1) / (kThreads * kJoinVec));
     if (blocks + a.V / a.fill_rows + 1 >= ((int64_t)1 << 31) || (int64_t)p.chunks * join_slabs >= ((int64_t)1 << 31)) return PPO_ERR_SHAPE;
     a.work_blocks = (int)blocks;
-    const unsigned extra = fill.take(a, true);
+    const unsigned extra = fill.take(a, 0);
     PPO_RETURN_IF_CUDA(launch_dependent(sum_kernel<TI, TO, VEC>, dim3((unsigned)blocks + extra), dim3(kThreads),
                                         (size_t)a.groups * a.chunk * sizeof(int2), s, a));
     if (p.chunks < 2) return PPO_OK;
