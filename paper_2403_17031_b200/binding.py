@@ -818,6 +818,8 @@ def lmhead_xent(H: torch.Tensor, W: torch.Tensor, labels: torch.Tensor, mask: Op
         raise ValueError("H [M,K] and W [K,V] disagree on K")
     for t, name in ((labels, "labels"), (mask, "mask")):
         _count(t, M, 1, name)
+    if denom is not None and denom.numel() != 1:
+        raise ValueError("denom is one number")
     if M <= 1 and not (H.is_contiguous() and K % 8 == 0):
         ldh = max(ldh, -(-K // 8) * 8)                  # (the pitch of a single row is anyone's choice)
     if out is None:

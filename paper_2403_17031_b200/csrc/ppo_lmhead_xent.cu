@@ -1187,7 +1187,7 @@ constexpr int64_t kLimit = ((int64_t)1 << 31) - 16384;
 static bool sizes_ok(int64_t M, int64_t K, int64_t V, int64_t piece_rows)
 {
     return M > 0 && K > 0 && V > 0 && M < kLimit && K < kLimit && V < kLimit && piece_rows >= 0 &&
-           ((K + 255) / 256) * ((V + 255) / 256) < ((int64_t)1 << 30) && ((M + 255) / 256) * ((V + 255) / 256) < ((int64_t)1 << 30);
+           ((K + 255) / 256) * ((V + 255) / 256) < ((int64_t)1 << 27) && ((M + 255) / 256) * ((V + 255) / 256) < ((int64_t)1 << 27);
 }
 
 }   // namespace xent

@@ -38,8 +38,8 @@ def test_xent_refusals(b):
     assert b.lib().ppo_lmhead_xent(*vk) == -2
     n = b.lmhead_xent_scratch_bytes
     assert n(0, 256, 1000) == 0 and n(4, 256, 0) == 0
-    # the piece bounds the scratch: 256 rows x V in 16 bits, the sums of dW, and what is per row of M
-    assert n(1 << 16, 64, 50304, 256) < 2 * 256 * 50304 + 4 * 256 * 50432 + (1 << 16) * (128 + 8) + 256 * (394 * 16 + 256) + (43 << 20)
+    # the piece bounds the scratch: 256 rows x V in 16 bits, the sums of dW (whole tiles), what is per row of M, and two tiles a pair of blocks
+    assert n(1 << 16, 64, 50304, 256) < 2 * 256 * 50304 + 4 * 512 * 50688 + (1 << 16) * (128 + 12) + 256 * (394 * 16 + 256) + (84 << 20)
     assert n(4, 256, 1000, 0, False, False) < n(4, 256, 1000, 0, True, False) < n(4, 256, 1000)
 
 
