@@ -51,17 +51,22 @@ constexpr float kLeast = 5.421010862427522e-20f, kMost = 1.8446744073709552e19f;
 // contractions.
 // kSingle: blocks alone on tiles of 128 x 128, for up to 128 rows: half of a pair's tile would be idle rows, the tensor cores would
 // take longer over them than memory over W, and there are too few wide tiles to share out evenly (197 of 256 columns at V =
-// 50304, on 148 SMs: 101 us for product 1 of 53 rows, now 88). Two groups of epilogue warps take turns at the tiles.
-enum Mode { kSingle, kPair, kWide };
+// 50304, on 148 SMs: 101 us for product 1 of 53 rows, now 88). Two groups of epilogue warps take turns at the tiles. What bounds
+// them is how much of W is on its way: more stages, and one staging buffer a warp (53 x 50304 x 4096 in all: 3 stages 302 us,
+// 4 279, 5 266).
+// kSmall: the same for products 1 and 2 of up to 64 rows: a stage holds 64 rows of A, so that there are eight. The matrix
+// instruction reads 128: the other 64 rows are what lies behind them (B), and their results are nobody's.
+enum Mode { kSingle, kPair, kWide, kSmall };
 
 template <int MODE>
 struct Shape {
-    static constexpr bool kIsPair = MODE != kSingle;
+    static constexpr bool kIsPair = MODE == kPair || MODE == kWide;
     static constexpr int kHalves = MODE == kWide ? 2 : 1;              // accumulators of a tile
     static constexpr int kM = kIsPair ? 2 * kBM : kBM, kAccN = kIsPair ? 256 : 128, kN = kHalves * kAccN;
     static constexpr int kRowsB = 128;                                 // a block's share of B, per accumulator
-    static constexpr int kBytesA = kBM * kBlockK * 2, kBytesB = kRowsB * kBlockK * 2, kStage = kBytesA + kHalves * kBytesB;
-    static constexpr int kStages = MODE == kWide ? 4 : 5, kBuffers = MODE == kWide ? 1 : 2;   // buffers: per epilogue warp
+    static constexpr int kBytesA = (MODE == kSmall ? 64 : kBM) * kBlockK * 2, kBytesB = kRowsB * kBlockK * 2, kStage = kBytesA + kHalves * kBytesB;
+    static constexpr int kStages = MODE == kWide ? 4 : MODE == kPair ? 5 : MODE == kSingle ? 6 : 8;
+    static constexpr int kBuffers = MODE == kPair ? 2 : 1;             // staging, per epilogue warp
     static constexpr int kSmem = kStages * kStage + kBuffers * kEpiWarps * kStageOut + 1024;
     static constexpr int kTileFloats = kM * kN;
     static_assert(kSmem <= 232448 - 1024, "shared memory of a block");
@@ -232,6 +237,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_out, const Args a)
 {
     using S = Shape<MODE>;
+    static_assert(MODE != kSmall || !A_MN, "rows of A are what there are few of");
     constexpr bool PAIR = S::kIsPair;
     constexpr int kStages = S::kStages, kHalves = S::kHalves;
     extern __shared__ __align__(1024) unsigned char smem_raw[];
@@ -498,20 +504,23 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             };
 
             if (PRODUCT == kLogits) {
-                // U with the row's reference. Where a lane's largest value has left the window, which is looked at when all
-                // 128 are there, once more with another one.
-                float s = 0.f, rounded = 0.f, c = a.c;
+                // U with the row's reference. Where a lane's largest value has left the window, once more with another one:
+                // with two staging buffers that is looked at when all 128 are there, with one for each 64 before they leave.
+                float s = 0.f, rounded = 0.f;
+                const float c = a.c;
                 const bool plain = __all_sync(0xffffffffu, ok) && n + 128 <= a.dim_n;
-                if (a.store) reuse();
 #pragma unroll 1
                 for (int turn = 0; turn < 2; ++turn) {
                     float top = 0.f;
+                    bool again = false;
                     s = rounded = 0.f;
 #pragma unroll 1
                     for (int half = 0; half < 2; ++half) {
+                        if (a.store && (S::kBuffers == 1 || half == 0)) reuse();
+                        unsigned char *buffer = stage + (S::kBuffers == 2 ? half : 0) * kStageOut;
                         float v[64];
                         read(half, v);
-                        if (turn == 0 && (unsigned)(label - half * 64) < 64u) {
+                        if ((unsigned)(label - half * 64) < 64u) {
 #pragma unroll
                             for (int j = 0; j < 64; ++j)
                                 if (label - half * 64 == j) a.picked[row] = v[j];
@@ -536,14 +545,22 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                                 rounded += low(w[e]);
                                 r1 += high(w[e]);
                             }
-                            if (a.store) stage8(stage + half * kStageOut, j, w);
+                            if (a.store) stage8(buffer, j, w);
                         }
                         s += s1;
                         rounded += r1;
+                        // (a lane without a column has 0 everywhere)
+                        if (turn == 0 && (S::kBuffers == 1 || half == 1)) {
+                            const bool out = ok && n + half * 64 < a.dim_n && !(top >= kLeast && top <= kMost);
+                            again = __any_sync(0xffffffffu, out);
+                            if (again) break;
+                        }
+                        if (a.store && S::kBuffers == 1) send(half, half + 1, 0x7fffffff, true);
                     }
-                    // (a lane without a column has 0 everywhere)
-                    const bool out = ok && n < a.dim_n && !(top >= kLeast && top <= kMost);
-                    if (turn == 1 || !__any_sync(0xffffffffu, out)) break;
+                    if (!again) break;
+                    // (what has left has arrived before it is written again)
+                    if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+                    __syncwarp();
                     float m = kNoRef;
 #pragma unroll 1
                     for (int half = 0; half < 2; ++half) {
@@ -553,10 +570,11 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
 #pragma unroll
                         for (int j = 0; j < 64; ++j) m = j < left ? fmaxf(m, v[j]) : m;
                     }
-                    if (out) ref += 128.f * rintf((fmaxf(m * c, -1e9f) - ref) * (1.f / 128.f));
+                    // (unchanged where the largest one is in the window)
+                    if (ok) ref += 128.f * rintf((fmaxf(m * c, -1e9f) - ref) * (1.f / 128.f));
                 }
                 release();
-                if (a.store) send(0, 2, 0x7fffffff, true);
+                if (a.store && S::kBuffers == 2) send(0, 2, 0x7fffffff, true);
                 if (ok && n < a.dim_n) a.part[(size_t)row * a.chunks + n / kChunk] = make_float4(ref, s, rounded, 0.f);
             } else if (PRODUCT == kHidden) {
                 // (four columns of a tile's rows follow one another in scratch: a warp writes 512 bytes at a time)
@@ -1136,6 +1154,9 @@ static bool wide(int64_t m, int64_t n, int64_t contraction, int sms)
     return (n + 255) / 256 % 2 == 0 && contraction >= 64 * kBlockK && (m + 255) / 256 * ((n + 511) / 512) >= sms;
 }
 
+// the mode of products 1 and 2 for few rows; product 3 has its rows along the contraction
+static bool few(int M) { return M <= 64; }
+
 template <int MODE>
 static void set_shape(RowArgs &r, const Args &a2, int sms)
 {
@@ -1150,7 +1171,11 @@ static int launch_piece(const Maps &m, RowArgs r, const Args &a1, Args a2, Args 
                         cudaStream_t s)
 {
     int rc;
-    if (single)
+    const bool small = few(a1.M);
+    if (small)
+        rc = vk ? launch_product<kSmall, false, false, kLogits>(m.packed, m.h, m.w1, m.u_out, a1, sms, s)
+                : launch_product<kSmall, false, true, kLogits>(m.packed, m.h, m.w1, m.u_out, a1, sms, s);
+    else if (single)
         rc = vk ? launch_product<kSingle, false, false, kLogits>(m.packed, m.h, m.w1, m.u_out, a1, sms, s)
                 : launch_product<kSingle, false, true, kLogits>(m.packed, m.h, m.w1, m.u_out, a1, sms, s);
     else
@@ -1168,7 +1193,8 @@ static int launch_piece(const Maps &m, RowArgs r, const Args &a1, Args a2, Args 
             a2.gn = 6;
             rc = launch_hidden<kWide>(m, a2, vk, sms, s);
         } else {
-            rc = single ? launch_hidden<kSingle>(m, a2, vk, sms, s) : launch_hidden<kPair>(m, a2, vk, sms, s);
+            rc = small ? launch_hidden<kSmall>(m, a2, vk, sms, s)
+                       : single ? launch_hidden<kSingle>(m, a2, vk, sms, s) : launch_hidden<kPair>(m, a2, vk, sms, s);
         }
         if (rc) return rc;
     }
@@ -1257,15 +1283,16 @@ extern "C" int ppo_lmhead_xent(const void *H, int64_t ldh, const void *W, int64_
     r.status = status;
 
     Maps m = {};
+    const int rows_a = few((int)M) ? 64 : kBM;                  // rows of A that a load brings
     const int rows_b = Shape<kPair>::kRowsB;                    // a block's share of B, stored by rows
-    if ((rc = make_map_pitch(&m.packed, r.packed, (uint64_t)K, (uint64_t)M, (uint64_t)l.Kp, kBM))) return rc;
-    if ((rc = make_map_pitch(&m.h, H, (uint64_t)K, (uint64_t)M, (uint64_t)ldh, kBM))) return rc;
+    if ((rc = make_map_pitch(&m.packed, r.packed, (uint64_t)K, (uint64_t)M, (uint64_t)l.Kp, rows_a))) return rc;
+    if ((rc = make_map_pitch(&m.h, H, (uint64_t)K, (uint64_t)M, (uint64_t)ldh, rows_a))) return rc;
     // product 1 takes W with the vocabulary as the result's columns, product 2 with the hidden size
     if ((rc = make_map_pitch(&m.w1, W, (uint64_t)w_inner, (uint64_t)w_outer, (uint64_t)ldw, vk ? rows_b : 64))) return rc;
     if ((rc = make_map_pitch(&m.w2, W, (uint64_t)w_inner, (uint64_t)w_outer, (uint64_t)ldw, vk ? 64 : rows_b))) return rc;
     if (grad) {
         if ((rc = make_map_pitch(&m.u_out, r.u, (uint64_t)V, (uint64_t)l.rows_max, (uint64_t)l.Vp, 32))) return rc;
-        if ((rc = make_map_pitch(&m.u2, r.u, (uint64_t)V, (uint64_t)l.rows_max, (uint64_t)l.Vp, kBM))) return rc;
+        if ((rc = make_map_pitch(&m.u2, r.u, (uint64_t)V, (uint64_t)l.rows_max, (uint64_t)l.Vp, rows_a))) return rc;
         if ((rc = make_map_pitch(&m.u3, r.u, (uint64_t)V, (uint64_t)l.rows_max, (uint64_t)l.Vp, 64))) return rc;
     }
 
