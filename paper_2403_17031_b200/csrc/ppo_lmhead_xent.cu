@@ -264,8 +264,9 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     if (PAIR) cluster_barrier();                                // the other block's barriers are ready too
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem_base = sm.tmem_base;
-    grid_dependents_may_launch();
+    // (in this order: what the launches before this one wrote is there when row_kernel starts)
     grid_dependency_wait();
+    grid_dependents_may_launch();
     const int rank = PAIR ? (int)cluster_rank() : 0;
     const int worker = PAIR ? blockIdx.x / 2 : blockIdx.x, workers = PAIR ? gridDim.x / 2 : gridDim.x;
     const int rows = rows_of(a);
@@ -919,9 +920,26 @@ __global__ void __launch_bounds__(kRowThreads)
 row_kernel(const RowArgs a)
 {
     __shared__ float red[3][kRowThreads / 32];
+    // What this kernel needs and product 1 does not write is loaded while that still runs: a chain of three loads from memory.
+    const int n_real = __ldcg(a.n_real), rows = max(0, min(a.rows_max, n_real - a.row0)), r = (int)blockIdx.x - 1;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int row = 0, label = -1;
+    uint4 ahead[2] = {};                                        // of the row of H: this thread's first two pieces of eight
+    const __nv_bfloat16 *h = a.H;
+    if (r >= 0 && r < rows) {
+        row = __ldcg(a.order + a.row0 + r);
+        label = __ldcg(&a.info[a.row0 + r].x);
+        h += (int64_t)row * a.ldh;
+        if (a.scaled) {
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const int k = (j * kRowThreads + threadIdx.x) * 8;
+                if (k + 8 <= a.K) ahead[j] = __ldcg(reinterpret_cast<const uint4 *>(h + k));
+            }
+        }
+    }
     grid_dependents_may_launch();
     grid_dependency_wait();
-    const int n_real = *a.n_real, rows = max(0, min(a.rows_max, n_real - a.row0)), r = (int)blockIdx.x - 1;
     if (r < 0) {
         choose_slices(a, rows);
         return;
@@ -933,12 +951,18 @@ row_kernel(const RowArgs a)
             for (int k = threadIdx.x; k < a.K; k += kRowThreads) scaled[k] = __float2bfloat16_rn(0.f);
         return;
     }
-    const int row = a.order[a.row0 + r], lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int label = a.labels[row];
     const bool bad = label < 0 || label >= a.V;
     const float4 *part = a.part + (size_t)r * a.chunks;
+    float4 mine[2];                                             // this thread's first two chunks
     float m = kNoRef;
-    for (int t = threadIdx.x; t < a.chunks; t += kRowThreads) m = fmaxf(m, part[t].x);
+    const float acc = bad ? __int_as_float(0x7fffffff) : a.picked[r];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const int t = j * kRowThreads + threadIdx.x;
+        mine[j] = t < a.chunks ? part[t] : make_float4(kNoRef, 0.f, 0.f, 0.f);
+        m = fmaxf(m, mine[j].x);
+    }
+    for (int t = threadIdx.x + 2 * kRowThreads; t < a.chunks; t += kRowThreads) m = fmaxf(m, part[t].x);
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, off));
     if (lane == 0) red[0][warp] = m;
@@ -947,7 +971,7 @@ row_kernel(const RowArgs a)
     for (int w = 0; w < kRowThreads / 32; ++w) m = fmaxf(m, red[0][w]);
     float s = 0.f, sr = 0.f;                                    // sums of U and of the rounded U
     for (int t = threadIdx.x; t < a.chunks; t += kRowThreads) {
-        const float4 p = part[t];
+        const float4 p = t < kRowThreads ? mine[0] : t < 2 * kRowThreads ? mine[1] : part[t];
         const float f = ex2(p.x - m);
         s = fmaf(p.y, f, s);
         sr = fmaf(p.z, f, sr);
@@ -978,7 +1002,6 @@ row_kernel(const RowArgs a)
         sr += red[2][w];
     }
     const float l2s = log2f(s), nan = __int_as_float(0x7fffffff);
-    const float acc = bad ? nan : a.picked[r];
     if (threadIdx.x == 0) {
         a.nll[row] = ((m - acc * a.c) + l2s) * kLn2;
         if (a.lse) a.lse[row] = (m + l2s) * kLn2;
@@ -1000,10 +1023,9 @@ row_kernel(const RowArgs a)
     }
     if (threadIdx.x == 0) a.row_scale[r] = make_float2(f, c);
     if (!scaled) return;
-    const __nv_bfloat16 *h = a.H + (int64_t)row * a.ldh;
     for (int k = threadIdx.x * 8; k < a.K; k += kRowThreads * 8) {
         if (k + 8 <= a.K) {
-            const uint4 v = *reinterpret_cast<const uint4 *>(h + k);
+            const uint4 v = k < kRowThreads * 8 ? ahead[0] : k < 2 * kRowThreads * 8 ? ahead[1] : *reinterpret_cast<const uint4 *>(h + k);
             uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
             for (int e = 0; e < 4; ++e) w[e] = pack2(low(w[e]) * f, high(w[e]) * f);
