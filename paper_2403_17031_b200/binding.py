@@ -6,6 +6,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+from array import array
 from typing import Optional
 
 import torch
@@ -913,6 +914,18 @@ def grad_clip_scratch_bytes(n: int) -> int:
     return int(lib().ppo_grad_clip_scratch_bytes(n))
 
 
+def _tensor_arrays(tensors, at: int, name: str):
+    """(addresses, elements, dtype codes) of contiguous fp32 / bf16 tensors on device `at`."""
+    ptr, numel, code = [], [], []
+    for t in tensors:
+        if t.get_device() != at or not t.is_contiguous():
+            raise TypeError("%s must be contiguous tensors on one device" % name)
+        ptr.append(t.data_ptr())
+        numel.append(t.numel())
+        code.append(_logits_dtype(t))
+    return array("Q", ptr), array("q", numel), array("i", code)
+
+
 def grad_clip(grads, max_norm: float, scale: float = 1.0, out=None, workspace: Optional[torch.Tensor] = None,
               scratch: Optional[torch.Tensor] = None, norm: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Scales a list of gradients (contiguous, fp32 or bf16) by scale * min(1, max_norm / norm) with the norm over all of
@@ -921,33 +934,28 @@ def grad_clip(grads, max_norm: float, scale: float = 1.0, out=None, workspace: O
     n = len(grads)
     if not n:
         raise ValueError("grad_clip needs a gradient")
-    at = grads[0].get_device()
-    if not grads[0].is_cuda:
+    first = grads[0]
+    at = first.get_device()
+    if at < 0:
         raise TypeError("gradients must be CUDA tensors")
-
-    def arrays(tensors, name):
-        for t in tensors:
-            if t.get_device() != at or not t.is_contiguous():
-                raise TypeError("%s must be contiguous tensors on one device" % name)
-        return (C.c_void_p * n)(*[t.data_ptr() for t in tensors]), (C.c_int32 * n)(*[_logits_dtype(t) for t in tensors])
-
-    ins, in_dtype = arrays(grads, "gradients")
-    numel = [t.numel() for t in grads]
+    # (plain arrays: a ctypes array costs more to make than a small call takes on the device)
+    ins, numel, in_dtype = _tensor_arrays(grads, at, "gradients")
     outs = out_dtype = None
     if out is not None:
-        if [t.numel() for t in out] != numel:
+        outs, sizes, out_dtype = _tensor_arrays(out, at, "out")
+        if sizes != numel:
             raise ValueError("out must hold a tensor of the same size for each gradient")
-        outs, out_dtype = arrays(out, "out")
     if norm is None:
-        norm = grads[0].new_empty(2, dtype=torch.float32)
+        norm = first.new_empty(2, dtype=torch.float32)
     elif norm.numel() != 2:
         raise ValueError("norm has two elements")
     need = grad_clip_scratch_bytes(n)
     if scratch is None:
-        scratch = grads[0].new_empty(need, dtype=torch.uint8)
+        scratch = first.new_empty(need, dtype=torch.uint8)
     elif scratch.numel() < need:
         raise ValueError("grad_clip needs %d bytes of scratch (grad_clip_scratch_bytes)" % need)
-    _call("ppo_grad_clip", at, n, ins, (C.c_int64 * n)(*numel), in_dtype, outs, out_dtype, float(scale), float(max_norm),
+    where = lambda x: None if x is None else x.buffer_info()[0]                     # noqa: E731
+    _call("ppo_grad_clip", at, n, where(ins), where(numel), where(in_dtype), where(outs), where(out_dtype), float(scale), float(max_norm),
           _addr(norm, torch.float32, at, "norm"), _addr(workspace, torch.uint8, at, "workspace"),
           _addr(scratch, torch.uint8, at, "scratch"))
     return norm
