@@ -656,16 +656,13 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
 constexpr int kJoinThreads = 256;
 template <int MODE> constexpr int join_blocks() { return (Shape<MODE>::kM / 32) * (Shape<MODE>::kN / 64); }
 template <int MODE>
-__global__ void __launch_bounds__(kJoinThreads)
-join_kernel(const Args a, int workers)
+__device__ __forceinline__ void join_tiles(const Args &a, int workers, int block)
 {
     constexpr int kM = Shape<MODE>::kM, kTileFloats = Shape<MODE>::kTileFloats, kBlocks = (kM / 32) * (Shape<MODE>::kN / 64);
     __shared__ float4 turn[32][17];
-    grid_dependents_may_launch();
-    grid_dependency_wait();
     const int rows = rows_of(a);
     const Plan p = plan_of<MODE, kHidden>(a, rows, workers);
-    const int rest = blockIdx.x / kBlocks, part_of = blockIdx.x % kBlocks;
+    const int rest = block / kBlocks, part_of = block % kBlocks;
     if (rest >= p.n_rest) return;
     const int row0 = (part_of % (kM / 32)) * 32, j0 = part_of / (kM / 32) * 16;
     const int2 t = tile_of(p.n_whole + rest, p.m_tiles, p.n_tiles, a.gm, a.gn);
@@ -702,6 +699,15 @@ join_kernel(const Args a, int workers)
     }
 }
 
+template <int MODE>
+__global__ void __launch_bounds__(kJoinThreads)
+join_kernel(const Args a, int workers)
+{
+    grid_dependents_may_launch();
+    grid_dependency_wait();
+    join_tiles<MODE>(a, workers, blockIdx.x);
+}
+
 // ---------------------------------------------------------------- rows
 struct RowArgs {
     const __nv_bfloat16 *H;
@@ -735,7 +741,7 @@ struct RowArgs {
     int *status;
 };
 
-// The mean of kSample neighbouring columns of W, from the middle of the vocabulary, for 128 hidden elements: a thread loads
+// The mean of kSample neighbouring columns of W, from the middle of the vocabulary, for some hidden elements: a thread loads
 // eight neighbours in memory, eight (stored [K, V]) or 64 (stored [V, K]) threads share an element. (One element after the
 // other, 64 loads each: 36 us at K = 4096, most of it misses of the address translation.)
 constexpr int kOrderThreads = 1024, kOrderPer = 8, kSample = 64, kMeanPer = kOrderThreads / 8;
@@ -744,7 +750,6 @@ __device__ __forceinline__ void mean_columns(const RowArgs &a, int k0, float (*p
     const int v0 = min(a.V / 2, max(0, a.V - kSample)) & ~7, n = min(kSample, a.V - v0);
     float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     if (a.vk) {
-        // four times 16 rows of W
         const int k = k0 + (threadIdx.x & 15) * 8;
 #pragma unroll
         for (int j = threadIdx.x >> 4; j < kSample; j += kOrderThreads / 16) {
@@ -1041,21 +1046,37 @@ row_kernel(const RowArgs a)
     }
 }
 
-constexpr int kLossThreads = 1024;
-__global__ void __launch_bounds__(kLossThreads)
-loss_kernel(const RowArgs a)
+template <int THREADS>
+__device__ __forceinline__ void sum_loss(const RowArgs &a)
 {
     __shared__ double red[32];
-    grid_dependency_wait();
     double s = 0.0;
-#pragma unroll 4
-    for (int i = threadIdx.x; i < a.M; i += kLossThreads) s += (double)a.nll[i];
-    s = block_sum<kLossThreads>(s, red);
+#pragma unroll 8
+    for (int i = threadIdx.x; i < a.M; i += THREADS) s += (double)a.nll[i];
+    s = block_sum<THREADS>(s, red);
     if (threadIdx.x == 0) {
         const int n = *a.n_real;
         *a.loss = n ? (float)(s / (a.denom ? (double)*a.denom : (double)n)) : 0.f;
         if (!n && a.status) atomicOr(a.status, PPO_DEV_EMPTY_MASK);
     }
+}
+
+constexpr int kLossThreads = 1024;
+__global__ void __launch_bounds__(kLossThreads)
+loss_kernel(const RowArgs a)
+{
+    grid_dependency_wait();
+    sum_loss<kLossThreads>(a);
+}
+
+// the last launch of some calls with one piece: the loss beside the joining of product 2's slices
+template <int MODE>
+__global__ void __launch_bounds__(kJoinThreads)
+tail_kernel(const RowArgs r, const Args a, int workers)
+{
+    grid_dependency_wait();
+    if (blockIdx.x == 0) sum_loss<kJoinThreads>(r);
+    else join_tiles<MODE>(a, workers, blockIdx.x - 1);
 }
 
 // ---------------------------------------------------------------- host side
@@ -1159,10 +1180,17 @@ static int launch_hidden(const Maps &m, const Args &a2, bool vk, int sms, cudaSt
 {
     const int rc = vk ? launch_product<MODE, false, true, kHidden>(m.u2, m.u2, m.w2, m.u2, a2, sms, s)
                       : launch_product<MODE, false, false, kHidden>(m.u2, m.u2, m.w2, m.u2, a2, sms, s);
-    if (rc) return rc;
+    return rc;
+}
+
+// what follows product 2, or (last: with the loss) product 3
+template <int MODE>
+static int launch_join(const RowArgs &r, const Args &a2, bool last, int sms, cudaStream_t s)
+{
     const int workers = Shape<MODE>::kIsPair ? sms / 2 : sms;
-    PPO_RETURN_IF_CUDA(launch_dependent(join_kernel<MODE>,
-                                        dim3((unsigned)((workers - 1) * join_blocks<MODE>())), dim3(kJoinThreads), 0, s, a2, workers));
+    const unsigned blocks = (unsigned)((workers - 1) * join_blocks<MODE>());
+    if (last) PPO_RETURN_IF_CUDA(launch_dependent(tail_kernel<MODE>, dim3(1 + blocks), dim3(kJoinThreads), 0, s, r, a2, workers));
+    else PPO_RETURN_IF_CUDA(launch_dependent(join_kernel<MODE>, dim3(blocks), dim3(kJoinThreads), 0, s, a2, workers));
     return PPO_OK;
 }
 
@@ -1194,8 +1222,8 @@ static void set_shape(RowArgs &r, const Args &a2, int sms)
     r.kbs = (a2.dim_k + kBlockK - 1) / kBlockK;
 }
 
-static int launch_piece(const Maps &m, RowArgs r, const Args &a1, Args a2, Args a3, bool single, bool vk, bool dh, bool dw, int sms,
-                        cudaStream_t s)
+static int launch_piece(const Maps &m, RowArgs r, const Args &a1, Args a2, Args a3, bool single, bool vk, bool dh, bool dw, bool only,
+                        int sms, cudaStream_t s)
 {
     int rc;
     const bool small = few(a1.M);
@@ -1214,25 +1242,32 @@ static int launch_piece(const Maps &m, RowArgs r, const Args &a1, Args a2, Args 
     else if (wide_hidden) set_shape<kWide>(r, a2, sms);
     else set_shape<kPair>(r, a2, sms);
     PPO_RETURN_IF_CUDA(launch_dependent(row_kernel, dim3(1 + (unsigned)r.rows_max), dim3(kRowThreads), 0, s, r));
+    const auto join = [&](bool last) {
+        return wide_hidden ? launch_join<kWide>(r, a2, last, sms, s) : small ? launch_join<kSmall>(r, a2, last, sms, s)
+               : single    ? launch_join<kSingle>(r, a2, last, sms, s) : launch_join<kPair>(r, a2, last, sms, s);
+    };
     if (dh) {
         if (wide_hidden) {
             a2.gm = 12;
             a2.gn = 6;
-            rc = launch_hidden<kWide>(m, a2, vk, sms, s);
+        }
+        rc = wide_hidden ? launch_hidden<kWide>(m, a2, vk, sms, s) : small ? launch_hidden<kSmall>(m, a2, vk, sms, s)
+             : single    ? launch_hidden<kSingle>(m, a2, vk, sms, s) : launch_hidden<kPair>(m, a2, vk, sms, s);
+        if (!rc && !only) rc = join(false);
+        if (rc) return rc;
+    }
+    if (dw) {
+        // (the number of pieces does not change the mode: their sums lie in its order)
+        if (!single && wide(a3.dim_m, a3.dim_n, a3.dim_k, sms)) {
+            a3.gm = 12;
+            a3.gn = 6;
+            rc = launch_weight<kWide>(m, a3, vk, sms, s);
         } else {
-            rc = small ? launch_hidden<kSmall>(m, a2, vk, sms, s)
-                       : single ? launch_hidden<kSingle>(m, a2, vk, sms, s) : launch_hidden<kPair>(m, a2, vk, sms, s);
+            rc = single ? launch_weight<kSingle>(m, a3, vk, sms, s) : launch_weight<kPair>(m, a3, vk, sms, s);
         }
         if (rc) return rc;
     }
-    if (!dw) return PPO_OK;
-    // (the number of pieces does not change the mode: their sums lie in its order)
-    if (!single && wide(a3.dim_m, a3.dim_n, a3.dim_k, sms)) {
-        a3.gm = 12;
-        a3.gn = 6;
-        return launch_weight<kWide>(m, a3, vk, sms, s);
-    }
-    return single ? launch_weight<kSingle>(m, a3, vk, sms, s) : launch_weight<kPair>(m, a3, vk, sms, s);
+    return dh && only ? join(true) : PPO_OK;
 }
 
 constexpr int64_t kLimit = ((int64_t)1 << 31) - 16384;
@@ -1350,11 +1385,15 @@ extern "C" int ppo_lmhead_xent(const void *H, int64_t ldh, const void *W, int64_
     order_kernel<<<1 + (unsigned)((K + kMeanPer - 1) / kMeanPer), kOrderThreads, 0, s>>>(r);
     if ((rc = launch_status())) return rc;
     PPO_RETURN_IF_CUDA(launch_dependent(pack_kernel, dim3((unsigned)M), dim3(kRowThreads), 0, s, r));
+    // The loss and the joining in one launch at the end, unless dW takes the slices out of L2 before that (100 x 20000 x 1032: 75 us in
+    // two launches, 70 in one; 300 x 50304 x 1032: 171 and
+    // 176)
+    const bool tail = l.pieces == 1 && K * V <= 1 << 25;
     for (int p = 0; p < l.pieces; ++p) {
         r.row0 = a1.row0 = a2.row0 = a3.row0 = p * l.rows_max;
-        rc = launch_piece(m, r, a1, a2, a3, M <= kBM, vk, dH != nullptr, dW != nullptr, sms, s);
+        rc = launch_piece(m, r, a1, a2, a3, M <= kBM, vk, dH != nullptr, dW != nullptr, tail, sms, s);
         if (rc) return rc;
     }
-    PPO_RETURN_IF_CUDA(launch_dependent(loss_kernel, dim3(1), dim3(kLossThreads), 0, s, r));
+    if (!dH || !tail) PPO_RETURN_IF_CUDA(launch_dependent(loss_kernel, dim3(1), dim3(kLossThreads), 0, s, r));
     return PPO_OK;
 }
