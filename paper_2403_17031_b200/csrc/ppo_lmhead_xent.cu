@@ -26,11 +26,11 @@
 // columns of W to take that out again.
 //
 // Product kernel: persistent pairs of blocks (cta_group::2) on 256 x 256 tiles; per block one TMA producer warp (stages of
-// 64 along the contraction, 128-byte swizzle), in the leader one issuer warp, eight epilogue warps that drain one 256-column
-// accumulator while the next is formed. Operands are read as they lie in memory, K-major or MN-major, so that W may be
+// 64 along the contraction, 128-byte swizzle), in the leader one issuer warp, eight epilogue warps in two groups that drain one
+// 256-column accumulator while the next is formed. Operands are read as they lie in memory, K-major or MN-major, so that W may be
 // stored [K, V] or [V, K].
 //
-// Bounds and times (calls one after the other): 27136 x 50304 x 4096 25 to 26.5 ms = 1260 to 1340 TFLOP/s, held by the board's
+// Bounds and times (calls one after the other): 27136 x 50304 x 4096 24.6 to 26.5 ms = 1260 to 1360 TFLOP/s, held by the board's
 // power (about 1.4 GHz); three bare library products of these shapes take 24 ms there. At full clock L2 bounds the pairs (13.4 TB/s into the SMs).
 // 1792 rows 1.52 ms (1460 TFLOP/s). 53 rows 258 us: W is streamed twice (products 1 and 2, 75 us each) and dW written once (75 us), 5.5 TB/s.
 #include "ppo_tcgen05.cuh"
@@ -49,15 +49,14 @@ constexpr float kNoRef = -1.0e30f;
 // 2^-64 and 2^64: the largest of a chunk's U lies between them, its smaller ones down to 2^-126 and their sums stay normal numbers
 constexpr float kLeast = 5.421010862427522e-20f, kMost = 1.8446744073709552e19f;
 
-// kPair: pairs of blocks share a tile of 256 x 256: each loads half of either operand, and its epilogue warps half of the columns
-// each; one accumulator is drained while the next is formed.
+// kPair: pairs of blocks share a tile of 256 x 256: each loads half of either operand and keeps half of the rows; one accumulator
+// is drained while the next is formed.
 // kWide: 256 x 512, both accumulators one tile's: a quarter less comes out of L2 per product (which bounds pairs: 64 KB in the
 // 512 cycles of a block of the contraction are all that an SM's port takes), but draining them is not hidden. For long
 // contractions.
 // kSingle: blocks alone on tiles of 128 x 128, for up to 128 rows: half of a pair's tile would be idle rows, the tensor cores would
 // take longer over them than memory over W, and there are too few wide tiles to share out evenly (197 of 256 columns at V =
-// 50304, on 148 SMs: 101 us for product 1 of 53 rows, now 88). Two groups of epilogue warps take turns at the tiles. What bounds
-// them is how much of W is on its way: more stages, and one staging buffer a warp (53 x 50304 x 4096 in all: 3 stages 302 us,
+// 50304, on 148 SMs: 101 us for product 1 of 53 rows, now 88). What bounds them is how much of W is on its way: more stages, and one staging buffer a warp (53 x 50304 x 4096 in all: 3 stages 302 us,
 // 4 279, 5 266).
 // kSmall: the same for products 1 and 2 of up to 64 rows: a stage holds 64 rows of A, so that there are eight. The matrix
 // instruction reads 128: the other 64 rows are what lies behind them (B), and their results are nobody's.
@@ -256,7 +255,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         }
         for (int b = 0; b < 2; ++b) {
             barrier_init(&sm.tmem_full[b], 1);
-            barrier_init(&sm.tmem_empty[b], PAIR ? 2 * kEpiWarps : kEpiWarps / 2);   // both blocks' warps; a group
+            barrier_init(&sm.tmem_empty[b], (PAIR ? 2 : 1) * kEpiWarps / 2);     // a group of each block
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -415,8 +414,9 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         }
         __syncwarp();
     } else if (warp >= 4) {
-        // lanes 32 q ..; of a pair's tile columns 128 h .., else all of them in every second tile
-        const int q = warp & 3, group = (warp - 4) >> 2, h = PAIR ? group : 0;
+        // lanes 32 q .. of every second accumulator: two groups of warps take turns, so that what a tile costs beside its columns
+        // (waits, loads, copies) falls into the other group's time
+        const int q = warp & 3, group = (warp - 4) >> 2;
         unsigned char *const stage = ring + (size_t)kStages * S::kStage + (warp - 4) * S::kBuffers * kStageOut;
         const uint32_t tmem_empty = PAIR ? leader_addr(&sm.tmem_empty[0]) : saddr(&sm.tmem_empty[0]);
         const float nan = __int_as_float(0x7fffffff);
@@ -427,23 +427,22 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         for (int part_of = kHalves; part_of < kHalves || work.next(plan, workers); ++tiles) {
             const int half_tile = kHalves == 2 ? tiles & 1 : 0;
             part_of = half_tile + 1;
-            if (!PAIR && (int)(tiles & 1) != group) continue;
+            if ((int)(tiles & 1) != group) continue;
             const int2 t = tile_of(work.u, plan.m_tiles, plan.n_tiles, a.gm, a.gn);
-            const int m_warp = t.x * S::kM + rank * kBM + q * 32, n = t.y * S::kN + half_tile * S::kAccN + h * 128;
+            const int m_warp = t.x * S::kM + rank * kBM + q * 32, n_tile = t.y * S::kN + half_tile * S::kAccN;
             const int row = m_warp + lane;
             const bool empty = work.kb0 == work.kb1;
             const uint32_t buf = tiles & 1;
-            const uint32_t taddr = tmem_base + buf * S::kAccN + h * 128 + ((uint32_t)(q * 32) << 16);
             bool ok = false;
-            int label = -1, out_row = -1;
-            float ref = 0.f;
+            int label_tile = -1, out_row = -1;
+            float ref_row = 0.f;
             float2 scale = make_float2(0.f, 0.f);
             if (PRODUCT == kLogits) {
                 ok = row < rows;
                 if (ok) {
                     const int2 info = a.info[a.row0 + row];
-                    label = (int)((unsigned)info.x - (unsigned)n);
-                    ref = __int_as_float(info.y);
+                    label_tile = (int)((unsigned)info.x - (unsigned)n_tile);
+                    ref_row = __int_as_float(info.y);
                 }
             } else if (PRODUCT == kHidden) {
                 ok = row < rows;
@@ -460,182 +459,189 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                 alive = __all_sync(0xffffffffu, alive);
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             }
-            // 64 columns of this lane's row
-            const auto read = [&](int half, float (&v)[64]) {
-                if (empty || !alive) {
-#pragma unroll
-                    for (int j = 0; j < 64; ++j) v[j] = alive ? 0.f : nan;
-                    return;
-                }
-                uint32_t r0[32], r1[32];
-                __syncwarp();
-                tmem_ld32(taddr + half * 64, r0);
-                tmem_ld32(taddr + half * 64 + 32, r1);
-                asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-#pragma unroll
-                for (int j = 0; j < 32; ++j) {
-                    v[j] = __uint_as_float(r0[j]);
-                    v[j + 32] = __uint_as_float(r1[j]);
-                }
-            };
-            const auto release = [&] {                          // nothing of the accumulator is needed any more
-                if (empty) return;
-                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-                __syncwarp();
-                const bool arrive = lane == 0 && alive && PPO_TEST_WITHHOLD_XENT != 2;
-                if (PAIR) barrier_arrive_cluster_if(tmem_empty + buf * 8, arrive);
-                else if (arrive) barrier_arrive(&sm.tmem_empty[buf]);
-            };
-            // the staging buffers, whose last copies have read them
-            const auto reuse = [&] {
-                if (lane == 0) tma_store_wait_read();
-                __syncwarp();
-            };
-            // 64-column parts from .. to of these 128, from their buffers, by bulk copies as far as they may go
-            const auto send = [&](int from, int to, int bulk_cols, bool rows_here) {
-                fence_async_proxy();
-                __syncwarp();
-#pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    const int col = n + half * 64;
-                    if (half < from || half >= to || col >= a.dim_n) continue;
-                    const unsigned char *buffer = stage + (S::kBuffers == 2 ? half : 0) * kStageOut;
-                    if (col + 64 <= bulk_cols) {
-                        if (lane == 0 && rows_here) tma_store_2d(&map_out, col, m_warp, buffer);
-                    } else {
-                        store_rows(buffer, a.out, a.ldo, out_row, col, a.dim_n);
-                    }
-                }
-                __syncwarp();
-            };
-
-            if (PRODUCT == kLogits) {
-                // U with the row's reference. Where a lane's largest value has left the window, once more with another one:
-                // with two staging buffers that is looked at when all 128 are there, with one for each 64 before they leave.
-                float s = 0.f, rounded = 0.f;
-                const float c = a.c;
-                const bool plain = __all_sync(0xffffffffu, ok) && n + 128 <= a.dim_n;
 #pragma unroll 1
-                for (int turn = 0; turn < 2; ++turn) {
-                    float top = 0.f;
-                    bool again = false;
-                    s = rounded = 0.f;
-#pragma unroll 1
-                    for (int half = 0; half < 2; ++half) {
-                        if (a.store && (S::kBuffers == 1 || half == 0)) reuse();
-                        unsigned char *buffer = stage + (S::kBuffers == 2 ? half : 0) * kStageOut;
-                        float v[64];
-                        read(half, v);
-                        if ((unsigned)(label - half * 64) < 64u) {
+            for (int h = 0; h < S::kAccN / 128; ++h) {              // 128 columns
+                const int n = n_tile + h * 128, label = label_tile - h * 128;
+                const bool last_read = h == S::kAccN / 128 - 1;
+                const uint32_t taddr = tmem_base + buf * S::kAccN + h * 128 + ((uint32_t)(q * 32) << 16);
+                float ref = ref_row;
+                // 64 columns of this lane's row
+                const auto read = [&](int half, float (&v)[64]) {
+                    if (empty || !alive) {
 #pragma unroll
-                            for (int j = 0; j < 64; ++j)
-                                if (label - half * 64 == j) a.picked[row] = v[j];
-                        }
-                        const int left = plain ? 64 : ok ? a.dim_n - n - half * 64 : 0;
-                        float s1 = 0.f, r1 = 0.f;
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) {
-                            uint32_t w[4];
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                const int i = j * 8 + e * 2;
-                                float x = ex2(fmaf(v[i], c, -ref)), y = ex2(fmaf(v[i + 1], c, -ref));
-                                if (!plain) {
-                                    x = i < left ? x : 0.f;
-                                    y = i + 1 < left ? y : 0.f;
-                                }
-                                top = fmaxf(top, fmaxf(x, y));
-                                s += x;
-                                s1 += y;
-                                w[e] = pack2(x, y);
-                                rounded += low(w[e]);
-                                r1 += high(w[e]);
-                            }
-                            if (a.store) stage8(buffer, j, w);
-                        }
-                        s += s1;
-                        rounded += r1;
-                        // (a lane without a column has 0 everywhere)
-                        if (turn == 0 && (S::kBuffers == 1 || half == 1)) {
-                            const bool out = ok && n + half * 64 < a.dim_n && !(top >= kLeast && top <= kMost);
-                            again = __any_sync(0xffffffffu, out);
-                            if (again) break;
-                        }
-                        if (a.store && S::kBuffers == 1) send(half, half + 1, 0x7fffffff, true);
+                        for (int j = 0; j < 64; ++j) v[j] = alive ? 0.f : nan;
+                        return;
                     }
-                    if (!again) break;
-                    // (what has left has arrived before it is written again)
-                    if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+                    uint32_t r0[32], r1[32];
                     __syncwarp();
-                    float m = kNoRef;
+                    tmem_ld32(taddr + half * 64, r0);
+                    tmem_ld32(taddr + half * 64 + 32, r1);
+                    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) {
+                        v[j] = __uint_as_float(r0[j]);
+                        v[j + 32] = __uint_as_float(r1[j]);
+                    }
+                };
+                const auto release = [&] {                          // nothing of the accumulator is needed any more
+                    if (empty) return;
+                    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                    __syncwarp();
+                    const bool arrive = lane == 0 && alive && PPO_TEST_WITHHOLD_XENT != 2;
+                    if (PAIR) barrier_arrive_cluster_if(tmem_empty + buf * 8, arrive);
+                    else if (arrive) barrier_arrive(&sm.tmem_empty[buf]);
+                };
+                // the staging buffers, whose last copies have read them
+                const auto reuse = [&] {
+                    if (lane == 0) tma_store_wait_read();
+                    __syncwarp();
+                };
+                // 64-column parts from .. to of these 128, from their buffers, by bulk copies as far as they may go
+                const auto send = [&](int from, int to, int bulk_cols, bool rows_here) {
+                    fence_async_proxy();
+                    __syncwarp();
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {
+                        const int col = n + half * 64;
+                        if (half < from || half >= to || col >= a.dim_n) continue;
+                        const unsigned char *buffer = stage + (S::kBuffers == 2 ? half : 0) * kStageOut;
+                        if (col + 64 <= bulk_cols) {
+                            if (lane == 0 && rows_here) tma_store_2d(&map_out, col, m_warp, buffer);
+                        } else {
+                            store_rows(buffer, a.out, a.ldo, out_row, col, a.dim_n);
+                        }
+                    }
+                    __syncwarp();
+                };
+
+                if (PRODUCT == kLogits) {
+                    // U with the row's reference. Where a lane's largest value has left the window, once more with another one:
+                    // with two staging buffers that is looked at when all 128 are there, with one for each 64 before they leave.
+                    float s = 0.f, rounded = 0.f;
+                    const float c = a.c;
+                    const bool plain = __all_sync(0xffffffffu, ok) && n + 128 <= a.dim_n;
+#pragma unroll 1
+                    for (int turn = 0; turn < 2; ++turn) {
+                        float top = 0.f;
+                        bool again = false;
+                        s = rounded = 0.f;
+#pragma unroll 1
+                        for (int half = 0; half < 2; ++half) {
+                            if (a.store && (S::kBuffers == 1 || half == 0)) reuse();
+                            unsigned char *buffer = stage + (S::kBuffers == 2 ? half : 0) * kStageOut;
+                            float v[64];
+                            read(half, v);
+                            if ((unsigned)(label - half * 64) < 64u) {
+#pragma unroll
+                                for (int j = 0; j < 64; ++j)
+                                    if (label - half * 64 == j) a.picked[row] = v[j];
+                            }
+                            const int left = plain ? 64 : ok ? a.dim_n - n - half * 64 : 0;
+                            float s1 = 0.f, r1 = 0.f;
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) {
+                                uint32_t w[4];
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) {
+                                    const int i = j * 8 + e * 2;
+                                    float x = ex2(fmaf(v[i], c, -ref)), y = ex2(fmaf(v[i + 1], c, -ref));
+                                    if (!plain) {
+                                        x = i < left ? x : 0.f;
+                                        y = i + 1 < left ? y : 0.f;
+                                    }
+                                    top = fmaxf(top, fmaxf(x, y));
+                                    s += x;
+                                    s1 += y;
+                                    w[e] = pack2(x, y);
+                                    rounded += low(w[e]);
+                                    r1 += high(w[e]);
+                                }
+                                if (a.store) stage8(buffer, j, w);
+                            }
+                            s += s1;
+                            rounded += r1;
+                            // (a lane without a column has 0 everywhere)
+                            if (turn == 0 && (S::kBuffers == 1 || half == 1)) {
+                                const bool out = ok && n + half * 64 < a.dim_n && !(top >= kLeast && top <= kMost);
+                                again = __any_sync(0xffffffffu, out);
+                                if (again) break;
+                            }
+                            if (a.store && S::kBuffers == 1) send(half, half + 1, 0x7fffffff, true);
+                        }
+                        if (!again) break;
+                        // (what has left has arrived before it is written again)
+                        if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+                        __syncwarp();
+                        float m = kNoRef;
+#pragma unroll 1
+                        for (int half = 0; half < 2; ++half) {
+                            float v[64];
+                            read(half, v);
+                            const int left = a.dim_n - n - half * 64;
+#pragma unroll
+                            for (int j = 0; j < 64; ++j) m = j < left ? fmaxf(m, v[j]) : m;
+                        }
+                        // (unchanged where the largest one is in the window)
+                        if (ok) ref += 128.f * rintf((fmaxf(m * c, -1e9f) - ref) * (1.f / 128.f));
+                    }
+                    if (last_read) release();
+                    if (a.store && S::kBuffers == 2) send(0, 2, 0x7fffffff, true);
+                    if (ok && n < a.dim_n) a.part[(size_t)row * a.chunks + n / kChunk] = make_float4(ref, s, rounded, 0.f);
+                } else if (PRODUCT == kHidden) {
+                    // (four columns of a tile's rows follow one another in scratch: a warp writes 512 bytes at a time)
+                    float4 *part = reinterpret_cast<float4 *>(a.scratch + (size_t)max(work.part, 0) * S::kTileFloats) +
+                                   (half_tile * 64 + h * 32) * S::kM + rank * kBM + q * 32 + lane;
 #pragma unroll 1
                     for (int half = 0; half < 2; ++half) {
                         float v[64];
                         read(half, v);
-                        const int left = a.dim_n - n - half * 64;
+                        if (half == 1 && last_read) release();
+                        if (work.part >= 0) {
+                            if (!ok) continue;
 #pragma unroll
-                        for (int j = 0; j < 64; ++j) m = j < left ? fmaxf(m, v[j]) : m;
-                    }
-                    // (unchanged where the largest one is in the window)
-                    if (ok) ref += 128.f * rintf((fmaxf(m * c, -1e9f) - ref) * (1.f / 128.f));
-                }
-                release();
-                if (a.store && S::kBuffers == 2) send(0, 2, 0x7fffffff, true);
-                if (ok && n < a.dim_n) a.part[(size_t)row * a.chunks + n / kChunk] = make_float4(ref, s, rounded, 0.f);
-            } else if (PRODUCT == kHidden) {
-                // (four columns of a tile's rows follow one another in scratch: a warp writes 512 bytes at a time)
-                float4 *part = reinterpret_cast<float4 *>(a.scratch + (size_t)max(work.part, 0) * S::kTileFloats) +
-                               (half_tile * 64 + h * 32) * S::kM + rank * kBM + q * 32 + lane;
-#pragma unroll 1
-                for (int half = 0; half < 2; ++half) {
-                    float v[64];
-                    read(half, v);
-                    if (half == 1) release();
-                    if (work.part >= 0) {
-                        if (!ok) continue;
-#pragma unroll
-                        for (int j = 0; j < 16; ++j)
-                            part[(half * 16 + j) * S::kM] = make_float4(v[j * 4], v[j * 4 + 1], v[j * 4 + 2], v[j * 4 + 3]);
-                        continue;
-                    }
-                    const float4 *mean = reinterpret_cast<const float4 *>(a.w_mean + n + half * 64);
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) {
-                        const float4 w = __ldg(mean + j);
-                        v[j * 4] = fmaf(v[j * 4], scale.x, scale.y * w.x);
-                        v[j * 4 + 1] = fmaf(v[j * 4 + 1], scale.x, scale.y * w.y);
-                        v[j * 4 + 2] = fmaf(v[j * 4 + 2], scale.x, scale.y * w.z);
-                        v[j * 4 + 3] = fmaf(v[j * 4 + 3], scale.x, scale.y * w.w);
-                    }
-                    stage64(stage + (S::kBuffers == 2 ? half : 0) * kStageOut, v);
-                    send(half, half + 1, 0, true);
-                }
-            } else {
-                float4 *sum = reinterpret_cast<float4 *>(a.scratch + ((size_t)t.x * plan.n_tiles + t.y) * S::kTileFloats) +
-                              (half_tile * 64 + h * 32) * S::kM + rank * kBM + q * 32 + lane;
-                if (last && S::kBuffers == 2) reuse();
-#pragma unroll 1
-                for (int half = 0; half < 2; ++half) {
-                    float v[64];
-                    read(half, v);
-                    if (half == 1) release();
-                    if (!first) {
-                        float4 old[16];
-#pragma unroll
-                        for (int j = 0; j < 16; ++j) old[j] = sum[(half * 16 + j) * S::kM];
+                            for (int j = 0; j < 16; ++j)
+                                part[(half * 16 + j) * S::kM] = make_float4(v[j * 4], v[j * 4 + 1], v[j * 4 + 2], v[j * 4 + 3]);
+                            continue;
+                        }
+                        const float4 *mean = reinterpret_cast<const float4 *>(a.w_mean + n + half * 64);
 #pragma unroll
                         for (int j = 0; j < 16; ++j) {
-                            v[j * 4] += old[j].x; v[j * 4 + 1] += old[j].y; v[j * 4 + 2] += old[j].z; v[j * 4 + 3] += old[j].w;
+                            const float4 w = __ldg(mean + j);
+                            v[j * 4] = fmaf(v[j * 4], scale.x, scale.y * w.x);
+                            v[j * 4 + 1] = fmaf(v[j * 4 + 1], scale.x, scale.y * w.y);
+                            v[j * 4 + 2] = fmaf(v[j * 4 + 2], scale.x, scale.y * w.z);
+                            v[j * 4 + 3] = fmaf(v[j * 4 + 3], scale.x, scale.y * w.w);
                         }
-                    }
-                    if (last) {
-                        if (S::kBuffers == 1) reuse();
                         stage64(stage + (S::kBuffers == 2 ? half : 0) * kStageOut, v);
-                        if (S::kBuffers == 1 || half == 1) send(S::kBuffers == 1 ? half : 0, half + 1, a.bulk_cols, m_warp < a.dim_m);
-                    } else {
+                        send(half, half + 1, 0, true);
+                    }
+                } else {
+                    float4 *sum = reinterpret_cast<float4 *>(a.scratch + ((size_t)t.x * plan.n_tiles + t.y) * S::kTileFloats) +
+                                  (half_tile * 64 + h * 32) * S::kM + rank * kBM + q * 32 + lane;
+                    if (last && S::kBuffers == 2) reuse();
+#pragma unroll 1
+                    for (int half = 0; half < 2; ++half) {
+                        float v[64];
+                        read(half, v);
+                        if (half == 1 && last_read) release();
+                        if (!first) {
+                            float4 old[16];
 #pragma unroll
-                        for (int j = 0; j < 16; ++j)
-                            sum[(half * 16 + j) * S::kM] = make_float4(v[j * 4], v[j * 4 + 1], v[j * 4 + 2], v[j * 4 + 3]);
+                            for (int j = 0; j < 16; ++j) old[j] = sum[(half * 16 + j) * S::kM];
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) {
+                                v[j * 4] += old[j].x; v[j * 4 + 1] += old[j].y; v[j * 4 + 2] += old[j].z; v[j * 4 + 3] += old[j].w;
+                            }
+                        }
+                        if (last) {
+                            if (S::kBuffers == 1) reuse();
+                            stage64(stage + (S::kBuffers == 2 ? half : 0) * kStageOut, v);
+                            if (S::kBuffers == 1 || half == 1) send(S::kBuffers == 1 ? half : 0, half + 1, a.bulk_cols, m_warp < a.dim_m);
+                        } else {
+#pragma unroll
+                            for (int j = 0; j < 16; ++j)
+                                sum[(half * 16 + j) * S::kM] = make_float4(v[j * 4], v[j * 4 + 1], v[j * 4 + 2], v[j * 4 + 3]);
+                        }
                     }
                 }
             }
@@ -652,7 +658,8 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     }
 }
 
-// The tiles of dH that were cut along the vocabulary: a block adds up 32 rows x 64 columns of their slices, in order, and turns them in shared memory so that rows leave in runs.
+// The tiles of dH that were cut along the vocabulary: a block adds up 32 rows x 64 columns of their slices, in order, and turns
+// them in shared memory so that rows leave in runs.
 constexpr int kJoinThreads = 256;
 template <int MODE> constexpr int join_blocks() { return (Shape<MODE>::kM / 32) * (Shape<MODE>::kN / 64); }
 template <int MODE>
@@ -1326,7 +1333,8 @@ extern "C" int ppo_lmhead_xent(const void *H, int64_t ldh, const void *W, int64_
     r.labels = labels; r.mask = mask; r.ignore_id = ignore_id;
     // The tensor cores cut off the sums that they keep: logits that grow evenly over the hidden elements come out smaller by 8.3e-10
     // of themselves per element (measured, K = 64 to 4096), which is made up for here (lse at K = 4096: 2.6e-6 off without, 4e-7 with).
-    r.c = (float)(1.4426950408889634 / (double)temperature * (1.0 + 8.3e-10 * (double)K)); r.inv_tau = 1.f / temperature; r.scale = scale; r.denom = denom;
+    r.c = (float)(1.4426950408889634 / (double)temperature * (1.0 + 8.3e-10 * (double)K));
+    r.inv_tau = 1.f / temperature; r.scale = scale; r.denom = denom;
     r.n_real = reinterpret_cast<int *>(mem + l.n_real);
     r.order = reinterpret_cast<int32_t *>(mem + l.order);
     r.W = reinterpret_cast<const __nv_bfloat16 *>(W); r.ldw = ldw; r.vk = vk;
