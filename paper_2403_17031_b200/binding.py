@@ -929,8 +929,8 @@ def _tensor_arrays(tensors, at: int, name: str):
 def grad_clip(grads, max_norm: float, scale: float = 1.0, out=None, workspace: Optional[torch.Tensor] = None,
               scratch: Optional[torch.Tensor] = None, norm: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Scales a list of gradients (contiguous, fp32 or bf16) by scale * min(1, max_norm / norm) with the norm over all of
-    scale * gradients; in place, or into the list `out` (each fp32 or bf16). Returns norm [2] f32: the norm before clipping
-    and the factor min(1, max_norm / norm)."""
+    scale * gradients; in place, or into the list `out` (each fp32 or bf16). No two tensors that are written may share memory.
+    Returns norm [2] f32: the norm before clipping and the factor min(1, max_norm / norm)."""
     n = len(grads)
     if not n:
         raise ValueError("grad_clip needs a gradient")
@@ -945,6 +945,9 @@ def grad_clip(grads, max_norm: float, scale: float = 1.0, out=None, workspace: O
         outs, sizes, out_dtype = _tensor_arrays(out, at, "out")
         if sizes != numel:
             raise ValueError("out must hold a tensor of the same size for each gradient")
+    written = ins if outs is None else outs
+    if len(set(written)) < n and len({p for p, k in zip(written, numel) if k}) < sum(1 for k in numel if k):
+        raise ValueError("a tensor that is written may be listed only once")
     if norm is None:
         norm = first.new_empty(2, dtype=torch.float32)
     elif norm.numel() != 2:

@@ -150,3 +150,16 @@ def test_refusals(P):
         P.grad_clip([g.double()], 1.0)
     with pytest.raises(ValueError):
         P.grad_clip([g], 1.0, out=[g[:5]])
+
+
+def test_a_tensor_is_written_once(P):
+    a, b = make([10, 10], [F32])
+    empty = a[:0]
+    for args in (dict(grads=[a, b, a]), dict(grads=[a, b], out=[a, a])):
+        with pytest.raises(ValueError):
+            P.grad_clip(max_norm=1.0, **args)
+    want = 2 * (f64(a) ** 2).sum()
+    out = [torch.empty_like(a), torch.empty_like(a)]
+    norm = P.grad_clip([a, a], 1e9, out=out)                    # read twice: allowed
+    assert abs(norm[0].item() ** 2 / want - 1) < 16 * 2.0 ** -24 and torch.equal(out[0], out[1])
+    P.grad_clip([a, empty, b, empty], 1.0)
