@@ -249,7 +249,7 @@ class SFTStep:
         scratch = lambda n: torch.empty(max(n, 256), dtype=u8, device=dev)          # noqa: E731
         # (one buffer: the two calls that need it do not overlap)
         self._scratch = scratch(max(_b.lmhead_xent_scratch_bytes(N, K, V, piece_rows), _b.embed_bwd_scratch_bytes(N, K, V)))
-        self._clip_scratch = None
+        self._clip_scratch = {}
         self.out = {"hidden": torch.empty((N, K), dtype=bf16, device=dev), "loss": torch.empty((), dtype=f32, device=dev),
                     "nll": torch.empty(N, dtype=f32, device=dev), "lse": torch.empty(N, dtype=f32, device=dev),
                     "dH": torch.empty((N, K), dtype=bf16, device=dev), "dW": torch.empty_like(W),
@@ -279,9 +279,10 @@ class SFTStep:
         dW = o["dW"] if o["dW"].is_contiguous() else o["dW"].t()                    # (the same elements, in memory's order)
         grads = [dW, o["dE"], *others]
         need = _b.grad_clip_scratch_bytes(len(grads))
-        if self._clip_scratch is None or self._clip_scratch.numel() < need:
-            self._clip_scratch = torch.empty(need, dtype=torch.uint8, device=o["norm"].device)
-        return _b.grad_clip(grads, max_norm, scale=scale, workspace=self.workspace, scratch=self._clip_scratch, norm=o["norm"])
+        # (one for each size, all kept: a captured graph may hold the address of any)
+        if need not in self._clip_scratch:
+            self._clip_scratch[need] = torch.empty(need, dtype=torch.uint8, device=o["norm"].device)
+        return _b.grad_clip(grads, max_norm, scale=scale, workspace=self.workspace, scratch=self._clip_scratch[need], norm=o["norm"])
 
     def device_status(self) -> int:
         return _b.last_device_status(self.workspace)

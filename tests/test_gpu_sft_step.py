@@ -140,3 +140,23 @@ def test_a_step_without_a_real_row(P):
     o = step.loss(step.out["hidden"], W, labels, torch.zeros_like(mask))
     step.grad_embed(o["dH"], tokens)
     assert float(o["loss"]) == 0 and step.clip(1.0).tolist() == [0.0, 1.0] and step.device_status() == 2
+
+
+def test_a_longer_list_leaves_a_captured_clip_its_scratch(P):
+    from paper_2403_17031_b200.pipeline import SFTStep
+    E, W, mid, tokens, labels, mask = setup(50, 64, 304, False)
+    step = SFTStep(W, 50, padding_id=1)
+    fill = lambda: (step.out["dW"].fill_(1), step.out["dE"].fill_(1))                # noqa: E731
+    fill()
+    step.clip(1.0)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step.clip(1.0)
+    scratch = next(iter(step._clip_scratch.values()))
+    fill()
+    step.clip(1.0, [torch.ones(3, device="cuda") for _ in range(1000)])
+    assert any(t is scratch for t in step._clip_scratch.values())
+    fill()
+    graph.replay()
+    n = step.out["dW"].numel() + step.out["dE"].numel()
+    assert abs(step.out["norm"][0].item() / n ** 0.5 - 1) < 2.0 ** -22
