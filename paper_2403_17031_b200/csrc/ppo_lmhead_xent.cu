@@ -731,6 +731,8 @@ struct RowArgs {
     int64_t ldw;
     int vk;
     float *w_mean;                                              // [K] mean of kSample columns of W
+    float *cut;                                                 // [M] what real row i's logits have lost, all alike
+    float cut_in_c;                                             // c is larger by this, relative
     int2 *info;                                                 // [M] label and reference of real row i
     int in_place;                                               // product 1 reads H where it lies when all rows are real
     __nv_bfloat16 *packed;                                      // [M, Kp] real rows (unless they can be read in place)
@@ -882,8 +884,12 @@ pack_kernel(const RowArgs a)
     const __nv_bfloat16 *from = a.H + (int64_t)row * a.ldh;
     __nv_bfloat16 *to = a.packed + (int64_t)i * a.Kp;
     const bool pack = n < a.M || !a.in_place;
-    float s = 0.f;
-    for (int k = threadIdx.x * 8; k < a.K; k += kRowThreads * 8) {
+    // Product with the mean column, and beside it what the tensor cores cut off of the sums that all columns have in common: after
+    // every 16 elements, to a quarter of the last place and then to the last place, 3/8 of it on average.
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    float before = 0.f, cut = 0.f;                              // the sum ahead of these 2048 elements; powers of two of the sums
+    for (int k = threadIdx.x * 8, k0 = 0; k0 < a.K; k += kRowThreads * 8, k0 += kRowThreads * 8) {
+        float s = 0.f;
         if (k + 8 <= a.K) {
             const uint4 v = *reinterpret_cast<const uint4 *>(from + k);
             if (pack) *reinterpret_cast<uint4 *>(to + k) = v;
@@ -896,14 +902,33 @@ pack_kernel(const RowArgs a)
                 s = fmaf(__bfloat162float(from[e]), a.w_mean[e], s);
             }
         }
+#pragma unroll
+        for (int off = 1; off < 32; off <<= 1) {
+            const float o = __shfl_up_sync(0xffffffffu, s, off);
+            if (lane >= off) s += o;
+        }
+        if (lane == 31) red[warp] = s;
+        __syncthreads();
+        float ahead = before;
+#pragma unroll
+        for (int w = 0; w < kRowThreads / 32; ++w) {
+            if (w < warp) ahead += red[w];
+            before += red[w];
+        }
+        if (k < a.K && (lane & 1 || k + 8 >= a.K)) cut += __int_as_float(__float_as_int(ahead + s) & 0xff800000);
+        __syncthreads();
     }
-    s = warp_sum_f(s);
-    if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = s;
+    cut = warp_sum_f(cut);
+    if (lane == 0) red[warp] = cut;
     __syncthreads();
     if (threadIdx.x == 0) {
-        s = 0.f;
+        float s = before;
+        cut = 0.f;
 #pragma unroll
-        for (int w = 0; w < kRowThreads / 32; ++w) s += red[w];
+        for (int w = 0; w < kRowThreads / 32; ++w) cut += red[w];
+        // (less what the factor c makes up for already; 3/8 of a last place is 3 * 2^-26 of the power of two)
+        cut = (cut * 4.4703484e-8f - a.cut_in_c * s) * a.inv_tau;
+        a.cut[i] = fabsf(cut) < 1.f ? cut : 0.f;
         // the middle of the window; whole numbers, so that y - reference loses nothing that y does not
         s = rintf(s * a.c) + 32.f;
         a.info[i] = make_int2(a.labels[row], __float_as_int(fabsf(s) < 1e9f ? s : 0.f));
@@ -1021,7 +1046,7 @@ row_kernel(const RowArgs a)
     const float l2s = log2f(s), nan = __int_as_float(0x7fffffff);
     if (threadIdx.x == 0) {
         a.nll[row] = ((m - acc * a.c) + l2s) * kLn2;
-        if (a.lse) a.lse[row] = (m + l2s) * kLn2;
+        if (a.lse) a.lse[row] = fmaf(m + l2s, kLn2, __ldcg(a.cut + a.row0 + r));
         if (bad && a.status) atomicOr(a.status, PPO_DEV_BAD_TOKEN);
     }
     if (!a.u) return;
@@ -1092,7 +1117,7 @@ constexpr int kPieceRows = 256;                                 // a piece is a 
 struct Layout {
     int pieces, rows_max, chunks, Kp;
     int64_t Vp;
-    size_t n_real, slices, order, info, w_mean, picked, row_scale, part, packed, scaled, u, parts, sums, bytes;
+    size_t n_real, slices, order, info, cut, w_mean, picked, row_scale, part, packed, scaled, u, parts, sums, bytes;
 };
 
 // Pieces of at most 8192 rows by default: at V = 50304 that is 824 MB of U, and the sums of dW, read and written once a
@@ -1121,6 +1146,7 @@ static Layout layout_of(int64_t M, int64_t K, int64_t V, int64_t piece_rows, boo
     l.slices = take(8);
     l.order = take((size_t)M * 4);
     l.info = take((size_t)M * sizeof(int2));
+    l.cut = take((size_t)M * 4);
     l.w_mean = take((size_t)(K + 511) / 512 * 512 * 4);
     l.picked = take(rows * 4);
     l.row_scale = take(rows * sizeof(float2));
@@ -1333,6 +1359,9 @@ extern "C" int ppo_lmhead_xent(const void *H, int64_t ldh, const void *W, int64_
     r.labels = labels; r.mask = mask; r.ignore_id = ignore_id;
     // The tensor cores cut off the sums that they keep: logits that grow evenly over the hidden elements come out smaller by 8.3e-10
     // of themselves per element (measured, K = 64 to 4096), which is made up for here (lse at K = 4096: 2.6e-6 off without, 4e-7 with).
+    // A part that all of a row's logits have in common may come in a few elements, and loses more: pack_kernel follows it, and lse
+    // gets that back (logits near -90 out of one element, K = 4096: 4.4e-4 off without, 2e-5 with); nll and the gradients do not depend on it.
+    r.cut_in_c = (float)(8.3e-10 * (double)K);
     r.c = (float)(1.4426950408889634 / (double)temperature * (1.0 + 8.3e-10 * (double)K));
     r.inv_tau = 1.f / temperature; r.scale = scale; r.denom = denom;
     r.n_real = reinterpret_cast<int *>(mem + l.n_real);
@@ -1340,6 +1369,7 @@ extern "C" int ppo_lmhead_xent(const void *H, int64_t ldh, const void *W, int64_
     r.W = reinterpret_cast<const __nv_bfloat16 *>(W); r.ldw = ldw; r.vk = vk;
     r.w_mean = reinterpret_cast<float *>(mem + l.w_mean);
     r.info = reinterpret_cast<int2 *>(mem + l.info);
+    r.cut = reinterpret_cast<float *>(mem + l.cut);
     r.in_place = ldh % 64 == 0 && reinterpret_cast<uintptr_t>(H) % 128 == 0;
     r.packed = reinterpret_cast<__nv_bfloat16 *>(mem + l.packed);
     r.scaled = dW ? reinterpret_cast<__nv_bfloat16 *>(mem + l.scaled) : nullptr;

@@ -268,3 +268,25 @@ def test_refuses_what_it_does_not_take(P):
         P.lmhead_xent(H, W.float(), labels)
     with pytest.raises(ValueError):
         P.lmhead_xent(H, W, labels, scratch=torch.empty(256, dtype=torch.uint8, device="cuda"))
+
+
+@pytest.mark.parametrize("kind", ["first", "last", "four", "even"])
+@pytest.mark.parametrize("shift", [-90.0, 40.0])
+def test_lse_of_logits_far_from_zero(P, kind, shift):
+    """The tensor cores cut their sums off after every 16 elements: at K = 4096 that is 256 times 3/8 of 2^-17 on average for sums between
+    64 and 128, 7.3e-4 in all where one element brings the sum there. What is common to a row's logits is given back to lse. Left is the
+    chance of single cuts (0 to 3 quarters of 2^-17, each 0.28 2^-17 off the mean: 16 * 0.28 * 2^-17 = 3.4e-5 for a column; five times that), what the factor on the logits
+    adds for columns up to 15 above the mean (3.4e-6 15 = 5e-5), and four roundings of 90 in fp32 (4.3e-5): 2.6e-4."""
+    M, K, V = 40, 4096, 3000
+    g = torch.Generator().manual_seed(11)
+    H, W = torch.randn(M, K, generator=g), torch.randn(K, V, generator=g) * (3 / K ** 0.5)
+    at = {"first": [0], "last": [K - 1], "four": [0, 700, 1400, 2100]}.get(kind)
+    if at:
+        H[:, at], W[at] = 8.0, shift / 8 / len(at)
+    else:
+        H, W = H + 1, W + shift / K
+    H, W = H.to(BF16).cuda(), W.to(BF16).cuda()
+    labels = torch.randint(0, V, (M,), generator=g, dtype=I32).cuda()
+    o = P.lmhead_xent(H, W, labels, want_dH=False, want_dW=False)
+    want = torch.logsumexp(H.double() @ W.double(), 1)
+    assert (o["lse"].double() - want).abs().max() <= 2.6e-4
