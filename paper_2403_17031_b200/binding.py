@@ -782,7 +782,7 @@ W_KV, W_VK = 0, 1
 
 
 def _head_weight(W: torch.Tensor, at: int, name: str):
-    """(address, row pitch, layout, V) of a bf16 weight [K, V] that is stored by rows ([K, V]) or by columns ([V, K], e.g. the
+    """(address, row pitch, layout) of a bf16 weight [K, V] that is stored by rows ([K, V]) or by columns ([V, K], e.g. the
     transpose of a linear layer's weight)."""
     if W.dim() != 2 or W.get_device() != at or W.dtype != torch.bfloat16:
         raise TypeError("%s must be a bfloat16 matrix on the device of the call's first tensor" % name)
@@ -793,6 +793,17 @@ def _head_weight(W: torch.Tensor, at: int, name: str):
     if s0 == 1 and (s1 >= K or V <= 1):
         return W.data_ptr(), s1 if V > 1 else -(-K // 8) * 8, W_VK
     raise TypeError("%s must be stored by rows or by columns" % name)
+
+
+def _head_gradient(dW: torch.Tensor, layout: int, at: int, name: str):
+    """(address, row pitch) of a gradient [K, V] that is stored as its weight is. A size of one has a stride that says nothing: the
+    layout is the weight's, not what the strides look like."""
+    if dW.dim() != 2 or dW.get_device() != at or dW.dtype != torch.bfloat16:
+        raise TypeError("%s must be a bfloat16 matrix on the device of the call's first tensor" % name)
+    (rows, inner), (pitch, step) = (dW.shape, dW.stride()) if layout == W_KV else (dW.shape[::-1], dW.stride()[::-1])
+    if (step != 1 and inner > 1) or (pitch < inner and rows > 1):
+        raise ValueError("%s must have the layout of its weight" % name)
+    return dW.data_ptr(), pitch if rows > 1 else inner
 
 
 def lmhead_xent_scratch_bytes(M: int, K: int, V: int, piece_rows: int = 0, want_dH: bool = True, want_dW: bool = True) -> int:
@@ -843,9 +854,9 @@ def lmhead_xent(H: torch.Tensor, W: torch.Tensor, labels: torch.Tensor, mask: Op
         if dH.shape != (M, K) or dH.dtype != bf16:
             raise ValueError("dH must be a bfloat16 [%d, %d]" % (M, K))
     if dW is not None:
-        dwp, lddw, dlayout = _head_weight(dW, at, "dW")
-        if dW.shape != W.shape or (dlayout != layout and min(K, V) > 1):
-            raise ValueError("dW must have the shape and the layout of W")
+        if dW.shape != W.shape:
+            raise ValueError("dW must have the shape of W")
+        dwp, lddw = _head_gradient(dW, layout, at, "dW")
     need = lmhead_xent_scratch_bytes(M, K, V, piece_rows, dH is not None, dW is not None)
     if scratch is None:
         scratch = H.new_empty(max(need, 1), dtype=torch.uint8)

@@ -290,3 +290,13 @@ def test_lse_of_logits_far_from_zero(P, kind, shift):
     o = P.lmhead_xent(H, W, labels, want_dH=False, want_dW=False)
     want = torch.logsumexp(H.double() @ W.double(), 1)
     assert (o["lse"].double() - want).abs().max() <= 2.6e-4
+
+
+@pytest.mark.parametrize("layout", ["kv", "vk"])
+@pytest.mark.parametrize("M,K,V", [(2, 1, 135), (70, 1, 135), (300, 1, 3), (5, 1, 1), (4, 40, 1), (200, 9, 1)])
+def test_sizes_of_one(P, M, K, V, layout):
+    H, W, labels = make(M, K, V, layout, seed=17)
+    before = W.clone()
+    o = P.lmhead_xent(H, W, labels)
+    check(o, H, W, labels, np.ones(M), 1.0)
+    assert torch.equal(W, before) and o["dW"].shape == (K, V)

@@ -91,3 +91,28 @@ def test_binding_refuses_what_does_not_fit(b):
         b.grad_clip([x], 1.0)
     with pytest.raises(ValueError):
         b.grad_clip([], 1.0)
+
+
+@pytest.mark.parametrize("K,V", [(1, 5), (5, 1), (1, 1), (3, 4), (1, 8), (8, 1)])
+@pytest.mark.parametrize("layout", [0, 1])
+@pytest.mark.parametrize("more", [0, 3])
+def test_a_gradient_lies_as_its_weight_says_also_with_a_size_of_one(b, K, V, layout, more):
+    """Strides of a size of one say nothing: address of (k, v) as the library forms it, against torch's."""
+    bf16 = torch.bfloat16
+    rows, inner = (K, V) if layout == b.W_KV else (V, K)
+    for t in (torch.empty(rows, inner + more, dtype=bf16)[:, :inner], torch.empty(rows, inner, dtype=bf16),
+              torch.empty(inner, rows, dtype=bf16).t(), torch.empty(rows, 2 * inner, dtype=bf16)[:, ::2]):
+        dW = t if layout == b.W_KV else t.t()
+        assert dW.shape == (K, V)
+        fits = all(k * dW.stride(0) + v * dW.stride(1) == (k * (dW.stride(0) if layout == b.W_KV else 1) + v * (1 if layout == b.W_KV else dW.stride(1)))
+                   for k in range(K) for v in range(V)) and (rows <= 1 or t.stride(0) >= inner)
+        if not fits:
+            with pytest.raises(ValueError):
+                b._head_gradient(dW, layout, -1, "dW")
+            continue
+        at, pitch = b._head_gradient(dW, layout, -1, "dW")
+        assert at == dW.data_ptr() and pitch >= inner
+        for k in range(K):
+            for v in range(V):
+                r, i = (k, v) if layout == b.W_KV else (v, k)
+                assert r * pitch + i == k * dW.stride(0) + v * dW.stride(1)
