@@ -1014,9 +1014,10 @@ row_kernel(const RowArgs a)
     float s = 0.f, sr = 0.f;                                    // sums of U and of the rounded U
     for (int t = threadIdx.x; t < a.chunks; t += kRowThreads) {
         const float4 p = t < kRowThreads ? mine[0] : t < 2 * kRowThreads ? mine[1] : part[t];
-        const float f = ex2(p.x - m);
-        s = fmaf(p.y, f, s);
-        sr = fmaf(p.z, f, sr);
+        // (2^-128 is no normal number, but 2^64 times it counts beside a largest value of 2^-64: in two steps)
+        const float f = ex2(0.5f * (p.x - m));
+        s = fmaf(p.y * f, f, s);
+        sr = fmaf(p.z * f, f, sr);
         if (p.x != m && a.u) {
             // (16-byte pieces of 8 columns; the columns behind V are not used)
             uint4 *u = reinterpret_cast<uint4 *>(a.u + (int64_t)r * a.Vp + (int64_t)t * kChunk);
@@ -1025,7 +1026,7 @@ row_kernel(const RowArgs a)
                 uint4 v = u[j];
                 uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-                for (int e = 0; e < 4; ++e) w[e] = pack2(low(w[e]) * f, high(w[e]) * f);
+                for (int e = 0; e < 4; ++e) w[e] = pack2(low(w[e]) * f * f, high(w[e]) * f * f);
                 u[j] = make_uint4(w[0], w[1], w[2], w[3]);
             }
         }
@@ -1054,7 +1055,7 @@ row_kernel(const RowArgs a)
     float f = nan, c = nan;
     if (!bad) {
         const float ref = part[label / kChunk].x;
-        const float u = __bfloat162float(__float2bfloat16_rn(ex2(fmaf(acc, a.c, -ref)))) * ex2(ref - m);
+        const float step = ex2(0.5f * (ref - m)), u = __bfloat162float(__float2bfloat16_rn(ex2(fmaf(acc, a.c, -ref)))) * step * step;
         const float want = u - sr;
         const __nv_bfloat16 stored = __float2bfloat16_rn(want);
         const float got = __bfloat162float(stored);

@@ -300,3 +300,20 @@ def test_sizes_of_one(P, M, K, V, layout):
     o = P.lmhead_xent(H, W, labels)
     check(o, H, W, labels, np.ones(M), 1.0)
     assert torch.equal(W, before) and o["dW"].shape == (K, V)
+
+
+@pytest.mark.parametrize("M", [1, 26, 100, 300])
+@pytest.mark.parametrize("layout", ["kv", "vk"])
+def test_columns_beside_the_largest_with_a_reference_of_their_own(P, M, layout):
+    """Logits 2^y with a row's mean at 0: the sampled columns and their reference lie there, the largest values at the edges of what it
+    serves (base 2: -32 to 96) and 128 from there, in chunks beside one another: each of them counts."""
+    H, W, labels = make(M, 64, 1500, layout, seed=18)
+    H.zero_()
+    H[:, 0], H[:, 1] = 8.0, 0.25
+    base = torch.zeros(1500, dtype=torch.float64)
+    for chunk, y in enumerate((95.5, 96.5, 97.0, 95.0, -40.0, 96.0, 97.5)):
+        base[128 * chunk + 5] = y
+        base[128 * chunk + 77] = y - 1
+    W[0] = (base * float(np.log(2.0)) / 8).to(BF16).cuda()
+    labels[::3] = 133
+    check(P.lmhead_xent(H, W, labels), H, W, labels, np.ones(M), 1.0)
