@@ -530,6 +530,7 @@ int ppo_fp8_matmul(const void *A, int64_t lda, const float *a_scales, const void
  *       uninitialised, for this call alone while it runs (NULL where M == 0)
  * Sums are fp32 on the tensor cores in an order that the sizes fix, so results are bit-reproducible; 2^(z - reference) and
  * gradient factor times H are rounded to bf16 on the way to the gradients, which are rounded once more.
+ * A probability under 2^-61 may count as 0 in the gradients.
  * Errors: PPO_ERR_PARAM (w_layout, temperature, scale), PPO_ERR_SHAPE, PPO_ERR_NULL, PPO_ERR_UNSUPPORTED, PPO_ERR_ALIGN.
  * M == 0: loss and dW are 0.
  */

@@ -14,7 +14,8 @@
 // A row's reference is set before product 1, from the mean of 64 neighbouring logits, and serves columns whose largest y lies
 // between 32 below and 96 above that mean: U and its sums stay inside fp32's (and bf16's) exponents, for logits of any size. 128
 // columns whose largest lies elsewhere move their own reference by multiples of 128; where a row's references differ, the columns
-// with a smaller one are multiplied by 2^(difference), which is exact, before product 2. (With references at multiples of 64,
+// with a smaller one are multiplied by 2^(difference), which is exact, before product 2 (what is then under 2^-126, less than
+// 2^-62 of the row's largest, becomes 0). (With references at multiples of 64,
 // whatever the row's logits, many rows had two: 1999 x 50277 x 1032 with logits near -90 took 704 us, 638 so.)
 //
 // Roundings to 16 bits: U, a H, and the results. Statistics, sums and nll are fp32, the loss fp64. What the rounding of U
@@ -562,7 +563,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                             rounded += r1;
                             // (a lane without a column has 0 everywhere)
                             if (turn == 0 && (S::kBuffers == 1 || half == 1)) {
-                                const bool out = ok && n + half * 64 < a.dim_n && !(top >= kLeast && top <= kMost);
+                                const bool out = ok && n + (S::kBuffers == 1 ? half * 64 : 0) < a.dim_n && !(top >= kLeast && top <= kMost);
                                 again = __any_sync(0xffffffffu, out);
                                 if (again) break;
                             }

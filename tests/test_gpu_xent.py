@@ -47,8 +47,8 @@ def make(M, K, V, layout="kv", seed=0, size=1.0, pad=0):
     return H, W if layout == "kv" else W.t(), labels
 
 
-def check(o, H, W, labels, real, tau, scale=1.0, denom=None):
-    """Compares a call's results with the definition; returns the oracle's."""
+def check(o, H, W, labels, real, tau, scale=1.0, denom=None, least=0.0):
+    """Compares a call's results with the definition; returns the oracle's. least: a probability that the gradients may take for 0."""
     h, w, real = f64(H), f64(W), np.asarray(real) != 0
     want = O.xent(h, w, npy(labels), real, tau, scale, denom)
     (M, K), V = h.shape, w.shape[1]
@@ -64,7 +64,7 @@ def check(o, H, W, labels, real, tau, scale=1.0, denom=None):
     assert not f64(o["nll"])[~real].any() and not f64(o["lse"])[~real].any()
     # p is off by twice the logits' error; at the label it is 1 - p that counts, off by that much of p
     D, er = np.abs(want["D"]), (2 * ez + 2 * es)[:, None]
-    p = D * er
+    p = D * er + least * abs(scale) / (d * tau) * real[:, None]
     for r in np.flatnonzero(real):
         p[r, npy(labels)[r]] = abs(scale) / (d * tau) * er[r, 0]
     tiny = 2.0 ** -120
@@ -317,3 +317,17 @@ def test_columns_beside_the_largest_with_a_reference_of_their_own(P, M, layout):
     W[0] = (base * float(np.log(2.0)) / 8).to(BF16).cuda()
     labels[::3] = 133
     check(P.lmhead_xent(H, W, labels), H, W, labels, np.ones(M), 1.0)
+
+
+@pytest.mark.parametrize("V", [300, 513, 576, 577, 640])
+@pytest.mark.parametrize("M", [5, 100, 300])
+@pytest.mark.parametrize("y", [-200.0, 120.0, 200.0])
+def test_the_last_columns_lie_far_from_the_others(P, M, V, y):
+    """One to 128 columns in the last chunk, with logits 2^y of their own; the largest ones, or the smallest. A row's largest U is 2^-64 at
+    least, and what is under 2^-126 beside it becomes 0: a probability of 2^-62."""
+    H, W, labels = make(M, 64, V, "vk", seed=19)
+    H[:, 0] = 8.0
+    W[0, :(V - 1) // 128 * 128] = 0
+    W[0, (V - 1) // 128 * 128:] = y * float(np.log(2.0)) / 8
+    labels[::3] = V - 1
+    check(P.lmhead_xent(H, W, labels), H, W, labels, np.ones(M), 1.0, least=2.0 ** -62)
