@@ -31,7 +31,7 @@
 // 256-column accumulator while the next is formed. Operands are read as they lie in memory, K-major or MN-major, so that W may be
 // stored [K, V] or [V, K].
 //
-// Bounds and times (calls one after the other): 27136 x 50304 x 4096 24.6 to 26.5 ms = 1260 to 1360 TFLOP/s, held by the board's
+// Bounds and times (calls one after the other): 27136 x 50304 x 4096 24.3 to 26.5 ms = 1260 to 1380 TFLOP/s, held by the board's
 // power (about 1.4 GHz); three bare library products of these shapes take 24 ms there. At full clock L2 bounds the pairs (13.4 TB/s into the SMs).
 // 1792 rows 1.52 ms (1460 TFLOP/s). 53 rows 258 us: W is streamed twice (products 1 and 2, 75 us each) and dW written once (75 us), 5.5 TB/s.
 #include "ppo_tcgen05.cuh"
@@ -57,8 +57,8 @@ constexpr float kLeast = 5.421010862427522e-20f, kMost = 1.8446744073709552e19f;
 // contractions.
 // kSingle: blocks alone on tiles of 128 x 128, for up to 128 rows: half of a pair's tile would be idle rows, the tensor cores would
 // take longer over them than memory over W, and there are too few wide tiles to share out evenly (197 of 256 columns at V =
-// 50304, on 148 SMs: 101 us for product 1 of 53 rows, now 88). What bounds them is how much of W is on its way: more stages, and one staging buffer a warp (53 x 50304 x 4096 in all: 3 stages 302 us,
-// 4 279, 5 266).
+// 50304, on 148 SMs: 101 us for product 1 of 53 rows, now 88). What bounds them is how much of W is on its way: more stages, and one
+// staging buffer a warp (53 x 50304 x 4096 in all: 3 stages 302 us, 4 279, 5 266).
 // kSmall: the same for products 1 and 2 of up to 64 rows: a stage holds 64 rows of A, so that there are eight. The matrix
 // instruction reads 128: the other 64 rows are what lies behind them (B), and their results are nobody's.
 enum Mode { kSingle, kPair, kWide, kSmall };
