@@ -1127,7 +1127,7 @@ struct Layout {
 static Layout layout_of(int64_t M, int64_t K, int64_t V, int64_t piece_rows, bool dh, bool dw)
 {
     Layout l;
-    const int64_t most = piece_rows > 0 ? piece_rows : 8192;
+    const int64_t asked = piece_rows > 0 ? piece_rows : 8192, most = asked < M ? asked : M;      // (any number may be asked for)
     l.pieces = (int)((M + most - 1) / most);
     const int64_t even = (M + l.pieces - 1) / l.pieces;
     l.rows_max = (int)((even + kPieceRows - 1) / kPieceRows * kPieceRows);
