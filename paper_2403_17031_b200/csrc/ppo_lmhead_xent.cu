@@ -87,10 +87,9 @@ struct Args {
     int gm, gn;
     int *status;
     // kLogits
-    float c;                                               // log2(e) / tau
     int in_place;                                          // H may be read where it lies
     const int32_t *order;                                  // order[i]: the original row of real row i
-    const int2 *info;                                      // [M] label and reference (as bits) of real row i
+    const int4 *info;                                      // [M] of real row i: label; as bits: reference, log2(e) / tau, `cut`
     float *picked;                                         // [rows] accumulator at the label
     float4 *part;                                          // [rows][chunks] reference, sum, sum of the rounded values
     int chunks, store;
@@ -436,14 +435,15 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             const uint32_t buf = tiles & 1;
             bool ok = false;
             int label_tile = -1, out_row = -1;
-            float ref_row = 0.f;
+            float ref_row = 0.f, c = 0.f;
             float2 scale = make_float2(0.f, 0.f);
             if (PRODUCT == kLogits) {
                 ok = row < rows;
                 if (ok) {
-                    const int2 info = a.info[a.row0 + row];
+                    const int4 info = a.info[a.row0 + row];
                     label_tile = (int)((unsigned)info.x - (unsigned)n_tile);
                     ref_row = __int_as_float(info.y);
+                    c = __int_as_float(info.z);
                 }
             } else if (PRODUCT == kHidden) {
                 ok = row < rows;
@@ -519,7 +519,6 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                     // U with the row's reference. Where a lane's largest value has left the window, once more with another one:
                     // with two staging buffers that is looked at when all 128 are there, with one for each 64 before they leave.
                     float s = 0.f, rounded = 0.f;
-                    const float c = a.c;
                     const bool plain = __all_sync(0xffffffffu, ok) && n + 128 <= a.dim_n;
 #pragma unroll 1
                     for (int turn = 0; turn < 2; ++turn) {
@@ -724,17 +723,16 @@ struct RowArgs {
     const int32_t *labels;
     const uint8_t *mask;
     int32_t ignore_id;
-    float c, inv_tau, scale;
+    double c;                                                   // log2(e) / tau
+    float inv_tau, scale;
     const float *denom;
     int32_t *order;                                             // [M] real rows, ascending; then the others
     int *n_real;
     const __nv_bfloat16 *W;
     int64_t ldw;
     int vk;
-    float *w_mean;                                              // [K] mean of kSample columns of W
-    float *cut;                                                 // [M] what real row i's logits have lost, all alike
-    float cut_in_c;                                             // c is larger by this, relative
-    int2 *info;                                                 // [M] label and reference of real row i
+    float *w_mean, *w_one;                                      // [K] mean of kSample columns of W, and the first of them
+    int4 *info;                                                 // [M] of real row i: label, reference, its c, what its logits have lost, all alike
     int in_place;                                               // product 1 reads H where it lies when all rows are real
     __nv_bfloat16 *packed;                                      // [M, Kp] real rows (unless they can be read in place)
     __nv_bfloat16 *scaled;                                      // [rows_max, Kp] a H; null: no gradients
@@ -751,7 +749,7 @@ struct RowArgs {
     int *status;
 };
 
-// The mean of kSample neighbouring columns of W, from the middle of the vocabulary, for some hidden elements: a thread loads
+// The mean of kSample neighbouring columns of W, from the middle of the vocabulary, and the first one, for some hidden elements: a thread loads
 // eight neighbours in memory, eight (stored [K, V]) or 64 (stored [V, K]) threads share an element. (One element after the
 // other, 64 loads each: 36 us at K = 4096, most of it misses of the address translation.)
 constexpr int kOrderThreads = 1024, kOrderPer = 8, kSample = 64, kMeanPer = kOrderThreads / 8;
@@ -775,6 +773,10 @@ __device__ __forceinline__ void mean_columns(const RowArgs &a, int k0, float (*p
                 for (int e = 0; e < 8; ++e)
                     if (k + e < a.K) x[e] += __bfloat162float(w[e]);
             }
+            if (j == 0)
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (k + e < a.K) a.w_one[k + e] = x[e];
         }
         // lanes 16 apart hold other rows for the same elements; then the warps
 #pragma unroll
@@ -802,6 +804,7 @@ __device__ __forceinline__ void mean_columns(const RowArgs &a, int k0, float (*p
             for (int e = 0; e < 8; ++e)
                 if (v + e < a.V) s += __bfloat162float(w[e]);
         }
+        if (v == v0) a.w_one[k] = __bfloat162float(w[0]);
     }
 #pragma unroll
     for (int off = 1; off < 8; off <<= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
@@ -864,11 +867,22 @@ order_kernel(const RowArgs a)
 }
 
 constexpr int kRowThreads = 256;
-// real rows: label and reference, and a packed copy where they are not read in place; the rows left out get their zeros
+// What the tensor cores cut off. After every 16 elements of the contraction they keep the sum to a quarter of its last place and
+// then to its last place, 3/8 of it on average (measured): 3 * 2^-26 of the sum's power of two. A logit that grows evenly passes through
+// sums whose powers of two average 0.36 of it, and loses 0.36 * 3 * 2^-26 / 16 = 1.0e-9 of itself for each element (measured: 0.9e-9 to
+// 1.1e-9 for K = 1024 to 131072 and logits up to 20; 1.4e-9 where all products have one sign). Nothing is lost where nothing can be: 16 elements
+// whose products (with a column of W that stands for all) are multiples of the last place of the sum of the absolute products so far
+// are not counted; such sums are exact whatever their order. Elements that are 0, in H or in W, are the plainest case.
+constexpr float kCutStep = 4.4703484e-8f;
+constexpr double kCutEven = 1.0e-9;
+constexpr unsigned kCutMost = 1u << 17;                        // elements: as far as it has been measured
+// real rows: label, reference and what they lose, and a packed copy where they are not read in place; the rows left out get their zeros
 __global__ void __launch_bounds__(kRowThreads)
 pack_kernel(const RowArgs a)
 {
-    __shared__ float red[kRowThreads / 32];
+    constexpr int kWarps = kRowThreads / 32;
+    __shared__ float red[2][kWarps];
+    __shared__ unsigned red_n[kWarps];
     grid_dependents_may_launch();
     grid_dependency_wait();
     const int n = *a.n_real, i = blockIdx.x;
@@ -885,54 +899,95 @@ pack_kernel(const RowArgs a)
     const __nv_bfloat16 *from = a.H + (int64_t)row * a.ldh;
     __nv_bfloat16 *to = a.packed + (int64_t)i * a.Kp;
     const bool pack = n < a.M || !a.in_place;
-    // Product with the mean column, and beside it what the tensor cores cut off of the sums that all columns have in common: after
-    // every 16 elements, to a quarter of the last place and then to the last place, 3/8 of it on average.
+    // Product with the mean column, and beside it what is cut off of the sums that all columns have in common.
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    float before = 0.f, cut = 0.f;                              // the sum ahead of these 2048 elements; powers of two of the sums
+    float before = 0.f, cut = 0.f, all = 0.f;                   // ahead of these 2048 elements: the sum, the absolute one; powers of two cut from
+    unsigned groups = 0;                                        // of 16 elements that cut
     for (int k = threadIdx.x * 8, k0 = 0; k0 < a.K; k += kRowThreads * 8, k0 += kRowThreads * 8) {
-        float s = 0.f;
+        float s = 0.f, size = 0.f, one[8];                      // `one`: products with a single column
+#pragma unroll
+        for (int e = 0; e < 8; ++e) one[e] = 0.f;
         if (k + 8 <= a.K) {
             const uint4 v = *reinterpret_cast<const uint4 *>(from + k);
             if (pack) *reinterpret_cast<uint4 *>(to + k) = v;
             const float4 p = *reinterpret_cast<const float4 *>(a.w_mean + k), q = *reinterpret_cast<const float4 *>(a.w_mean + k + 4);
             s = fmaf(low(v.x), p.x, s); s = fmaf(high(v.x), p.y, s); s = fmaf(low(v.y), p.z, s); s = fmaf(high(v.y), p.w, s);
             s = fmaf(low(v.z), q.x, s); s = fmaf(high(v.z), q.y, s); s = fmaf(low(v.w), q.z, s); s = fmaf(high(v.w), q.w, s);
+            const float4 x = *reinterpret_cast<const float4 *>(a.w_one + k), y = *reinterpret_cast<const float4 *>(a.w_one + k + 4);
+            one[0] = low(v.x) * x.x; one[1] = high(v.x) * x.y; one[2] = low(v.y) * x.z; one[3] = high(v.y) * x.w;
+            one[4] = low(v.z) * y.x; one[5] = high(v.z) * y.y; one[6] = low(v.w) * y.z; one[7] = high(v.w) * y.w;
         } else {
-            for (int e = k; e < a.K; ++e) {
-                if (pack) to[e] = from[e];
-                s = fmaf(__bfloat162float(from[e]), a.w_mean[e], s);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                if (k + e >= a.K) break;
+                if (pack) to[k + e] = from[k + e];
+                const float h = __bfloat162float(from[k + e]);
+                s = fmaf(h, a.w_mean[k + e], s);
+                one[e] = h * a.w_one[k + e];
             }
         }
 #pragma unroll
+        for (int e = 0; e < 8; ++e) size += fabsf(one[e]);
+#pragma unroll
         for (int off = 1; off < 32; off <<= 1) {
-            const float o = __shfl_up_sync(0xffffffffu, s, off);
-            if (lane >= off) s += o;
+            const float o = __shfl_up_sync(0xffffffffu, s, off), p = __shfl_up_sync(0xffffffffu, size, off);
+            if (lane >= off) {
+                s += o;
+                size += p;
+            }
         }
-        if (lane == 31) red[warp] = s;
+        if (lane == 31) {
+            red[0][warp] = s;
+            red[1][warp] = size;
+        }
         __syncthreads();
         float ahead = before;
+        size += all;
 #pragma unroll
-        for (int w = 0; w < kRowThreads / 32; ++w) {
-            if (w < warp) ahead += red[w];
-            before += red[w];
+        for (int w = 0; w < kWarps; ++w) {
+            if (w < warp) {
+                ahead += red[0][w];
+                size += red[1][w];
+            }
+            before += red[0][w];
+            all += red[1][w];
         }
-        if (k < a.K && (lane & 1 || k + 8 >= a.K)) cut += __int_as_float(__float_as_int(ahead + s) & 0xff800000);
+        // a number is a multiple of the last place of a power of two where 1.5 times that, added and taken off, leaves it alone
+        const float power = 1.5f * __int_as_float(__float_as_int(size) & 0x7f800000);
+        bool cuts = false;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) cuts |= __fsub_rn(__fadd_rn(one[e], power), power) != one[e];
+        const unsigned group = __ballot_sync(0xffffffffu, cuts) >> (lane & 30) & 3u;
+        if (group && k < a.K && (lane & 1 || k + 8 >= a.K)) {
+            cut += __int_as_float(__float_as_int(ahead + s) & 0xff800000);
+            ++groups;
+        }
         __syncthreads();
     }
     cut = warp_sum_f(cut);
-    if (lane == 0) red[warp] = cut;
+    groups = __reduce_add_sync(0xffffffffu, groups);
+    if (lane == 0) {
+        red[0][warp] = cut;
+        red_n[warp] = groups;
+    }
     __syncthreads();
     if (threadIdx.x == 0) {
         float s = before;
         cut = 0.f;
+        groups = 0;
 #pragma unroll
-        for (int w = 0; w < kRowThreads / 32; ++w) cut += red[w];
-        // (less what the factor c makes up for already; 3/8 of a last place is 3 * 2^-26 of the power of two)
-        cut = (cut * 4.4703484e-8f - a.cut_in_c * s) * a.inv_tau;
-        a.cut[i] = fabsf(cut) < 1.f ? cut : 0.f;
+        for (int w = 0; w < kWarps; ++w) {
+            cut += red[0][w];
+            groups += red_n[w];
+        }
+        // by a factor, what logits lose that grow evenly; to lse, what the common part has lost beyond that
+        const double even = kCutEven * 16.0 * (double)min(groups, kCutMost / 16);
+        const float c = (float)(a.c * (1.0 + even));
+        cut = (cut * kCutStep - (float)even * s) * a.inv_tau;
         // the middle of the window; whole numbers, so that y - reference loses nothing that y does not
-        s = rintf(s * a.c) + 32.f;
-        a.info[i] = make_int2(a.labels[row], __float_as_int(fabsf(s) < 1e9f ? s : 0.f));
+        s = rintf(s * c) + 32.f;
+        a.info[i] = make_int4(a.labels[row], __float_as_int(fabsf(s) < 1e9f ? s : 0.f), __float_as_int(c),
+                              __float_as_int(fabsf(cut) < 1.f ? cut : 0.f));
     }
 }
 
@@ -966,12 +1021,13 @@ row_kernel(const RowArgs a)
     // What this kernel needs and product 1 does not write is loaded while that still runs: a chain of three loads from memory.
     const int n_real = __ldcg(a.n_real), rows = max(0, min(a.rows_max, n_real - a.row0)), r = (int)blockIdx.x - 1;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    int row = 0, label = -1;
+    int row = 0;
+    int4 info = make_int4(-1, 0, 0, 0);
     uint4 ahead[2] = {};                                        // of the row of H: this thread's first two pieces of eight
     const __nv_bfloat16 *h = a.H;
     if (r >= 0 && r < rows) {
         row = __ldcg(a.order + a.row0 + r);
-        label = __ldcg(&a.info[a.row0 + r].x);
+        info = __ldcg(a.info + a.row0 + r);
         h += (int64_t)row * a.ldh;
         if (a.scaled) {
 #pragma unroll
@@ -994,6 +1050,8 @@ row_kernel(const RowArgs a)
             for (int k = threadIdx.x; k < a.K; k += kRowThreads) scaled[k] = __float2bfloat16_rn(0.f);
         return;
     }
+    const int label = info.x;
+    const float row_c = __int_as_float(info.z);
     const bool bad = label < 0 || label >= a.V;
     const float4 *part = a.part + (size_t)r * a.chunks;
     float4 mine[2];                                             // this thread's first two chunks
@@ -1047,8 +1105,8 @@ row_kernel(const RowArgs a)
     }
     const float l2s = log2f(s), nan = __int_as_float(0x7fffffff);
     if (threadIdx.x == 0) {
-        a.nll[row] = ((m - acc * a.c) + l2s) * kLn2;
-        if (a.lse) a.lse[row] = fmaf(m + l2s, kLn2, __ldcg(a.cut + a.row0 + r));
+        a.nll[row] = ((m - acc * row_c) + l2s) * kLn2;
+        if (a.lse) a.lse[row] = fmaf(m + l2s, kLn2, __int_as_float(info.w));
         if (bad && a.status) atomicOr(a.status, PPO_DEV_BAD_TOKEN);
     }
     if (!a.u) return;
@@ -1056,7 +1114,7 @@ row_kernel(const RowArgs a)
     float f = nan, c = nan;
     if (!bad) {
         const float ref = part[label / kChunk].x;
-        const float step = ex2(0.5f * (ref - m)), u = __bfloat162float(__float2bfloat16_rn(ex2(fmaf(acc, a.c, -ref)))) * step * step;
+        const float step = ex2(0.5f * (ref - m)), u = __bfloat162float(__float2bfloat16_rn(ex2(fmaf(acc, row_c, -ref)))) * step * step;
         const float want = u - sr;
         const __nv_bfloat16 stored = __float2bfloat16_rn(want);
         const float got = __bfloat162float(stored);
@@ -1119,7 +1177,7 @@ constexpr int kPieceRows = 256;                                 // a piece is a 
 struct Layout {
     int pieces, rows_max, chunks, Kp;
     int64_t Vp;
-    size_t n_real, slices, order, info, cut, w_mean, picked, row_scale, part, packed, scaled, u, parts, sums, bytes;
+    size_t n_real, slices, order, info, w_mean, w_one, picked, row_scale, part, packed, scaled, u, parts, sums, bytes;
 };
 
 // Pieces of at most 8192 rows by default: at V = 50304 that is 824 MB of U, and the sums of dW, read and written once a
@@ -1147,9 +1205,9 @@ static Layout layout_of(int64_t M, int64_t K, int64_t V, int64_t piece_rows, boo
     l.n_real = take(4);
     l.slices = take(8);
     l.order = take((size_t)M * 4);
-    l.info = take((size_t)M * sizeof(int2));
-    l.cut = take((size_t)M * 4);
+    l.info = take((size_t)M * sizeof(int4));
     l.w_mean = take((size_t)(K + 511) / 512 * 512 * 4);
+    l.w_one = take((size_t)K * 4);
     l.picked = take(rows * 4);
     l.row_scale = take(rows * sizeof(float2));
     l.part = take(rows * (size_t)l.chunks * sizeof(float4));
@@ -1359,19 +1417,14 @@ extern "C" int ppo_lmhead_xent(const void *H, int64_t ldh, const void *W, int64_
     r.H = reinterpret_cast<const __nv_bfloat16 *>(H);
     r.ldh = ldh; r.lddh = lddh; r.M = (int)M; r.K = (int)K; r.V = (int)V; r.Kp = l.Kp;
     r.labels = labels; r.mask = mask; r.ignore_id = ignore_id;
-    // The tensor cores cut off the sums that they keep: logits that grow evenly over the hidden elements come out smaller by 8.3e-10
-    // of themselves per element (measured, K = 64 to 4096), which is made up for here (lse at K = 4096: 2.6e-6 off without, 4e-7 with).
-    // A part that all of a row's logits have in common may come in a few elements, and loses more: pack_kernel follows it, and lse
-    // gets that back (logits near -90 out of one element, K = 4096: 4.4e-4 off without, 2e-5 with); nll and the gradients do not depend on it.
-    r.cut_in_c = (float)(8.3e-10 * (double)K);
-    r.c = (float)(1.4426950408889634 / (double)temperature * (1.0 + 8.3e-10 * (double)K));
+    r.c = 1.4426950408889634 / (double)temperature;
     r.inv_tau = 1.f / temperature; r.scale = scale; r.denom = denom;
     r.n_real = reinterpret_cast<int *>(mem + l.n_real);
     r.order = reinterpret_cast<int32_t *>(mem + l.order);
     r.W = reinterpret_cast<const __nv_bfloat16 *>(W); r.ldw = ldw; r.vk = vk;
     r.w_mean = reinterpret_cast<float *>(mem + l.w_mean);
-    r.info = reinterpret_cast<int2 *>(mem + l.info);
-    r.cut = reinterpret_cast<float *>(mem + l.cut);
+    r.w_one = reinterpret_cast<float *>(mem + l.w_one);
+    r.info = reinterpret_cast<int4 *>(mem + l.info);
     r.in_place = ldh % 64 == 0 && reinterpret_cast<uintptr_t>(H) % 128 == 0;
     r.packed = reinterpret_cast<__nv_bfloat16 *>(mem + l.packed);
     r.scaled = dW ? reinterpret_cast<__nv_bfloat16 *>(mem + l.scaled) : nullptr;
@@ -1400,7 +1453,7 @@ extern "C" int ppo_lmhead_xent(const void *H, int64_t ldh, const void *W, int64_
 
     Args a = {};
     a.n_real = r.n_real; a.M = (int)M; a.rows_max = l.rows_max; a.status = status;
-    a.c = r.c; a.order = r.order; a.info = r.info; a.in_place = r.in_place;
+    a.order = r.order; a.info = r.info; a.in_place = r.in_place;
     a.picked = r.picked; a.part = r.part; a.chunks = l.chunks; a.store = grad;
     a.row_scale = r.row_scale;
     Args a1 = a, a2 = a, a3 = a;
