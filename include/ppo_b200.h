@@ -581,7 +581,7 @@ int ppo_embed_bwd(const void *dY, int dtype, int64_t N, int64_t K, int64_t ldy, 
  *     norm[0] = |scale| * sqrt(sum over all tensors and elements of x^2),   norm[1] = coef = min(1, max_norm / norm[0]),
  *     out = x * (scale * coef), rounded once
  *   in, out           host arrays of n device pointers; out NULL: in place. out[i] may be in[i] (same type); apart from
- *                     that no two tensors overlap
+ *                     that no tensor that is written shares memory with another (PPO_ERR_PARAM)
  *   numel, in_dtype   host arrays [n]: elements (>= 0, contiguous, any element-aligned address) and PPO_F32 or PPO_BF16
  *   out_dtype         host array [n], NULL with out
  *   scale             finite, not 0: e.g. 1 / (loss scale), applied before the norm;  max_norm > 0, may be infinite

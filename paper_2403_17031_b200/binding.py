@@ -940,7 +940,8 @@ def _tensor_arrays(tensors, at: int, name: str):
 def grad_clip(grads, max_norm: float, scale: float = 1.0, out=None, workspace: Optional[torch.Tensor] = None,
               scratch: Optional[torch.Tensor] = None, norm: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Scales a list of gradients (contiguous, fp32 or bf16) by scale * min(1, max_norm / norm) with the norm over all of
-    scale * gradients; in place, or into the list `out` (each fp32 or bf16). No two tensors that are written may share memory.
+    scale * gradients; in place, or into the list `out` (each fp32 or bf16). out[i] may be grads[i]; apart from that no tensor that is
+    written may share memory with another, read or written.
     Returns norm [2] f32: the norm before clipping and the factor min(1, max_norm / norm)."""
     n = len(grads)
     if not n:
@@ -959,6 +960,10 @@ def grad_clip(grads, max_norm: float, scale: float = 1.0, out=None, workspace: O
     written = ins if outs is None else outs
     if len(set(written)) < n and len({p for p, k in zip(written, numel) if k}) < sum(1 for k in numel if k):
         raise ValueError("a tensor that is written may be listed only once")
+    if outs is not None and not set(ins).isdisjoint(outs):
+        own = {p: i for i, (p, k) in enumerate(zip(outs, numel)) if k}
+        if any(k and own.get(p, i) != i for i, (p, k) in enumerate(zip(ins, numel))):
+            raise ValueError("out[i] may be grads[i], but no other gradient")
     if norm is None:
         norm = first.new_empty(2, dtype=torch.float32)
     elif norm.numel() != 2:

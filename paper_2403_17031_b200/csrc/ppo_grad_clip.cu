@@ -14,6 +14,9 @@
 // clock and SM). Eight squares that overflow, or that are small enough to lose digits, are taken again in fp64.
 #include "ppo_packs.cuh"
 
+#include <algorithm>
+#include <cstdlib>
+
 namespace ppo {
 namespace clip {
 
@@ -215,6 +218,37 @@ static int launch_group(bool scale, const void *const *in, void *const *out, con
     return launch_status();
 }
 
+struct Range {
+    uintptr_t from, to;
+    bool written;
+};
+
+// Whether a tensor that is written shares memory with another one, read or written: blocks of pass 2 would read what others have
+// scaled. (Tensors that are only read may share theirs.) `ranges` holds 2 n.
+static bool clash(int32_t n, const void *const *in, void *const *out, const int64_t *numel, const int32_t *in_dtype,
+                  const int32_t *out_dtype, Range *ranges)
+{
+    int64_t count = 0;
+    for (int32_t i = 0; i < n; ++i) {
+        if (numel[i] == 0) continue;
+        const uintptr_t from = reinterpret_cast<uintptr_t>(in[i]);
+        const bool in_place = !out || out[i] == in[i];
+        ranges[count++] = {from, from + (uintptr_t)numel[i] * (in_dtype[i] == PPO_F32 ? 4 : 2), in_place};
+        if (in_place) continue;
+        const uintptr_t to = reinterpret_cast<uintptr_t>(out[i]);
+        ranges[count++] = {to, to + (uintptr_t)numel[i] * (out_dtype[i] == PPO_F32 ? 4 : 2), true};
+    }
+    std::sort(ranges, ranges + count, [](const Range &a, const Range &b) { return a.from < b.from; });
+    uintptr_t end = 0, end_written = 0;                        // of the ranges so far, and of those that are written
+    for (int64_t i = 0; i < count; ++i) {
+        const Range r = ranges[i];
+        if (r.from < (r.written ? end : end_written)) return true;
+        end = std::max(end, r.to);
+        if (r.written) end_written = std::max(end_written, r.to);
+    }
+    return false;
+}
+
 static int groups_of(int32_t n) { return n <= kSmall ? 1 : (n + kLarge - 1) / kLarge; }
 
 }   // namespace clip
@@ -248,6 +282,13 @@ extern "C" int ppo_grad_clip(int32_t n, const void *const *in, const int64_t *nu
             return PPO_ERR_ALIGN;
         if (out && out[i] == in[i] && od != in_dtype[i]) return PPO_ERR_PARAM;
         chunks += (numel[i] + kChunk - 1) / kChunk;
+    }
+    {
+        Range few[2 * kSmall], *many = n <= kSmall ? few : static_cast<Range *>(std::malloc((size_t)n * 2 * sizeof(Range)));
+        if (!many) return (int)cudaErrorMemoryAllocation;
+        const bool bad = clash(n, in, out, numel, in_dtype, out_dtype, many);
+        if (many != few) std::free(many);
+        if (bad) return PPO_ERR_PARAM;
     }
     int dev = 0, sms = 148;
     PPO_RETURN_IF_CUDA(cudaGetDevice(&dev));
