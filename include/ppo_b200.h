@@ -589,7 +589,8 @@ int ppo_embed_bwd(const void *dY, int dtype, int64_t N, int64_t K, int64_t ldy, 
  *   scratch           ppo_grad_clip_scratch_bytes(n) bytes, 256-byte aligned, uninitialised, for this call alone while it runs
  * In place, where scale * coef is 1 nothing is written.  A NaN or an infinity among the gradients makes norm (norm[0] may
  * be an infinity) and every result NaN and sets PPO_DEV_BAD_GRAD.  Squares are summed in fp64 (runs of eight in fp32) in a
- * fixed order, whatever the values' magnitude; a norm beyond fp32's range is returned as an infinity, coef stays right.
+ * fixed order, whatever the values' magnitude; a norm beyond fp32's range is returned as an infinity, coef as the nearest fp32 number
+ * (below 2^-126 those lose digits), and results stay right: factors that small are applied in fp64.
  * The pointers travel as kernel arguments: the host arrays may be reused when the call returns, and a captured call keeps
  * them.  Errors: PPO_ERR_SHAPE (n, numel), PPO_ERR_PARAM, PPO_ERR_NULL, PPO_ERR_DTYPE, PPO_ERR_ALIGN.
  */

@@ -126,6 +126,23 @@ __device__ __forceinline__ void scale_chunk(const TI *in, TO *out, float f, int6
     }
 }
 
+// A factor below fp32's normal numbers has lost digits as an fp32 number, or is 0, while the results may well be normal (values of 3e38
+// and a small max_norm): products in fp64.
+constexpr float kLeastFactor = 1.17549435e-38f;
+template <typename TI>
+__device__ __forceinline__ void scale_chunk_wide(const TI *in, void *out, bool out16, double f, int64_t e0, int64_t e1)
+{
+    for (int64_t j = e0 + threadIdx.x; j < e1; j += kThreads) {
+        Pack<TI, 1> p;
+        p.load(in + j);
+        float x[1];
+        p.get(x);
+        x[0] = (float)((double)x[0] * f);
+        if (out16) Pack<__nv_bfloat16, 1>::store(reinterpret_cast<__nv_bfloat16 *>(out) + j, x);
+        else Pack<float, 1>::store(reinterpret_cast<float *>(out) + j, x);
+    }
+}
+
 template <int N>
 __global__ void __launch_bounds__(kThreads)
 norm_kernel(const __grid_constant__ Table<N> t, const Args a)
@@ -145,7 +162,7 @@ norm_kernel(const __grid_constant__ Table<N> t, const Args a)
 }
 
 template <int N>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, kBlocksPerSm)
 scale_kernel(const __grid_constant__ Table<N> t, const Args a)
 {
     __shared__ double red[32];
@@ -164,7 +181,11 @@ scale_kernel(const __grid_constant__ Table<N> t, const Args a)
         a.norm[1] = (float)coef;
         if (bad && a.status) atomicOr(a.status, PPO_DEV_BAD_GRAD);
     }
-    const float f = (float)(coef * (double)a.scale);
+    // (one more number in the threads' registers would cost a quarter of the blocks on an SM: 1667 us for 1632)
+    __shared__ double factor;
+    if (threadIdx.x == 0) factor = coef * (double)a.scale;
+    __syncthreads();
+    const float f = (float)factor;
     for (int c0 = blockIdx.x; c0 < a.chunks; c0 += gridDim.x) {
         const int c = a.chunks - 1 - c0;
         const int i = tensor_of(t, a.n, c);
@@ -175,6 +196,11 @@ scale_kernel(const __grid_constant__ Table<N> t, const Args a)
         const __nv_bfloat16 *in16 = reinterpret_cast<const __nv_bfloat16 *>(t.in[i]);
         float *out32 = reinterpret_cast<float *>(t.out[i]);
         __nv_bfloat16 *out16 = reinterpret_cast<__nv_bfloat16 *>(t.out[i]);
+        if (fabsf(f) < kLeastFactor) {
+            if (type & 1) scale_chunk_wide(in16, t.out[i], type & 2, factor, e0, e1);
+            else scale_chunk_wide(in32, t.out[i], type & 2, factor, e0, e1);
+            continue;
+        }
         switch (type & 3) {
         case 0: scale_chunk(in32, out32, f, e0, e1, type & 4); break;
         case 1: scale_chunk(in16, out32, f, e0, e1, type & 4); break;
