@@ -774,7 +774,7 @@ extern "C" int ppo_embed(const void *table, int dtype, int64_t V, int64_t K, int
     if (N == 0) return PPO_OK;
     if (!table || !tokens || !out) return PPO_ERR_NULL;
     if (reinterpret_cast<uintptr_t>(table) % size_of(dtype) || reinterpret_cast<uintptr_t>(out) % size_of(out_dtype) ||
-        reinterpret_cast<uintptr_t>(tokens) % 4)
+        reinterpret_cast<uintptr_t>(tokens) % 4 || reinterpret_cast<uintptr_t>(workspace) % 256)
         return PPO_ERR_ALIGN;
     FwdArgs a = {};
     a.table = table; a.tokens = tokens; a.out = out;
@@ -805,7 +805,7 @@ extern "C" int ppo_embed_bwd(const void *dY, int dtype, int64_t N, int64_t K, in
     if (!dE) return PPO_ERR_NULL;
     if (N > 0 && (!dY || !tokens || !scratch)) return PPO_ERR_NULL;
     if (reinterpret_cast<uintptr_t>(dY) % size_of(dtype) || reinterpret_cast<uintptr_t>(dE) % size_of(out_dtype) ||
-        reinterpret_cast<uintptr_t>(tokens) % 4 || reinterpret_cast<uintptr_t>(scratch) % 256)
+        reinterpret_cast<uintptr_t>(tokens) % 4 || reinterpret_cast<uintptr_t>(scratch) % 256 || reinterpret_cast<uintptr_t>(workspace) % 256)
         return PPO_ERR_ALIGN;
     cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
     if (N == 0) {

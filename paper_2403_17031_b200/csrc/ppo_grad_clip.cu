@@ -295,7 +295,8 @@ extern "C" int ppo_grad_clip(int32_t n, const void *const *in, const int64_t *nu
     if (n <= 0 || n > 1000000) return PPO_ERR_SHAPE;
     if (!finite_f(scale) || scale == 0.f || !(max_norm > 0.f)) return PPO_ERR_PARAM;
     if (!in || !numel || !in_dtype || !norm || !scratch || (out && !out_dtype)) return PPO_ERR_NULL;
-    if (reinterpret_cast<uintptr_t>(norm) % 4 || reinterpret_cast<uintptr_t>(scratch) % 256) return PPO_ERR_ALIGN;
+    if (reinterpret_cast<uintptr_t>(norm) % 4 || reinterpret_cast<uintptr_t>(scratch) % 256 || reinterpret_cast<uintptr_t>(workspace) % 256)
+        return PPO_ERR_ALIGN;
     int64_t chunks = 0;
     for (int i = 0; i < n; ++i) {
         const int32_t od = out ? out_dtype[i] : in_dtype[i];

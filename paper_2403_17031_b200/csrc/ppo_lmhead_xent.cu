@@ -1397,7 +1397,9 @@ extern "C" int ppo_lmhead_xent(const void *H, int64_t ldh, const void *W, int64_
     if (M > 0 && (!H || !labels || !nll || !scratch)) return PPO_ERR_NULL;
     if (ldh % 8 || ldw % 8) return PPO_ERR_UNSUPPORTED;
     if (reinterpret_cast<uintptr_t>(H) % 16 || reinterpret_cast<uintptr_t>(W) % 16 || reinterpret_cast<uintptr_t>(scratch) % 256 ||
-        reinterpret_cast<uintptr_t>(dH) % 2 || reinterpret_cast<uintptr_t>(dW) % 2 || reinterpret_cast<uintptr_t>(labels) % 4)
+        reinterpret_cast<uintptr_t>(dH) % 2 || reinterpret_cast<uintptr_t>(dW) % 2 || reinterpret_cast<uintptr_t>(labels) % 4 ||
+        reinterpret_cast<uintptr_t>(loss) % 4 || reinterpret_cast<uintptr_t>(nll) % 4 || reinterpret_cast<uintptr_t>(lse) % 4 ||
+        reinterpret_cast<uintptr_t>(denom) % 4 || reinterpret_cast<uintptr_t>(workspace) % 256)
         return PPO_ERR_ALIGN;
     cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
     int *status = workspace ? &ws_header(workspace)->status : nullptr;

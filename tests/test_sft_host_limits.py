@@ -58,3 +58,20 @@ def test_no_tensor_that_is_clipped_shares_memory_with_another(b):
                  ([A, B], [8, 8], [F, F], [A, Y], [F, F]), ([A, A], [8, 0], [F, F]), ([A, B], [8, 8], [H, H], [X, X + 32], [F, F]),
                  ([A + 64 * i for i in range(300)][::-1], [16] * 300, [F] * 300)]:
         assert call(*args) > 0, args
+
+
+def test_addresses_that_numbers_cannot_have(b):
+    """Every pointer whose misalignment would fault is refused: results, the divisor, and a workspace that ppo_workspace_init cannot have made."""
+    # H ldh W ldw layout M K V | labels mask ignore temperature scale denom piece | loss nll lse dH lddh dW lddw | ws scratch stream
+    ok = [P(FAKE), 256, P(FAKE), 1000, 0, 4, 256, 1000, P(FAKE), None, -100, 1.0, 1.0, None, 0, P(FAKE), P(FAKE), None, P(FAKE), 256,
+          P(FAKE), 1000, None, P(FAKE), None]
+    embed = [P(FAKE), b.PPO_BF16, 1000, 64, 64, P(FAKE), 4, 1.0, P(FAKE), b.PPO_F32, 64, None, None]
+    bwd = [P(FAKE), b.PPO_BF16, 4, 64, 64, P(FAKE), 1000, 1.0, -1, P(2 * FAKE), b.PPO_F32, 64, 0, None, P(FAKE), None]
+    one = lambda t, x: (t * 1)(x)                                                   # noqa: E731
+    clip = [1, one(C.c_void_p, FAKE), one(C.c_int64, 8), one(C.c_int32, 0), None, None, 1.0, 1.0, P(FAKE), None, P(FAKE), None]
+    for name, args, at in (("ppo_lmhead_xent", ok, ((13, 2), (15, 2), (16, 1), (17, 3), (22, 64))), ("ppo_embed", embed, ((11, 128),)),
+                           ("ppo_embed_bwd", bwd, ((13, 8),)), ("ppo_grad_clip", clip, ((8, 2), (9, 4)))):
+        for i, off in at:
+            bad = list(args)
+            bad[i] = P(FAKE + off)
+            assert getattr(b.lib(), name)(*bad) == -4, (name, i)
