@@ -236,7 +236,11 @@ class SFTStep:
     are this object's buffers, overwritten by the next step.
 
     W [K, V] is the LM head's weight, stored by rows or by columns (the transpose of a linear layer's weight): its gradient is
-    stored the same way. N: positions of a batch. grad_dtype: of the table's gradient."""
+    stored the same way. N: positions of a batch. grad_dtype: of the table's gradient.
+
+    A batch in several parts (micro-batches): loss(denom=) divides each part's sum by the number of all parts' real positions,
+    grad_embed(accumulate=True) adds to the table's gradient from the second part on. dW is a part's own: the caller adds the parts' up,
+    in fp32 say, and gives the sum to clip(dW=). clip() refuses a dW of the last part beside a table's gradient of several."""
 
     def __init__(self, W: torch.Tensor, N: int, padding_id: int = -1, ignore_id: int = -100, temperature: float = 1.0,
                  embed_scale: float = 1.0, grad_dtype: torch.dtype = torch.bfloat16, piece_rows: int = 0):
@@ -250,6 +254,8 @@ class SFTStep:
         # (one buffer: the two calls that need it do not overlap)
         self._scratch = scratch(max(_b.lmhead_xent_scratch_bytes(N, K, V, piece_rows), _b.embed_bwd_scratch_bytes(N, K, V)))
         self._clip_scratch = {}
+        # loss() calls so far; how many there were when dE was begun (None: not since the last clip()), and whether others were added to it
+        self._losses, self._begun, self._mixed = 0, None, False
         self.out = {"hidden": torch.empty((N, K), dtype=bf16, device=dev), "loss": torch.empty((), dtype=f32, device=dev),
                     "nll": torch.empty(N, dtype=f32, device=dev), "lse": torch.empty(N, dtype=f32, device=dev),
                     "dH": torch.empty((N, K), dtype=bf16, device=dev), "dW": torch.empty_like(W),
@@ -259,24 +265,35 @@ class SFTStep:
         """Rows of the table [V, K] for tokens [N] int32, times embed_scale, in bf16."""
         return _b.embed(table, tokens, scale=self.embed_scale, workspace=self.workspace, out=self.out["hidden"])
 
-    def loss(self, H, W, labels, mask=None, scale: float = 1.0):
+    def loss(self, H, W, labels, mask=None, scale: float = 1.0, denom: Optional[torch.Tensor] = None):
         """Mean cross entropy of labels [N] under the head's logits for the hidden states H [N, K], without masked rows and
-        ignored labels; dH and dW are the gradients of scale * loss. Returns the dict of buffers."""
+        ignored labels; dH and dW are the gradients of scale * loss. denom: [1] f32, divides the sum instead of the number of
+        real rows. Returns the dict of buffers."""
         o = self.out
-        _b.lmhead_xent(H, W, labels, mask=mask, ignore_id=self.ignore_id, temperature=self.temperature, scale=scale,
+        _b.lmhead_xent(H, W, labels, mask=mask, ignore_id=self.ignore_id, temperature=self.temperature, scale=scale, denom=denom,
                        piece_rows=self.piece_rows, workspace=self.workspace, scratch=self._scratch,
                        out={n: o[n] for n in ("loss", "nll", "lse", "dH", "dW")})
+        self._losses += 1
         return o
 
     def grad_embed(self, dX, tokens, accumulate: bool = False):
         """Gradient dX [N, K] on embed()'s result -> gradient of the table (accumulate: added to the one there is)."""
+        if not accumulate or self._begun is None:
+            self._begun, self._mixed = self._losses, False
+        self._mixed |= self._losses != self._begun
         return _b.embed_bwd(dX, tokens, self.V, scale=self.embed_scale, padding_id=self.padding_id, accumulate=accumulate,
                             workspace=self.workspace, scratch=self._scratch, out=self.out["dE"])
 
-    def clip(self, max_norm: float, others=(), scale: float = 1.0):
-        """Clips dW, dE and the model's other gradients together, in place. Returns [norm before clipping, factor]."""
+    def clip(self, max_norm: float, others=(), scale: float = 1.0, dW: Optional[torch.Tensor] = None):
+        """Clips dW (the last loss()'s, or the caller's sum over several), dE and the model's other gradients together, in place.
+        Returns [norm before clipping, factor]."""
         o = self.out
-        dW = o["dW"] if o["dW"].is_contiguous() else o["dW"].t()                    # (the same elements, in memory's order)
+        if dW is None:
+            if self._mixed:
+                raise ValueError("the table's gradient is of several loss() calls and dW of the last one: give clip() the sum of theirs")
+            dW = o["dW"]
+        self._begun, self._mixed = None, False
+        dW = dW if dW.is_contiguous() else dW.t()                                   # (the same elements, in memory's order)
         grads = [dW, o["dE"], *others]
         need = _b.grad_clip_scratch_bytes(len(grads))
         # (one for each size, all kept: a captured graph may hold the address of any)
