@@ -529,7 +529,8 @@ int ppo_fp8_matmul(const void *A, int64_t lda, const float *a_scales, const void
  *   scratch  ppo_lmhead_xent_scratch_bytes(M, K, V, piece_rows, dH given, dW given) bytes, 256-byte aligned,
  *       uninitialised, for this call alone while it runs (NULL where M == 0)
  * Sums are fp32 on the tensor cores in an order that the sizes fix, so results are bit-reproducible; 2^(z - reference) and
- * gradient factor times H are rounded to bf16 on the way to the gradients, which are rounded once more.
+ * gradient factor times H are rounded to bf16 on the way to the gradients, which are rounded once more (up to 64 rows the second is kept
+ * as a sum of two bf16 numbers).
  * A probability under 2^-61 may count as 0 in the gradients.
  * Logits are sums of K products on the tensor cores, which cut their sums off every 16 elements; what that takes on average (1.0e-9 K
  * of a logit, measured for K up to 131072 and taken as that of 131072 beyond; and for lse what a row's logits have in common) is given back

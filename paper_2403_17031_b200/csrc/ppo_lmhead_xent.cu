@@ -18,7 +18,7 @@
 // 2^-62 of the row's largest, becomes 0). (With references at multiples of 64,
 // whatever the row's logits, many rows had two: 1999 x 50277 x 1032 with logits near -90 took 704 us, 638 so.)
 //
-// Roundings to 16 bits: U, a H, and the results. Statistics, sums and nll are fp32, the loss fp64. What the rounding of U
+// Roundings to 16 bits: U, a H (with more than 64 rows), and the results. Statistics, sums and nll are fp32, the loss fp64. What the rounding of U
 // would do to the gradients is kept small in two ways. S in the gradient is the sum of the rounded U, so that D is the
 // gradient of a softmax whose probabilities are off by half a step each and still add up to 1. U' at the label, about -S, is the
 // largest element of its row by far: its own rounding is undone by a factor on a that makes a U' exact there, at the cost of
@@ -61,16 +61,23 @@ constexpr float kLeast = 5.421010862427522e-20f, kMost = 1.8446744073709552e19f;
 // staging buffer a warp (53 x 50304 x 4096 in all: 3 stages 302 us, 4 279, 5 266).
 // kSmall: the same for products 1 and 2 of up to 64 rows: a stage holds 64 rows of A, so that there are eight. The matrix
 // instruction reads 128: the other 64 rows are what lies behind them (B), and their results are nobody's.
-enum Mode { kSingle, kPair, kWide, kSmall };
+// kTwice: pairs, for product 3 of up to 64 rows, with a H as the sum of two bf16 numbers: a stage holds both, and both are multiplied with
+// the same U. With one block of contraction the products are hidden by the stores of dW (for 65 to 128 rows the whole call would take 3 to 5 %
+// longer, beyond that a third), and what rounding a H once does to dW, as much as rounding dW itself, is gone: 53 x 50304 x 4096 dW 0.0024
+// of its norm off with one, 0.0017 so, in the same 259 us; 53 x 50304 x 1064 109 and 113 us. (Blocks alone, which read half as much again
+// out of L2: 265 and 112.)
+enum Mode { kSingle, kPair, kWide, kSmall, kTwice };
 
 template <int MODE>
 struct Shape {
-    static constexpr bool kIsPair = MODE == kPair || MODE == kWide;
+    static constexpr bool kIsPair = MODE == kPair || MODE == kWide || MODE == kTwice;
     static constexpr int kHalves = MODE == kWide ? 2 : 1;              // accumulators of a tile
     static constexpr int kM = kIsPair ? 2 * kBM : kBM, kAccN = kIsPair ? 256 : 128, kN = kHalves * kAccN;
     static constexpr int kRowsB = 128;                                 // a block's share of B, per accumulator
-    static constexpr int kBytesA = (MODE == kSmall ? 64 : kBM) * kBlockK * 2, kBytesB = kRowsB * kBlockK * 2, kStage = kBytesA + kHalves * kBytesB;
-    static constexpr int kStages = MODE == kWide ? 4 : MODE == kPair ? 5 : MODE == kSingle ? 6 : 8;
+    static constexpr int kBytesA = (MODE == kSmall ? 64 : kBM) * kBlockK * 2, kBytesB = kRowsB * kBlockK * 2;
+    static constexpr int kSecond = kBytesA + kHalves * kBytesB;        // where the second part of a H lies
+    static constexpr int kStage = kSecond + (MODE == kTwice ? kBytesA : 0);
+    static constexpr int kStages = MODE == kWide || MODE == kTwice ? 4 : MODE == kPair ? 5 : MODE == kSingle ? 6 : 8;
     static constexpr int kBuffers = MODE == kPair ? 2 : 1;             // staging, per epilogue warp
     static constexpr int kSmem = kStages * kStage + kBuffers * kEpiWarps * kStageOut + 1024;
     static constexpr int kTileFloats = kM * kN;
@@ -97,6 +104,8 @@ struct Args {
     __nv_bfloat16 *out;
     int64_t ldo;
     int bulk_cols;                                         // bulk stores take boxes that end at or before this column
+    // kTwice
+    int vk, second;                                        // a H is B (else A); first row of its second part
     // kHidden
     const float2 *row_scale;                               // [rows] a, c
     const float *w_mean;                                   // [K, in whole tiles]
@@ -242,6 +251,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
 {
     using S = Shape<MODE>;
     static_assert(MODE != kSmall || !A_MN, "rows of A are what there are few of");
+    static_assert(MODE != kTwice || (A_MN && B_MN && S::kBytesA == S::kBytesB), "either operand may be the one in two parts");
     constexpr bool PAIR = S::kIsPair;
     constexpr int kStages = S::kStages, kHalves = S::kHalves;
     extern __shared__ __align__(1024) unsigned char smem_raw[];
@@ -317,6 +327,12 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                             load(to, &map_b, kb * kBlockK, n0 + i * S::kAccN);
                         }
                     }
+                    if (MODE == kTwice) {
+                        const CUtensorMap *map = a.vk ? &map_b : ma;
+                        const int x = a.vk ? n0 : m0, y = a.second + kb * kBlockK;
+                        load(stage + S::kSecond, map, x, y);
+                        load(stage + S::kSecond + kBox, map, x + 64, y);
+                    }
                     if (++s == kStages) { s = 0; parity ^= 1; }
                 }
             }
@@ -344,6 +360,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             bool alive = true;
             uint32_t s = 0, s_parity = 0, tiles = 0;
             // one block of the contraction into accumulator `acc`, from stage `from`
+            const uint32_t a_second = a.vk ? 0 : S::kSecond >> 4, b_second = a.vk ? (S::kSecond - S::kBytesA) >> 4 : 0;
             const auto multiply = [&](uint32_t acc, uint32_t from, int half, uint32_t accumulate) {
                 const uint64_t ad = a_desc + from * (S::kStage >> 4), bd = b_desc + (from * S::kStage + half * S::kBytesB >> 4);
 #pragma unroll
@@ -352,6 +369,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                     const uint64_t ak = ad + kk * (A_MN ? 2048 >> 4 : 32 >> 4), bk = bd + kk * (B_MN ? 2048 >> 4 : 32 >> 4);
                     if (PAIR) mma_pair(tmem_base + acc * S::kAccN, ak, bk, idesc, kk ? 1u : accumulate);
                     else mma(tmem_base + acc * S::kAccN, ak, bk, idesc, kk ? 1u : accumulate);
+                    if (MODE == kTwice) mma_pair(tmem_base + acc * S::kAccN, ak + a_second, bk + b_second, idesc, 1u);
                 }
             };
             const auto step = [&] { if (++s == kStages) { s = 0; s_parity ^= 1; } };
@@ -736,6 +754,7 @@ struct RowArgs {
     int in_place;                                               // product 1 reads H where it lies when all rows are real
     __nv_bfloat16 *packed;                                      // [M, Kp] real rows (unless they can be read in place)
     __nv_bfloat16 *scaled;                                      // [rows_max, Kp] a H; null: no gradients
+    int64_t second;                                             // 0, or elements from there to what its rounding leaves, rounded
     __nv_bfloat16 *u;                                           // [rows_max, Vp]
     int64_t Vp;
     float *picked;
@@ -1013,6 +1032,13 @@ __device__ __forceinline__ void choose_slices(const RowArgs &a, int rows)
     }
 }
 
+// what rounding x leaves; nothing where that is no number
+__device__ __forceinline__ float left_over(float x, float rounded)
+{
+    const float d = x - rounded;
+    return fabsf(d) < __int_as_float(0x7f800000) ? d : 0.f;
+}
+
 // A row's statistics out of its chunks', its loss and the factors of its gradient; U at the label; a H
 __global__ void __launch_bounds__(kRowThreads)
 row_kernel(const RowArgs a)
@@ -1047,7 +1073,10 @@ row_kernel(const RowArgs a)
     if (r >= rows) {
         // up to the next block of the contraction: zeros that product 3 reads (U has its own)
         if (scaled && r < (rows + kBlockK - 1) / kBlockK * kBlockK)
-            for (int k = threadIdx.x; k < a.K; k += kRowThreads) scaled[k] = __float2bfloat16_rn(0.f);
+            for (int k = threadIdx.x; k < a.K; k += kRowThreads) {
+                scaled[k] = __float2bfloat16_rn(0.f);
+                if (a.second) scaled[a.second + k] = __float2bfloat16_rn(0.f);
+            }
         return;
     }
     const int label = info.x;
@@ -1128,12 +1157,22 @@ row_kernel(const RowArgs a)
     for (int k = threadIdx.x * 8; k < a.K; k += kRowThreads * 8) {
         if (k + 8 <= a.K) {
             const uint4 v = k < kRowThreads * 8 ? ahead[0] : k < 2 * kRowThreads * 8 ? ahead[1] : *reinterpret_cast<const uint4 *>(h + k);
-            uint32_t w[4] = {v.x, v.y, v.z, v.w};
+            uint32_t w[4] = {v.x, v.y, v.z, v.w}, rest[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) w[e] = pack2(low(w[e]) * f, high(w[e]) * f);
+            for (int e = 0; e < 4; ++e) {
+                const float x = low(w[e]) * f, y = high(w[e]) * f;
+                w[e] = pack2(x, y);
+                rest[e] = pack2(left_over(x, low(w[e])), left_over(y, high(w[e])));
+            }
             *reinterpret_cast<uint4 *>(scaled + k) = make_uint4(w[0], w[1], w[2], w[3]);
+            if (a.second) *reinterpret_cast<uint4 *>(scaled + a.second + k) = make_uint4(rest[0], rest[1], rest[2], rest[3]);
         } else {
-            for (int e = k; e < a.K; ++e) scaled[e] = __float2bfloat16_rn(__bfloat162float(h[e]) * f);
+            for (int e = k; e < a.K; ++e) {
+                const float x = __bfloat162float(h[e]) * f;
+                const __nv_bfloat16 y = __float2bfloat16_rn(x);
+                scaled[e] = y;
+                if (a.second) scaled[a.second + e] = __float2bfloat16_rn(left_over(x, __bfloat162float(y)));
+            }
         }
     }
 }
@@ -1174,6 +1213,9 @@ tail_kernel(const RowArgs r, const Args a, int workers)
 // ---------------------------------------------------------------- host side
 constexpr int kPieceRows = 256;                                 // a piece is a multiple of this
 
+// few rows: the mode of products 1 and 2 (product 3 has its rows along the contraction), and a H in two parts
+static bool few(int M) { return M <= 64; }
+
 struct Layout {
     int pieces, rows_max, chunks, Kp;
     int64_t Vp;
@@ -1212,7 +1254,7 @@ static Layout layout_of(int64_t M, int64_t K, int64_t V, int64_t piece_rows, boo
     l.row_scale = take(rows * sizeof(float2));
     l.part = take(rows * (size_t)l.chunks * sizeof(float4));
     l.packed = take((size_t)M * l.Kp * 2);
-    l.scaled = take(dw ? rows * l.Kp * 2 : 0);
+    l.scaled = take(dw ? rows * l.Kp * 2 * (few((int)M) ? 2 : 1) : 0);
     l.u = take(grad ? rows * (size_t)l.Vp * 2 : 0);
     l.parts = take(!dh ? 0 : (size_t)2 * 4 * (M <= kBM ? kMaxSms * Shape<kSingle>::kTileFloats : kMaxSms / 2 * Shape<kWide>::kTileFloats));
     // (whole tiles, in either layout)
@@ -1302,9 +1344,6 @@ static bool wide(int64_t m, int64_t n, int64_t contraction, int sms)
     return (n + 255) / 256 % 2 == 0 && contraction >= 64 * kBlockK && (m + 255) / 256 * ((n + 511) / 512) >= sms;
 }
 
-// the mode of products 1 and 2 for few rows; product 3 has its rows along the contraction
-static bool few(int M) { return M <= 64; }
-
 template <int MODE>
 static void set_shape(RowArgs &r, const Args &a2, int sms)
 {
@@ -1356,7 +1395,7 @@ static int launch_piece(const Maps &m, RowArgs r, const Args &a1, Args a2, Args 
             a3.gn = 6;
             rc = launch_weight<kWide>(m, a3, vk, sms, s);
         } else {
-            rc = single ? launch_weight<kSingle>(m, a3, vk, sms, s) : launch_weight<kPair>(m, a3, vk, sms, s);
+            rc = small ? launch_weight<kTwice>(m, a3, vk, sms, s) : single ? launch_weight<kSingle>(m, a3, vk, sms, s) : launch_weight<kPair>(m, a3, vk, sms, s);
         }
         if (rc) return rc;
     }
@@ -1430,6 +1469,8 @@ extern "C" int ppo_lmhead_xent(const void *H, int64_t ldh, const void *W, int64_
     r.in_place = ldh % 64 == 0 && reinterpret_cast<uintptr_t>(H) % 128 == 0;
     r.packed = reinterpret_cast<__nv_bfloat16 *>(mem + l.packed);
     r.scaled = dW ? reinterpret_cast<__nv_bfloat16 *>(mem + l.scaled) : nullptr;
+    const bool twice = few((int)M);                              // (product 3's mode: see there)
+    r.second = twice ? (int64_t)l.rows_max * l.Kp : 0;
     r.u = grad ? reinterpret_cast<__nv_bfloat16 *>(mem + l.u) : nullptr;
     r.Vp = l.Vp;
     r.picked = reinterpret_cast<float *>(mem + l.picked);
@@ -1467,8 +1508,9 @@ extern "C" int ppo_lmhead_xent(const void *H, int64_t ldh, const void *W, int64_
     a3.dim_m = (int)w_outer; a3.dim_n = (int)w_inner; a3.dim_k = l.rows_max; a3.gm = 8; a3.gn = 9;
     a3.out = reinterpret_cast<__nv_bfloat16 *>(dW); a3.ldo = lddw;
     a3.scratch = reinterpret_cast<float *>(mem + l.sums);
+    a3.vk = vk; a3.second = l.rows_max;
     if (dW) {
-        if ((rc = make_map_pitch(&m.scaled, r.scaled, (uint64_t)K, (uint64_t)l.rows_max, (uint64_t)l.Kp, 64))) return rc;
+        if ((rc = make_map_pitch(&m.scaled, r.scaled, (uint64_t)K, (uint64_t)l.rows_max * (twice ? 2 : 1), (uint64_t)l.Kp, 64))) return rc;
         if (reinterpret_cast<uintptr_t>(dW) % 16 == 0 && lddw % 8 == 0 && lddw < ((int64_t)1 << 38)) {
             // (a box is clipped in units of 16 bytes: it would write zeros behind a row whose end is none)
             a3.bulk_cols = w_inner % 8 ? (int)w_inner : 0x7fffffff;
