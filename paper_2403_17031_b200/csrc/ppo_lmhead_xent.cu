@@ -1157,15 +1157,16 @@ row_kernel(const RowArgs a)
     for (int k = threadIdx.x * 8; k < a.K; k += kRowThreads * 8) {
         if (k + 8 <= a.K) {
             const uint4 v = k < kRowThreads * 8 ? ahead[0] : k < 2 * kRowThreads * 8 ? ahead[1] : *reinterpret_cast<const uint4 *>(h + k);
-            uint32_t w[4] = {v.x, v.y, v.z, v.w}, rest[4];
+            const uint32_t u[4] = {v.x, v.y, v.z, v.w};
+            uint32_t w[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float x = low(w[e]) * f, y = high(w[e]) * f;
-                w[e] = pack2(x, y);
-                rest[e] = pack2(left_over(x, low(w[e])), left_over(y, high(w[e])));
-            }
+            for (int e = 0; e < 4; ++e) w[e] = pack2(low(u[e]) * f, high(u[e]) * f);
             *reinterpret_cast<uint4 *>(scaled + k) = make_uint4(w[0], w[1], w[2], w[3]);
-            if (a.second) *reinterpret_cast<uint4 *>(scaled + a.second + k) = make_uint4(rest[0], rest[1], rest[2], rest[3]);
+            if (a.second) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) w[e] = pack2(left_over(low(u[e]) * f, low(w[e])), left_over(high(u[e]) * f, high(w[e])));
+                *reinterpret_cast<uint4 *>(scaled + a.second + k) = make_uint4(w[0], w[1], w[2], w[3]);
+            }
         } else {
             for (int e = k; e < a.K; ++e) {
                 const float x = __bfloat162float(h[e]) * f;
