@@ -14,7 +14,7 @@
 // block per token would leave them to a few blocks. A run of one token inside a chunk is summed in registers and
 // written once; a run that crosses chunks leaves a partial sum per chunk, and those are added in the order of the chunks.
 // Every sum is fp32 in ascending order of the positions, without atomics: results do not depend on timing. Rows of tokens
-// that do not occur are zero-filled by other blocks of the same launch.
+// that do not occur are zero-filled by other blocks of the same launches.
 #include "ppo_packs.cuh"
 
 namespace ppo {
@@ -133,7 +133,7 @@ __device__ __forceinline__ void write_row(const BwdArgs &a, int64_t v, int k, fl
 }
 
 // The zero rows are most of what few positions write, so they go along with the launches that sort, which leave nearly all of
-// the memory's time unused.
+// the memory's time unused; up to 8192 positions, which are ranked in one short launch, with the one that sums.
 template <typename TO>
 __device__ __forceinline__ void zero_row(const BwdArgs &a, int64_t v)
 {

@@ -33,7 +33,7 @@
 //
 // Bounds and times (calls one after the other): 27136 x 50304 x 4096 24.3 to 26.5 ms = 1260 to 1380 TFLOP/s, held by the board's
 // power (about 1.4 GHz); three bare library products of these shapes take 24 ms there. At full clock L2 bounds the pairs (13.4 TB/s into the SMs).
-// 1792 rows 1.52 ms (1460 TFLOP/s). 53 rows 258 us: W is streamed twice (products 1 and 2, 75 us each) and dW written once (75 us), 5.5 TB/s.
+// 1792 rows 1.52 ms (1460 TFLOP/s). 53 rows 259 us: W is streamed twice (products 1 and 2, 72 us each) and dW written once (78 us), 5.5 TB/s.
 #include "ppo_tcgen05.cuh"
 
 namespace ppo {
@@ -1338,8 +1338,9 @@ static int launch_weight(const Maps &m, const Args &a3, bool vk, int sms, cudaSt
 }
 
 // Wide tiles where they are half as many, the contraction is at least 64 blocks long (their epilogue, 6000 cycles for two
-// accumulators, has to be small against 1024 a block) and the pairs get two tiles or more each (6912 x 4096 x 50304: dH
-// 1973 us against 2049, dW 2017 against 2077; 1792 rows, whose 56 wide tiles are all cut: dH 598 against 544).
+// accumulators, has to be small against 1024 a block) and the pairs get two tiles or more each (6912 x 4096 x 50304, W [V, K]: dH
+// 1973 us against 2049, dW 2017 against 2077; 1792 rows, whose 56 wide tiles are all cut: dH 598 against 544). (dW of W [K, V] at V = 50304,
+// 197 tiles of 256, is not among them.)
 static bool wide(int64_t m, int64_t n, int64_t contraction, int sms)
 {
     return (n + 255) / 256 % 2 == 0 && contraction >= 64 * kBlockK && (m + 255) / 256 * ((n + 511) / 512) >= sms;
@@ -1501,6 +1502,7 @@ extern "C" int ppo_lmhead_xent(const void *H, int64_t ldh, const void *W, int64_
     a.picked = r.picked; a.part = r.part; a.chunks = l.chunks; a.store = grad;
     a.row_scale = r.row_scale;
     Args a1 = a, a2 = a, a3 = a;
+    // (blocks of gm x gn = 72 tiles, which as many pairs work on at a time, near square in elements: they share panels through L2)
     a1.dim_m = l.rows_max; a1.dim_n = (int)V; a1.dim_k = (int)K; a1.gm = 9; a1.gn = 8;
     a2.dim_m = l.rows_max; a2.dim_n = (int)K; a2.dim_k = (int)V; a2.gm = 9; a2.gn = 8;
     a2.out = r.dH; a2.ldo = lddh; a2.w_mean = r.w_mean;
