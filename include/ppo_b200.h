@@ -550,7 +550,8 @@ int ppo_lmhead_xent(const void *H, int64_t ldh, const void *W, int64_t ldw, int 
  * Rows of an embedding table, scaled: out[i, :] = scale * E[tokens[i], :]   (i < N)
  *   table E [V, K] dtype, row pitch lde >= K elements;  out [N, K] out_dtype, row pitch ldo >= K; elements behind a row's K
  *         are left alone.  Either may be fp32 or bf16, at any element-aligned address (widest accesses where K is a
- *         multiple of 8 and addresses and pitches are multiples of 16 bytes for bf16, 32 for fp32); each element is rounded once
+ *         multiple of 8 and addresses and pitches are multiples of 16 bytes for bf16, 32 for fp32); each element is rounded once.
+ *         out must not overlap the table
  *   tokens [N] i32;  a token outside [0, V) makes its row NaN and sets PPO_DEV_BAD_TOKEN
  *   workspace nullable (status word)
  * Errors: PPO_ERR_DTYPE, PPO_ERR_SHAPE, PPO_ERR_PARAM (scale not finite), PPO_ERR_NULL, PPO_ERR_ALIGN.  N == 0 is a

@@ -818,7 +818,7 @@ def lmhead_xent(H: torch.Tensor, W: torch.Tensor, labels: torch.Tensor, mask: Op
     logits in memory. W (and dW) may be stored by rows or by columns. Rows with mask 0 or label ignore_id are left out of the
     mean; denom (a [1] f32 tensor) divides the sum instead of their number; scale multiplies the gradients.
     Returns dict(loss (0-d f32), nll, lse [M] f32, dH [M, K] | None, dW [K, V] | None bf16); `out`: the same dict with the
-    tensors to write to (lse, dH and dW may be absent). scratch: at least lmhead_xent_scratch_bytes(...) bytes (uint8),
+    tensors to write to (lse, dH and dW may be absent; none may share memory with an input). scratch: at least lmhead_xent_scratch_bytes(...) bytes (uint8),
     allocated here where none is given."""
     at, f32, bf16 = H.get_device(), torch.float32, torch.bfloat16
     if H.dim() != 2 or H.dtype != bf16 or not H.is_cuda:
@@ -873,7 +873,7 @@ def lmhead_xent(H: torch.Tensor, W: torch.Tensor, labels: torch.Tensor, mask: Op
 def embed(table: torch.Tensor, tokens: torch.Tensor, scale: float = 1.0, out_dtype: Optional[torch.dtype] = None,
           workspace: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """scale * table[tokens]: table [V, K] fp32 or bf16, tokens [...] int32 -> [..., K] in out_dtype (default: the table's).
-    `out`: the tensor to write to, [..., K] contiguous or [N, K] with a row pitch."""
+    `out`: the tensor to write to, [..., K] contiguous or [N, K] with a row pitch, apart from the table."""
     at = table.get_device()
     tp, lde, dt = _matrix(table, at, "table")
     V, K = table.shape

@@ -292,14 +292,15 @@ class SFTStep:
             if self._mixed:
                 raise ValueError("the table's gradient is of several loss() calls and dW of the last one: give clip() the sum of theirs")
             dW = o["dW"]
-        self._begun, self._mixed = None, False
         dW = dW if dW.is_contiguous() else dW.t()                                   # (the same elements, in memory's order)
         grads = [dW, o["dE"], *others]
         need = _b.grad_clip_scratch_bytes(len(grads))
         # (one for each size, all kept: a captured graph may hold the address of any)
         if need not in self._clip_scratch:
             self._clip_scratch[need] = torch.empty(need, dtype=torch.uint8, device=o["norm"].device)
-        return _b.grad_clip(grads, max_norm, scale=scale, workspace=self.workspace, scratch=self._clip_scratch[need], norm=o["norm"])
+        norm = _b.grad_clip(grads, max_norm, scale=scale, workspace=self.workspace, scratch=self._clip_scratch[need], norm=o["norm"])
+        self._begun, self._mixed = None, False
+        return norm
 
     def device_status(self) -> int:
         return _b.last_device_status(self.workspace)

@@ -91,3 +91,17 @@ def test_a_table_used_twice_in_a_part_and_a_frozen_one(P):
         step.loss(step.embed(E, tokens), W, labels, mask)
         step.clip(1.0)
     assert step.device_status() == 0
+
+
+def test_a_clip_that_is_refused_changes_nothing(P):
+    from paper_2403_17031_b200.pipeline import SFTStep
+    E, W, tokens, labels, mask = setup(100, 64, 304)
+    step = SFTStep(W, 100)
+    for i in range(2):
+        o = step.loss(step.embed(E, tokens), W, labels, mask)
+        step.grad_embed(o["dH"], tokens, accumulate=i > 0)
+    with pytest.raises(P.PPOError):
+        step.clip(0.0, dW=o["dW"].clone())
+    with pytest.raises(ValueError):
+        step.clip(1.0)
+    step.clip(1.0, dW=o["dW"].clone())
